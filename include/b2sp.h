@@ -233,6 +233,117 @@ b2sp_status b2sp_fusedmm_batched_bf16(int batch, int M, int K, int Kd, int N, lo
                                       size_t workspace_bytes, int algo, void *stream);
 
 /*
+ * Attention over a CSR pattern, forward and backward: FusedMM with a softmax over each row of sampled products,
+ *
+ *   O_i = sum_j p_ij V_j,   p_ij = exp(scale Q_i . K_j - lse_i),   lse_i = log sum_j exp(scale Q_i . K_j),
+ *
+ * the sums over the columns j that row i of the pattern stores.  A row that stores nothing (or whose products are all
+ * -inf) gives a zero row of O and lse_i = -inf.  Only stored positions count: what Q, K, V or dO hold in rows that no
+ * entry names, NaN and infinities too, changes nothing.
+ *
+ * batch x heads problems of the same sizes; heads / kv_heads neighbouring query heads share one head of K and V.  The pattern (M x K, no
+ * stored values) belongs to all problems (patterns = 1), to a sequence (patterns = batch) or to a problem (patterns =
+ * batch * heads, sequence by sequence); pattern p has its row pointers, counted from 0, at row_ptr + p * row_ptr_stride and its
+ * column indices at col_idx + p * nnz_stride; nnz_stride >= every row_ptr_p[M].
+ * Operands are b2sp_heads: element (b, h, i, e) of a [batch][heads][rows][d] operand is data[b * stride_batch + h * stride_head +
+ * i * ld + e], strides in elements; an input's strides may be 0, the elements of an output must not overlap.  Q, O, dO, dQ have `heads`
+ * heads of M rows; K, V, dK, dV have kv_heads heads of K rows.  lse is fp32 [batch][heads][M].  d <= 256.
+ * The fp32 entry points take and give fp32; the _bf16 ones bfloat16 (lse, sums and softmax statistics stay fp32).
+ *
+ * Patterns that more than one call uses are analysed once: b2sp_attention_count_tiles says how many 128 x 128 tiles hold an entry
+ * (it synchronises `stream`), b2sp_attention_plan_bytes how much device memory a plan of that many takes, and
+ * b2sp_attention_prepare builds it there.  The problem names the plan and the pattern it was built from, whose contents must not have
+ * changed.  The backward pass needs a plan; the forward pass without one takes the row kernels (each stored entry is its own term
+ * then), which suits a pattern that is used once.  A plan needs distinct columns in each row, in any order, and at most
+ * 4194304 columns; b2sp_attention_plan_status (which synchronises) reports B2SP_ERR_BAD_CSR for a plan whose pattern has a column twice in
+ * a row, a column out of range or row pointers that are not monotone within [0, nnz_stride]: such a plan must not be used.
+ *
+ * algo: B2SP_ALGO_ROW = CUDA-core row kernels (any sizes and alignment); B2SP_ALGO_TILE = tcgen05 kernels over the tiles of the plan
+ * (bfloat16, d <= 128 and a multiple of 8, every operand's address and strides a multiple of 16 bytes; B2SP_ERR_UNSUPPORTED
+ * otherwise); B2SP_ALGO_AUTO chooses by the number of entries and tiles.  The tile kernels round the weights p (and, backward, p (dp - delta))
+ * to bfloat16 before the second products, as the operands are; the row kernels do not.
+ * Results do not depend on the order in which anything runs: the same call gives the same bits.
+ * workspace: b2sp_attention_workspace_bytes bytes, as for the ops above (b2sp_device_status reads it too).
+ */
+typedef struct { void *data; long long ld, stride_head, stride_batch; } b2sp_heads;
+typedef struct {
+    int batch, heads, kv_heads, M, K, d, patterns;
+    float scale;
+    const int *row_ptr; long long row_ptr_stride;
+    const int *col_idx; long long nnz_stride;
+    const void *plan;        /* NULL: none */
+    long long plan_tiles;    /* what b2sp_attention_count_tiles said */
+} b2sp_attention_problem;
+/* workspace: 256 bytes; tiles_host: HOST pointer.  Synchronises `stream`. */
+b2sp_status b2sp_attention_count_tiles(int patterns, int M, int K, long long nnz_stride, const int *row_ptr, long long row_ptr_stride,
+                                       const int *col_idx, void *workspace, size_t workspace_bytes, long long *tiles_host,
+                                       void *stream);
+/* 0 on invalid arguments. */
+size_t b2sp_attention_plan_bytes(int patterns, int M, int K, long long nnz_stride, long long tiles);
+b2sp_status b2sp_attention_prepare(int patterns, int M, int K, long long nnz_stride, const int *row_ptr, long long row_ptr_stride,
+                                   const int *col_idx, long long tiles, void *plan, size_t plan_bytes, void *stream);
+b2sp_status b2sp_attention_plan_status(const void *plan, void *stream);
+/* Bytes for the forward (backward = 0) or the backward call, whatever algo and type; 0 on invalid arguments. */
+size_t b2sp_attention_workspace_bytes(const b2sp_attention_problem *problem, int backward);
+b2sp_status b2sp_attention(const b2sp_attention_problem *problem, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V,
+                           const b2sp_heads *O, float *lse, void *workspace, size_t workspace_bytes, int algo, void *stream);
+b2sp_status b2sp_attention_bf16(const b2sp_attention_problem *problem, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V,
+                                const b2sp_heads *O, float *lse, void *workspace, size_t workspace_bytes, int algo, void *stream);
+/*
+ * dQ, dK, dV of sum(O * dO) from O and lse as the forward call left them; the probabilities are computed again, never stored.
+ *   delta_i = dO_i . O_i;  ds_ij = p_ij (dO_i . V_j - delta_i);  dQ_i = scale sum_j ds_ij K_j;  dK_j = scale sum_i ds_ij Q_i;
+ *   dV_j = sum_i p_ij dO_i
+ * dK and dV of a shared head are summed over its query heads (and only over the sequences of its own b: with inputs shared by
+ * stride 0 the caller adds the gradients up).
+ */
+b2sp_status b2sp_attention_backward(const b2sp_attention_problem *problem, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V,
+                                    const b2sp_heads *O, const float *lse, const b2sp_heads *dO, const b2sp_heads *dQ,
+                                    const b2sp_heads *dK, const b2sp_heads *dV, void *workspace, size_t workspace_bytes, int algo,
+                                    void *stream);
+b2sp_status b2sp_attention_backward_bf16(const b2sp_attention_problem *problem, const b2sp_heads *Q, const b2sp_heads *K,
+                                         const b2sp_heads *V, const b2sp_heads *O, const float *lse, const b2sp_heads *dO,
+                                         const b2sp_heads *dQ, const b2sp_heads *dK, const b2sp_heads *dV, void *workspace,
+                                         size_t workspace_bytes, int algo, void *stream);
+
+/*
+ * A cache of keys or values in 4 bits, and attention over it: the serving form of the above.
+ *
+ * A cache has heads x slots rows of d elements in G = ceil(d / 32) groups of 32 neighbours.  Row (h, slot): 16 G bytes of codes at
+ * codes + h * code_stride_head + slot * code_ld, G bfloat16 scales at scales + h * scale_stride_head + slot * scale_ld (elements).
+ *   scale s = bf16(max |x| / 7) of the group; code = clamp(rint(x / s), -7, 7) + 8 (8 if s = 0), half to even throughout;
+ *   halfword g G + c of the codes (g = 0..7, c = 0..G-1) holds elements 32 c + 4 g + {0, 1, 2, 3}, the first in the lowest four bits.
+ * A group with a NaN or an infinity gets the scale NaN, and reads as NaN.  codes: 16-byte aligned address and strides.  scales: address a multiple
+ * of 4 bytes (8 for G = 4); strides multiples of G elements where G is 2 or 4.
+ *
+ * b2sp_kv4_write quantises X[tokens][heads][d] (ld, stride_head) into the rows `slots` (device, one per token); a slot outside [0, cache
+ * slots) is skipped (padding), and of several tokens with one slot the last one's row stays.
+ * b2sp_kv4_read gives the rows back, rounded once to the output type; slots outside the cache read as zeros.
+ * b2sp_attention_kv4: M query tokens, each with its own list of slots: row_ptr[M+1] (from 0), col_idx = slots (each stored one is its own term; those
+ * outside the cache are left out), O and lse as for b2sp_attention with lse[M][heads]; Q, O: token i, head h at data + i * ld +
+ * h * stride_head, bfloat16; d <= 128; heads / kv_heads neighbouring query heads share a head of the caches.  The weights are rounded to
+ * bfloat16, times the scale of their value's group, before the second product; everything else is fp32.
+ * Any M, but made for few tokens with long rows: a row is cut into parts when there are few.
+ */
+typedef struct {
+    void *codes; long long code_ld, code_stride_head;
+    void *scales; long long scale_ld, scale_stride_head;
+    int slots;
+} b2sp_kv4;
+b2sp_status b2sp_kv4_write(int tokens, int heads, int d, const float *X, long long ld, long long stride_head, const int *slots,
+                           const b2sp_kv4 *cache, void *stream);
+b2sp_status b2sp_kv4_write_bf16(int tokens, int heads, int d, const void *X, long long ld, long long stride_head, const int *slots,
+                                const b2sp_kv4 *cache, void *stream);
+b2sp_status b2sp_kv4_read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *cache, float *X, long long ld,
+                          long long stride_head, void *stream);
+b2sp_status b2sp_kv4_read_bf16(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *cache, void *X, long long ld,
+                               long long stride_head, void *stream);
+size_t b2sp_attention_kv4_workspace_bytes(int M, int heads, int kv_heads, int d, long long nnz);
+b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long nnz, const int *row_ptr, const int *col_idx,
+                               const void *Q, long long ldq, long long stride_head_q, const b2sp_kv4 *keys, const b2sp_kv4 *values,
+                               float scale, void *O, long long ldo, long long stride_head_o, float *lse, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
  * Host-buffer forms of the three ops: every data pointer is a HOST pointer (pinned memory
  * makes the copies asynchronous and faster, pageable memory also works).  Each call copies
  * its inputs to the device, runs the device entry point above with algo = B2SP_ALGO_AUTO,

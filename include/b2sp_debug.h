@@ -41,6 +41,9 @@ b2sp_status b2sp_probe_l2_pull(void *scratch, size_t scratch_bytes, double *gbs_
  */
 int b2sp_last_algo(int op);
 int b2sp_last_launches(int op);
+/* The same for b2sp_attention (backward = 0) and b2sp_attention_backward (1): the family, and the kernels enqueued. */
+int b2sp_attention_last_algo(int backward);
+int b2sp_attention_last_launches(int backward);
 
 /*
  * Overrides, process-wide, the number of K splits the dense-tile planner picks (how many CTAs share

@@ -1,0 +1,191 @@
+// Entry points of the 4-bit cache: argument checks and launches.  See include/b2sp.h.
+#include <algorithm>
+#include <climits>
+
+#include "kv4.cuh"
+
+namespace b2sp {
+namespace kv4 {
+
+inline b2sp_status launched() { return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA; }
+
+b2sp_status check_cache(const b2sp_kv4 *c, int heads, int G)
+{
+    if (!c || c->slots < 0 || c->code_ld < 0 || c->code_stride_head < 0 || c->scale_ld < 0 || c->scale_stride_head < 0) return B2SP_ERR_INVALID_ARG;
+    if (c->slots && (!c->codes || !c->scales)) return B2SP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(c->codes) | (uintptr_t)c->code_ld | (uintptr_t)c->code_stride_head) & 15) return B2SP_ERR_INVALID_ARG;
+    const int unit = G == 4 ? 4 : G == 2 ? 2 : 1;   // elements that are loaded together
+    if (reinterpret_cast<uintptr_t>(c->scales) & (unit == 4 ? 7 : 3)) return B2SP_ERR_INVALID_ARG;
+    if (((uintptr_t)c->scale_ld | (uintptr_t)c->scale_stride_head) & (unit - 1)) return B2SP_ERR_INVALID_ARG;
+    if (c->slots > 1 && (c->code_ld < 16ll * G || c->scale_ld < G)) return B2SP_ERR_INVALID_ARG;
+    return B2SP_OK;
+}
+// Rows of a cache that is written must not overlap.
+b2sp_status check_written(const b2sp_kv4 *c, int heads, int G)
+{
+    const long long ld[2] = {c->code_ld, c->scale_ld}, sh[2] = {c->code_stride_head, c->scale_stride_head}, row[2] = {16ll * G, G};
+    for (int k = 0; k < 2; ++k)
+        if (heads > 1 && c->slots > 0 && sh[k] < ld[k] * (c->slots - 1ll) + row[k] && (sh[k] < row[k] || (c->slots > 1 && ld[k] < sh[k] * (heads - 1ll) + row[k])))
+            return B2SP_ERR_INVALID_ARG;
+    return B2SP_OK;
+}
+Cache cache(const b2sp_kv4 *c)
+{
+    return Cache{static_cast<uint8_t *>(c->codes), static_cast<Bf16 *>(c->scales), c->code_ld, c->code_stride_head, c->scale_ld, c->scale_stride_head, c->slots};
+}
+template <typename T> bool fours(const T *p, long long ld, long long sh, int d)
+{
+    return ((reinterpret_cast<uintptr_t>(p) / sizeof(T) | (uintptr_t)ld | (uintptr_t)sh | (uintptr_t)d) & 3) == 0;
+}
+
+template <typename T>
+b2sp_status write(int tokens, int heads, int d, const T *X, long long ld, long long sh, const int *slots, const b2sp_kv4 *c, void *stream)
+{
+    if (tokens < 0 || heads < 1 || d < 1 || ld < 0 || sh < 0) return B2SP_ERR_INVALID_ARG;
+    if (d > 32 * 1024 || heads > 65535) return B2SP_ERR_UNSUPPORTED;
+    if (tokens && (!X || !slots)) return B2SP_ERR_INVALID_ARG;
+    const int G = (d + 31) / 32;
+    b2sp_status rc = check_cache(c, heads, G);
+    if (rc == B2SP_OK) rc = check_written(c, heads, G);
+    if (rc != B2SP_OK) return rc;
+    if (c->slots == 0 || tokens == 0) return B2SP_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool wide = fours(X, ld, sh, d);
+    for (int t = 0; t < tokens; t += std::min(kWriteChunk, tokens - t)) {
+        const int n = std::min(kWriteChunk, tokens - t);
+        const unsigned blocks = (unsigned)((n + kWriteTokens - 1) / kWriteTokens);
+        const T *x = X + (long long)t * ld;
+        if (wide) kv4_write_kernel<T, 4><<<blocks, kWriteThreads, 0, st>>>(x, ld, sh, n, heads, d, G, slots + t, cache(c));
+        else kv4_write_kernel<T, 1><<<blocks, kWriteThreads, 0, st>>>(x, ld, sh, n, heads, d, G, slots + t, cache(c));
+    }
+    return launched();
+}
+
+template <typename T>
+b2sp_status read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *c, T *X, long long ld, long long sh, void *stream)
+{
+    if (tokens < 0 || heads < 1 || d < 1 || ld < 0 || sh < 0) return B2SP_ERR_INVALID_ARG;
+    if (d > 32 * 1024) return B2SP_ERR_UNSUPPORTED;
+    if (tokens && (!X || !slots)) return B2SP_ERR_INVALID_ARG;
+    const int G = (d + 31) / 32;
+    const b2sp_status rc = check_cache(c, heads, G);
+    if (rc != B2SP_OK) return rc;
+    if (tokens > 1 && heads > 1 && std::max(ld, sh) < std::min(ld, sh) * ((ld < sh ? tokens : heads) - 1ll) + d) return B2SP_ERR_INVALID_ARG;
+    if ((tokens > 1 && ld < d) || (heads > 1 && sh < d)) return B2SP_ERR_INVALID_ARG;
+    if (tokens == 0) return B2SP_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const long long n = (long long)tokens * heads * ((d + 3) / 4), blocks = (n + 255) / 256;
+    if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (fours(X, ld, sh, d)) kv4_read_kernel<T, 4><<<(unsigned)blocks, 256, 0, st>>>(slots, tokens, heads, d, G, cache(c), X, ld, sh);
+    else kv4_read_kernel<T, 1><<<(unsigned)blocks, 256, 0, st>>>(slots, tokens, heads, d, G, cache(c), X, ld, sh);
+    return launched();
+}
+
+struct ServePlan {
+    int mh, head_blocks, splits;
+    size_t ml, part, bytes;
+};
+// Parts of a row: as many CTAs as give every SM four, but at least 128 slots to a part on average.
+ServePlan serve_plan(int M, int heads, int kv_heads, int d, long long nnz)
+{
+    ServePlan p;
+    const int group = heads / kv_heads;
+    p.mh = group > 8 ? 2 : 1;
+    p.head_blocks = (group + 8 * p.mh - 1) / (8 * p.mh);
+    const long long units = std::max(1ll, (long long)M * kv_heads * p.head_blocks), avg = M ? nnz / M : 0;
+    p.splits = (int)std::max(1ll, std::min({(148ll * 4 + units - 1) / units * 4, 4096ll, avg / 128}));
+    const long long parts = (long long)M * heads * p.splits;
+    p.ml = 512;
+    p.part = p.ml + attn::up256(p.splits > 1 ? parts * 8 : 0);
+    p.bytes = p.part + attn::up256(p.splits > 1 ? parts * attn::part_width(attn::kForward, d) * 4 : 0);
+    return p;
+}
+
+template <int G> void launch(const AttnArgs &a, int mh, unsigned blocks, cudaStream_t st)
+{
+    if (mh == 2) kv4_attention_kernel<G, 2><<<blocks, attn::kWarps * 32, 0, st>>>(a);
+    else kv4_attention_kernel<G, 1><<<blocks, attn::kWarps * 32, 0, st>>>(a);
+}
+
+}  // namespace kv4
+}  // namespace b2sp
+
+using namespace b2sp;
+using namespace b2sp::kv4;
+
+extern "C" b2sp_status b2sp_kv4_write(int tokens, int heads, int d, const float *X, long long ld, long long stride_head, const int *slots, const b2sp_kv4 *c,
+                                      void *stream)
+{
+    return write<float>(tokens, heads, d, X, ld, stride_head, slots, c, stream);
+}
+extern "C" b2sp_status b2sp_kv4_write_bf16(int tokens, int heads, int d, const void *X, long long ld, long long stride_head, const int *slots,
+                                           const b2sp_kv4 *c, void *stream)
+{
+    return write<Bf16>(tokens, heads, d, static_cast<const Bf16 *>(X), ld, stride_head, slots, c, stream);
+}
+extern "C" b2sp_status b2sp_kv4_read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *c, float *X, long long ld, long long stride_head,
+                                     void *stream)
+{
+    return read<float>(tokens, heads, d, slots, c, X, ld, stride_head, stream);
+}
+extern "C" b2sp_status b2sp_kv4_read_bf16(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *c, void *X, long long ld, long long stride_head,
+                                          void *stream)
+{
+    return read<Bf16>(tokens, heads, d, slots, c, static_cast<Bf16 *>(X), ld, stride_head, stream);
+}
+
+static bool serve_args_ok(int M, int heads, int kv_heads, int d, long long nnz)
+{
+    return M >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1 && nnz >= 0 && nnz <= INT_MAX;
+}
+
+extern "C" size_t b2sp_attention_kv4_workspace_bytes(int M, int heads, int kv_heads, int d, long long nnz)
+{
+    return serve_args_ok(M, heads, kv_heads, d, nnz) ? serve_plan(M, heads, kv_heads, d, nnz).bytes : 0;
+}
+
+extern "C" b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long nnz, const int *row_ptr, const int *col_idx, const void *Q,
+                                          long long ldq, long long stride_head_q, const b2sp_kv4 *keys, const b2sp_kv4 *values, float scale, void *O,
+                                          long long ldo, long long stride_head_o, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!serve_args_ok(M, heads, kv_heads, d, nnz) || ldq < 0 || stride_head_q < 0 || !(scale == scale)) return B2SP_ERR_INVALID_ARG;
+    if (d > 128) return B2SP_ERR_UNSUPPORTED;
+    if (M && (!row_ptr || !Q || !O || !lse || (nnz && !col_idx))) return B2SP_ERR_INVALID_ARG;
+    if ((M > 1 && ldo < d) || (heads > 1 && stride_head_o < d)) return B2SP_ERR_INVALID_ARG;
+    if (M > 1 && heads > 1 && std::max(ldo, stride_head_o) < std::min(ldo, stride_head_o) * ((ldo < stride_head_o ? M : heads) - 1ll) + d) return B2SP_ERR_INVALID_ARG;
+    const int G = (d + 31) / 32;
+    b2sp_status rc = check_cache(keys, kv_heads, G);
+    if (rc == B2SP_OK) rc = check_cache(values, kv_heads, G);
+    if (rc != B2SP_OK) return rc;
+    const ServePlan p = serve_plan(M, heads, kv_heads, d, nnz);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes) return B2SP_ERR_WORKSPACE;
+    if (M == 0) return B2SP_OK;
+    const long long blocks = (long long)M * kv_heads * p.head_blocks * p.splits;
+    if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    char *ws = static_cast<char *>(workspace);
+    AttnArgs a = {};
+    a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.splits = p.splits; a.head_blocks = p.head_blocks;
+    a.row_ptr = row_ptr; a.col_idx = col_idx;
+    a.q = static_cast<const Bf16 *>(Q); a.q_ld = ldq; a.q_sh = stride_head_q;
+    a.k = cache(keys); a.v = cache(values); a.scale = scale;
+    a.out = attn::View<Bf16>{static_cast<Bf16 *>(O), ldo, stride_head_o, 0};
+    a.lse = lse;
+    if (p.splits > 1) { a.part = reinterpret_cast<float *>(ws + p.part); a.part_ml = reinterpret_cast<float2 *>(ws + p.ml); }
+    switch (G) {
+        case 1: launch<1>(a, p.mh, (unsigned)blocks, st); break;
+        case 2: launch<2>(a, p.mh, (unsigned)blocks, st); break;
+        case 3: launch<3>(a, p.mh, (unsigned)blocks, st); break;
+        default: launch<4>(a, p.mh, (unsigned)blocks, st); break;
+    }
+    if (p.splits > 1) {
+        attn::RowArgs<Bf16> g = {};
+        g.s = attn::Shape{1, heads, kv_heads, M, 0, d, 1, scale};
+        g.ptr = row_ptr; g.rows = M; g.splits = p.splits;
+        g.out1 = a.out; g.lse = lse; g.lse_head = 1; g.lse_row = heads;
+        g.part = a.part; g.part_ml = a.part_ml;
+        const unsigned joins = (unsigned)(((long long)M * heads + attn::kWarps - 1) / attn::kWarps);
+        attn::attention_join_kernel<attn::kForward, Bf16, 1><<<joins, attn::kWarps * 32, 0, st>>>(g);
+    }
+    return launched();
+}
