@@ -316,7 +316,7 @@ b2sp_status b2sp_attention_backward_bf16(const b2sp_attention_problem *problem, 
  * of 4 bytes (8 for G = 4); strides multiples of G elements where G is 2 or 4.
  *
  * b2sp_kv4_write quantises X[tokens][heads][d] (ld, stride_head) into the rows `slots` (device, one per token); a slot outside [0, cache
- * slots) is skipped (padding), and of several tokens with one slot the last one's row stays.
+ * slots) is skipped (padding), and of several tokens with one slot the last one's row stays.  Up to 1024 tokens need no workspace.
  * b2sp_kv4_read gives the rows back, rounded once to the output type; slots outside the cache read as zeros.
  * b2sp_attention_kv4: M query tokens, each with its own list of slots: row_ptr[M+1] (from 0), col_idx = slots (each stored one is its own term; those
  * outside the cache are left out), O and lse as for b2sp_attention with lse[M][heads]; Q, O: token i, head h at data + i * ld +
@@ -329,10 +329,11 @@ typedef struct {
     void *scales; long long scale_ld, scale_stride_head;
     int slots;
 } b2sp_kv4;
+size_t b2sp_kv4_write_workspace_bytes(int tokens, int slots);   /* 0 on invalid arguments */
 b2sp_status b2sp_kv4_write(int tokens, int heads, int d, const float *X, long long ld, long long stride_head, const int *slots,
-                           const b2sp_kv4 *cache, void *stream);
+                           const b2sp_kv4 *cache, void *workspace, size_t workspace_bytes, void *stream);
 b2sp_status b2sp_kv4_write_bf16(int tokens, int heads, int d, const void *X, long long ld, long long stride_head, const int *slots,
-                                const b2sp_kv4 *cache, void *stream);
+                                const b2sp_kv4 *cache, void *workspace, size_t workspace_bytes, void *stream);
 b2sp_status b2sp_kv4_read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *cache, float *X, long long ld,
                           long long stride_head, void *stream);
 b2sp_status b2sp_kv4_read_bf16(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *cache, void *X, long long ld,

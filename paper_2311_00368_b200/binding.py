@@ -138,7 +138,9 @@ lib.b2sp_attention_last_launches.restype = _i
 lib.b2sp_attention_last_launches.argtypes = [_i]
 for _name in ("b2sp_kv4_write", "b2sp_kv4_write_bf16"):
     getattr(lib, _name).restype = _i
-    getattr(lib, _name).argtypes = [_i, _i, _i, _vp, _ll, _ll, _vp, _pk, _vp]
+    getattr(lib, _name).argtypes = [_i, _i, _i, _vp, _ll, _ll, _vp, _pk, _vp, _sz, _vp]
+lib.b2sp_kv4_write_workspace_bytes.restype = _sz
+lib.b2sp_kv4_write_workspace_bytes.argtypes = [_i, _i]
 for _name in ("b2sp_kv4_read", "b2sp_kv4_read_bf16"):
     getattr(lib, _name).restype = _i
     getattr(lib, _name).argtypes = [_i, _i, _i, _vp, _pk, _vp, _ll, _ll, _vp]
@@ -660,6 +662,9 @@ def _kv4(codes, scales, heads, d, name):
     return _Kv4(codes.data_ptr(), codes.stride(1), codes.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0), codes.shape[1])
 
 
+_KV4_SCAN_TOKENS = 1024   # up to here b2sp_kv4_write needs no workspace
+
+
 def _slot_list(slots, n=None):
     _want(slots, torch.int32, "slots")
     if slots.dim() != 1 or not slots.is_contiguous() or (n is not None and slots.numel() != n):
@@ -667,7 +672,7 @@ def _slot_list(slots, n=None):
     return slots
 
 
-def kv4_write(x, slots, codes, scales, dtype=torch.float32):
+def kv4_write(x, slots, codes, scales, workspace=None, dtype=torch.float32):
     """b2sp_kv4_write: the rows x [tokens, heads, d] are quantised into the rows `slots` (int32 [tokens]) of a cache (see kv4_cache); slots outside
     the cache are skipped, and of several tokens with one slot the last one's row stays.  dtype: x's, fp32 or bfloat16."""
     _want(x, dtype, "x")
@@ -678,7 +683,10 @@ def kv4_write(x, slots, codes, scales, dtype=torch.float32):
     _slot_list(slots, T)
     _on_current_device(_same_device(x, slots, codes, scales))
     fn, name = (lib.b2sp_kv4_write, "b2sp_kv4_write") if dtype == torch.float32 else (lib.b2sp_kv4_write_bf16, "b2sp_kv4_write_bf16")
-    _check(fn(T, H, d, _ptr(x), x.stride(0), x.stride(1), _ptr(slots), c, _stream()), name)
+    ws = workspace
+    if T > _KV4_SCAN_TOKENS:
+        ws = _scratch(lib.b2sp_kv4_write_workspace_bytes(T, c.slots), x.device, workspace)
+    _check(fn(T, H, d, _ptr(x), x.stride(0), x.stride(1), _ptr(slots), c, _ptr(ws), 0 if ws is None else ws.numel(), _stream()), name)
 
 
 def kv4_read(slots, codes, scales, d, out=None, dtype=torch.float32):

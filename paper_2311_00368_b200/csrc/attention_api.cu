@@ -122,8 +122,7 @@ template <int MODE, typename T, int V> b2sp_status launch_rows(const RowArgs<T> 
     else attention_row_kernel<MODE, T, V, 256><<<(unsigned)blocks, kWarps * 32, 0, st>>>(g);
     ++*launches;
     if (g.part) {
-        const long long rows = (long long)g.s.batch * (MODE == kGradKV ? g.s.kv_heads : g.s.heads) * g.rows;
-        attention_join_kernel<MODE, T, V><<<(unsigned)((rows + kWarps - 1) / kWarps), kWarps * 32, 0, st>>>(g);
+        if (!launch_join<MODE, T, V>(g, st)) return B2SP_ERR_UNSUPPORTED;
         ++*launches;
     }
     return launched();

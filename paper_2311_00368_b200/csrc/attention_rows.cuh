@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_row_kernel(const RowArg
 {
     const long long unit = blockIdx.x * (long long)kWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (MODE == kForward && g.status && blockIdx.x == 0 && threadIdx.x == 0) *g.status = 0;
     const long long per_problem = (long long)g.rows * g.splits;
     const long long prob = unit / per_problem;
@@ -269,18 +270,22 @@ __global__ void __launch_bounds__(kWarps * 32) attention_row_kernel(const RowArg
     if (MODE == kForward && lane == 0) g.part_ml[unit] = make_float2(w.m, w.l);
 }
 
-// Joins the parts of a row (kGradKV: of all query heads that share it), in order; a warp per row.
-template <int MODE, typename T, int V>
+// Joins the parts of a row (kGradKV: of all query heads that share it) in a fixed order.  ROWW warps per row: with many parts (few rows) each
+// warp takes every ROWW-th, and the warps' sums are added up in order.
+template <int MODE, typename T, int V, int ROWW>
 __global__ void __launch_bounds__(kWarps * 32) attention_join_kernel(const RowArgs<T> g)
 {
-    const int lane = threadIdx.x & 31, d = g.s.d, group = g.s.heads / g.s.kv_heads;
-    const int heads = MODE == kGradKV ? g.s.kv_heads : g.s.heads;
-    const long long unit = blockIdx.x * (long long)kWarps + (threadIdx.x >> 5);
+    __shared__ float sums[ROWW == 1 ? 1 : kWarps][MODE == kGradKV ? 2 : 1][256];
+    __shared__ float weight[kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = g.s.d, group = g.s.heads / g.s.kv_heads;
+    const int heads = MODE == kGradKV ? g.s.kv_heads : g.s.heads, mine = ROWW == 1 ? 0 : warp;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const long long unit = ROWW == 1 ? blockIdx.x * (long long)kWarps + warp : blockIdx.x;
     const long long prob = unit / g.rows;
     if (prob >= (long long)g.s.batch * heads) return;
     const int row = (int)(unit % g.rows), b = (int)(prob / heads), ho = (int)(prob % heads);
     const int width = part_width(MODE, d), half = part_width(kForward, d);
-    float acc[2][2][4] = {};
+    float acc[MODE == kGradKV ? 2 : 1][2][4] = {};
     float m = -CUDART_INF_F, l = 0.f;
     for (int i = 0; i < (MODE == kGradKV ? group : 1); ++i) {
         const int h = MODE == kGradKV ? ho * group + i : ho;
@@ -288,15 +293,14 @@ __global__ void __launch_bounds__(kWarps * 32) attention_join_kernel(const RowAr
         const int len = ptr[row + 1] - ptr[row], per = part_len(len, g.splits);
         const int parts = per ? (int)(((long long)len + per - 1) / per) : 1;
         const long long u0 = (((long long)b * g.s.heads + h) * g.rows + row) * g.splits;
-        if (MODE == kForward)
-            for (int p = lane; p < parts; p += 32) m = fmaxf(m, g.part_ml[u0 + p].x);
         if (MODE == kForward) {
+            for (int p = lane; p < parts; p += 32) m = fmaxf(m, g.part_ml[u0 + p].x);
 #pragma unroll
             for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
         }
         const float ref = m == -CUDART_INF_F ? 0.f : m;
 #pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
+        for (int p = mine; p < parts; p += ROWW) {
             float f = 1.f;
             if (MODE == kForward) {
                 const float2 ml = g.part_ml[u0 + p];
@@ -315,6 +319,28 @@ __global__ void __launch_bounds__(kWarps * 32) attention_join_kernel(const RowAr
                 }
         }
     }
+    if (ROWW > 1) {
+#pragma unroll
+        for (int z = 0; z < (MODE == kGradKV ? 2 : 1); ++z)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                *reinterpret_cast<float4 *>(&sums[warp][z][u * 128 + lane * 4]) = make_float4(acc[z][u][0], acc[z][u][1], acc[z][u][2], acc[z][u][3]);
+        if (lane == 0) weight[warp] = l;
+        __syncthreads();
+        if (warp) return;
+        l = 0.f;
+#pragma unroll
+        for (int z = 0; z < (MODE == kGradKV ? 2 : 1); ++z)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float x = 0.f;
+                    for (int w = 0; w < ROWW; ++w) x += sums[w][z][u * 128 + lane * 4 + k];
+                    acc[z][u][k] = x;
+                }
+        for (int w = 0; w < ROWW; ++w) l += weight[w];
+    }
     const float f = MODE == kForward ? (l == 0.f ? 0.f : 1.f / l) : g.s.scale;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -322,9 +348,35 @@ __global__ void __launch_bounds__(kWarps * 32) attention_join_kernel(const RowAr
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = acc[0][u][k] * f;
         store4<T, V>(g.out1.at(b, ho, row), u * 128 + lane * 4, d, x);
-        if (MODE == kGradKV) store4<T, V>(g.out2.at(b, ho, row), u * 128 + lane * 4, d, acc[1][u]);
+        if constexpr (MODE == kGradKV) store4<T, V>(g.out2.at(b, ho, row), u * 128 + lane * 4, d, acc[1][u]);
     }
     if (MODE == kForward && lane == 0) g.lse[(long long)b * g.s.heads * g.s.M + ho * g.lse_head + row * g.lse_row] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+}
+
+// Launches a kernel that begins with griddepcontrol.wait while the one before it still runs.
+template <class... KArgs, class... Args>
+inline void launch_behind(void (*kern)(KArgs...), unsigned blocks, unsigned threads, cudaStream_t st, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
+}
+constexpr int kManyParts = 8;   // from here on four warps join a row
+template <int MODE, typename T, int V> inline bool launch_join(const RowArgs<T> &g, cudaStream_t st)
+{
+    const long long rows = (long long)g.s.batch * (MODE == kGradKV ? g.s.kv_heads : g.s.heads) * g.rows;
+    const long long blocks = g.splits >= kManyParts ? rows : (rows + kWarps - 1) / kWarps;
+    if (blocks > 0x7fffffff) return false;
+    if (g.splits >= kManyParts) launch_behind(attention_join_kernel<MODE, T, V, kWarps>, (unsigned)blocks, kWarps * 32, st, g);
+    else launch_behind(attention_join_kernel<MODE, T, V, 1>, (unsigned)blocks, kWarps * 32, st, g);
+    return true;
 }
 
 // The backward pass's row statistics: (lse log2(e), dO_i.O_i), a warp per row, `stat_rows` rows a problem.  A row without entries

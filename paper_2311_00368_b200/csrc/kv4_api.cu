@@ -33,30 +33,42 @@ Cache cache(const b2sp_kv4 *c)
 {
     return Cache{static_cast<uint8_t *>(c->codes), static_cast<Bf16 *>(c->scales), c->code_ld, c->code_stride_head, c->scale_ld, c->scale_stride_head, c->slots};
 }
-template <typename T> bool fours(const T *p, long long ld, long long sh, int d)
+template <typename T> bool eights(const T *p, long long ld, long long sh, int d)
 {
-    return ((reinterpret_cast<uintptr_t>(p) / sizeof(T) | (uintptr_t)ld | (uintptr_t)sh | (uintptr_t)d) & 3) == 0;
+    return ((reinterpret_cast<uintptr_t>(p) & 15) | (uintptr_t)(ld & 7) | (uintptr_t)(sh & 7) | (uintptr_t)(d & 7)) == 0;
 }
+constexpr int kMost = 0x7fffff00;   // threads of a launch (indices stay below 2^31)
+
+size_t write_bytes(int tokens, int slots) { return tokens <= kScanTokens ? 0 : (size_t)slots * 4; }
 
 template <typename T>
-b2sp_status write(int tokens, int heads, int d, const T *X, long long ld, long long sh, const int *slots, const b2sp_kv4 *c, void *stream)
+b2sp_status write(int tokens, int heads, int d, const T *X, long long ld, long long sh, const int *slots, const b2sp_kv4 *c, void *workspace,
+                  size_t workspace_bytes, void *stream)
 {
     if (tokens < 0 || heads < 1 || d < 1 || ld < 0 || sh < 0) return B2SP_ERR_INVALID_ARG;
-    if (d > 32 * 1024 || heads > 65535) return B2SP_ERR_UNSUPPORTED;
     if (tokens && (!X || !slots)) return B2SP_ERR_INVALID_ARG;
     const int G = (d + 31) / 32;
     b2sp_status rc = check_cache(c, heads, G);
     if (rc == B2SP_OK) rc = check_written(c, heads, G);
     if (rc != B2SP_OK) return rc;
+    const long long threads = (long long)tokens * heads * G * 4;
+    if (d > 32 * 1024 || threads > kMost) return B2SP_ERR_UNSUPPORTED;
+    const size_t need = write_bytes(tokens, c->slots);
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return B2SP_ERR_WORKSPACE;
     if (c->slots == 0 || tokens == 0) return B2SP_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool wide = fours(X, ld, sh, d);
-    for (int t = 0; t < tokens; t += std::min(kWriteChunk, tokens - t)) {
-        const int n = std::min(kWriteChunk, tokens - t);
-        const unsigned blocks = (unsigned)((n + kWriteTokens - 1) / kWriteTokens);
-        const T *x = X + (long long)t * ld;
-        if (wide) kv4_write_kernel<T, 4><<<blocks, kWriteThreads, 0, st>>>(x, ld, sh, n, heads, d, G, slots + t, cache(c));
-        else kv4_write_kernel<T, 1><<<blocks, kWriteThreads, 0, st>>>(x, ld, sh, n, heads, d, G, slots + t, cache(c));
+    RowsArgs a = {tokens, heads, d, G, ld, sh, slots, cache(c), Div(heads), Div(4 * G), 0, static_cast<int *>(workspace)};
+    const unsigned blocks = (unsigned)((threads + kWriteThreads - 1) / kWriteThreads);
+    const bool wide = eights(X, ld, sh, d);
+    if (tokens <= kScanTokens) {
+        if (wide) kv4_write_kernel<T, 8, true><<<blocks, kWriteThreads, 0, st>>>(X, a);
+        else kv4_write_kernel<T, 1, true><<<blocks, kWriteThreads, 0, st>>>(X, a);
+    } else {
+        const unsigned marks = (tokens + 255) / 256;
+        kv4_disown_kernel<<<marks, 256, 0, st>>>(slots, tokens, c->slots, a.owner);
+        attn::launch_behind(kv4_own_kernel, marks, 256, st, slots, tokens, c->slots, a.owner);
+        if (wide) attn::launch_behind(kv4_write_kernel<T, 8, false>, blocks, kWriteThreads, st, X, a);
+        else attn::launch_behind(kv4_write_kernel<T, 1, false>, blocks, kWriteThreads, st, X, a);
     }
     return launched();
 }
@@ -65,35 +77,39 @@ template <typename T>
 b2sp_status read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *c, T *X, long long ld, long long sh, void *stream)
 {
     if (tokens < 0 || heads < 1 || d < 1 || ld < 0 || sh < 0) return B2SP_ERR_INVALID_ARG;
-    if (d > 32 * 1024) return B2SP_ERR_UNSUPPORTED;
+    if (d > 32 * 1024 || (long long)tokens * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (tokens && (!X || !slots)) return B2SP_ERR_INVALID_ARG;
     const int G = (d + 31) / 32;
     const b2sp_status rc = check_cache(c, heads, G);
     if (rc != B2SP_OK) return rc;
     if (tokens > 1 && heads > 1 && std::max(ld, sh) < std::min(ld, sh) * ((ld < sh ? tokens : heads) - 1ll) + d) return B2SP_ERR_INVALID_ARG;
     if ((tokens > 1 && ld < d) || (heads > 1 && sh < d)) return B2SP_ERR_INVALID_ARG;
-    if (tokens == 0) return B2SP_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const long long n = (long long)tokens * heads * ((d + 3) / 4), blocks = (n + 255) / 256;
-    if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    if (fours(X, ld, sh, d)) kv4_read_kernel<T, 4><<<(unsigned)blocks, 256, 0, st>>>(slots, tokens, heads, d, G, cache(c), X, ld, sh);
-    else kv4_read_kernel<T, 1><<<(unsigned)blocks, 256, 0, st>>>(slots, tokens, heads, d, G, cache(c), X, ld, sh);
-    return launched();
+    const unsigned pieces = (unsigned)((d + 7) / 8), most = (unsigned)kMost / pieces;
+    const bool wide = eights(X, ld, sh, d);
+    for (unsigned first = 0, rows = (unsigned)((long long)tokens * heads); first < rows; first += std::min(most, rows - first)) {
+        const RowsArgs a = {tokens, heads, d, G, ld, sh, slots, cache(c), Div(heads), Div(pieces), first, nullptr};
+        const unsigned blocks = (unsigned)(((unsigned long long)std::min(most, rows - first) * pieces + 255) / 256);
+        if (wide) kv4_read_kernel<T, 8><<<blocks, 256, 0, st>>>(a, X);
+        else kv4_read_kernel<T, 1><<<blocks, 256, 0, st>>>(a, X);
+    }
+    return tokens ? launched() : B2SP_OK;
 }
 
 struct ServePlan {
-    int mh, head_blocks, splits;
+    int nb, head_blocks, splits;
     size_t ml, part, bytes;
 };
-// Parts of a row: as many CTAs as give every SM four, but at least 128 slots to a part on average.
+// Parts of a row, of at least 128 slots on average: for one token as many CTAs as run at once (four on an SM); for several tokens, whose rows
+// differ in length, four times as many, so that those with short parts make room early.
 ServePlan serve_plan(int M, int heads, int kv_heads, int d, long long nnz)
 {
     ServePlan p;
     const int group = heads / kv_heads;
-    p.mh = group > 8 ? 2 : 1;
-    p.head_blocks = (group + 8 * p.mh - 1) / (8 * p.mh);
-    const long long units = std::max(1ll, (long long)M * kv_heads * p.head_blocks), avg = M ? nnz / M : 0;
-    p.splits = (int)std::max(1ll, std::min({(148ll * 4 + units - 1) / units * 4, 4096ll, avg / 128}));
+    p.nb = group > 8 ? 2 : 1;
+    p.head_blocks = (group + 8 * p.nb - 1) / (8 * p.nb);
+    const long long units = std::max(1ll, (long long)M * kv_heads * p.head_blocks), avg = M ? nnz / M : 0, want = 148ll * (p.nb == 1 ? 4 : 3) * (M > 1 ? 4 : 1);
+    p.splits = (int)std::max(1ll, std::min({M > 1 ? (want + units - 1) / units : want / units, 4096ll, avg / 128}));
     const long long parts = (long long)M * heads * p.splits;
     p.ml = 512;
     p.part = p.ml + attn::up256(p.splits > 1 ? parts * 8 : 0);
@@ -101,9 +117,9 @@ ServePlan serve_plan(int M, int heads, int kv_heads, int d, long long nnz)
     return p;
 }
 
-template <int G> void launch(const AttnArgs &a, int mh, unsigned blocks, cudaStream_t st)
+template <int G> void launch(const AttnArgs &a, int nb, unsigned blocks, cudaStream_t st)
 {
-    if (mh == 2) kv4_attention_kernel<G, 2><<<blocks, attn::kWarps * 32, 0, st>>>(a);
+    if (nb == 2) kv4_attention_kernel<G, 2><<<blocks, attn::kWarps * 32, 0, st>>>(a);
     else kv4_attention_kernel<G, 1><<<blocks, attn::kWarps * 32, 0, st>>>(a);
 }
 
@@ -113,15 +129,19 @@ template <int G> void launch(const AttnArgs &a, int mh, unsigned blocks, cudaStr
 using namespace b2sp;
 using namespace b2sp::kv4;
 
-extern "C" b2sp_status b2sp_kv4_write(int tokens, int heads, int d, const float *X, long long ld, long long stride_head, const int *slots, const b2sp_kv4 *c,
-                                      void *stream)
+extern "C" size_t b2sp_kv4_write_workspace_bytes(int tokens, int slots)
 {
-    return write<float>(tokens, heads, d, X, ld, stride_head, slots, c, stream);
+    return tokens < 0 || slots < 0 ? 0 : std::max<size_t>(256, attn::up256(write_bytes(tokens, slots)));
+}
+extern "C" b2sp_status b2sp_kv4_write(int tokens, int heads, int d, const float *X, long long ld, long long stride_head, const int *slots, const b2sp_kv4 *c,
+                                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    return write<float>(tokens, heads, d, X, ld, stride_head, slots, c, workspace, workspace_bytes, stream);
 }
 extern "C" b2sp_status b2sp_kv4_write_bf16(int tokens, int heads, int d, const void *X, long long ld, long long stride_head, const int *slots,
-                                           const b2sp_kv4 *c, void *stream)
+                                           const b2sp_kv4 *c, void *workspace, size_t workspace_bytes, void *stream)
 {
-    return write<Bf16>(tokens, heads, d, static_cast<const Bf16 *>(X), ld, stride_head, slots, c, stream);
+    return write<Bf16>(tokens, heads, d, static_cast<const Bf16 *>(X), ld, stride_head, slots, c, workspace, workspace_bytes, stream);
 }
 extern "C" b2sp_status b2sp_kv4_read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 *c, float *X, long long ld, long long stride_head,
                                      void *stream)
@@ -173,10 +193,10 @@ extern "C" b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d,
     a.lse = lse;
     if (p.splits > 1) { a.part = reinterpret_cast<float *>(ws + p.part); a.part_ml = reinterpret_cast<float2 *>(ws + p.ml); }
     switch (G) {
-        case 1: launch<1>(a, p.mh, (unsigned)blocks, st); break;
-        case 2: launch<2>(a, p.mh, (unsigned)blocks, st); break;
-        case 3: launch<3>(a, p.mh, (unsigned)blocks, st); break;
-        default: launch<4>(a, p.mh, (unsigned)blocks, st); break;
+        case 1: launch<1>(a, p.nb, (unsigned)blocks, st); break;
+        case 2: launch<2>(a, p.nb, (unsigned)blocks, st); break;
+        case 3: launch<3>(a, p.nb, (unsigned)blocks, st); break;
+        default: launch<4>(a, p.nb, (unsigned)blocks, st); break;
     }
     if (p.splits > 1) {
         attn::RowArgs<Bf16> g = {};
@@ -184,8 +204,7 @@ extern "C" b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d,
         g.ptr = row_ptr; g.rows = M; g.splits = p.splits;
         g.out1 = a.out; g.lse = lse; g.lse_head = 1; g.lse_row = heads;
         g.part = a.part; g.part_ml = a.part_ml;
-        const unsigned joins = (unsigned)(((long long)M * heads + attn::kWarps - 1) / attn::kWarps);
-        attn::attention_join_kernel<attn::kForward, Bf16, 1><<<joins, attn::kWarps * 32, 0, st>>>(g);
+        if (!attn::launch_join<attn::kForward, Bf16, 1>(g, st)) return B2SP_ERR_UNSUPPORTED;
     }
     return launched();
 }

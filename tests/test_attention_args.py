@@ -89,7 +89,7 @@ def _cache(b, G=2, **other):
 
 def test_kv4_refusals(b):
     write, read, att = b.lib.b2sp_kv4_write, b.lib.b2sp_kv4_read, b.lib.b2sp_attention_kv4
-    w = lambda c, tokens=4, heads=2, d=64, x=1 << 20: write(tokens, heads, d, x, 128, 64, 4096, c, None)  # noqa: E731
+    w = lambda c, tokens=4, heads=2, d=64, x=1 << 20, ws=None, wsb=0: write(tokens, heads, d, x, 128, 64, 4096, c, ws, wsb, None)  # noqa: E731
     r = lambda c, tokens=4, heads=2, d=64, ld=128, sh=64: read(tokens, heads, d, 4096, c, 1 << 20, ld, sh, None)  # noqa: E731
     for bad in (dict(codes=(1 << 20) + 8), dict(code_ld=40), dict(code_ld=16), dict(scale_ld=1), dict(scales=(1 << 16) + 2), dict(slots=-1),
                 dict(codes=None), dict(scale_stride_head=255)):
@@ -100,6 +100,7 @@ def test_kv4_refusals(b):
     assert w(_cache(b, code_stride_head=64)) == INVALID               # heads of the cache overlap
     assert w(_cache(b), tokens=-1) == w(_cache(b), heads=0) == w(_cache(b), d=0) == w(_cache(b), x=None) == INVALID
     assert r(_cache(b), ld=64) == r(_cache(b), sh=32) == r(_cache(b), ld=100) == INVALID
+    assert w(_cache(b), tokens=1025) == w(_cache(b), tokens=1025, ws=4096 + 8, wsb=1 << 20) == w(_cache(b), tokens=1025, ws=4096, wsb=127) == WORKSPACE
     assert w(_cache(b), tokens=0) == r(_cache(b), tokens=0) == OK
     a = lambda M=1, H=4, Hkv=2, d=64, nnz=8, q=4096, ldo=256, sho=64, lse=4096, ws=1 << 20, wsb=1 << 30: att(  # noqa: E731
         M, H, Hkv, d, nnz, 4096, 4096, q, 256, 64, _cache(b, (d + 31) // 32 if d <= 64 else 4), _cache(b, (d + 31) // 32 if d <= 64 else 4), 0.1,
