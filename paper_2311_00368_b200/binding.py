@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import torch
 
@@ -95,25 +96,11 @@ lib.b2sp_debug_inject_wait_timeout.restype = _i
 lib.b2sp_debug_inject_wait_timeout.argtypes = [_i, ctypes.c_ulonglong]
 
 
-class _Heads(ctypes.Structure):
-    """b2sp_heads"""
-    _fields_ = [("data", _vp), ("ld", _ll), ("stride_head", _ll), ("stride_batch", _ll)]
-
-
-class _AttentionProblem(ctypes.Structure):
-    """b2sp_attention_problem"""
-    _fields_ = [("batch", _i), ("heads", _i), ("kv_heads", _i), ("M", _i), ("K", _i), ("d", _i), ("patterns", _i),
-                ("scale", ctypes.c_float), ("row_ptr", _vp), ("row_ptr_stride", _ll), ("col_idx", _vp), ("nnz_stride", _ll),
-                ("plan", _vp), ("plan_tiles", _ll)]
-
-
-class _Kv4(ctypes.Structure):
-    """b2sp_kv4"""
-    _fields_ = [("codes", _vp), ("code_ld", _ll), ("code_stride_head", _ll), ("scales", _vp), ("scale_ld", _ll),
-                ("scale_stride_head", _ll), ("slots", _i)]
-
-
-_ph, _pp, _pk = (ctypes.POINTER(t) for t in (_Heads, _AttentionProblem, _Kv4))
+# Structures go to the library as packed bytes (a ctypes.Structure costs five times as long to fill as struct.pack).
+_HEADS = struct.Struct("Pqqq").pack                        # b2sp_heads: data, ld, stride_head, stride_batch
+_PROBLEM = struct.Struct("7ifPqPqPq").pack                 # b2sp_attention_problem, in the order of its members
+_KV4 = struct.Struct("PqqPqqi4x").pack                     # b2sp_kv4
+_ph = _pp = _pk = _vp
 lib.b2sp_attention_count_tiles.restype = _i
 lib.b2sp_attention_count_tiles.argtypes = [_i, _i, _i, _ll, _vp, _ll, _vp, _vp, _sz, ctypes.POINTER(_ll), _vp]
 lib.b2sp_attention_plan_bytes.restype = _sz
@@ -486,28 +473,34 @@ def device_status(workspace) -> int:
 
 
 # ---- attention over a CSR pattern ------------------------------------------------------------------------------------------------
-def _same_device(first, *others):
-    """The device that all tensors are on, made the current one's index; raises where they differ."""
+# The checks of these calls stand on the critical path of small ones: they are written out instead of shared, and run on shapes and strides
+# that are fetched once.
+def _ready(device, *others):
+    """Raises where tensors are not on `device`, or that is not the current one."""
     for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device}")
-    return first.device
-
-
-def _on_current_device(device):
+        if t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device}")
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a CUDA device")
     if device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}: "
                          "call under torch.cuda.device(...)")
 
 
-def _scratch(need, device, workspace):
+try:
+    _capturing = torch._C._cuda_isCurrentStreamCapturing
+except AttributeError:
+    _capturing = torch.cuda.is_current_stream_capturing
+
+
+def _scratch(need, device, workspace, stream):
     """`workspace`, or one that this module keeps per device and stream; a call that is being captured gets one of its own, which
     belongs to the graph, so that graphs can be replayed side by side."""
     if workspace is not None:
         return workspace
-    if torch.cuda.is_current_stream_capturing():
+    if _capturing():
         return torch.empty(need, dtype=torch.uint8, device=device)
-    key = (device.index, _raw_stream(device.index), "attention")
+    key = (device.index, stream, "attention")
     workspace = _ws_cache.get(key)
     if workspace is None or workspace.numel() < need:
         workspace = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=device)
@@ -517,23 +510,23 @@ def _scratch(need, device, workspace):
 
 def _mask_dims(row_ptr, col_idx):
     """(patterns, M, row_ptr stride, nnz stride) of 1-D tensors (one pattern), [batch, .] or [batch, heads, .] ones."""
-    _want(row_ptr, torch.int32, "row_ptr"); _want(col_idx, torch.int32, "col_idx")
-    if row_ptr.dim() != col_idx.dim() or not 1 <= row_ptr.dim() <= 3 or row_ptr.shape[:-1] != col_idx.shape[:-1]:
+    if row_ptr.dtype is not torch.int32 or col_idx.dtype is not torch.int32:
+        raise TypeError("row_ptr and col_idx must be torch.int32")
+    a, b = row_ptr.shape, col_idx.shape
+    n = len(a)
+    if n != len(b) or not 1 <= n <= 3 or (n > 1 and a[:-1] != b[:-1]):
         raise ValueError("row_ptr and col_idx: [.], [batch, .] or [batch, heads, .], alike but for the last size")
-    if row_ptr.shape[-1] < 1:
+    if a[-1] < 1:
         raise ValueError("row_ptr has M + 1 elements")
     if not (row_ptr.is_contiguous() and col_idx.is_contiguous()):
         raise ValueError("row_ptr and col_idx must be contiguous")
-    patterns = 1
-    for n in row_ptr.shape[:-1]:
-        patterns *= n
-    return patterns, row_ptr.shape[-1] - 1, row_ptr.shape[-1], col_idx.shape[-1]
+    return 1 if n == 1 else a[0] if n == 2 else a[0] * a[1], a[-1] - 1, a[-1], b[-1]
 
 
 class AttentionPlan:
     """What b2sp_attention_prepare found out about a pattern, in device memory of its own; see attention_plan.  The plan holds on to the
     pattern's tensors: they must not change while it is used."""
-    __slots__ = ("row_ptr", "col_idx", "K", "patterns", "M", "nnz_stride", "tiles", "memory")
+    __slots__ = ("row_ptr", "col_idx", "K", "patterns", "M", "nnz_stride", "tiles", "memory", "pattern")
 
 
 def attention_plan(row_ptr, col_idx, K):
@@ -541,8 +534,8 @@ def attention_plan(row_ptr, col_idx, K):
     (synchronises).  row_ptr [M + 1] and col_idx [nnz] for one mask that all problems share, [batch, .] for one per sequence,
     [batch, heads, .] for one per problem (col_idx padded to a common length).  The columns of a row must be distinct, in any order."""
     patterns, M, rps, nzs = _mask_dims(row_ptr, col_idx)
-    device = _same_device(row_ptr, col_idx)
-    _on_current_device(device)
+    device = row_ptr.device
+    _ready(device, col_idx)
     if patterns < 1:
         raise ValueError("no pattern")
     tiles = _ll(0)
@@ -552,47 +545,59 @@ def attention_plan(row_ptr, col_idx, K):
     need = lib.b2sp_attention_plan_bytes(patterns, M, K, nzs, tiles.value)
     plan = AttentionPlan()
     plan.row_ptr, plan.col_idx, plan.K, plan.patterns, plan.M, plan.nnz_stride, plan.tiles = row_ptr, col_idx, K, patterns, M, nzs, tiles.value
+    plan.pattern = (_ptr(row_ptr), _ptr(col_idx), K, patterns, M, nzs)
     plan.memory = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
     _check(lib.b2sp_attention_prepare(*args, tiles.value, _ptr(plan.memory), plan.memory.numel(), _stream()), "b2sp_attention_prepare")
     _check(lib.b2sp_attention_plan_status(_ptr(plan.memory), _stream()), "b2sp_attention_plan_status")
     return plan
 
 
-def _heads(t):
+def _rows(t, shape, dtype, name):
+    """A [batch, heads, rows, d] tensor as b2sp_heads."""
     s = t.stride()
-    return _Heads(t.data_ptr(), s[2], s[1], s[0])
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.shape != shape or (s[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be {list(shape)} with neighbouring elements along d")
+    return _HEADS(t.data_ptr(), s[2], s[1], s[0])
 
 
-def _attention_problem(row_ptr, col_idx, q, k, v, scale, plan, dtype):
+@functools.lru_cache(maxsize=4096)
+def _attention_need(sizes, nnz_stride, backward):
+    """b2sp_attention_workspace_bytes, which goes by sizes only."""
+    return lib.b2sp_attention_workspace_bytes(_PROBLEM(*sizes, 1.0, 256, sizes[3] + 1, 256, nnz_stride, 0, 0), backward)
+
+
+def _attention_problem(row_ptr, col_idx, q, k, scale, plan):
+    """(sizes, nnz stride, b2sp_attention_problem, K's shape)"""
     patterns, M, rps, nzs = _mask_dims(row_ptr, col_idx)
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        _want(t, dtype, n)
-        if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
-            raise ValueError(f"{n} must be [batch, heads, rows, d] with neighbouring elements along d")
-    B, H, _, d = q.shape
-    Hkv, K = k.shape[1], k.shape[2]
-    if q.shape[2] != M or k.shape != (B, Hkv, K, d) or v.shape != k.shape or Hkv < 1 or H % Hkv:
+    qs, ks = q.shape, k.shape
+    if len(qs) != 4 or len(ks) != 4:
+        raise ValueError("q, k and v must be [batch, heads, rows, d]")
+    B, H, _, d = qs
+    Hkv, K = ks[1], ks[2]
+    if qs[2] != M or ks[0] != B or ks[3] != d or Hkv < 1 or H % Hkv:
         raise ValueError("q must be [batch, heads, M, d], k and v [batch, kv_heads, K, d], heads a multiple of kv_heads")
-    if row_ptr.dim() > 1 and (row_ptr.shape[0] != B or (row_ptr.dim() == 3 and row_ptr.shape[1] != H)):
+    n = len(row_ptr.shape)
+    if n > 1 and (row_ptr.shape[0] != B or (n == 3 and row_ptr.shape[1] != H)):
         raise ValueError("row_ptr: [M + 1], [batch, M + 1] or [batch, heads, M + 1]")
+    rp, ci = row_ptr.data_ptr(), col_idx.data_ptr()
+    memory, tiles = 0, 0
     if plan is not None:
-        if not isinstance(plan, AttentionPlan):
+        if type(plan) is not AttentionPlan:
             raise TypeError("plan must come from attention_plan")
-        if (plan.row_ptr.data_ptr(), plan.col_idx.data_ptr(), plan.K, plan.patterns, plan.M, plan.nnz_stride) != (
-                row_ptr.data_ptr(), col_idx.data_ptr(), K, patterns, M, nzs):
+        if plan.pattern != (rp, ci, K, patterns, M, nzs):
             raise ValueError("the plan is of another pattern")
-    _on_current_device(_same_device(q, k, v, row_ptr, col_idx, plan.memory if plan is not None else None))
-    return _AttentionProblem(B, H, Hkv, M, K, d, patterns, d ** -0.5 if scale is None else scale, row_ptr.data_ptr(), rps,
-                             col_idx.data_ptr(), nzs, plan.memory.data_ptr() if plan is not None else None, plan.tiles if plan is not None else 0)
+        memory, tiles = plan.memory.data_ptr(), plan.tiles
+    sizes = (B, H, Hkv, M, K, d, patterns)
+    return sizes, nzs, _PROBLEM(*sizes, d ** -0.5 if scale is None else scale, rp, rps, ci, nzs, memory, tiles)
 
 
-def _given(t, shape, dtype, name, like):
-    """An operand or output that the caller passes: of this shape and type, elements of its last dimension neighbours."""
-    _want(t, dtype, name)
-    if tuple(t.shape) != tuple(shape) or (shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name} must be {list(shape)} with neighbouring elements in the last dimension")
-    _same_device(like, t)
-    return t
+def _lse(lse, shape):
+    if lse.dtype is not torch.float32:
+        raise TypeError("lse must be torch.float32")
+    if lse.shape != shape or not lse.is_contiguous():
+        raise ValueError(f"lse must be {list(shape)}, contiguous")
 
 
 def attention(row_ptr, col_idx, q, k, v, scale=None, plan=None, out=None, lse=None, workspace=None, algo=ALGO_AUTO, dtype=torch.float32):
@@ -600,15 +605,23 @@ def attention(row_ptr, col_idx, q, k, v, scale=None, plan=None, out=None, lse=No
     [batch, kv_heads, K, d] (any strides but the last; heads / kv_heads neighbouring query heads share a k and v), scale d ** -0.5
     unless given; the mask as in attention_plan, whose result goes into `plan`.  O is like q, in `dtype`; lse fp32 [batch, heads, M]
     (-inf, and a zero row of O, where a row stores nothing).  dtype=torch.bfloat16: b2sp_attention_bf16."""
-    p = _attention_problem(row_ptr, col_idx, q, k, v, scale, plan, dtype)
-    out = torch.empty_like(q) if out is None else _given(out, q.shape, dtype, "out", q)
+    sizes, nzs, p = _attention_problem(row_ptr, col_idx, q, k, scale, plan)
+    qs, ks, device = q.shape, k.shape, q.device
+    hq, hk, hv = _rows(q, qs, dtype, "q"), _rows(k, ks, dtype, "k"), _rows(v, ks, dtype, "v")
+    _ready(device, k, v, row_ptr, col_idx)
+    if out is None:
+        out = torch.empty_like(q) if 0 not in q.stride() else torch.empty(qs, dtype=dtype, device=device)
+    else:
+        _ready(device, out)
     if lse is None:
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-    elif not _given(lse, q.shape[:3], torch.float32, "lse", q).is_contiguous():
-        raise ValueError("lse must be contiguous")
-    ws = _scratch(lib.b2sp_attention_workspace_bytes(ctypes.byref(p), 0), q.device, workspace)
+        lse = torch.empty(qs[:3], dtype=torch.float32, device=device)
+    else:
+        _lse(lse, qs[:3])
+        _ready(device, lse)
+    stream = _raw_stream(device.index)
+    ws = _scratch(_attention_need(sizes, nzs, 0), device, workspace, stream)
     fn, name = ((lib.b2sp_attention, "b2sp_attention") if dtype == torch.float32 else (lib.b2sp_attention_bf16, "b2sp_attention_bf16"))
-    _check(fn(ctypes.byref(p), _heads(q), _heads(k), _heads(v), _heads(out), _ptr(lse), _ptr(ws), ws.numel(), algo, _stream()), name)
+    _check(fn(p, hq, hk, hv, _rows(out, qs, dtype, "out"), lse.data_ptr(), ws.data_ptr(), ws.numel(), algo, stream), name)
     return out, lse
 
 
@@ -618,20 +631,23 @@ def attention_backward(row_ptr, col_idx, q, k, v, out, lse, dout, plan, scale=No
     again.  dout is like q; dk and dv of shared heads are summed over the query heads that share them."""
     if plan is None:
         raise ValueError("the backward pass needs a plan")
-    p = _attention_problem(row_ptr, col_idx, q, k, v, scale, plan, dtype)
-    _given(out, q.shape, dtype, "out", q); _given(dout, q.shape, dtype, "dout", q)
-    if not _given(lse, q.shape[:3], torch.float32, "lse", q).is_contiguous():
-        raise ValueError("lse must be contiguous")
+    sizes, nzs, p = _attention_problem(row_ptr, col_idx, q, k, scale, plan)
+    qs, ks, device = q.shape, k.shape, q.device
+    _lse(lse, qs[:3])
+    h = [_rows(t, s, dtype, n) for t, s, n in ((q, qs, "q"), (k, ks, "k"), (v, ks, "v"), (out, qs, "out"), (dout, qs, "dout"))]
+    _ready(device, k, v, row_ptr, col_idx, out, lse, dout)
     # (gradients of operands that the caller expanded get elements of their own)
     fresh = lambda t: torch.empty_like(t) if 0 not in t.stride() or t.numel() == 0 else torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
-    dq = fresh(q) if dq is None else _given(dq, q.shape, dtype, "dq", q)
-    dk = fresh(k) if dk is None else _given(dk, k.shape, dtype, "dk", q)
-    dv = fresh(v) if dv is None else _given(dv, v.shape, dtype, "dv", q)
-    ws = _scratch(lib.b2sp_attention_workspace_bytes(ctypes.byref(p), 1), q.device, workspace)
+    given = [t for t in (dq, dk, dv) if t is not None]
+    if given:
+        _ready(device, *given)
+    dq, dk, dv = fresh(q) if dq is None else dq, fresh(k) if dk is None else dk, fresh(v) if dv is None else dv
+    stream = _raw_stream(device.index)
+    ws = _scratch(_attention_need(sizes, nzs, 1), device, workspace, stream)
     fn, name = ((lib.b2sp_attention_backward, "b2sp_attention_backward") if dtype == torch.float32
                 else (lib.b2sp_attention_backward_bf16, "b2sp_attention_backward_bf16"))
-    _check(fn(ctypes.byref(p), _heads(q), _heads(k), _heads(v), _heads(out), _ptr(lse), _heads(dout), _heads(dq), _heads(dk), _heads(dv),
-              _ptr(ws), ws.numel(), algo, _stream()), name)
+    _check(fn(p, h[0], h[1], h[2], h[3], lse.data_ptr(), h[4], _rows(dq, qs, dtype, "dq"), _rows(dk, ks, dtype, "dk"), _rows(dv, ks, dtype, "dv"),
+              ws.data_ptr(), ws.numel(), algo, stream), name)
     return dq, dk, dv
 
 
@@ -653,77 +669,100 @@ def kv4_cache(heads: int, slots: int, d: int, device=None):
 
 
 def _kv4(codes, scales, heads, d, name):
-    _want(codes, torch.uint8, name + "codes"); _want(scales, torch.bfloat16, name + "scales")
-    G = (d + 31) // 32
-    if codes.dim() != 3 or codes.shape[0] != heads or codes.shape[2] != 16 * G or codes.stride(2) != 1:
+    """A cache as b2sp_kv4."""
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.bfloat16:
+        raise TypeError(f"{name}codes must be torch.uint8, {name}scales torch.bfloat16")
+    G, a, s, t = (d + 31) // 32, codes.shape, codes.stride(), scales.stride()
+    if len(a) != 3 or a[0] != heads or a[2] != 16 * G or s[2] != 1:
         raise ValueError(f"{name}codes must be [heads, slots, 16 * ceil(d / 32)] with neighbouring bytes in the last dimension")
-    if tuple(scales.shape) != (heads, codes.shape[1], G) or (G > 1 and scales.stride(2) != 1):
+    if scales.shape != (heads, a[1], G) or (G > 1 and t[2] != 1):
         raise ValueError(f"{name}scales must be [heads, slots, ceil(d / 32)] with neighbouring elements in the last dimension")
-    return _Kv4(codes.data_ptr(), codes.stride(1), codes.stride(0), scales.data_ptr(), scales.stride(1), scales.stride(0), codes.shape[1])
+    return _KV4(codes.data_ptr(), s[1], s[0], scales.data_ptr(), t[1], t[0], a[1])
 
 
 _KV4_SCAN_TOKENS = 1024   # up to here b2sp_kv4_write needs no workspace
 
 
-def _slot_list(slots, n=None):
-    _want(slots, torch.int32, "slots")
-    if slots.dim() != 1 or not slots.is_contiguous() or (n is not None and slots.numel() != n):
+def _slot_list(slots):
+    if slots.dtype is not torch.int32:
+        raise TypeError("slots must be torch.int32")
+    if slots.dim() != 1 or not slots.is_contiguous():
         raise ValueError("slots must be contiguous, one per token")
-    return slots
+    return slots.shape[0]
 
 
 def kv4_write(x, slots, codes, scales, workspace=None, dtype=torch.float32):
     """b2sp_kv4_write: the rows x [tokens, heads, d] are quantised into the rows `slots` (int32 [tokens]) of a cache (see kv4_cache); slots outside
     the cache are skipped, and of several tokens with one slot the last one's row stays.  dtype: x's, fp32 or bfloat16."""
-    _want(x, dtype, "x")
-    if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+    if x.dtype is not dtype:
+        raise TypeError(f"x must be {dtype}")
+    shape, s, device = x.shape, x.stride(), x.device
+    if len(shape) != 3 or (shape[2] > 1 and s[2] != 1):
         raise ValueError("x must be [tokens, heads, d] with neighbouring elements along d")
-    T, H, d = x.shape
+    T, H, d = shape
     c = _kv4(codes, scales, H, d, "")
-    _slot_list(slots, T)
-    _on_current_device(_same_device(x, slots, codes, scales))
-    fn, name = (lib.b2sp_kv4_write, "b2sp_kv4_write") if dtype == torch.float32 else (lib.b2sp_kv4_write_bf16, "b2sp_kv4_write_bf16")
-    ws = workspace
+    if _slot_list(slots) != T:
+        raise ValueError("slots must be contiguous, one per token")
+    _ready(device, slots, codes, scales)
+    stream, ws, size = _raw_stream(device.index), None, 0
     if T > _KV4_SCAN_TOKENS:
-        ws = _scratch(lib.b2sp_kv4_write_workspace_bytes(T, c.slots), x.device, workspace)
-    _check(fn(T, H, d, _ptr(x), x.stride(0), x.stride(1), _ptr(slots), c, _ptr(ws), 0 if ws is None else ws.numel(), _stream()), name)
+        ws = _scratch(lib.b2sp_kv4_write_workspace_bytes(T, codes.shape[1]), device, workspace, stream)
+        ws, size = ws.data_ptr(), ws.numel()
+    fn, name = (lib.b2sp_kv4_write, "b2sp_kv4_write") if dtype == torch.float32 else (lib.b2sp_kv4_write_bf16, "b2sp_kv4_write_bf16")
+    _check(fn(T, H, d, x.data_ptr(), s[0], s[1], slots.data_ptr(), c, ws, size, stream), name)
 
 
 def kv4_read(slots, codes, scales, d, out=None, dtype=torch.float32):
     """b2sp_kv4_read: [tokens, heads, d] in `dtype`, the values that the rows `slots` of a cache stand for (zeros outside the cache)."""
-    H = codes.shape[0]
+    H, device = codes.shape[0], codes.device
     c = _kv4(codes, scales, H, d, "")
-    T = _slot_list(slots).numel()
+    T = _slot_list(slots)
     if out is None:
-        out = torch.empty((T, H, d), dtype=dtype, device=codes.device)
-    _given(out, (T, H, d), dtype, "out", codes)
-    _on_current_device(_same_device(codes, slots, scales))
+        out = torch.empty((T, H, d), dtype=dtype, device=device)
+    s = out.stride()
+    if out.dtype is not dtype:
+        raise TypeError(f"out must be {dtype}")
+    if out.shape != (T, H, d) or (d > 1 and s[2] != 1):
+        raise ValueError("out must be [tokens, heads, d] with neighbouring elements along d")
+    _ready(device, slots, scales, out)
     fn, name = (lib.b2sp_kv4_read, "b2sp_kv4_read") if dtype == torch.float32 else (lib.b2sp_kv4_read_bf16, "b2sp_kv4_read_bf16")
-    _check(fn(T, H, d, _ptr(slots), c, _ptr(out), out.stride(0), out.stride(1), _stream()), name)
+    _check(fn(T, H, d, slots.data_ptr(), c, out.data_ptr(), s[0], s[1], _raw_stream(device.index)), name)
     return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _attention_kv4_need(M, heads, kv_heads, d, nnz):
+    return lib.b2sp_attention_kv4_workspace_bytes(M, heads, kv_heads, d, nnz)
 
 
 def attention_kv4(row_ptr, col_idx, q, k_codes, k_scales, v_codes, v_scales, scale=None, out=None, lse=None, workspace=None):
     """b2sp_attention_kv4: (O, lse) of query tokens q [M, heads, d] (bfloat16) over caches held in 4 bits; row i of the CSR arrays
     names the slots that token i sees, for all heads.  O is like q, lse fp32 [M, heads]; scale d ** -0.5 unless given."""
-    _want(row_ptr, torch.int32, "row_ptr"); _want(col_idx, torch.int32, "col_idx"); _want(q, torch.bfloat16, "q")
-    if q.dim() != 3 or (q.shape[2] > 1 and q.stride(2) != 1) or row_ptr.dim() != 1 or col_idx.dim() != 1:
-        raise ValueError("q must be [M, heads, d] with neighbouring elements along d, row_ptr [M + 1], col_idx [nnz]")
-    if not (row_ptr.is_contiguous() and col_idx.is_contiguous()) or row_ptr.numel() != q.shape[0] + 1:
-        raise ValueError("row_ptr must be [M + 1], contiguous as col_idx")
-    M, H, d = q.shape
-    Hkv, nnz = k_codes.shape[0], col_idx.numel()
+    if row_ptr.dtype is not torch.int32 or col_idx.dtype is not torch.int32 or q.dtype is not torch.bfloat16:
+        raise TypeError("row_ptr and col_idx must be torch.int32, q torch.bfloat16")
+    shape, s, device = q.shape, q.stride(), q.device
+    if len(shape) != 3 or (shape[2] > 1 and s[2] != 1):
+        raise ValueError("q must be [M, heads, d] with neighbouring elements along d")
+    M, H, d = shape
+    if row_ptr.shape != (M + 1,) or col_idx.dim() != 1 or not (row_ptr.is_contiguous() and col_idx.is_contiguous()):
+        raise ValueError("row_ptr must be [M + 1] and col_idx [nnz], contiguous")
+    Hkv, nnz = k_codes.shape[0], col_idx.shape[0]
     if Hkv < 1 or H % Hkv:
         raise ValueError("heads must be a multiple of the cache's")
     k, v = _kv4(k_codes, k_scales, Hkv, d, "k_"), _kv4(v_codes, v_scales, Hkv, d, "v_")
-    out = torch.empty_like(q) if out is None else _given(out, q.shape, torch.bfloat16, "out", q)
+    if out is None:
+        out = torch.empty_like(q) if 0 not in s else torch.empty(shape, dtype=q.dtype, device=device)
+    t = out.stride()
+    if out.dtype is not torch.bfloat16 or out.shape != shape or (d > 1 and t[2] != 1):
+        raise ValueError("out must be like q, with neighbouring elements along d")
     if lse is None:
-        lse = torch.empty((M, H), dtype=torch.float32, device=q.device)
-    elif not _given(lse, (M, H), torch.float32, "lse", q).is_contiguous():
-        raise ValueError("lse must be contiguous")
-    _on_current_device(_same_device(q, row_ptr, col_idx, k_codes, k_scales, v_codes, v_scales))
-    ws = _scratch(lib.b2sp_attention_kv4_workspace_bytes(M, H, Hkv, d, nnz), q.device, workspace)
-    _check(lib.b2sp_attention_kv4(M, H, Hkv, d, nnz, _ptr(row_ptr), _ptr(col_idx), _ptr(q), q.stride(0), q.stride(1), k, v,
-                                  d ** -0.5 if scale is None else scale, _ptr(out), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws),
-                                  ws.numel(), _stream()), "b2sp_attention_kv4")
+        lse = torch.empty((M, H), dtype=torch.float32, device=device)
+    else:
+        _lse(lse, (M, H))
+    _ready(device, row_ptr, col_idx, k_codes, k_scales, v_codes, v_scales, out, lse)
+    stream = _raw_stream(device.index)
+    ws = _scratch(_attention_kv4_need(M, H, Hkv, d, nnz), device, workspace, stream)
+    _check(lib.b2sp_attention_kv4(M, H, Hkv, d, nnz, row_ptr.data_ptr(), col_idx.data_ptr(), q.data_ptr(), s[0], s[1], k, v,
+                                  d ** -0.5 if scale is None else scale, out.data_ptr(), t[0], t[1], lse.data_ptr(), ws.data_ptr(),
+                                  ws.numel(), stream), "b2sp_attention_kv4")
     return out, lse

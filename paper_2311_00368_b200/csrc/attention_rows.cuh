@@ -33,6 +33,13 @@ __device__ __forceinline__ unsigned bf16x2(float lo, float hi)   // round to nea
 __device__ __forceinline__ void narrow(float x, float &o) { o = x; }
 __device__ __forceinline__ void narrow(float x, Bf16 &o) { o.bits = (unsigned short)bf16x2(x, 0.f); }
 
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // Elements [c, c + 4) of a row of d elements; V = 4: rows are aligned groups of four.
 template <typename T, int V> __device__ __forceinline__ void load4(const T *row, int c, int d, float (&x)[4])
 {

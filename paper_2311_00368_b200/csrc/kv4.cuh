@@ -194,31 +194,64 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const RowsArgs a, T *out)
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------
 struct AttnArgs {
-    int M, heads, kv_heads, d, splits, head_blocks;   // head_blocks: eights (or sixteens, NB = 2) of query heads that share one K and V
+    int M, heads, kv_heads, d, head_blocks;   // head_blocks: eights (or sixteens, NB = 2) of query heads that share one K and V
+    int ctas, share;     // of a key/value head and head block; entries of each
+    long long nnz;
     const int *row_ptr, *col_idx;
     const Bf16 *q;
     long long q_ld, q_sh;
+    int q_wide;          // 16-byte loads of q
     Cache k, v;
     float scale;
     attn::View<Bf16> out;
-    float *lse, *part;
+    float *lse, *part;   // part: two slots per CTA of `ctas` (see the kernel), [heads][part_width]
     float2 *part_ml;
 };
+__device__ __forceinline__ long long part_slot(const AttnArgs &a, int cta, int slot, int h) { return ((long long)cta * 2 + slot) * a.heads + h; }
 
-__device__ __forceinline__ void mma_bf16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
+__device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// 128 + code of nibble I of both halves, as two bf16 (exact: bf16 holds whole numbers up to 256)
-template <int I> __device__ __forceinline__ unsigned nibble_pair(unsigned y)
+// The same onto zeros.
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
-    return ((y >> (4 * I)) & 0x000f000fu) | 0x43004300u;
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ unsigned minus136(unsigned x)   // (128 + code) - 136, exact
+__device__ __forceinline__ unsigned f16x2(float lo, float hi)   // round to nearest even
 {
     unsigned r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x43084308u));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// The codes of nibbles 0 and 1 of both halves of y, less 8, as two f16 each.  A nibble in the lowest bits of the f16 1024 makes 1024 + code, one
+// in the next four bits 1024 + 16 code; both differences are exact.  `k1024` is two f16 of 1024 in a register whose value the compiler does not know:
+// with two constants it takes two instructions for (y & mask) | k1024, with one of them in a register one (263 -> 135 logical instructions
+// per 32 slots).
+__device__ __forceinline__ unsigned two_1024()
+{
+    unsigned r;
+    asm volatile("mov.b32 %0, 0x64006400;" : "=r"(r));
+    return r;
+}
+template <unsigned MASK> __device__ __forceinline__ unsigned onto_1024(unsigned y, unsigned k1024)
+{
+    unsigned r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(y), "n"(MASK), "r"(k1024));   // (y & MASK) | k1024
+    return r;
+}
+__device__ __forceinline__ unsigned codes_low(unsigned y, unsigned k1024)
+{
+    unsigned r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(onto_1024<0x000f000fu>(y, k1024)), "r"(0x64086408u));
+    return r;
+}
+__device__ __forceinline__ unsigned codes_high(unsigned y, unsigned k1024)
+{
+    unsigned r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(onto_1024<0x00f000f0u>(y, k1024)), "r"(0x2c002c00u), "r"(0xd480d480u));   // / 16 - 72
     return r;
 }
 __device__ __forceinline__ void cp_async(unsigned dst, const void *src, int bytes, int keep)
@@ -238,23 +271,29 @@ __device__ __forceinline__ unsigned transpose8(unsigned x)   // an 8 x 8 matrix 
 // O = softmax(scale Q K^T) V of one query token's heads over (a part of) the slots that its row names.
 //
 // A CTA takes one token, one key/value head with up to 8 NB query heads that share it, and one part of the row; its four warps take
-// every fourth 16 slots each and join at the end.  What it has to read is 36 G bytes a slot, so everything is done to keep loads in
-// flight and instructions few: a ring of kStages tiles per warp filled by cp.async; codes become bf16 by one mask each (128 + code);
-// the tensor core's legacy form multiplies them (m16n8k16: 16 slots of K by 8 query heads, then 16 elements of V by 8 query heads), the weights
-// pass from the one product's layout to the other's by movmatrix.
-//   * K: the row scale of a group multiplies the products of its 32 elements, in fp32; the 136 that each code carries too much is
-//     taken off there as 136 sum(q), instead of off each code.
-//   * V: the scale of (slot, group) multiplies the slot's weight before that is rounded to bf16 (half a step, 2^-8 of each weight --
-//     the one rounding of this kernel beside that of the output); codes are made whole numbers -7 .. 7 first, as the sum over slots
-//     would lose the small result in 136 sum(p).
-//   * the running maximum moves only when a logit exceeds it by 8 (to base 2), so that O is rarely rescaled: weights up to 2^8.
-// Slot r of a tile is row r of the first product; V's rows lie in the order (r & 1) * 4 + r / 2 of each half tile, so that the four lanes of
+// every fourth 32 slots each and join at the end.  What it has to read is 36 G bytes a slot; what bounds it beside that is the integer pipe, which
+// makes numbers of the codes (64 lanes a clock), so instructions are kept few: cp.async brings the next 32 slots into the other half of
+// a warp's ring; a code becomes an f16 by one mask and one f16 addition or multiply-add on the other pipe; the tensor core's legacy form
+// multiplies (m16n8k16: 16 slots of K by 8 query heads, then 16 elements of V by 8 query heads); the weights pass from the one product's layout to
+// the other's by movmatrix.
+//   * Q goes to f16 exactly: divided by a power of two that brings each head's largest element below 2; what is more than 2^-14 smaller
+//     than that loses at most 2^-25 of it, as much as fp32 sums would.  The scale of a group of K multiplies the products of its 32 elements.
+//   * The scale of (slot, group) of V multiplies the slot's weight, divided by a power of two per group that keeps all scales met so far below
+//     2^7, and that is rounded to f16 (half a step: 2^-11 of a weight down to 2^-29 of the largest, below that 2^-40 of the largest).  It is the
+//     one rounding of this kernel beside that of the output.
+//   * The running maximum moves only when a logit exceeds it by 8 (to base 2): weights up to 2^8.
+// Slot r of a half tile is row r of the first product; V's rows lie in the order (r & 1) * 4 + r / 2 of each eight, so that the four lanes of
 // a column of V read different banks.
-constexpr int kStages = 4, kSlots = 16;
+//
+// The entries of all rows, one behind the other, are dealt in equal shares to as many CTAs as run at once, so that rows of any lengths
+// keep all SMs busy to the end.  A row inside one share is finished there; of a row that goes on, each CTA leaves its part in the workspace: in slot 0
+// if the row began in an earlier share, else in slot 1; kv4_join_kernel joins the parts in order, and writes the rows without entries.
+constexpr int kStages = 2, kSlots = 32;
 template <int G, int NB> struct Smem {
     static constexpr int ROW = 16 * G;
-    static constexpr int K = 0, V = kSlots * ROW, KS = 2 * kSlots * ROW, VS = KS + kSlots * 8, IDX = VS + kSlots * 8, STAGE = IDX + kSlots * 4;
-    static constexpr int RING = attn::kWarps * kStages * STAGE;
+    static constexpr int K = 0, V = kSlots * ROW, KS = 2 * kSlots * ROW, VS = KS + kSlots * 8, STAGE = VS + kSlots * 8;
+    static constexpr int WIDE = attn::kWarps * kStages * STAGE;   // behind the rings: 32 rows of scales of K and of V in fp32 per warp, four apart
+    static constexpr int RING = WIDE + attn::kWarps * 2 * kSlots * 16;
     static constexpr int JOIN = attn::kWarps * (8 * NB * 32 * G + 16 * NB) * 4;
     static constexpr int BYTES = RING > JOIN ? RING : JOIN;
 };
@@ -279,7 +318,18 @@ template <int A, int B, int N> __device__ __forceinline__ unsigned pick(const un
     constexpr unsigned lo = (A & 1) ? 0x32 : 0x10, hi = (B & 1) ? 0x76 : 0x54;
     return __byte_perm(a[A / 2], b[B / 2], hi << 8 | lo);
 }
-template <int G> __device__ __forceinline__ void lds_scales(const char *p, int odd, float (&s)[G])
+// The same halfwords, each shifted right by eight bits (their lower bytes are of no interest afterwards).
+template <int A, int B, int N> __device__ __forceinline__ unsigned pick_high(const unsigned (&a)[N], const unsigned (&b)[N])
+{
+    constexpr unsigned lo = (A & 1) ? 0x33 : 0x11, hi = (B & 1) ? 0x77 : 0x55;
+    return __byte_perm(a[A / 2], b[B / 2], hi << 8 | lo);
+}
+// Whether a row of an odd number of scales begins in the middle of a word (cp.async brings whole words).
+template <int G> __device__ __forceinline__ int odd_row(const Bf16 *scales, int slot, int ld)
+{
+    return (G & 1) ? (int)((reinterpret_cast<uintptr_t>(scales + (long long)slot * ld) >> 1) & 1) : 0;
+}
+template <int G> __device__ __forceinline__ void lds_scales(const char *p, int odd, float (&s)[G])   // bf16
 {
     if constexpr (G == 4) {
         const uint2 u = *reinterpret_cast<const uint2 *>(p);
@@ -293,6 +343,25 @@ template <int G> __device__ __forceinline__ void lds_scales(const char *p, int o
         for (int c = 0; c < G; ++c) s[c] = __uint_as_float((unsigned)reinterpret_cast<const unsigned short *>(p)[odd + c] << 16);
     }
 }
+template <int G> __device__ __forceinline__ void sts_wide(char *p, const float (&s)[G])
+{
+    if constexpr (G >= 3) *reinterpret_cast<float4 *>(p) = make_float4(s[0], s[1], s[2], G == 4 ? s[G - 1] : 0.f);
+    else if constexpr (G == 2) *reinterpret_cast<float2 *>(p) = make_float2(s[0], s[1]);
+    else *reinterpret_cast<float *>(p) = s[0];
+}
+template <int G> __device__ __forceinline__ void lds_wide(const char *p, float (&s)[G])
+{
+    if constexpr (G >= 3) {
+        const float4 v = *reinterpret_cast<const float4 *>(p);
+        s[0] = v.x; s[1] = v.y; s[2] = v.z;
+        if (G == 4) s[G - 1] = v.w;
+    } else if constexpr (G == 2) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        s[0] = v.x; s[1] = v.y;
+    } else {
+        s[0] = *reinterpret_cast<const float *>(p);
+    }
+}
 // f(std::integral_constant<int, i>) for i = 0 .. N - 1
 template <int N, int I = 0, class F> __device__ __forceinline__ void each(F &&f)
 {
@@ -302,255 +371,410 @@ template <int N, int I = 0, class F> __device__ __forceinline__ void each(F &&f)
     }
 }
 
+// The row that entry `at` (< row_ptr[M]) lies in: 32 ends are looked at at a time.
+__device__ __forceinline__ int row_of(const int *row_ptr, int M, long long at)
+{
+    int lo = 0, hi = M;   // row_ptr[lo] <= at < row_ptr[hi]
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, k = min(lo + step * ((int)(threadIdx.x & 31) + 1), hi);
+        const int n = __popc(__ballot_sync(~0u, row_ptr[k] <= at));   // the first n of them are not beyond it
+        hi = min(lo + step * (n + 1), hi);
+        lo += step * n;
+    }
+    return lo;
+}
+
 template <int G, int NB>
-__global__ void __launch_bounds__(attn::kWarps * 32, NB == 1 ? 4 : 3) kv4_attention_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(const AttnArgs a)
 {
     using S = Smem<G, NB>;
     __shared__ __align__(16) char smem[S::BYTES];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int group = a.heads / a.kv_heads;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the joining kernel waits for this grid's end where it reads)
-    long long u = blockIdx.x;
-    const int part = (int)(u % a.splits); u /= a.splits;
-    const int hb = (int)(u % a.head_blocks); u /= a.head_blocks;
-    const int hkv = (int)(u % a.kv_heads), row = (int)(u / a.kv_heads);
-    const int first = a.row_ptr[row], last = a.row_ptr[row + 1], per = attn::part_len(last - first, a.splits);
-    const long long begin = first + (long long)part * per;
-    if (part && begin >= last) return;
-    const int n = (int)min((long long)per, last - begin);
-    const int *idx = a.col_idx + begin;
-    const int tiles = (n + kSlots - 1) / kSlots, mine = tiles > warp ? (tiles - warp + attn::kWarps - 1) / attn::kWarps : 0;
-    char *ring = smem + warp * kStages * S::STAGE;
+    const int cta = blockIdx.x % a.ctas, of = blockIdx.x / a.ctas, hb = of % a.head_blocks, hkv = of / a.head_blocks;
+    const long long from0 = (long long)cta * a.share, to0 = min(from0 + a.share, min(a.nnz, (long long)a.row_ptr[a.M]));
+    if (from0 >= to0) return;
+    char *ring = smem + warp * kStages * S::STAGE, *wide = smem + S::WIDE + warp * 2 * kSlots * 16;
     const unsigned ring_s = (unsigned)__cvta_generic_to_shared(ring);
     const uint8_t *kc = a.k.codes + hkv * a.k.code_head, *vc = a.v.codes + hkv * a.v.code_head;
     const Bf16 *ksc = a.k.scales + hkv * a.k.scale_head, *vsc = a.v.scales + hkv * a.v.scale_head;
     const int slots = min(a.k.slots, a.v.slots);
-
-    auto fetch_idx = [&](int i) {   // the slot of lane & 15 of this warp's tile i, or -1
-        const int at = (warp + i * attn::kWarps) * kSlots + (lane & 15);
-        const int s = i < mine && at < n ? idx[at] : -1;
-        return (unsigned)s < (unsigned)slots ? s : -1;
-    };
-    auto issue = [&](int i, int slot) {
-        if (i < mine) {
-            const int st = (i % kStages) * S::STAGE;
+    // where this lane's pieces of a tile go: G pieces of 16 bytes of K's codes and of V's
+    unsigned dst_k[G], dst_v[G];   // shared addresses in stage 0
 #pragma unroll
-            for (int c = 0; c < G; ++c) {
-                const int id = c * 32 + lane;
-                const bool is_v = id >= kSlots * G;
-                const int in = is_v ? id - kSlots * G : id, r = in / G, ch = in % G;
-                const int s = __shfl_sync(~0u, slot, r);
-                const uint8_t *src = is_v ? vc + (long long)max(s, 0) * a.v.code_ld : kc + (long long)max(s, 0) * a.k.code_ld;
-                const int vrow = (r & 8) | ((r & 1) << 2) | (r >> 1 & 3);
-                const int dst = is_v ? S::V + vrow * S::ROW + (G == 4 ? ch ^ (vrow & 2) : ch) * 16 : S::K + r * S::ROW + ch * 16;
-                cp_async(ring_s + st + dst, src + ch * 16, 16, s >= 0 ? 16 : 0);
-            }
-            {
-                const int r = lane & 15;
-                const bool is_v = lane >= 16;
-                const long long at = (long long)max(slot, 0) * (is_v ? a.v.scale_ld : a.k.scale_ld);
-                const Bf16 *src = (is_v ? vsc : ksc) + at;
-                const unsigned dst = ring_s + st + (is_v ? S::VS : S::KS) + r * 8;
-                if constexpr (G == 4) cp_async(dst, src, 8, slot >= 0 ? 8 : 0);
-                else if constexpr (G == 2) cp_async(dst, src, 4, slot >= 0 ? 4 : 0);
-                else {   // whole words around an odd number of halfwords; bytes behind the row are not read
-                    const int off = (int)(reinterpret_cast<uintptr_t>(src) & 2);
-                    const char *p = reinterpret_cast<const char *>(src) - off;
-                    const int bytes = off + 2 * G;
-                    cp_async(dst, p, 4, slot >= 0 ? min(bytes, 4) : 0);
-                    if (G == 3) cp_async(dst + 4, p + 4, 4, slot >= 0 ? bytes - 4 : 0);
-                }
-                if (lane < 16) *reinterpret_cast<int *>(ring + st + S::IDX + r * 4) = slot;
-            }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-
-    // The first tiles are on their way while Q is read.  Q: lane (g, t) has elements 8 t .. 8 t + 7 of each group of query head g (of each eight)
-    int next = fetch_idx(0);
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) {
-        const int now = next;
-        next = fetch_idx(i + 1);
-        issue(i, now);
+    for (int c = 0; c < G; ++c) {
+        const int id = c * 32 + lane, r = id / G, ch = id % G, vrow = (r & 24) | ((r & 1) << 2) | (r >> 1 & 3);
+        dst_k[c] = ring_s + S::K + r * S::ROW + ch * 16;
+        dst_v[c] = ring_s + S::V + vrow * S::ROW + (G == 4 ? ch ^ (vrow & 2) : ch) * 16;
     }
-    unsigned qa[G][2][2][NB];   // [group][k step][half of k]
-    float qsum[G][NB][2];       // 136 times the sum over the group, of query heads 2 t and 2 t + 1
+    const unsigned k1024 = two_1024();
+    const int k_ld = (int)a.k.code_ld, v_ld = (int)a.v.code_ld, ks_ld = (int)a.k.scale_ld, vs_ld = (int)a.v.scale_ld;
+
+    for (int row = row_of(a.row_ptr, a.M, from0); row < a.M; ++row) {
+        const int first = a.row_ptr[row], last = a.row_ptr[row + 1];
+        if (first >= to0) break;
+        const long long begin = max((long long)first, from0), end = min((long long)last, to0);
+        if (begin >= end) continue;
+        const int n = (int)(end - begin);
+        const int *idx = a.col_idx + begin;
+        const int tiles = (n + kSlots - 1) / kSlots, mine = tiles > warp ? (tiles - warp + attn::kWarps - 1) / attn::kWarps : 0;
+
+        auto fetch_idx = [&](int i) {   // this lane's slot of the warp's tile i, or -1
+            const int at = (warp + i * attn::kWarps) * kSlots + lane;
+            const int s = i < mine && at < n ? idx[at] : -1;
+            return (unsigned)s < (unsigned)slots ? s : -1;
+        };
+        auto scale_row = [&](unsigned dst, const Bf16 *src, int slot) {
+            if constexpr (G == 4) cp_async(dst, src, 8, slot >= 0 ? 8 : 0);
+            else if constexpr (G == 2) cp_async(dst, src, 4, slot >= 0 ? 4 : 0);
+            else {   // whole words around an odd number of halfwords; bytes behind the row are not read
+                const int off = (int)(reinterpret_cast<uintptr_t>(src) & 2);
+                const char *p = reinterpret_cast<const char *>(src) - off;
+                const int bytes = off + 2 * G;
+                cp_async(dst, p, 4, slot >= 0 ? min(bytes, 4) : 0);
+                if (G == 3) cp_async(dst + 4, p + 4, 4, slot >= 0 ? bytes - 4 : 0);
+            }
+        };
+        auto issue = [&](int i, int slot) {
+            if (i < mine) {
+                const unsigned st = (unsigned)(i % kStages) * S::STAGE;
+                const int at = max(slot, 0);
 #pragma unroll
-    for (int c = 0; c < G; ++c)
+                for (int c = 0; c < G; ++c) {
+                    const int s = __shfl_sync(~0u, slot, (c * 32 + lane) / G), r = max(s, 0), keep = s >= 0 ? 16 : 0, ch = (c * 32 + lane) % G * 16;
+                    cp_async(dst_k[c] + st, kc + ((long long)r * k_ld + ch), 16, keep);
+                    cp_async(dst_v[c] + st, vc + ((long long)r * v_ld + ch), 16, keep);
+                }
+                scale_row(ring_s + st + S::KS + lane * 8, ksc + (long long)at * ks_ld, slot);
+                scale_row(ring_s + st + S::VS + lane * 8, vsc + (long long)at * vs_ld, slot);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+
+        // The first tile is on its way while Q is read.  Q: lane (g, t) has elements 8 t .. 8 t + 7 of each group of query head g (of each eight)
+        int cur = -1, now = fetch_idx(0), next = fetch_idx(1);   // slots of the tile at hand, of the one being fetched, of the one behind it
+        issue(0, now);
+        unsigned qa[G][2][2][NB];   // [group][k step][half of k]
+        float c2[NB][2];            // scale log2(e) and what Q is divided by, of query heads 2 t and 2 t + 1
 #pragma unroll
         for (int m = 0; m < NB; ++m) {
             const int hq = hb * 8 * NB + m * 8 + g;
-            unsigned short x[8];
-            float sum = 0.f;
+            const Bf16 *q = a.q + (long long)row * a.q_ld + (long long)(hkv * group + hq) * a.q_sh;
+            uint4 x[G];
+            float high = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int e = 32 * c + 8 * t + i;
-                x[i] = hq < group && e < a.d ? a.q[(long long)row * a.q_ld + (long long)(hkv * group + hq) * a.q_sh + e].bits : 0;
-                sum += __uint_as_float((unsigned)x[i] << 16);
-            }
+            for (int c = 0; c < G; ++c) {
+                const int e = 32 * c + 8 * t;
+                x[c] = make_uint4(0, 0, 0, 0);
+                if (hq < group) {
+                    if (a.q_wide) {
+                        if (e < a.d) x[c] = __ldg(reinterpret_cast<const uint4 *>(q + e));
+                    } else {
+                        unsigned short y[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qa[c][i >> 1][i & 1][m] = x[i] | (unsigned)x[i + 4] << 16;
-            sum += __shfl_xor_sync(~0u, sum, 1);
-            sum += __shfl_xor_sync(~0u, sum, 2);
-            qsum[c][m][0] = 136.f * __shfl_sync(~0u, sum, 8 * t);
-            qsum[c][m][1] = 136.f * __shfl_sync(~0u, sum, 8 * t + 4);
-        }
-    float o[G][2][NB][4] = {};   // [group][pair of elements]: rows g (the first of the pair) and g + 8 (the second), columns 2 t, 2 t + 1
-    float top[NB][2], sum[NB][2];
-#pragma unroll
-    for (int m = 0; m < NB; ++m) { top[m][0] = top[m][1] = -CUDART_INF_F; sum[m][0] = sum[m][1] = 0.f; }
-    const float c2 = a.scale * attn::kLog2e;
-
-    for (int i = 0; i < mine; ++i) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-        __syncwarp();
-        {
-            const int now = next;
-            next = fetch_idx(i + kStages);
-            issue(i + kStages - 1, now);   // into the stage that the last iteration read (all lanes are past it)
-        }
-        const char *st = ring + (i % kStages) * S::STAGE;
-        const int sl0 = *reinterpret_cast<const int *>(st + S::IDX + 4 * g), sl1 = *reinterpret_cast<const int *>(st + S::IDX + 4 * g + 32);
-        float x[NB][4];   // logits: slots g (two heads), g + 8 (two heads)
-        {
-            unsigned w0[G], w1[G];
-            lds_halves<2 * G, 4>(st + S::K + g * S::ROW + 4 * G * t, w0);
-            lds_halves<2 * G, 4>(st + S::K + (g + 8) * S::ROW + 4 * G * t, w1);
-            float s0[G], s1[G];
-            lds_scales<G>(st + S::KS + g * 8, (G & 1) ? (int)((reinterpret_cast<uintptr_t>(ksc + sl0 * a.k.scale_ld) >> 1) & 1) : 0, s0);
-            lds_scales<G>(st + S::KS + g * 8 + 64, (G & 1) ? (int)((reinterpret_cast<uintptr_t>(ksc + sl1 * a.k.scale_ld) >> 1) & 1) : 0, s1);
-#pragma unroll
-            for (int m = 0; m < NB; ++m) x[m][0] = x[m][1] = x[m][2] = x[m][3] = 0.f;
-            each<G>([&](auto cc) {
-                constexpr int c = decltype(cc)::value;
-                const unsigned y0 = pick<c, G + c>(w0, w0), y1 = pick<c, G + c>(w1, w1);
-                const unsigned a0 = nibble_pair<0>(y0), a1 = nibble_pair<0>(y1), a2 = nibble_pair<1>(y0), a3 = nibble_pair<1>(y1);
-                const unsigned b0 = nibble_pair<2>(y0), b1 = nibble_pair<2>(y1), b2 = nibble_pair<3>(y0), b3 = nibble_pair<3>(y1);
-#pragma unroll
-                for (int m = 0; m < NB; ++m) {
-                    float f[4] = {};
-                    mma_bf16(f, a0, a1, a2, a3, qa[c][0][0][m], qa[c][0][1][m]);
-                    mma_bf16(f, b0, b1, b2, b3, qa[c][1][0][m], qa[c][1][1][m]);
-                    x[m][0] = fmaf(s0[c], f[0] - qsum[c][m][0], x[m][0]);
-                    x[m][1] = fmaf(s0[c], f[1] - qsum[c][m][1], x[m][1]);
-                    x[m][2] = fmaf(s1[c], f[2] - qsum[c][m][0], x[m][2]);
-                    x[m][3] = fmaf(s1[c], f[3] - qsum[c][m][1], x[m][3]);
+                        for (int i = 0; i < 8; ++i) y[i] = e + i < a.d ? q[e + i].bits : 0;
+                        x[c] = make_uint4(y[0] | (unsigned)y[1] << 16, y[2] | (unsigned)y[3] << 16, y[4] | (unsigned)y[5] << 16, y[6] | (unsigned)y[7] << 16);
+                    }
                 }
-            });
-        }
-        bool move = false;
+                const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
-        for (int m = 0; m < NB; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[m][e] = (e < 2 ? sl0 : sl1) >= 0 ? x[m][e] * c2 : -CUDART_INF_F;
-                move |= x[m][e] > top[m][e & 1] + 8.f;
+                for (int i = 0; i < 4; ++i) high = fmaxf(high, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
             }
-        if (__any_sync(~0u, move)) {
+            high = fmaxf(high, __shfl_xor_sync(~0u, high, 1));
+            high = fmaxf(high, __shfl_xor_sync(~0u, high, 2));
+            const int e = min(max((int)(__float_as_uint(high) >> 23) - 127, -126), 126);   // (a NaN or an infinity stays one)
+            const float by = __uint_as_float((unsigned)(127 - e) << 23), up = a.scale * attn::kLog2e * __uint_as_float((unsigned)(127 + e) << 23);
+            c2[m][0] = __shfl_sync(~0u, up, 8 * t);
+            c2[m][1] = __shfl_sync(~0u, up, 8 * t + 4);
+#pragma unroll
+            for (int c = 0; c < G; ++c) {
+                const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f[2 * i] = __uint_as_float(w[i] << 16) * by;
+                    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u) * by;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) qa[c][i >> 1][i & 1][m] = f16x2(f[i], f[i + 4]);
+            }
+        }
+        float o[G][2][NB][4] = {};   // [group][pair of elements]: rows g (the first of the pair) and g + 8 (the second), columns 2 t, 2 t + 1
+        float top[NB][2], base[NB][2], sum[NB][2];   // base: top, or 0 as long as that is -inf
+        float down[G];               // what V's scales are multiplied by (2^100 at first, which any scale above 2^-93 moves)
+#pragma unroll
+        for (int c = 0; c < G; ++c) down[c] = 1.2676506e30f;
+#pragma unroll
+        for (int m = 0; m < NB; ++m) { top[m][0] = top[m][1] = -CUDART_INF_F; base[m][0] = base[m][1] = 0.f; sum[m][0] = sum[m][1] = 0.f; }
+
+        for (int i = 0; i < mine; ++i) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            cur = now;
+            now = next;
+            next = fetch_idx(i + 2);
+            issue(i + 1, now);   // into the stage that the last iteration read (all lanes are past it)
+            const char *st = ring + (i % kStages) * S::STAGE;
+            const unsigned valid = __ballot_sync(~0u, cur >= 0);
+            {
+                // a slot's scales per lane, to fp32
+                float ks[G], vs[G], high = 0.f;
+                lds_scales<G>(st + S::KS + lane * 8, odd_row<G>(ksc, max(cur, 0), ks_ld), ks);
+                lds_scales<G>(st + S::VS + lane * 8, odd_row<G>(vsc, max(cur, 0), vs_ld), vs);
+#pragma unroll
+                for (int c = 0; c < G; ++c) high = fmaxf(high, vs[c] * down[c]);
+                if (__any_sync(~0u, high > 128.f)) {   // a power of two that brings the largest of the group to 64 .. 128
+#pragma unroll
+                    for (int c = 0; c < G; ++c) {
+                        float x = vs[c] * down[c] > 128.f ? vs[c] : 0.f;
+#pragma unroll
+                        for (int w = 1; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, w));
+                        if (x > 0.f) {   // (the same for all lanes)
+                            const float to = __uint_as_float((unsigned)min(max(254 + 6 - (int)(__float_as_uint(x) >> 23), 1), 253) << 23);
+                            const float f = to * __uint_as_float((254u << 23) - __float_as_uint(down[c]));
+                            down[c] = to;
+#pragma unroll
+                            for (int m = 0; m < NB; ++m)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) { o[c][0][m][e] *= f; o[c][1][m][e] *= f; }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < G; ++c) vs[c] *= down[c];
+                sts_wide<G>(wide + lane * 16, ks);
+                sts_wide<G>(wide + kSlots * 16 + lane * 16, vs);
+            }
+            __syncwarp();
+            float x[2][NB][4];   // of each half tile: logits of slots g (two heads) and g + 8 (two heads)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r0 = 16 * j + g, r1 = r0 + 8;
+                unsigned w0[G], w1[G];
+                lds_halves<2 * G, 4>(st + S::K + r0 * S::ROW + 4 * G * t, w0);
+                lds_halves<2 * G, 4>(st + S::K + r1 * S::ROW + 4 * G * t, w1);
+                float s0[G], s1[G];
+                lds_wide<G>(wide + r0 * 16, s0);
+                lds_wide<G>(wide + r1 * 16, s1);
+                each<G>([&](auto cc) {
+                    constexpr int c = decltype(cc)::value;
+                    const unsigned y0 = pick<c, G + c>(w0, w0), y1 = pick<c, G + c>(w1, w1), z0 = pick_high<c, G + c>(w0, w0), z1 = pick_high<c, G + c>(w1, w1);
+                    const unsigned a0 = codes_low(y0, k1024), a1 = codes_low(y1, k1024), a2 = codes_high(y0, k1024), a3 = codes_high(y1, k1024);
+                    const unsigned b0 = codes_low(z0, k1024), b1 = codes_low(z1, k1024), b2 = codes_high(z0, k1024), b3 = codes_high(z1, k1024);
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) {
+                        float f[4];
+                        mma_f16_first(f, a0, a1, a2, a3, qa[c][0][0][m], qa[c][0][1][m]);
+                        mma_f16(f, b0, b1, b2, b3, qa[c][1][0][m], qa[c][1][1][m]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[j][m][e] = c == 0 ? (e < 2 ? s0[0] : s1[0]) * f[e] : fmaf(e < 2 ? s0[c] : s1[c], f[e], x[j][m][e]);
+                    }
+                });
+#pragma unroll
+                for (int m = 0; m < NB; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[j][m][e] *= c2[m][e & 1];
+                if (valid != ~0u) {
+#pragma unroll
+                    for (int m = 0; m < NB; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(valid >> (e < 2 ? r0 : r1) & 1)) x[j][m][e] = -CUDART_INF_F;
+                }
+            }
+            bool move = false;
 #pragma unroll
             for (int m = 0; m < NB; ++m)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float to = fmaxf(x[m][e], x[m][e + 2]);
+                for (int e = 0; e < 2; ++e) move |= fmaxf(fmaxf(x[0][m][e], x[0][m][e + 2]), fmaxf(x[1][m][e], x[1][m][e + 2])) > top[m][e] + 8.f;
+            if (__any_sync(~0u, move)) {
 #pragma unroll
-                    for (int w = 4; w < 32; w <<= 1) to = fmaxf(to, __shfl_xor_sync(~0u, to, w));
-                    to = fmaxf(to, top[m][e]);
-                    const float fall = to == -CUDART_INF_F ? 1.f : exp2f(top[m][e] - to);
-                    top[m][e] = to;
-                    sum[m][e] *= fall;
+                for (int m = 0; m < NB; ++m)
 #pragma unroll
-                    for (int c = 0; c < G; ++c)
+                    for (int e = 0; e < 2; ++e) {
+                        float to = fmaxf(fmaxf(x[0][m][e], x[0][m][e + 2]), fmaxf(x[1][m][e], x[1][m][e + 2]));
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            o[c][k][m][e] *= fall;
-                            o[c][k][m][e + 2] *= fall;
-                        }
-                }
+                        for (int w = 4; w < 32; w <<= 1) to = fmaxf(to, __shfl_xor_sync(~0u, to, w));
+                        to = fmaxf(to, top[m][e]);
+                        base[m][e] = to == -CUDART_INF_F ? 0.f : to;
+                        const float fall = attn::ex2(top[m][e] - base[m][e]);
+                        top[m][e] = to;
+                        sum[m][e] *= fall;
+#pragma unroll
+                        for (int c = 0; c < G; ++c)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                o[c][k][m][e] *= fall;
+                                o[c][k][m][e + 2] *= fall;
+                            }
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int m = 0; m < NB; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[j][m][e] = attn::ex2(x[j][m][e] - base[m][e & 1]);
+                        sum[m][e & 1] += x[j][m][e];
+                    }
+                // V: slots 2 t, 2 t + 1 and those eight on, this lane's row g of every product
+                unsigned w[4][(G + 1) / 2];
+                const int at = G == 4 ? ((((g >> 1) ^ (t & 2)) << 4) | ((g & 1) << 3)) : 2 * G * g;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) lds_halves<G, (G & 1) ? 2 : 4>(st + S::V + (16 * j + (k >> 1) * 8 + (k & 1) * 4 + t) * S::ROW + at, w[k]);
+                float s0[G], s1[G];
+                lds_wide<G>(wide + kSlots * 16 + (16 * j + g) * 16, s0);
+                lds_wide<G>(wide + kSlots * 16 + (16 * j + g + 8) * 16, s1);
+                each<G>([&](auto cc) {
+                    constexpr int c = decltype(cc)::value;
+                    const unsigned y0 = pick<c, c>(w[0], w[1]), y1 = pick<c, c>(w[2], w[3]), z0 = pick_high<c, c>(w[0], w[1]), z1 = pick_high<c, c>(w[2], w[3]);
+                    const unsigned a0 = codes_low(y0, k1024), a1 = codes_high(y0, k1024), a2 = codes_low(y1, k1024), a3 = codes_high(y1, k1024);
+                    const unsigned b0 = codes_low(z0, k1024), b1 = codes_high(z0, k1024), b2 = codes_low(z1, k1024), b3 = codes_high(z1, k1024);
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) {
+                        const unsigned p0 = transpose8(f16x2(x[j][m][0] * s0[c], x[j][m][1] * s0[c]));
+                        const unsigned p1 = transpose8(f16x2(x[j][m][2] * s1[c], x[j][m][3] * s1[c]));
+                        mma_f16(o[c][0][m], a0, a1, a2, a3, p0, p1);
+                        mma_f16(o[c][1][m], b0, b1, b2, b3, p0, p1);
+                    }
+                });
+            }
+            __syncwarp();
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();   // the ring is free: the warps join in it
+
+        constexpr int W = 32 * G, HEADS = 8 * NB, PER = HEADS * W + 2 * HEADS;
+#pragma unroll
+        for (int c = 0; c < G; ++c) {
+            const float up = __uint_as_float((254u << 23) - __float_as_uint(down[c]));   // 1 / a power of two
+#pragma unroll
+            for (int m = 0; m < NB; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { o[c][0][m][e] *= up; o[c][1][m][e] *= up; }
+        }
+        float *join = reinterpret_cast<float *>(smem) + warp * PER;
 #pragma unroll
         for (int m = 0; m < NB; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[m][e] = exp2f(x[m][e] - (top[m][e & 1] == -CUDART_INF_F ? 0.f : top[m][e & 1]));
-                sum[m][e & 1] += x[m][e];
-            }
-        {
-            // V: slots 2 t, 2 t + 1 and those eight on, this lane's row g of every product
-            constexpr int H = (G + 1) / 2;
-            unsigned w[4][H];
-            const int at = G == 4 ? ((((g >> 1) ^ (t & 2)) << 4) | ((g & 1) << 3)) : 2 * G * g;
+            for (int e = 0; e < 2; ++e) {
+                float l = sum[m][e];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) lds_halves<G, (G & 1) ? 2 : 4>(st + S::V + ((k >> 1) * 8 + (k & 1) * 4 + t) * S::ROW + at, w[k]);
-            float s0[G], s1[G];
-            lds_scales<G>(st + S::VS + g * 8, (G & 1) ? (int)((reinterpret_cast<uintptr_t>(vsc + sl0 * a.v.scale_ld) >> 1) & 1) : 0, s0);
-            lds_scales<G>(st + S::VS + g * 8 + 64, (G & 1) ? (int)((reinterpret_cast<uintptr_t>(vsc + sl1 * a.v.scale_ld) >> 1) & 1) : 0, s1);
-            each<G>([&](auto cc) {
-                constexpr int c = decltype(cc)::value;
-                const unsigned y0 = pick<c, c>(w[0], w[1]), y1 = pick<c, c>(w[2], w[3]);
-                const unsigned a0 = minus136(nibble_pair<0>(y0)), a1 = minus136(nibble_pair<1>(y0)), a2 = minus136(nibble_pair<0>(y1)), a3 = minus136(nibble_pair<1>(y1));
-                const unsigned b0 = minus136(nibble_pair<2>(y0)), b1 = minus136(nibble_pair<3>(y0)), b2 = minus136(nibble_pair<2>(y1)), b3 = minus136(nibble_pair<3>(y1));
-#pragma unroll
-                for (int m = 0; m < NB; ++m) {
-                    const unsigned p0 = transpose8(attn::bf16x2(x[m][0] * s0[c], x[m][1] * s0[c])), p1 = transpose8(attn::bf16x2(x[m][2] * s1[c], x[m][3] * s1[c]));
-                    mma_bf16(o[c][0][m], a0, a1, a2, a3, p0, p1);
-                    mma_bf16(o[c][1][m], b0, b1, b2, b3, p0, p1);
+                for (int w = 4; w < 32; w <<= 1) l += __shfl_xor_sync(~0u, l, w);
+                const int head = m * 8 + 2 * t + e;
+                if (g == 0) {
+                    join[HEADS * W + head] = top[m][e];
+                    join[HEADS * W + HEADS + head] = l;
                 }
-            });
-        }
-        __syncwarp();
-    }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();   // the ring is free: the warps join in it
-
-    constexpr int W = 32 * G, HEADS = 8 * NB, PER = HEADS * W + 2 * HEADS;
-    float *join = reinterpret_cast<float *>(smem) + warp * PER;
 #pragma unroll
-    for (int m = 0; m < NB; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float l = sum[m][e];
-#pragma unroll
-            for (int w = 4; w < 32; w <<= 1) l += __shfl_xor_sync(~0u, l, w);
-            const int head = m * 8 + 2 * t + e;
-            if (g == 0) {
-                join[HEADS * W + head] = top[m][e];
-                join[HEADS * W + HEADS + head] = l;
+                for (int c = 0; c < G; ++c)
+                    *reinterpret_cast<float4 *>(join + head * W + 32 * c + 4 * g) = make_float4(o[c][0][m][e], o[c][0][m][e + 2], o[c][1][m][e], o[c][1][m][e + 2]);
             }
+        __syncthreads();
+        join = reinterpret_cast<float *>(smem);
+        const int width = attn::part_width(attn::kForward, a.d);
+        const bool alone = begin == first && end == last;
+        for (int i = threadIdx.x; i < HEADS * (W / 4); i += attn::kWarps * 32) {
+            const int m = i / (W / 4), e = i % (W / 4) * 4, hq = hb * HEADS + m;
+            if (hq >= group || e >= width) continue;
+            float high = -CUDART_INF_F, l = 0.f, x[4] = {};
 #pragma unroll
-            for (int c = 0; c < G; ++c)
-                *reinterpret_cast<float4 *>(join + head * W + 32 * c + 4 * g) = make_float4(o[c][0][m][e], o[c][0][m][e + 2], o[c][1][m][e], o[c][1][m][e + 2]);
+            for (int w = 0; w < attn::kWarps; ++w) high = fmaxf(high, join[w * PER + HEADS * W + m]);
+            const float ref = high == -CUDART_INF_F ? 0.f : high;
+#pragma unroll
+            for (int w = 0; w < attn::kWarps; ++w) {
+                const float f = exp2f(join[w * PER + HEADS * W + m] - ref);
+                l = fmaf(f, join[w * PER + HEADS * W + HEADS + m], l);
+                const float4 y = *reinterpret_cast<const float4 *>(join + w * PER + m * W + e);
+                x[0] = fmaf(f, y.x, x[0]); x[1] = fmaf(f, y.y, x[1]); x[2] = fmaf(f, y.z, x[2]); x[3] = fmaf(f, y.w, x[3]);
+            }
+            const int h = hkv * group + hq;
+            if (!alone) {
+                const long long unit = part_slot(a, cta, first < from0 ? 0 : 1, h);
+                attn::store4<float, 4>(a.part + unit * width, e, width, x);
+                if (e == 0) a.part_ml[unit] = make_float2(high, l);
+            } else {
+                const float f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] *= f;
+                attn::store4<Bf16, 1>(a.out.at(0, h, row), e, a.d, x);
+                if (e == 0) a.lse[(long long)row * a.heads + h] = l == 0.f ? -CUDART_INF_F : (high + log2f(l)) * attn::kLn2;
+            }
         }
-    __syncthreads();
-    join = reinterpret_cast<float *>(smem);
-    const int width = attn::part_width(attn::kForward, a.d);
-    for (int i = threadIdx.x; i < HEADS * (W / 4); i += attn::kWarps * 32) {
-        const int m = i / (W / 4), e = i % (W / 4) * 4, hq = hb * HEADS + m;
-        if (hq >= group || e >= width) continue;
-        float high = -CUDART_INF_F, l = 0.f, x[4] = {};
+        __syncthreads();   // the next row's tiles go into the ring
+    }
+}
+
+// A CTA per (row, query head): joins the parts of a row that several shares hold, each warp every eighth of them (all their loads at once) and the
+// warps in order; zeros for a row without entries.
+constexpr int kJoinWarps = 8;
+__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(const AttnArgs a)
+{
+    __shared__ float sums[kJoinWarps][128], weight[kJoinWarps], highs[kJoinWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
+    const int first = a.row_ptr[row], last = (int)min((long long)a.row_ptr[row + 1], a.nnz);
+    const int c0 = first / a.share, c1 = (last - 1) / a.share, width = attn::part_width(attn::kForward, a.d);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (last > first && c0 == c1) return;
+    float x[4] = {}, high = -CUDART_INF_F, l = 0.f;
+    if (last > first) {
+        constexpr int AT = 8;
+        for (int b = c0 + warp; b <= c1; b += kJoinWarps * AT) {   // (one round up to 64 parts)
+            float y[AT][4];
+            float2 ml[AT];
 #pragma unroll
-        for (int w = 0; w < attn::kWarps; ++w) high = fmaxf(high, join[w * PER + HEADS * W + m]);
-        const float ref = high == -CUDART_INF_F ? 0.f : high;
+            for (int i = 0; i < AT; ++i) {
+                const int c = b + i * kJoinWarps;
+                ml[i] = make_float2(-CUDART_INF_F, 0.f);
+                y[i][0] = y[i][1] = y[i][2] = y[i][3] = 0.f;
+                if (c <= c1) {
+                    const long long unit = part_slot(a, c, c == c0, h);
+                    ml[i] = a.part_ml[unit];
+                    attn::load4<float, 4>(a.part + unit * width, lane * 4, width, y[i]);
+                }
+            }
+            float to = high;
 #pragma unroll
-        for (int w = 0; w < attn::kWarps; ++w) {
-            const float f = exp2f(join[w * PER + HEADS * W + m] - ref);
-            l = fmaf(f, join[w * PER + HEADS * W + HEADS + m], l);
-            const float4 y = *reinterpret_cast<const float4 *>(join + w * PER + m * W + e);
-            x[0] = fmaf(f, y.x, x[0]); x[1] = fmaf(f, y.y, x[1]); x[2] = fmaf(f, y.z, x[2]); x[3] = fmaf(f, y.w, x[3]);
-        }
-        const int h = hkv * group + hq;
-        if (a.part) {
-            const long long unit = ((long long)h * a.M + row) * a.splits + part;
-            attn::store4<float, 4>(a.part + unit * width, e, width, x);
-            if (e == 0) a.part_ml[unit] = make_float2(high, l);
-        } else {
-            const float f = l == 0.f ? 0.f : 1.f / l;
+            for (int i = 0; i < AT; ++i) to = fmaxf(to, ml[i].x);
+            const float ref = to == -CUDART_INF_F ? 0.f : to, fall = exp2f(high - ref);
+            high = to;
+            l *= fall;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] *= f;
-            attn::store4<Bf16, 1>(a.out.at(0, h, row), e, a.d, x);
-            if (e == 0) a.lse[(long long)row * a.heads + h] = l == 0.f ? -CUDART_INF_F : (high + log2f(l)) * attn::kLn2;
+            for (int k = 0; k < 4; ++k) x[k] *= fall;
+#pragma unroll
+            for (int i = 0; i < AT; ++i) {
+                const float f = exp2f(ml[i].x - ref);
+                l = fmaf(ml[i].y, f, l);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = fmaf(f, y[i][k], x[k]);
+            }
         }
     }
+    *reinterpret_cast<float4 *>(&sums[warp][lane * 4]) = make_float4(x[0], x[1], x[2], x[3]);
+    if (lane == 0) { weight[warp] = l; highs[warp] = high; }
+    __syncthreads();
+    if (warp) return;
+    high = -CUDART_INF_F;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) high = fmaxf(high, highs[w]);
+    const float ref = high == -CUDART_INF_F ? 0.f : high;
+    l = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = exp2f(highs[w] - ref);
+        l = fmaf(f, weight[w], l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = fmaf(f, sums[w][lane * 4 + k], x[k]);
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] *= f;
+    attn::store4<Bf16, 1>(a.out.at(0, h, row), lane * 4, a.d, x);
+    if (lane == 0) a.lse[(long long)row * a.heads + h] = l == 0.f ? -CUDART_INF_F : (high + log2f(l)) * attn::kLn2;
 }
 
 }  // namespace kv4

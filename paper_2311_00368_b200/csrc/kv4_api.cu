@@ -97,23 +97,25 @@ b2sp_status read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 
 }
 
 struct ServePlan {
-    int nb, head_blocks, splits;
+    int nb, head_blocks, ctas, share;
     size_t ml, part, bytes;
 };
-// Parts of a row, of at least 128 slots on average: for one token as many CTAs as run at once (four on an SM); for several tokens, whose rows
-// differ in length, four times as many, so that those with short parts make room early.
+// As many CTAs as run at once (three on an SM), with at least 128 entries each.
 ServePlan serve_plan(int M, int heads, int kv_heads, int d, long long nnz)
 {
     ServePlan p;
     const int group = heads / kv_heads;
     p.nb = group > 8 ? 2 : 1;
     p.head_blocks = (group + 8 * p.nb - 1) / (8 * p.nb);
-    const long long units = std::max(1ll, (long long)M * kv_heads * p.head_blocks), avg = M ? nnz / M : 0, want = 148ll * (p.nb == 1 ? 4 : 3) * (M > 1 ? 4 : 1);
-    p.splits = (int)std::max(1ll, std::min({M > 1 ? (want + units - 1) / units : want / units, 4096ll, avg / 128}));
-    const long long parts = (long long)M * heads * p.splits;
+    const long long units = (long long)kv_heads * p.head_blocks, most = std::max(1ll, 148ll * 3 / units);
+    const long long ctas = std::max(1ll, std::min(most, (nnz + 127) / 128));
+    p.share = (int)(((nnz + ctas - 1) / ctas + kSlots - 1) / kSlots * kSlots);
+    if (p.share == 0) p.share = kSlots;
+    p.ctas = (int)std::max(1ll, (nnz + p.share - 1) / p.share);
+    const long long parts = M > 0 && p.ctas > 1 ? 2ll * p.ctas * heads : 0;
     p.ml = 512;
-    p.part = p.ml + attn::up256(p.splits > 1 ? parts * 8 : 0);
-    p.bytes = p.part + attn::up256(p.splits > 1 ? parts * attn::part_width(attn::kForward, d) * 4 : 0);
+    p.part = p.ml + attn::up256(parts * 8);
+    p.bytes = p.part + attn::up256(parts * attn::part_width(attn::kForward, d) * 4);
     return p;
 }
 
@@ -177,34 +179,34 @@ extern "C" b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d,
     b2sp_status rc = check_cache(keys, kv_heads, G);
     if (rc == B2SP_OK) rc = check_cache(values, kv_heads, G);
     if (rc != B2SP_OK) return rc;
+    if (keys->code_ld > INT_MAX || values->code_ld > INT_MAX || keys->scale_ld > INT_MAX || values->scale_ld > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     const ServePlan p = serve_plan(M, heads, kv_heads, d, nnz);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
-    const long long blocks = (long long)M * kv_heads * p.head_blocks * p.splits;
-    if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    const long long blocks = (long long)kv_heads * p.head_blocks * p.ctas, joins = (long long)M * heads;
+    if (blocks > INT_MAX || joins > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
     AttnArgs a = {};
-    a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.splits = p.splits; a.head_blocks = p.head_blocks;
+    a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.head_blocks = p.head_blocks; a.ctas = p.ctas; a.share = p.share; a.nnz = nnz;
     a.row_ptr = row_ptr; a.col_idx = col_idx;
     a.q = static_cast<const Bf16 *>(Q); a.q_ld = ldq; a.q_sh = stride_head_q;
+    a.q_wide = eights(a.q, ldq, stride_head_q, d);
     a.k = cache(keys); a.v = cache(values); a.scale = scale;
     a.out = attn::View<Bf16>{static_cast<Bf16 *>(O), ldo, stride_head_o, 0};
     a.lse = lse;
-    if (p.splits > 1) { a.part = reinterpret_cast<float *>(ws + p.part); a.part_ml = reinterpret_cast<float2 *>(ws + p.ml); }
-    switch (G) {
-        case 1: launch<1>(a, p.nb, (unsigned)blocks, st); break;
-        case 2: launch<2>(a, p.nb, (unsigned)blocks, st); break;
-        case 3: launch<3>(a, p.nb, (unsigned)blocks, st); break;
-        default: launch<4>(a, p.nb, (unsigned)blocks, st); break;
-    }
-    if (p.splits > 1) {
-        attn::RowArgs<Bf16> g = {};
-        g.s = attn::Shape{1, heads, kv_heads, M, 0, d, 1, scale};
-        g.ptr = row_ptr; g.rows = M; g.splits = p.splits;
-        g.out1 = a.out; g.lse = lse; g.lse_head = 1; g.lse_row = heads;
-        g.part = a.part; g.part_ml = a.part_ml;
-        if (!attn::launch_join<attn::kForward, Bf16, 1>(g, st)) return B2SP_ERR_UNSUPPORTED;
+    a.part = reinterpret_cast<float *>(ws + p.part);
+    a.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
+    if (nnz) {
+        switch (G) {
+            case 1: launch<1>(a, p.nb, (unsigned)blocks, st); break;
+            case 2: launch<2>(a, p.nb, (unsigned)blocks, st); break;
+            case 3: launch<3>(a, p.nb, (unsigned)blocks, st); break;
+            default: launch<4>(a, p.nb, (unsigned)blocks, st); break;
+        }
+        attn::launch_behind(kv4_join_kernel, (unsigned)joins, kJoinWarps * 32, st, a);
+    } else {
+        kv4_join_kernel<<<(unsigned)joins, kJoinWarps * 32, 0, st>>>(a);
     }
     return launched();
 }

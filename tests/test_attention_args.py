@@ -18,14 +18,18 @@ def b():
 
 def _problem(b, **other):
     base = dict(batch=2, heads=4, kv_heads=2, M=8, K=16, d=64, patterns=1, scale=0.125, row_ptr=4096, row_ptr_stride=9, col_idx=8192,
-                nnz_stride=32, plan=None, plan_tiles=0)
-    base.update(other)
-    return b._AttentionProblem(**base)
+                nnz_stride=32, plan=0, plan_tiles=0)
+    base.update({k: v or 0 if k in ("row_ptr", "col_idx", "plan") else v for k, v in other.items()})
+    return b._PROBLEM(*base.values())
+
+
+def _heads(b, data, *strides):
+    return b._HEADS(data or 0, *strides)
 
 
 def _forward(b, p, q=None, o=None, lse=4096, ws=1 << 20, ws_bytes=1 << 40, algo=0, fn="b2sp_attention"):
-    rows, kv = b._Heads(1 << 20, 64, 64 * 64, 64 * 64 * 8), b._Heads(1 << 20, 64, 64 * 64, 64 * 64 * 8)
-    return getattr(b.lib, fn)(ctypes.byref(p) if p is not None else None, q or rows, kv, kv, o or rows, lse, ws, ws_bytes, algo, None)
+    rows, kv = _heads(b, 1 << 20, 64, 64 * 64, 64 * 64 * 8), _heads(b, 1 << 20, 64, 64 * 64, 64 * 64 * 8)
+    return getattr(b.lib, fn)(p, q or rows, kv, kv, o or rows, lse, ws, ws_bytes, algo, None)
 
 
 def test_problem_sizes(b):
@@ -34,19 +38,19 @@ def test_problem_sizes(b):
                 dict(patterns=2, row_ptr_stride=8), dict(plan=1 << 20, plan_tiles=-1), dict(plan=(1 << 20) + 8)):
         p = _problem(b, **bad)
         assert _forward(b, p) == INVALID, bad
-        assert b.lib.b2sp_attention_workspace_bytes(ctypes.byref(p), 0) == 0, bad
+        assert b.lib.b2sp_attention_workspace_bytes(p, 0) == 0, bad
     assert _forward(b, None) == INVALID
     assert _forward(b, _problem(b, d=257)) == UNSUPPORTED
 
 
 def test_operands_workspace_and_algo(b):
     p = _problem(b)
-    need = b.lib.b2sp_attention_workspace_bytes(ctypes.byref(p), 0)
+    need = b.lib.b2sp_attention_workspace_bytes(p, 0)
     assert need >= 512 and need % 256 == 0
-    assert _forward(b, p, q=b._Heads(None, 64, 1, 1)) == INVALID
+    assert _forward(b, p, q=_heads(b, None, 64, 1, 1)) == INVALID
     assert _forward(b, p, lse=None) == INVALID
-    for over in (b._Heads(1 << 20, 63, 64 * 64, 64 * 64 * 8), b._Heads(1 << 20, 64, 0, 64 * 64), b._Heads(1 << 20, 64, 64 * 7, 64 * 64),
-                 b._Heads(1 << 20, 64, 64 * 8, 64 * 31)):
+    for over in (_heads(b, 1 << 20, 63, 64 * 64, 64 * 64 * 8), _heads(b, 1 << 20, 64, 0, 64 * 64), _heads(b, 1 << 20, 64, 64 * 7, 64 * 64),
+                 _heads(b, 1 << 20, 64, 64 * 8, 64 * 31)):
         assert _forward(b, p, o=over) == INVALID
     assert _forward(b, p, ws=None) == WORKSPACE
     assert _forward(b, p, ws=(1 << 20) + 128) == WORKSPACE
@@ -55,17 +59,17 @@ def test_operands_workspace_and_algo(b):
     assert _forward(b, p, algo=b.ALGO_TILE) == UNSUPPORTED                                       # fp32
     assert _forward(b, p, algo=b.ALGO_TILE, fn="b2sp_attention_bf16") == UNSUPPORTED             # no plan
     for bad in (dict(d=60), dict(d=136)):
-        assert _forward(b, _problem(b, plan=1 << 20, plan_tiles=1, **bad), o=b._Heads(1 << 20, 136, 136 * 64, 136 * 64 * 8), algo=b.ALGO_TILE,
+        assert _forward(b, _problem(b, plan=1 << 20, plan_tiles=1, **bad), o=_heads(b, 1 << 20, 136, 136 * 64, 136 * 64 * 8), algo=b.ALGO_TILE,
                         fn="b2sp_attention_bf16") == UNSUPPORTED
-    odd = b._Heads((1 << 20) + 2, 64, 64 * 64, 64 * 64 * 8)
+    odd = _heads(b, (1 << 20) + 2, 64, 64 * 64, 64 * 64 * 8)
     assert _forward(b, _problem(b, plan=1 << 20, plan_tiles=1), q=odd, algo=b.ALGO_TILE, fn="b2sp_attention_bf16") == UNSUPPORTED
     # nothing to do: no launch, so this passes without a device
     assert _forward(b, _problem(b, M=0)) == OK
 
 
 def test_backward_needs_a_plan(b):
-    p, x = _problem(b), b._Heads(1 << 20, 64, 64 * 64, 64 * 64 * 8)
-    assert b.lib.b2sp_attention_backward(ctypes.byref(p), x, x, x, x, 4096, x, x, x, x, 1 << 20, 1 << 40, 0, None) == INVALID
+    p, x = _problem(b), _heads(b, 1 << 20, 64, 64 * 64, 64 * 64 * 8)
+    assert b.lib.b2sp_attention_backward(p, x, x, x, x, 4096, x, x, x, x, 1 << 20, 1 << 40, 0, None) == INVALID
 
 
 def test_plan_sizes(b):
@@ -83,8 +87,8 @@ def test_plan_sizes(b):
 
 def _cache(b, G=2, **other):
     base = dict(codes=1 << 20, code_ld=16 * G, code_stride_head=1 << 12, scales=1 << 16, scale_ld=G, scale_stride_head=1 << 8, slots=32)
-    base.update(other)
-    return b._Kv4(**base)
+    base.update({k: v or 0 for k, v in other.items()})
+    return b._KV4(*base.values())
 
 
 def test_kv4_refusals(b):
