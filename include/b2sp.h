@@ -313,7 +313,8 @@ b2sp_status b2sp_attention_backward_bf16(const b2sp_attention_problem *problem, 
  *   scale s = bf16(max |x| / 7) of the group; code = clamp(rint(x / s), -7, 7) + 8 (8 if s = 0), half to even throughout;
  *   halfword g G + c of the codes (g = 0..7, c = 0..G-1) holds elements 32 c + 4 g + {0, 1, 2, 3}, the first in the lowest four bits.
  * A group with a NaN or an infinity gets the scale NaN, and reads as NaN.  codes: 16-byte aligned address and strides.  scales: address a multiple
- * of 4 bytes (8 for G = 4); strides multiples of G elements where G is 2 or 4.
+ * of 4 bytes (8 for G = 4); strides multiples of G elements where G is 2 or 4.  Strides of 2^32 and more (bytes of codes, elements of all else;
+ * b2sp_attention_kv4: a row's of 2^31) are B2SP_ERR_UNSUPPORTED.
  *
  * b2sp_kv4_write quantises X[tokens][heads][d] (ld, stride_head) into the rows `slots` (device, one per token); a slot outside [0, cache
  * slots) is skipped (padding), and of several tokens with one slot the last one's row stays.  Up to 1024 tokens need no workspace.

@@ -477,16 +477,20 @@ def device_status(workspace) -> int:
 # that are fetched once.
 def _ready(device, *others):
     """Raises where tensors are not on `device`, or that is not the current one."""
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a CUDA device")
     for t in others:
         if t.device != device:
             raise ValueError(f"tensors on {device} and {t.device}")
-    if device.type != "cuda":
-        raise ValueError("tensors must be on a CUDA device")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}: "
+    if device.index != _current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{_current_device()}: "
                          "call under torch.cuda.device(...)")
 
 
+try:
+    _current_device = torch._C._cuda_getDevice
+except AttributeError:
+    _current_device = torch.cuda.current_device
 try:
     _capturing = torch._C._cuda_isCurrentStreamCapturing
 except AttributeError:
@@ -614,7 +618,8 @@ def attention(row_ptr, col_idx, q, k, v, scale=None, plan=None, out=None, lse=No
     else:
         _ready(device, out)
     if lse is None:
-        lse = torch.empty(qs[:3], dtype=torch.float32, device=device)
+        n, m = qs[1], qs[2]
+        lse = torch.empty_strided(qs[:3], (n * m, m, 1), dtype=torch.float32, device=device)   # (half the price of torch.empty)
     else:
         _lse(lse, qs[:3])
         _ready(device, lse)
@@ -718,7 +723,7 @@ def kv4_read(slots, codes, scales, d, out=None, dtype=torch.float32):
     c = _kv4(codes, scales, H, d, "")
     T = _slot_list(slots)
     if out is None:
-        out = torch.empty((T, H, d), dtype=dtype, device=device)
+        out = torch.empty_strided((T, H, d), (H * d, d, 1), dtype=dtype, device=device)
     s = out.stride()
     if out.dtype is not dtype:
         raise TypeError(f"out must be {dtype}")
@@ -756,7 +761,7 @@ def attention_kv4(row_ptr, col_idx, q, k_codes, k_scales, v_codes, v_scales, sca
     if out.dtype is not torch.bfloat16 or out.shape != shape or (d > 1 and t[2] != 1):
         raise ValueError("out must be like q, with neighbouring elements along d")
     if lse is None:
-        lse = torch.empty((M, H), dtype=torch.float32, device=device)
+        lse = torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=device)
     else:
         _lse(lse, (M, H))
     _ready(device, row_ptr, col_idx, k_codes, k_scales, v_codes, v_scales, out, lse)

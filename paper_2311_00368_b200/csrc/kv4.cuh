@@ -38,10 +38,16 @@ struct Div {
     __device__ __forceinline__ unsigned operator()(unsigned n) const { return (__umulhi(n, m) + n) >> s; }
 };
 
+// i * a + j * b
+__device__ __forceinline__ unsigned long long offset(unsigned i, unsigned a, unsigned j, unsigned b)
+{
+    return (unsigned long long)i * a + (unsigned long long)j * b;
+}
+
 // Slots that several tokens name take the last one's row.  Up to kScanTokens tokens a CTA of the writing kernel compares its tokens' slots
 // with those of all later tokens; more go through an owner per slot in the workspace (two small launches ahead of the writing one: the owners of
 // the slots named become -1, then the largest token): 16384 tokens cost 4 us this way, and the comparisons would be 1.3e8.
-constexpr int kScanTokens = 1024, kWriteThreads = 256;
+constexpr int kScanTokens = 1024, kWriteThreads = 256, kWritePieces = 4;
 
 __global__ void __launch_bounds__(256) kv4_disown_kernel(const int *slots, int tokens, int cache_slots, int *owner)
 {
@@ -100,30 +106,54 @@ template <typename T, int V> __device__ __forceinline__ void store8(T *row, int 
 
 struct RowsArgs {
     int tokens, heads, d, G;
-    long long ld, sh;        // of the rows in 16 or 32 bits
+    unsigned ld, sh;         // of the rows in 16 or 32 bits (all strides below 2^32: a product with an index is one instruction)
     const int *slots;
-    Cache c;
+    uint8_t *codes;          // as in Cache
+    Bf16 *scales;
+    unsigned code_ld, code_head, scale_ld, scale_head;
+    int cache_slots;
     Div by_head, by_piece;   // divisors: heads, and the pieces of a row that threads take (write: 4 G quarters of groups; read: ceil(d / 8))
-    unsigned first;          // (token, head) rows of earlier launches
+    unsigned first;          // read: (four tokens, head) rows of earlier launches
     int *owner;              // write: NULL with few tokens
 };
 
-// Four lanes per group, eight elements each.  What bounds it is memory: 2 d bytes in, 18 G out; one thread per 16 bytes in flight.
+__device__ __forceinline__ unsigned max_nan2(unsigned a, unsigned b)   // of two bf16; a NaN stays one
+{
+    unsigned r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Four lanes per group, eight elements each.  Bound by instructions next to memory (2 d bytes in, 18 G out), so bfloat16 rows have a way of
+// their own: the largest element is found on pairs, and eight divisions become multiplications by 1 / s.  Rounding x (1 / s) to a whole number r
+// by adding 1.5 * 2^23 gives what rounding x / s gives, unless x / s lies halfway between whole numbers: x and s have eight significant bits, so x / s
+// is either exactly halfway or at least 2^-10 of itself away from there, far more than the error of x (1 / s).  Halfway, x - r s is
+// exactly half of s, and r is made even.  Scales near the ends of the exponent range take the divisions.
+// With many tokens a thread takes the same piece of four neighbouring tokens, so that the loads of all of them are in flight at once.
 template <typename T, int V, bool SCAN>
 __global__ void __launch_bounds__(kWriteThreads) kv4_write_kernel(const T *x, const RowsArgs a)
 {
+    constexpr int N = SCAN ? 1 : kWritePieces;
     __shared__ int gone[kWriteThreads / 4];   // SCAN: which of the CTA's tokens a later one replaces
-    const unsigned u = blockIdx.x * (unsigned)kWriteThreads + threadIdx.x;
-    const unsigned row = a.by_piece(u), piece = u - row * a.by_piece.d, t = a.by_head(row), h = row - t * a.by_head.d;
-    const bool on = t < (unsigned)a.tokens;
-    const int slot = on ? a.slots[t] : -1;
-    const int grp = piece >> 2, j = piece & 3;
-    const bool live = (unsigned)slot < (unsigned)a.c.slots;
+    constexpr bool PAIRS = sizeof(T) == 2 && V == 8;
+    const unsigned u0 = blockIdx.x * (unsigned)kWriteThreads, u = u0 + threadIdx.x, row = a.by_piece(u), piece = u - row * a.by_piece.d;
+    const unsigned tn = a.by_head(row), h = row - tn * a.by_head.d, t = tn * N;
+    const int e = (int)piece * 8, grp = piece >> 2, j = piece & 3;
+    const T *from = x + (offset(t, a.ld, h, a.sh) + e);
+    int slot[N], owner[N];
+    uint4 raw[N];
     float v[8] = {};
-    if (live) load8<T, V>(x + (long long)t * a.ld + (long long)h * a.sh, grp * 32 + j * 8, a.d, v);
-    const unsigned t0 = a.by_head(a.by_piece(blockIdx.x * (unsigned)kWriteThreads));
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const bool on = t + k < (unsigned)a.tokens;
+        slot[k] = on ? a.slots[t + k] : -1;
+        raw[k] = make_uint4(0, 0, 0, 0);
+        if constexpr (PAIRS) {
+            if (on && e < a.d) raw[k] = *reinterpret_cast<const uint4 *>(from + (unsigned long long)k * a.ld);
+        }
+    }
     if (SCAN) {
-        const unsigned t1 = min((unsigned)a.tokens - 1, a.by_head(a.by_piece(blockIdx.x * (unsigned)kWriteThreads + kWriteThreads - 1)));
+        const unsigned t0 = a.by_head(a.by_piece(u0)), t1 = min((unsigned)a.tokens - 1, a.by_head(a.by_piece(u0 + kWriteThreads - 1)));
         if (threadIdx.x < kWriteThreads / 4) gone[threadIdx.x] = 0;
         __syncthreads();
         for (unsigned k = t0 + 1 + threadIdx.x; k < (unsigned)a.tokens; k += kWriteThreads) {
@@ -132,64 +162,127 @@ __global__ void __launch_bounds__(kWriteThreads) kv4_write_kernel(const T *x, co
                 if (a.slots[i] == s) gone[i - t0] = 1;
         }
         __syncthreads();
-    }
-    float top = 0.f;
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        top = fmaxf(top, fabsf(v[i]));
-        odd |= !(fabsf(v[i]) <= 3.402823466e38f);
-    }
-    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-    odd = __ballot_sync(~0u, odd) >> (threadIdx.x & 28) & 15;
-    Bf16 s;
-    attn::narrow(__fdiv_rn(top, 7.f), s);
-    if (odd) s.bits = 0x7fff;
-    const float f = attn::widen(s);
-    unsigned word[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float q = f > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(v[i], f)), -7.f), 7.f) : 0.f;
-        word[i >> 2] |= (unsigned)((int)q + 8) << (4 * (i & 3));
-    }
-    bool keep = live;
-    if (SCAN) {
-        keep = live && !gone[t - t0];
+        owner[0] = (unsigned)slot[0] < (unsigned)a.cache_slots && gone[t - t0] == 0 ? (int)t : -1;
     } else {
         asm volatile("griddepcontrol.wait;" ::: "memory");   // the owners
-        if (live) keep = a.owner[slot] == (int)t;
+#pragma unroll
+        for (int k = 0; k < N; ++k) owner[k] = (unsigned)slot[k] < (unsigned)a.cache_slots ? a.owner[slot[k]] : -1;
     }
-    if (!keep) return;
-    unsigned short *codes = reinterpret_cast<unsigned short *>(a.c.codes + (long long)h * a.c.code_head + (long long)slot * a.c.code_ld);
-    codes[(2 * j) * a.G + grp] = (unsigned short)word[0];
-    codes[(2 * j + 1) * a.G + grp] = (unsigned short)word[1];
-    if (j == 0) a.c.scales[(long long)h * a.c.scale_head + (long long)slot * a.c.scale_ld + grp] = s;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const unsigned w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+        float top = 0.f;
+        bool odd = false;   // a NaN or an infinity in the group
+        if constexpr (PAIRS) {
+            unsigned m = max_nan2(max_nan2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_nan2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+            m = max_nan2(m, __shfl_xor_sync(~0u, m, 1));
+            m = max_nan2(m, __shfl_xor_sync(~0u, m, 2));
+            m = max_nan2(m, m >> 16);
+            top = __uint_as_float(m << 16);
+            odd = !(top <= 3.402823466e38f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        } else {
+            if (t + k < (unsigned)a.tokens) load8<T, V>(from - e + (unsigned long long)k * a.ld, e, a.d, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                top = fmaxf(top, fabsf(v[i]));
+                odd |= !(fabsf(v[i]) <= 3.402823466e38f);
+            }
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+            odd = __ballot_sync(~0u, odd) >> (threadIdx.x & 28) & 15;
+        }
+        Bf16 s;
+        attn::narrow(__fdiv_rn(top, 7.f), s);
+        if (odd) s.bits = 0x7fff;
+        const float f = attn::widen(s);
+        unsigned word[2] = {0, 0};
+        bool divide = true;
+        if (PAIRS) {
+            const float inv = __frcp_rn(f), half = 0.5f * f;
+            divide = !(f > 1e-30f && f < 1e30f);
+            // on pairs: y = x / s + 1.5 * 2^23 rounded, minus = -r, rest = x - r s
+            const uint64_t magic = attn::two(12582912.f, 12582912.f), by = attn::two(inv, inv), s2 = attn::two(f, f), neg = attn::two(-1.f, -1.f);
+            float y[8], rest[8];
+            bool halfway = false;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const uint64_t x2 = attn::two(v[i], v[i + 1]), y2 = attn::fma2(x2, by, magic), minus = attn::fma2(y2, neg, magic);
+                attn::split(y2, y[i], y[i + 1]);
+                attn::split(attn::fma2(minus, s2, x2), rest[i], rest[i + 1]);
+                halfway |= fabsf(rest[i]) == half || fabsf(rest[i + 1]) == half;
+            }
+            if (halfway) {   // (one thread in a hundred) r is made even
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (fabsf(rest[i]) == half && (__float_as_uint(y[i]) & 1)) y[i] += copysignf(1.f, rest[i]);
+            }
+#pragma unroll
+            for (int i = 7; i >= 0; --i) word[i >> 2] = word[i >> 2] * 16 + (__float_as_uint(y[i]) & 15);
+            word[0] ^= 0x8888u;   // two's complement to offset by 8
+            word[1] ^= 0x8888u;
+        }
+        if (divide) {
+            word[0] = word[1] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = f > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(v[i], f)), -7.f), 7.f) : 0.f;
+                word[i >> 2] |= (unsigned)((int)q + 8) << (4 * (i & 3));
+            }
+        }
+        if (owner[k] >= 0 && owner[k] == (int)(t + k)) {
+            unsigned short *codes = reinterpret_cast<unsigned short *>(a.codes + offset(h, a.code_head, slot[k], a.code_ld)) + (2 * j * a.G + grp);
+            codes[0] = (unsigned short)word[0];
+            codes[a.G] = (unsigned short)word[1];
+            if (j == 0) a.scales[offset(h, a.scale_head, slot[k], a.scale_ld) + grp] = s;
+        }
+    }
 }
 
-// A thread per eight elements of the output; rows of slots outside the cache read as zeros.
+// A thread takes the same eight elements of four neighbouring tokens, so that the loads of all of them are in flight (slots, then codes and
+// scales); rows of slots outside the cache read as zeros.
+constexpr int kReadTokens = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const RowsArgs a, T *out)
 {
-    const unsigned u = blockIdx.x * 256u + threadIdx.x;
-    unsigned row = a.by_piece(u);
-    const int e = (int)(u - row * a.by_piece.d), grp = e >> 2, j = e & 3;
-    row += a.first;
-    const unsigned t = a.by_head(row), h = row - t * a.by_head.d;
-    if (t >= (unsigned)a.tokens) return;
-    const int slot = a.slots[t];
-    float v[8] = {};
-    if ((unsigned)slot < (unsigned)a.c.slots) {
-        const unsigned short *codes = reinterpret_cast<const unsigned short *>(a.c.codes + (long long)h * a.c.code_head + (long long)slot * a.c.code_ld);
-        const unsigned w0 = codes[(2 * j) * a.G + grp], w1 = codes[(2 * j + 1) * a.G + grp];
-        const float s = attn::widen(a.c.scales[(long long)h * a.c.scale_head + (long long)slot * a.c.scale_ld + grp]);
+    const unsigned u = blockIdx.x * 256u + threadIdx.x, row = a.by_piece(u);
+    const unsigned tn = a.by_head(row + a.first), h = row + a.first - tn * a.by_head.d, t = tn * kReadTokens;
+    const int e = (int)(u - row * a.by_piece.d), grp = e >> 2, j = e & 3, at = 2 * j * a.G + grp;
+    unsigned w0[kReadTokens], w1[kReadTokens];
+    int slot[kReadTokens];
+    float s[kReadTokens];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = s * (float)((int)(w0 >> (4 * i) & 15) - 8);
-            v[4 + i] = s * (float)((int)(w1 >> (4 * i) & 15) - 8);
+    for (int k = 0; k < kReadTokens; ++k) slot[k] = t + k < (unsigned)a.tokens ? a.slots[t + k] : -1;
+    const uint8_t *codes = a.codes + (unsigned long long)h * a.code_head;
+    const Bf16 *scales = a.scales + ((unsigned long long)h * a.scale_head + grp);
+#pragma unroll
+    for (int k = 0; k < kReadTokens; ++k) {
+        w0[k] = w1[k] = 0x8888u;
+        s[k] = 0.f;
+        if ((unsigned)slot[k] < (unsigned)a.cache_slots) {
+            const unsigned short *c = reinterpret_cast<const unsigned short *>(codes + (unsigned long long)(unsigned)slot[k] * a.code_ld) + at;
+            w0[k] = c[0];
+            w1[k] = c[a.G];
+            s[k] = attn::widen(scales[(unsigned long long)(unsigned)slot[k] * a.scale_ld]);
         }
     }
-    store8<T, V>(out + (long long)t * a.ld + (long long)h * a.sh, e * 8, a.d, v);
+    T *to = out + offset(t, a.ld, h, a.sh);
+#pragma unroll
+    for (int k = 0; k < kReadTokens; ++k) {
+        if (t + k >= (unsigned)a.tokens) break;
+        // a nibble below the exponent of 2^23 is 2^23 + code
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = s[k] * (__uint_as_float((w0[k] >> (4 * i) & 15) | 0x4b000000u) - 8388616.f);
+            v[4 + i] = s[k] * (__uint_as_float((w1[k] >> (4 * i) & 15) | 0x4b000000u) - 8388616.f);
+        }
+        store8<T, V>(to + (unsigned long long)k * a.ld, e * 8, a.d, v);
+    }
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------

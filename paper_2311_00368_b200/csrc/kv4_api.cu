@@ -29,6 +29,10 @@ b2sp_status check_written(const b2sp_kv4 *c, int heads, int G)
             return B2SP_ERR_INVALID_ARG;
     return B2SP_OK;
 }
+bool below_32_bits(const b2sp_kv4 *c, long long ld, long long sh)
+{
+    return std::max({c->code_ld, c->code_stride_head, c->scale_ld, c->scale_stride_head, ld, sh}) <= (long long)UINT_MAX;
+}
 Cache cache(const b2sp_kv4 *c)
 {
     return Cache{static_cast<uint8_t *>(c->codes), static_cast<Bf16 *>(c->scales), c->code_ld, c->code_stride_head, c->scale_ld, c->scale_stride_head, c->slots};
@@ -37,7 +41,14 @@ template <typename T> bool eights(const T *p, long long ld, long long sh, int d)
 {
     return ((reinterpret_cast<uintptr_t>(p) & 15) | (uintptr_t)(ld & 7) | (uintptr_t)(sh & 7) | (uintptr_t)(d & 7)) == 0;
 }
-constexpr int kMost = 0x7fffff00;   // threads of a launch (indices stay below 2^31)
+constexpr int kMost = 0x7fff0000;   // pieces of a launch (indices stay below 2^31)
+
+RowsArgs rows_args(int tokens, int heads, int d, long long ld, long long sh, const int *slots, const b2sp_kv4 *c, unsigned pieces, unsigned first, int *owner)
+{
+    return RowsArgs{tokens, heads, d, (d + 31) / 32, (unsigned)ld, (unsigned)sh, slots, static_cast<uint8_t *>(c->codes), static_cast<Bf16 *>(c->scales),
+                    (unsigned)c->code_ld, (unsigned)c->code_stride_head, (unsigned)c->scale_ld, (unsigned)c->scale_stride_head, c->slots,
+                    Div(heads), Div(pieces), first, owner};
+}
 
 size_t write_bytes(int tokens, int slots) { return tokens <= kScanTokens ? 0 : (size_t)slots * 4; }
 
@@ -51,13 +62,14 @@ b2sp_status write(int tokens, int heads, int d, const T *X, long long ld, long l
     b2sp_status rc = check_cache(c, heads, G);
     if (rc == B2SP_OK) rc = check_written(c, heads, G);
     if (rc != B2SP_OK) return rc;
-    const long long threads = (long long)tokens * heads * G * 4;
-    if (d > 32 * 1024 || threads > kMost) return B2SP_ERR_UNSUPPORTED;
+    const int each = tokens <= kScanTokens ? 1 : kWritePieces;
+    const long long threads = ((long long)tokens + each - 1) / each * heads * G * 4;
+    if (d > 32 * 1024 || threads > kMost || !below_32_bits(c, ld, sh)) return B2SP_ERR_UNSUPPORTED;
     const size_t need = write_bytes(tokens, c->slots);
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return B2SP_ERR_WORKSPACE;
     if (c->slots == 0 || tokens == 0) return B2SP_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    RowsArgs a = {tokens, heads, d, G, ld, sh, slots, cache(c), Div(heads), Div(4 * G), 0, static_cast<int *>(workspace)};
+    const RowsArgs a = rows_args(tokens, heads, d, ld, sh, slots, c, 4 * G, 0, static_cast<int *>(workspace));
     const unsigned blocks = (unsigned)((threads + kWriteThreads - 1) / kWriteThreads);
     const bool wide = eights(X, ld, sh, d);
     if (tokens <= kScanTokens) {
@@ -84,11 +96,12 @@ b2sp_status read(int tokens, int heads, int d, const int *slots, const b2sp_kv4 
     if (rc != B2SP_OK) return rc;
     if (tokens > 1 && heads > 1 && std::max(ld, sh) < std::min(ld, sh) * ((ld < sh ? tokens : heads) - 1ll) + d) return B2SP_ERR_INVALID_ARG;
     if ((tokens > 1 && ld < d) || (heads > 1 && sh < d)) return B2SP_ERR_INVALID_ARG;
+    if (!below_32_bits(c, ld, sh)) return B2SP_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const unsigned pieces = (unsigned)((d + 7) / 8), most = (unsigned)kMost / pieces;
     const bool wide = eights(X, ld, sh, d);
-    for (unsigned first = 0, rows = (unsigned)((long long)tokens * heads); first < rows; first += std::min(most, rows - first)) {
-        const RowsArgs a = {tokens, heads, d, G, ld, sh, slots, cache(c), Div(heads), Div(pieces), first, nullptr};
+    for (unsigned first = 0, rows = (unsigned)(((long long)tokens + kReadTokens - 1) / kReadTokens * heads); first < rows; first += std::min(most, rows - first)) {
+        const RowsArgs a = rows_args(tokens, heads, d, ld, sh, slots, c, pieces, first, nullptr);
         const unsigned blocks = (unsigned)(((unsigned long long)std::min(most, rows - first) * pieces + 255) / 256);
         if (wide) kv4_read_kernel<T, 8><<<blocks, 256, 0, st>>>(a, X);
         else kv4_read_kernel<T, 1><<<blocks, 256, 0, st>>>(a, X);

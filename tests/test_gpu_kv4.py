@@ -81,6 +81,26 @@ def test_values_at_the_edges_of_the_format():
     assert torch.isnan(got[4, 0, 32:]).all() and (got[4, 0, :32] == 0).all()
 
 
+def test_every_quotient_of_two_bfloat16():
+    """Rows whose largest element has each eight-bit significand in turn, with elements at and beside every half step of its scale."""
+    b = _binding()
+    tops = (torch.arange(128, 256).float() / 128 * 2.0 ** torch.arange(-3, 5).repeat(16).float()).to(torch.bfloat16)
+    x = torch.zeros((128, 1, 64), dtype=torch.bfloat16)
+    x[:, 0, 0] = tops
+    x[:, 0, 32] = -tops
+    s = (tops.float() / 7).to(torch.bfloat16).float()
+    for i in range(1, 16):
+        half = (s * (i - 0.5) / 2).clamp(max=tops.float())
+        x[:, 0, i] = half.to(torch.bfloat16)
+        x[:, 0, 15 + i] = -((s * (i // 2 + 0.5)).clamp(max=tops.float())).to(torch.bfloat16)
+        x[:, 0, 32 + i] = torch.nextafter((s * (i % 7 + 0.5)).to(torch.bfloat16), torch.tensor(0.0, dtype=torch.bfloat16)).clamp(max=tops)
+        x[:, 0, 47 + i] = (s * (i % 7 + 0.5)).to(torch.bfloat16).clamp(max=tops)
+    codes, scales = b.kv4_cache(1, 128, 64)
+    b.kv4_write(x.cuda(), torch.arange(128, dtype=torch.int32, device="cuda"), codes, scales, dtype=torch.bfloat16)
+    want_c, want_s, _ = quantised(x)
+    assert torch.equal(codes.cpu()[0], want_c[:, 0]) and torch.equal(scales.cpu()[0], want_s[:, 0])
+
+
 def test_slots_outside_and_slots_twice():
     """Slots outside the cache are skipped and read as zeros; of several tokens with one slot the last one stays, across launches too."""
     b = _binding()
