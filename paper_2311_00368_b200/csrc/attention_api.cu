@@ -91,7 +91,7 @@ struct RowPlan {
     size_t stat, ml, part, bytes;         // offsets
     int stat_rows;
 };
-RowPlan row_plan(const Shape &s, long long nnz, bool backward)
+RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles)
 {
     RowPlan r;
     const long long problems = (long long)s.batch * s.heads;
@@ -107,7 +107,7 @@ RowPlan row_plan(const Shape &s, long long nnz, bool backward)
     size_t part = r.splits_m > 1 ? um * part_width(kForward, s.d) * 4 : 0;
     if (backward && r.parts_kv) part = std::max(part, uk * part_width(kGradKV, s.d) * 4);
     r.part = take(part);
-    r.bytes = at;
+    r.bytes = backward ? std::max(at, tiles_backward_bytes(s, tiles, r.ml)) : at;   // (the tile kernels use what lies behind the statistics)
     return r;
 }
 
@@ -153,7 +153,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
         return rc;
     if (p->M && !lse) return B2SP_ERR_INVALID_ARG;
     const Shape s = shape(p);
-    const RowPlan w = row_plan(s, p->nnz_stride, false);
+    const RowPlan w = row_plan(s, p->nnz_stride, false, p->plan_tiles);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < w.bytes) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
@@ -207,7 +207,7 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         return rc;
     if (p->M && !lse) return B2SP_ERR_INVALID_ARG;
     const Shape s = shape(p);
-    const RowPlan w = row_plan(s, p->nnz_stride, true);
+    const RowPlan w = row_plan(s, p->nnz_stride, true, p->plan_tiles);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < w.bytes) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
@@ -216,8 +216,8 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
     const Plan plan = plan_view(p->plan, plan_layout(s.patterns, s.M, s.K, p->nnz_stride, p->plan_tiles));
     bool tiles = false;
     if constexpr (sizeof(T) == 2) {
-        const View<const T> ops[7] = {view<const T>(Q), view<const T>(K), view<const T>(V), view<const T>(dO), view<const T>(dQ), view<const T>(dK), view<const T>(dV)};
-        const bool can = s.M > 0 && s.K > 0 && tiles_possible(s, ops, 7);
+        const View<const T> ops[8] = {view<const T>(Q), view<const T>(K), view<const T>(V), view<const T>(O), view<const T>(dO), view<const T>(dQ), view<const T>(dK), view<const T>(dV)};
+        const bool can = s.M > 0 && s.K > 0 && tiles_possible(s, ops, 8);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
         tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true)));
     } else if (algo == B2SP_ALGO_TILE) {
@@ -225,6 +225,21 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
     }
     g_algo[1] = tiles ? B2SP_ALGO_TILE : B2SP_ALGO_ROW;
     float2 *stat = reinterpret_cast<float2 *>(ws + w.stat);
+    if constexpr (sizeof(T) == 2) {
+        if (tiles) {
+            TileCall c = {};
+            c.s = s;
+            c.plan = plan;
+            c.tiles = p->plan_tiles;
+            c.row_ptr = p->row_ptr; c.col_idx = p->col_idx; c.row_ptr_stride = p->row_ptr_stride; c.nnz_stride = p->nnz_stride;
+            c.q = view<const T>(Q); c.k = view<const T>(K); c.v = view<const T>(V); c.dout = view<const T>(dO);
+            c.o = view<const T>(O); c.lse = const_cast<float *>(lse); c.workspace = workspace; c.scratch_at = w.ml;
+            c.dq = view<T>(dQ); c.dk = view<T>(dK); c.dv = view<T>(dV);
+            c.stat = stat; c.stat_stride = w.stat_rows;
+            c.status = reinterpret_cast<int *>(ws + 256);
+            return tiles_backward(c, st, &launches);
+        }
+    }
     if (s.M) {
         const View<const T> o = view<const T>(O), d = view<const T>(dO);
         const long long blocks = ((long long)s.batch * s.heads * w.stat_rows + 7) / 8;
@@ -234,20 +249,6 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         else attention_stat_kernel<T, 1><<<(unsigned)blocks, 256, 0, st>>>(s, o, d, lse, w.stat_rows, stat, status);
         ++launches;
         if ((rc = launched()) != B2SP_OK) return rc;
-    }
-    if constexpr (sizeof(T) == 2) {
-        if (tiles) {
-            TileCall c = {};
-            c.s = s;
-            c.plan = plan;
-            c.tiles = p->plan_tiles;
-            c.row_ptr = p->row_ptr; c.col_idx = p->col_idx; c.row_ptr_stride = p->row_ptr_stride; c.nnz_stride = p->nnz_stride;
-            c.q = view<const T>(Q); c.k = view<const T>(K); c.v = view<const T>(V); c.dout = view<const T>(dO);
-            c.dq = view<T>(dQ); c.dk = view<T>(dK); c.dv = view<T>(dV);
-            c.stat = stat; c.stat_stride = w.stat_rows;
-            c.status = reinterpret_cast<int *>(ws + 256);
-            return tiles_backward(c, st, &launches);
-        }
     }
     RowArgs<T> g = {};
     g.s = s;
@@ -347,7 +348,7 @@ extern "C" b2sp_status b2sp_attention_plan_status(const void *plan, void *stream
 extern "C" size_t b2sp_attention_workspace_bytes(const b2sp_attention_problem *p, int backward)
 {
     if (check_problem(p) != B2SP_OK) return 0;
-    return row_plan(shape(p), p->nnz_stride, backward != 0).bytes;
+    return row_plan(shape(p), p->nnz_stride, backward != 0, p->plan_tiles).bytes;
 }
 
 extern "C" b2sp_status b2sp_attention(const b2sp_attention_problem *p, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V, const b2sp_heads *O,

@@ -109,7 +109,7 @@ template <typename T> struct RowArgs {
     long long ptr_stride, idx_stride;
     View<const T> q, k, v, dout;
     View<T> out1, out2;                   // O / dQ / dK and dV
-    const float2 *stat;                   // backward: (lse log2(e), delta) of each row, `stat_stride` rows a problem
+    const float2 *stat;                   // backward: (-lse log2(e), -delta) of each row, `stat_stride` rows a problem
     long long stat_stride;
     float *lse;                           // forward; of (b, h, i): lse[b * heads * M + h * lse_head + i * lse_row]
     long long lse_head, lse_row;
@@ -213,8 +213,8 @@ template <int MODE, typename T, int V, int DW> struct RowWork {
                     for (int k = 0; k < 4; ++k) acc1[u][k] *= fall;
                 w1 = p;
             } else {
-                p = lane < n ? exp2f(fmaf(s, c2, -st.x)) : 0.f;
-                w1 = lane < n ? p * (dp - st.y) : 0.f;
+                p = lane < n ? exp2f(fmaf(s, c2, st.x)) : 0.f;
+                w1 = lane < n ? p * (dp + st.y) : 0.f;
                 w2 = p;
             }
             const int group = HALVES == 2 ? lane >> 4 : 0, col = (HALVES == 2 ? lane & 15 : lane) * 4;
@@ -413,8 +413,8 @@ template <int MODE, typename T, int V> inline bool launch_join(const RowArgs<T> 
     return true;
 }
 
-// The backward pass's row statistics: (lse log2(e), dO_i.O_i), a warp per row, `stat_rows` rows a problem.  A row without entries
-// (lse = -inf) and the rows behind the last one get (+inf, 0): exp2(s - inf) = 0, they weigh nothing.
+// The backward pass's row statistics: (-lse log2(e), -dO_i.O_i), a warp per row, `stat_rows` rows a problem.  A row without entries
+// (lse = -inf) and the rows behind the last one get (-inf, 0): exp2(s - inf) = 0, they weigh nothing.
 template <typename T, int V>
 __global__ void __launch_bounds__(256) attention_stat_kernel(Shape s, View<const T> out, View<const T> dout, const float *lse, int stat_rows, float2 *stat, int *status)
 {
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(256) attention_stat_kernel(Shape s, View<const
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    if (lane == 0) stat[unit] = top == -CUDART_INF_F ? make_float2(CUDART_INF_F, 0.f) : make_float2(top * kLog2e, sum);
+    if (lane == 0) stat[unit] = top == -CUDART_INF_F ? make_float2(-CUDART_INF_F, 0.f) : make_float2(-top * kLog2e, -sum);
 }
 
 }  // namespace attn

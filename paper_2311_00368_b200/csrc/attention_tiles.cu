@@ -10,6 +10,8 @@ namespace b2sp {
 namespace attn {
 namespace {
 
+constexpr int kSMs = 148;
+
 using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                    const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn encode_fn()
@@ -53,6 +55,22 @@ template <class K> bool allow_smem(K *kernel, int bytes, std::atomic<unsigned lo
     return true;
 }
 
+template <class... KArgs, class... Args>
+void launch_behind_smem(void (*kern)(KArgs...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, const Args &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 TileArgs args(const TileCall &c)
 {
     TileArgs a = {};
@@ -84,27 +102,83 @@ template <int DP> b2sp_status forward(const TileCall &c, cudaStream_t st, int *l
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
 
+// How the backward pass is dealt out: shares of tiles for dQ (0) and for dK and dV (1), and where things lie in the workspace.
+struct GradPlan {
+    long long tiles[2];
+    int outers[2], NB[2], share[2], ctas[2];
+    size_t starts[2], bad[2], part, bytes;   // offsets from `at`
+};
+GradPlan grad_plan(const Shape &s, long long tiles, size_t at)
+{
+    GradPlan p;
+    const int DP = s.d <= 64 ? 64 : 128;
+    size_t part = 0;
+    for (int k = 0; k < 2; ++k) {
+        p.tiles[k] = tiles * ((long long)s.batch * s.heads / s.patterns);
+        p.outers[k] = s.batch * (k == 0 ? s.heads : s.kv_heads);
+        p.NB[k] = ((k == 0 ? s.M : s.K) + kTile - 1) / kTile;
+        p.share[k] = (int)std::max(1ll, (p.tiles[k] + kSMs - 1) / kSMs);
+        p.ctas[k] = (int)((p.tiles[k] + p.share[k] - 1) / p.share[k]);
+        p.starts[k] = at;
+        at += up256((size_t)p.ctas[k] * 16);
+        p.bad[k] = at;
+        at += up256((size_t)p.outers[k] * p.NB[k] * 4);
+        part = std::max(part, (size_t)p.ctas[k] * 2 * (k + 1) * kTile * DP * 4);
+    }
+    p.part = at;
+    p.bytes = at + up256(part);
+    return p;
+}
+
+template <int MODE, int DP> b2sp_status grad(const TileCall &c, const GradPlan &p, GradArgs g, cudaStream_t st, int *launches)
+{
+    static std::atomic<unsigned long long> done{0};
+    using C = GradCfg<MODE, DP>;
+    const Shape &s = c.s;
+    CUtensorMap x1, x2, y1, y2;
+    const bool q = MODE == kDq;
+    const int box_q = q ? 128 : 64, box_k = q ? 64 : 128;
+    if (!make_map(q ? &x1 : &y1, c.q, s.batch, s.heads, s.M, s.d, box_q, &g.a.q) || !make_map(q ? &x2 : &y2, c.dout, s.batch, s.heads, s.M, s.d, box_q, &g.a.dout) ||
+        !make_map(q ? &y1 : &x1, c.k, s.batch, s.kv_heads, s.K, s.d, box_k, &g.a.k) || !make_map(q ? &y2 : &x2, c.v, s.batch, s.kv_heads, s.K, s.d, box_k, &g.a.v) ||
+        !allow_smem(tile_grad_kernel<MODE, DP>, C::BYTES, done))
+        return B2SP_ERR_CUDA;
+    if (g.ctas) {
+        launch_behind_smem(tile_grad_kernel<MODE, DP>, (unsigned)g.ctas, C::THREADS, C::BYTES, st, x1, x2, y1, y2, g);
+        ++*launches;
+    }
+    launch_behind(tile_grad_join_kernel<MODE, DP>, (unsigned)(p.outers[MODE] * p.NB[MODE] * (kTile / kJoinRows)), 256, st, g);
+    ++*launches;
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
+}
+
 template <int DP> b2sp_status backward(const TileCall &c, cudaStream_t st, int *launches)
 {
-    static std::atomic<unsigned long long> done_q{0}, done_kv{0};
-    TileArgs a = args(c);
-    CUtensorMap q, o, k, v;
     const Shape &s = c.s;
-    if (!allow_smem(tile_dq_kernel<DP>, DqCfg<DP>::BYTES, done_q) || !allow_smem(tile_dkv_kernel<DP>, DkvCfg<DP>::BYTES, done_kv)) return B2SP_ERR_CUDA;
-    const long long qb = (long long)s.batch * s.heads * c.plan.RB, kb = (long long)s.batch * s.kv_heads * c.plan.CB;
-    if (qb > INT_MAX || kb > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    if (!make_map(&q, c.q, s.batch, s.heads, s.M, s.d, 128, &a.q) || !make_map(&o, c.dout, s.batch, s.heads, s.M, s.d, 128, &a.dout) ||
-        !make_map(&k, c.k, s.batch, s.kv_heads, s.K, s.d, 64, &a.k) || !make_map(&v, c.v, s.batch, s.kv_heads, s.K, s.d, 64, &a.v))
-        return B2SP_ERR_CUDA;
-    a.g.out1 = c.dq; a.g.rows = s.M;
-    tile_dq_kernel<DP><<<(unsigned)qb, kTileThreads, DqCfg<DP>::BYTES, st>>>(q, o, k, v, a);
-    if (!make_map(&q, c.q, s.batch, s.heads, s.M, s.d, 64, &a.q) || !make_map(&o, c.dout, s.batch, s.heads, s.M, s.d, 64, &a.dout) ||
-        !make_map(&k, c.k, s.batch, s.kv_heads, s.K, s.d, 128, &a.k) || !make_map(&v, c.v, s.batch, s.kv_heads, s.K, s.d, 128, &a.v))
-        return B2SP_ERR_CUDA;
-    a.g.out1 = c.dk; a.g.out2 = c.dv; a.g.rows = s.K;
-    tile_dkv_kernel<DP><<<(unsigned)kb, DkvCfg<DP>::THREADS, DkvCfg<DP>::BYTES, st>>>(q, o, k, v, a);
-    *launches += 2;
-    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
+    const GradPlan p = grad_plan(s, c.tiles, c.scratch_at);
+    char *ws = static_cast<char *>(c.workspace);
+    if ((long long)p.outers[0] * p.NB[0] > INT_MAX / 4 || (long long)p.outers[1] * p.NB[1] > INT_MAX / 4) return B2SP_ERR_UNSUPPORTED;
+    GradArgs g[2] = {};
+    ShareArgs h = {};
+    for (int k = 0; k < 2; ++k) {
+        g[k].a = args(c);
+        g[k].w = Tiles{k == 0 ? c.plan.rb_ptr : c.plan.cb_ptr, p.NB[k], k == 0 ? s.heads : s.kv_heads, k == 0 ? 1 : s.heads / s.kv_heads, s.patterns, s.batch, s.heads, p.outers[k]};
+        g[k].tile_at = k == 0 ? c.plan.tile_cb : reinterpret_cast<const int *>(c.plan.ctile);
+        g[k].share = p.share[k]; g[k].ctas = p.ctas[k]; g[k].tiles = p.tiles[k];
+        g[k].starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
+        g[k].bad = reinterpret_cast<int *>(ws + p.bad[k]);
+        g[k].part = reinterpret_cast<float *>(ws + p.part);
+        h.w[k] = g[k].w; h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.blocks[k] = p.outers[k] * p.NB[k];
+        h.starts[k] = reinterpret_cast<int4 *>(ws + p.starts[k]); h.bad[k] = g[k].bad;
+    }
+    g[0].a.g.out1 = c.dq; g[0].a.g.rows = s.M;
+    g[1].a.g.out1 = c.dk; g[1].a.g.out2 = c.dv; g[1].a.g.rows = s.K;
+    const long long rows = (long long)s.batch * s.heads * c.stat_stride, blocks = (rows + 15) / 16;
+    const int share_blocks = (std::max(1, std::max(p.ctas[0] + p.ctas[1], std::max(h.blocks[0], h.blocks[1]))) + 255) / 256;
+    if (blocks + share_blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    tile_grad_stat_kernel<><<<(unsigned)(blocks + share_blocks), 256, 0, st>>>(s, c.o, c.dout, c.lse, (int)c.stat_stride, const_cast<float2 *>(c.stat), h, share_blocks, c.status);
+    ++*launches;
+    const b2sp_status rc = grad<kDq, DP>(c, p, g[0], st, launches);
+    return rc == B2SP_OK ? grad<kDkv, DP>(c, p, g[1], st, launches) : rc;
 }
 
 }  // namespace
@@ -122,6 +196,10 @@ bool tiles_possible(const Shape &s, const View<const Bf16> *views, int n)
     return true;
 }
 
+size_t tiles_backward_bytes(const Shape &s, long long tiles, size_t at)
+{
+    return s.d <= kMaxTileHeadDim ? grad_plan(s, tiles, at).bytes : at;
+}
 b2sp_status tiles_forward(const TileCall &c, cudaStream_t st, int *launches)
 {
     return c.s.d <= 64 ? forward<64>(c, st, launches) : forward<128>(c, st, launches);

@@ -39,6 +39,31 @@ struct TileArgs {
     int *status;
 };
 
+// Bounded wait, asking again and again: the waits here are a few hundred cycles each and on the critical path of a step, and a try_wait
+// that may be parked for longer (ptx::mbar_wait) wakes late.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity)
+{
+    {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    uint64_t t0 = 0;
+    for (uint32_t round = 0;; ++round) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+            uint32_t ok;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+            if (ok) return true;
+        }
+        const uint64_t t = ptx::global_timer_ns();
+        if (round == 0) t0 = t;
+        if (t - t0 > ptx::c_wait_limit_ns || round > (1u << 22)) return false;
+    }
+}
+
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1, int c2, int c3)
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -54,15 +79,25 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int N, bool b_along_n)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((b_along_n ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// Descriptors of shared-memory operands come as their lower halves (the upper one is the same for all): steps along an operand are
+// 32-bit additions.
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | ptx::kLayoutSw128 << 29;   // eight rows 1024 bytes apart, version 1, 128-byte swizzle
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tmov.b64 y, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 // After tmem_ld_wait(): nothing that uses the loaded registers moves in front of the wait.
 __device__ __forceinline__ void settle(uint32_t (&x)[32])
@@ -70,15 +105,29 @@ __device__ __forceinline__ void settle(uint32_t (&x)[32])
     asm volatile("" : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]), "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15]), "+r"(x[16]), "+r"(x[17]), "+r"(x[18]), "+r"(x[19]), "+r"(x[20]), "+r"(x[21]), "+r"(x[22]), "+r"(x[23]), "+r"(x[24]), "+r"(x[25]), "+r"(x[26]), "+r"(x[27]), "+r"(x[28]), "+r"(x[29]), "+r"(x[30]), "+r"(x[31]));
 }
 
-// Operand tiles in shared memory: blocks of 64 columns, each ROWS rows of 128 bytes, 128-byte swizzle.  The same bytes are an operand whose
-// contraction runs along the columns (steps of 16: 32 bytes) or along the rows (steps of 16: 2 KB).
-template <int ROWS> __device__ __forceinline__ uint64_t along_columns(uint32_t base, int step)
+__device__ __forceinline__ void settle(uint32_t (&x)[16])
 {
-    return ptx::smem_desc_sw128(base + (step >> 2) * (ROWS * 128) + (step & 3) * 32, 16, 1024);
+    asm volatile("" : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]), "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15]));
 }
-template <int ROWS> __device__ __forceinline__ uint64_t along_rows(uint32_t base, int step)
+
+// Operand tiles in shared memory: blocks of 64 columns, each ROWS rows of 128 bytes, 128-byte swizzle.  The same bytes are an operand whose
+// contraction runs along the columns (steps of 16: 32 bytes) or along the rows (steps of 16: 2 KB; blocks of 64 columns ROWS * 128 bytes apart).
+__device__ __forceinline__ uint32_t desc_columns(uint32_t base) { return base >> 4 | 1u << 16; }
+template <int ROWS> __device__ __forceinline__ uint32_t desc_rows(uint32_t base) { return base >> 4 | (ROWS * 128u >> 4) << 16; }
+template <int ROWS> __host__ __device__ constexpr uint32_t column_step(int k) { return ((k >> 2) * (ROWS * 128) + (k & 3) * 32) >> 4; }
+__host__ __device__ constexpr uint32_t row_step(int k) { return k * 2048 >> 4; }
+// D = A B^T over DP columns (those behind `ks` steps of 16 are zeros), A 128 rows, B N rows.
+template <int DP, int N> __device__ __forceinline__ void product_columns(uint32_t d, uint32_t a, uint32_t b, int ks)
 {
-    return ptx::smem_desc_sw128(base + step * 2048, ROWS * 128, 1024);
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+        if (k < ks) mma_ss(d, a + column_step<128>(k), b + column_step<N>(k), idesc_bf16(N, false), k > 0);
+}
+// D (+)= A B, A 128 x ROWS in tensor memory (32 elements of a row in 16 columns; the next 32 follow SKIP columns on), B ROWS x DP.
+template <int DP, int ROWS, int SKIP = 16> __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, bool onto)
+{
+#pragma unroll
+    for (int k = 0; k < ROWS / 16; ++k) mma_ts(d, a + (k >> 1) * SKIP + (k & 1) * 8, b + row_step(k), idesc_bf16(DP, true), k > 0 || onto);
 }
 template <int DP, int ROWS> __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *tm, uint32_t bar, int row, int h, int b)
 {
@@ -189,7 +238,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t tmem = ptx::lds32(slot);
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
         return ok;
     };
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
@@ -209,8 +258,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 load_tile<DP, 128>(base + C::V + st * C::TILE, &tm_v, v_full(st), cb * kTile, hkv * a.v.hm, b * a.v.bm);
             }
             if (!ok) {   // copies in flight land before the CTA ends
-                ptx::mbar_wait(q_full, 0);
-                for (int k = max(0, i - C::STAGES); k <= i; ++k) { ptx::mbar_wait(k_full(k % C::STAGES), k / C::STAGES & 1); if (k < i) ptx::mbar_wait(v_full(k % C::STAGES), k / C::STAGES & 1); }
+                wait_for(q_full, 0);
+                for (int k = max(0, i - C::STAGES); k <= i; ++k) { wait_for(k_full(k % C::STAGES), k / C::STAGES & 1); if (k < i) wait_for(v_full(k % C::STAGES), k / C::STAGES & 1); }
             }
         }
         __syncwarp();
@@ -222,19 +271,16 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const int st = i % C::STAGES, ph = i / C::STAGES & 1;
                 if (!wait(k_full(st), ph)) break;
                 // (S of this tile overwrites the weights of the last: the tensor core takes its products in order)
-                for (int k = 0; k < ks; ++k)
-                    mma_ss(tmem + C::COL_S, along_columns<128>(base + C::Q, k), along_columns<128>(base + C::K + st * C::TILE, k), idesc_bf16(128, false), k > 0);
+                product_columns<DP, 128>(tmem + C::COL_S, desc_columns(base + C::Q), desc_columns(base + C::K + st * C::TILE), ks);
                 ptx::mma_commit(k_free(st));
                 ptx::mma_commit(s_full);
                 if (!wait(p_full, i & 1) || !wait(v_full(st), ph)) break;
                 ptx::tc_fence_after_sync();
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    mma_ts(tmem + C::COL_O, tmem + C::COL_S + k * 8, along_rows<128>(base + C::V + st * C::TILE, k), idesc_bf16(DP, true), (i | k) > 0);
+                product_rows<DP, 128>(tmem + C::COL_O, tmem + C::COL_S, desc_rows<128>(base + C::V + st * C::TILE), i > 0);
                 ptx::mma_commit(v_free(st));
             }
             ptx::mma_commit(o_full);
-            if (!ok) ptx::mbar_wait(o_full, 0);   // products in flight end before tensor memory is freed
+            if (!ok) wait_for(o_full, 0);   // products in flight end before tensor memory is freed
         }
         __syncwarp();
     } else {
@@ -341,365 +387,519 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     if (warp == 5) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
 }
 
-// ---- dQ --------------------------------------------------------------------------------------------------------------------------
-// 64 keys a step.  (One stage of K and V at width 128: two CTAs per SM hold 96 KB each.)
-template <int DP> struct DqCfg {
-    static constexpr int STAGES = DP == 64 ? 3 : 1;
-    static constexpr int TILE = 128 * DP * 2, HALF = 64 * DP * 2;
-    static constexpr int Q = 0, DO = TILE, K = 2 * TILE, V = K + STAGES * HALF, BAR = V + STAGES * HALF, BYTES = BAR + 256 + 1024;
-    static constexpr uint32_t COL_S = 0, COL_P = 64, COL_Q = 128, COLS = 256;
+// ---- the backward pass: dQ, and dK with dV -----------------------------------------------------------------------------------------
+// Both walk tiles with two operands of a block of 128 rows resident (X) and two streaming by, 64 rows a step (Y):
+//   dQ       X1 = Q, X2 = dO; Y1 = K, Y2 = V;   S = X1 Y1^T, dP = X2 Y2^T;              dQ += dS Y1
+//   dK, dV   X1 = K, X2 = V;  Y1 = Q, Y2 = dO;  S^T = X1 Y1^T, dP^T = X2 Y2^T (rows: keys); dK += dS^T Y1, dV += P^T Y2
+// Sets of eight softmax warps (two per quarter of the rows, 32 columns each) take alternate steps, each set with S and dP of its own in tensor
+// memory, so that the tensor core works on the next steps while one is exponentiated; the second products' A operand (bfloat16) lies
+// over what its warp has read of S and dP.
+//
+// Work is dealt by tiles: the tiles of all blocks in one order (problem, block, query head of the group, tile), `share` to each CTA, so
+// that blocks of any lengths -- the keys that every query sees -- keep all SMs busy.  A block that lies in one share is finished there; of others each CTA leaves a
+// part in fp32: in slot 0 if the block began in an earlier share, in slot 1 if it begins in this one; tile_grad_join_kernel adds them up in order.
+enum { kDq = 0, kDkv = 1 };
+
+// Tiles of the pattern by block (rb_ptr or cb_ptr) and who uses them.  An outer problem is a (sequence, query head) for dQ, a (sequence,
+// key head) with its group of query heads for dK and dV.
+struct Tiles {
+    const int *ptr;
+    int NB, outer, group, patterns, batch, heads, outers;
+    __device__ __forceinline__ int pattern(int o, int i) const { return pattern_of(patterns, batch, heads, o / outer, o % outer * group + i); }
+    __device__ __forceinline__ int at(int pat, int blk) const { return ptr[(long long)pat * NB + blk]; }
+    // tiles ahead of outer problem o
+    __device__ __forceinline__ long long base(int o) const
+    {
+        const int b = o / outer, x = o % outer;
+        if (patterns == 1) return (long long)o * group * at(1, 0);
+        if (patterns == batch) {
+            const long long t = at(b, 0);
+            return group * (outer * t + (x ? x * (at(b + 1, 0) - t) : 0));
+        }
+        return at(b * heads + x * group, 0);
+    }
+    // tiles of outer problem o ahead of its block blk
+    __device__ __forceinline__ long long ahead(int o, int blk) const
+    {
+        if (patterns == 1 || patterns == batch) {
+            const int p = pattern(o, 0);
+            return (long long)group * (at(p, blk) - at(p, 0));
+        }
+        long long n = 0;
+        for (int i = 0; i < group; ++i) {
+            const int p = pattern(o, i);
+            n += at(p, blk) - at(p, 0);
+        }
+        return n;
+    }
 };
 
-template <int DP>
-__global__ void __launch_bounds__(kTileThreads, 2)
-tile_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
-               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ TileArgs a)
+// Where share c begins: (outer problem, block, query head of the group, tile).
+__device__ __forceinline__ int4 share_start(const Tiles &w, long long pos)
 {
-    using C = DqCfg<DP>;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (ptx::smem_u32(raw) + 1023u) & ~1023u, bars = base + C::BAR;
-    auto full = [&](int s) { return bars + 8u * s; };
-    auto free_ = [&](int s) { return bars + 32u + 8u * s; };
-    const uint32_t q_full = bars + 64, s_full = bars + 72, p_full = bars + 80, o_full = bars + 88, slot = bars + 96;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Shape &s = a.g.s;
-    const int problems = s.batch * s.heads, RB = a.plan.RB;
-    const int prob = blockIdx.x % problems, rb = RB - 1 - blockIdx.x / problems;
-    const int b = prob / s.heads, h = prob % s.heads, hkv = h / (s.heads / s.kv_heads);
-    const int pat = pattern_of(s.patterns, s.batch, s.heads, b, h);
-    const int t0 = a.plan.rb_ptr[pat * RB + rb], steps = 2 * (a.plan.rb_ptr[pat * RB + rb + 1] - t0);
-    const int row = rb * kTile + threadIdx.x;
-    if (steps == 0) {
-        if (threadIdx.x < 128 && row < s.M) {
-            Bf16 *o = a.g.out1.at(b, h, row);
-            for (int c = 0; c < s.d; c += 8) *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
-        }
-        return;
+    int lo = 0, hi = w.outers;
+    while (hi - lo > 1) {
+        const int m = lo + ((hi - lo) >> 1);
+        if (w.base(m) <= pos) lo = m; else hi = m;
     }
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
-        ptx::mbar_init(q_full, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(p_full, 128); ptx::mbar_init(o_full, 1);
-        ptx::fence_mbar_init();
+    // (of problems without tiles, which share a base, the last one: it is the one with tiles behind `pos`)
+    const int o = lo;
+    pos -= w.base(o);
+    lo = 0, hi = w.NB;
+    while (hi - lo > 1) {
+        const int m = lo + ((hi - lo) >> 1);
+        if (w.ahead(o, m) <= pos) lo = m; else hi = m;
     }
-    if (warp == 5) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
-    ptx::tc_fence_before_sync();
-    __syncthreads();
-    ptx::tc_fence_after_sync();
-    const uint32_t tmem = ptx::lds32(slot);
-    bool ok = true;
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
-        return ok;
-    };
-    auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
-    if (warp == 4) {
-        if (ptx::elect_one()) {
-            ptx::mbar_arrive_expect_tx(q_full, 2 * C::TILE);
-            load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
-            load_tile<DP, 128>(base + C::DO, &tm_do, q_full, rb * kTile, h * a.dout.hm, b * a.dout.bm);
-            int i = 0, now = 0, next = a.plan.tile_cb[t0];
-            for (; i < steps; ++i) {
-                if (!(i & 1)) {
-                    now = next * kTile;
-                    if (i + 2 < steps) next = a.plan.tile_cb[t0 + (i >> 1) + 1];
-                }
-                const int st = i % C::STAGES, ph = i / C::STAGES & 1, at = now + (i & 1) * 64;
-                if (!wait(free_(st), ph ^ 1)) break;
-                ptx::mbar_arrive_expect_tx(full(st), 2 * C::HALF);
-                load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, full(st), at, hkv * a.k.hm, b * a.k.bm);
-                load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, full(st), at, hkv * a.v.hm, b * a.v.bm);
-            }
-            if (!ok) {
-                ptx::mbar_wait(q_full, 0);
-                for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
-            }
-        }
-        __syncwarp();
-    } else if (warp == 5) {
-        if (ptx::elect_one()) {
-            const int ks = (s.d + 15) >> 4;
-            wait(q_full, 0);
-            for (int i = 0; i < steps; ++i) {
-                const int st = i % C::STAGES, ph = i / C::STAGES & 1;
-                const uint32_t K = base + C::K + st * C::HALF, V = base + C::V + st * C::HALF;
-                if (!wait(full(st), ph)) break;
-                for (int k = 0; k < ks; ++k) mma_ss(tmem + C::COL_S, along_columns<128>(base + C::Q, k), along_columns<64>(K, k), idesc_bf16(64, false), k > 0);
-                for (int k = 0; k < ks; ++k) mma_ss(tmem + C::COL_P, along_columns<128>(base + C::DO, k), along_columns<64>(V, k), idesc_bf16(64, false), k > 0);
-                ptx::mma_commit(s_full);
-                if (!wait(p_full, i & 1)) break;
-                ptx::tc_fence_after_sync();
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    mma_ts(tmem + C::COL_Q, tmem + C::COL_S + k * 8, along_rows<64>(K, k), idesc_bf16(DP, true), (i | k) > 0);
-                ptx::mma_commit(free_(st));
-            }
-            ptx::mma_commit(o_full);
-            if (!ok) ptx::mbar_wait(o_full, 0);   // products in flight end before tensor memory is freed
-        }
-        __syncwarp();
-    } else {
-        const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
-        const float2 st = a.g.stat[(long long)prob * a.g.stat_stride + row];
-        const float c2 = s.scale * kLog2e;
-        const uint64_t f2 = two(c2, c2), l2 = two(-st.x, -st.x), d2 = two(-st.y, -st.y);
-        const uint4 *mask = a.plan.masks + (long long)t0 * kTile + threadIdx.x;
-        uint4 bits = __ldg(mask), now = bits;
-        unsigned some = 0;
-        for (int i = 0; i < steps; ++i) {
-            if (!(i & 1)) {
-                now = bits;
-                some |= now.x | now.y | now.z | now.w;
-                if (i + 2 < steps) bits = __ldg(mask + (long long)((i >> 1) + 1) * kTile);
-            }
-            if (!wait_all(s_full, i & 1)) break;
-            ptx::tc_fence_after_sync();
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t x[32], y[32];
-                ptx::tmem_ld_32x32(mine + C::COL_S + 32 * c, x);
-                ptx::tmem_ld_32x32(mine + C::COL_P + 32 * c, y);
-                ptx::tmem_ld_wait();
-                settle(x);
-                settle(y);
-                const uint32_t w = (i & 1) ? (c ? now.w : now.z) : (c ? now.y : now.x);
-                uint32_t o[16];
-#pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    float p0, p1, e0, e1;
-                    split(fma2(two(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, l2), p0, p1);
-                    split(mul2(two(ex2(p0), ex2(p1)), add2(two(__uint_as_float(y[k]), __uint_as_float(y[k + 1])), d2)), e0, e1);
-                    o[k >> 1] = bf16x2(w >> k & 1 ? e0 : 0.f, w >> (k + 1) & 1 ? e1 : 0.f);
-                }
-                ptx::tmem_st_32x16(mine + C::COL_S + 16 * c, o);
-            }
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before_sync();
-            ptx::mbar_arrive(p_full);
-        }
-        wait_all(o_full, 0);
-        ptx::tc_fence_after_sync();
-        const bool in = row < s.M, live = in && some;
-        bool bad = false;
-        Bf16 *o = a.g.out1.at(b, h, in ? row : 0);
-#pragma unroll 1
-        for (int c = 0; c < DP; c += 32) {
-            uint32_t x[32];
-            ptx::tmem_ld_32x32(mine + C::COL_Q + c, x);
-            ptx::tmem_ld_wait();
-            settle(x);
-            if (live) bad |= !store32(o, c, s.d, x, s.scale);
-            else if (in)
-                for (int k = c; k < min(c + 32, s.d); k += 8) *reinterpret_cast<uint4 *>(o + k) = make_uint4(0, 0, 0, 0);
-        }
-        const unsigned redo = __ballot_sync(~0u, bad);
-        if (redo && ok) rows_one_by_one<kGradQ, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, rb * kTile + warp * 32, redo, a.g.ptr_stride, a.g.idx_stride);
+    pos -= w.ahead(o, lo);
+    int i = 0, t = 0;
+    for (; i < w.group; ++i) {
+        const int p = w.pattern(o, i), t0 = w.at(p, lo), n = w.at(p, lo + 1) - t0;
+        t = t0 + (int)pos;
+        if (pos < n) break;
+        pos -= n;
     }
-    ptx::tc_fence_before_sync();
-    __syncthreads();
-    if (warp == 5) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
+    return make_int4(o, lo, i, t);
 }
 
-// ---- dK and dV -------------------------------------------------------------------------------------------------------------------
-// Steps of 64 queries.  Width 64: two CTAs per SM, one set of four softmax warps each.  Width 128 fills tensor memory with the two
-// accumulators and two sets of S and dP, so one CTA per SM has two sets of warps that take alternate steps.
-template <int DP> struct DkvCfg {
-    static constexpr int SETS = DP == 64 ? 1 : 2, THREADS = 128 * SETS + 64;
-    static constexpr int STAGES = DP == 64 ? 3 : 3;
-    static constexpr int TILE = 128 * DP * 2, HALF = 64 * DP * 2, STAT = 512;
-    static constexpr int K = 0, V = TILE, Q = 2 * TILE, DO = Q + STAGES * HALF, ST = DO + STAGES * HALF, BAR = ST + STAGES * STAT, BYTES = BAR + 256 + 1024;
-    static constexpr uint32_t COL_V = 0, COL_K = DP, COL_S = 2 * DP, COLS = DP == 64 ? 256 : 512;   // S and dP of set i: COL_S + 128 i
+// A warp's walk over its CTA's tiles; all lanes hold the same state.
+struct Walk {
+    int o, blk, i, t, t1, left;   // the tile at hand: query head i of the group, tile t of [.., t1); tiles left, this one included
+    bool fresh;                   // it is the first of its block here
+    __device__ __forceinline__ void start(const Tiles &w, int4 at, int n)
+    {
+        o = at.x; blk = at.y; i = at.z; t = at.w; left = n; fresh = true;
+        t1 = w.at(w.pattern(o, i), blk + 1);
+    }
+    // Whether the next tile (if there is one) is of another block; moves on to it.
+    __device__ __forceinline__ bool next(const Tiles &w)
+    {
+        fresh = false;
+        if (--left == 0) return true;
+        if (++t < t1) return false;
+        while (++i < w.group) {
+            const int p = w.pattern(o, i);
+            t = w.at(p, blk);
+            t1 = w.at(p, blk + 1);
+            if (t < t1) return false;
+        }
+        // the next block with tiles: 32 blocks at a time
+        const int lane = threadIdx.x & 31;
+        fresh = true;
+        ++blk;
+        for (;;) {
+            if (blk >= w.NB) { blk = 0; ++o; }
+            if (o >= w.outers) {   // (fewer tiles than the caller said)
+                o = blk = i = t = t1 = left = 0;
+                return true;
+            }
+            const int k = blk + lane;
+            bool any = false;
+            for (int g = 0; g < (w.patterns == w.batch * w.heads ? w.group : 1) && !any; ++g) {
+                const int p = w.pattern(o, g);
+                any = k < w.NB && w.at(p, k + 1) > w.at(p, k);
+            }
+            const unsigned found = __ballot_sync(~0u, any);
+            if (found) {
+                blk += __ffs(found) - 1;
+                break;
+            }
+            blk = min(blk + 32, w.NB);
+        }
+        for (i = 0;; ++i) {
+            const int p = w.pattern(o, i);
+            t = w.at(p, blk);
+            t1 = w.at(p, blk + 1);
+            if (t < t1) break;
+        }
+        return true;
+    }
 };
 
-template <int DP>
-__global__ void __launch_bounds__(DkvCfg<DP>::THREADS, DP == 64 ? 2 : 1)
-tile_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
-                const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ TileArgs a)
+struct GradArgs {
+    TileArgs a;
+    Tiles w;
+    const int *tile_at;       // of a tile: its row or column block, the first of two ints for dK and dV
+    int share, ctas;
+    long long tiles;          // of all problems
+    const int4 *starts;       // of the CTAs
+    float *part;              // [ctas][2][dK: 2][128][DP]
+    int *bad;                 // [outers][blocks]: the sums of a block are not finite (its rows are taken one by one)
+};
+
+// Two warps issue products: one S and dP, as far ahead as sets of tensor memory are free, one the second products.  The tensor core takes
+// products from them in turn (about 52 cycles each at 128 x 64 x 16 from shared memory, 61 at 128 x 128 x 16 with A in tensor memory), and what
+// a warp spends between its batches -- 100 to 250 cycles a barrier -- is hidden by the other's; with one issuer it was idle 44% of the time.
+template <int MODE, int DP> struct GradCfg {
+    static constexpr int SETS = MODE == kDkv && DP == 128 ? 2 : 3, THREADS = 256 * SETS + 96;
+    static constexpr int STAGES = DP == 64 ? 6 : 4;
+    static constexpr int ACCS = MODE == kDkv ? 2 : 1;
+    static constexpr int TILE = 128 * DP * 2, HALF = 64 * DP * 2, STAT = MODE == kDkv ? 512 : 0;
+    static constexpr int X1 = 0, X2 = TILE, Y1 = 2 * TILE, Y2 = Y1 + STAGES * HALF, ST = Y2 + STAGES * HALF, BAR = ST + STAGES * STAT, BYTES = BAR + 512 + 1024;
+    static constexpr uint32_t COL_S = ACCS * DP, COLS = 512;   // accumulators (dQ, or dK and dV) first; S and dP of set i: COL_S + 128 i
+    static_assert(COL_S + 128 * SETS <= 512 && BYTES <= 232448, "tensor memory or shared memory");
+};
+constexpr uint32_t kStepFirst = 1, kStepLast = 2;   // what the loading warp says of a step: its block's first, its block's last here
+
+template <int MODE, int DP>
+__global__ void __launch_bounds__(GradCfg<MODE, DP>::THREADS, 1)
+tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2, const __grid_constant__ CUtensorMap tm_y1,
+                 const __grid_constant__ CUtensorMap tm_y2, const __grid_constant__ GradArgs g)
 {
-    using C = DkvCfg<DP>;
-    constexpr int SETS = C::SETS, TMA_WARP = 4 * SETS, MMA_WARP = TMA_WARP + 1;
+    using C = GradCfg<MODE, DP>;
+    constexpr int SETS = C::SETS, TMA_WARP = 8 * SETS, FIRST_WARP = TMA_WARP + 1, SECOND_WARP = TMA_WARP + 2;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (ptx::smem_u32(raw) + 1023u) & ~1023u, bars = base + C::BAR;
     auto full = [&](int s) { return bars + 8u * s; };
-    auto free_ = [&](int s) { return bars + 32u + 8u * s; };
-    auto s_full = [&](int w) { return bars + 64u + 8u * w; };
-    auto p_full = [&](int w) { return bars + 80u + 8u * w; };
-    const uint32_t k_full = bars + 96, o_full = bars + 104, slot = bars + 112;
+    auto free_ = [&](int s) { return bars + 64u + 8u * s; };
+    auto s_full = [&](int w) { return bars + 128u + 8u * w; };
+    auto p_full = [&](int w) { return bars + 152u + 8u * w; };
+    auto s_free = [&](int w) { return bars + 176u + 8u * w; };
+    auto flags = [&](int s) { return bars + 320u + 4u * s; };
+    const uint32_t x_full = bars + 200, x_free = bars + 208, o_full = bars + 216, o_free = bars + 224, slot = bars + 232;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const TileArgs &a = g.a;
     const Shape &s = a.g.s;
-    const int CB = a.plan.CB, group = s.heads / s.kv_heads, problems = s.batch * s.kv_heads;
-    const int prob = blockIdx.x % problems, cb = blockIdx.x / problems;
-    const int b = prob / s.kv_heads, hkv = prob % s.kv_heads;
-    // the walk: query heads of the group, tiles of the column block, halves of a tile
-    int steps = 0;
-    for (int i = 0; i < group; ++i) {
-        const int pat = pattern_of(s.patterns, s.batch, s.heads, b, hkv * group + i);
-        steps += 2 * (a.plan.cb_ptr[pat * CB + cb + 1] - a.plan.cb_ptr[pat * CB + cb]);
-    }
-    const int key = cb * kTile + (threadIdx.x & 127);
-    if (steps == 0) {
-        if (threadIdx.x < 128 && key < s.K) {
-            Bf16 *o1 = a.g.out1.at(b, hkv, key), *o2 = a.g.out2.at(b, hkv, key);
-            for (int c = 0; c < s.d; c += 8) *reinterpret_cast<uint4 *>(o1 + c) = *reinterpret_cast<uint4 *>(o2 + c) = make_uint4(0, 0, 0, 0);
-        }
-        return;
-    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
-        for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 128); }
-        ptx::mbar_init(k_full, 1); ptx::mbar_init(o_full, 1);
+        for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 256); ptx::mbar_init(s_free(i), 1); }
+        ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1); ptx::mbar_init(o_full, 1); ptx::mbar_init(o_free, 256 * SETS);
+        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // only for leaving early
         ptx::fence_mbar_init();
     }
-    if (warp == MMA_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
+    if (warp == FIRST_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the row statistics and the shares' starts
     const uint32_t tmem = ptx::lds32(slot);
+    const int tiles = (int)min((long long)g.share, g.tiles - (long long)blockIdx.x * g.share), steps = 2 * tiles;
     bool ok = true;
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+    auto wait = [&](uint32_t bar, uint32_t parity) {   // of a single thread
+        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
         return ok;
     };
-    auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
+    auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a whole warp
     if (warp == TMA_WARP) {
-        if (ptx::elect_one()) {
-            ptx::mbar_arrive_expect_tx(k_full, 2 * C::TILE);
-            load_tile<DP, 128>(base + C::K, &tm_k, k_full, cb * kTile, hkv * a.k.hm, b * a.k.bm);
-            load_tile<DP, 128>(base + C::V, &tm_v, k_full, cb * kTile, hkv * a.v.hm, b * a.v.bm);
-            int i = 0;
-            for (int hh = 0; hh < group && ok; ++hh) {
-                const int h = hkv * group + hh, pat = pattern_of(s.patterns, s.batch, s.heads, b, h);
-                const float2 *stat = a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride;
-                const int t1 = a.plan.cb_ptr[pat * CB + cb + 1];
-                for (int t = a.plan.cb_ptr[pat * CB + cb]; t < t1 && ok; ++t) {
-                    const int r0 = a.plan.ctile[t].x * kTile;
-                    for (int half = 0; half < 2; ++half, ++i) {
-                        const int st = i % C::STAGES, ph = i / C::STAGES & 1, at = r0 + half * 64;
-                        if (!wait(free_(st), ph ^ 1)) break;
-                        ptx::mbar_arrive_expect_tx(full(st), 2 * C::HALF + C::STAT);
-                        load_tile<DP, 64>(base + C::Q + st * C::HALF, &tm_q, full(st), at, h * a.q.hm, b * a.q.bm);
-                        load_tile<DP, 64>(base + C::DO + st * C::HALF, &tm_do, full(st), at, h * a.dout.hm, b * a.dout.bm);
-                        bulk_load(base + C::ST + st * C::STAT, stat + at, C::STAT, full(st));
-                    }
+        Walk w;
+        w.start(g.w, g.starts[blockIdx.x], tiles);
+        int i = 0, blocks = 0;
+        for (bool more = true; more && ok;) {
+            const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
+            const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
+            const bool fresh = w.fresh, last = w.next(g.w);
+            more = w.left > 0;
+            if (fresh) {   // the block's own operands, behind the last product that reads the previous block's
+                if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(x_full, 2 * C::TILE);
+                    const Op &o1 = MODE == kDq ? a.q : a.k, &o2 = MODE == kDq ? a.dout : a.v;
+                    load_tile<DP, 128>(base + C::X1, &tm_x1, x_full, blk * kTile, x * o1.hm, b * o1.bm);
+                    load_tile<DP, 128>(base + C::X2, &tm_x2, x_full, blk * kTile, x * o2.hm, b * o2.bm);
                 }
+                __syncwarp();
+                ++blocks;
             }
-            if (!ok) {
-                ptx::mbar_wait(k_full, 0);
-                for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
+            for (int half = 0; half < 2; ++half, ++i) {
+                const int st = i % C::STAGES, at = r0 + half * 64;
+                if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
+                if (ptx::elect_one()) {
+                    ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
+                    ptx::mbar_arrive_expect_tx(full(st), 2 * C::HALF + C::STAT);
+                    const Op &o1 = MODE == kDq ? a.k : a.q, &o2 = MODE == kDq ? a.v : a.dout;
+                    load_tile<DP, 64>(base + C::Y1 + st * C::HALF, &tm_y1, full(st), at, hy * o1.hm, b * o1.bm);
+                    load_tile<DP, 64>(base + C::Y2 + st * C::HALF, &tm_y2, full(st), at, hy * o2.hm, b * o2.bm);
+                    if (MODE == kDkv) bulk_load(base + C::ST + st * C::STAT, a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride + at, C::STAT, full(st));
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok) {   // copies in flight land before the CTA ends
+            if (blocks) wait_for(x_full, (blocks - 1) & 1);
+            for (int k = max(0, i - C::STAGES); k < i; ++k) wait_for(full(k % C::STAGES), k / C::STAGES & 1);
+        }
+    } else if (warp == FIRST_WARP) {
+        if (ptx::elect_one()) {
+            const int ks = (s.d + 15) >> 4;
+            const uint32_t x1 = desc_columns(base + C::X1), x2 = desc_columns(base + C::X2), y1 = desc_columns(base + C::Y1), y2 = desc_columns(base + C::Y2);
+            int st = 0, ph = 0, set = 0, round = 0, blocks = 0;
+            for (int i = 0; i < steps; ++i) {
+                if (!wait(full(st), ph)) break;
+                if ((ptx::lds32(flags(st)) & kStepFirst) && !wait(x_full, blocks++ & 1)) break;
+                if (round && !wait(s_free(set), (round - 1) & 1)) break;   // the second products of the step before last here are done
+                const uint32_t to = tmem + C::COL_S + set * 128;
+                product_columns<DP, 64>(to, x1, y1 + st * (C::HALF >> 4), ks);
+                product_columns<DP, 64>(to + 64, x2, y2 + st * (C::HALF >> 4), ks);
+                ptx::mma_commit(s_full(set));
+                if (++st == C::STAGES) { st = 0; ph ^= 1; }
+                if (++set == SETS) { set = 0; ++round; }
+            }
+            if (!ok) {   // products in flight end before tensor memory is freed
+                ptx::mma_commit(slot + 16);
+                wait_for(slot + 16, 0);
             }
         }
         __syncwarp();
-    } else if (warp == MMA_WARP) {
+    } else if (warp == SECOND_WARP) {
         if (ptx::elect_one()) {
-            const int ks = (s.d + 15) >> 4;
-            auto first = [&](int i) {   // S^T and dP^T of step i
-                const int st = i % C::STAGES;
-                if (!wait(full(st), i / C::STAGES & 1)) return;
-                const uint32_t to = tmem + C::COL_S + (i % SETS) * 128;
-                for (int k = 0; k < ks; ++k) mma_ss(to, along_columns<128>(base + C::K, k), along_columns<64>(base + C::Q + st * C::HALF, k), idesc_bf16(64, false), k > 0);
-                for (int k = 0; k < ks; ++k) mma_ss(to + 64, along_columns<128>(base + C::V, k), along_columns<64>(base + C::DO + st * C::HALF, k), idesc_bf16(64, false), k > 0);
-                ptx::mma_commit(s_full(i % SETS));
-            };
-            wait(k_full, 0);
-            for (int i = 0; i < SETS && i < steps; ++i) first(i);
-            for (int i = 0; i < steps && ok; ++i) {
-                const int st = i % C::STAGES;
-                const uint32_t from = tmem + C::COL_S + (i % SETS) * 128;
-                if (!wait(p_full(i % SETS), i / SETS & 1)) break;
+            const uint32_t y1 = desc_rows<64>(base + C::Y1), y2 = desc_rows<64>(base + C::Y2);
+            int st = 0, ph = 0, set = 0, round = 0, blocks = 0;
+            bool onto = false;
+            for (int i = 0; i < steps; ++i) {
+                if (!wait(full(st), ph)) break;   // (long complete: what it says of the step is visible here)
+                const uint32_t f = ptx::lds32(flags(st));
+                if (f & kStepFirst) {
+                    onto = false;
+                    if (blocks && !wait(o_free, (blocks - 1) & 1)) break;   // the accumulators are read
+                }
+                if (!wait(p_full(set), round & 1)) break;
                 ptx::tc_fence_after_sync();
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mma_ts(tmem + C::COL_V, from + k * 8, along_rows<64>(base + C::DO + st * C::HALF, k), idesc_bf16(DP, true), (i | k) > 0);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mma_ts(tmem + C::COL_K, from + 64 + k * 8, along_rows<64>(base + C::Q + st * C::HALF, k), idesc_bf16(DP, true), (i | k) > 0);
+                const uint32_t from = tmem + C::COL_S + set * 128;
+                // (dQ: dS lies over S.  dK, dV: P over S, dS over dP.)
+                if (MODE == kDkv) product_rows<DP, 64, 32>(tmem + DP, from, y2 + st * (C::HALF >> 4), onto);
+                product_rows<DP, 64, 32>(tmem, from + (MODE == kDkv ? 64 : 0), y1 + st * (C::HALF >> 4), onto);
+                onto = true;
+                ptx::mma_commit(s_free(set));
                 ptx::mma_commit(free_(st));
-                if (i + SETS < steps) first(i + SETS);
+                if (f & kStepLast) {
+                    ptx::mma_commit(x_free);
+                    ptx::mma_commit(o_full);
+                    ++blocks;
+                }
+                if (++st == C::STAGES) { st = 0; ph ^= 1; }
+                if (++set == SETS) { set = 0; ++round; }
             }
-            ptx::mma_commit(o_full);
-            if (!ok) ptx::mbar_wait(o_full, 0);   // products in flight end before tensor memory is freed
+            if (!ok) {
+                ptx::mma_commit(slot + 24);
+                wait_for(slot + 24, 0);
+            }
         }
         __syncwarp();
     } else {
-        const int set = SETS == 1 ? 0 : warp >> 2;
-        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), from = mine + C::COL_S + set * 128;
+        const int set = warp >> 3, part = warp >> 2 & 1, lane_row = threadIdx.x & 127;
+        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), from = mine + C::COL_S + set * 128 + part * 32;
         const float c2 = s.scale * kLog2e;
         const uint64_t f2 = two(c2, c2);
+        Walk w;
+        w.start(g.w, g.starts[blockIdx.x], tiles);
+        int i = 0, blocks = 0, at_set = 0, round = 0, st = 0;   // step, and which set, which of its turns and which stage it has
+        float2 own = make_float2(0.f, 0.f);
         unsigned some = 0;
-        int i = 0;
-        for (int hh = 0; hh < group && ok; ++hh) {
-            const int h = hkv * group + hh, pat = pattern_of(s.patterns, s.batch, s.heads, b, h);
-            const int t1 = a.plan.cb_ptr[pat * CB + cb + 1];
-            for (int t = a.plan.cb_ptr[pat * CB + cb]; t < t1 && ok; ++t) {
-                const uint4 now = __ldg(a.plan.tmasks + (long long)t * kTile + (threadIdx.x & 127));
-                some |= now.x | now.y | now.z | now.w;
-                for (int half = 0; half < 2; ++half, ++i) {
-                    if (SETS == 2 && (i & 1) != set) continue;
-                    if (!wait_all(s_full(set), i / SETS & 1)) break;
-                    ptx::tc_fence_after_sync();
-                    const uint32_t stat = base + C::ST + (i % C::STAGES) * C::STAT;
+        int first_i = w.i, first_t = w.t;   // where the block's part began (is it the block's beginning?)
+        for (bool more = true; more && ok;) {
+            const int blk = w.blk, o = w.o;
+            if (w.fresh) {
+                some = 0;
+                first_i = w.i;
+                first_t = w.t;
+                if (MODE == kDq) own = a.g.stat[(long long)o * a.g.stat_stride + blk * kTile + lane_row];
+            }
+            const uint4 now = __ldg((MODE == kDq ? a.plan.masks : a.plan.tmasks) + (long long)w.t * kTile + lane_row);
+            some |= now.x | now.y | now.z | now.w;
+            const uint64_t l2 = two(own.x, own.x), d2 = two(own.y, own.y);
+            for (int half = 0; half < 2; ++half, ++i) {
+                const bool my_turn = at_set == set;
+                const int stage = st, turn = round;
+                if (++st == C::STAGES) st = 0;
+                if (++at_set == SETS) { at_set = 0; ++round; }
+                if (!my_turn) continue;
+                if (!wait_all(s_full(set), turn & 1)) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t stat = base + C::ST + stage * C::STAT + part * 256;
+                const uint32_t m = half ? (part ? now.w : now.z) : (part ? now.y : now.x);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t x[32], y[32];
-                        ptx::tmem_ld_32x32(from + 32 * c, x);
-                        ptx::tmem_ld_32x32(from + 64 + 32 * c, y);
-                        ptx::tmem_ld_wait();
-                        settle(x);
-                        settle(y);
-                        const uint32_t w = half ? (c ? now.w : now.z) : (c ? now.y : now.x);
-                        uint32_t p[16], o[16];
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t x[16], y[16];
+                    ptx::tmem_ld_32x16(from + 16 * c, x);
+                    ptx::tmem_ld_32x16(from + 64 + 16 * c, y);
+                    ptx::tmem_ld_wait();
+                    settle(x);
+                    settle(y);
+                    uint32_t p[8], q[8];
 #pragma unroll
-                        for (int k = 0; k < 32; k += 2) {
-                            float l0, d0, l1, d1, p0, p1, e0, e1;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(stat + (32 * c + k) * 8));
-                            split(fma2(two(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, two(-l0, -l1)), p0, p1);
-                            p0 = w >> k & 1 ? ex2(p0) : 0.f;
-                            p1 = w >> (k + 1) & 1 ? ex2(p1) : 0.f;
-                            split(mul2(two(p0, p1), add2(two(__uint_as_float(y[k]), __uint_as_float(y[k + 1])), two(-d0, -d1))), e0, e1);
-                            p[k >> 1] = bf16x2(p0, p1);
-                            o[k >> 1] = bf16x2(e0, e1);
+                    for (int k = 0; k < 16; k += 2) {
+                        float p0, p1, e0, e1;
+                        uint64_t nl = l2, nd = d2;
+                        if (MODE == kDkv) {
+                            float l0, d0, l1, d1;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l0), "=f"(d0), "=f"(l1), "=f"(d1) : "r"(stat + (16 * c + k) * 8));
+                            nl = two(l0, l1);
+                            nd = two(d0, d1);
                         }
-                        ptx::tmem_st_32x16(from + 16 * c, p);
-                        ptx::tmem_st_32x16(from + 64 + 16 * c, o);
+                        split(fma2(two(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, nl), p0, p1);
+                        p0 = m >> (16 * c + k) & 1 ? ex2(p0) : 0.f;
+                        p1 = m >> (16 * c + k + 1) & 1 ? ex2(p1) : 0.f;
+                        split(mul2(two(p0, p1), add2(two(__uint_as_float(y[k]), __uint_as_float(y[k + 1])), nd)), e0, e1);
+                        if (MODE == kDkv) p[k >> 1] = bf16x2(p0, p1);
+                        q[k >> 1] = bf16x2(e0, e1);
                     }
-                    ptx::tmem_st_wait();
-                    ptx::tc_fence_before_sync();
-                    ptx::mbar_arrive(p_full(set));
+                    if (MODE == kDkv) {
+                        tmem_st_32x8(from + 8 * c, p);
+                        tmem_st_32x8(from + 64 + 8 * c, q);
+                    } else {
+                        tmem_st_32x8(from + 8 * c, q);
+                    }
+                }
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before_sync();
+                ptx::mbar_arrive(p_full(set));
+            }
+            const int last_i = w.i;
+            const bool ended = w.t + 1 == w.t1;   // of the query head's tiles
+            const bool ends = w.next(g.w);
+            more = w.left > 0;
+            if (!ends || !ok) continue;
+            // the block's part is done: its sums leave tensor memory, the halves of the sets take the groups of 32 columns in turn
+            if (!wait_all(o_full, blocks & 1)) break;
+            ptx::tc_fence_after_sync();
+            const int rows = MODE == kDq ? s.M : s.K, row = blk * kTile + lane_row;
+            const int b = o / g.w.outer, h = o % g.w.outer;
+            bool begun = true, whole = true;
+            {
+                // is the first tile here the block's first, the last one its last?
+                for (int k = 0; k <= first_i; ++k) {
+                    const int p = g.w.pattern(o, k), t0 = g.w.at(p, blk);
+                    if (k < first_i ? g.w.at(p, blk + 1) > t0 : first_t > t0) begun = false;
+                }
+                whole = begun && ended;
+                for (int k = last_i + 1; k < g.w.group && whole; ++k) {
+                    const int p = g.w.pattern(o, k);
+                    if (g.w.at(p, blk + 1) > g.w.at(p, blk)) whole = false;
                 }
             }
-        }
-        wait_all(o_full, 0);
-        ptx::tc_fence_after_sync();
-        const bool in = key < s.K, live = in && some;
-        bool bad = false;
+            bool bad = false;
+            const bool in = row < rows;
 #pragma unroll 1
-        for (int which = SETS == 2 ? set : 0; which < (SETS == 2 ? set + 1 : 2); ++which) {   // dV, dK
-            Bf16 *o = which ? a.g.out1.at(b, hkv, in ? key : 0) : a.g.out2.at(b, hkv, in ? key : 0);
-#pragma unroll 1
-            for (int c = 0; c < DP; c += 32) {
+            for (int c = warp >> 2; c < C::ACCS * (DP / 32); c += 2 * SETS) {
+                const int acc = c / (DP / 32), col = c % (DP / 32) * 32;
                 uint32_t x[32];
-                ptx::tmem_ld_32x32(mine + (which ? C::COL_K : C::COL_V) + c, x);
+                ptx::tmem_ld_32x32(mine + c * 32, x);
                 ptx::tmem_ld_wait();
                 settle(x);
-                if (live) bad |= !store32(o, c, s.d, x, which ? s.scale : 1.f);
-                else if (in)
-                    for (int k = c; k < min(c + 32, s.d); k += 8) *reinterpret_cast<uint4 *>(o + k) = make_uint4(0, 0, 0, 0);
+                if (whole) {
+                    Bf16 *to = (acc ? a.g.out2 : a.g.out1).at(b, h, in ? row : 0);
+                    if (in && some) bad |= !store32(to, col, s.d, x, acc ? 1.f : s.scale);
+                    else if (in)
+                        for (int k = col; k < min(col + 32, s.d); k += 8) *reinterpret_cast<uint4 *>(to + k) = make_uint4(0, 0, 0, 0);
+                } else {
+                    float *to = g.part + ((((long long)blockIdx.x * 2 + begun) * C::ACCS + acc) * kTile + lane_row) * DP + col;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<float4 *>(to + k) = make_float4(__uint_as_float(x[k]), __uint_as_float(x[k + 1]), __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                }
             }
-        }
-        if (SETS == 2) {   // a column of either gradient that is not finite: both are computed again, by the second set, after both are stored
-            uint32_t *flag = reinterpret_cast<uint32_t *>(raw) + ((base + C::BAR + 128 - ptx::smem_u32(raw)) >> 2);   // one word per warp of the first set
-            const unsigned vote = __ballot_sync(~0u, bad);
-            if (set == 0 && lane == 0) flag[warp] = vote;
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (set == 1) {
-                const unsigned redo = vote | flag[warp & 3];
-                if (redo && ok) rows_one_by_one<kGradKV, DP>(a.g, a.col_ptr, a.row_idx, b, hkv * group, group, cb * kTile + (warp & 3) * 32, redo, s.K + 1ll, a.g.idx_stride);
-            }
-        } else {
-            const unsigned redo = __ballot_sync(~0u, bad);
-            if (redo && ok) rows_one_by_one<kGradKV, DP>(a.g, a.col_ptr, a.row_idx, b, hkv * group, group, cb * kTile + warp * 32, redo, s.K + 1ll, a.g.idx_stride);
+            if (bad) g.bad[(long long)o * g.w.NB + blk] = 1;
+            ptx::tc_fence_before_sync();
+            ptx::mbar_arrive(o_free);
+            ++blocks;
         }
     }
+    __syncwarp();
     ptx::tc_fence_before_sync();
     __syncthreads();
-    if (warp == MMA_WARP) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
+    if (warp == FIRST_WARP) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
+}
+
+// Behind tile_grad_kernel, a CTA of eight warps per 32 rows of a block: zeros for a block without tiles; the parts of one that several shares hold, added
+// up in order; the rows of one whose sums are not finite, one by one.
+constexpr int kJoinRows = 32;
+template <int MODE, int DP>
+__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgs g)
+{
+    constexpr int ACCS = MODE == kDkv ? 2 : 1, WIDE = ACCS * DP, LANES = WIDE / 4;   // lanes that a row takes
+    const TileArgs &a = g.a;
+    const Shape &s = a.g.s;
+    const int block = blockIdx.x / (kTile / kJoinRows), part = blockIdx.x % (kTile / kJoinRows);
+    const int o = block / g.w.NB, blk = block % g.w.NB, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rows = MODE == kDq ? s.M : s.K, b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
+    if (row0 >= rows) return;
+    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, n = g.w.ahead(o, blk + 1) - ahead;
+    const int c0 = (int)(p0 / g.share), c1 = (int)((p0 + n - 1) / g.share);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const bool one = n > 0 && c0 == c1;
+    if (one && g.bad[block] == 0) return;
+    if (!one) {
+        __shared__ int redo;
+        if (threadIdx.x == 0) redo = 0;
+        __syncthreads();
+        // four elements a thread (of dK, then of dV), neighbouring rows in neighbouring threads
+#pragma unroll
+        for (int u = threadIdx.x; u < kJoinRows * LANES; u += 256) {
+            const int r = part * kJoinRows + u / LANES, e = u % LANES * 4, acc = e / DP, col = e % DP, row = blk * kTile + r;
+            if (row >= rows) continue;
+            float x[4] = {};
+            if (n > 0) {
+                const float *from = g.part + ((long long)acc * kTile + r) * DP + col;
+#pragma unroll 4
+                for (int c = c0; c <= c1; ++c) {
+                    const float4 v = *reinterpret_cast<const float4 *>(from + ((long long)c * 2 + (c == c0)) * (ACCS * kTile * DP));
+                    x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
+                }
+            }
+            bool bad = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[k] *= acc ? 1.f : s.scale;
+                bad |= col + k < s.d && !(fabsf(x[k]) <= 3.402823466e38f);
+            }
+            store4<Bf16, 4>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x);
+            if (bad) redo = 1;
+        }
+        __syncthreads();
+        if (redo == 0) return;
+    }
+    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) {
+        if (MODE == kDq) rows_one_by_one<kGradQ, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + r, 1u, a.g.ptr_stride, a.g.idx_stride);
+        else rows_one_by_one<kGradKV, DP>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row0 + r, 1u, s.K + 1ll, a.g.idx_stride);
+    }
+}
+
+// Ahead of both: row statistics (see attention_stat_kernel) and, in its last CTAs, where the shares begin; clears the flags of blocks.
+struct ShareArgs {
+    Tiles w[2];
+    int share[2], ctas[2], blocks[2];
+    int4 *starts[2];
+    int *bad[2];
+};
+template <int DUMMY = 0>
+__global__ void __launch_bounds__(256) tile_grad_stat_kernel(Shape s, View<const Bf16> out, View<const Bf16> dout, const float *lse, int stat_rows, float2 *stat,
+                                                             const __grid_constant__ ShareArgs h, int share_blocks, int *status)
+{
+    if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if ((int)blockIdx.x < share_blocks) {   // (first, as they wait longest)
+        const int u = blockIdx.x * 256 + threadIdx.x, total = h.ctas[0] + h.ctas[1];
+        for (int i = u; i < total; i += share_blocks * 256) {
+            const int k = i < h.ctas[0] ? 0 : 1, c = k ? i - h.ctas[0] : i;
+            h.starts[k][c] = share_start(h.w[k], (long long)c * h.share[k]);
+        }
+        for (int k = 0; k < 2; ++k)
+            for (int i = u; i < h.blocks[k]; i += share_blocks * 256) h.bad[k][i] = 0;
+        return;
+    }
+    // half a warp per row, eight elements a lane
+    const int half = threadIdx.x & 15;
+    const long long unit = (blockIdx.x - share_blocks) * 16ll + (threadIdx.x >> 4);
+    const long long prob = unit / stat_rows;
+    if (prob >= (long long)s.batch * s.heads) return;
+    const int row = (int)(unit % stat_rows), b = (int)(prob / s.heads), head = (int)(prob % s.heads);
+    float sum = 0.f, top = -CUDART_INF_F;
+    if (row < s.M) {
+        top = lse[prob * s.M + row];
+        const int c = half * 8;
+        if (c < s.d) {
+            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(out.at(b, head, row) + c)), y = __ldg(reinterpret_cast<const uint4 *>(dout.at(b, head, row) + c));
+            const unsigned u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sum = fmaf(__uint_as_float(u[k] << 16), __uint_as_float(v[k] << 16), sum);
+                sum = fmaf(__uint_as_float(u[k] & 0xffff0000u), __uint_as_float(v[k] & 0xffff0000u), sum);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (half == 0) stat[unit] = top == -CUDART_INF_F ? make_float2(-CUDART_INF_F, 0.f) : make_float2(-top * kLog2e, -sum);
 }
 
 }  // namespace attn

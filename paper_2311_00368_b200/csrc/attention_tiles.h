@@ -11,15 +11,19 @@ struct TileCall {
     long long tiles;                     // of all patterns
     const int *row_ptr, *col_idx;        // for rows that have to be taken one by one (see attention_tiles.cuh)
     long long row_ptr_stride, nnz_stride;
-    View<const Bf16> q, k, v, dout;
+    View<const Bf16> q, k, v, dout, o;   // o: the forward pass's result, in the backward pass
     View<Bf16> out, dq, dk, dv;
-    float *lse;
+    float *lse;                          // backward: read
     const float2 *stat;
     long long stat_stride;
     int *status;
+    void *workspace;
+    size_t scratch_at;                   // where the workspace is free
 };
 
 bool tiles_possible(const Shape &s, const View<const Bf16> *views, int n);
+// The end of what the backward pass needs of the workspace, from offset `at` on.
+size_t tiles_backward_bytes(const Shape &s, long long tiles, size_t at);
 b2sp_status tiles_forward(const TileCall &c, cudaStream_t st, int *launches);
 b2sp_status tiles_backward(const TileCall &c, cudaStream_t st, int *launches);
 
