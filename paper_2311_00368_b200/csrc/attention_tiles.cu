@@ -144,10 +144,9 @@ template <int MODE, int DP> b2sp_status grad(const TileCall &c, const GradPlan &
         return B2SP_ERR_CUDA;
     if (g.ctas) {
         launch_behind_smem(tile_grad_kernel<MODE, DP>, (unsigned)g.ctas, C::THREADS, C::BYTES, st, x1, x2, y1, y2, g);
-        ++*launches;
+        launch_behind(tile_grad_join_kernel<MODE, DP>, (unsigned)(g.ctas * kJoinParts), 256, st, g);
+        *launches += 2;
     }
-    launch_behind(tile_grad_join_kernel<MODE, DP>, (unsigned)(p.outers[MODE] * p.NB[MODE] * (kTile / kJoinRows)), 256, st, g);
-    ++*launches;
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
 
@@ -167,13 +166,14 @@ template <int DP> b2sp_status backward(const TileCall &c, cudaStream_t st, int *
         g[k].starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
         g[k].bad = reinterpret_cast<int *>(ws + p.bad[k]);
         g[k].part = reinterpret_cast<float *>(ws + p.part);
-        h.w[k] = g[k].w; h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.blocks[k] = p.outers[k] * p.NB[k];
+        h.w[k] = g[k].w; h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.rows[k] = k == 0 ? s.M : s.K;
         h.starts[k] = reinterpret_cast<int4 *>(ws + p.starts[k]); h.bad[k] = g[k].bad;
     }
     g[0].a.g.out1 = c.dq; g[0].a.g.rows = s.M;
     g[1].a.g.out1 = c.dk; g[1].a.g.out2 = c.dv; g[1].a.g.rows = s.K;
-    const long long rows = (long long)s.batch * s.heads * c.stat_stride, blocks = (rows + 15) / 16;
-    const int share_blocks = (std::max(1, std::max(p.ctas[0] + p.ctas[1], std::max(h.blocks[0], h.blocks[1]))) + 255) / 256;
+    h.out[0] = c.dq; h.out[1] = c.dk; h.out[2] = c.dv;
+    const long long rows = (long long)s.batch * s.heads * c.stat_stride, blocks = (rows + 16 * kStatRows - 1) / (16 * kStatRows);
+    const int share_blocks = (std::max(std::max(1, p.ctas[0] + p.ctas[1]), std::max(p.outers[0] * p.NB[0], p.outers[1] * p.NB[1])) + 255) / 256;
     if (blocks + share_blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     tile_grad_stat_kernel<><<<(unsigned)(blocks + share_blocks), 256, 0, st>>>(s, c.o, c.dout, c.lse, (int)c.stat_stride, const_cast<float2 *>(c.stat), h, share_blocks, c.status);
     ++*launches;

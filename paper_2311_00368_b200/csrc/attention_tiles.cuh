@@ -39,31 +39,6 @@ struct TileArgs {
     int *status;
 };
 
-// Bounded wait, asking again and again: the waits here are a few hundred cycles each and on the critical path of a step, and a try_wait
-// that may be parked for longer (ptx::mbar_wait) wakes late.
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity)
-{
-    {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
-    }
-    uint64_t t0 = 0;
-    for (uint32_t round = 0;; ++round) {
-#pragma unroll 1
-        for (int i = 0; i < 64; ++i) {
-            uint32_t ok;
-            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-            if (ok) return true;
-        }
-        const uint64_t t = ptx::global_timer_ns();
-        if (round == 0) t0 = t;
-        if (t - t0 > ptx::c_wait_limit_ns || round > (1u << 22)) return false;
-    }
-}
-
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1, int c2, int c3)
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -238,7 +213,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t tmem = ptx::lds32(slot);
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
         return ok;
     };
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
@@ -258,8 +233,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 load_tile<DP, 128>(base + C::V + st * C::TILE, &tm_v, v_full(st), cb * kTile, hkv * a.v.hm, b * a.v.bm);
             }
             if (!ok) {   // copies in flight land before the CTA ends
-                wait_for(q_full, 0);
-                for (int k = max(0, i - C::STAGES); k <= i; ++k) { wait_for(k_full(k % C::STAGES), k / C::STAGES & 1); if (k < i) wait_for(v_full(k % C::STAGES), k / C::STAGES & 1); }
+                ptx::mbar_wait(q_full, 0);
+                for (int k = max(0, i - C::STAGES); k <= i; ++k) { ptx::mbar_wait(k_full(k % C::STAGES), k / C::STAGES & 1); if (k < i) ptx::mbar_wait(v_full(k % C::STAGES), k / C::STAGES & 1); }
             }
         }
         __syncwarp();
@@ -280,7 +255,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 ptx::mma_commit(v_free(st));
             }
             ptx::mma_commit(o_full);
-            if (!ok) wait_for(o_full, 0);   // products in flight end before tensor memory is freed
+            if (!ok) ptx::mbar_wait(o_full, 0);   // products in flight end before tensor memory is freed
         }
         __syncwarp();
     } else {
@@ -576,7 +551,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     const int tiles = (int)min((long long)g.share, g.tiles - (long long)blockIdx.x * g.share), steps = 2 * tiles;
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {   // of a single thread
-        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
         return ok;
     };
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a whole warp
@@ -615,8 +590,8 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
             }
         }
         if (!ok) {   // copies in flight land before the CTA ends
-            if (blocks) wait_for(x_full, (blocks - 1) & 1);
-            for (int k = max(0, i - C::STAGES); k < i; ++k) wait_for(full(k % C::STAGES), k / C::STAGES & 1);
+            if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
+            for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
         }
     } else if (warp == FIRST_WARP) {
         if (ptx::elect_one()) {
@@ -636,7 +611,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
             }
             if (!ok) {   // products in flight end before tensor memory is freed
                 ptx::mma_commit(slot + 16);
-                wait_for(slot + 16, 0);
+                ptx::mbar_wait(slot + 16, 0);
             }
         }
         __syncwarp();
@@ -671,7 +646,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
             }
             if (!ok) {
                 ptx::mma_commit(slot + 24);
-                wait_for(slot + 24, 0);
+                ptx::mbar_wait(slot + 24, 0);
             }
         }
         __syncwarp();
@@ -800,67 +775,75 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     if (warp == FIRST_WARP) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
 }
 
-// Behind tile_grad_kernel, a CTA of eight warps per 32 rows of a block: zeros for a block without tiles; the parts of one that several shares hold, added
-// up in order; the rows of one whose sums are not finite, one by one.
-constexpr int kJoinRows = 32;
+// Behind tile_grad_kernel.  Four CTAs of eight warps per share but the first: if a block that begins in the share before goes on in this one, its parts are
+// added up in order, 32 rows a CTA; rows whose sums are not finite are taken one by one.  The CTAs also go through the flags of the blocks that
+// were finished in one share.
+constexpr int kJoinRows = 32, kJoinParts = kTile / kJoinRows;
+template <int MODE, int DP>
+__device__ __forceinline__ void tile_grad_rows(const GradArgs &g, int o, int blk, int r)
+{
+    const TileArgs &a = g.a;
+    const int b = o / g.w.outer, h = o % g.w.outer, row = blk * kTile + r;
+    if (MODE == kDq) rows_one_by_one<kGradQ, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
+    else rows_one_by_one<kGradKV, DP>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
+}
 template <int MODE, int DP>
 __global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgs g)
 {
-    constexpr int ACCS = MODE == kDkv ? 2 : 1, WIDE = ACCS * DP, LANES = WIDE / 4;   // lanes that a row takes
+    constexpr int ACCS = MODE == kDkv ? 2 : 1, WIDE = ACCS * DP, LANES = WIDE / 4;   // threads that a row takes
     const TileArgs &a = g.a;
     const Shape &s = a.g.s;
-    const int block = blockIdx.x / (kTile / kJoinRows), part = blockIdx.x % (kTile / kJoinRows);
-    const int o = block / g.w.NB, blk = block % g.w.NB, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rows = MODE == kDq ? s.M : s.K, b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
-    if (row0 >= rows) return;
-    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, n = g.w.ahead(o, blk + 1) - ahead;
-    const int c0 = (int)(p0 / g.share), c1 = (int)((p0 + n - 1) / g.share);
+    const int share = blockIdx.x / kJoinParts, part = blockIdx.x % kJoinParts, warp = threadIdx.x >> 5;
+    const int rows = MODE == kDq ? s.M : s.K;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const bool one = n > 0 && c0 == c1;
-    if (one && g.bad[block] == 0) return;
-    if (!one) {
-        __shared__ int redo;
-        if (threadIdx.x == 0) redo = 0;
-        __syncthreads();
-        // four elements a thread (of dK, then of dV), neighbouring rows in neighbouring threads
+    for (int block = blockIdx.x; block < g.w.outers * g.w.NB; block += gridDim.x)
+        if (g.bad[block])
+            for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DP>(g, block / g.w.NB, block % g.w.NB, r);
+    if (share == 0) return;
+    const int4 at = g.starts[share];
+    const int o = at.x, blk = at.y, b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
+    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, p1 = p0 + g.w.ahead(o, blk + 1) - ahead;
+    const int c0 = (int)(p0 / g.share), c1 = (int)((p1 - 1) / g.share);
+    if (c0 != share - 1 || row0 >= rows) return;   // (the block begins with this share, or began before the last one)
+    __shared__ int redo;
+    if (threadIdx.x == 0) redo = 0;
+    __syncthreads();
+    // four elements a thread (of dK, then of dV)
 #pragma unroll
-        for (int u = threadIdx.x; u < kJoinRows * LANES; u += 256) {
-            const int r = part * kJoinRows + u / LANES, e = u % LANES * 4, acc = e / DP, col = e % DP, row = blk * kTile + r;
-            if (row >= rows) continue;
-            float x[4] = {};
-            if (n > 0) {
-                const float *from = g.part + ((long long)acc * kTile + r) * DP + col;
+    for (int u = threadIdx.x; u < kJoinRows * LANES; u += 256) {
+        const int r = part * kJoinRows + u / LANES, e = u % LANES * 4, acc = e / DP, col = e % DP, row = blk * kTile + r;
+        if (row >= rows) continue;
+        float x[4] = {};
+        const float *from = g.part + ((long long)acc * kTile + r) * DP + col;
 #pragma unroll 4
-                for (int c = c0; c <= c1; ++c) {
-                    const float4 v = *reinterpret_cast<const float4 *>(from + ((long long)c * 2 + (c == c0)) * (ACCS * kTile * DP));
-                    x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
-                }
-            }
-            bool bad = false;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[k] *= acc ? 1.f : s.scale;
-                bad |= col + k < s.d && !(fabsf(x[k]) <= 3.402823466e38f);
-            }
-            store4<Bf16, 4>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x);
-            if (bad) redo = 1;
+        for (int c = c0; c <= c1; ++c) {
+            const float4 v = *reinterpret_cast<const float4 *>(from + ((long long)c * 2 + (c == c0)) * (ACCS * kTile * DP));
+            x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
         }
-        __syncthreads();
-        if (redo == 0) return;
+        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[k] *= acc ? 1.f : s.scale;
+            bad |= col + k < s.d && !(fabsf(x[k]) <= 3.402823466e38f);
+        }
+        store4<Bf16, 4>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x);
+        if (bad) redo = 1;
     }
-    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) {
-        if (MODE == kDq) rows_one_by_one<kGradQ, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + r, 1u, a.g.ptr_stride, a.g.idx_stride);
-        else rows_one_by_one<kGradKV, DP>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row0 + r, 1u, s.K + 1ll, a.g.idx_stride);
-    }
+    __syncthreads();
+    if (redo == 0) return;
+    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) tile_grad_rows<MODE, DP>(g, o, blk, part * kJoinRows + r);
 }
 
-// Ahead of both: row statistics (see attention_stat_kernel) and, in its last CTAs, where the shares begin; clears the flags of blocks.
+// Ahead of both: row statistics (see attention_stat_kernel); and, in the first CTAs, where the shares begin, cleared flags of the blocks, and zeros for
+// the blocks that have no tiles.
 struct ShareArgs {
     Tiles w[2];
-    int share[2], ctas[2], blocks[2];
+    int share[2], ctas[2], rows[2];
     int4 *starts[2];
     int *bad[2];
+    View<Bf16> out[3];   // dQ, dK, dV
 };
+constexpr int kStatRows = 4;   // rows of half a warp
 template <int DUMMY = 0>
 __global__ void __launch_bounds__(256) tile_grad_stat_kernel(Shape s, View<const Bf16> out, View<const Bf16> dout, const float *lse, int stat_rows, float2 *stat,
                                                              const __grid_constant__ ShareArgs h, int share_blocks, int *status)
@@ -868,38 +851,63 @@ __global__ void __launch_bounds__(256) tile_grad_stat_kernel(Shape s, View<const
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if ((int)blockIdx.x < share_blocks) {   // (first, as they wait longest)
-        const int u = blockIdx.x * 256 + threadIdx.x, total = h.ctas[0] + h.ctas[1];
+        const int u = blockIdx.x * 256 + threadIdx.x, lane = threadIdx.x & 31, total = h.ctas[0] + h.ctas[1];
         for (int i = u; i < total; i += share_blocks * 256) {
             const int k = i < h.ctas[0] ? 0 : 1, c = k ? i - h.ctas[0] : i;
             h.starts[k][c] = share_start(h.w[k], (long long)c * h.share[k]);
         }
-        for (int k = 0; k < 2; ++k)
-            for (int i = u; i < h.blocks[k]; i += share_blocks * 256) h.bad[k][i] = 0;
+        for (int k = 0; k < 2; ++k) {
+            const Tiles &w = h.w[k];
+            for (int i0 = u - lane; i0 < w.outers * w.NB; i0 += share_blocks * 256) {
+                const int i = i0 + lane, o = i / w.NB, blk = i % w.NB;
+                bool none = false;
+                if (i < w.outers * w.NB) {
+                    h.bad[k][i] = 0;
+                    none = w.ahead(o, blk + 1) == w.ahead(o, blk);
+                }
+                for (unsigned left = __ballot_sync(~0u, none); left; left &= left - 1) {
+                    const int z = i0 + __ffs(left) - 1, zo = z / w.NB, z0 = z % w.NB * kTile, n = min(kTile, h.rows[k] - z0), wide = s.d / 8;
+                    for (int e = lane; e < n * wide; e += 32)
+                        for (int x = k; x < (k ? 3 : 1); ++x)
+                            *reinterpret_cast<uint4 *>(h.out[x].at(zo / w.outer, zo % w.outer, z0 + e / wide) + e % wide * 8) = make_uint4(0, 0, 0, 0);
+                }
+            }
+        }
         return;
     }
-    // half a warp per row, eight elements a lane
-    const int half = threadIdx.x & 15;
-    const long long unit = (blockIdx.x - share_blocks) * 16ll + (threadIdx.x >> 4);
-    const long long prob = unit / stat_rows;
+    // half a warp per row, eight elements a lane, four rows at once
+    const int half = threadIdx.x & 15, c = half * 8;
+    const long long first = ((blockIdx.x - share_blocks) * 16ll + (threadIdx.x >> 4)) * kStatRows;   // (a problem has a multiple of 128 rows)
+    const long long prob = first / stat_rows;
     if (prob >= (long long)s.batch * s.heads) return;
-    const int row = (int)(unit % stat_rows), b = (int)(prob / s.heads), head = (int)(prob % s.heads);
-    float sum = 0.f, top = -CUDART_INF_F;
-    if (row < s.M) {
-        top = lse[prob * s.M + row];
-        const int c = half * 8;
-        if (c < s.d) {
-            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(out.at(b, head, row) + c)), y = __ldg(reinterpret_cast<const uint4 *>(dout.at(b, head, row) + c));
-            const unsigned u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+    const int row0 = (int)(first - prob * stat_rows), b = (int)(prob / s.heads), head = (int)(prob % s.heads);
+    uint4 x[kStatRows], y[kStatRows];
+    float top[kStatRows];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                sum = fmaf(__uint_as_float(u[k] << 16), __uint_as_float(v[k] << 16), sum);
-                sum = fmaf(__uint_as_float(u[k] & 0xffff0000u), __uint_as_float(v[k] & 0xffff0000u), sum);
+    for (int k = 0; k < kStatRows; ++k) {
+        x[k] = y[k] = make_uint4(0, 0, 0, 0);
+        top[k] = -CUDART_INF_F;
+        if (row0 + k < s.M) {
+            top[k] = lse[prob * s.M + row0 + k];
+            if (c < s.d) {
+                x[k] = __ldg(reinterpret_cast<const uint4 *>(out.at(b, head, row0 + k) + c));
+                y[k] = __ldg(reinterpret_cast<const uint4 *>(dout.at(b, head, row0 + k) + c));
             }
         }
     }
 #pragma unroll
-    for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    if (half == 0) stat[unit] = top == -CUDART_INF_F ? make_float2(-CUDART_INF_F, 0.f) : make_float2(-top * kLog2e, -sum);
+    for (int k = 0; k < kStatRows; ++k) {
+        const unsigned u[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, v[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sum = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), sum);
+            sum = fmaf(__uint_as_float(u[i] & 0xffff0000u), __uint_as_float(v[i] & 0xffff0000u), sum);
+        }
+#pragma unroll
+        for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        if (half == 0) stat[first + k] = top[k] == -CUDART_INF_F ? make_float2(-CUDART_INF_F, 0.f) : make_float2(-top[k] * kLog2e, -sum);
+    }
 }
 
 }  // namespace attn
