@@ -92,8 +92,8 @@ template <int DP> b2sp_status forward(const TileCall &c, cudaStream_t st, int *l
     TileArgs a = args(c);
     a.g.out1 = c.out; a.g.rows = c.s.M;
     CUtensorMap q, k, v;
-    if (!make_map(&q, c.q, c.s.batch, c.s.heads, c.s.M, c.s.d, 128, &a.q) || !make_map(&k, c.k, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 128, &a.k) ||
-        !make_map(&v, c.v, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 128, &a.v) || !allow_smem(tile_forward_kernel<DP>, FwdCfg<DP>::BYTES, done))
+    if (!make_map(&q, c.q, c.s.batch, c.s.heads, c.s.M, c.s.d, 128, &a.q) || !make_map(&k, c.k, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 64, &a.k) ||
+        !make_map(&v, c.v, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 64, &a.v) || !allow_smem(tile_forward_kernel<DP>, FwdCfg<DP>::BYTES, done))
         return B2SP_ERR_CUDA;
     const long long blocks = (long long)c.s.batch * c.s.heads * c.plan.RB;
     if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;

@@ -160,10 +160,12 @@ __device__ __noinline__ void rows_one_by_one(const RowArgs<Bf16> &g, const int *
 constexpr int kTileThreads = 192;   // four softmax warps, a TMA warp, an MMA warp
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------------
+// A CTA per (problem, row block), two per SM; 64 keys a step.  S has two buffers in tensor memory, so that the products of the next step are
+// there when the softmax warps come to it; the weights (bfloat16) lie over the S that they come from.
 template <int DP> struct FwdCfg {
-    static constexpr int STAGES = DP == 64 ? 2 : 1;
-    static constexpr int TILE = 128 * DP * 2;
-    static constexpr int Q = 0, K = TILE, V = K + STAGES * TILE, BAR = V + STAGES * TILE, BYTES = BAR + 256 + 1024;
+    static constexpr int STAGES = DP == 64 ? 4 : 2;
+    static constexpr int TILE = 128 * DP * 2, HALF = 64 * DP * 2;
+    static constexpr int Q = 0, K = TILE, V = K + STAGES * HALF, BAR = V + STAGES * HALF, BYTES = BAR + 256 + 1024;
     static constexpr uint32_t COL_S = 0, COL_O = 128, COLS = 256;
 };
 
@@ -176,21 +178,23 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     extern __shared__ uint8_t raw[];
     const uint32_t base = (ptx::smem_u32(raw) + 1023u) & ~1023u, bars = base + C::BAR;
     auto k_full = [&](int s) { return bars + 8u * s; };
-    auto k_free = [&](int s) { return bars + 16u + 8u * s; };
-    auto v_full = [&](int s) { return bars + 32u + 8u * s; };
-    auto v_free = [&](int s) { return bars + 48u + 8u * s; };
-    const uint32_t q_full = bars + 64, s_full = bars + 72, p_full = bars + 80, o_full = bars + 88, slot = bars + 96;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto k_free = [&](int s) { return bars + 32u + 8u * s; };
+    auto v_full = [&](int s) { return bars + 64u + 8u * s; };
+    auto v_free = [&](int s) { return bars + 96u + 8u * s; };
+    auto s_full = [&](int b) { return bars + 128u + 8u * b; };
+    auto p_full = [&](int b) { return bars + 144u + 8u * b; };   // (one per buffer: a fast warp may be a step ahead of a slow one)
+    const uint32_t q_full = bars + 160, o_full = bars + 168, slot = bars + 176;   // o_full: after every step's second product
+    const int warp = threadIdx.x >> 5;
     const Shape &s = a.g.s;
     const int problems = s.batch * s.heads, RB = a.plan.RB;
     const int prob = blockIdx.x % problems, rb = RB - 1 - blockIdx.x / problems;   // (a causal mask's longest rows first)
     const int b = prob / s.heads, h = prob % s.heads, hkv = h / (s.heads / s.kv_heads);
     const int pat = pattern_of(s.patterns, s.batch, s.heads, b, h);
-    const int t0 = a.plan.rb_ptr[pat * RB + rb], nt = a.plan.rb_ptr[pat * RB + rb + 1] - t0;
+    const int t0 = a.plan.rb_ptr[pat * RB + rb], steps = 2 * (a.plan.rb_ptr[pat * RB + rb + 1] - t0);
     const int row = rb * kTile + threadIdx.x;   // of a softmax thread
     float *lse = a.g.lse + (long long)prob * s.M;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-    if (nt == 0) {
+    if (steps == 0) {
         if (threadIdx.x < 128 && row < s.M) {
             Bf16 *o = a.g.out1.at(b, h, row);
             for (int c = 0; c < s.d; c += 8) *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
@@ -203,7 +207,9 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             ptx::mbar_init(k_full(i), 1); ptx::mbar_init(k_free(i), 1);
             ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_free(i), 1);
         }
-        ptx::mbar_init(q_full, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(p_full, 128); ptx::mbar_init(o_full, 1);
+        ptx::mbar_init(s_full(0), 1); ptx::mbar_init(s_full(1), 1);
+        ptx::mbar_init(q_full, 1); ptx::mbar_init(p_full(0), 128); ptx::mbar_init(p_full(1), 128); ptx::mbar_init(o_full, 1);
+        ptx::mbar_init(slot + 8, 1);   // only for leaving early
         ptx::fence_mbar_init();
     }
     if (warp == 5) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
@@ -221,120 +227,136 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (ptx::elect_one()) {
             ptx::mbar_arrive_expect_tx(q_full, C::TILE);
             load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
-            int i = 0, next = a.plan.tile_cb[t0];
-            for (; i < nt; ++i) {
-                const int st = i % C::STAGES, ph = i / C::STAGES & 1, cb = next;
-                if (i + 1 < nt) next = a.plan.tile_cb[t0 + i + 1];
+            int i = 0, now = 0, next = a.plan.tile_cb[t0];
+            bool half_done = false;
+            for (; i < steps; ++i) {
+                if (!(i & 1)) {
+                    now = next * kTile;
+                    if (i + 2 < steps) next = a.plan.tile_cb[t0 + (i >> 1) + 1];
+                }
+                const int st = i % C::STAGES, ph = i / C::STAGES & 1, at = now + (i & 1) * 64;
+                half_done = false;
                 if (!wait(k_free(st), ph ^ 1)) break;
-                ptx::mbar_arrive_expect_tx(k_full(st), C::TILE);
-                load_tile<DP, 128>(base + C::K + st * C::TILE, &tm_k, k_full(st), cb * kTile, hkv * a.k.hm, b * a.k.bm);
+                ptx::mbar_arrive_expect_tx(k_full(st), C::HALF);
+                load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at, hkv * a.k.hm, b * a.k.bm);
+                half_done = true;
                 if (!wait(v_free(st), ph ^ 1)) break;
-                ptx::mbar_arrive_expect_tx(v_full(st), C::TILE);
-                load_tile<DP, 128>(base + C::V + st * C::TILE, &tm_v, v_full(st), cb * kTile, hkv * a.v.hm, b * a.v.bm);
+                ptx::mbar_arrive_expect_tx(v_full(st), C::HALF);
+                load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at, hkv * a.v.hm, b * a.v.bm);
             }
             if (!ok) {   // copies in flight land before the CTA ends
                 ptx::mbar_wait(q_full, 0);
-                for (int k = max(0, i - C::STAGES); k <= i; ++k) { ptx::mbar_wait(k_full(k % C::STAGES), k / C::STAGES & 1); if (k < i) ptx::mbar_wait(v_full(k % C::STAGES), k / C::STAGES & 1); }
+                for (int k = max(0, i - C::STAGES); k < i; ++k) { ptx::mbar_wait(k_full(k % C::STAGES), k / C::STAGES & 1); ptx::mbar_wait(v_full(k % C::STAGES), k / C::STAGES & 1); }
+                if (half_done) ptx::mbar_wait(k_full(i % C::STAGES), i / C::STAGES & 1);
             }
         }
         __syncwarp();
     } else if (warp == 5) {
         if (ptx::elect_one()) {
             const int ks = (s.d + 15) >> 4;
-            wait(q_full, 0);
-            for (int i = 0; i < nt; ++i) {
-                const int st = i % C::STAGES, ph = i / C::STAGES & 1;
-                if (!wait(k_full(st), ph)) break;
-                // (S of this tile overwrites the weights of the last: the tensor core takes its products in order)
-                product_columns<DP, 128>(tmem + C::COL_S, desc_columns(base + C::Q), desc_columns(base + C::K + st * C::TILE), ks);
+            const uint32_t q = desc_columns(base + C::Q), k0 = desc_columns(base + C::K), v0 = desc_rows<64>(base + C::V);
+            auto first = [&](int i) {
+                const int st = i % C::STAGES;
+                product_columns<DP, 64>(tmem + C::COL_S + (i & 1) * 64, q, k0 + st * (C::HALF >> 4), ks);
                 ptx::mma_commit(k_free(st));
-                ptx::mma_commit(s_full);
-                if (!wait(p_full, i & 1) || !wait(v_full(st), ph)) break;
+                ptx::mma_commit(s_full(i & 1));
+            };
+            wait(q_full, 0);
+            for (int i = 0; i < 2 && i < steps; ++i)
+                if (wait(k_full(i % C::STAGES), 0)) first(i);
+            for (int i = 0; i < steps && ok; ++i) {
+                const int st = i % C::STAGES, n = i + 2;
+                // everything that the next products wait for, so that both are issued as soon as the weights are there
+                if (!wait(v_full(st), i / C::STAGES & 1)) break;
+                if (n < steps && !wait(k_full(n % C::STAGES), n / C::STAGES & 1)) break;
+                if (!wait(p_full(i & 1), i >> 1 & 1)) break;
                 ptx::tc_fence_after_sync();
-                product_rows<DP, 128>(tmem + C::COL_O, tmem + C::COL_S, desc_rows<128>(base + C::V + st * C::TILE), i > 0);
+                product_rows<DP, 64>(tmem + C::COL_O, tmem + C::COL_S + (i & 1) * 64, v0 + st * (C::HALF >> 4), i > 0);
                 ptx::mma_commit(v_free(st));
+                ptx::mma_commit(o_full);
+                if (n < steps) first(n);   // (over the weights just taken: the tensor core takes one thread's products in order)
             }
-            ptx::mma_commit(o_full);
-            if (!ok) ptx::mbar_wait(o_full, 0);   // products in flight end before tensor memory is freed
+            if (!ok) {   // products in flight end before tensor memory is freed
+                ptx::mma_commit(slot + 8);
+                ptx::mbar_wait(slot + 8, 0);
+            }
         }
         __syncwarp();
     } else {
         const float c2 = s.scale * kLog2e;
         const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
         const uint4 *mask = a.plan.masks + (long long)t0 * kTile + threadIdx.x;
-        uint4 bits = __ldg(mask);
+        uint4 bits = __ldg(mask), now = bits;
         float ref = 0.f;                       // reference of the exponentials, of the products before scaling
         uint64_t sums = two(0.f, 0.f);
+        const uint64_t f2 = two(c2, c2);
         unsigned some = 0;
-        for (int i = 0; i < nt; ++i) {
-            const uint4 now = bits;
-            if (i + 1 < nt) bits = __ldg(mask + (long long)(i + 1) * kTile);
-            some |= now.x | now.y | now.z | now.w;
-            if (!wait_all(s_full, i & 1)) break;
-            ptx::tc_fence_after_sync();
-            float top = -CUDART_INF_F;
-            {
-                uint32_t x[2][32];
-                ptx::tmem_ld_32x32(mine + C::COL_S, x[0]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    ptx::tmem_ld_wait();
-                    settle(x[c & 1]);
-                    if (c < 3) ptx::tmem_ld_32x32(mine + C::COL_S + 32 * (c + 1), x[(c + 1) & 1]);
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) top = fmaxf(top, __uint_as_float(x[c & 1][k]));
-                }
+        for (int i = 0; i < steps; ++i) {
+            if (!(i & 1)) {
+                now = bits;
+                some |= now.x | now.y | now.z | now.w;
+                if (i + 2 < steps) bits = __ldg(mask + (long long)((i >> 1) + 1) * kTile);
             }
-            const bool move = i == 0 || (top - ref) * c2 > 8.f;
-            if (__any_sync(~0u, move)) {
-                const float to = top == -CUDART_INF_F ? 0.f : i == 0 ? top : fmaxf(top, ref), fall = i == 0 ? 0.f : ex2((ref - to) * c2);
-                ref = to;
-                sums = mul2(sums, two(fall, fall));
-                if (i) {
-                    const uint64_t f2 = two(fall, fall);
-#pragma unroll 1
-                    for (int c = 0; c < DP; c += 32) {
-                        uint32_t x[32];
-                        ptx::tmem_ld_32x32(mine + C::COL_O + c, x);
-                        ptx::tmem_ld_wait();
-                        settle(x);
+            const uint32_t from = mine + C::COL_S + (i & 1) * 64;
+            if (!wait_all(s_full(i & 1), i >> 1 & 1)) break;
+            ptx::tc_fence_after_sync();
+            uint32_t x[2][32];
+            ptx::tmem_ld_32x32(from, x[0]);
+            ptx::tmem_ld_32x32(from + 32, x[1]);
+            ptx::tmem_ld_wait();
+            settle(x[0]);
+            settle(x[1]);
+            float top = -CUDART_INF_F;
 #pragma unroll
-                        for (int k = 0; k < 32; k += 2) {
+            for (int k = 0; k < 32; ++k) top = fmaxf(top, fmaxf(__uint_as_float(x[0][k]), __uint_as_float(x[1][k])));
+            if (__any_sync(~0u, i == 0 || (top - ref) * c2 > 8.f)) {
+                const float to = top == -CUDART_INF_F ? ref : i == 0 ? top : fmaxf(top, ref), fall = i == 0 ? 0.f : ex2((ref - to) * c2);
+                ref = to;
+                const uint64_t fall2 = two(fall, fall);
+                sums = mul2(sums, fall2);
+                if (i) {
+                    if (!wait_all(o_full, (i - 1) & 1)) break;   // the last step's second product
+                    ptx::tc_fence_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < DP; c += 16) {
+                        uint32_t y[16];
+                        ptx::tmem_ld_32x16(mine + C::COL_O + c, y);
+                        ptx::tmem_ld_wait();
+                        settle(y);
+#pragma unroll
+                        for (int k = 0; k < 16; k += 2) {
                             float y0, y1;
-                            split(mul2(two(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2), y0, y1);
-                            x[k] = __float_as_uint(y0);
-                            x[k + 1] = __float_as_uint(y1);
+                            split(mul2(two(__uint_as_float(y[k]), __uint_as_float(y[k + 1])), fall2), y0, y1);
+                            y[k] = __float_as_uint(y0);
+                            y[k + 1] = __float_as_uint(y1);
                         }
-                        ptx::tmem_st_32x32(mine + C::COL_O + c, x);
+                        ptx::tmem_st_32x16(mine + C::COL_O + c, y);
                     }
                 }
             }
-            const uint64_t f2 = two(c2, c2), r2 = two(-ref * c2, -ref * c2);
-            uint32_t x[2][32];
-            ptx::tmem_ld_32x32(mine + C::COL_S, x[0]);
+            const uint64_t r2 = two(-ref * c2, -ref * c2);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                ptx::tmem_ld_wait();
-                settle(x[c & 1]);
-                if (c < 3) ptx::tmem_ld_32x32(mine + C::COL_S + 32 * (c + 1), x[(c + 1) & 1]);
-                const uint32_t w = c == 0 ? now.x : c == 1 ? now.y : c == 2 ? now.z : now.w;
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t m = (i & 1) ? (c ? now.w : now.z) : (c ? now.y : now.x);
                 uint32_t p[16];
 #pragma unroll
                 for (int k = 0; k < 32; k += 2) {
                     float y0, y1;
-                    split(fma2(two(__uint_as_float(x[c & 1][k]), __uint_as_float(x[c & 1][k + 1])), f2, r2), y0, y1);
-                    y0 = w >> k & 1 ? ex2(y0) : 0.f;
-                    y1 = w >> (k + 1) & 1 ? ex2(y1) : 0.f;
+                    split(fma2(two(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), f2, r2), y0, y1);
+                    y0 = m >> k & 1 ? ex2(y0) : 0.f;
+                    y1 = m >> (k + 1) & 1 ? ex2(y1) : 0.f;
                     sums = add2(sums, two(y0, y1));
                     p[k >> 1] = bf16x2(y0, y1);
                 }
-                ptx::tmem_st_32x16(mine + C::COL_S + 16 * c, p);   // over columns of S that are read already
+                ptx::tmem_st_32x16(from + 16 * c, p);
             }
             ptx::tmem_st_wait();
             ptx::tc_fence_before_sync();
-            ptx::mbar_arrive(p_full);
+            ptx::mbar_arrive(p_full(i & 1));
         }
-        wait_all(o_full, 0);
+        // (S of the last step was there, so the second product of the step before last but one is done: a wait by parity may be one phase behind)
+        wait_all(o_full, (steps - 2) & 1);
+        wait_all(o_full, (steps - 1) & 1);
         ptx::tc_fence_after_sync();
         float l, l1;
         split(sums, l, l1);
