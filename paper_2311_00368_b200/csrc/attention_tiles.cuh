@@ -39,6 +39,15 @@ struct TileArgs {
     int *status;
 };
 
+// Bounded wait that asks for a complete phase with a test first (36 cycles; the try_wait of ptx::mbar_wait answers in 92).
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0 || ptx::mbar_wait(bar, parity);
+}
+
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1, int c2, int c3)
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -163,9 +172,10 @@ constexpr int kTileThreads = 192;   // four softmax warps, a TMA warp, an MMA wa
 // A CTA per (problem, row block), two per SM; 64 keys a step.  S has two buffers in tensor memory, so that the products of the next step are
 // there when the softmax warps come to it; the weights (bfloat16) lie over the S that they come from.
 template <int DP> struct FwdCfg {
-    static constexpr int STAGES = DP == 64 ? 4 : 2;
+    static constexpr int KSTAGES = DP == 64 ? 4 : 3, VSTAGES = DP == 64 ? 4 : 2;   // (K is read two steps ahead of V)
     static constexpr int TILE = 128 * DP * 2, HALF = 64 * DP * 2;
-    static constexpr int Q = 0, K = TILE, V = K + STAGES * HALF, BAR = V + STAGES * HALF, BYTES = BAR + 256 + 1024;
+    // (without room to align in: two CTAs at width 128 take all of an SM's shared memory, which begins on a multiple of 1024 bytes)
+    static constexpr int Q = 0, K = TILE, V = K + KSTAGES * HALF, BAR = V + VSTAGES * HALF, BYTES = BAR + 256;
     static constexpr uint32_t COL_S = 0, COL_O = 128, COLS = 256;
 };
 
@@ -175,8 +185,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const __grid_constant__ TileArgs a)
 {
     using C = FwdCfg<DP>;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (ptx::smem_u32(raw) + 1023u) & ~1023u, bars = base + C::BAR;
+    extern __shared__ __align__(1024) uint8_t aligned_raw[];
+    const uint32_t base = ptx::smem_u32(aligned_raw), bars = base + C::BAR;
     auto k_full = [&](int s) { return bars + 8u * s; };
     auto k_free = [&](int s) { return bars + 32u + 8u * s; };
     auto v_full = [&](int s) { return bars + 64u + 8u * s; };
@@ -203,10 +213,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return;
     }
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) {
-            ptx::mbar_init(k_full(i), 1); ptx::mbar_init(k_free(i), 1);
-            ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_free(i), 1);
-        }
+        for (int i = 0; i < C::KSTAGES; ++i) { ptx::mbar_init(k_full(i), 1); ptx::mbar_init(k_free(i), 1); }
+        for (int i = 0; i < C::VSTAGES; ++i) { ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_free(i), 1); }
         ptx::mbar_init(s_full(0), 1); ptx::mbar_init(s_full(1), 1);
         ptx::mbar_init(q_full, 1); ptx::mbar_init(p_full(0), 128); ptx::mbar_init(p_full(1), 128); ptx::mbar_init(o_full, 1);
         ptx::mbar_init(slot + 8, 1);   // only for leaving early
@@ -219,7 +227,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t tmem = ptx::lds32(slot);
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
         return ok;
     };
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
@@ -227,27 +235,30 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (ptx::elect_one()) {
             ptx::mbar_arrive_expect_tx(q_full, C::TILE);
             load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
-            int i = 0, now = 0, next = a.plan.tile_cb[t0];
-            bool half_done = false;
-            for (; i < steps; ++i) {
-                if (!(i & 1)) {
-                    now = next * kTile;
-                    if (i + 2 < steps) next = a.plan.tile_cb[t0 + (i >> 1) + 1];
+            // K runs ahead of V by the stages that it has more
+            constexpr int AHEAD = C::KSTAGES - C::VSTAGES;
+            int ik = 0, iv = 0;
+            auto key = [&](int i) { return a.plan.tile_cb[t0 + (i >> 1)] * kTile + (i & 1) * 64; };
+            int at_k = key(0), at_v = at_k;
+            while (iv < steps) {
+                if (ik < steps && ik <= iv + AHEAD) {
+                    const int st = ik % C::KSTAGES;
+                    if (!wait(k_free(st), (ik / C::KSTAGES & 1) ^ 1)) break;
+                    ptx::mbar_arrive_expect_tx(k_full(st), C::HALF);
+                    load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at_k, hkv * a.k.hm, b * a.k.bm);
+                    if (++ik < steps) at_k = key(ik);
+                } else {
+                    const int st = iv % C::VSTAGES;
+                    if (!wait(v_free(st), (iv / C::VSTAGES & 1) ^ 1)) break;
+                    ptx::mbar_arrive_expect_tx(v_full(st), C::HALF);
+                    load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at_v, hkv * a.v.hm, b * a.v.bm);
+                    if (++iv < steps) at_v = key(iv);
                 }
-                const int st = i % C::STAGES, ph = i / C::STAGES & 1, at = now + (i & 1) * 64;
-                half_done = false;
-                if (!wait(k_free(st), ph ^ 1)) break;
-                ptx::mbar_arrive_expect_tx(k_full(st), C::HALF);
-                load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at, hkv * a.k.hm, b * a.k.bm);
-                half_done = true;
-                if (!wait(v_free(st), ph ^ 1)) break;
-                ptx::mbar_arrive_expect_tx(v_full(st), C::HALF);
-                load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at, hkv * a.v.hm, b * a.v.bm);
             }
             if (!ok) {   // copies in flight land before the CTA ends
                 ptx::mbar_wait(q_full, 0);
-                for (int k = max(0, i - C::STAGES); k < i; ++k) { ptx::mbar_wait(k_full(k % C::STAGES), k / C::STAGES & 1); ptx::mbar_wait(v_full(k % C::STAGES), k / C::STAGES & 1); }
-                if (half_done) ptx::mbar_wait(k_full(i % C::STAGES), i / C::STAGES & 1);
+                for (int k = max(0, ik - C::KSTAGES); k < ik; ++k) ptx::mbar_wait(k_full(k % C::KSTAGES), k / C::KSTAGES & 1);
+                for (int k = max(0, iv - C::VSTAGES); k < iv; ++k) ptx::mbar_wait(v_full(k % C::VSTAGES), k / C::VSTAGES & 1);
             }
         }
         __syncwarp();
@@ -256,19 +267,19 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const int ks = (s.d + 15) >> 4;
             const uint32_t q = desc_columns(base + C::Q), k0 = desc_columns(base + C::K), v0 = desc_rows<64>(base + C::V);
             auto first = [&](int i) {
-                const int st = i % C::STAGES;
+                const int st = i % C::KSTAGES;
                 product_columns<DP, 64>(tmem + C::COL_S + (i & 1) * 64, q, k0 + st * (C::HALF >> 4), ks);
                 ptx::mma_commit(k_free(st));
                 ptx::mma_commit(s_full(i & 1));
             };
             wait(q_full, 0);
             for (int i = 0; i < 2 && i < steps; ++i)
-                if (wait(k_full(i % C::STAGES), 0)) first(i);
+                if (wait(k_full(i % C::KSTAGES), 0)) first(i);
             for (int i = 0; i < steps && ok; ++i) {
-                const int st = i % C::STAGES, n = i + 2;
+                const int st = i % C::VSTAGES, n = i + 2;
                 // everything that the next products wait for, so that both are issued as soon as the weights are there
-                if (!wait(v_full(st), i / C::STAGES & 1)) break;
-                if (n < steps && !wait(k_full(n % C::STAGES), n / C::STAGES & 1)) break;
+                if (!wait(v_full(st), i / C::VSTAGES & 1)) break;
+                if (n < steps && !wait(k_full(n % C::KSTAGES), n / C::KSTAGES & 1)) break;
                 if (!wait(p_full(i & 1), i >> 1 & 1)) break;
                 ptx::tc_fence_after_sync();
                 product_rows<DP, 64>(tmem + C::COL_O, tmem + C::COL_S + (i & 1) * 64, v0 + st * (C::HALF >> 4), i > 0);
@@ -306,9 +317,12 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             ptx::tmem_ld_wait();
             settle(x[0]);
             settle(x[1]);
-            float top = -CUDART_INF_F;
+            float tops[4];   // (four chains: one is 32 dependent steps)
 #pragma unroll
-            for (int k = 0; k < 32; ++k) top = fmaxf(top, fmaxf(__uint_as_float(x[0][k]), __uint_as_float(x[1][k])));
+            for (int k = 0; k < 4; ++k) tops[k] = fmaxf(__uint_as_float(x[0][k]), __uint_as_float(x[1][k]));
+#pragma unroll
+            for (int k = 4; k < 32; ++k) tops[k & 3] = fmaxf(tops[k & 3], fmaxf(__uint_as_float(x[0][k]), __uint_as_float(x[1][k])));
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
             if (__any_sync(~0u, i == 0 || (top - ref) * c2 > 8.f)) {
                 const float to = top == -CUDART_INF_F ? ref : i == 0 ? top : fmaxf(top, ref), fall = i == 0 ? 0.f : ex2((ref - to) * c2);
                 ref = to;
@@ -573,7 +587,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     const int tiles = (int)min((long long)g.share, g.tiles - (long long)blockIdx.x * g.share), steps = 2 * tiles;
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {   // of a single thread
-        if (ok && !ptx::mbar_wait(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
         return ok;
     };
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a whole warp
