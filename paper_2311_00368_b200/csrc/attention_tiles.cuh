@@ -216,7 +216,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         for (int i = 0; i < C::KSTAGES; ++i) { ptx::mbar_init(k_full(i), 1); ptx::mbar_init(k_free(i), 1); }
         for (int i = 0; i < C::VSTAGES; ++i) { ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_free(i), 1); }
         ptx::mbar_init(s_full(0), 1); ptx::mbar_init(s_full(1), 1);
-        ptx::mbar_init(q_full, 1); ptx::mbar_init(p_full(0), 128); ptx::mbar_init(p_full(1), 128); ptx::mbar_init(o_full, 1);
+        ptx::mbar_init(q_full, 1); ptx::mbar_init(p_full(0), 4); ptx::mbar_init(p_full(1), 4); ptx::mbar_init(o_full, 1);
         ptx::mbar_init(slot + 8, 1);   // only for leaving early
         ptx::fence_mbar_init();
     }
@@ -352,13 +352,19 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const uint32_t m = (i & 1) ? (c ? now.w : now.z) : (c ? now.y : now.x);
+                // all exponentials first, masked ones too (the reference bounds them): a chain per element that waits for its exponential
+                // is what the loop otherwise becomes
                 uint32_t p[16];
+                float e[32];
 #pragma unroll
                 for (int k = 0; k < 32; k += 2) {
-                    float y0, y1;
-                    split(fma2(two(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), f2, r2), y0, y1);
-                    y0 = m >> k & 1 ? ex2(y0) : 0.f;
-                    y1 = m >> (k + 1) & 1 ? ex2(y1) : 0.f;
+                    split(fma2(two(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), f2, r2), e[k], e[k + 1]);
+                    e[k] = ex2(e[k]);
+                    e[k + 1] = ex2(e[k + 1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    const float y0 = m >> k & 1 ? e[k] : 0.f, y1 = m >> (k + 1) & 1 ? e[k + 1] : 0.f;
                     sums = add2(sums, two(y0, y1));
                     p[k >> 1] = bf16x2(y0, y1);
                 }
@@ -366,7 +372,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
             ptx::tmem_st_wait();
             ptx::tc_fence_before_sync();
-            ptx::mbar_arrive(p_full(i & 1));
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(p_full(i & 1));   // (one arrival per warp: 32 on one word take turns)
         }
         // (S of the last step was there, so the second product of the step before last but one is done: a wait by parity may be one phase behind)
         wait_all(o_full, (steps - 2) & 1);
@@ -573,8 +580,8 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
-        for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 256); ptx::mbar_init(s_free(i), 1); }
-        ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1); ptx::mbar_init(o_full, 1); ptx::mbar_init(o_free, 256 * SETS);
+        for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 8); ptx::mbar_init(s_free(i), 1); }
+        ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1); ptx::mbar_init(o_full, 1); ptx::mbar_init(o_free, 8 * SETS);
         ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // only for leaving early
         ptx::fence_mbar_init();
     }
@@ -753,7 +760,8 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
                 }
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before_sync();
-                ptx::mbar_arrive(p_full(set));
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(p_full(set));   // (one arrival per warp: 32 on one word take turns)
             }
             const int last_i = w.i;
             const bool ended = w.t + 1 == w.t1;   // of the query head's tiles
@@ -801,7 +809,8 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
             }
             if (bad) g.bad[(long long)o * g.w.NB + blk] = 1;
             ptx::tc_fence_before_sync();
-            ptx::mbar_arrive(o_free);
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(o_free);
             ++blocks;
         }
     }
