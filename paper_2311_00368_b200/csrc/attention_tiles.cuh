@@ -171,6 +171,8 @@ constexpr int kTileThreads = 192;   // four softmax warps, a TMA warp, an MMA wa
 // ---- forward ---------------------------------------------------------------------------------------------------------------------
 // A CTA per (problem, row block), two per SM; 64 keys a step.  S has two buffers in tensor memory, so that the products of the next step are
 // there when the softmax warps come to it; the weights (bfloat16) lie over the S that they come from.
+// Not kept: eight softmax warps with 32 keys each, which tell each other their largest products (eight problems of 4096 x 4096 at 20%, d = 64:
+// 63 -> 70 us), and the next step's products fetched and compared among the exponentials of this one (64 -> 70 us, 168 registers).
 template <int DP> struct FwdCfg {
     static constexpr int KSTAGES = DP == 64 ? 4 : 3, VSTAGES = DP == 64 ? 4 : 2;   // (K is read two steps ahead of V)
     static constexpr int TILE = 128 * DP * 2, HALF = 64 * DP * 2;
@@ -193,7 +195,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     auto v_free = [&](int s) { return bars + 96u + 8u * s; };
     auto s_full = [&](int b) { return bars + 128u + 8u * b; };
     auto p_full = [&](int b) { return bars + 144u + 8u * b; };   // (one per buffer: a fast warp may be a step ahead of a slow one)
-    const uint32_t q_full = bars + 160, o_full = bars + 168, slot = bars + 176;   // o_full: after every step's second product
+    const uint32_t q_full = bars + 160, o_full = bars + 168, slot = bars + 176, done = bars + 192;   // o_full: after every step's second product; done: after the last
     const int warp = threadIdx.x >> 5;
     const Shape &s = a.g.s;
     const int problems = s.batch * s.heads, RB = a.plan.RB;
@@ -217,6 +219,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         for (int i = 0; i < C::VSTAGES; ++i) { ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_free(i), 1); }
         ptx::mbar_init(s_full(0), 1); ptx::mbar_init(s_full(1), 1);
         ptx::mbar_init(q_full, 1); ptx::mbar_init(p_full(0), 4); ptx::mbar_init(p_full(1), 4); ptx::mbar_init(o_full, 1);
+        ptx::mbar_init(done, 1);
         ptx::mbar_init(slot + 8, 1);   // only for leaving early
         ptx::fence_mbar_init();
     }
@@ -285,6 +288,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 product_rows<DP, 64>(tmem + C::COL_O, tmem + C::COL_S + (i & 1) * 64, v0 + st * (C::HALF >> 4), i > 0);
                 ptx::mma_commit(v_free(st));
                 ptx::mma_commit(o_full);
+                if (i + 1 == steps) ptx::mma_commit(done);   // (a warp may come too late to tell the last phase of o_full from the one before)
                 if (n < steps) first(n);   // (over the weights just taken: the tensor core takes one thread's products in order)
             }
             if (!ok) {   // products in flight end before tensor memory is freed
@@ -375,9 +379,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             __syncwarp();
             if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(p_full(i & 1));   // (one arrival per warp: 32 on one word take turns)
         }
-        // (S of the last step was there, so the second product of the step before last but one is done: a wait by parity may be one phase behind)
-        wait_all(o_full, (steps - 2) & 1);
-        wait_all(o_full, (steps - 1) & 1);
+        wait_all(done, 0);
         ptx::tc_fence_after_sync();
         float l, l1;
         split(sums, l, l1);
