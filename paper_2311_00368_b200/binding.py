@@ -568,8 +568,9 @@ def _rows(t, shape, dtype, name):
 
 @functools.lru_cache(maxsize=4096)
 def _attention_need(sizes, nnz_stride, tiles, backward):
-    """b2sp_attention_workspace_bytes, which goes by sizes only."""
-    return lib.b2sp_attention_workspace_bytes(_PROBLEM(*sizes, 1.0, 256, sizes[3] + 1, 256, nnz_stride, 0, tiles), backward)
+    """b2sp_attention_workspace_bytes, which goes by sizes only (tiles: -1 without a plan)."""
+    return lib.b2sp_attention_workspace_bytes(_PROBLEM(*sizes, 1.0, 256, sizes[3] + 1, 256, nnz_stride, 256 if tiles >= 0 else 0,
+                                                               max(tiles, 0)), backward)
 
 
 def _attention_problem(row_ptr, col_idx, q, k, scale, plan):
@@ -624,7 +625,7 @@ def attention(row_ptr, col_idx, q, k, v, scale=None, plan=None, out=None, lse=No
         _lse(lse, qs[:3])
         _ready(device, lse)
     stream = _raw_stream(device.index)
-    ws = _scratch(_attention_need(sizes, nzs, 0 if plan is None else plan.tiles, 0), device, workspace, stream)
+    ws = _scratch(_attention_need(sizes, nzs, -1 if plan is None else plan.tiles, 0), device, workspace, stream)
     fn, name = ((lib.b2sp_attention, "b2sp_attention") if dtype == torch.float32 else (lib.b2sp_attention_bf16, "b2sp_attention_bf16"))
     _check(fn(p, hq, hk, hv, _rows(out, qs, dtype, "out"), lse.data_ptr(), ws.data_ptr(), ws.numel(), algo, stream), name)
     return out, lse

@@ -91,7 +91,7 @@ struct RowPlan {
     size_t stat, ml, part, bytes;         // offsets
     int stat_rows;
 };
-RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles)
+RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles, bool planned)
 {
     RowPlan r;
     const long long problems = (long long)s.batch * s.heads;
@@ -107,7 +107,9 @@ RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles)
     size_t part = r.splits_m > 1 ? um * part_width(kForward, s.d) * 4 : 0;
     if (backward && r.parts_kv) part = std::max(part, uk * part_width(kGradKV, s.d) * 4);
     r.part = take(part);
-    r.bytes = backward ? std::max(at, tiles_backward_bytes(s, tiles, r.ml)) : at;   // (the tile kernels use what lies behind the statistics)
+    r.bytes = at;   // (the tile kernels use what lies behind the statistics)
+    if (planned) r.bytes = std::max(r.bytes, tiles32_bytes(s, tiles, r.ml, backward));
+    if (planned && backward) r.bytes = std::max(r.bytes, tiles_backward_bytes(s, tiles, r.ml));
     return r;
 }
 
@@ -141,6 +143,24 @@ bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward)
     return true;
 }
 
+bool prefer_tiles32(const Shape &s, long long nnz, long long tiles, bool backward)
+{
+    (void)s; (void)nnz; (void)tiles; (void)backward;
+    return true;
+}
+
+Call32 call32(const b2sp_attention_problem *p, const Shape &s, char *ws)
+{
+    Call32 c = {};
+    c.s = s;
+    c.plan = plan_view(p->plan, plan_layout(s.patterns, s.M, s.K, p->nnz_stride, p->plan_tiles));
+    c.tiles = p->plan_tiles;
+    c.row_ptr = p->row_ptr; c.col_idx = p->col_idx; c.row_ptr_stride = p->row_ptr_stride; c.nnz_stride = p->nnz_stride;
+    c.workspace = ws;
+    c.status = reinterpret_cast<int *>(ws + 256);
+    return c;
+}
+
 template <typename T>
 b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V, const b2sp_heads *O,
                     float *lse, void *workspace, size_t workspace_bytes, int algo, void *stream)
@@ -153,7 +173,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
         return rc;
     if (p->M && !lse) return B2SP_ERR_INVALID_ARG;
     const Shape s = shape(p);
-    const RowPlan w = row_plan(s, p->nnz_stride, false, p->plan_tiles);
+    const RowPlan w = row_plan(s, p->nnz_stride, false, p->plan_tiles, p->plan != nullptr);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < w.bytes) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
@@ -177,8 +197,18 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
             g_algo[0] = B2SP_ALGO_TILE;
             return tiles_forward(c, st, &launches);
         }
-    } else if (algo == B2SP_ALGO_TILE) {
-        return B2SP_ERR_UNSUPPORTED;
+    } else {
+        const bool can = p->plan && tiles32_possible(s);
+        if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
+        if (can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles32(s, p->nnz_stride, p->plan_tiles, false)))) {
+            Call32 c = call32(p, s, ws);
+            c.q = view<const T>(Q); c.k = view<const T>(K); c.v = view<const T>(V); c.out = view<T>(O); c.lse = lse;
+            c.wide_in = fours(c.q, s.d) && fours(c.k, s.d) && fours(c.v, s.d);
+            c.wide = fours(c.out, s.d);
+            c.scratch_at = w.ml;
+            g_algo[0] = B2SP_ALGO_TILE;
+            return tiles32_forward(c, st, &launches);
+        }
     }
     g_algo[0] = B2SP_ALGO_ROW;
     RowArgs<T> g = {};
@@ -207,7 +237,7 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         return rc;
     if (p->M && !lse) return B2SP_ERR_INVALID_ARG;
     const Shape s = shape(p);
-    const RowPlan w = row_plan(s, p->nnz_stride, true, p->plan_tiles);
+    const RowPlan w = row_plan(s, p->nnz_stride, true, p->plan_tiles, true);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < w.bytes) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
@@ -220,8 +250,10 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         const bool can = s.M > 0 && s.K > 0 && tiles_possible(s, ops, 8);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
         tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true)));
-    } else if (algo == B2SP_ALGO_TILE) {
-        return B2SP_ERR_UNSUPPORTED;
+    } else {
+        const bool can = tiles32_possible(s);
+        if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
+        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles32(s, p->nnz_stride, p->plan_tiles, true)));
     }
     g_algo[1] = tiles ? B2SP_ALGO_TILE : B2SP_ALGO_ROW;
     float2 *stat = reinterpret_cast<float2 *>(ws + w.stat);
@@ -249,6 +281,18 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         else attention_stat_kernel<T, 1><<<(unsigned)blocks, 256, 0, st>>>(s, o, d, lse, w.stat_rows, stat, status);
         ++launches;
         if ((rc = launched()) != B2SP_OK) return rc;
+    }
+    if constexpr (sizeof(T) == 4) {
+        if (tiles) {
+            Call32 c = call32(p, s, ws);
+            c.q = view<const T>(Q); c.k = view<const T>(K); c.v = view<const T>(V); c.dout = view<const T>(dO);
+            c.dq = view<T>(dQ); c.dk = view<T>(dK); c.dv = view<T>(dV);
+            c.wide_in = fours(c.q, s.d) && fours(c.k, s.d) && fours(c.v, s.d) && fours(c.dout, s.d);
+            c.wide = fours(c.dq, s.d) && fours(c.dk, s.d) && fours(c.dv, s.d);
+            c.stat = stat; c.stat_stride = w.stat_rows;
+            c.scratch_at = w.ml;
+            return tiles32_backward(c, st, &launches);
+        }
     }
     RowArgs<T> g = {};
     g.s = s;
@@ -348,7 +392,7 @@ extern "C" b2sp_status b2sp_attention_plan_status(const void *plan, void *stream
 extern "C" size_t b2sp_attention_workspace_bytes(const b2sp_attention_problem *p, int backward)
 {
     if (check_problem(p) != B2SP_OK) return 0;
-    return row_plan(shape(p), p->nnz_stride, backward != 0, p->plan_tiles).bytes;
+    return row_plan(shape(p), p->nnz_stride, backward != 0, p->plan_tiles, p->plan != nullptr || backward).bytes;
 }
 
 extern "C" b2sp_status b2sp_attention(const b2sp_attention_problem *p, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V, const b2sp_heads *O,

@@ -31,13 +31,14 @@ struct Op {              // a tensor map's coordinates of (b, h): 0 where the op
     int hm, bm;
 };
 
-struct TileArgs {
-    RowArgs<Bf16> g;     // operands, pattern and outputs for rows that are taken one by one
+template <typename T> struct TileArgsOf {
+    RowArgs<T> g;        // operands, pattern and outputs for rows that are taken one by one
     Plan plan;
     Op q, k, v, dout;
     const int *col_ptr, *row_idx;        // transposed pattern
     int *status;
 };
+using TileArgs = TileArgsOf<Bf16>;
 
 // Bounded wait that asks for a complete phase with a test first (36 cycles; the try_wait of ptx::mbar_wait answers in 92).
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity)
@@ -139,13 +140,13 @@ __device__ __forceinline__ bool store32(Bf16 *row, int c0, int d, const uint32_t
 
 // Rows of the 32 that a warp owns whose lane says `bad`, entry by entry (rows of the pattern; kGradKV: columns, over the query heads
 // [h0, h0 + heads) that share them).
-template <int MODE, int DW>
-__device__ __noinline__ void rows_one_by_one(const RowArgs<Bf16> &g, const int *ptr, const int *idx, int b, int h0, int heads, int row0, unsigned bad,
+template <int MODE, int DW, typename T = Bf16, int V = 4>
+__device__ __noinline__ void rows_one_by_one(const RowArgs<T> &g, const int *ptr, const int *idx, int b, int h0, int heads, int row0, unsigned bad,
                                              long long ptr_stride, long long idx_stride)
 {
     for (; bad; bad &= bad - 1) {
         const int row = row0 + __ffs(bad) - 1;
-        RowWork<MODE, Bf16, 4, DW> w, all;
+        RowWork<MODE, T, V, DW> w, all;
         for (int i = 0; i < heads; ++i) {
             const int pat = pattern_of(g.s.patterns, g.s.batch, g.s.heads, b, h0 + i);
             const int *p = ptr + pat * ptr_stride;
@@ -535,8 +536,8 @@ struct Walk {
     }
 };
 
-struct GradArgs {
-    TileArgs a;
+template <typename T> struct GradArgsOf {
+    TileArgsOf<T> a;
     Tiles w;
     const int *tile_at;       // of a tile: its row or column block, the first of two ints for dK and dV
     int share, ctas;
@@ -545,6 +546,7 @@ struct GradArgs {
     float *part;              // [ctas][2][dK: 2][128][DP]
     int *bad;                 // [outers][blocks]: the sums of a block are not finite (its rows are taken one by one)
 };
+using GradArgs = GradArgsOf<Bf16>;
 
 // Two warps issue products: one S and dP, as far ahead as sets of tensor memory are free, one the second products.  The tensor core takes
 // products from them in turn (about 52 cycles each at 128 x 64 x 16 from shared memory, 61 at 128 x 128 x 16 with A in tensor memory), and what
@@ -826,26 +828,26 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
 // added up in order, 32 rows a CTA; rows whose sums are not finite are taken one by one.  The CTAs also go through the flags of the blocks that
 // were finished in one share.
 constexpr int kJoinRows = 32, kJoinParts = kTile / kJoinRows;
-template <int MODE, int DP>
-__device__ __forceinline__ void tile_grad_rows(const GradArgs &g, int o, int blk, int r)
+template <int MODE, int DP, typename T, int V>
+__device__ __forceinline__ void tile_grad_rows(const GradArgsOf<T> &g, int o, int blk, int r)
 {
-    const TileArgs &a = g.a;
+    const TileArgsOf<T> &a = g.a;
     const int b = o / g.w.outer, h = o % g.w.outer, row = blk * kTile + r;
-    if (MODE == kDq) rows_one_by_one<kGradQ, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
-    else rows_one_by_one<kGradKV, DP>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
+    if (MODE == kDq) rows_one_by_one<kGradQ, DP, T, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
+    else rows_one_by_one<kGradKV, DP, T, V>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
 }
-template <int MODE, int DP>
-__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgs g)
+template <int MODE, int DP, typename T = Bf16, int V = 4>
+__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgsOf<T> g)
 {
     constexpr int ACCS = MODE == kDkv ? 2 : 1, WIDE = ACCS * DP, LANES = WIDE / 4;   // threads that a row takes
-    const TileArgs &a = g.a;
+    const TileArgsOf<T> &a = g.a;
     const Shape &s = a.g.s;
     const int share = blockIdx.x / kJoinParts, part = blockIdx.x % kJoinParts, warp = threadIdx.x >> 5;
     const int rows = MODE == kDq ? s.M : s.K;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int block = blockIdx.x; block < g.w.outers * g.w.NB; block += gridDim.x)
         if (g.bad[block])
-            for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DP>(g, block / g.w.NB, block % g.w.NB, r);
+            for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, block / g.w.NB, block % g.w.NB, r);
     if (share == 0) return;
     const int4 at = g.starts[share];
     const int o = at.x, blk = at.y, b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
@@ -873,23 +875,50 @@ __global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_consta
             x[k] *= acc ? 1.f : s.scale;
             bad |= col + k < s.d && !(fabsf(x[k]) <= 3.402823466e38f);
         }
-        store4<Bf16, 4>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x);
+        store4<T, V>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x);
         if (bad) redo = 1;
     }
     __syncthreads();
     if (redo == 0) return;
-    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) tile_grad_rows<MODE, DP>(g, o, blk, part * kJoinRows + r);
+    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, o, blk, part * kJoinRows + r);
 }
 
 // Ahead of both: row statistics (see attention_stat_kernel); and, in the first CTAs, where the shares begin, cleared flags of the blocks, and zeros for
 // the blocks that have no tiles.
-struct ShareArgs {
+template <typename T> struct ShareArgsOf {
     Tiles w[2];
+    int kinds;           // 1: only w[0]
     int share[2], ctas[2], rows[2];
     int4 *starts[2];
-    int *bad[2];
-    View<Bf16> out[3];   // dQ, dK, dV
+    int *bad[2];         // NULL: neither flags nor zeros
+    View<T> out[3];      // dQ, dK, dV
 };
+using ShareArgs = ShareArgsOf<Bf16>;
+template <typename T> __device__ __forceinline__ void prepare_shares(const ShareArgsOf<T> &h, int d, int share_blocks)
+{
+    const int u = blockIdx.x * 256 + threadIdx.x, lane = threadIdx.x & 31, total = h.ctas[0] + (h.kinds > 1 ? h.ctas[1] : 0);
+    for (int i = u; i < total; i += share_blocks * 256) {
+        const int k = i < h.ctas[0] ? 0 : 1, c = k ? i - h.ctas[0] : i;
+        h.starts[k][c] = share_start(h.w[k], (long long)c * h.share[k]);
+    }
+    for (int k = 0; k < h.kinds; ++k) {
+        const Tiles &w = h.w[k];
+        if (!h.bad[k]) continue;
+        for (int i0 = u - lane; i0 < w.outers * w.NB; i0 += share_blocks * 256) {
+            const int i = i0 + lane, o = i / w.NB, blk = i % w.NB;
+            bool none = false;
+            if (i < w.outers * w.NB) {
+                h.bad[k][i] = 0;
+                none = w.ahead(o, blk + 1) == w.ahead(o, blk);
+            }
+            for (unsigned left = __ballot_sync(~0u, none); left; left &= left - 1) {
+                const int z = i0 + __ffs(left) - 1, zo = z / w.NB, z0 = z % w.NB * kTile, n = min(kTile, h.rows[k] - z0);
+                for (int e = lane; e < n * d; e += 32)
+                    for (int x = k; x < (k ? 3 : 1); ++x) narrow(0.f, h.out[x].at(zo / w.outer, zo % w.outer, z0 + e / d)[e % d]);
+            }
+        }
+    }
+}
 constexpr int kStatRows = 4;   // rows of half a warp
 template <int DUMMY = 0>
 __global__ void __launch_bounds__(256) tile_grad_stat_kernel(Shape s, View<const Bf16> out, View<const Bf16> dout, const float *lse, int stat_rows, float2 *stat,
@@ -898,28 +927,7 @@ __global__ void __launch_bounds__(256) tile_grad_stat_kernel(Shape s, View<const
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if ((int)blockIdx.x < share_blocks) {   // (first, as they wait longest)
-        const int u = blockIdx.x * 256 + threadIdx.x, lane = threadIdx.x & 31, total = h.ctas[0] + h.ctas[1];
-        for (int i = u; i < total; i += share_blocks * 256) {
-            const int k = i < h.ctas[0] ? 0 : 1, c = k ? i - h.ctas[0] : i;
-            h.starts[k][c] = share_start(h.w[k], (long long)c * h.share[k]);
-        }
-        for (int k = 0; k < 2; ++k) {
-            const Tiles &w = h.w[k];
-            for (int i0 = u - lane; i0 < w.outers * w.NB; i0 += share_blocks * 256) {
-                const int i = i0 + lane, o = i / w.NB, blk = i % w.NB;
-                bool none = false;
-                if (i < w.outers * w.NB) {
-                    h.bad[k][i] = 0;
-                    none = w.ahead(o, blk + 1) == w.ahead(o, blk);
-                }
-                for (unsigned left = __ballot_sync(~0u, none); left; left &= left - 1) {
-                    const int z = i0 + __ffs(left) - 1, zo = z / w.NB, z0 = z % w.NB * kTile, n = min(kTile, h.rows[k] - z0), wide = s.d / 8;
-                    for (int e = lane; e < n * wide; e += 32)
-                        for (int x = k; x < (k ? 3 : 1); ++x)
-                            *reinterpret_cast<uint4 *>(h.out[x].at(zo / w.outer, zo % w.outer, z0 + e / wide) + e % wide * 8) = make_uint4(0, 0, 0, 0);
-                }
-            }
-        }
+        prepare_shares(h, s.d, share_blocks);
         return;
     }
     // half a warp per row, eight elements a lane, four rows at once

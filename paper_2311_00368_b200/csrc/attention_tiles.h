@@ -27,5 +27,27 @@ size_t tiles_backward_bytes(const Shape &s, long long tiles, size_t at);
 b2sp_status tiles_forward(const TileCall &c, cudaStream_t st, int *launches);
 b2sp_status tiles_backward(const TileCall &c, cudaStream_t st, int *launches);
 
+// The same on fp32 operands, of any alignment.
+struct Call32 {
+    Shape s;
+    Plan plan;
+    long long tiles;
+    const int *row_ptr, *col_idx;
+    long long row_ptr_stride, nnz_stride;
+    View<const float> q, k, v, dout;
+    View<float> out, dq, dk, dv;
+    int wide_in, wide;                   // all inputs (outputs) have rows that are aligned groups of four elements
+    float *lse;
+    const float2 *stat;
+    long long stat_stride;
+    int *status;
+    void *workspace;
+    size_t scratch_at;
+};
+bool tiles32_possible(const Shape &s);
+size_t tiles32_bytes(const Shape &s, long long tiles, size_t at, bool backward);
+b2sp_status tiles32_forward(const Call32 &c, cudaStream_t st, int *launches);
+b2sp_status tiles32_backward(const Call32 &c, cudaStream_t st, int *launches);
+
 }  // namespace attn
 }  // namespace b2sp

@@ -1,0 +1,195 @@
+// Launches of the tensor-core attention kernels on fp32 operands: planes, shares, tensor maps.
+#include "attention_tiles32.cuh"
+
+#include <algorithm>
+#include <atomic>
+#include <climits>
+
+#include "attention_maps.h"
+
+namespace b2sp {
+namespace attn {
+namespace {
+
+constexpr int kSMs = 148;
+
+// Where things lie in the workspace from offset `at` on, and how tiles are dealt out: [0] forward and dQ (by rows), [1] dK and dV (by columns).
+struct Plan32 {
+    long long tiles[2], blocks[2];
+    int outers[2], NB[2], share[2], ctas[2];
+    size_t starts[2], bad[2], q, k, v, dout, ml, part, bytes;
+};
+Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
+{
+    Plan32 p = {};
+    auto take = [&](size_t b) { const size_t a = at; at += up256(b); return a; };
+    const size_t row = kPlanes * 2, qs = (size_t)s.batch * s.heads * s.M, ks = (size_t)s.batch * s.kv_heads * s.K;
+    p.q = take(qs * row);
+    p.k = take(ks * row);
+    p.v = take(ks * row);
+    p.dout = take(backward ? qs * row : 0);
+    for (int k = 0; k < (backward ? 2 : 1); ++k) {
+        p.tiles[k] = tiles * ((long long)s.batch * s.heads / s.patterns);
+        p.outers[k] = s.batch * (k == 0 ? s.heads : s.kv_heads);
+        p.NB[k] = ((k == 0 ? s.M : s.K) + kTile - 1) / kTile;
+        p.blocks[k] = (long long)p.outers[k] * p.NB[k];
+        p.share[k] = (int)std::max(1ll, (p.tiles[k] + kSMs - 1) / kSMs);
+        p.ctas[k] = (int)((p.tiles[k] + p.share[k] - 1) / p.share[k]);
+        p.starts[k] = take((size_t)p.ctas[k] * 16);
+        p.bad[k] = take(backward ? (size_t)p.blocks[k] * 4 : 0);
+    }
+    if (backward) {
+        p.part = take((size_t)std::max(p.ctas[0], 2 * p.ctas[1]) * 2 * kTile * 64 * 4);
+    } else {
+        const size_t parts = (size_t)(p.ctas[0] + p.blocks[0]) * Fwd32::SETS * kTile;
+        p.ml = take(parts * 8);
+        p.part = take(parts * 64 * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+Tiles tiles_of(const Call32 &c, const Plan32 &p, int k)
+{
+    const Shape &s = c.s;
+    return Tiles{k == 0 ? c.plan.rb_ptr : c.plan.cb_ptr, p.NB[k], k == 0 ? s.heads : s.kv_heads, k == 0 ? 1 : s.heads / s.kv_heads, s.patterns, s.batch, s.heads, p.outers[k]};
+}
+
+Args32 args(const Call32 &c, const Plan32 &p, int k)
+{
+    char *ws = static_cast<char *>(c.workspace);
+    Args32 f = {};
+    RowArgs<float> &r = f.g.a.g;
+    r.s = c.s;
+    r.ptr = c.row_ptr; r.idx = c.col_idx; r.ptr_stride = c.row_ptr_stride; r.idx_stride = c.nnz_stride;
+    r.q = c.q; r.k = c.k; r.v = c.v; r.dout = c.dout;
+    r.stat = c.stat; r.stat_stride = c.stat_stride;
+    r.lse = c.lse; r.lse_head = c.s.M; r.lse_row = 1;
+    r.splits = 1;
+    f.g.a.plan = c.plan;
+    f.g.a.col_ptr = c.plan.col_ptr; f.g.a.row_idx = c.plan.row_idx;
+    f.g.a.status = c.status;
+    f.g.w = tiles_of(c, p, k);
+    f.g.tile_at = k == 0 ? c.plan.tile_cb : reinterpret_cast<const int *>(c.plan.ctile);
+    f.g.share = p.share[k]; f.g.ctas = p.ctas[k]; f.g.tiles = p.tiles[k];
+    f.g.starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
+    f.g.bad = reinterpret_cast<int *>(ws + p.bad[k]);
+    f.g.part = reinterpret_cast<float *>(ws + p.part);
+    f.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
+    f.wide = c.wide;
+    return f;
+}
+
+View<const Bf16> planes(const Call32 &c, size_t at, int heads, int rows)
+{
+    return View<const Bf16>{reinterpret_cast<const Bf16 *>(static_cast<char *>(c.workspace) + at), kPlanes, (long long)rows * kPlanes, (long long)heads * rows * kPlanes};
+}
+
+// Planes of the operands, and where the shares begin.
+b2sp_status split(const Call32 &c, const Plan32 &p, bool backward, cudaStream_t st, int *launches)
+{
+    const Shape &s = c.s;
+    char *ws = static_cast<char *>(c.workspace);
+    SplitArgs a = {};
+    a.d = s.d; a.batch = s.batch;
+    auto add = [&](const View<const float> &x, size_t at, int heads, int rows) {
+        const int t = a.count++;
+        a.x[t] = x; a.planes[t] = reinterpret_cast<Bf16 *>(ws + at); a.heads[t] = heads; a.rows[t] = rows;
+        a.before[t + 1] = a.before[t] + (long long)s.batch * heads * rows;
+    };
+    add(c.q, p.q, s.heads, s.M);
+    add(c.k, p.k, s.kv_heads, s.K);
+    add(c.v, p.v, s.kv_heads, s.K);
+    if (backward) add(c.dout, p.dout, s.heads, s.M);
+    ShareArgsOf<float> h = {};
+    h.kinds = backward ? 2 : 1;
+    long long most = 1;
+    for (int k = 0; k < h.kinds; ++k) {
+        h.w[k] = tiles_of(c, p, k);
+        h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.rows[k] = k == 0 ? s.M : s.K;
+        h.starts[k] = reinterpret_cast<int4 *>(ws + p.starts[k]);
+        h.bad[k] = backward ? reinterpret_cast<int *>(ws + p.bad[k]) : nullptr;
+        most = std::max(most, std::max(p.blocks[k], (long long)p.ctas[0] + p.ctas[1]));
+    }
+    h.out[0] = c.dq; h.out[1] = c.dk; h.out[2] = c.dv;
+    const int share_blocks = (int)((most + 255) / 256);
+    const long long blocks = (a.before[a.count] + 15) / 16 + share_blocks;
+    if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (c.wide_in) split_planes_kernel<4><<<(unsigned)blocks, 256, 0, st>>>(a, h, share_blocks, c.status);
+    else split_planes_kernel<1><<<(unsigned)blocks, 256, 0, st>>>(a, h, share_blocks, c.status);
+    ++*launches;
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
+}
+
+template <int MODE> b2sp_status grad(const Call32 &c, const Plan32 &p, cudaStream_t st, int *launches)
+{
+    static std::atomic<unsigned long long> done{0};
+    using C = Grad32<MODE>;
+    const Shape &s = c.s;
+    if (p.ctas[MODE] == 0) return B2SP_OK;
+    Args32 f = args(c, p, MODE);
+    if (MODE == kDq) { f.g.a.g.out1 = c.dq; f.g.a.g.rows = s.M; }
+    else { f.g.a.g.out1 = c.dk; f.g.a.g.out2 = c.dv; f.g.a.g.rows = s.K; }
+    CUtensorMap x1, x2, y1, y2;
+    Op op;
+    const bool q = MODE == kDq;
+    const int bq = q ? 128 : 64, bk = q ? 64 : 128;
+    if (!make_map(q ? &x1 : &y1, planes(c, p.q, s.heads, s.M), s.batch, s.heads, s.M, kPlanes, bq, &op) ||
+        !make_map(q ? &x2 : &y2, planes(c, p.dout, s.heads, s.M), s.batch, s.heads, s.M, kPlanes, bq, &op) ||
+        !make_map(q ? &y1 : &x1, planes(c, p.k, s.kv_heads, s.K), s.batch, s.kv_heads, s.K, kPlanes, bk, &op) ||
+        !make_map(q ? &y2 : &x2, planes(c, p.v, s.kv_heads, s.K), s.batch, s.kv_heads, s.K, kPlanes, bk, &op) ||
+        !allow_smem(tile_grad32_kernel<MODE>, C::BYTES, done))
+        return B2SP_ERR_CUDA;
+    launch_behind_smem(tile_grad32_kernel<MODE>, (unsigned)p.ctas[MODE], C::THREADS, C::BYTES, st, x1, x2, y1, y2, f);
+    if (c.wide) launch_behind(tile_grad_join_kernel<MODE, 64, float, 4>, (unsigned)(p.ctas[MODE] * kJoinParts), 256, st, f.g);
+    else launch_behind(tile_grad_join_kernel<MODE, 64, float, 1>, (unsigned)(p.ctas[MODE] * kJoinParts), 256, st, f.g);
+    *launches += 2;
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
+}
+
+}  // namespace
+
+bool tiles32_possible(const Shape &s) { return s.d <= 64 && s.scale > 0.f && s.scale <= 3.4e38f && s.M > 0 && s.K > 0; }
+size_t tiles32_bytes(const Shape &s, long long tiles, size_t at, bool backward)
+{
+    return s.d <= 64 ? plan32(s, tiles, at, backward).bytes : at;
+}
+
+b2sp_status tiles32_forward(const Call32 &c, cudaStream_t st, int *launches)
+{
+    static std::atomic<unsigned long long> done{0};
+    const Shape &s = c.s;
+    const Plan32 p = plan32(s, c.tiles, c.scratch_at, false);
+    if (p.blocks[0] > INT_MAX / kJoinParts) return B2SP_ERR_UNSUPPORTED;
+    const b2sp_status rc = split(c, p, false, st, launches);
+    if (rc != B2SP_OK) return rc;
+    Args32 f = args(c, p, 0);
+    f.g.a.g.out1 = c.out; f.g.a.g.rows = s.M;
+    CUtensorMap q, k, v;
+    Op op;
+    if (!make_map(&q, planes(c, p.q, s.heads, s.M), s.batch, s.heads, s.M, kPlanes, 128, &op) ||
+        !make_map(&k, planes(c, p.k, s.kv_heads, s.K), s.batch, s.kv_heads, s.K, kPlanes, 64, &op) ||
+        !make_map(&v, planes(c, p.v, s.kv_heads, s.K), s.batch, s.kv_heads, s.K, kPlanes, 64, &op) || !allow_smem(tile_forward32_kernel, Fwd32::BYTES, done))
+        return B2SP_ERR_CUDA;
+    if (p.ctas[0]) {
+        launch_behind_smem(tile_forward32_kernel, (unsigned)p.ctas[0], Fwd32::THREADS, Fwd32::BYTES, st, q, k, v, f);
+        ++*launches;
+    }
+    const unsigned joins = (unsigned)(p.blocks[0] * kJoinParts);
+    if (c.wide) launch_behind(tile_forward32_join_kernel<4>, joins, 256, st, f);
+    else launch_behind(tile_forward32_join_kernel<1>, joins, 256, st, f);
+    ++*launches;
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
+}
+
+b2sp_status tiles32_backward(const Call32 &c, cudaStream_t st, int *launches)
+{
+    const Plan32 p = plan32(c.s, c.tiles, c.scratch_at, true);
+    if (p.blocks[0] > INT_MAX / 4 || p.blocks[1] > INT_MAX / 4) return B2SP_ERR_UNSUPPORTED;
+    b2sp_status rc = split(c, p, true, st, launches);
+    if (rc == B2SP_OK) rc = grad<kDq>(c, p, st, launches);
+    return rc == B2SP_OK ? grad<kDkv>(c, p, st, launches) : rc;
+}
+
+}  // namespace attn
+}  // namespace b2sp

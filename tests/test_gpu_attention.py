@@ -123,15 +123,37 @@ def test_tile_kernels(i):
     Problem(300 + i, dtype=torch.bfloat16, **TILE_SHAPES[i]).check(_binding().ALGO_TILE)
 
 
+TILE32_SHAPES = [
+    dict(M=1, K=1, d=1, kind="full"),
+    dict(M=1, K=300, d=64, kind="full"),
+    dict(M=128, K=128, d=64),
+    dict(B=2, H=3, Hkv=3, M=150, K=290, d=50, per="sequence"),
+    dict(H=6, Hkv=2, M=513, K=513, d=33, kind="window", strided=True),
+    dict(B=2, H=4, Hkv=1, M=1100, K=1300, d=64, per="problem", strided=True),
+    dict(H=2, Hkv=1, M=900, K=640, d=16, kind="sparse"),
+    dict(M=200, K=200, d=64, kind="nothing"),
+    dict(M=1000, K=1000, d=48, kind="full", spread=4.0),
+    dict(B=3, H=2, Hkv=2, M=260, K=2100, d=64, spread=8.0),
+]
+
+
+@pytest.mark.parametrize("i", range(len(TILE32_SHAPES)))
+def test_tile_kernels_on_fp32(i):
+    """fp32 operands on the tensor cores: what is left out of a product of planes is below 2^-23 of each term, and 24 truncated additions
+    are off by 24 u at most; the bound of the dot products, 2 (d + 6) u sum|terms| with one product of six planes per 16 elements, holds them."""
+    Problem(350 + i, **TILE32_SHAPES[i]).check(_binding().ALGO_TILE)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_the_choice_of_the_library(dtype):
     Problem(400, B=2, H=4, Hkv=2, M=300, K=400, d=64, dtype=dtype).check(0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("algo", [1, 3])
-def test_what_no_entry_names_does_not_matter(algo):
+def test_what_no_entry_names_does_not_matter(algo, dtype):
     """NaN and infinities in rows of Q, K, V and dO that no entry names, next to ones that entries do name."""
-    p = Problem(500, H=2, M=300, K=300, d=64, dtype=torch.bfloat16)
+    p = Problem(500, H=2, M=300, K=300, d=64, dtype=dtype)
     m = p.mask[0, 0].clone()
     m[:, 40:50] = False
     m[200:210] = False
@@ -148,9 +170,10 @@ def test_what_no_entry_names_does_not_matter(algo):
     p.check(algo)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("algo", [1, 3])
-def test_nan_reaches_the_rows_that_name_it(algo):
-    p = Problem(501, M=256, K=256, d=64, dtype=torch.bfloat16)
+def test_nan_reaches_the_rows_that_name_it(algo, dtype):
+    p = Problem(501, M=256, K=256, d=64, dtype=dtype)
     p.v[0, 0, 7, 3] = float("nan")
     o, lse = p.forward(algo, p.plan())
     rows = p.mask[0, 0, :, 7]
@@ -219,9 +242,10 @@ def test_gradients_against_differences():
 
 
 @pytest.mark.parametrize("algo", [1, 3])
-def test_captured_and_replayed_beside_another_graph(algo):
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_captured_and_replayed_beside_another_graph(algo, dtype):
     """Two graphs of forward and backward, captured on one stream, replayed at once on two: neither disturbs the other."""
-    ps = [Problem(600 + i, H=2, M=600, K=700, d=64, dtype=torch.bfloat16) for i in range(2)]
+    ps = [Problem(600 + i, H=2, M=600, K=700, d=64, dtype=dtype) for i in range(2)]
     plans = [p.plan() for p in ps]
     want = []
     for p, plan in zip(ps, plans):
