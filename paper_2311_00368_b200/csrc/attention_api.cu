@@ -109,7 +109,7 @@ RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles, 
     r.part = take(part);
     r.bytes = at;   // (the tile kernels use what lies behind the statistics)
     if (planned) r.bytes = std::max(r.bytes, tiles32_bytes(s, tiles, r.ml, backward));
-    if (planned && backward) r.bytes = std::max(r.bytes, tiles_backward_bytes(s, tiles, r.ml));
+    if (planned) r.bytes = std::max(r.bytes, tiles_bytes(s, tiles, r.ml, backward));
     return r;
 }
 
@@ -135,18 +135,37 @@ template <int MODE, typename T> b2sp_status launch_rows_v(bool wide, const RowAr
 }
 
 // ---- the choice between the families -------------------------------------------------------------------------------------------------
-// Microseconds that each would take, from what was measured on both (see the comments at the kernels): the row kernels by entries and
-// width, with a start; the tile kernels by the tiles of the longest CTA.
-bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward)
+// Microseconds that each would take.  The row kernels' work is that of the stored entries, but a warp takes a row's (or a part's, about 64 and
+// more) one after the other.  The tile kernels' work is that of the tiles, whatever they hold; the forward pass takes a block's one after the
+// other.  Measured, rows against tiles, bf16, width 64, forward and backward:
+//     one row of 4096 of 8192, one head              26 and  32    87 and  30
+//     512 x 512 at 2%, one head                       7 and  15    10 and  28
+//     1024 x 1024 at 0.5%, 8 heads                   11 and  27    16 and  45
+//     2048 x 2048 at 1%, 8 heads over 2              33 and  81    27 and  78
+//     2048 x 2048 at 4%, 8 heads over 2              85 and 212    27 and  78
+//     200 x 8000 at 2%, one head                     30 and  38    85 and  46
+//     4 x 5 heads over one, width 32, 700 x 700, 3%  28 and  73    13 and  52
+// fp32:
+//     one row of 4096 of 8192, one head              26 and  36    36 and  48
+//     64 x 64 at 30%, one head                        7 and  17    14 and  30
+//     2048 x 2048 at 2%, 8 heads over 2              52 and 156    66 and 204
+//     2048 x 2048 at 4%, 8 heads over 2              88 and 267    66 and 205
+//     200 x 8000 at 2%, one head                     31 and  47    38 and  58
+double row_time(const Shape &s, double entries, double in_row, bool backward, bool wide)
 {
-    (void)s; (void)nnz; (void)tiles; (void)backward;
-    return true;
+    const double width = std::max(s.d, 64) / 64.0;
+    return backward ? 12 + std::max(0.25 * std::min(in_row, 128.0), (wide ? 0.19e-3 : 0.15e-3) * entries * width)
+                    : 5 + std::max(0.2 * std::min(in_row, 128.0), 0.06e-3 * entries * width);
 }
-
-bool prefer_tiles32(const Shape &s, long long nnz, long long tiles, bool backward)
+bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward, bool fp32)
 {
-    (void)s; (void)nnz; (void)tiles; (void)backward;
-    return true;
+    const double problems = (double)s.batch * s.heads, entries = nnz * problems, all = tiles * (problems / s.patterns);
+    const double in_row = (double)nnz / s.M, in_block = all / (problems * ((s.M + kTile - 1) / kTile));
+    double t;
+    if (fp32) t = backward ? 30 + 0.5 * std::min(all, 16.0) + 0.082 * all : 14 + 0.06 * std::min(all, 128.0) + 0.25 * in_block + 0.0225 * all;
+    else if (backward) t = 20 + 0.6 * std::min(all, 16.0) + 0.022 * all * (s.d <= 64 ? 1 : 1.6);
+    else t = 5 + 1.3 * std::max(in_block, all / 296);
+    return t < row_time(s, entries, in_row, backward, fp32);
 }
 
 Call32 call32(const b2sp_attention_problem *p, const Shape &s, char *ws)
@@ -185,7 +204,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
         const View<const T> ops[4] = {view<const T>(Q), view<const T>(K), view<const T>(V), view<const T>(O)};
         const bool can = p->plan && s.K > 0 && tiles_possible(s, ops, 4);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
-        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, false)));
+        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, false, false)));
         if (tiles) {
             TileCall c = {};
             c.s = s;
@@ -193,6 +212,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
             c.tiles = p->plan_tiles;
             c.row_ptr = p->row_ptr; c.col_idx = p->col_idx; c.row_ptr_stride = p->row_ptr_stride; c.nnz_stride = p->nnz_stride;
             c.q = ops[0]; c.k = ops[1]; c.v = ops[2]; c.out = view<T>(O); c.lse = lse;
+            c.workspace = workspace; c.scratch_at = w.ml;
             c.status = reinterpret_cast<int *>(ws + 256);
             g_algo[0] = B2SP_ALGO_TILE;
             return tiles_forward(c, st, &launches);
@@ -200,7 +220,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
     } else {
         const bool can = p->plan && tiles32_possible(s);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
-        if (can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles32(s, p->nnz_stride, p->plan_tiles, false)))) {
+        if (can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, false, true)))) {
             Call32 c = call32(p, s, ws);
             c.q = view<const T>(Q); c.k = view<const T>(K); c.v = view<const T>(V); c.out = view<T>(O); c.lse = lse;
             c.wide_in = fours(c.q, s.d) && fours(c.k, s.d) && fours(c.v, s.d);
@@ -249,11 +269,11 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         const View<const T> ops[8] = {view<const T>(Q), view<const T>(K), view<const T>(V), view<const T>(O), view<const T>(dO), view<const T>(dQ), view<const T>(dK), view<const T>(dV)};
         const bool can = s.M > 0 && s.K > 0 && tiles_possible(s, ops, 8);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
-        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true)));
+        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true, false)));
     } else {
         const bool can = tiles32_possible(s);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
-        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles32(s, p->nnz_stride, p->plan_tiles, true)));
+        tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true, true)));
     }
     g_algo[1] = tiles ? B2SP_ALGO_TILE : B2SP_ALGO_ROW;
     float2 *stat = reinterpret_cast<float2 *>(ws + w.stat);

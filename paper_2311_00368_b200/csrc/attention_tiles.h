@@ -22,8 +22,8 @@ struct TileCall {
 };
 
 bool tiles_possible(const Shape &s, const View<const Bf16> *views, int n);
-// The end of what the backward pass needs of the workspace, from offset `at` on.
-size_t tiles_backward_bytes(const Shape &s, long long tiles, size_t at);
+// The end of what a pass needs of the workspace, from offset `at` on.
+size_t tiles_bytes(const Shape &s, long long tiles, size_t at, bool backward);
 b2sp_status tiles_forward(const TileCall &c, cudaStream_t st, int *launches);
 b2sp_status tiles_backward(const TileCall &c, cudaStream_t st, int *launches);
 

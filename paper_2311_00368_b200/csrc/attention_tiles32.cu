@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <atomic>
 #include <climits>
+#include <cmath>
 
 #include "attention_maps.h"
 
@@ -33,7 +34,10 @@ Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
         p.outers[k] = s.batch * (k == 0 ? s.heads : s.kv_heads);
         p.NB[k] = ((k == 0 ? s.M : s.K) + kTile - 1) / kTile;
         p.blocks[k] = (long long)p.outers[k] * p.NB[k];
-        p.share[k] = (int)std::max(1ll, (p.tiles[k] + kSMs - 1) / kSMs);
+        // Equal shares for all SMs; where a block's tiles are few that would leave more sums to join (0.7 us each, one after the other) than
+        // it saves tiles (4 us each): not below the square root of a sixth of a block's tiles.
+        const long long least = (long long)std::sqrt((double)p.tiles[k] / std::max(1ll, p.blocks[k]) / 6);
+        p.share[k] = (int)std::max(std::max(1ll, least), (p.tiles[k] + kSMs - 1) / kSMs);
         p.ctas[k] = (int)((p.tiles[k] + p.share[k] - 1) / p.share[k]);
         p.starts[k] = take((size_t)p.ctas[k] * 16);
         p.bad[k] = take(backward ? (size_t)p.blocks[k] * 4 : 0);
@@ -160,7 +164,7 @@ b2sp_status tiles32_forward(const Call32 &c, cudaStream_t st, int *launches)
     static std::atomic<unsigned long long> done{0};
     const Shape &s = c.s;
     const Plan32 p = plan32(s, c.tiles, c.scratch_at, false);
-    if (p.blocks[0] > INT_MAX / kJoinParts) return B2SP_ERR_UNSUPPORTED;
+    if (p.blocks[0] > INT_MAX / kJoinParts32) return B2SP_ERR_UNSUPPORTED;
     const b2sp_status rc = split(c, p, false, st, launches);
     if (rc != B2SP_OK) return rc;
     Args32 f = args(c, p, 0);
@@ -175,7 +179,7 @@ b2sp_status tiles32_forward(const Call32 &c, cudaStream_t st, int *launches)
         launch_behind_smem(tile_forward32_kernel, (unsigned)p.ctas[0], Fwd32::THREADS, Fwd32::BYTES, st, q, k, v, f);
         ++*launches;
     }
-    const unsigned joins = (unsigned)(p.blocks[0] * kJoinParts);
+    const unsigned joins = (unsigned)(p.blocks[0] * kJoinParts32);
     if (c.wide) launch_behind(tile_forward32_join_kernel<4>, joins, 256, st, f);
     else launch_behind(tile_forward32_join_kernel<1>, joins, 256, st, f);
     ++*launches;

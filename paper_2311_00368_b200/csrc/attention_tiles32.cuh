@@ -334,46 +334,52 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     if (warp == FIRST_WARP) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
 }
 
-// A CTA per 32 rows of a block: the sums of all sets of all CTAs that had tiles of it, in order.
+// A CTA per 16 rows of a block, a thread per four elements: the sums of all sets of all CTAs that had tiles of it, in order, each rescaled
+// when the reference moves.
+constexpr int kJoinRows32 = 16, kJoinParts32 = kTile / kJoinRows32;
 template <int V>
 __global__ void __launch_bounds__(256) tile_forward32_join_kernel(const __grid_constant__ Args32 f)
 {
     const GradArgsOf<float> &g = f.g;
     const TileArgsOf<float> &a = g.a;
     const Shape &s = a.g.s;
-    const int block = blockIdx.x / kJoinParts, part = blockIdx.x % kJoinParts, o = block / g.w.NB, blk = block % g.w.NB;
-    const int b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int block = blockIdx.x / kJoinParts32, part = blockIdx.x % kJoinParts32, o = block / g.w.NB, blk = block % g.w.NB;
+    const int b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows32;
     if (row0 >= s.M) return;
-    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, n = g.w.ahead(o, blk + 1) - ahead;
-    const int c0 = (int)(p0 / g.share), c1 = (int)((p0 + n - 1) / g.share);
     const int pat = pattern_of(s.patterns, s.batch, s.heads, b, h);
     const int *ptr = a.g.ptr + pat * a.g.ptr_stride;
+    const int col = (threadIdx.x & 15) * 4, r = threadIdx.x >> 4, row = row0 + r;
     __shared__ unsigned redo;
     if (threadIdx.x == 0) redo = 0;
     __syncthreads();
-    const int col = (threadIdx.x & 15) * 4;
-    for (int r = threadIdx.x >> 4; r < kJoinRows; r += 16) {
-        const int row = row0 + r;
-        if (row >= s.M) continue;
-        const bool live = n > 0 && ptr[row + 1] > ptr[row];
+    // (of the pattern and its plan, which the kernels ahead do not write)
+    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, n = g.w.ahead(o, blk + 1) - ahead;
+    const int c0 = (int)(p0 / g.share), c1 = (int)((p0 + n - 1) / g.share);
+    const bool live = row < s.M && n > 0 && ptr[row + 1] > ptr[row];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (row < s.M) {
         float x[4] = {}, m = -CUDART_INF_F, l = 0.f;
         if (live) {
-            for (int c = c0; c <= c1; ++c)
-#pragma unroll
-                for (int set = 0; set < Fwd32::SETS; ++set) m = fmaxf(m, f.part_ml[part_of(c, block, set, Fwd32::SETS) * kTile + part * kJoinRows + r].x);
-            for (int c = c0; c <= c1; ++c)
+            for (int c = c0; c <= c1; ++c) {
+                float2 ml[Fwd32::SETS];
+                float4 v[Fwd32::SETS];
 #pragma unroll
                 for (int set = 0; set < Fwd32::SETS; ++set) {
-                    const long long at = part_of(c, block, set, Fwd32::SETS) * kTile + part * kJoinRows + r;
-                    const float2 ml = f.part_ml[at];
-                    const float w = ex2(ml.x - m);   // (m is finite unless a product is infinite or NaN: then the row is taken one by one)
-                    const float4 v = *reinterpret_cast<const float4 *>(g.part + at * 64 + col);
-                    if (ml.x != -CUDART_INF_F) {
-                        l = fmaf(ml.y, w, l);
-                        x[0] = fmaf(v.x, w, x[0]); x[1] = fmaf(v.y, w, x[1]); x[2] = fmaf(v.z, w, x[2]); x[3] = fmaf(v.w, w, x[3]);
-                    }
+                    const long long at = part_of(c, block, set, Fwd32::SETS) * kTile + part * kJoinRows32 + r;
+                    ml[set] = f.part_ml[at];
+                    v[set] = *reinterpret_cast<const float4 *>(g.part + at * 64 + col);
                 }
+#pragma unroll
+                for (int set = 0; set < Fwd32::SETS; ++set) {
+                    if (ml[set].x == -CUDART_INF_F) continue;
+                    // (a reference is finite unless a product is infinite or NaN: then the row is taken one by one)
+                    const float to = fmaxf(m, ml[set].x), was = ex2(m - to), w = ex2(ml[set].x - to);
+                    m = to;
+                    l = fmaf(ml[set].y, w, l * was);
+                    x[0] = fmaf(v[set].x, w, x[0] * was); x[1] = fmaf(v[set].y, w, x[1] * was);
+                    x[2] = fmaf(v[set].z, w, x[2] * was); x[3] = fmaf(v[set].w, w, x[3] * was);
+                }
+            }
         }
         bool bad = live && !(l >= 7.8886091e-31f && l <= 3.402823466e38f);
         const float inv = live ? 1.f / l : 0.f;

@@ -59,7 +59,7 @@ def test_operands_workspace_and_algo(b):
     assert _forward(b, p, algo=b.ALGO_TILE) == UNSUPPORTED                                       # no plan
     assert _forward(b, _problem(b, d=65, plan=1 << 20, plan_tiles=1), o=_heads(b, 1 << 20, 65, 65 * 64, 65 * 64 * 8), algo=b.ALGO_TILE) == UNSUPPORTED   # fp32
     assert _forward(b, p, algo=b.ALGO_TILE, fn="b2sp_attention_bf16") == UNSUPPORTED             # no plan
-    for bad in (dict(d=60), dict(d=136)):
+    for bad in (dict(d=130), dict(d=136)):
         assert _forward(b, _problem(b, plan=1 << 20, plan_tiles=1, **bad), o=_heads(b, 1 << 20, 136, 136 * 64, 136 * 64 * 8), algo=b.ALGO_TILE,
                         fn="b2sp_attention_bf16") == UNSUPPORTED
     odd = _heads(b, (1 << 20) + 2, 64, 64 * 64, 64 * 64 * 8)

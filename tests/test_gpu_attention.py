@@ -115,6 +115,10 @@ TILE_SHAPES = [
     dict(M=200, K=200, d=64, kind="nothing"),
     dict(M=1000, K=1000, d=96, kind="full", spread=4.0),
     dict(M=700, K=2100, d=128, spread=8.0),
+    dict(M=1, K=1, d=1, kind="full"),                                       # widths that are staged
+    dict(B=2, H=4, Hkv=2, M=300, K=410, d=83, per="sequence", strided=True),
+    dict(H=3, Hkv=3, M=513, K=513, d=121, kind="window"),
+    dict(B=3, H=2, Hkv=1, M=140, K=700, d=50, per="problem", spread=4.0),
 ]
 
 
@@ -147,6 +151,16 @@ def test_tile_kernels_on_fp32(i):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_the_choice_of_the_library(dtype):
     Problem(400, B=2, H=4, Hkv=2, M=300, K=400, d=64, dtype=dtype).check(0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_few_entries_go_row_by_row_and_many_by_tiles(dtype):
+    b = _binding()
+    for more, algo in ((dict(M=1, K=8192, kind="full"), b.ALGO_ROW), (dict(M=1000, K=1000, kind="sparse"), b.ALGO_ROW),
+                       (dict(H=8, Hkv=2, M=2000, K=2000, kind="full"), b.ALGO_TILE)):
+        p = Problem(401, d=64, dtype=dtype, **more)
+        p.forward(0, p.plan())
+        assert b.attention_last_algo() == algo, more
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
