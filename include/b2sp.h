@@ -258,10 +258,14 @@ b2sp_status b2sp_fusedmm_batched_bf16(int batch, int M, int K, int Kd, int N, lo
  * 4194304 columns; b2sp_attention_plan_status (which synchronises) reports B2SP_ERR_BAD_CSR for a plan whose pattern has a column twice in
  * a row, a column out of range or row pointers that are not monotone within [0, nnz_stride]: such a plan must not be used.
  *
- * algo: B2SP_ALGO_ROW = CUDA-core row kernels (any sizes and alignment); B2SP_ALGO_TILE = tcgen05 kernels over the tiles of the plan
- * (bfloat16, d <= 128 and a multiple of 8, every operand's address and strides a multiple of 16 bytes; B2SP_ERR_UNSUPPORTED
- * otherwise); B2SP_ALGO_AUTO chooses by the number of entries and tiles.  The tile kernels round the weights p (and, backward, p (dp - delta))
- * to bfloat16 before the second products, as the operands are; the row kernels do not.
+ * algo: B2SP_ALGO_ROW = CUDA-core row kernels (any sizes and alignment); B2SP_ALGO_TILE = tcgen05 kernels over the tiles of the plan, for
+ * scale > 0 and
+ *   bfloat16: d <= 128; where d is a multiple of 8 every operand's address and strides have to be multiples of 16 bytes (other widths are
+ *             copied into the workspace).  The weights p (and, backward, p (dp - delta)) are rounded to bfloat16 before the second
+ *             products, as the operands are; the row kernels do not round them.
+ *   fp32:     d <= 64, any alignment.  Every number is taken apart into three bfloat16 numbers that add up to it; products keep what is above
+ *             2^-23 of each term.
+ * B2SP_ERR_UNSUPPORTED otherwise.  B2SP_ALGO_AUTO chooses by the number of entries and tiles.
  * Results do not depend on the order in which anything runs: the same call gives the same bits.
  * workspace: b2sp_attention_workspace_bytes bytes, as for the ops above (b2sp_device_status reads it too).
  */

@@ -3,16 +3,14 @@
 // At the densities that masks have (10% to 30% scattered, or dense inside a window) a 128 x 128 tile of the pattern is cheaper multiplied
 // whole than entry by entry: what is not stored is masked by the tile's 128 x 128 bits, which the plan holds ready.  Tiles without an entry are never
 // visited.
-//   forward  S = Q K^T into tensor memory; each thread of four softmax warps takes a row, masks, exponentiates, and writes the
-//            weights back to tensor memory as bfloat16, over S; O += P V accumulates in tensor memory.
-//   dQ       the same walk, S and dP = dO V^T side by side, ds = p (dp - delta) back as bfloat16, dQ += dS K.
-//   dK, dV   a CTA per 128 keys walks the tiles of its column block, 64 queries at a time, with everything transposed (rows of
-//            tensor memory are keys): dV += P^T dO, dK += dS^T Q, over all query heads that share the keys.
-// Two passes over the tiles in the backward direction (seven products instead of five, the weights twice) need neither atomics nor a slab
-// of fp32 gradients, so results are the same bits every time.
+//   forward  a CTA per 128 rows, 64 keys a step, two CTAs per SM: S = Q K^T into one of two places in tensor memory; each thread of four softmax
+//            warps takes a row, masks, exponentiates and writes the weights over S as bfloat16; O += P V accumulates in tensor memory.
+//   backward dQ, then dK with dV: see there.  Two passes over the tiles (seven products instead of five, the weights twice) need neither
+//            atomics nor a slab of fp32 gradients, so results are the same bits every time.
 //
-// What bounds them: the exponentials (16 a clock on an SM: 1024 clocks a tile) at width 64, together with the tensor core (two products of 512
-// clocks a tile) at width 128.  Two CTAs per SM take turns between the two.
+// What bounds the forward pass at width 64: the exponentials (16 a clock on an SM: 1024 clocks a tile of 128 x 128) and what stands around them, 64 us for
+// 8 x 4096 x 4096 at 20% (their unit is busy 54% to 68% of the time); at width 128 the tensor core (two products of 512 clocks a tile) is as
+// long: 83 us for 16 heads over 4 of 8192 under a window of 1024, 820 Tflop/s of the stored entries.
 //
 // The reference of the exponentials (the "maximum") is taken over all 128 products of a row's tile, masked or not, which spares the mask in
 // that sweep; it moves only when it grows by more than 8 (to base 2), so O is rarely rescaled.  A row that loses its weights to
@@ -551,6 +549,8 @@ using GradArgs = GradArgsOf<Bf16>;
 // Two warps issue products: one S and dP, as far ahead as sets of tensor memory are free, one the second products.  The tensor core takes
 // products from them in turn (about 52 cycles each at 128 x 64 x 16 from shared memory, 61 at 128 x 128 x 16 with A in tensor memory), and what
 // a warp spends between its batches -- 100 to 250 cycles a barrier -- is hidden by the other's; with one issuer it was idle 44% of the time.
+// 8 x 4096 x 4096 at 20%, width 64: 207 us with one issuer and a CTA per block, 193 us now; 16 heads over 4 of 8192, width 128, window
+// of 1024 and 64 keys that all see: 677 us, with shares (the 64 keys' column block is as long as 64 others) and two issuers 350 us.
 template <int MODE, int DP> struct GradCfg {
     static constexpr int SETS = MODE == kDkv && DP == 128 ? 2 : 3, THREADS = 256 * SETS + 96;
     static constexpr int STAGES = DP == 64 ? 6 : 4;
