@@ -49,13 +49,12 @@ template <int DP> b2sp_status forward(const TileCall &c, cudaStream_t st, int *l
 struct GradPlan {
     long long tiles[2];
     int outers[2], NB[2], share[2], ctas[2];
-    size_t starts[2], bad[2], part, bytes;   // offsets from `at`
+    size_t starts[2], bad[2], part[2], bytes;
 };
 GradPlan grad_plan(const Shape &s, long long tiles, size_t at)
 {
     GradPlan p;
     const int DP = s.d <= 64 ? 64 : 128;
-    size_t part = 0;
     for (int k = 0; k < 2; ++k) {
         p.tiles[k] = tiles * ((long long)s.batch * s.heads / s.patterns);
         p.outers[k] = s.batch * (k == 0 ? s.heads : s.kv_heads);
@@ -66,14 +65,14 @@ GradPlan grad_plan(const Shape &s, long long tiles, size_t at)
         at += up256((size_t)p.ctas[k] * 16);
         p.bad[k] = at;
         at += up256((size_t)p.outers[k] * p.NB[k] * 4);
-        part = std::max(part, (size_t)p.ctas[k] * 2 * (k + 1) * kTile * DP * 4);
+        p.part[k] = at;
+        at += (size_t)p.ctas[k] * 2 * (k + 1) * kTile * DP * 4;
     }
-    p.part = at;
-    p.bytes = at + up256(part);
+    p.bytes = at;
     return p;
 }
 
-template <int MODE, int DP> b2sp_status grad(const TileCall &c, const GradPlan &p, GradArgs g, cudaStream_t st, int *launches)
+template <int MODE, int DP> b2sp_status grad(const TileCall &c, const GradPlan &p, GradArgs &g, cudaStream_t st, int *launches)
 {
     static std::atomic<unsigned long long> done{0};
     using C = GradCfg<MODE, DP>;
@@ -87,8 +86,7 @@ template <int MODE, int DP> b2sp_status grad(const TileCall &c, const GradPlan &
         return B2SP_ERR_CUDA;
     if (g.ctas) {
         launch_behind_smem(tile_grad_kernel<MODE, DP>, (unsigned)g.ctas, C::THREADS, C::BYTES, st, x1, x2, y1, y2, g);
-        launch_behind(tile_grad_join_kernel<MODE, DP>, (unsigned)(g.ctas * kJoinParts), 256, st, g);
-        *launches += 2;
+        ++*launches;
     }
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
@@ -109,7 +107,7 @@ template <int DP> b2sp_status backward(const TileCall &c, cudaStream_t st, int *
         g[k].share = p.share[k]; g[k].ctas = p.ctas[k]; g[k].tiles = p.tiles[k];
         g[k].starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
         g[k].bad = reinterpret_cast<int *>(ws + p.bad[k]);
-        g[k].part = reinterpret_cast<float *>(ws + p.part);
+        g[k].part = reinterpret_cast<float *>(ws + p.part[k]);
         h.w[k] = g[k].w; h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.rows[k] = k == 0 ? s.M : s.K;
         h.starts[k] = reinterpret_cast<int4 *>(ws + p.starts[k]); h.bad[k] = g[k].bad;
     }
@@ -121,8 +119,12 @@ template <int DP> b2sp_status backward(const TileCall &c, cudaStream_t st, int *
     if (blocks + share_blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     tile_grad_stat_kernel<><<<(unsigned)(blocks + share_blocks), 256, 0, st>>>(s, c.o, c.dout, c.lse, (int)c.stat_stride, const_cast<float2 *>(c.stat), h, share_blocks, c.status);
     ++*launches;
-    const b2sp_status rc = grad<kDq, DP>(c, p, g[0], st, launches);
-    return rc == B2SP_OK ? grad<kDkv, DP>(c, p, g[1], st, launches) : rc;
+    b2sp_status rc = grad<kDq, DP>(c, p, g[0], st, launches);
+    if (rc == B2SP_OK) rc = grad<kDkv, DP>(c, p, g[1], st, launches);
+    if (rc != B2SP_OK || p.ctas[0] == 0) return rc;   // (both have CTAs, or neither)
+    launch_behind(tile_grad_join_kernel<DP>, (unsigned)((g[0].ctas + g[1].ctas) * kJoinParts), 256, st, g[0], g[1]);
+    ++*launches;
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
 
 // ---- widths that are no multiple of eight --------------------------------------------------------------------------------------------

@@ -824,9 +824,9 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     if (warp == FIRST_WARP) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
 }
 
-// Behind tile_grad_kernel.  Four CTAs of eight warps per share but the first: if a block that begins in the share before goes on in this one, its parts are
-// added up in order, 32 rows a CTA; rows whose sums are not finite are taken one by one.  The CTAs also go through the flags of the blocks that
-// were finished in one share.
+// Behind both passes of tile_grad_kernel.  Four CTAs of eight warps per share: if a block that begins in the share before goes on in this one, its
+// parts are added up in order, 32 rows a CTA, a thread's up to eight groups of four elements at once; rows whose sums are not finite are taken one by
+// one.  The CTAs also go through the flags of the blocks that were finished in one share.
 constexpr int kJoinRows = 32, kJoinParts = kTile / kJoinRows;
 template <int MODE, int DP, typename T, int V>
 __device__ __forceinline__ void tile_grad_rows(const GradArgsOf<T> &g, int o, int blk, int r)
@@ -836,16 +836,14 @@ __device__ __forceinline__ void tile_grad_rows(const GradArgsOf<T> &g, int o, in
     if (MODE == kDq) rows_one_by_one<kGradQ, DP, T, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
     else rows_one_by_one<kGradKV, DP, T, V>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
 }
-template <int MODE, int DP, typename T = Bf16, int V = 4>
-__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgsOf<T> g)
+template <int MODE, int DP, typename T, int V> __device__ __forceinline__ void tile_grad_join(const GradArgsOf<T> &g, int cta, int ctas, int &redo)
 {
-    constexpr int ACCS = MODE == kDkv ? 2 : 1, WIDE = ACCS * DP, LANES = WIDE / 4;   // threads that a row takes
+    constexpr int ACCS = MODE == kDkv ? 2 : 1, LANES = ACCS * DP / 4, GROUPS = kJoinRows * LANES / 256;   // threads that a row takes; groups of a thread
     const TileArgsOf<T> &a = g.a;
     const Shape &s = a.g.s;
-    const int share = blockIdx.x / kJoinParts, part = blockIdx.x % kJoinParts, warp = threadIdx.x >> 5;
+    const int share = cta / kJoinParts, part = cta % kJoinParts, warp = threadIdx.x >> 5;
     const int rows = MODE == kDq ? s.M : s.K;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int block = blockIdx.x; block < g.w.outers * g.w.NB; block += gridDim.x)
+    for (int block = cta; block < g.w.outers * g.w.NB; block += ctas)
         if (g.bad[block])
             for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, block / g.w.NB, block % g.w.NB, r);
     if (share == 0) return;
@@ -854,33 +852,45 @@ __global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_consta
     const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, p1 = p0 + g.w.ahead(o, blk + 1) - ahead;
     const int c0 = (int)(p0 / g.share), c1 = (int)((p1 - 1) / g.share);
     if (c0 != share - 1 || row0 >= rows) return;   // (the block begins with this share, or began before the last one)
-    __shared__ int redo;
-    if (threadIdx.x == 0) redo = 0;
-    __syncthreads();
-    // four elements a thread (of dK, then of dV)
+    // four elements a group (of dK, then of dV)
+    const int e = threadIdx.x % LANES * 4, acc = e / DP, col = e % DP, r0 = part * kJoinRows + threadIdx.x / LANES;
+    const float *from = g.part + ((long long)acc * kTile + r0) * DP + col;
+    float x[GROUPS][4] = {};
+    for (int c = c0; c <= c1; ++c) {
+        const float *p = from + ((long long)c * 2 + (c == c0)) * (ACCS * kTile * DP);
 #pragma unroll
-    for (int u = threadIdx.x; u < kJoinRows * LANES; u += 256) {
-        const int r = part * kJoinRows + u / LANES, e = u % LANES * 4, acc = e / DP, col = e % DP, row = blk * kTile + r;
-        if (row >= rows) continue;
-        float x[4] = {};
-        const float *from = g.part + ((long long)acc * kTile + r) * DP + col;
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-            const float4 v = *reinterpret_cast<const float4 *>(from + ((long long)c * 2 + (c == c0)) * (ACCS * kTile * DP));
-            x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
+        for (int u = 0; u < GROUPS; ++u) {
+            const float4 v = *reinterpret_cast<const float4 *>(p + u * (256 / LANES) * DP);
+            x[u][0] += v.x; x[u][1] += v.y; x[u][2] += v.z; x[u][3] += v.w;
         }
-        bool bad = false;
+    }
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < GROUPS; ++u) {
+        const int row = blk * kTile + r0 + u * (256 / LANES);
+        if (row >= rows) continue;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            x[k] *= acc ? 1.f : s.scale;
-            bad |= col + k < s.d && !(fabsf(x[k]) <= 3.402823466e38f);
+            x[u][k] *= acc ? 1.f : s.scale;
+            bad |= col + k < s.d && !(fabsf(x[u][k]) <= 3.402823466e38f);
         }
-        store4<T, V>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x);
-        if (bad) redo = 1;
+        store4<T, V>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x[u]);
     }
+    if (bad) redo = 1;
     __syncthreads();
     if (redo == 0) return;
     for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, o, blk, part * kJoinRows + r);
+}
+template <int DP, typename T = Bf16, int V = 4>
+__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgsOf<T> dq, const __grid_constant__ GradArgsOf<T> dkv)
+{
+    __shared__ int redo;
+    const int first = dkv.ctas * kJoinParts, cta = blockIdx.x;   // (dK and dV first: they have the longer blocks)
+    if (threadIdx.x == 0) redo = 0;
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (cta < first) tile_grad_join<kDkv, DP, T, V>(dkv, cta, first, redo);
+    else tile_grad_join<kDq, DP, T, V>(dq, cta - first, gridDim.x - first, redo);
 }
 
 // Ahead of both: row statistics (see attention_stat_kernel); and, in the first CTAs, where the shares begin, cleared flags of the blocks, and zeros for

@@ -18,7 +18,7 @@ constexpr int kSMs = 148;
 struct Plan32 {
     long long tiles[2], blocks[2];
     int outers[2], NB[2], share[2], ctas[2];
-    size_t starts[2], bad[2], q, k, v, dout, ml, part, bytes;
+    size_t starts[2], bad[2], part[2], q, k, v, dout, ml, bytes;
 };
 Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
 {
@@ -41,13 +41,12 @@ Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
         p.ctas[k] = (int)((p.tiles[k] + p.share[k] - 1) / p.share[k]);
         p.starts[k] = take((size_t)p.ctas[k] * 16);
         p.bad[k] = take(backward ? (size_t)p.blocks[k] * 4 : 0);
+        p.part[k] = take(backward ? (size_t)p.ctas[k] * 2 * (k + 1) * kTile * 64 * 4 : 0);
     }
-    if (backward) {
-        p.part = take((size_t)std::max(p.ctas[0], 2 * p.ctas[1]) * 2 * kTile * 64 * 4);
-    } else {
+    if (!backward) {
         const size_t parts = (size_t)(p.ctas[0] + p.blocks[0]) * Fwd32::SETS * kTile;
         p.ml = take(parts * 8);
-        p.part = take(parts * 64 * 4);
+        p.part[0] = take(parts * 64 * 4);
     }
     p.bytes = at;
     return p;
@@ -78,7 +77,7 @@ Args32 args(const Call32 &c, const Plan32 &p, int k)
     f.g.share = p.share[k]; f.g.ctas = p.ctas[k]; f.g.tiles = p.tiles[k];
     f.g.starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
     f.g.bad = reinterpret_cast<int *>(ws + p.bad[k]);
-    f.g.part = reinterpret_cast<float *>(ws + p.part);
+    f.g.part = reinterpret_cast<float *>(ws + p.part[k]);
     f.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
     f.wide = c.wide;
     return f;
@@ -125,13 +124,13 @@ b2sp_status split(const Call32 &c, const Plan32 &p, bool backward, cudaStream_t 
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
 
-template <int MODE> b2sp_status grad(const Call32 &c, const Plan32 &p, cudaStream_t st, int *launches)
+template <int MODE> b2sp_status grad(const Call32 &c, const Plan32 &p, Args32 &f, cudaStream_t st, int *launches)
 {
     static std::atomic<unsigned long long> done{0};
     using C = Grad32<MODE>;
     const Shape &s = c.s;
     if (p.ctas[MODE] == 0) return B2SP_OK;
-    Args32 f = args(c, p, MODE);
+    f = args(c, p, MODE);
     if (MODE == kDq) { f.g.a.g.out1 = c.dq; f.g.a.g.rows = s.M; }
     else { f.g.a.g.out1 = c.dk; f.g.a.g.out2 = c.dv; f.g.a.g.rows = s.K; }
     CUtensorMap x1, x2, y1, y2;
@@ -145,9 +144,7 @@ template <int MODE> b2sp_status grad(const Call32 &c, const Plan32 &p, cudaStrea
         !allow_smem(tile_grad32_kernel<MODE>, C::BYTES, done))
         return B2SP_ERR_CUDA;
     launch_behind_smem(tile_grad32_kernel<MODE>, (unsigned)p.ctas[MODE], C::THREADS, C::BYTES, st, x1, x2, y1, y2, f);
-    if (c.wide) launch_behind(tile_grad_join_kernel<MODE, 64, float, 4>, (unsigned)(p.ctas[MODE] * kJoinParts), 256, st, f.g);
-    else launch_behind(tile_grad_join_kernel<MODE, 64, float, 1>, (unsigned)(p.ctas[MODE] * kJoinParts), 256, st, f.g);
-    *launches += 2;
+    ++*launches;
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
 
@@ -191,8 +188,15 @@ b2sp_status tiles32_backward(const Call32 &c, cudaStream_t st, int *launches)
     const Plan32 p = plan32(c.s, c.tiles, c.scratch_at, true);
     if (p.blocks[0] > INT_MAX / 4 || p.blocks[1] > INT_MAX / 4) return B2SP_ERR_UNSUPPORTED;
     b2sp_status rc = split(c, p, true, st, launches);
-    if (rc == B2SP_OK) rc = grad<kDq>(c, p, st, launches);
-    return rc == B2SP_OK ? grad<kDkv>(c, p, st, launches) : rc;
+    Args32 f[2];
+    if (rc == B2SP_OK) rc = grad<kDq>(c, p, f[0], st, launches);
+    if (rc == B2SP_OK) rc = grad<kDkv>(c, p, f[1], st, launches);
+    if (rc != B2SP_OK || p.ctas[0] == 0) return rc;
+    const unsigned joins = (unsigned)((p.ctas[0] + p.ctas[1]) * kJoinParts);
+    if (c.wide) launch_behind(tile_grad_join_kernel<64, float, 4>, joins, 256, st, f[0].g, f[1].g);
+    else launch_behind(tile_grad_join_kernel<64, float, 1>, joins, 256, st, f[0].g, f[1].g);
+    ++*launches;
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
 
 }  // namespace attn
