@@ -12,7 +12,7 @@ namespace b2sp {
 namespace attn {
 namespace {
 
-constexpr int kSMs = 148;
+constexpr int kBlockCost = 2;   // tiles that a block's start and end take: under a window 0, 2, 4 give 339, 322, 322 us; with blocks of equal length no difference
 
 TileArgs args(const TileCall &c)
 {
@@ -49,7 +49,8 @@ template <int DP> b2sp_status forward(const TileCall &c, cudaStream_t st, int *l
 struct GradPlan {
     long long tiles[2];
     int outers[2], NB[2], share[2], ctas[2];
-    size_t starts[2], bad[2], part[2], bytes;
+    int per[2];
+    size_t starts[2], first[2], bad[2], part[2], bytes;
 };
 GradPlan grad_plan(const Shape &s, long long tiles, size_t at)
 {
@@ -59,10 +60,12 @@ GradPlan grad_plan(const Shape &s, long long tiles, size_t at)
         p.tiles[k] = tiles * ((long long)s.batch * s.heads / s.patterns);
         p.outers[k] = s.batch * (k == 0 ? s.heads : s.kv_heads);
         p.NB[k] = ((k == 0 ? s.M : s.K) + kTile - 1) / kTile;
-        p.share[k] = (int)std::max(1ll, (p.tiles[k] + kSMs - 1) / kSMs);
-        p.ctas[k] = (int)((p.tiles[k] + p.share[k] - 1) / p.share[k]);
+        const Shares x = deal(p.tiles[k], (long long)p.outers[k] * p.NB[k], kBlockCost, 1);
+        p.per[k] = x.per; p.share[k] = x.share; p.ctas[k] = x.ctas;
         p.starts[k] = at;
         at += up256((size_t)p.ctas[k] * 16);
+        p.first[k] = at;
+        at += up256((size_t)(p.ctas[k] + 1) * 8);
         p.bad[k] = at;
         at += up256((size_t)p.outers[k] * p.NB[k] * 4);
         p.part[k] = at;
@@ -102,20 +105,22 @@ template <int DP> b2sp_status backward(const TileCall &c, cudaStream_t st, int *
     h.kinds = 2;
     for (int k = 0; k < 2; ++k) {
         g[k].a = args(c);
-        g[k].w = Tiles{k == 0 ? c.plan.rb_ptr : c.plan.cb_ptr, p.NB[k], k == 0 ? s.heads : s.kv_heads, k == 0 ? 1 : s.heads / s.kv_heads, s.patterns, s.batch, s.heads, p.outers[k]};
+        g[k].w = Tiles{k == 0 ? c.plan.rb_ptr : c.plan.cb_ptr, p.NB[k], k == 0 ? s.heads : s.kv_heads, k == 0 ? 1 : s.heads / s.kv_heads, s.patterns, s.batch, s.heads, p.outers[k], p.per[k]};
         g[k].tile_at = k == 0 ? c.plan.tile_cb : reinterpret_cast<const int *>(c.plan.ctile);
-        g[k].share = p.share[k]; g[k].ctas = p.ctas[k]; g[k].tiles = p.tiles[k];
+        g[k].share = p.share[k]; g[k].ctas = p.ctas[k];
+        g[k].first = reinterpret_cast<long long *>(ws + p.first[k]);
         g[k].starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
         g[k].bad = reinterpret_cast<int *>(ws + p.bad[k]);
         g[k].part = reinterpret_cast<float *>(ws + p.part[k]);
         h.w[k] = g[k].w; h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.rows[k] = k == 0 ? s.M : s.K;
         h.starts[k] = reinterpret_cast<int4 *>(ws + p.starts[k]); h.bad[k] = g[k].bad;
+        h.first[k] = reinterpret_cast<long long *>(ws + p.first[k]); h.tiles[k] = p.tiles[k];
     }
     g[0].a.g.out1 = c.dq; g[0].a.g.rows = s.M;
     g[1].a.g.out1 = c.dk; g[1].a.g.out2 = c.dv; g[1].a.g.rows = s.K;
     h.out[0] = c.dq; h.out[1] = c.dk; h.out[2] = c.dv;
     const long long rows = (long long)s.batch * s.heads * c.stat_stride, blocks = (rows + 16 * kStatRows - 1) / (16 * kStatRows);
-    const int share_blocks = (std::max(std::max(1, p.ctas[0] + p.ctas[1]), std::max(p.outers[0] * p.NB[0], p.outers[1] * p.NB[1])) + 255) / 256;
+    const int share_blocks = (std::max(p.ctas[0] + p.ctas[1] + 2, std::max(p.outers[0] * p.NB[0], p.outers[1] * p.NB[1])) + 255) / 256;
     if (blocks + share_blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     tile_grad_stat_kernel<><<<(unsigned)(blocks + share_blocks), 256, 0, st>>>(s, c.o, c.dout, c.lse, (int)c.stat_stride, const_cast<float2 *>(c.stat), h, share_blocks, c.status);
     ++*launches;

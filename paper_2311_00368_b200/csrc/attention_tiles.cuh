@@ -414,7 +414,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 // memory, so that the tensor core works on the next steps while one is exponentiated; the second products' A operand (bfloat16) lies
 // over what its warp has read of S and dP.
 //
-// Work is dealt by tiles: the tiles of all blocks in one order (problem, block, query head of the group, tile), `share` to each CTA, so
+// Work is dealt by tiles: the tiles of all blocks in one order (problem, block, query head of the group, tile), to each CTA as many as cost `share` with what
+// the blocks cost that begin there (loading X, the sums' way out), so
 // that blocks of any lengths -- the keys that every query sees -- keep all SMs busy.  A block that lies in one share is finished there; of others each CTA leaves a
 // part in fp32: in slot 0 if the block began in an earlier share, in slot 1 if it begins in this one; tile_grad_join_kernel adds them up in order.
 enum { kDq = 0, kDkv = 1 };
@@ -424,6 +425,7 @@ enum { kDq = 0, kDkv = 1 };
 struct Tiles {
     const int *ptr;
     int NB, outer, group, patterns, batch, heads, outers;
+    int per;   // what a block costs beside its tiles, in tiles
     __device__ __forceinline__ int pattern(int o, int i) const { return pattern_of(patterns, batch, heads, o / outer, o % outer * group + i); }
     __device__ __forceinline__ int at(int pat, int blk) const { return ptr[(long long)pat * NB + blk]; }
     // tiles ahead of outer problem o
@@ -453,7 +455,27 @@ struct Tiles {
     }
 };
 
-// Where share c begins: (outer problem, block, query head of the group, tile).
+// The number of the first tile of the share that begins at cost `pos`: blocks cost `per` ahead of their tiles.
+__device__ __forceinline__ long long share_tile(const Tiles &w, long long pos)
+{
+    const long long each = (long long)w.per * w.NB;
+    int lo = 0, hi = w.outers;
+    while (hi - lo > 1) {
+        const int m = lo + ((hi - lo) >> 1);
+        if (w.base(m) + each * m <= pos) lo = m; else hi = m;
+    }
+    const int o = lo;
+    const long long before = w.base(o);
+    pos -= before + each * o;
+    lo = 0, hi = w.NB;
+    while (hi - lo > 1) {
+        const int m = lo + ((hi - lo) >> 1);
+        if (w.ahead(o, m) + (long long)w.per * m <= pos) lo = m; else hi = m;
+    }
+    const long long ahead = w.ahead(o, lo);
+    return before + ahead + max(0ll, pos - ahead - (long long)w.per * (lo + 1));
+}
+// Where tile number `pos` lies: (outer problem, block, query head of the group, tile).
 __device__ __forceinline__ int4 share_start(const Tiles &w, long long pos)
 {
     int lo = 0, hi = w.outers;
@@ -538,11 +560,20 @@ template <typename T> struct GradArgsOf {
     TileArgsOf<T> a;
     Tiles w;
     const int *tile_at;       // of a tile: its row or column block, the first of two ints for dK and dV
-    int share, ctas;
-    long long tiles;          // of all problems
-    const int4 *starts;       // of the CTAs
+    int share, ctas;          // cost of a CTA's blocks and tiles; CTAs
+    const int4 *starts;       // of the CTAs: where their first tile lies
+    const long long *first;   // its number, and that of the one behind the last CTA's
     float *part;              // [ctas][2][dK: 2][128][DP]
     int *bad;                 // [outers][blocks]: the sums of a block are not finite (its rows are taken one by one)
+    // The first and the last CTA that have tiles of a block (c1 < c0: it has none); returns their number.
+    __device__ __forceinline__ long long holders(int o, int blk, int &c0, int &c1) const
+    {
+        const long long ahead = w.ahead(o, blk), n = w.ahead(o, blk + 1) - ahead;
+        const long long p0 = w.base(o) + ahead + (long long)w.per * ((long long)o * w.NB + blk + 1);
+        c0 = (int)(p0 / share);
+        c1 = n ? (int)((p0 + n - 1) / share) : c0 - 1;
+        return n;
+    }
 };
 using GradArgs = GradArgsOf<Bf16>;
 
@@ -550,7 +581,8 @@ using GradArgs = GradArgsOf<Bf16>;
 // products from them in turn (about 52 cycles each at 128 x 64 x 16 from shared memory, 61 at 128 x 128 x 16 with A in tensor memory), and what
 // a warp spends between its batches -- 100 to 250 cycles a barrier -- is hidden by the other's; with one issuer it was idle 44% of the time.
 // 8 x 4096 x 4096 at 20%, width 64: 207 us with one issuer and a CTA per block, 193 us now; 16 heads over 4 of 8192, width 128, window
-// of 1024 and 64 keys that all see: 677 us, with shares (the 64 keys' column block is as long as 64 others) and two issuers 350 us.
+// of 1024 and 64 keys that all see: 677 us, with shares (the 64 keys' column block is as long as 64 others), two issuers and one join 339 us, and with blocks
+// counted as two tiles more 322 us.
 template <int MODE, int DP> struct GradCfg {
     static constexpr int SETS = MODE == kDkv && DP == 128 ? 2 : 3, THREADS = 256 * SETS + 96;
     static constexpr int STAGES = DP == 64 ? 6 : 4;
@@ -595,7 +627,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     ptx::tc_fence_after_sync();
     asm volatile("griddepcontrol.wait;" ::: "memory");   // the row statistics and the shares' starts
     const uint32_t tmem = ptx::lds32(slot);
-    const int tiles = (int)min((long long)g.share, g.tiles - (long long)blockIdx.x * g.share), steps = 2 * tiles;
+    const int tiles = (int)(g.first[blockIdx.x + 1] - g.first[blockIdx.x]), steps = 2 * tiles;
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {   // of a single thread
         if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
@@ -606,7 +638,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
         int i = 0, blocks = 0;
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
@@ -708,7 +740,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
         float2 own = make_float2(0.f, 0.f);
         unsigned some = 0;
         int first_i = w.i, first_t = w.t;   // where the block's part began (is it the block's beginning?)
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             const int blk = w.blk, o = w.o;
             if (w.fresh) {
                 some = 0;
@@ -846,11 +878,11 @@ template <int MODE, int DP, typename T, int V> __device__ __forceinline__ void t
     for (int block = cta; block < g.w.outers * g.w.NB; block += ctas)
         if (g.bad[block])
             for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, block / g.w.NB, block % g.w.NB, r);
-    if (share == 0) return;
+    if (share == 0 || g.first[share] == g.first[g.ctas]) return;
     const int4 at = g.starts[share];
     const int o = at.x, blk = at.y, b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
-    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, p1 = p0 + g.w.ahead(o, blk + 1) - ahead;
-    const int c0 = (int)(p0 / g.share), c1 = (int)((p1 - 1) / g.share);
+    int c0, c1;
+    g.holders(o, blk, c0, c1);
     if (c0 != share - 1 || row0 >= rows) return;   // (the block begins with this share, or began before the last one)
     // four elements a group (of dK, then of dV)
     const int e = threadIdx.x % LANES * 4, acc = e / DP, col = e % DP, r0 = part * kJoinRows + threadIdx.x / LANES;
@@ -900,6 +932,7 @@ template <typename T> struct ShareArgsOf {
     int kinds;           // 1: only w[0]
     int share[2], ctas[2], rows[2];
     int4 *starts[2];
+    long long *first[2], tiles[2];
     int *bad[2];         // NULL: neither flags nor zeros
     View<T> out[3];      // dQ, dK, dV
 };
@@ -907,9 +940,11 @@ using ShareArgs = ShareArgsOf<Bf16>;
 template <typename T> __device__ __forceinline__ void prepare_shares(const ShareArgsOf<T> &h, int d, int share_blocks)
 {
     const int u = blockIdx.x * 256 + threadIdx.x, lane = threadIdx.x & 31, total = h.ctas[0] + (h.kinds > 1 ? h.ctas[1] : 0);
-    for (int i = u; i < total; i += share_blocks * 256) {
-        const int k = i < h.ctas[0] ? 0 : 1, c = k ? i - h.ctas[0] : i;
-        h.starts[k][c] = share_start(h.w[k], (long long)c * h.share[k]);
+    for (int i = u; i < total + h.kinds; i += share_blocks * 256) {
+        const int k = i <= h.ctas[0] ? 0 : 1, c = k ? i - h.ctas[0] - 1 : i;
+        const long long first = c == h.ctas[k] ? h.tiles[k] : min(h.tiles[k], share_tile(h.w[k], (long long)c * h.share[k]));
+        h.first[k][c] = first;
+        if (c < h.ctas[k]) h.starts[k][c] = first < h.tiles[k] ? share_start(h.w[k], first) : make_int4(0, 0, 0, 0);
     }
     for (int k = 0; k < h.kinds; ++k) {
         const Tiles &w = h.w[k];

@@ -1,9 +1,25 @@
 // Interface between the attention entry points and the tensor-core kernels.
 #pragma once
+#include <algorithm>
+
 #include "attention_rows.cuh"
 
 namespace b2sp {
 namespace attn {
+
+// How tiles are dealt to CTAs, one per SM: equal shares of what tiles and blocks cost, a block `cost` tiles ahead of its own, but a quarter
+// of the average block at most (blocks without tiles cost nothing in truth); `least`: the smallest share.
+struct Shares { int per, share, ctas; };
+inline Shares deal(long long tiles, long long blocks, int cost, long long least)
+{
+    constexpr int kSMs = 148;
+    Shares x;
+    x.per = (int)std::min((long long)cost, tiles / std::max(1ll, 4 * blocks));
+    const long long total = tiles ? tiles + x.per * blocks : 0;
+    x.share = (int)std::max(std::max(least, 1ll), (total + kSMs - 1) / kSMs);
+    x.ctas = (int)((total + x.share - 1) / x.share);
+    return x;
+}
 
 struct TileCall {
     Shape s;

@@ -12,13 +12,13 @@ namespace b2sp {
 namespace attn {
 namespace {
 
-constexpr int kSMs = 148;
+constexpr int kBlockCost = 1;   // 1501 x 2903, six heads, 12%: 0, 1, 2, 4 give 63.5, 59.0, 62.6, 64.9 us forward and 184, 185, 190, 201 backward
 
 // Where things lie in the workspace from offset `at` on, and how tiles are dealt out: [0] forward and dQ (by rows), [1] dK and dV (by columns).
 struct Plan32 {
     long long tiles[2], blocks[2];
-    int outers[2], NB[2], share[2], ctas[2];
-    size_t starts[2], bad[2], part[2], q, k, v, dout, ml, bytes;
+    int outers[2], NB[2], share[2], ctas[2], per[2];
+    size_t starts[2], first[2], bad[2], part[2], q, k, v, dout, ml, bytes;
 };
 Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
 {
@@ -37,9 +37,10 @@ Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
         // Equal shares for all SMs; where a block's tiles are few that would leave more sums to join (0.7 us each, one after the other) than
         // it saves tiles (4 us each): not below the square root of a sixth of a block's tiles.
         const long long least = (long long)std::sqrt((double)p.tiles[k] / std::max(1ll, p.blocks[k]) / 6);
-        p.share[k] = (int)std::max(std::max(1ll, least), (p.tiles[k] + kSMs - 1) / kSMs);
-        p.ctas[k] = (int)((p.tiles[k] + p.share[k] - 1) / p.share[k]);
+        const Shares x = deal(p.tiles[k], p.blocks[k], kBlockCost, least);
+        p.per[k] = x.per; p.share[k] = x.share; p.ctas[k] = x.ctas;
         p.starts[k] = take((size_t)p.ctas[k] * 16);
+        p.first[k] = take((size_t)(p.ctas[k] + 1) * 8);
         p.bad[k] = take(backward ? (size_t)p.blocks[k] * 4 : 0);
         p.part[k] = take(backward ? (size_t)p.ctas[k] * 2 * (k + 1) * kTile * 64 * 4 : 0);
     }
@@ -55,7 +56,7 @@ Plan32 plan32(const Shape &s, long long tiles, size_t at, bool backward)
 Tiles tiles_of(const Call32 &c, const Plan32 &p, int k)
 {
     const Shape &s = c.s;
-    return Tiles{k == 0 ? c.plan.rb_ptr : c.plan.cb_ptr, p.NB[k], k == 0 ? s.heads : s.kv_heads, k == 0 ? 1 : s.heads / s.kv_heads, s.patterns, s.batch, s.heads, p.outers[k]};
+    return Tiles{k == 0 ? c.plan.rb_ptr : c.plan.cb_ptr, p.NB[k], k == 0 ? s.heads : s.kv_heads, k == 0 ? 1 : s.heads / s.kv_heads, s.patterns, s.batch, s.heads, p.outers[k], p.per[k]};
 }
 
 Args32 args(const Call32 &c, const Plan32 &p, int k)
@@ -74,7 +75,8 @@ Args32 args(const Call32 &c, const Plan32 &p, int k)
     f.g.a.status = c.status;
     f.g.w = tiles_of(c, p, k);
     f.g.tile_at = k == 0 ? c.plan.tile_cb : reinterpret_cast<const int *>(c.plan.ctile);
-    f.g.share = p.share[k]; f.g.ctas = p.ctas[k]; f.g.tiles = p.tiles[k];
+    f.g.share = p.share[k]; f.g.ctas = p.ctas[k];
+    f.g.first = reinterpret_cast<long long *>(ws + p.first[k]);
     f.g.starts = reinterpret_cast<int4 *>(ws + p.starts[k]);
     f.g.bad = reinterpret_cast<int *>(ws + p.bad[k]);
     f.g.part = reinterpret_cast<float *>(ws + p.part[k]);
@@ -111,8 +113,9 @@ b2sp_status split(const Call32 &c, const Plan32 &p, bool backward, cudaStream_t 
         h.w[k] = tiles_of(c, p, k);
         h.share[k] = p.share[k]; h.ctas[k] = p.ctas[k]; h.rows[k] = k == 0 ? s.M : s.K;
         h.starts[k] = reinterpret_cast<int4 *>(ws + p.starts[k]);
+        h.first[k] = reinterpret_cast<long long *>(ws + p.first[k]); h.tiles[k] = p.tiles[k];
         h.bad[k] = backward ? reinterpret_cast<int *>(ws + p.bad[k]) : nullptr;
-        most = std::max(most, std::max(p.blocks[k], (long long)p.ctas[0] + p.ctas[1]));
+        most = std::max(most, std::max(p.blocks[k], (long long)p.ctas[0] + p.ctas[1] + 2));
     }
     h.out[0] = c.dq; h.out[1] = c.dk; h.out[2] = c.dv;
     const int share_blocks = (int)((most + 255) / 256);

@@ -144,7 +144,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     ptx::tc_fence_after_sync();
     asm volatile("griddepcontrol.wait;" ::: "memory");   // planes and shares
     const uint32_t tmem = ptx::lds32(slot);
-    const int tiles = (int)min((long long)g.share, g.tiles - (long long)blockIdx.x * g.share), steps = 2 * tiles;
+    const int tiles = (int)(g.first[blockIdx.x + 1] - g.first[blockIdx.x]), steps = 2 * tiles;
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
         if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
@@ -155,7 +155,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
         int i = 0, blocks = 0;
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
             more = w.left > 0;
@@ -250,7 +250,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 for (int k = 0; k < 16; ++k) acc[c + k] += __uint_as_float(x[k]);
             }
         };
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             const int blk = w.blk, o = w.o;
             const uint4 now = __ldg(a.plan.masks + (long long)w.t * kTile + lane_row);
             for (int half = 0; half < 2; ++half) {
@@ -355,8 +355,8 @@ __global__ void __launch_bounds__(256) tile_forward32_join_kernel(const __grid_c
     if (threadIdx.x == 0) redo = 0;
     __syncthreads();
     // (of the pattern and its plan, which the kernels ahead do not write)
-    const long long ahead = g.w.ahead(o, blk), p0 = g.w.base(o) + ahead, n = g.w.ahead(o, blk + 1) - ahead;
-    const int c0 = (int)(p0 / g.share), c1 = (int)((p0 + n - 1) / g.share);
+    int c0, c1;
+    const long long n = g.holders(o, blk, c0, c1);
     const bool live = row < s.M && n > 0 && ptr[row + 1] > ptr[row];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (row < s.M) {
@@ -448,7 +448,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
     ptx::tc_fence_after_sync();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t tmem = ptx::lds32(slot);
-    const int tiles = (int)min((long long)g.share, g.tiles - (long long)blockIdx.x * g.share), steps = 2 * tiles;
+    const int tiles = (int)(g.first[blockIdx.x + 1] - g.first[blockIdx.x]), steps = 2 * tiles;
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
         if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
@@ -459,7 +459,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
         int i = 0, blocks = 0;
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
@@ -548,7 +548,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
         w.start(g.w, g.starts[blockIdx.x], tiles);
         int at_set = 0, round = 0, st = 0;
         float2 own = make_float2(0.f, 0.f);
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             if (MODE == kDq && w.fresh) own = a.g.stat[(long long)w.o * a.g.stat_stride + w.blk * kTile + lane_row];
             const uint4 now = __ldg((MODE == kDq ? a.plan.masks : a.plan.tmasks) + (long long)w.t * kTile + lane_row);
             const uint64_t l2 = two(own.x, own.x), d2 = two(own.y, own.y);
@@ -617,7 +617,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
         w.start(g.w, g.starts[blockIdx.x], tiles);
         int i = 0, first_i = w.i, first_t = w.t;
         unsigned some = 0;
-        for (bool more = true; more && ok;) {
+        for (bool more = tiles > 0; more && ok;) {
             const int blk = w.blk, o = w.o;
             if (w.fresh) {
                 some = 0;
