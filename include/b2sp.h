@@ -246,7 +246,7 @@ b2sp_status b2sp_fusedmm_batched_bf16(int batch, int M, int K, int Kd, int N, lo
  * batch * heads, sequence by sequence); pattern p has its row pointers, counted from 0, at row_ptr + p * row_ptr_stride and its
  * column indices at col_idx + p * nnz_stride; nnz_stride >= every row_ptr_p[M].
  * Operands are b2sp_heads: element (b, h, i, e) of a [batch][heads][rows][d] operand is data[b * stride_batch + h * stride_head +
- * i * ld + e], strides in elements; an input's strides may be 0, the elements of an output must not overlap.  Q, O, dO, dQ have `heads`
+ * i * ld + e], strides in elements; an input's strides may be 0, the elements of an output must not overlap, nor lie in an input.  Q, O, dO, dQ have `heads`
  * heads of M rows; K, V, dK, dV have kv_heads heads of K rows.  lse is fp32 [batch][heads][M].  d <= 256.
  * The fp32 entry points take and give fp32; the _bf16 ones bfloat16 (lse, sums and softmax statistics stay fp32).
  *

@@ -501,6 +501,8 @@ def _scratch(need, device, workspace, stream):
     """`workspace`, or one that this module keeps per device and stream; a call that is being captured gets one of its own, which
     belongs to the graph, so that graphs can be replayed side by side."""
     if workspace is not None:
+        if workspace.dtype is not torch.uint8 or workspace.device != device:
+            raise ValueError(f"workspace must be uint8 on {device}")
         return workspace
     if _capturing():
         return torch.empty(need, dtype=torch.uint8, device=device)

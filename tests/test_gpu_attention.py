@@ -336,3 +336,24 @@ def test_no_rows_or_no_columns():
     assert (o == 0).all() and (lse == -np.inf).all()
     dq, dk, dv = b.attention_backward(rp, ci, z(1, 1, 2, 8), z(1, 1, 0, 8), z(1, 1, 0, 8), o, lse, z(1, 1, 2, 8), plan)
     assert (dq == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("more", [dict(H=8, Hkv=2, M=1200, K=1200, kind="window"), dict(B=2, H=3, Hkv=3, M=513, K=300, per="problem"),
+                                  dict(H=2, Hkv=1, M=150, K=4000), dict(B=4, M=4000, K=140)])
+def test_no_wait_runs_out(more, dtype):
+    """The tile kernels' waits are bounded and a row that one of them gives up is taken otherwise: the status word tells."""
+    b, p = _binding(), Problem(700, d=64, dtype=dtype, **more)
+    plan, ws = p.plan(), torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    for _ in range(5):
+        o, lse = p.forward(b.ALGO_TILE, plan, workspace=ws)
+        assert b.device_status(ws) == 0
+        p.backward(o, lse, plan, b.ALGO_TILE, workspace=ws)
+        assert b.device_status(ws) == 0
+
+
+def test_a_workspace_of_the_wrong_kind():
+    p = Problem(701)
+    for ws in (torch.empty(1 << 20, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            p.forward(0, p.plan(), workspace=ws)
