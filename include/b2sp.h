@@ -263,7 +263,8 @@ b2sp_status b2sp_fusedmm_batched_bf16(int batch, int M, int K, int Kd, int N, lo
  *   bfloat16: d <= 128; where d is a multiple of 8 every operand's address and strides have to be multiples of 16 bytes (other widths are
  *             copied into the workspace).  The weights p (and, backward, p (dp - delta)) are rounded to bfloat16 before the second
  *             products, as the operands are; the row kernels do not round them.
- *   fp32:     d <= 64, any alignment.  Every number is taken apart into three bfloat16 numbers that add up to it; products keep what is above
+ *   fp32:     d <= 128, any alignment; above 64 the products of the tiles lie in the workspace, 64 KB a tile and problem (backward 128), up to
+ *             2 GB of them.  Every number is taken apart into three bfloat16 numbers that add up to it; products keep what is above
  *             2^-23 of each term.
  * B2SP_ERR_UNSUPPORTED otherwise.  B2SP_ALGO_AUTO chooses by the number of entries and tiles.
  * Results do not depend on the order in which anything runs: the same call gives the same bits.
@@ -287,8 +288,9 @@ size_t b2sp_attention_plan_bytes(int patterns, int M, int K, long long nnz_strid
 b2sp_status b2sp_attention_prepare(int patterns, int M, int K, long long nnz_stride, const int *row_ptr, long long row_ptr_stride,
                                    const int *col_idx, long long tiles, void *plan, size_t plan_bytes, void *stream);
 b2sp_status b2sp_attention_plan_status(const void *plan, void *stream);
-/* Bytes for the forward (backward = 0) or the backward call, whatever algo and type; 0 on invalid arguments. */
+/* Bytes for the forward (backward = 0) or the backward call of a type, whatever algo; 0 on invalid arguments. */
 size_t b2sp_attention_workspace_bytes(const b2sp_attention_problem *problem, int backward);
+size_t b2sp_attention_workspace_bytes_bf16(const b2sp_attention_problem *problem, int backward);
 b2sp_status b2sp_attention(const b2sp_attention_problem *problem, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V,
                            const b2sp_heads *O, float *lse, void *workspace, size_t workspace_bytes, int algo, void *stream);
 b2sp_status b2sp_attention_bf16(const b2sp_attention_problem *problem, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V,

@@ -111,6 +111,8 @@ lib.b2sp_attention_plan_status.restype = _i
 lib.b2sp_attention_plan_status.argtypes = [_vp, _vp]
 lib.b2sp_attention_workspace_bytes.restype = _sz
 lib.b2sp_attention_workspace_bytes.argtypes = [_pp, _i]
+lib.b2sp_attention_workspace_bytes_bf16.restype = _sz
+lib.b2sp_attention_workspace_bytes_bf16.argtypes = [_pp, _i]
 lib.b2sp_attention.restype = _i
 lib.b2sp_attention.argtypes = [_pp, _ph, _ph, _ph, _ph, _vp, _vp, _sz, _i, _vp]
 lib.b2sp_attention_bf16.restype = _i
@@ -569,9 +571,10 @@ def _rows(t, shape, dtype, name):
 
 
 @functools.lru_cache(maxsize=4096)
-def _attention_need(sizes, nnz_stride, tiles, backward):
+def _attention_need(sizes, nnz_stride, tiles, backward, dtype):
     """b2sp_attention_workspace_bytes, which goes by sizes only (tiles: -1 without a plan)."""
-    return lib.b2sp_attention_workspace_bytes(_PROBLEM(*sizes, 1.0, 256, sizes[3] + 1, 256, nnz_stride, 256 if tiles >= 0 else 0,
+    fn = lib.b2sp_attention_workspace_bytes if dtype == torch.float32 else lib.b2sp_attention_workspace_bytes_bf16
+    return fn(_PROBLEM(*sizes, 1.0, 256, sizes[3] + 1, 256, nnz_stride, 256 if tiles >= 0 else 0,
                                                                max(tiles, 0)), backward)
 
 
@@ -627,7 +630,7 @@ def attention(row_ptr, col_idx, q, k, v, scale=None, plan=None, out=None, lse=No
         _lse(lse, qs[:3])
         _ready(device, lse)
     stream = _raw_stream(device.index)
-    ws = _scratch(_attention_need(sizes, nzs, -1 if plan is None else plan.tiles, 0), device, workspace, stream)
+    ws = _scratch(_attention_need(sizes, nzs, -1 if plan is None else plan.tiles, 0, dtype), device, workspace, stream)
     fn, name = ((lib.b2sp_attention, "b2sp_attention") if dtype == torch.float32 else (lib.b2sp_attention_bf16, "b2sp_attention_bf16"))
     _check(fn(p, hq, hk, hv, _rows(out, qs, dtype, "out"), lse.data_ptr(), ws.data_ptr(), ws.numel(), algo, stream), name)
     return out, lse
@@ -651,7 +654,7 @@ def attention_backward(row_ptr, col_idx, q, k, v, out, lse, dout, plan, scale=No
         _ready(device, *given)
     dq, dk, dv = fresh(q) if dq is None else dq, fresh(k) if dk is None else dk, fresh(v) if dv is None else dv
     stream = _raw_stream(device.index)
-    ws = _scratch(_attention_need(sizes, nzs, plan.tiles, 1), device, workspace, stream)
+    ws = _scratch(_attention_need(sizes, nzs, plan.tiles, 1, dtype), device, workspace, stream)
     fn, name = ((lib.b2sp_attention_backward, "b2sp_attention_backward") if dtype == torch.float32
                 else (lib.b2sp_attention_backward_bf16, "b2sp_attention_backward_bf16"))
     _check(fn(p, h[0], h[1], h[2], h[3], lse.data_ptr(), h[4], _rows(dq, qs, dtype, "dq"), _rows(dk, ks, dtype, "dk"), _rows(dv, ks, dtype, "dv"),

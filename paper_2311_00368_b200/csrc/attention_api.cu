@@ -91,7 +91,7 @@ struct RowPlan {
     size_t stat, ml, part, bytes;         // offsets
     int stat_rows;
 };
-RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles, bool planned)
+RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles, bool planned, bool fp32)
 {
     RowPlan r;
     const long long problems = (long long)s.batch * s.heads;
@@ -108,8 +108,7 @@ RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles, 
     if (backward && r.parts_kv) part = std::max(part, uk * part_width(kGradKV, s.d) * 4);
     r.part = take(part);
     r.bytes = at;   // (the tile kernels use what lies behind the statistics)
-    if (planned) r.bytes = std::max(r.bytes, tiles32_bytes(s, tiles, r.ml, backward));
-    if (planned) r.bytes = std::max(r.bytes, tiles_bytes(s, tiles, r.ml, backward));
+    if (planned) r.bytes = std::max(r.bytes, fp32 ? tiles32_bytes(s, tiles, r.ml, backward) : tiles_bytes(s, tiles, r.ml, backward));
     return r;
 }
 
@@ -192,7 +191,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
         return rc;
     if (p->M && !lse) return B2SP_ERR_INVALID_ARG;
     const Shape s = shape(p);
-    const RowPlan w = row_plan(s, p->nnz_stride, false, p->plan_tiles, p->plan != nullptr);
+    const RowPlan w = row_plan(s, p->nnz_stride, false, p->plan_tiles, p->plan != nullptr, sizeof(T) == 4);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < w.bytes) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
@@ -218,7 +217,7 @@ b2sp_status forward(const b2sp_attention_problem *p, const b2sp_heads *Q, const 
             return tiles_forward(c, st, &launches);
         }
     } else {
-        const bool can = p->plan && tiles32_possible(s);
+        const bool can = p->plan && tiles32_possible(s, p->plan_tiles, false);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
         if (can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, false, true)))) {
             Call32 c = call32(p, s, ws);
@@ -257,7 +256,7 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         return rc;
     if (p->M && !lse) return B2SP_ERR_INVALID_ARG;
     const Shape s = shape(p);
-    const RowPlan w = row_plan(s, p->nnz_stride, true, p->plan_tiles, true);
+    const RowPlan w = row_plan(s, p->nnz_stride, true, p->plan_tiles, true, sizeof(T) == 4);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < w.bytes) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
@@ -271,7 +270,7 @@ b2sp_status backward(const b2sp_attention_problem *p, const b2sp_heads *Q, const
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
         tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true, false)));
     } else {
-        const bool can = tiles32_possible(s);
+        const bool can = tiles32_possible(s, p->plan_tiles, true);
         if (algo == B2SP_ALGO_TILE && !can) return B2SP_ERR_UNSUPPORTED;
         tiles = can && (algo == B2SP_ALGO_TILE || (algo == B2SP_ALGO_AUTO && prefer_tiles(s, p->nnz_stride, p->plan_tiles, true, true)));
     }
@@ -409,11 +408,15 @@ extern "C" b2sp_status b2sp_attention_plan_status(const void *plan, void *stream
     return h == 0 ? B2SP_OK : B2SP_ERR_BAD_CSR;
 }
 
-extern "C" size_t b2sp_attention_workspace_bytes(const b2sp_attention_problem *p, int backward)
+namespace {
+size_t need(const b2sp_attention_problem *p, int backward, bool fp32)
 {
     if (check_problem(p) != B2SP_OK) return 0;
-    return row_plan(shape(p), p->nnz_stride, backward != 0, p->plan_tiles, p->plan != nullptr || backward).bytes;
+    return row_plan(shape(p), p->nnz_stride, backward != 0, p->plan_tiles, p->plan != nullptr || backward, fp32).bytes;
 }
+}  // namespace
+extern "C" size_t b2sp_attention_workspace_bytes(const b2sp_attention_problem *p, int backward) { return need(p, backward, true); }
+extern "C" size_t b2sp_attention_workspace_bytes_bf16(const b2sp_attention_problem *p, int backward) { return need(p, backward, false); }
 
 extern "C" b2sp_status b2sp_attention(const b2sp_attention_problem *p, const b2sp_heads *Q, const b2sp_heads *K, const b2sp_heads *V, const b2sp_heads *O,
                                       float *lse, void *workspace, size_t workspace_bytes, int algo, void *stream)

@@ -127,7 +127,7 @@ template <int DP> b2sp_status backward(const TileCall &c, cudaStream_t st, int *
     b2sp_status rc = grad<kDq, DP>(c, p, g[0], st, launches);
     if (rc == B2SP_OK) rc = grad<kDkv, DP>(c, p, g[1], st, launches);
     if (rc != B2SP_OK || p.ctas[0] == 0) return rc;   // (both have CTAs, or neither)
-    launch_behind(tile_grad_join_kernel<DP>, (unsigned)((g[0].ctas + g[1].ctas) * kJoinParts), 256, st, g[0], g[1]);
+    launch_behind(tile_grad_join_kernel<DP>, (unsigned)((g[0].ctas + g[1].ctas) * kJoinParts), 256, st, g[0], g[1], 0, s.d);
     ++*launches;
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }

@@ -860,15 +860,17 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
 // parts are added up in order, 32 rows a CTA, a thread's up to eight groups of four elements at once; rows whose sums are not finite are taken one by
 // one.  The CTAs also go through the flags of the blocks that were finished in one share.
 constexpr int kJoinRows = 32, kJoinParts = kTile / kJoinRows;
-template <int MODE, int DP, typename T, int V>
+template <int MODE, int DW, typename T, int V>
 __device__ __forceinline__ void tile_grad_rows(const GradArgsOf<T> &g, int o, int blk, int r)
 {
     const TileArgsOf<T> &a = g.a;
     const int b = o / g.w.outer, h = o % g.w.outer, row = blk * kTile + r;
-    if (MODE == kDq) rows_one_by_one<kGradQ, DP, T, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
-    else rows_one_by_one<kGradKV, DP, T, V>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
+    if (MODE == kDq) rows_one_by_one<kGradQ, DW, T, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
+    else rows_one_by_one<kGradKV, DW, T, V>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
 }
-template <int MODE, int DP, typename T, int V> __device__ __forceinline__ void tile_grad_join(const GradArgsOf<T> &g, int cta, int ctas, int &redo)
+// DP: columns of the sums; they are columns col0 and on of the outputs, dc of them.  DW: width class of whole rows.
+template <int MODE, int DP, int DW, typename T, int V>
+__device__ __forceinline__ void tile_grad_join(const GradArgsOf<T> &g, int cta, int ctas, int col0, int dc, int &redo)
 {
     constexpr int ACCS = MODE == kDkv ? 2 : 1, LANES = ACCS * DP / 4, GROUPS = kJoinRows * LANES / 256;   // threads that a row takes; groups of a thread
     const TileArgsOf<T> &a = g.a;
@@ -877,7 +879,7 @@ template <int MODE, int DP, typename T, int V> __device__ __forceinline__ void t
     const int rows = MODE == kDq ? s.M : s.K;
     for (int block = cta; block < g.w.outers * g.w.NB; block += ctas)
         if (g.bad[block])
-            for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, block / g.w.NB, block % g.w.NB, r);
+            for (int r = warp; r < kTile && block % g.w.NB * kTile + r < rows; r += 8) tile_grad_rows<MODE, DW, T, V>(g, block / g.w.NB, block % g.w.NB, r);
     if (share == 0 || g.first[share] == g.first[g.ctas]) return;
     const int4 at = g.starts[share];
     const int o = at.x, blk = at.y, b = o / g.w.outer, h = o % g.w.outer, row0 = blk * kTile + part * kJoinRows;
@@ -904,25 +906,25 @@ template <int MODE, int DP, typename T, int V> __device__ __forceinline__ void t
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             x[u][k] *= acc ? 1.f : s.scale;
-            bad |= col + k < s.d && !(fabsf(x[u][k]) <= 3.402823466e38f);
+            bad |= col + k < dc && !(fabsf(x[u][k]) <= 3.402823466e38f);
         }
-        store4<T, V>((acc ? a.g.out2 : a.g.out1).at(b, h, row), col, s.d, x[u]);
+        store4<T, V>((acc ? a.g.out2 : a.g.out1).at(b, h, row) + col0, col, dc, x[u]);
     }
     if (bad) redo = 1;
     __syncthreads();
     if (redo == 0) return;
-    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) tile_grad_rows<MODE, DP, T, V>(g, o, blk, part * kJoinRows + r);
+    for (int r = warp; r < kJoinRows && row0 + r < rows; r += 8) tile_grad_rows<MODE, DW, T, V>(g, o, blk, part * kJoinRows + r);
 }
-template <int DP, typename T = Bf16, int V = 4>
-__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgsOf<T> dq, const __grid_constant__ GradArgsOf<T> dkv)
+template <int DP, typename T = Bf16, int V = 4, int DW = DP>
+__global__ void __launch_bounds__(256) tile_grad_join_kernel(const __grid_constant__ GradArgsOf<T> dq, const __grid_constant__ GradArgsOf<T> dkv, int col0, int dc)
 {
     __shared__ int redo;
     const int first = dkv.ctas * kJoinParts, cta = blockIdx.x;   // (dK and dV first: they have the longer blocks)
     if (threadIdx.x == 0) redo = 0;
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (cta < first) tile_grad_join<kDkv, DP, T, V>(dkv, cta, first, redo);
-    else tile_grad_join<kDq, DP, T, V>(dq, cta - first, gridDim.x - first, redo);
+    if (cta < first) tile_grad_join<kDkv, DP, DW, T, V>(dkv, cta, first, col0, dc, redo);
+    else tile_grad_join<kDq, DP, DW, T, V>(dq, cta - first, gridDim.x - first, col0, dc, redo);
 }
 
 // Ahead of both: row statistics (see attention_stat_kernel); and, in the first CTAs, where the shares begin, cleared flags of the blocks, and zeros for

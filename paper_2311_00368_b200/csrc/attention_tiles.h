@@ -60,7 +60,7 @@ struct Call32 {
     void *workspace;
     size_t scratch_at;
 };
-bool tiles32_possible(const Shape &s);
+bool tiles32_possible(const Shape &s, long long tiles, bool backward);
 size_t tiles32_bytes(const Shape &s, long long tiles, size_t at, bool backward);
 b2sp_status tiles32_forward(const Call32 &c, cudaStream_t st, int *launches);
 b2sp_status tiles32_backward(const Call32 &c, cudaStream_t st, int *launches);

@@ -38,11 +38,11 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t &p1, uint32_t 
 // ---- operands to planes --------------------------------------------------------------------------------------------------------------
 struct SplitArgs {
     View<const float> x[4];
-    Bf16 *planes[4];         // [batch][heads][rows][192]
-    int heads[4], rows[4], count, d, batch;
+    Bf16 *planes[4];         // [batch][heads][rows][chunks][192]
+    int heads[4], rows[4], count, d, batch, chunks;
     long long before[5];     // rows of the tensors ahead
 };
-// Sixteen threads per row, four elements each; in the first CTAs, where the shares begin.
+// Sixteen threads per row and chunk of 64 columns, four elements each; in the first CTAs, where the shares begin.
 template <int V>
 __global__ void __launch_bounds__(256) split_planes_kernel(const __grid_constant__ SplitArgs a, const __grid_constant__ ShareArgsOf<float> h, int share_blocks, int *status)
 {
@@ -52,35 +52,38 @@ __global__ void __launch_bounds__(256) split_planes_kernel(const __grid_constant
         prepare_shares(h, a.d, share_blocks);
         return;
     }
-    const long long row = (blockIdx.x - share_blocks) * 16ll + (threadIdx.x >> 4);
+    const int lanes = 16 * a.chunks;   // 16 or 32
+    const long long row = (blockIdx.x - share_blocks) * (256ll / lanes) + threadIdx.x / lanes;
     if (row >= a.before[a.count]) return;
     int t = 0;
     while (t + 1 < a.count && row >= a.before[t + 1]) ++t;
     const long long in = row - a.before[t];
-    const int prob = (int)(in / a.rows[t]), c = (threadIdx.x & 15) * 4;
+    const int prob = (int)(in / a.rows[t]), c = threadIdx.x % lanes * 4;
     float x[4];
     load4<float, V>(a.x[t].at(prob / a.heads[t], prob % a.heads[t], in % a.rows[t]), c, a.d, x);
     uint2 p[3];
     split3(x[0], x[1], p[0].x, p[1].x, p[2].x);
     split3(x[2], x[3], p[0].y, p[1].y, p[2].y);
-    uint2 *to = reinterpret_cast<uint2 *>(a.planes[t] + in * kPlanes + c);
+    uint2 *to = reinterpret_cast<uint2 *>(a.planes[t] + (in * a.chunks + c / kPlane) * kPlanes + c % kPlane);
 #pragma unroll
     for (int k = 0; k < 3; ++k) to[k * (kPlane / 4)] = p[k];
 }
 
-template <int ROWS> __device__ __forceinline__ void load_planes(uint32_t dst, const CUtensorMap *tm, uint32_t bar, int row, int h, int b)
+template <int ROWS> __device__ __forceinline__ void load_planes(uint32_t dst, const CUtensorMap *tm, uint32_t bar, int chunk, int row, int h, int b)
 {
 #pragma unroll
-    for (int p = 0; p < 3; ++p) tma_load_4d(dst + p * ROWS * 128, tm, bar, p * kPlane, row, h, b);
+    for (int p = 0; p < 3; ++p) tma_load_4d(dst + p * ROWS * 128, tm, bar, chunk * kPlanes + p * kPlane, row, h, b);
 }
 // D = A B^T over 64 columns of planes, A 128 rows, B N rows.
-template <int N> __device__ __forceinline__ void product_columns32(uint32_t d, uint32_t a, uint32_t b, int ks)
+template <int N> __device__ __forceinline__ void product_columns32(uint32_t d, uint32_t a, uint32_t b, int ks, bool onto = false)
 {
 #pragma unroll
     for (int p = 0; p < kPairs; ++p)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (k < ks) mma_ss(d, a + pair_a(p) * (128 * 128 >> 4) + column_step<128>(k), b + pair_b(p) * (N * 128 >> 4) + column_step<N>(k), idesc_bf16(N, false), p > 0 || k > 0);
+            if (k < ks)
+                mma_ss(d, a + pair_a(p) * (128 * 128 >> 4) + column_step<128>(k), b + pair_b(p) * (N * 128 >> 4) + column_step<N>(k), idesc_bf16(N, false),
+                       p > 0 || k > 0 || onto);
 }
 // D = A B, A's planes in tensor memory (place(plane, step of 16): columns behind `a`), B 64 rows of planes.
 template <class F> __device__ __forceinline__ void product_rows32(uint32_t d, uint32_t a, uint32_t b, F place)
@@ -97,13 +100,154 @@ struct Args32 {
     GradArgsOf<float> g;
     float2 *part_ml;     // forward
     int wide;            // outputs: rows are aligned groups of four elements
+    // Widths above 64: products of tile_product32_kernel, and the 64 columns at hand
+    Tiles rows;          // tiles in row order, for their numbers
+    float *scores[2];    // S, and (backward) dP, of a tile: [128 keys][128 queries]
+    int col0, dc;        // first column of the outputs' chunk, its width; 0 and d up to 64
 };
+constexpr int kScores = kTile * kTile;
+// The number of tile t of the pattern of problem o = (sequence, head).
+__device__ __forceinline__ long long tile_number(const Tiles &rows, int o, int t) { return rows.base(o) + t - rows.at(rows.pattern(o, 0), 0); }
+
+// ---- products of two operands over all tiles, widths 65 to 128 --------------------------------------------------------------------------
+// With rows of two chunks of 64 columns the operands of all products do not fit the shared memory of an SM, so S (and dP) of the tiles are
+// computed ahead, 64 KB a tile, and the kernels below read them, once per chunk of the outputs' columns.  Sets of four warps take alternate steps of
+// 64 keys out of tensor memory.
+struct Prod32 {
+    static constexpr int SETS = 3, THREADS = 128 * SETS + 64, STAGES = 2, X = 0, Y = 2 * kPlaneTile, BAR = Y + STAGES * 2 * kPlaneHalf, BYTES = BAR + 512 + 1024;
+    static constexpr uint32_t COLS = 256;
+};
+static_assert(Prod32::BYTES <= 232448, "shared memory");
+
+__global__ void __launch_bounds__(Prod32::THREADS, 1)
+tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ Args32 f, float *scores)
+{
+    using C = Prod32;
+    constexpr int SETS = C::SETS, TMA_WARP = 4 * SETS, FIRST_WARP = TMA_WARP + 1;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (ptx::smem_u32(raw) + 1023u) & ~1023u, bars = base + C::BAR;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto free_ = [&](int s) { return bars + 64u + 8u * s; };
+    auto s_full = [&](int w) { return bars + 128u + 8u * w; };
+    auto s_free = [&](int w) { return bars + 176u + 8u * w; };
+    auto flags = [&](int s) { return bars + 320u + 4u * s; };
+    const uint32_t x_full = bars + 200, x_free = bars + 208, slot = bars + 232;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const GradArgsOf<float> &g = f.g;
+    const TileArgsOf<float> &a = g.a;
+    const Shape &s = a.g.s;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
+        for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(s_free(i), 4); }
+        ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1);
+        ptx::mbar_init(slot + 16, 1);   // only for leaving early
+        ptx::fence_mbar_init();
+    }
+    if (warp == FIRST_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // planes and shares
+    const uint32_t tmem = ptx::lds32(slot);
+    const int tiles = (int)(g.first[blockIdx.x + 1] - g.first[blockIdx.x]), steps = 2 * tiles;
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok && !wait_for(bar, parity)) { ok = false; *a.status = B2SP_ERR_TIMEOUT; }
+        return ok;
+    };
+    auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };
+    if (warp == TMA_WARP) {
+        Walk w;
+        w.start(g.w, g.starts[blockIdx.x], tiles);
+        int i = 0, blocks = 0;
+        for (bool more = tiles > 0; more && ok;) {
+            const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
+            const bool fresh = w.fresh, last = w.next(g.w);
+            more = w.left > 0;
+            if (fresh) {
+                if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(x_full, 2 * kPlaneTile);
+                    for (int c = 0; c < 2; ++c) load_planes<128>(base + C::X + c * kPlaneTile, &tm_x, x_full, c, blk * kTile, h, b);
+                }
+                __syncwarp();
+                ++blocks;
+            }
+            for (int half = 0; half < 2; ++half, ++i) {
+                const int st = i % C::STAGES, at = r0 + half * 64;
+                if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
+                if (ptx::elect_one()) {
+                    ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
+                    ptx::mbar_arrive_expect_tx(full(st), 2 * kPlaneHalf);
+                    for (int c = 0; c < 2; ++c) load_planes<64>(base + C::Y + (2 * st + c) * kPlaneHalf, &tm_y, full(st), c, at, hkv, b);
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok) {   // copies in flight land before the CTA ends
+            if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
+            for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
+        }
+    } else if (warp == FIRST_WARP) {
+        if (ptx::elect_one()) {
+            const int ks = (s.d - kPlane + 15) >> 4;   // of the second chunk
+            const uint32_t x = desc_columns(base + C::X), y0 = desc_columns(base + C::Y);
+            int st = 0, ph = 0, set = 0, round = 0, blocks = 0;
+            for (int i = 0; i < steps; ++i) {
+                if (!wait(full(st), ph)) break;
+                const uint32_t fl = ptx::lds32(flags(st));
+                if ((fl & kStepFirst) && !wait(x_full, blocks++ & 1)) break;
+                if (round && !wait(s_free(set), (round - 1) & 1)) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t to = tmem + set * 64, y = y0 + st * (2 * kPlaneHalf >> 4);
+                product_columns32<64>(to, x, y, 4);
+                product_columns32<64>(to, x + (kPlaneTile >> 4), y + (kPlaneHalf >> 4), ks, true);
+                ptx::mma_commit(s_full(set));
+                ptx::mma_commit(free_(st));
+                if (fl & kStepLast) ptx::mma_commit(x_free);
+                if (++st == C::STAGES) { st = 0; ph ^= 1; }
+                if (++set == SETS) { set = 0; ++round; }
+            }
+            if (!ok) {
+                ptx::mma_commit(slot + 16);
+                ptx::mbar_wait(slot + 16, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int set = warp >> 2, lane_row = threadIdx.x & 127;
+        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + set * 64;
+        const long long n0 = g.first[blockIdx.x];
+        for (int i = set, round = 0; i < steps && ok; i += SETS, ++round) {
+            if (!wait_all(s_full(set), round & 1)) break;
+            ptx::tc_fence_after_sync();
+            float *to = scores + (n0 + (i >> 1)) * kScores + (i & 1) * (64 * kTile) + lane_row;
+#pragma unroll
+            for (int c = 0; c < 64; c += 16) {
+                uint32_t x[16];
+                ptx::tmem_ld_32x16(mine + c, x);
+                ptx::tmem_ld_wait();
+                settle(x);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) to[(c + k) * kTile] = __uint_as_float(x[k]);
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(s_free(set));
+        }
+    }
+    __syncwarp();
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == FIRST_WARP) { ptx::tc_fence_after_sync(); ptx::tmem_dealloc(tmem, C::COLS); }
+}
 // Where the sums that CTA c leaves of a block lie, forward: pairs (c, block) ascend together, so c + block is theirs alone.
 __device__ __forceinline__ long long part_of(int c, long long block, int set, int sets) { return (c + block) * sets + set; }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------------
 // Three sets of four softmax warps take alternate steps of 64 keys, each with a softmax of its own (reference, sum, output), which the joining
-// kernel merges; so a set waits for nobody between its steps.
+// kernel merges; so a set waits for nobody between its steps.  READ: S comes from memory (see tile_product32_kernel), and O has the columns of a chunk.
 struct Fwd32 {
     static constexpr int SETS = 3, THREADS = 128 * SETS + 96, STAGES = 3;
     static constexpr int Q = 0, K = kPlaneTile, V = K + STAGES * kPlaneHalf, BAR = V + STAGES * kPlaneHalf, BYTES = BAR + 512 + 1024;
@@ -111,6 +255,7 @@ struct Fwd32 {
 };
 static_assert(Fwd32::BYTES <= 232448, "shared memory");
 
+template <bool READ>
 __global__ void __launch_bounds__(Fwd32::THREADS, 1)
 tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                       const __grid_constant__ Args32 f)
@@ -159,11 +304,11 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
             more = w.left > 0;
-            if (fresh) {
+            if (!READ && fresh) {
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, kPlaneTile);
-                    load_planes<128>(base + C::Q, &tm_q, x_full, blk * kTile, h, b);
+                    load_planes<128>(base + C::Q, &tm_q, x_full, 0, blk * kTile, h, b);
                 }
                 __syncwarp();
                 ++blocks;
@@ -173,9 +318,9 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
-                    ptx::mbar_arrive_expect_tx(full(st), 2 * kPlaneHalf);
-                    load_planes<64>(base + C::K + st * kPlaneHalf, &tm_k, full(st), at, hkv, b);
-                    load_planes<64>(base + C::V + st * kPlaneHalf, &tm_v, full(st), at, hkv, b);
+                    ptx::mbar_arrive_expect_tx(full(st), (READ ? 1 : 2) * kPlaneHalf);
+                    if (!READ) load_planes<64>(base + C::K + st * kPlaneHalf, &tm_k, full(st), 0, at, hkv, b);
+                    load_planes<64>(base + C::V + st * kPlaneHalf, &tm_v, full(st), f.col0 / kPlane, at, hkv, b);
                 }
                 __syncwarp();
             }
@@ -185,7 +330,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
         }
     } else if (warp == FIRST_WARP) {
-        if (ptx::elect_one()) {
+        if (!READ && ptx::elect_one()) {
             const int ks = (s.d + 15) >> 4;
             const uint32_t q = desc_columns(base + C::Q), k0 = desc_columns(base + C::K);
             int st = 0, ph = 0, set = 0, round = 0, blocks = 0;
@@ -258,16 +403,26 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 const int turn = round;
                 if (++at_set == SETS) { at_set = 0; ++round; }
                 if (!my_turn) continue;
-                if (!wait_all(s_full(set), turn & 1)) break;
+                // (S of this step came behind the set's last product; read from memory it did not)
+                if (READ ? turn && !wait_all(s_free(set), (turn - 1) & 1) : !wait_all(s_full(set), turn & 1)) break;
                 ptx::tc_fence_after_sync();
-                if (pending) collect();   // (S of this step came behind that product)
+                if (pending) collect();
+                const float *from = READ ? f.scores[0] + tile_number(g.w, o, w.t) * kScores + half * (64 * kTile) + lane_row : nullptr;
+                auto load = [&](int c, uint32_t (&x)[16]) {
+                    if (READ) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(from[(c + k) * kTile]);
+                    } else {
+                        ptx::tmem_ld_32x16(mine + c, x);
+                        ptx::tmem_ld_wait();
+                        settle(x);
+                    }
+                };
                 float top4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
                 for (int c = 0; c < 64; c += 16) {
                     uint32_t x[16];
-                    ptx::tmem_ld_32x16(mine + c, x);
-                    ptx::tmem_ld_wait();
-                    settle(x);
+                    load(c, x);
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) top4[k >> 1 & 3] = fmaxf(top4[k >> 1 & 3], fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 1])));
                 }
@@ -284,9 +439,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t x[16], p1[8], p2[8], p3[8];
-                    ptx::tmem_ld_32x16(mine + 16 * c, x);
-                    ptx::tmem_ld_wait();
-                    settle(x);
+                    load(16 * c, x);
                     const uint32_t m = (half ? (c & 2 ? now.w : now.z) : (c & 2 ? now.y : now.x)) >> (16 * (c & 1));
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
@@ -339,7 +492,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 // A CTA per 16 rows of a block, a thread per four elements: the sums of all sets of all CTAs that had tiles of it, in order, each rescaled
 // when the reference moves.
 constexpr int kJoinRows32 = 16, kJoinParts32 = kTile / kJoinRows32;
-template <int V>
+template <int V, int DW>
 __global__ void __launch_bounds__(256) tile_forward32_join_kernel(const __grid_constant__ Args32 f)
 {
     const GradArgsOf<float> &g = f.g;
@@ -388,15 +541,15 @@ __global__ void __launch_bounds__(256) tile_forward32_join_kernel(const __grid_c
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             x[k] *= inv;
-            bad |= live && col + k < s.d && !(fabsf(x[k]) <= 3.402823466e38f);
+            bad |= live && col + k < f.dc && !(fabsf(x[k]) <= 3.402823466e38f);
         }
-        store4<float, V>(a.g.out1.at(b, h, row), col, s.d, x);
+        store4<float, V>(a.g.out1.at(b, h, row) + f.col0, col, f.dc, x);
         if (col == 0) a.g.lse[(long long)o * s.M + row] = live ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
         if (bad) atomicOr(&redo, 1u << r);
     }
     __syncthreads();
     for (unsigned left = redo >> (threadIdx.x >> 5), r = threadIdx.x >> 5; left; left >>= 8, r += 8)
-        if (left & 1) rows_one_by_one<kForward, 64, float, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + (int)r, 1u, a.g.ptr_stride, a.g.idx_stride);
+        if (left & 1) rows_one_by_one<kForward, DW, float, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + (int)r, 1u, a.g.ptr_stride, a.g.idx_stride);
 }
 
 // ---- the backward pass -------------------------------------------------------------------------------------------------------------
@@ -414,7 +567,7 @@ template <int MODE> struct Grad32 {
     __device__ static constexpr int pp(int p, int k) { return p == 2 ? 128 + 16 * k : 16 * k + 8 * p; }
 };
 
-template <int MODE>
+template <int MODE, bool READ>
 __global__ void __launch_bounds__(Grad32<MODE>::THREADS, 1)
 tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2, const __grid_constant__ CUtensorMap tm_y1,
                    const __grid_constant__ CUtensorMap tm_y2, const __grid_constant__ Args32 f)
@@ -464,12 +617,12 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
             more = w.left > 0;
-            if (fresh) {
+            if (!READ && fresh) {
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * kPlaneTile);
-                    load_planes<128>(base + C::X1, &tm_x1, x_full, blk * kTile, x, b);
-                    load_planes<128>(base + C::X2, &tm_x2, x_full, blk * kTile, x, b);
+                    load_planes<128>(base + C::X1, &tm_x1, x_full, 0, blk * kTile, x, b);
+                    load_planes<128>(base + C::X2, &tm_x2, x_full, 0, blk * kTile, x, b);
                 }
                 __syncwarp();
                 ++blocks;
@@ -479,9 +632,10 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
-                    ptx::mbar_arrive_expect_tx(full(st), 2 * kPlaneHalf + C::STAT);
-                    load_planes<64>(base + C::Y1 + st * kPlaneHalf, &tm_y1, full(st), at, hy, b);
-                    load_planes<64>(base + C::Y2 + st * kPlaneHalf, &tm_y2, full(st), at, hy, b);
+                    constexpr bool BOTH = !READ || MODE == kDkv;   // (V serves dP alone)
+                    ptx::mbar_arrive_expect_tx(full(st), (BOTH ? 2 : 1) * kPlaneHalf + C::STAT);
+                    load_planes<64>(base + C::Y1 + st * kPlaneHalf, &tm_y1, full(st), f.col0 / kPlane, at, hy, b);
+                    if (BOTH) load_planes<64>(base + C::Y2 + st * kPlaneHalf, &tm_y2, full(st), f.col0 / kPlane, at, hy, b);
                     if (MODE == kDkv) bulk_load(base + C::ST + st * C::STAT, a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride + at, C::STAT, full(st));
                 }
                 __syncwarp();
@@ -492,7 +646,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
             for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
         }
     } else if (warp == FIRST_WARP) {
-        if (ptx::elect_one()) {
+        if (!READ && ptx::elect_one()) {
             const int ks = (s.d + 15) >> 4;
             const uint32_t x1 = desc_columns(base + C::X1), x2 = desc_columns(base + C::X2), y1 = desc_columns(base + C::Y1), y2 = desc_columns(base + C::Y2);
             int st = 0, ph = 0, set = 0, round = 0, blocks = 0;
@@ -546,7 +700,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
         const uint64_t f2 = two(c2, c2);
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int at_set = 0, round = 0, st = 0;
+        int at_set = 0, round = 0, st = 0, ph = 0;
         float2 own = make_float2(0.f, 0.f);
         for (bool more = tiles > 0; more && ok;) {
             if (MODE == kDq && w.fresh) own = a.g.stat[(long long)w.o * a.g.stat_stride + w.blk * kTile + lane_row];
@@ -554,21 +708,48 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
             const uint64_t l2 = two(own.x, own.x), d2 = two(own.y, own.y);
             for (int half = 0; half < 2; ++half) {
                 const bool my_turn = at_set == set;
-                const int stage = st, turn = round;
-                if (++st == C::STAGES) st = 0;
+                const int stage = st, turn = round, at_stage = ph;
+                if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++at_set == SETS) { at_set = 0; ++round; }
                 if (!my_turn) continue;
-                if (!wait_all(s_full(set), turn & 1)) break;
+                if (READ) {   // (what the set left in tensor memory is read by then, and the statistics are there)
+                    if (turn && !wait_all(s_free(set), (turn - 1) & 1)) break;
+                    if (MODE == kDkv && !wait_all(full(stage), at_stage & 1)) break;
+                } else if (!wait_all(s_full(set), turn & 1)) {
+                    break;
+                }
                 ptx::tc_fence_after_sync();
+                const float *sc = nullptr;
+                long long dp_at = 0;
+                if (READ) {
+                    const int head = w.o / g.w.outer * s.heads + w.o % g.w.outer * g.w.group + w.i;
+                    sc = f.scores[0] + tile_number(f.rows, head, MODE == kDq ? w.t : g.tile_at[2 * w.t + 1]) * kScores;
+                    sc += MODE == kDq ? half * (64 * kTile) + lane_row : lane_row * kTile + half * 64;
+                    dp_at = f.scores[1] - f.scores[0];
+                }
                 const uint32_t stat = base + C::ST + stage * C::STAT;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t x[16], y[16];
-                    ptx::tmem_ld_32x16(from + 16 * c, x);
-                    ptx::tmem_ld_32x16(from + 64 + 16 * c, y);
-                    ptx::tmem_ld_wait();
-                    settle(x);
-                    settle(y);
+                    if (READ && MODE == kDq) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(sc[(16 * c + k) * kTile]);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(sc[dp_at + (16 * c + k) * kTile]);
+                    } else if (READ) {
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4) {
+                            const uint4 u = *reinterpret_cast<const uint4 *>(sc + 16 * c + k), v = *reinterpret_cast<const uint4 *>(sc + dp_at + 16 * c + k);
+                            x[k] = u.x; x[k + 1] = u.y; x[k + 2] = u.z; x[k + 3] = u.w;
+                            y[k] = v.x; y[k + 1] = v.y; y[k + 2] = v.z; y[k + 3] = v.w;
+                        }
+                    } else {
+                        ptx::tmem_ld_32x16(from + 16 * c, x);
+                        ptx::tmem_ld_32x16(from + 64 + 16 * c, y);
+                        ptx::tmem_ld_wait();
+                        settle(x);
+                        settle(y);
+                    }
                     const uint32_t m = (half ? (c & 2 ? now.w : now.z) : (c & 2 ? now.y : now.x)) >> (16 * (c & 1));
                     uint32_t p1[8], p2[8], p3[8], q1[8], q2[8], q3[8];
 #pragma unroll
@@ -660,7 +841,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
             bool bad = false;
             if (whole) {
                 if (row < rows) {
-                    float *to = (acc_of ? a.g.out2 : a.g.out1).at(b, h, row);
+                    float *to = (acc_of ? a.g.out2 : a.g.out1).at(b, h, row) + f.col0;
                     const float by = acc_of ? 1.f : s.scale;
 #pragma unroll
                     for (int k = 0; k < N; k += 4) {
@@ -668,10 +849,10 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             x[e] = some ? acc[k + e] * by : 0.f;
-                            bad |= col0 + k + e < s.d && !(fabsf(x[e]) <= 3.402823466e38f);
+                            bad |= col0 + k + e < f.dc && !(fabsf(x[e]) <= 3.402823466e38f);
                         }
-                        if (f.wide) store4<float, 4>(to, col0 + k, s.d, x);
-                        else store4<float, 1>(to, col0 + k, s.d, x);
+                        if (f.wide) store4<float, 4>(to, col0 + k, f.dc, x);
+                        else store4<float, 1>(to, col0 + k, f.dc, x);
                     }
                 }
             } else {

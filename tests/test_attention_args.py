@@ -57,13 +57,19 @@ def test_operands_workspace_and_algo(b):
     assert _forward(b, p, ws_bytes=need - 1) == WORKSPACE
     assert _forward(b, p, algo=4) == INVALID and _forward(b, p, algo=-1) == INVALID
     assert _forward(b, p, algo=b.ALGO_TILE) == UNSUPPORTED                                       # no plan
-    assert _forward(b, _problem(b, d=65, plan=1 << 20, plan_tiles=1), o=_heads(b, 1 << 20, 65, 65 * 64, 65 * 64 * 8), algo=b.ALGO_TILE) == UNSUPPORTED   # fp32
+    assert _forward(b, _problem(b, d=129, plan=1 << 20, plan_tiles=1), o=_heads(b, 1 << 20, 129, 129 * 64, 129 * 64 * 8), algo=b.ALGO_TILE) == UNSUPPORTED   # fp32
     assert _forward(b, p, algo=b.ALGO_TILE, fn="b2sp_attention_bf16") == UNSUPPORTED             # no plan
     for bad in (dict(d=130), dict(d=136)):
         assert _forward(b, _problem(b, plan=1 << 20, plan_tiles=1, **bad), o=_heads(b, 1 << 20, 136, 136 * 64, 136 * 64 * 8), algo=b.ALGO_TILE,
                         fn="b2sp_attention_bf16") == UNSUPPORTED
     odd = _heads(b, (1 << 20) + 2, 64, 64 * 64, 64 * 64 * 8)
     assert _forward(b, _problem(b, plan=1 << 20, plan_tiles=1), q=odd, algo=b.ALGO_TILE, fn="b2sp_attention_bf16") == UNSUPPORTED
+    # fp32, d > 64: 64 KB a tile and problem, 2 GB at most
+    wide = dict(d=80, plan=1 << 20, heads=4, kv_heads=4)
+    assert b.lib.b2sp_attention_workspace_bytes(_problem(b, plan_tiles=4096, **wide), 0) > 1 << 31
+    assert b.lib.b2sp_attention_workspace_bytes(_problem(b, plan_tiles=4097, **wide), 0) < 1 << 31
+    assert b.lib.b2sp_attention_workspace_bytes_bf16(_problem(b, plan_tiles=4096, **wide), 0) < 1 << 28
+    assert _forward(b, _problem(b, plan_tiles=4097, **wide), o=_heads(b, 1 << 20, 80, 80 * 64, 80 * 64 * 8), algo=b.ALGO_TILE) == UNSUPPORTED
     # nothing to do: no launch, so this passes without a device
     assert _forward(b, _problem(b, M=0)) == OK
 

@@ -138,6 +138,12 @@ TILE32_SHAPES = [
     dict(M=200, K=200, d=64, kind="nothing"),
     dict(M=1000, K=1000, d=48, kind="full", spread=4.0),
     dict(B=3, H=2, Hkv=2, M=260, K=2100, d=64, spread=8.0),
+    dict(M=1, K=1, d=65, kind="full"),                                     # widths whose products go through memory
+    dict(H=4, Hkv=2, M=300, K=410, d=128, strided=True),
+    dict(B=2, H=4, Hkv=2, M=513, K=513, d=97, kind="window", per="sequence"),
+    dict(B=3, H=2, Hkv=1, M=260, K=900, d=80, per="problem", spread=4.0),
+    dict(M=200, K=200, d=100, kind="nothing"),
+    dict(H=2, Hkv=1, M=900, K=640, d=128, kind="sparse"),
 ]
 
 
