@@ -75,15 +75,13 @@ template <int ROWS> __device__ __forceinline__ void load_planes(uint32_t dst, co
     for (int p = 0; p < 3; ++p) tma_load_4d(dst + p * ROWS * 128, tm, bar, chunk * kPlanes + p * kPlane, row, h, b);
 }
 // D = A B^T over 64 columns of planes, A 128 rows, B N rows.
-template <int N> __device__ __forceinline__ void product_columns32(uint32_t d, uint32_t a, uint32_t b, int ks, bool onto = false)
+template <int N> __device__ __forceinline__ void product_columns32(uint32_t d, uint32_t a, uint32_t b, int ks)
 {
 #pragma unroll
     for (int p = 0; p < kPairs; ++p)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (k < ks)
-                mma_ss(d, a + pair_a(p) * (128 * 128 >> 4) + column_step<128>(k), b + pair_b(p) * (N * 128 >> 4) + column_step<N>(k), idesc_bf16(N, false),
-                       p > 0 || k > 0 || onto);
+            if (k < ks) mma_ss(d, a + pair_a(p) * (128 * 128 >> 4) + column_step<128>(k), b + pair_b(p) * (N * 128 >> 4) + column_step<N>(k), idesc_bf16(N, false), p > 0 || k > 0);
 }
 // D = A B, A's planes in tensor memory (place(plane, step of 16): columns behind `a`), B 64 rows of planes.
 template <class F> __device__ __forceinline__ void product_rows32(uint32_t d, uint32_t a, uint32_t b, F place)
@@ -115,7 +113,7 @@ __device__ __forceinline__ long long tile_number(const Tiles &rows, int o, int t
 // 64 keys out of tensor memory.
 struct Prod32 {
     static constexpr int SETS = 3, THREADS = 128 * SETS + 64, STAGES = 2, X = 0, Y = 2 * kPlaneTile, BAR = Y + STAGES * 2 * kPlaneHalf, BYTES = BAR + 512 + 1024;
-    static constexpr uint32_t COLS = 256;
+    static constexpr uint32_t SET = 128, COLS = 512;   // of a set: the sums of either chunk, added up in registers (the tensor core truncates)
 };
 static_assert(Prod32::BYTES <= 232448, "shared memory");
 
@@ -200,9 +198,9 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
                 if ((fl & kStepFirst) && !wait(x_full, blocks++ & 1)) break;
                 if (round && !wait(s_free(set), (round - 1) & 1)) break;
                 ptx::tc_fence_after_sync();
-                const uint32_t to = tmem + set * 64, y = y0 + st * (2 * kPlaneHalf >> 4);
+                const uint32_t to = tmem + set * C::SET, y = y0 + st * (2 * kPlaneHalf >> 4);
                 product_columns32<64>(to, x, y, 4);
-                product_columns32<64>(to, x + (kPlaneTile >> 4), y + (kPlaneHalf >> 4), ks, true);
+                product_columns32<64>(to + 64, x + (kPlaneTile >> 4), y + (kPlaneHalf >> 4), ks);
                 ptx::mma_commit(s_full(set));
                 ptx::mma_commit(free_(st));
                 if (fl & kStepLast) ptx::mma_commit(x_free);
@@ -217,7 +215,7 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
         __syncwarp();
     } else {
         const int set = warp >> 2, lane_row = threadIdx.x & 127;
-        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + set * 64;
+        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + set * C::SET;
         const long long n0 = g.first[blockIdx.x];
         for (int i = set, round = 0; i < steps && ok; i += SETS, ++round) {
             if (!wait_all(s_full(set), round & 1)) break;
@@ -225,12 +223,14 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
             float *to = scores + (n0 + (i >> 1)) * kScores + (i & 1) * (64 * kTile) + lane_row;
 #pragma unroll
             for (int c = 0; c < 64; c += 16) {
-                uint32_t x[16];
+                uint32_t x[16], y[16];
                 ptx::tmem_ld_32x16(mine + c, x);
+                ptx::tmem_ld_32x16(mine + 64 + c, y);
                 ptx::tmem_ld_wait();
                 settle(x);
+                settle(y);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) to[(c + k) * kTile] = __uint_as_float(x[k]);
+                for (int k = 0; k < 16; ++k) to[(c + k) * kTile] = __uint_as_float(x[k]) + __uint_as_float(y[k]);
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
