@@ -104,6 +104,11 @@ struct Args32 {
     int col0, dc;        // first column of the outputs' chunk, its width; 0 and d up to 64
 };
 constexpr int kScores = kTile * kTile;
+// Into L2, `bytes` from `p` on (multiples of 16).
+__device__ __forceinline__ void prefetch(const void *p, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(p)), "r"(bytes) : "memory");
+}
 // The number of tile t of the pattern of problem o = (sequence, head).
 __device__ __forceinline__ long long tile_number(const Tiles &rows, int o, int t) { return rows.base(o) + t - rows.at(rows.pattern(o, 0), 0); }
 
@@ -302,6 +307,11 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         int i = 0, blocks = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
+            if (READ) {
+                const float *at = f.scores[0] + tile_number(g.w, w.o, w.t) * kScores;
+                if (ptx::elect_one()) prefetch(at, kScores * 4);
+                __syncwarp();
+            }
             const bool fresh = w.fresh, last = w.next(g.w);
             more = w.left > 0;
             if (!READ && fresh) {
@@ -412,6 +422,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     if (READ) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(from[(c + k) * kTile]);
+                        settle(x);   // (all sixteen in flight)
                     } else {
                         ptx::tmem_ld_32x16(mine + c, x);
                         ptx::tmem_ld_wait();
@@ -615,6 +626,14 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
+            if (READ) {
+                const long long at = tile_number(f.rows, b * s.heads + h, MODE == kDq ? w.t : g.tile_at[2 * w.t + 1]) * kScores;
+                if (ptx::elect_one()) {
+                    prefetch(f.scores[0] + at, kScores * 4);
+                    prefetch(f.scores[1] + at, kScores * 4);
+                }
+                __syncwarp();
+            }
             const bool fresh = w.fresh, last = w.next(g.w);
             more = w.left > 0;
             if (!READ && fresh) {
@@ -736,6 +755,8 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                         for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(sc[(16 * c + k) * kTile]);
 #pragma unroll
                         for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(sc[dp_at + (16 * c + k) * kTile]);
+                        settle(x);   // (all in flight)
+                        settle(y);
                     } else if (READ) {
 #pragma unroll
                         for (int k = 0; k < 16; k += 4) {
@@ -743,6 +764,8 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                             x[k] = u.x; x[k + 1] = u.y; x[k + 2] = u.z; x[k + 3] = u.w;
                             y[k] = v.x; y[k + 1] = v.y; y[k + 2] = v.z; y[k + 3] = v.w;
                         }
+                        settle(x);   // (all in flight)
+                        settle(y);
                     } else {
                         ptx::tmem_ld_32x16(from + 16 * c, x);
                         ptx::tmem_ld_32x16(from + 64 + 16 * c, y);
