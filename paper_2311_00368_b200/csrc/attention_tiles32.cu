@@ -156,7 +156,7 @@ b2sp_status product(const Call32 &c, const Plan32 &p, int which, cudaStream_t st
 template <int MODE, bool READ> b2sp_status grad(const Call32 &c, const Plan32 &p, const Args32 &f, cudaStream_t st, int *launches)
 {
     static std::atomic<unsigned long long> done{0};
-    using C = Grad32<MODE>;
+    using C = Grad32<MODE, READ>;
     const Shape &s = c.s;
     CUtensorMap x1, x2, y1, y2;
     const bool q = MODE == kDq;

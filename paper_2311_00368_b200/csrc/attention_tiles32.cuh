@@ -565,8 +565,8 @@ __global__ void __launch_bounds__(256) tile_forward32_join_kernel(const __grid_c
 
 // ---- the backward pass -------------------------------------------------------------------------------------------------------------
 // Two sets of four softmax warps; eight warps that add up the second products, step by step, in registers.
-template <int MODE> struct Grad32 {
-    static constexpr int SETS = 2, THREADS = 128 * SETS + 256 + 96, STAGES = 2, ACCS = MODE == kDkv ? 2 : 1;
+template <int MODE, bool READ = false> struct Grad32 {
+    static constexpr int SETS = READ && MODE == kDq ? 3 : 2, THREADS = 128 * SETS + 256 + 96, STAGES = 2, ACCS = MODE == kDkv ? 2 : 1;
     static constexpr int STAT = MODE == kDkv ? 512 : 0;
     static constexpr int X1 = 0, X2 = kPlaneTile, Y1 = 2 * kPlaneTile, Y2 = Y1 + STAGES * kPlaneHalf, ST = Y2 + STAGES * kPlaneHalf, BAR = ST + STAGES * STAT;
     static constexpr int BYTES = BAR + 512 + 1024;
@@ -579,11 +579,11 @@ template <int MODE> struct Grad32 {
 };
 
 template <int MODE, bool READ>
-__global__ void __launch_bounds__(Grad32<MODE>::THREADS, 1)
+__global__ void __launch_bounds__(Grad32<MODE, READ>::THREADS, 1)
 tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2, const __grid_constant__ CUtensorMap tm_y1,
                    const __grid_constant__ CUtensorMap tm_y2, const __grid_constant__ Args32 f)
 {
-    using C = Grad32<MODE>;
+    using C = Grad32<MODE, READ>;
     constexpr int SETS = C::SETS, SUM_WARP = 4 * SETS, TMA_WARP = SUM_WARP + 8, FIRST_WARP = TMA_WARP + 1, SECOND_WARP = TMA_WARP + 2;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (ptx::smem_u32(raw) + 1023u) & ~1023u, bars = base + C::BAR;
