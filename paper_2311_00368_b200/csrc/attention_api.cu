@@ -150,6 +150,11 @@ template <int MODE, typename T> b2sp_status launch_rows_v(bool wide, const RowAr
 //     2048 x 2048 at 2%, 8 heads over 2              52 and 156    66 and 204
 //     2048 x 2048 at 4%, 8 heads over 2              88 and 267    66 and 205
 //     200 x 8000 at 2%, one head                     31 and  47    38 and  58
+// fp32, width 128 (see tile_product32_kernel):
+//     64 x 64 at 30%, one head                        9 and  24    38 and  82
+//     2048 x 2048 at 2%, 8 heads over 2              74 and 283   228 and 733
+//     4096 x 4096 at 30%, 8 heads                  2752           875
+//     4096 x 4096, window of 1229, 8 heads over 2         9534            928
 double row_time(const Shape &s, double entries, double in_row, bool backward, bool wide)
 {
     const double width = std::max(s.d, 64) / 64.0;
@@ -161,7 +166,8 @@ bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward,
     const double problems = (double)s.batch * s.heads, entries = nnz * problems, all = tiles * (problems / s.patterns);
     const double in_row = (double)nnz / s.M, in_block = all / (problems * ((s.M + kTile - 1) / kTile));
     double t;
-    if (fp32) t = backward ? 30 + 0.5 * std::min(all, 16.0) + 0.082 * all : 14 + 0.06 * std::min(all, 128.0) + 0.25 * in_block + 0.0225 * all;
+    if (fp32 && s.d > 64) t = backward ? 85 + 0.32 * all : 38 + 0.06 * std::min(all, 128.0) + 0.6 * in_block + 0.085 * all;
+    else if (fp32) t = backward ? 30 + 0.5 * std::min(all, 16.0) + 0.082 * all : 14 + 0.06 * std::min(all, 128.0) + 0.25 * in_block + 0.0225 * all;
     else if (backward) t = 20 + 0.6 * std::min(all, 16.0) + 0.022 * all * (s.d <= 64 ? 1 : 1.6);
     else t = 5 + 1.3 * std::max(in_block, all / 296);
     return t < row_time(s, entries, in_row, backward, fp32);

@@ -1,4 +1,4 @@
-// Attention over the tiles of a plan on the tensor cores, fp32 operands, head widths up to 64.
+// Attention over the tiles of a plan on the tensor cores, fp32 operands, head widths up to 128.
 //
 // Every operand is split into three bfloat16 planes, x = x1 + x2 + x3 exactly (8 + 8 + 8 significant bits; a plane is what is left of x
 // rounded to nearest), and a product is six products of planes, smallest first: x2 y2, x1 y3, x3 y1, x1 y2, x2 y1, x1 y1.  What is left out is below
@@ -9,7 +9,7 @@
 // What bounds it is the tensor core, six times the products of the bfloat16 kernels: two batches of 2 x 4 x 128 x 64 x 64 x 6 multiplications a
 // tile forward, seven backward.  1501 x 2903, six heads of width 50 at 12% (1656 tiles): forward 61 us (of it the tiles 46), backward 180 us
 // (dQ 71, dK and dV 107, side by side with what stands ahead and behind); the row kernels take 265 and 818 us.  A tile costs the same at any density: see prefer_tiles.
-// Width 64 and not 128: Q, dO and a step of K and V as planes would take 294 KB of shared memory.
+// Above width 64 the planes of Q, dO and a step of K and V would take 294 KB of shared memory: there the products of all tiles are computed ahead.
 //
 // The walk over shares of tiles, the roles and the barriers are those of tile_grad_kernel (attention_tiles.cuh).
 #pragma once
@@ -115,7 +115,9 @@ __device__ __forceinline__ long long tile_number(const Tiles &rows, int o, int t
 // ---- products of two operands over all tiles, widths 65 to 128 --------------------------------------------------------------------------
 // With rows of two chunks of 64 columns the operands of all products do not fit the shared memory of an SM, so S (and dP) of the tiles are
 // computed ahead, 64 KB a tile, and the kernels below read them, once per chunk of the outputs' columns.  Sets of four warps take alternate steps of
-// 64 keys out of tensor memory.
+// 64 keys out of tensor memory.  2048 tiles of width 128: 60 us for S and for dP each (tensor core 37, 134 MB written), then per chunk the forward pass
+// 78 us and its join, dQ 96 and dK with dV 175 us and their join.  A query's neighbours lie side by side (score reads of the forward pass and dQ, writes); with
+// eight queries side by side and then the keys dK and dV take 164 us, dQ 100, the forward pass 87.
 struct Prod32 {
     static constexpr int SETS = 3, THREADS = 128 * SETS + 64, STAGES = 2, X = 0, Y = 2 * kPlaneTile, BAR = Y + STAGES * 2 * kPlaneHalf, BYTES = BAR + 512 + 1024;
     static constexpr uint32_t SET = 128, COLS = 512;   // of a set: the sums of either chunk, added up in registers (the tensor core truncates)
