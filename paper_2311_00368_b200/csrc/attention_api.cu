@@ -135,14 +135,15 @@ template <int MODE, typename T> b2sp_status launch_rows_v(bool wide, const RowAr
 
 // ---- the choice between the families -------------------------------------------------------------------------------------------------
 // Microseconds that each would take.  The row kernels' work is that of the stored entries, but a warp takes a row's (or a part's, about 64 and
-// more) one after the other.  The tile kernels' work is that of the tiles, whatever they hold; the forward pass takes a block's one after the
-// other.  Measured, rows against tiles, bf16, width 64, forward and backward:
-//     one row of 4096 of 8192, one head              26 and  32    87 and  30
+// more) one after the other.  The tile kernels' work is that of the tiles, whatever they hold; the forward pass takes a block's (or
+// a part's) one after the other.  Measured, rows against tiles, bf16, width 64, forward and backward:
+//     one row of 4096 of 8192, one head              26 and  32    14 and  30   (87 before long blocks were cut into parts)
 //     512 x 512 at 2%, one head                       7 and  15    10 and  28
 //     1024 x 1024 at 0.5%, 8 heads                   11 and  27    16 and  45
 //     2048 x 2048 at 1%, 8 heads over 2              33 and  81    27 and  78
 //     2048 x 2048 at 4%, 8 heads over 2              85 and 212    27 and  78
-//     200 x 8000 at 2%, one head                     30 and  38    85 and  46
+//     200 x 8000 at 2%, one head                     30 and  38    16 and  46   (85)
+//     128 x 8192 at 50%, 8 heads, width 128         400            17          (86)
 //     4 x 5 heads over one, width 32, 700 x 700, 3%  28 and  73    13 and  52
 // fp32:
 //     one row of 4096 of 8192, one head              26 and  36    36 and  48
@@ -169,7 +170,7 @@ bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward,
     if (fp32 && s.d > 64) t = backward ? 85 + 0.32 * all : 38 + 0.06 * std::min(all, 128.0) + 0.6 * in_block + 0.085 * all;
     else if (fp32) t = backward ? 30 + 0.5 * std::min(all, 16.0) + 0.082 * all : 14 + 0.06 * std::min(all, 128.0) + 0.25 * in_block + 0.0225 * all;
     else if (backward) t = 20 + 0.6 * std::min(all, 16.0) + 0.022 * all * (s.d <= 64 ? 1 : 1.6);
-    else t = 5 + 1.3 * std::max(in_block, all / 296);
+    else t = 5 + 1.3 * std::max(in_block / tile_splits(s, tiles), all / 296) + (tile_splits(s, tiles) > 1 ? 5 : 0);
     return t < row_time(s, entries, in_row, backward, fp32);
 }
 

@@ -29,18 +29,42 @@ TileArgs args(const TileCall &c)
     return a;
 }
 
-template <int DP> b2sp_status forward(const TileCall &c, cudaStream_t st, int *launches)
+struct FwdPlan { int splits; size_t part, ml, bytes; };   // offsets
+FwdPlan forward_plan(const Shape &s, long long tiles, size_t at)
+{
+    FwdPlan p;
+    const long long blocks = (long long)s.batch * s.heads * ((s.M + kTile - 1) / kTile);
+    p.splits = tile_splits(s, tiles);
+    p.part = at;
+    p.ml = at + (p.splits > 1 ? (size_t)blocks * p.splits * kTile * (s.d <= 64 ? 64 : 128) * 4 : 0);
+    p.bytes = p.ml + up256(p.splits > 1 ? (size_t)blocks * p.splits * kTile * 8 : 0);
+    return p;
+}
+template <int DP, bool SPLIT> b2sp_status launch_forward(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const TileArgs &a, const FwdParts &f, unsigned ctas, cudaStream_t st)
 {
     static std::atomic<unsigned long long> done{0};
+    if (!allow_smem(tile_forward_kernel<DP, SPLIT>, FwdCfg<DP>::BYTES, done)) return B2SP_ERR_CUDA;
+    tile_forward_kernel<DP, SPLIT><<<ctas, kTileThreads, FwdCfg<DP>::BYTES, st>>>(q, k, v, a, f);
+    return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
+}
+template <int DP> b2sp_status forward(const TileCall &c, cudaStream_t st, int *launches)
+{
     TileArgs a = args(c);
     a.g.out1 = c.out; a.g.rows = c.s.M;
     CUtensorMap q, k, v;
     if (!make_map(&q, c.q, c.s.batch, c.s.heads, c.s.M, c.s.d, 128, &a.q) || !make_map(&k, c.k, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 64, &a.k) ||
-        !make_map(&v, c.v, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 64, &a.v) || !allow_smem(tile_forward_kernel<DP>, FwdCfg<DP>::BYTES, done))
+        !make_map(&v, c.v, c.s.batch, c.s.kv_heads, c.s.K, c.s.d, 64, &a.v))
         return B2SP_ERR_CUDA;
+    const FwdPlan p = forward_plan(c.s, c.tiles, c.scratch_at);
     const long long blocks = (long long)c.s.batch * c.s.heads * c.plan.RB;
     if (blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    tile_forward_kernel<DP><<<(unsigned)blocks, kTileThreads, FwdCfg<DP>::BYTES, st>>>(q, k, v, a);
+    char *ws = static_cast<char *>(c.workspace);
+    const FwdParts f{p.splits, reinterpret_cast<float *>(ws + p.part), reinterpret_cast<float2 *>(ws + p.ml)};
+    ++*launches;
+    if (p.splits == 1) return launch_forward<DP, false>(q, k, v, a, f, (unsigned)blocks, st);
+    const b2sp_status rc = launch_forward<DP, true>(q, k, v, a, f, (unsigned)(blocks * p.splits), st);
+    if (rc != B2SP_OK) return rc;
+    launch_behind(tile_forward_join_kernel<DP>, (unsigned)(blocks * (kTile * DP / 4 / 256)), 256, st, a, f);
     ++*launches;
     return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
 }
@@ -250,7 +274,7 @@ size_t tiles_bytes(const Shape &s, long long tiles, size_t at, bool backward)
         stage(c, backward);
         at = c.scratch_at;
     }
-    return backward ? grad_plan(s, tiles, at).bytes : at;
+    return backward ? grad_plan(s, tiles, at).bytes : forward_plan(s, tiles, at).bytes;
 }
 b2sp_status tiles_forward(const TileCall &c, cudaStream_t st, int *launches)
 {

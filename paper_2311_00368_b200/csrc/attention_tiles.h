@@ -21,6 +21,14 @@ inline Shares deal(long long tiles, long long blocks, int cost, long long least)
     return x;
 }
 
+// The bfloat16 forward pass: parts of a row block's tiles, for two CTAs per SM and four tiles a part (5 us, what joining them takes).
+inline int tile_splits(const Shape &s, long long tiles)
+{
+    const long long blocks = std::max(1ll, (long long)s.batch * s.heads * ((s.M + kTile - 1) / kTile));
+    const long long in_block = tiles * ((long long)s.batch * s.heads / s.patterns) / blocks;
+    return in_block < 12 ? 1 : (int)std::max(1ll, std::min(2 * 148 / blocks, in_block / 4));
+}
+
 struct TileCall {
     Shape s;
     Plan plan;

@@ -119,6 +119,10 @@ TILE_SHAPES = [
     dict(B=2, H=4, Hkv=2, M=300, K=410, d=83, per="sequence", strided=True),
     dict(H=3, Hkv=3, M=513, K=513, d=121, kind="window"),
     dict(B=3, H=2, Hkv=1, M=140, K=700, d=50, per="problem", spread=4.0),
+    dict(M=1, K=8192, d=64, kind="full"),                                   # few blocks with many tiles: cut into parts
+    dict(H=4, Hkv=2, M=130, K=5000, d=128, spread=8.0, strided=True),
+    dict(B=2, H=2, Hkv=1, M=300, K=3001, d=72, kind="window", per="sequence"),
+    dict(H=2, Hkv=2, M=100, K=2500, d=43),
 ]
 
 
@@ -162,7 +166,7 @@ def test_the_choice_of_the_library(dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_few_entries_go_row_by_row_and_many_by_tiles(dtype):
     b = _binding()
-    for more, algo in ((dict(M=1, K=8192, kind="full"), b.ALGO_ROW), (dict(M=1000, K=1000, kind="sparse"), b.ALGO_ROW),
+    for more, algo in ((dict(M=4000, K=300, kind="sparse"), b.ALGO_ROW), (dict(M=1000, K=1000, kind="sparse"), b.ALGO_ROW),
                        (dict(H=8, Hkv=2, M=2000, K=2000, kind="full"), b.ALGO_TILE)):
         p = Problem(401, d=64, dtype=dtype, **more)
         p.forward(0, p.plan())
