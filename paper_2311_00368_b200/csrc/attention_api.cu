@@ -145,6 +145,7 @@ template <int MODE, typename T> b2sp_status launch_rows_v(bool wide, const RowAr
 //     200 x 8000 at 2%, one head                     30 and  38    16 and  46   (85)
 //     128 x 8192 at 50%, 8 heads, width 128         400            17          (86)
 //     4 x 5 heads over one, width 32, 700 x 700, 3%  28 and  73    13 and  52
+//     256 x 256, 12 heads over 3, width 119, 29%     43 and 141    14 and  47
 // fp32:
 //     one row of 4096 of 8192, one head              26 and  36    36 and  48
 //     64 x 64 at 30%, one head                        7 and  17    14 and  30
@@ -153,14 +154,15 @@ template <int MODE, typename T> b2sp_status launch_rows_v(bool wide, const RowAr
 //     200 x 8000 at 2%, one head                     31 and  47    38 and  58
 // fp32, width 128 (see tile_product32_kernel):
 //     64 x 64 at 30%, one head                        9 and  24    38 and  82
+//     256 x 256 at 29%, 12 heads over 3              31 and 144    42 and 100   (width 120; 119: 43 and 155, 43 and 103)
 //     2048 x 2048 at 2%, 8 heads over 2              74 and 283   228 and 733
 //     4096 x 4096 at 30%, 8 heads                  2752           875
 //     4096 x 4096, window of 1229, 8 heads over 2         9534            928
-double row_time(const Shape &s, double entries, double in_row, bool backward, bool wide)
+double row_time(const Shape &s, double entries, double in_row, bool backward, bool fp32)
 {
-    const double width = std::max(s.d, 64) / 64.0;
-    return backward ? 12 + std::max(0.25 * std::min(in_row, 128.0), (wide ? 0.19e-3 : 0.15e-3) * entries * width)
-                    : 5 + std::max(0.2 * std::min(in_row, 128.0), 0.06e-3 * entries * width);
+    // (elements one by one where rows are no whole groups of four; a row's or a column's entries one after the other, up to about 128)
+    const double work = entries * (std::max(s.d, 64) / 64.0) * (s.d & 3 ? 1.3 : 1);
+    return backward ? 12 + 0.2 * std::min(in_row, 128.0) + (fp32 ? 0.19e-3 : 0.15e-3) * work : 5 + 0.15 * std::min(in_row, 128.0) + 0.06e-3 * work;
 }
 bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward, bool fp32)
 {
@@ -170,7 +172,8 @@ bool prefer_tiles(const Shape &s, long long nnz, long long tiles, bool backward,
     if (fp32 && s.d > 64) t = backward ? 85 + 0.32 * all : 38 + 0.06 * std::min(all, 128.0) + 0.6 * in_block + 0.085 * all;
     else if (fp32) t = backward ? 30 + 0.5 * std::min(all, 16.0) + 0.082 * all : 14 + 0.06 * std::min(all, 128.0) + 0.25 * in_block + 0.0225 * all;
     else if (backward) t = 20 + 0.6 * std::min(all, 16.0) + 0.022 * all * (s.d <= 64 ? 1 : 1.6);
-    else t = 5 + 1.3 * std::max(in_block / tile_splits(s, tiles), all / 296) + (tile_splits(s, tiles) > 1 ? 5 : 0);
+    else t = 5 + 1.3 * std::max(in_block / tile_splits(s, tiles).splits, all / 296) + tile_splits(s, tiles).cost;
+    if (!fp32 && (s.d & 7)) t += backward ? 10 : 5;   // copies
     return t < row_time(s, entries, in_row, backward, fp32);
 }
 

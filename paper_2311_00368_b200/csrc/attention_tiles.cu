@@ -34,7 +34,7 @@ FwdPlan forward_plan(const Shape &s, long long tiles, size_t at)
 {
     FwdPlan p;
     const long long blocks = (long long)s.batch * s.heads * ((s.M + kTile - 1) / kTile);
-    p.splits = tile_splits(s, tiles);
+    p.splits = tile_splits(s, tiles).splits;
     p.part = at;
     p.ml = at + (p.splits > 1 ? (size_t)blocks * p.splits * kTile * (s.d <= 64 ? 64 : 128) * 4 : 0);
     p.bytes = p.ml + up256(p.splits > 1 ? (size_t)blocks * p.splits * kTile * 8 : 0);

@@ -21,12 +21,19 @@ inline Shares deal(long long tiles, long long blocks, int cost, long long least)
     return x;
 }
 
-// The bfloat16 forward pass: parts of a row block's tiles, for two CTAs per SM and four tiles a part (5 us, what joining them takes).
-inline int tile_splits(const Shape &s, long long tiles)
+// The bfloat16 forward pass: parts of a row block's tiles, up to two CTAs per SM and four tiles a part, where the tiles that a CTA is spared (1.3 us
+// each) are worth more than writing and joining the parts.  128 blocks of 32 tiles, width 64, in two parts: 48 -> 36 us; of 16 tiles 27 -> 28, at
+// width 128 28 -> 38 us.
+struct FwdSplit { int splits; double cost; };   // us
+inline FwdSplit tile_splits(const Shape &s, long long tiles)
 {
     const long long blocks = std::max(1ll, (long long)s.batch * s.heads * ((s.M + kTile - 1) / kTile));
     const long long in_block = tiles * ((long long)s.batch * s.heads / s.patterns) / blocks;
-    return in_block < 12 ? 1 : (int)std::max(1ll, std::min(2 * 148 / blocks, in_block / 4));
+    const long long splits = std::min(2 * 148 / blocks, in_block / 4);
+    if (splits < 2) return {1, 0};
+    const double cost = 6 + blocks * splits / 256.0 * (s.d <= 64 ? 5 : 14);
+    if (1.3 * (in_block - in_block / splits) < cost) return {1, 0};
+    return {(int)splits, cost};
 }
 
 struct TileCall {
