@@ -175,14 +175,15 @@ def test_few_entries_go_row_by_row_and_many_by_tiles(dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("algo", [1, 3])
-def test_what_no_entry_names_does_not_matter(algo, dtype):
+@pytest.mark.parametrize("K, d", [(300, 64), (300, 100), (4000, 100)])
+def test_what_no_entry_names_does_not_matter(algo, dtype, K, d):
     """NaN and infinities in rows of Q, K, V and dO that no entry names, next to ones that entries do name."""
-    p = Problem(500, H=2, M=300, K=300, d=64, dtype=dtype)
+    p = Problem(500, H=2, M=300, K=K, d=d, dtype=dtype)
     m = p.mask[0, 0].clone()
     m[:, 40:50] = False
     m[200:210] = False
     p.row_ptr, p.col_idx = (t.cuda() for t in plain.csr(m.cpu().numpy()))
-    p.mask = m.expand(1, 2, 300, 300)
+    p.mask = m.expand(1, 2, 300, K)
     p.k[:, :, 40:45] = float("nan")
     p.v[:, :, 40:45] = float("nan")
     p.k[:, :, 45:50] = float("inf")
@@ -196,8 +197,9 @@ def test_what_no_entry_names_does_not_matter(algo, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("algo", [1, 3])
-def test_nan_reaches_the_rows_that_name_it(algo, dtype):
-    p = Problem(501, M=256, K=256, d=64, dtype=dtype)
+@pytest.mark.parametrize("K, d", [(256, 64), (2500, 90)])
+def test_nan_reaches_the_rows_that_name_it(algo, dtype, K, d):
+    p = Problem(501, M=256, K=K, d=d, dtype=dtype)
     p.v[0, 0, 7, 3] = float("nan")
     o, lse = p.forward(algo, p.plan())
     rows = p.mask[0, 0, :, 7]
@@ -267,9 +269,10 @@ def test_gradients_against_differences():
 
 @pytest.mark.parametrize("algo", [1, 3])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_captured_and_replayed_beside_another_graph(algo, dtype):
+@pytest.mark.parametrize("sizes", [dict(M=600, K=700, d=64), dict(M=100, K=2600, d=100)])   # (and: products in memory, copies, parts)
+def test_captured_and_replayed_beside_another_graph(algo, dtype, sizes):
     """Two graphs of forward and backward, captured on one stream, replayed at once on two: neither disturbs the other."""
-    ps = [Problem(600 + i, H=2, M=600, K=700, d=64, dtype=dtype) for i in range(2)]
+    ps = [Problem(600 + i, H=2, dtype=dtype, **sizes) for i in range(2)]
     plans = [p.plan() for p in ps]
     want = []
     for p, plan in zip(ps, plans):
@@ -350,11 +353,11 @@ def test_no_rows_or_no_columns():
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("more", [dict(H=8, Hkv=2, M=1200, K=1200, kind="window"), dict(B=2, H=3, Hkv=3, M=513, K=300, per="problem"),
-                                  dict(H=2, Hkv=1, M=150, K=4000), dict(B=4, M=4000, K=140)])
+                                  dict(H=2, Hkv=1, M=150, K=4000), dict(B=4, M=4000, K=140), dict(H=2, Hkv=1, M=1000, K=900, d=111)])
 def test_no_wait_runs_out(more, dtype):
     """The tile kernels' waits are bounded and a row that one of them gives up is taken otherwise: the status word tells."""
-    b, p = _binding(), Problem(700, d=64, dtype=dtype, **more)
-    plan, ws = p.plan(), torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    b, p = _binding(), Problem(700, **{"d": 64, "dtype": dtype, **more})
+    plan, ws = p.plan(), torch.empty(1 << 29, dtype=torch.uint8, device="cuda")
     for _ in range(5):
         o, lse = p.forward(b.ALGO_TILE, plan, workspace=ws)
         assert b.device_status(ws) == 0
