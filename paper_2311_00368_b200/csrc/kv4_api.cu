@@ -113,7 +113,8 @@ struct ServePlan {
     int nb, head_blocks, ctas, share;
     size_t ml, part, bytes;
 };
-// As many CTAs as run at once (three on an SM), with at least 128 entries each.
+// As many CTAs as run at once (three on an SM), with at least 128 entries each, or one for each token: a CTA takes its tokens one after the other,
+// 3 us each however short their lists (122 tokens of up to four slots, 4 heads: 148 us with three CTAs a head, 18 with the call itself with one a token).
 ServePlan serve_plan(int M, int heads, int kv_heads, int d, long long nnz)
 {
     ServePlan p;
@@ -121,9 +122,9 @@ ServePlan serve_plan(int M, int heads, int kv_heads, int d, long long nnz)
     p.nb = group > 8 ? 2 : 1;
     p.head_blocks = (group + 8 * p.nb - 1) / (8 * p.nb);
     const long long units = (long long)kv_heads * p.head_blocks, most = std::max(1ll, 148ll * 3 / units);
-    const long long ctas = std::max(1ll, std::min(most, (nnz + 127) / 128));
-    p.share = (int)(((nnz + ctas - 1) / ctas + kSlots - 1) / kSlots * kSlots);
-    if (p.share == 0) p.share = kSlots;
+    const long long ctas = std::max(1ll, std::min(most, std::max((nnz + 127) / 128, std::min((long long)M, nnz))));
+    p.share = (int)std::max(1ll, (nnz + ctas - 1) / ctas);
+    if (p.share >= 128) p.share = (p.share + kSlots - 1) / kSlots * kSlots;
     p.ctas = (int)std::max(1ll, (nnz + p.share - 1) / p.share);
     const long long parts = M > 0 && p.ctas > 1 ? 2ll * p.ctas * heads : 0;
     p.ml = 512;

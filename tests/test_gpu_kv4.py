@@ -192,6 +192,8 @@ class Served:
     ([5000], 8, 2, 128, 6000, 6.0),
     ([40] * 33, 32, 8, 80, 900, 1.0),
     ([3000, 10, 0, 800], 40, 1, 128, 3000, 1.0),
+    ([2, 0, 4, 1] * 30, 4, 4, 128, 1024, 1.0),      # shares of a few entries
+    ([1, 3] * 100 + [3000], 8, 2, 64, 3000, 2.0),
 ])
 def test_attention_kv4(lengths, H, Hkv, d, slots, spread):
     Served(len(lengths) + d, lengths, H, Hkv, d, slots, spread).check()
