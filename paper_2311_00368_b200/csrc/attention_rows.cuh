@@ -117,6 +117,7 @@ template <typename T> struct RowArgs {
     int rows, splits;                     // rows: M, or K for kGradKV
     float *part;                          // several parts, or (kGradKV) several query heads per K and V: see part_floats()
     float2 *part_ml;
+    int fours_in;                         // rows taken again by the fp32 tile kernels: those of all inputs are aligned groups of four
 };
 // The partial results of one part of one row: `acc` (kGradKV: two of them), d rounded up to four.
 __host__ __device__ constexpr int part_width(int mode, int d) { return ((d + 3) & ~3) * (mode == kGradKV ? 2 : 1); }

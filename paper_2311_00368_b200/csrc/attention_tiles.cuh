@@ -138,7 +138,7 @@ __device__ __forceinline__ bool store32(Bf16 *row, int c0, int d, const uint32_t
 
 // Rows of the 32 that a warp owns whose lane says `bad`, entry by entry (rows of the pattern; kGradKV: columns, over the query heads
 // [h0, h0 + heads) that share them).
-template <int MODE, int DW, typename T = Bf16, int V = 4>
+template <int MODE, int DW, typename T, int V>
 __device__ __noinline__ void rows_one_by_one(const RowArgs<T> &g, const int *ptr, const int *idx, int b, int h0, int heads, int row0, unsigned bad,
                                              long long ptr_stride, long long idx_stride)
 {
@@ -163,6 +163,15 @@ __device__ __noinline__ void rows_one_by_one(const RowArgs<T> &g, const int *ptr
         }
         all.finish(g, b, h0, row);
     }
+}
+// The same for a kernel that stores the outputs in groups of V.  Those rows are read as they lie: fp32 inputs may have any alignment beside
+// aligned outputs.
+template <int MODE, int DW, typename T, int V>
+__device__ __forceinline__ void take_rows_again(const RowArgs<T> &g, const int *ptr, const int *idx, int b, int h0, int heads, int row0, unsigned bad,
+                                                long long ptr_stride, long long idx_stride)
+{
+    if (V == 4 && (sizeof(T) == 2 || g.fours_in)) rows_one_by_one<MODE, DW, T, 4>(g, ptr, idx, b, h0, heads, row0, bad, ptr_stride, idx_stride);
+    else rows_one_by_one<MODE, DW, T, sizeof(T) == 2 ? 4 : 1>(g, ptr, idx, b, h0, heads, row0, bad, ptr_stride, idx_stride);
 }
 
 constexpr int kTileThreads = 192;   // four softmax warps, a TMA warp, an MMA warp
@@ -431,7 +440,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         if (in) lse[row] = live ? fmaf(ref, c2, log2f(l)) * kLn2 : -CUDART_INF_F;
         const unsigned redo = __ballot_sync(~0u, bad);
-        if (redo && ok) rows_one_by_one<kForward, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, rb * kTile + warp * 32, redo, a.g.ptr_stride, a.g.idx_stride);
+        if (redo && ok) take_rows_again<kForward, DP, Bf16, 4>(a.g, a.g.ptr, a.g.idx, b, h, 1, rb * kTile + warp * 32, redo, a.g.ptr_stride, a.g.idx_stride);
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
@@ -481,7 +490,7 @@ template <int DP> __global__ void __launch_bounds__(256) tile_forward_join_kerne
     __syncthreads();
     const int row0 = rb * kTile + blockIdx.x % PARTS * ROWS;
     for (unsigned left = redo >> (threadIdx.x >> 5), k = threadIdx.x >> 5; left; left >>= 8, k += 8)
-        if (left & 1) rows_one_by_one<kForward, DP>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + (int)k, 1u, a.g.ptr_stride, a.g.idx_stride);
+        if (left & 1) take_rows_again<kForward, DP, Bf16, 4>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + (int)k, 1u, a.g.ptr_stride, a.g.idx_stride);
 }
 
 // ---- the backward pass: dQ, and dK with dV -----------------------------------------------------------------------------------------
@@ -943,8 +952,8 @@ __device__ __forceinline__ void tile_grad_rows(const GradArgsOf<T> &g, int o, in
 {
     const TileArgsOf<T> &a = g.a;
     const int b = o / g.w.outer, h = o % g.w.outer, row = blk * kTile + r;
-    if (MODE == kDq) rows_one_by_one<kGradQ, DW, T, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
-    else rows_one_by_one<kGradKV, DW, T, V>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
+    if (MODE == kDq) take_rows_again<kGradQ, DW, T, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row, 1u, a.g.ptr_stride, a.g.idx_stride);
+    else take_rows_again<kGradKV, DW, T, V>(a.g, a.col_ptr, a.row_idx, b, h * g.w.group, g.w.group, row, 1u, a.g.s.K + 1ll, a.g.idx_stride);
 }
 // DP: columns of the sums; they are columns col0 and on of the outputs, dc of them.  DW: width class of whole rows.
 template <int MODE, int DP, int DW, typename T, int V>

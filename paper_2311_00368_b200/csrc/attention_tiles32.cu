@@ -73,6 +73,7 @@ Args32 args(const Call32 &c, const Plan32 &p, int k)
     r.stat = c.stat; r.stat_stride = c.stat_stride;
     r.lse = c.lse; r.lse_head = c.s.M; r.lse_row = 1;
     r.splits = 1;
+    r.fours_in = c.wide_in;
     f.g.a.plan = c.plan;
     f.g.a.col_ptr = c.plan.col_ptr; f.g.a.row_idx = c.plan.row_idx;
     f.g.a.status = c.status;

@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(256) tile_forward32_join_kernel(const __grid_c
     }
     __syncthreads();
     for (unsigned left = redo >> (threadIdx.x >> 5), r = threadIdx.x >> 5; left; left >>= 8, r += 8)
-        if (left & 1) rows_one_by_one<kForward, DW, float, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + (int)r, 1u, a.g.ptr_stride, a.g.idx_stride);
+        if (left & 1) take_rows_again<kForward, DW, float, V>(a.g, a.g.ptr, a.g.idx, b, h, 1, row0 + (int)r, 1u, a.g.ptr_stride, a.g.idx_stride);
 }
 
 // ---- the backward pass -------------------------------------------------------------------------------------------------------------
