@@ -389,11 +389,15 @@ extern "C" b2sp_status b2sp_attention_prepare(int patterns, int M, int K, long l
     char *b = static_cast<char *>(plan);
     // (everything but the transposed indices begins as zeros: the masks are built by setting bits)
     if (cudaMemsetAsync(plan, 0, l.row_idx, st) != cudaSuccess) return B2SP_ERR_CUDA;
-    if (M == 0 || K == 0 || tiles == 0) return B2SP_OK;
+    if (M == 0) return B2SP_OK;
     auto i32 = [&](size_t at) { return reinterpret_cast<int *>(b + at); };
     auto u32 = [&](size_t at) { return reinterpret_cast<unsigned *>(b + at); };
     const Csr s{row_ptr, col_idx, row_ptr_stride, nnz_stride, M, K};
     const int rbs = patterns * l.RB, cbs = patterns * l.CB;
+    if (K == 0 || tiles == 0) {   // nothing to list, but row pointers and columns are still checked (all columns may be out of range)
+        plan_mark_kernel<<<rbs, 256, l.words * 4, st>>>(s, l.RB, l.CB, l.words, nullptr, nullptr, nullptr, nullptr, i32(0));
+        return launched();
+    }
     plan_mark_kernel<<<rbs, 256, l.words * 4, st>>>(s, l.RB, l.CB, l.words, u32(l.bitmap), u32(l.rank), i32(l.rb_ptr), nullptr, i32(0));
     plan_scan_kernel<<<1, 1024, 0, st>>>(i32(l.rb_ptr), rbs, 0);
     plan_column_count_kernel<<<(cbs + 127) / 128, 128, 0, st>>>(patterns, l.RB, l.CB, l.words, u32(l.bitmap), i32(l.cb_ptr));
