@@ -373,8 +373,12 @@ __device__ __forceinline__ unsigned transpose8(unsigned x)   // an 8 x 8 matrix 
 //   * Q goes to f16 exactly: divided by a power of two that brings each head's largest element below 2; what is more than 2^-14 smaller
 //     than that loses at most 2^-25 of it, as much as fp32 sums would.  The scale of a group of K multiplies the products of its 32 elements.
 //   * The scale of (slot, group) of V multiplies the slot's weight, divided by a power of two per group that keeps all scales met so far below
-//     2^7, and that is rounded to f16 (half a step: 2^-11 of a weight down to 2^-29 of the largest, below that 2^-40 of the largest).  It is the
-//     one rounding of this kernel beside that of the output.
+//     2^7, and that is rounded to f16: half a step is 2^-11 of the product, 2^-25 at least.  Scales are not below 1 then, so a weight is off by no
+//     more than 2^-11 of itself or 2^-25 of the row's largest.  That holds while the scales of a group lie within 2^7 of each other; where they do not,
+//     the slot with the largest may weigh nothing, and the others would vanish beside it.  From the first such slots of a row on, each head's and
+//     group's largest product among 16 slots is brought to 2^8 of its own, and the products of the 16 are added up in fp32 (32 heads over 8, width 128:
+//     one token of 32768 slots 19.3 us, with every eighth scale 2^20 times the others 22.9; 64 tokens 308 and 318).  It is the one rounding of
+//     this kernel beside that of the output.
 //   * The running maximum moves only when a logit exceeds it by 8 (to base 2): weights up to 2^8.
 // Slot r of a half tile is row r of the first product; V's rows lie in the order (r & 1) * 4 + r / 2 of each eight, so that the four lanes of
 // a column of V read different banks.
@@ -383,6 +387,7 @@ __device__ __forceinline__ unsigned transpose8(unsigned x)   // an 8 x 8 matrix 
 // keep all SMs busy to the end.  A row inside one share is finished there; of a row that goes on, each CTA leaves its part in the workspace: in slot 0
 // if the row began in an earlier share, else in slot 1; kv4_join_kernel joins the parts in order, and writes the rows without entries.
 constexpr int kStages = 2, kSlots = 32;
+constexpr float kDownFirst = 1.2676506e30f;   // 2^100
 template <int G, int NB> struct Smem {
     static constexpr int ROW = 16 * G;
     static constexpr int K = 0, V = kSlots * ROW, KS = 2 * kSlots * ROW, VS = KS + kSlots * 8, STAGE = VS + kSlots * 8;
@@ -596,9 +601,11 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
         }
         float o[G][2][NB][4] = {};   // [group][pair of elements]: rows g (the first of the pair) and g + 8 (the second), columns 2 t, 2 t + 1
         float top[NB][2], base[NB][2], sum[NB][2];   // base: top, or 0 as long as that is -inf
-        float down[G];               // what V's scales are multiplied by (2^100 at first, which any scale above 2^-93 moves)
+        float down[G];               // what V's scales are multiplied by (at first kDownFirst, which any scale above 2^-93 moves)
+        int fallen = 0;              // by how many powers of two, in all
+        bool far = false;            // scales of a group of V more than 2^7 apart have been met
 #pragma unroll
-        for (int c = 0; c < G; ++c) down[c] = 1.2676506e30f;
+        for (int c = 0; c < G; ++c) down[c] = kDownFirst;
 #pragma unroll
         for (int m = 0; m < NB; ++m) { top[m][0] = top[m][1] = -CUDART_INF_F; base[m][0] = base[m][1] = 0.f; sum[m][0] = sum[m][1] = 0.f; }
 
@@ -627,6 +634,7 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
                         if (x > 0.f) {   // (the same for all lanes)
                             const float to = __uint_as_float((unsigned)min(max(254 + 6 - (int)(__float_as_uint(x) >> 23), 1), 253) << 23);
                             const float f = to * __uint_as_float((254u << 23) - __float_as_uint(down[c]));
+                            if (down[c] != kDownFirst) fallen += (int)((__float_as_uint(down[c]) - __float_as_uint(to)) >> 23);
                             down[c] = to;
 #pragma unroll
                             for (int m = 0; m < NB; ++m)
@@ -636,10 +644,14 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
                     }
                 }
 #pragma unroll
-                for (int c = 0; c < G; ++c) vs[c] *= down[c];
+                for (int c = 0; c < G; ++c) {
+                    vs[c] *= down[c];
+                    far |= vs[c] > 0.f && vs[c] < 1.f;
+                }
                 sts_wide<G>(wide + lane * 16, ks);
                 sts_wide<G>(wide + kSlots * 16 + lane * 16, vs);
             }
+            far = __any_sync(~0u, far) || fallen > 7;
             __syncwarp();
             float x[2][NB][4];   // of each half tile: logits of slots g (two heads) and g + 8 (two heads)
 #pragma unroll
@@ -704,8 +716,8 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
                             }
                     }
             }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            auto half_tile = [&](auto jj, auto uneven) {   // 16 slots; uneven: scales too far apart for one power of two
+                constexpr int j = decltype(jj)::value;
 #pragma unroll
                 for (int m = 0; m < NB; ++m)
 #pragma unroll
@@ -728,12 +740,42 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
                     const unsigned b0 = codes_low(z0, k1024), b1 = codes_high(z0, k1024), b2 = codes_low(z1, k1024), b3 = codes_high(z1, k1024);
 #pragma unroll
                     for (int m = 0; m < NB; ++m) {
-                        const unsigned p0 = transpose8(f16x2(x[j][m][0] * s0[c], x[j][m][1] * s0[c]));
-                        const unsigned p1 = transpose8(f16x2(x[j][m][2] * s1[c], x[j][m][3] * s1[c]));
-                        mma_f16(o[c][0][m], a0, a1, a2, a3, p0, p1);
-                        mma_f16(o[c][1][m], b0, b1, b2, b3, p0, p1);
+                        float y[4];   // weights times scales: slot g, heads 2 t and 2 t + 1; slot g + 8
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = x[j][m][e] * (e < 2 ? s0[c] : s1[c]);
+                        if constexpr (!decltype(uneven)::value) {
+                            const unsigned p0 = transpose8(f16x2(y[0], y[1])), p1 = transpose8(f16x2(y[2], y[3]));
+                            mma_f16(o[c][0][m], a0, a1, a2, a3, p0, p1);
+                            mma_f16(o[c][1][m], b0, b1, b2, b3, p0, p1);
+                        } else {   // each head's largest product to 2^8 .. 2^9
+                            float by[2], back[2], part0[4], part1[4];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float most = fmaxf(y[e], y[e + 2]);
+#pragma unroll
+                                for (int k = 4; k < 32; k <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, k));
+                                const int to = min(max(262 - (int)(__float_as_uint(most) >> 23), 1), 253);
+                                by[e] = __uint_as_float((unsigned)to << 23);
+                                back[e] = __uint_as_float((unsigned)(254 - to) << 23);
+                            }
+                            const unsigned p0 = transpose8(f16x2(y[0] * by[0], y[1] * by[1])), p1 = transpose8(f16x2(y[2] * by[0], y[3] * by[1]));
+                            mma_f16_first(part0, a0, a1, a2, a3, p0, p1);
+                            mma_f16_first(part1, b0, b1, b2, b3, p0, p1);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                o[c][0][m][e] = fmaf(part0[e], back[e & 1], o[c][0][m][e]);
+                                o[c][1][m][e] = fmaf(part1[e], back[e & 1], o[c][1][m][e]);
+                            }
+                        }
                     }
                 });
+            };
+            if (!far) {
+                half_tile(std::integral_constant<int, 0>{}, std::false_type{});
+                half_tile(std::integral_constant<int, 1>{}, std::false_type{});
+            } else {
+                half_tile(std::integral_constant<int, 0>{}, std::true_type{});
+                half_tile(std::integral_constant<int, 1>{}, std::true_type{});
             }
             __syncwarp();
         }
