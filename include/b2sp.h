@@ -23,7 +23,8 @@
  *     into a CUDA graph (make one ordinary call first: it does the library's one-time driver queries);
  *   - `workspace` is scratch of at least b2sp_workspace_bytes(...) bytes, 256-byte aligned;
  *     its contents are overwritten by every call, so two calls that may overlap in time on
- *     the GPU (different streams) need different workspaces;
+ *     the GPU (different streams) need different workspaces, and so do calls that two host threads
+ *     make at once on one stream (their kernels may take turns);
  *   - argument errors are reported synchronously with no kernel launched; a launch failure
  *     is reported as B2SP_ERR_CUDA; nothing traps, asserts or exits.
  *   - M = 0, nnz = 0 and zero widths are valid (outputs of the stated size are zero-filled).

@@ -14,6 +14,7 @@ import ctypes
 import functools
 import os
 import struct
+import threading
 
 import torch
 
@@ -193,7 +194,14 @@ def workspace_bytes(op: int, M: int, K: int, Kd: int, N: int, nnz: int, algo=Non
     return int(lib.b2sp_workspace_bytes_algo(op, algo, M, K, Kd, N, nnz))
 
 
-_ws_cache = {}
+class _Kept(threading.local):
+    """Workspaces that this module keeps, per device and stream, for each thread of its own: a call's kernels pass partial results through
+    its workspace, and the launches of two threads may take turns on one stream."""
+    def __init__(self):
+        self.workspaces = {}
+
+
+_kept = _Kept()
 
 
 _planner_setting = 0   # counts the calls of the debug hooks that change the planner's choice
@@ -208,11 +216,11 @@ def _workspace_need(op, M, K, Kd, N, nnz, algo, setting):
 def _workspace(op, M, K, Kd, N, nnz, device, workspace, algo=0):
     if workspace is None:
         need = _workspace_need(op, M, K, Kd, N, nnz, algo, _planner_setting)
-        key = (device.index, _raw_stream(device.index))
-        workspace = _ws_cache.get(key)
+        key, workspaces = (device.index, _raw_stream(device.index)), _kept.workspaces
+        workspace = workspaces.get(key)
         if workspace is None or workspace.numel() < need:
             workspace = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=device)
-            _ws_cache[key] = workspace
+            workspaces[key] = workspace
     return workspace, workspace.numel()
 
 
@@ -500,7 +508,7 @@ except AttributeError:
 
 
 def _scratch(need, device, workspace, stream):
-    """`workspace`, or one that this module keeps per device and stream; a call that is being captured gets one of its own, which
+    """`workspace`, or one that this module keeps per thread, device and stream; a call that is being captured gets one of its own, which
     belongs to the graph, so that graphs can be replayed side by side."""
     if workspace is not None:
         if workspace.dtype is not torch.uint8 or workspace.device != device:
@@ -508,11 +516,11 @@ def _scratch(need, device, workspace, stream):
         return workspace
     if _capturing():
         return torch.empty(need, dtype=torch.uint8, device=device)
-    key = (device.index, stream, "attention")
-    workspace = _ws_cache.get(key)
+    key, workspaces = (device.index, stream, "attention"), _kept.workspaces
+    workspace = workspaces.get(key)
     if workspace is None or workspace.numel() < need:
         workspace = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=device)
-        _ws_cache[key] = workspace
+        workspaces[key] = workspace
     return workspace
 
 
