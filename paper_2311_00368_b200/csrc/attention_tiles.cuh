@@ -35,6 +35,7 @@ template <typename T> struct TileArgsOf {
     Op q, k, v, dout;
     const int *col_ptr, *row_idx;        // transposed pattern
     int *status;
+    int drop_chunk;      // test hook: the loading warp leaves this one of its CTA's loads out (-1: none), so that waits run out
 };
 using TileArgs = TileArgsOf<Bf16>;
 
@@ -247,7 +248,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         ptx::mbar_init(s_full(0), 1); ptx::mbar_init(s_full(1), 1);
         ptx::mbar_init(q_full, 1); ptx::mbar_init(p_full(0), 4); ptx::mbar_init(p_full(1), 4); ptx::mbar_init(o_full, 1);
         ptx::mbar_init(done, 1);
-        ptx::mbar_init(slot + 8, 1);   // only for leaving early
+        ptx::mbar_init(slot + 8, 1);   // the last products
         ptx::fence_mbar_init();
     }
     if (warp == 5) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
@@ -263,8 +264,9 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
     if (warp == 4) {
         if (ptx::elect_one()) {
+            int chunk = 0;
             ptx::mbar_arrive_expect_tx(q_full, C::TILE);
-            load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
+            if (chunk++ != a.drop_chunk) load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
             // K runs ahead of V by the stages that it has more
             constexpr int AHEAD = C::KSTAGES - C::VSTAGES;
             int ik = 0, iv = 0;
@@ -275,21 +277,20 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const int st = ik % C::KSTAGES;
                     if (!wait(k_free(st), (ik / C::KSTAGES & 1) ^ 1)) break;
                     ptx::mbar_arrive_expect_tx(k_full(st), C::HALF);
-                    load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at_k, hkv * a.k.hm, b * a.k.bm);
+                    if (chunk++ != a.drop_chunk) load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at_k, hkv * a.k.hm, b * a.k.bm);
                     if (++ik < steps) at_k = key(ik);
                 } else {
                     const int st = iv % C::VSTAGES;
                     if (!wait(v_free(st), (iv / C::VSTAGES & 1) ^ 1)) break;
                     ptx::mbar_arrive_expect_tx(v_full(st), C::HALF);
-                    load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at_v, hkv * a.v.hm, b * a.v.bm);
+                    if (chunk++ != a.drop_chunk) load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at_v, hkv * a.v.hm, b * a.v.bm);
                     if (++iv < steps) at_v = key(iv);
                 }
             }
-            if (!ok) {   // copies in flight land before the CTA ends
-                ptx::mbar_wait(q_full, 0);
-                for (int k = max(0, ik - C::KSTAGES); k < ik; ++k) ptx::mbar_wait(k_full(k % C::KSTAGES), k / C::KSTAGES & 1);
-                for (int k = max(0, iv - C::VSTAGES); k < iv; ++k) ptx::mbar_wait(v_full(k % C::VSTAGES), k / C::VSTAGES & 1);
-            }
+            // copies in flight land before the CTA ends, also where another warp gave up a wait
+            ptx::mbar_wait(q_full, 0);
+            for (int k = max(0, ik - C::KSTAGES); k < ik; ++k) ptx::mbar_wait(k_full(k % C::KSTAGES), k / C::KSTAGES & 1);
+            for (int k = max(0, iv - C::VSTAGES); k < iv; ++k) ptx::mbar_wait(v_full(k % C::VSTAGES), k / C::VSTAGES & 1);
         }
         __syncwarp();
     } else if (warp == 5) {
@@ -318,10 +319,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (i + 1 == steps) ptx::mma_commit(done);   // (a warp may come too late to tell the last phase of o_full from the one before)
                 if (n < steps) first(n);   // (over the weights just taken: the tensor core takes one thread's products in order)
             }
-            if (!ok) {   // products in flight end before tensor memory is freed
-                ptx::mma_commit(slot + 8);
-                ptx::mbar_wait(slot + 8, 0);
-            }
+            ptx::mma_commit(slot + 8);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 8, 0);
         }
         __syncwarp();
     } else {
@@ -705,7 +704,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
         for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
         for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 8); ptx::mbar_init(s_free(i), 1); }
         ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1); ptx::mbar_init(o_full, 1); ptx::mbar_init(o_free, 8 * SETS);
-        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // only for leaving early
+        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // the last products
         ptx::fence_mbar_init();
     }
     if (warp == FIRST_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
@@ -724,7 +723,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0;
+        int i = 0, blocks = 0, chunk = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
@@ -735,30 +734,30 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * C::TILE);
                     const Op &o1 = MODE == kDq ? a.q : a.k, &o2 = MODE == kDq ? a.dout : a.v;
-                    load_tile<DP, 128>(base + C::X1, &tm_x1, x_full, blk * kTile, x * o1.hm, b * o1.bm);
+                    if (chunk != a.drop_chunk) load_tile<DP, 128>(base + C::X1, &tm_x1, x_full, blk * kTile, x * o1.hm, b * o1.bm);
                     load_tile<DP, 128>(base + C::X2, &tm_x2, x_full, blk * kTile, x * o2.hm, b * o2.bm);
                 }
                 __syncwarp();
                 ++blocks;
+                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i) {
+            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     ptx::mbar_arrive_expect_tx(full(st), 2 * C::HALF + C::STAT);
                     const Op &o1 = MODE == kDq ? a.k : a.q, &o2 = MODE == kDq ? a.v : a.dout;
-                    load_tile<DP, 64>(base + C::Y1 + st * C::HALF, &tm_y1, full(st), at, hy * o1.hm, b * o1.bm);
+                    if (chunk != a.drop_chunk) load_tile<DP, 64>(base + C::Y1 + st * C::HALF, &tm_y1, full(st), at, hy * o1.hm, b * o1.bm);
                     load_tile<DP, 64>(base + C::Y2 + st * C::HALF, &tm_y2, full(st), at, hy * o2.hm, b * o2.bm);
                     if (MODE == kDkv) bulk_load(base + C::ST + st * C::STAT, a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride + at, C::STAT, full(st));
                 }
                 __syncwarp();
             }
         }
-        if (!ok) {   // copies in flight land before the CTA ends
-            if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
-            for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
-        }
+        // copies in flight land before the CTA ends, also where another warp gave up a wait
+        if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
+        for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
     } else if (warp == FIRST_WARP) {
         if (ptx::elect_one()) {
             const int ks = (s.d + 15) >> 4;
@@ -775,10 +774,8 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {   // products in flight end before tensor memory is freed
-                ptx::mma_commit(slot + 16);
-                ptx::mbar_wait(slot + 16, 0);
-            }
+            ptx::mma_commit(slot + 16);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 16, 0);
         }
         __syncwarp();
     } else if (warp == SECOND_WARP) {
@@ -810,10 +807,8 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {
-                ptx::mma_commit(slot + 24);
-                ptx::mbar_wait(slot + 24, 0);
-            }
+            ptx::mma_commit(slot + 24);
+            ptx::mbar_wait(slot + 24, 0);
         }
         __syncwarp();
     } else {

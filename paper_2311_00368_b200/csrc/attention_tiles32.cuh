@@ -146,7 +146,7 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
         for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
         for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(s_free(i), 4); }
         ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1);
-        ptx::mbar_init(slot + 16, 1);   // only for leaving early
+        ptx::mbar_init(slot + 16, 1);   // the last products
         ptx::fence_mbar_init();
     }
     if (warp == FIRST_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
@@ -165,7 +165,7 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0;
+        int i = 0, blocks = 0, chunk = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
@@ -174,26 +174,26 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * kPlaneTile);
-                    for (int c = 0; c < 2; ++c) load_planes<128>(base + C::X + c * kPlaneTile, &tm_x, x_full, c, blk * kTile, h, b);
+                    for (int c = chunk == a.drop_chunk; c < 2; ++c) load_planes<128>(base + C::X + c * kPlaneTile, &tm_x, x_full, c, blk * kTile, h, b);
                 }
                 __syncwarp();
                 ++blocks;
+                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i) {
+            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     ptx::mbar_arrive_expect_tx(full(st), 2 * kPlaneHalf);
-                    for (int c = 0; c < 2; ++c) load_planes<64>(base + C::Y + (2 * st + c) * kPlaneHalf, &tm_y, full(st), c, at, hkv, b);
+                    for (int c = chunk == a.drop_chunk; c < 2; ++c) load_planes<64>(base + C::Y + (2 * st + c) * kPlaneHalf, &tm_y, full(st), c, at, hkv, b);
                 }
                 __syncwarp();
             }
         }
-        if (!ok) {   // copies in flight land before the CTA ends
-            if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
-            for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
-        }
+        // copies in flight land before the CTA ends, also where another warp gave up a wait
+        if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
+        for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
     } else if (warp == FIRST_WARP) {
         if (ptx::elect_one()) {
             const int ks = (s.d - kPlane + 15) >> 4;   // of the second chunk
@@ -214,10 +214,8 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {
-                ptx::mma_commit(slot + 16);
-                ptx::mbar_wait(slot + 16, 0);
-            }
+            ptx::mma_commit(slot + 16);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 16, 0);
         }
         __syncwarp();
     } else {
@@ -287,7 +285,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
         for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 4); ptx::mbar_init(s_free(i), 1); }
         ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1);
-        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // only for leaving early
+        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // the last products
         ptx::fence_mbar_init();
     }
     if (warp == FIRST_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
@@ -306,7 +304,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0;
+        int i = 0, blocks = 0, chunk = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
             if (READ) {
@@ -320,27 +318,27 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, kPlaneTile);
-                    load_planes<128>(base + C::Q, &tm_q, x_full, 0, blk * kTile, h, b);
+                    if (chunk != a.drop_chunk) load_planes<128>(base + C::Q, &tm_q, x_full, 0, blk * kTile, h, b);
                 }
                 __syncwarp();
                 ++blocks;
+                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i) {
+            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     ptx::mbar_arrive_expect_tx(full(st), (READ ? 1 : 2) * kPlaneHalf);
                     if (!READ) load_planes<64>(base + C::K + st * kPlaneHalf, &tm_k, full(st), 0, at, hkv, b);
-                    load_planes<64>(base + C::V + st * kPlaneHalf, &tm_v, full(st), f.col0 / kPlane, at, hkv, b);
+                    if (chunk != a.drop_chunk) load_planes<64>(base + C::V + st * kPlaneHalf, &tm_v, full(st), f.col0 / kPlane, at, hkv, b);
                 }
                 __syncwarp();
             }
         }
-        if (!ok) {   // copies in flight land before the CTA ends
-            if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
-            for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
-        }
+        // copies in flight land before the CTA ends, also where another warp gave up a wait
+        if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
+        for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
     } else if (warp == FIRST_WARP) {
         if (!READ && ptx::elect_one()) {
             const int ks = (s.d + 15) >> 4;
@@ -357,10 +355,8 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {
-                ptx::mma_commit(slot + 16);
-                ptx::mbar_wait(slot + 16, 0);
-            }
+            ptx::mma_commit(slot + 16);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 16, 0);
         }
         __syncwarp();
     } else if (warp == SECOND_WARP) {
@@ -377,10 +373,8 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {
-                ptx::mma_commit(slot + 24);
-                ptx::mbar_wait(slot + 24, 0);
-            }
+            ptx::mma_commit(slot + 24);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 24, 0);
         }
         __syncwarp();
     } else {
@@ -605,7 +599,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
         for (int i = 0; i < C::STAGES; ++i) { ptx::mbar_init(full(i), 1); ptx::mbar_init(free_(i), 1); }
         for (int i = 0; i < SETS; ++i) { ptx::mbar_init(s_full(i), 1); ptx::mbar_init(p_full(i), 4); ptx::mbar_init(s_free(i), 1); }
         ptx::mbar_init(x_full, 1); ptx::mbar_init(x_free, 1); ptx::mbar_init(o_full, 1); ptx::mbar_init(o_free, 8);
-        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // only for leaving early
+        ptx::mbar_init(slot + 16, 1); ptx::mbar_init(slot + 24, 1);   // the last products
         ptx::fence_mbar_init();
     }
     if (warp == FIRST_WARP) { ptx::tmem_alloc(slot, C::COLS); ptx::tmem_relinquish(); }
@@ -624,7 +618,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0;
+        int i = 0, blocks = 0, chunk = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
@@ -642,30 +636,30 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * kPlaneTile);
-                    load_planes<128>(base + C::X1, &tm_x1, x_full, 0, blk * kTile, x, b);
+                    if (chunk != a.drop_chunk) load_planes<128>(base + C::X1, &tm_x1, x_full, 0, blk * kTile, x, b);
                     load_planes<128>(base + C::X2, &tm_x2, x_full, 0, blk * kTile, x, b);
                 }
                 __syncwarp();
                 ++blocks;
+                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i) {
+            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     constexpr bool BOTH = !READ || MODE == kDkv;   // (V serves dP alone)
                     ptx::mbar_arrive_expect_tx(full(st), (BOTH ? 2 : 1) * kPlaneHalf + C::STAT);
-                    load_planes<64>(base + C::Y1 + st * kPlaneHalf, &tm_y1, full(st), f.col0 / kPlane, at, hy, b);
+                    if (chunk != a.drop_chunk) load_planes<64>(base + C::Y1 + st * kPlaneHalf, &tm_y1, full(st), f.col0 / kPlane, at, hy, b);
                     if (BOTH) load_planes<64>(base + C::Y2 + st * kPlaneHalf, &tm_y2, full(st), f.col0 / kPlane, at, hy, b);
                     if (MODE == kDkv) bulk_load(base + C::ST + st * C::STAT, a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride + at, C::STAT, full(st));
                 }
                 __syncwarp();
             }
         }
-        if (!ok) {
-            if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
-            for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
-        }
+        // copies in flight land before the CTA ends, also where another warp gave up a wait
+        if (blocks) ptx::mbar_wait(x_full, (blocks - 1) & 1);
+        for (int k = max(0, i - C::STAGES); k < i; ++k) ptx::mbar_wait(full(k % C::STAGES), k / C::STAGES & 1);
     } else if (warp == FIRST_WARP) {
         if (!READ && ptx::elect_one()) {
             const int ks = (s.d + 15) >> 4;
@@ -684,10 +678,8 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {
-                ptx::mma_commit(slot + 16);
-                ptx::mbar_wait(slot + 16, 0);
-            }
+            ptx::mma_commit(slot + 16);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 16, 0);
         }
         __syncwarp();
     } else if (warp == SECOND_WARP) {
@@ -708,10 +700,8 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                 if (++st == C::STAGES) { st = 0; ph ^= 1; }
                 if (++set == SETS) { set = 0; ++round; }
             }
-            if (!ok) {
-                ptx::mma_commit(slot + 24);
-                ptx::mbar_wait(slot + 24, 0);
-            }
+            ptx::mma_commit(slot + 24);   // products in flight end before tensor memory is freed, also where another warp gave up a wait
+            ptx::mbar_wait(slot + 24, 0);
         }
         __syncwarp();
     } else if (warp < SUM_WARP) {
