@@ -377,7 +377,7 @@ __device__ __forceinline__ unsigned transpose8(unsigned x)   // an 8 x 8 matrix 
 //     more than 2^-11 of itself or 2^-25 of the row's largest.  That holds while the scales of a group lie within 2^7 of each other; where they do not,
 //     the slot with the largest may weigh nothing, and the others would vanish beside it.  From the first such slots of a row on, each head's and
 //     group's largest product among 16 slots is brought to 2^8 of its own, and the products of the 16 are added up in fp32 (32 heads over 8, width 128:
-//     one token of 32768 slots 19.3 us, with every eighth scale 2^20 times the others 22.9; 64 tokens 308 and 318).  It is the one rounding of
+//     one token of 32768 slots 19.1 us, with every eighth scale 2^20 times the others 22.8; 64 tokens 315 and 333).  It is the one rounding of
 //     this kernel beside that of the output.
 //   * The running maximum moves only when a logit exceeds it by 8 (to base 2): weights up to 2^8.
 // Slot r of a half tile is row r of the first product; V's rows lie in the order (r & 1) * 4 + r / 2 of each eight, so that the four lanes of
@@ -602,8 +602,7 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
         float o[G][2][NB][4] = {};   // [group][pair of elements]: rows g (the first of the pair) and g + 8 (the second), columns 2 t, 2 t + 1
         float top[NB][2], base[NB][2], sum[NB][2];   // base: top, or 0 as long as that is -inf
         float down[G];               // what V's scales are multiplied by (at first kDownFirst, which any scale above 2^-93 moves)
-        int fallen = 0;              // by how many powers of two, in all
-        bool far = false;            // scales of a group of V more than 2^7 apart have been met
+        int fallen = 0;              // by how many powers of two, in all; above 7: scales of a group more than 2^7 apart have been met
 #pragma unroll
         for (int c = 0; c < G; ++c) down[c] = kDownFirst;
 #pragma unroll
@@ -618,6 +617,7 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
             issue(i + 1, now);   // into the stage that the last iteration read (all lanes are past it)
             const char *st = ring + (i % kStages) * S::STAGE;
             const unsigned valid = __ballot_sync(~0u, cur >= 0);
+            bool small = false;
             {
                 // a slot's scales per lane, to fp32
                 float ks[G], vs[G], high = 0.f;
@@ -646,12 +646,12 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
 #pragma unroll
                 for (int c = 0; c < G; ++c) {
                     vs[c] *= down[c];
-                    far |= vs[c] > 0.f && vs[c] < 1.f;
+                    small |= __float_as_uint(vs[c]) - 1u < 0x3f7fffffu;   // (above 0 and below 1)
                 }
                 sts_wide<G>(wide + lane * 16, ks);
                 sts_wide<G>(wide + kSlots * 16 + lane * 16, vs);
             }
-            far = __any_sync(~0u, far) || fallen > 7;
+            if (__any_sync(~0u, small)) fallen = 8;
             __syncwarp();
             float x[2][NB][4];   // of each half tile: logits of slots g (two heads) and g + 8 (two heads)
 #pragma unroll
@@ -770,7 +770,7 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
                     }
                 });
             };
-            if (!far) {
+            if (fallen <= 7) {
                 half_tile(std::integral_constant<int, 0>{}, std::false_type{});
                 half_tile(std::integral_constant<int, 1>{}, std::false_type{});
             } else {
