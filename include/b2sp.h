@@ -240,7 +240,9 @@ b2sp_status b2sp_fusedmm_batched_bf16(int batch, int M, int K, int Kd, int N, lo
  *
  * the sums over the columns j that row i of the pattern stores.  A row that stores nothing (or whose products are all
  * -inf) gives a zero row of O and lse_i = -inf.  Only stored positions count: what Q, K, V or dO hold in rows that no
- * entry names, NaN and infinities too, changes nothing.
+ * entry names, NaN and infinities too, does not enter the results.  (By tiles, see below, bfloat16 results can move by their own rounding with it, fp32
+ * ones keep their bits while it is finite.  Rows that meet a NaN or an infinity in a tile, stored or not, are taken entry by entry there, a warp
+ * each: right, but slow.  Padding is best zeros.)
  *
  * batch x heads problems of the same sizes; heads / kv_heads neighbouring query heads share one head of K and V.  The pattern (M x K, no
  * stored values) belongs to all problems (patterns = 1), to a sequence (patterns = batch) or to a problem (patterns =

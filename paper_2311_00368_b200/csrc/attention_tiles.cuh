@@ -15,7 +15,9 @@
 // The reference of the exponentials (the "maximum") is taken over all 128 products of a row's tile, masked or not, which spares the mask in
 // that sweep; it moves only when it grows by more than 8 (to base 2), so O is rarely rescaled.  A row that loses its weights to
 // a larger masked product (their sum below 2^-100), or meets a NaN or an infinity -- a masked weight of 0 times a row of V that holds one, which
-// no entry names, is NaN -- is computed again entry by entry, by the row kernels' code.  Results are thus those of the stored entries alone.
+// no entry names, is NaN -- is computed again entry by entry, by the row kernels' code.  Results are thus those of the stored entries alone, but
+// the reference rounds the exponents' arguments: 2^-18 of a weight at most, with the weight's own rounding to bfloat16 at 2^-8.  (A reference of the
+// stored products alone, found where all products exceed the last one: 7.8 -> 8.6 us for four heads of 256 x 256, 63.8 -> 64.1 for 8 x 4096.)
 #pragma once
 #include <cuda.h>
 
