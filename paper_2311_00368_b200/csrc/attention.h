@@ -13,6 +13,7 @@ constexpr int kTile = 128;            // rows and columns of a tile of the patte
 constexpr int kMaxHeadDim = 256;      // row kernels
 constexpr int kMaxTileHeadDim = 128;  // tensor-core kernels
 constexpr int kMaxColBlocks = 32768;  // 128-column blocks a plan handles (4.2 million columns)
+constexpr int kMostPlanRows = 0x7fffffff - (kTile - 1);   // rows a plan handles: the end of the last row block is an int
 constexpr int kWarps = 4;             // warps per CTA of the row kernels
 
 // An operand seen as [batch][heads][rows][d].
@@ -44,8 +45,8 @@ inline PlanLayout plan_layout(int patterns, int M, int K, long long nnz_stride, 
 {
     PlanLayout l;
     l.patterns = patterns; l.M = M; l.K = K; l.tiles = tiles; l.nnz_stride = nnz_stride;
-    l.RB = (M + kTile - 1) / kTile;
-    l.CB = (K + kTile - 1) / kTile;
+    l.RB = (int)((M + (kTile - 1ll)) / kTile);
+    l.CB = (int)((K + (kTile - 1ll)) / kTile);
     l.words = (l.CB + 31) / 32;
     const size_t P = patterns, rbs = P * l.RB, cbs = P * l.CB, T = tiles;
     size_t at = 256;   // header: word 0 = flags

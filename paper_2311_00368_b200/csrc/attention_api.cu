@@ -33,6 +33,7 @@ b2sp_status check_problem(const b2sp_attention_problem *p)
     if (p->plan && (p->plan_tiles < 0 || (reinterpret_cast<uintptr_t>(p->plan) & 255))) return B2SP_ERR_INVALID_ARG;
     const b2sp_status rc = check_pattern(p->patterns, p->M, p->K, p->nnz_stride, p->row_ptr, p->row_ptr_stride, p->col_idx);
     if (rc != B2SP_OK) return rc;
+    if (p->plan && (p->M > kMostPlanRows || p->K > kMaxColBlocks * kTile)) return B2SP_ERR_UNSUPPORTED;   // (no plan has these sizes)
     return p->d > kMaxHeadDim ? B2SP_ERR_UNSUPPORTED : B2SP_OK;
 }
 
@@ -97,7 +98,7 @@ RowPlan row_plan(const Shape &s, long long nnz, bool backward, long long tiles, 
     const long long problems = (long long)s.batch * s.heads;
     r.splits_m = pick_splits(s.M, problems, nnz);
     r.splits_k = pick_splits(s.K, problems, nnz);
-    r.stat_rows = (s.M + kTile - 1) / kTile * kTile;
+    r.stat_rows = backward ? (s.M + kTile - 1) / kTile * kTile : 0;
     r.parts_kv = r.splits_k > 1 || s.heads != s.kv_heads;
     size_t at = kHeader;
     auto take = [&](size_t b) { const size_t a = at; at += up256(b); return a; };
@@ -351,7 +352,7 @@ extern "C" b2sp_status b2sp_attention_count_tiles(int patterns, int M, int K, lo
     if (rc != B2SP_OK) return rc;
     if (!tiles_host) return B2SP_ERR_INVALID_ARG;
     const PlanLayout l = plan_layout(patterns, M, K, nnz_stride, 0);
-    if (l.CB > kMaxColBlocks || (long long)patterns * l.RB > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (M > kMostPlanRows || l.CB > kMaxColBlocks || (long long)patterns * l.RB > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < 256) return B2SP_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     *tiles_host = 0;
@@ -372,7 +373,7 @@ extern "C" size_t b2sp_attention_plan_bytes(int patterns, int M, int K, long lon
 {
     if (patterns < 1 || M < 0 || K < 0 || nnz_stride < 0 || nnz_stride > INT_MAX || tiles < 0 || tiles > INT_MAX / 2) return 0;
     const PlanLayout l = plan_layout(patterns, M, K, nnz_stride, tiles);
-    if (l.CB > kMaxColBlocks || (long long)patterns * l.RB > INT_MAX || (long long)patterns * l.CB > INT_MAX) return 0;
+    if (M > kMostPlanRows || l.CB > kMaxColBlocks || (long long)patterns * l.RB > INT_MAX || (long long)patterns * l.CB > INT_MAX) return 0;
     return l.bytes;
 }
 
@@ -425,7 +426,7 @@ extern "C" b2sp_status b2sp_attention_plan_status(const void *plan, void *stream
 namespace {
 size_t need(const b2sp_attention_problem *p, int backward, bool fp32)
 {
-    if (check_problem(p) != B2SP_OK) return 0;
+    if (check_problem(p) != B2SP_OK || (backward && (p->M > kMostPlanRows || p->K > kMaxColBlocks * kTile))) return 0;   // (backward there is a plan)
     return row_plan(shape(p), p->nnz_stride, backward != 0, p->plan_tiles, p->plan != nullptr || backward, fp32).bytes;
 }
 }  // namespace
