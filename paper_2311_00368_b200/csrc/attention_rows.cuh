@@ -88,6 +88,12 @@ template <typename T, int V> __device__ __forceinline__ void load4(const T *row,
         for (int k = 0; k < 4; ++k) x[k] = c + k < d ? widen(row[c + k]) : 0.f;
     }
 }
+// The same of partial sums.  They are written by the kernel ahead, which may still run when this one begins: no read-only loads.
+__device__ __forceinline__ void load_part(const float *row, int c, int d, float (&x)[4])
+{
+    const float4 f = c < d ? *reinterpret_cast<const float4 *>(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+}
 template <typename T, int V> __device__ __forceinline__ void store4(T *row, int c, int d, const float (&x)[4])
 {
     if (V == 4) {
@@ -348,7 +354,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_join_kernel(const RowAr
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float y[4];
-                    load4<float, 4>(x + z * half, u * 128 + lane * 4, half, y);
+                    load_part(x + z * half, u * 128 + lane * 4, half, y);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[z][u][k] = fmaf(f, y[k], acc[z][u][k]);
                 }

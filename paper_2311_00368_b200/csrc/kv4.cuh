@@ -868,7 +868,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(const AttnArg
                 if (c <= c1) {
                     const long long unit = part_slot(a, c, c == c0, h);
                     ml[i] = a.part_ml[unit];
-                    attn::load4<float, 4>(a.part + unit * width, lane * 4, width, y[i]);
+                    attn::load_part(a.part + unit * width, lane * 4, width, y[i]);
                 }
             }
             float to = high;
