@@ -441,6 +441,7 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         if (in) lse[row] = live ? fmaf(ref, c2, log2f(l)) * kLn2 : -CUDART_INF_F;
         const unsigned redo = __ballot_sync(~0u, bad);
+        __syncwarp();   // (other lanes write these rows again)
         if (redo && ok) take_rows_again<kForward, DP, Bf16, 4>(a.g, a.g.ptr, a.g.idx, b, h, 1, rb * kTile + warp * 32, redo, a.g.ptr_stride, a.g.idx_stride);
     }
     ptx::tc_fence_before_sync();
