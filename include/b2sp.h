@@ -329,7 +329,7 @@ b2sp_status b2sp_attention_backward_bf16(const b2sp_attention_problem *problem, 
  * slots) is skipped (padding), and of several tokens with one slot the last one's row stays.  Up to 1024 tokens need no workspace.
  * b2sp_kv4_read gives the rows back, rounded once to the output type; slots outside the cache read as zeros.
  * b2sp_attention_kv4: M query tokens, each with its own list of slots: row_ptr[M+1] (from 0), col_idx = slots (each stored one is its own term; those
- * outside the cache are left out), O and lse as for b2sp_attention with lse[M][heads]; Q, O: token i, head h at data + i * ld +
+ * outside the cache are left out, as are entries from nnz on), O and lse as for b2sp_attention with lse[M][heads]; Q, O: token i, head h at data + i * ld +
  * h * stride_head, bfloat16; d <= 128; heads / kv_heads neighbouring query heads share a head of the caches.  A weight times the scale of its
  * value's group is rounded to eleven bits before the second product (weights below 2^-14 of the row's largest: to within 2^-25 of that largest
  * one), whatever the scales; everything else is fp32.

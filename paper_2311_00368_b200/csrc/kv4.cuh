@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(attn::kWarps * 32, 3) kv4_attention_kernel(con
     const int k_ld = (int)a.k.code_ld, v_ld = (int)a.v.code_ld, ks_ld = (int)a.k.scale_ld, vs_ld = (int)a.v.scale_ld;
 
     for (int row = row_of(a.row_ptr, a.M, from0); row < a.M; ++row) {
-        const int first = a.row_ptr[row], last = a.row_ptr[row + 1];
+        const int first = a.row_ptr[row], last = (int)min((long long)a.row_ptr[row + 1], a.nnz);
         if (first >= to0) break;
         const long long begin = max((long long)first, from0), end = min((long long)last, to0);
         if (begin >= end) continue;

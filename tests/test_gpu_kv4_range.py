@@ -144,3 +144,13 @@ def test_scales_that_grow_along_the_list():
     b.kv4_write(k.cuda(), everything, *s.caches[:2])
     b.kv4_write((s.v * 2.0 ** step.view(-1, 1, 1)).cuda(), everything, *s.caches[2:])
     check(s)
+
+
+def test_row_pointers_beyond_the_entries():
+    """Entries that are not there are left out, of the token they would belong to and of those behind."""
+    s = Served(980, [40, 20, 0], 8, 2, 64, 100)
+    want = s.run()
+    for beyond in ([0, 40, 100, 130], [0, 40, 60, 2 ** 31 - 1]):
+        s.row_ptr = torch.tensor(beyond, dtype=torch.int32, device="cuda")
+        got = s.run()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
