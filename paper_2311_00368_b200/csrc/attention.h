@@ -91,10 +91,5 @@ inline Plan plan_view(const void *plan, const PlanLayout &l)
 }
 constexpr int kPlanBadColumn = 1, kPlanDuplicate = 2;   // bits of a plan's flag word
 
-// What b2sp_debug_inject_wait_timeout (b2sp_debug.h) does to the tensor-core kernels.  The limit lies in constant memory of each source file.
-b2sp_status debug_wait_limit(int chunk, unsigned long long limit_ns);
-b2sp_status debug_wait_limit32(unsigned long long limit_ns);
-int drop_chunk();   // the load that is left out, -1: none
-
 }  // namespace attn
 }  // namespace b2sp

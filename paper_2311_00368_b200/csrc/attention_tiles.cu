@@ -26,7 +26,6 @@ TileArgs args(const TileCall &c)
     a.plan = c.plan;
     a.col_ptr = c.plan.col_ptr; a.row_idx = c.plan.row_idx;
     a.status = c.status;
-    a.drop_chunk = drop_chunk();
     return a;
 }
 
@@ -250,17 +249,7 @@ template <class F> b2sp_status staged(TileCall c, bool backward, cudaStream_t st
     return rc == B2SP_OK ? copy<false>(g.out, st, launches) : rc;
 }
 
-std::atomic<int> g_drop_chunk{-1};
-
 }  // namespace
-
-int drop_chunk() { return g_drop_chunk.load(std::memory_order_relaxed); }
-b2sp_status debug_wait_limit(int chunk, unsigned long long limit_ns)
-{
-    if (cudaMemcpyToSymbol(ptx::c_wait_limit_ns, &limit_ns, sizeof(limit_ns)) != cudaSuccess) return B2SP_ERR_CUDA;
-    g_drop_chunk.store(chunk, std::memory_order_relaxed);
-    return debug_wait_limit32(limit_ns);
-}
 
 // Widths up to 128, and a factor that keeps the order of the products (the reference of the exponentials is the largest of them).  Widths in
 // whole 16-byte pieces are read where they lie: every address and stride a multiple of 16 bytes.

@@ -37,7 +37,6 @@ template <typename T> struct TileArgsOf {
     Op q, k, v, dout;
     const int *col_ptr, *row_idx;        // transposed pattern
     int *status;
-    int drop_chunk;      // test hook: the loading warp leaves this one of its CTA's loads out (-1: none), so that waits run out
 };
 using TileArgs = TileArgsOf<Bf16>;
 
@@ -266,9 +265,8 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     auto wait_all = [&](uint32_t bar, uint32_t parity) { return ok = __all_sync(~0u, wait(bar, parity)); };   // of a softmax warp
     if (warp == 4) {
         if (ptx::elect_one()) {
-            int chunk = 0;
             ptx::mbar_arrive_expect_tx(q_full, C::TILE);
-            if (chunk++ != a.drop_chunk) load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
+            load_tile<DP, 128>(base + C::Q, &tm_q, q_full, rb * kTile, h * a.q.hm, b * a.q.bm);
             // K runs ahead of V by the stages that it has more
             constexpr int AHEAD = C::KSTAGES - C::VSTAGES;
             int ik = 0, iv = 0;
@@ -279,13 +277,13 @@ tile_forward_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const int st = ik % C::KSTAGES;
                     if (!wait(k_free(st), (ik / C::KSTAGES & 1) ^ 1)) break;
                     ptx::mbar_arrive_expect_tx(k_full(st), C::HALF);
-                    if (chunk++ != a.drop_chunk) load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at_k, hkv * a.k.hm, b * a.k.bm);
+                    load_tile<DP, 64>(base + C::K + st * C::HALF, &tm_k, k_full(st), at_k, hkv * a.k.hm, b * a.k.bm);
                     if (++ik < steps) at_k = key(ik);
                 } else {
                     const int st = iv % C::VSTAGES;
                     if (!wait(v_free(st), (iv / C::VSTAGES & 1) ^ 1)) break;
                     ptx::mbar_arrive_expect_tx(v_full(st), C::HALF);
-                    if (chunk++ != a.drop_chunk) load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at_v, hkv * a.v.hm, b * a.v.bm);
+                    load_tile<DP, 64>(base + C::V + st * C::HALF, &tm_v, v_full(st), at_v, hkv * a.v.hm, b * a.v.bm);
                     if (++iv < steps) at_v = key(iv);
                 }
             }
@@ -726,7 +724,7 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0, chunk = 0;
+        int i = 0, blocks = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
@@ -737,21 +735,20 @@ tile_grad_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constan
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * C::TILE);
                     const Op &o1 = MODE == kDq ? a.q : a.k, &o2 = MODE == kDq ? a.dout : a.v;
-                    if (chunk != a.drop_chunk) load_tile<DP, 128>(base + C::X1, &tm_x1, x_full, blk * kTile, x * o1.hm, b * o1.bm);
+                    load_tile<DP, 128>(base + C::X1, &tm_x1, x_full, blk * kTile, x * o1.hm, b * o1.bm);
                     load_tile<DP, 128>(base + C::X2, &tm_x2, x_full, blk * kTile, x * o2.hm, b * o2.bm);
                 }
                 __syncwarp();
                 ++blocks;
-                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
+            for (int half = 0; half < 2; ++half, ++i) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     ptx::mbar_arrive_expect_tx(full(st), 2 * C::HALF + C::STAT);
                     const Op &o1 = MODE == kDq ? a.k : a.q, &o2 = MODE == kDq ? a.v : a.dout;
-                    if (chunk != a.drop_chunk) load_tile<DP, 64>(base + C::Y1 + st * C::HALF, &tm_y1, full(st), at, hy * o1.hm, b * o1.bm);
+                    load_tile<DP, 64>(base + C::Y1 + st * C::HALF, &tm_y1, full(st), at, hy * o1.hm, b * o1.bm);
                     load_tile<DP, 64>(base + C::Y2 + st * C::HALF, &tm_y2, full(st), at, hy * o2.hm, b * o2.bm);
                     if (MODE == kDkv) bulk_load(base + C::ST + st * C::STAT, a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride + at, C::STAT, full(st));
                 }

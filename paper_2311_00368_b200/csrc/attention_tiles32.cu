@@ -77,7 +77,6 @@ Args32 args(const Call32 &c, const Plan32 &p, int k)
     f.g.a.plan = c.plan;
     f.g.a.col_ptr = c.plan.col_ptr; f.g.a.row_idx = c.plan.row_idx;
     f.g.a.status = c.status;
-    f.g.a.drop_chunk = drop_chunk();
     f.g.w = tiles_of(c, p, k);
     f.g.tile_at = k == 0 ? c.plan.tile_cb : reinterpret_cast<const int *>(c.plan.ctile);
     f.g.share = p.share[k]; f.g.ctas = p.ctas[k];
@@ -217,11 +216,6 @@ template <bool READ> b2sp_status forward(const Call32 &c, const Plan32 &p, int c
 }
 
 }  // namespace
-
-b2sp_status debug_wait_limit32(unsigned long long limit_ns)
-{
-    return cudaMemcpyToSymbol(ptx::c_wait_limit_ns, &limit_ns, sizeof(limit_ns)) == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA;
-}
 
 // Widths above 64 keep S (and dP) of all tiles in the workspace: up to 2 GB of them.
 bool tiles32_possible(const Shape &s, long long tiles, bool backward)

@@ -165,7 +165,7 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0, chunk = 0;
+        int i = 0, blocks = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
             const bool fresh = w.fresh, last = w.next(g.w);
@@ -174,19 +174,18 @@ tile_product32_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * kPlaneTile);
-                    for (int c = chunk == a.drop_chunk; c < 2; ++c) load_planes<128>(base + C::X + c * kPlaneTile, &tm_x, x_full, c, blk * kTile, h, b);
+                    for (int c = 0; c < 2; ++c) load_planes<128>(base + C::X + c * kPlaneTile, &tm_x, x_full, c, blk * kTile, h, b);
                 }
                 __syncwarp();
                 ++blocks;
-                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
+            for (int half = 0; half < 2; ++half, ++i) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     ptx::mbar_arrive_expect_tx(full(st), 2 * kPlaneHalf);
-                    for (int c = chunk == a.drop_chunk; c < 2; ++c) load_planes<64>(base + C::Y + (2 * st + c) * kPlaneHalf, &tm_y, full(st), c, at, hkv, b);
+                    for (int c = 0; c < 2; ++c) load_planes<64>(base + C::Y + (2 * st + c) * kPlaneHalf, &tm_y, full(st), c, at, hkv, b);
                 }
                 __syncwarp();
             }
@@ -306,7 +305,7 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0, chunk = 0;
+        int i = 0, blocks = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, h = w.o % g.w.outer, hkv = h / (s.heads / s.kv_heads), blk = w.blk, r0 = g.tile_at[w.t] * kTile;
             if (READ) {
@@ -320,20 +319,19 @@ tile_forward32_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, kPlaneTile);
-                    if (chunk != a.drop_chunk) load_planes<128>(base + C::Q, &tm_q, x_full, 0, blk * kTile, h, b);
+                    load_planes<128>(base + C::Q, &tm_q, x_full, 0, blk * kTile, h, b);
                 }
                 __syncwarp();
                 ++blocks;
-                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
+            for (int half = 0; half < 2; ++half, ++i) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     ptx::mbar_arrive_expect_tx(full(st), (READ ? 1 : 2) * kPlaneHalf);
                     if (!READ) load_planes<64>(base + C::K + st * kPlaneHalf, &tm_k, full(st), 0, at, hkv, b);
-                    if (chunk != a.drop_chunk) load_planes<64>(base + C::V + st * kPlaneHalf, &tm_v, full(st), f.col0 / kPlane, at, hkv, b);
+                    load_planes<64>(base + C::V + st * kPlaneHalf, &tm_v, full(st), f.col0 / kPlane, at, hkv, b);
                 }
                 __syncwarp();
             }
@@ -632,7 +630,7 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
     if (warp == TMA_WARP) {
         Walk w;
         w.start(g.w, g.starts[blockIdx.x], tiles);
-        int i = 0, blocks = 0, chunk = 0;
+        int i = 0, blocks = 0;
         for (bool more = tiles > 0; more && ok;) {
             const int b = w.o / g.w.outer, x = w.o % g.w.outer, h = x * g.w.group + w.i, hy = MODE == kDq ? h / (s.heads / s.kv_heads) : h, blk = w.blk;
             const int r0 = (MODE == kDq ? g.tile_at[w.t] : g.tile_at[2 * w.t]) * kTile;
@@ -650,21 +648,20 @@ tile_grad32_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_const
                 if (!wait_all(x_free, (blocks & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::mbar_arrive_expect_tx(x_full, 2 * kPlaneTile);
-                    if (chunk != a.drop_chunk) load_planes<128>(base + C::X1, &tm_x1, x_full, 0, blk * kTile, x, b);
+                    load_planes<128>(base + C::X1, &tm_x1, x_full, 0, blk * kTile, x, b);
                     load_planes<128>(base + C::X2, &tm_x2, x_full, 0, blk * kTile, x, b);
                 }
                 __syncwarp();
                 ++blocks;
-                ++chunk;
             }
-            for (int half = 0; half < 2; ++half, ++i, ++chunk) {
+            for (int half = 0; half < 2; ++half, ++i) {
                 const int st = i % C::STAGES, at = r0 + half * 64;
                 if (!wait_all(free_(st), (i / C::STAGES & 1) ^ 1)) break;
                 if (ptx::elect_one()) {
                     ptx::sts32(flags(st), (fresh && !half ? kStepFirst : 0) | (last && half ? kStepLast : 0));
                     constexpr bool BOTH = !READ || MODE == kDkv;   // (V serves dP alone)
                     ptx::mbar_arrive_expect_tx(full(st), (BOTH ? 2 : 1) * kPlaneHalf + C::STAT);
-                    if (chunk != a.drop_chunk) load_planes<64>(base + C::Y1 + st * kPlaneHalf, &tm_y1, full(st), f.col0 / kPlane, at, hy, b);
+                    load_planes<64>(base + C::Y1 + st * kPlaneHalf, &tm_y1, full(st), f.col0 / kPlane, at, hy, b);
                     if (BOTH) load_planes<64>(base + C::Y2 + st * kPlaneHalf, &tm_y2, full(st), f.col0 / kPlane, at, hy, b);
                     if (MODE == kDkv) bulk_load(base + C::ST + st * C::STAT, a.g.stat + ((long long)b * s.heads + h) * a.g.stat_stride + at, C::STAT, full(st));
                 }
