@@ -216,6 +216,9 @@ def _workspace_need(op, M, K, Kd, N, nnz, algo, setting):
 def _workspace(op, M, K, Kd, N, nnz, device, workspace, algo=0):
     if workspace is None:
         need = _workspace_need(op, M, K, Kd, N, nnz, algo, _planner_setting)
+        if _capturing():   # (as in _scratch: it belongs to the graph)
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            return workspace, need
         key, workspaces = (device.index, _raw_stream(device.index)), _kept.workspaces
         workspace = workspaces.get(key)
         if workspace is None or workspace.numel() < need:

@@ -1,4 +1,5 @@
-"""Workspaces that the binding keeps: one per thread, since the launches of two threads may take turns on one stream."""
+"""Workspaces that the binding keeps: one per thread, since the launches of two threads may take turns on one stream, and none for a call
+that is captured, which gets one of its own."""
 import sys
 import threading
 
@@ -49,6 +50,46 @@ def test_each_thread_has_a_workspace_of_its_own(b, monkeypatch):
             return a
         kept = _in_threads(4, twice)
         assert len({t.data_ptr() for t in kept}) == 4
+
+
+def test_a_captured_call_has_a_workspace_of_its_own(b, monkeypatch):
+    monkeypatch.setattr(b, "_raw_stream", lambda i: 0)
+    cpu = torch.device("cpu")
+    for get in (lambda: b._scratch(5000, cpu, None, 0), lambda: b._workspace(b.OP_SPMM, 64, 64, 0, 64, 100, cpu, None)[0]):
+        monkeypatch.setattr(b, "_capturing", lambda: False)
+        kept = get()
+        monkeypatch.setattr(b, "_capturing", lambda: True)
+        one, other = get(), get()
+        assert len({t.data_ptr() for t in (kept, one, other)}) == 3
+        monkeypatch.setattr(b, "_capturing", lambda: False)
+        assert get().data_ptr() == kept.data_ptr()
+
+
+@pytest.mark.gpu
+def test_two_graphs_of_a_matrix_product(b):
+    """Captured on one stream, replayed at once on two: neither disturbs the other."""
+    from paper_2311_00368_b200 import workloads as W
+    calls, want, graphs, outs = [], [], [], []
+    for i in range(2):
+        p = W.small_random(1030 + i, 2000, 2000, 0.2, 64, 64)
+        rp, ci, A, B, D = (torch.from_numpy(x).cuda() for x in (p.row_ptr, p.col_idx, p.A, p.B, p.D))
+        calls.append(lambda rp=rp, ci=ci, A=A, B=B, D=D: b.fusedmm(rp, ci, None, A, B, D, algo=b.ALGO_TILE))
+        want.append(calls[-1]())
+    torch.cuda.synchronize()
+    for c in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c())
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for x, y in zip(outs, want):
+        assert torch.equal(x, y)
 
 
 @pytest.mark.gpu
