@@ -267,8 +267,8 @@ b2sp_status b2sp_fusedmm_batched_bf16(int batch, int M, int K, int Kd, int N, lo
  *             copied into the workspace).  The weights p (and, backward, p (dp - delta)) are rounded to bfloat16 before the second
  *             products, as the operands are; the row kernels do not round them.
  *   fp32:     d <= 128, any alignment; above 64 the products of the tiles lie in the workspace, 64 KB a tile and problem (backward 128), up to
- *             2 GB of them.  Every number is taken apart into three bfloat16 numbers that add up to it; products keep what is above
- *             2^-23 of each term.
+ *             2 GB of them.  Every number is taken apart into three bfloat16 numbers that add up to it (below about 2^-110 the last one
+ *             loses bits); products keep what is above 2^-23 of each term.
  * B2SP_ERR_UNSUPPORTED otherwise.  B2SP_ALGO_AUTO chooses by the number of entries and tiles.
  * Results do not depend on the order in which anything runs: the same call gives the same bits.
  * workspace: b2sp_attention_workspace_bytes bytes, as for the ops above (b2sp_device_status reads it too).

@@ -625,7 +625,8 @@ def attention(row_ptr, col_idx, q, k, v, scale=None, plan=None, out=None, lse=No
     """b2sp_attention: (O, lse), O = softmax(scale q k^T over the stored positions of each row) v.  q [batch, heads, M, d], k and v
     [batch, kv_heads, K, d] (any strides but the last; heads / kv_heads neighbouring query heads share a k and v), scale d ** -0.5
     unless given; the mask as in attention_plan, whose result goes into `plan`.  O is like q, in `dtype`; lse fp32 [batch, heads, M]
-    (-inf, and a zero row of O, where a row stores nothing).  dtype=torch.bfloat16: b2sp_attention_bf16."""
+    (-inf, and a zero row of O, where a row stores nothing).  The results carry no autograd graph: attention_backward gives the gradients.
+    dtype=torch.bfloat16: b2sp_attention_bf16."""
     sizes, nzs, p = _attention_problem(row_ptr, col_idx, q, k, scale, plan)
     qs, ks, device = q.shape, k.shape, q.device
     hq, hk, hv = _rows(q, qs, dtype, "q"), _rows(k, ks, dtype, "k"), _rows(v, ks, dtype, "v")

@@ -157,7 +157,7 @@ template <int MODE, typename T> b2sp_status launch_rows_v(bool wide, const RowAr
 //     64 x 64 at 30%, one head                        9 and  24    38 and  82
 //     256 x 256 at 29%, 12 heads over 3              31 and 144    42 and 100   (width 120; 119: 43 and 155, 43 and 103)
 //     2048 x 2048 at 2%, 8 heads over 2              74 and 283   228 and 733
-//     4096 x 4096 at 30%, 8 heads                  2752           875
+//     4096 x 4096 at 30%, 8 heads                  2752           751
 //     4096 x 4096, window of 1229, 8 heads over 2         9534            928
 double row_time(const Shape &s, double entries, double in_row, bool backward, bool fp32)
 {
