@@ -356,6 +356,77 @@ b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long 
                                size_t workspace_bytes, void *stream);
 
 /*
+ * A cache of keys or values in pages, in the operands' own type (fp32, or bfloat16 in the _bf16 forms), for serving.
+ *
+ * A cache has `pages` pages of `page` rows for each of kv_heads heads: row r of page c, head h begins at element
+ * c * stride_page + h * stride_head + r * ld of data; data and all strides are multiples of 16 bytes (so rows of any width d are padded to that; what lies
+ * behind d is neither used nor changed).  Request r's position p lies in row p % page of page entries[r * ld + p / page] of its tables (b2sp_page_tables:
+ * requests x width entries); an entry outside [0, pages) stands for no page: nothing is written there, and its positions are left out.
+ * A token i of a call belongs to request rows[i] (rows = NULL: to request i) and sees its first seen[i] positions, as many as the table reaches; a
+ * token whose request is not in [0, requests) sees nothing.  Lengths below 0 count as 0.  All of these numbers are on the device; the host gives sizes only.
+ * Results do not depend on the order in which anything runs.
+ *
+ * b2sp_paged_tables makes a step's tables.  Request r has lengths[r] positions and gets max(added[r], 0) more; added[r] < 0: it ends.
+ *   free_pages, free_room, free_count: a stack of the pages that no request has, free_count (device) of them in free_pages[0 .. free_room).  The pages
+ *     of the requests that end are pushed in order of requests (those beyond free_room are lost), then the pages that are missing are popped and entered
+ *     in the tables, again in order of requests.  Popped pages stay in the array, and entries of requests that end stay in the tables.
+ *   lengths_out[requests]: positions after the step.  row_ptr[requests + 1]: prefix sums of the new tokens (2^31 - 1 at most, as all sums here).
+ *   rows, seen, slots (tokens of each: the step's room): of each new token its request, its position + 1, and its slot, page * (rows of a page) + row, as
+ *     b2sp_kv4_write and b2sp_attention_kv4 count slots.  No page for it: seen = 0, slot = -1.  Behind the last token: -1, 0, -1.
+ *   counts[4]: free pages after the step (the next step's free_count; negative: so many were missing), new tokens, those of them that found no free
+ *     page, no place in their table or none in `tokens`, pages taken.
+ *   Nothing that the call reads is changed but by the pushes: with the old lengths and count a step that did not fit can be made again, and repeating a
+ *   step gives the same.  lengths_out and counts must not lie in lengths or free_count.  At most 8192 requests; pages * page < 2^31.
+ * b2sp_paged_lists gives the slots that tokens see as lists for b2sp_attention_kv4 over caches whose rows are given out by pages: row_ptr[M + 1],
+ *   col_idx[entries]; lists are cut where `entries` end, -1 stands for a missing page and behind the last list.
+ * b2sp_paged_write copies the new rows into the pages: request r's tokens row_ptr[r] .. row_ptr[r + 1] - 1 of K and V (token t, head h at t * ld + h *
+ *   stride_head) become its positions from lengths[r] (BEFORE the step) on.  means (NULL: none): [pages][kv_heads][d], its ld unused; the mean of K's
+ *   rows of every page that gets rows, over those that are filled, is entered there.  Sums in fp32, rounded once.  A page that gets rows must belong to one
+ *   request alone.  At most 8192 requests, d <= 1024.
+ * b2sp_paged_select chooses pages by a score, (sum of the queries of the head's group) . (mean of the page), formed in 64 bits: of the pages that a token
+ *   sees the first `first`, the last `last` and the best others, `keep` in all; of equal scores the lower page; NaN scores last.  lists[M][kv_heads][keep]: ascending
+ *   indices into the request's table, -1 behind the last.  means->page: rows of the cache's pages.  first + last <= keep, d <= 256.
+ * b2sp_attention_paged: O and lse[M][heads] as for b2sp_attention_kv4, of M tokens over the positions that they see, or (lists not NULL, as above; each
+ *   entry is its own term) those of them that lie in the pages named for the token and key head.  Q, O: token i, head h at i * ld + h * stride_head.
+ *   Any M, but made for few tokens with long rows: a row is cut into parts and joined.  d <= 256.
+ */
+typedef struct {
+    void *data; long long ld, stride_head, stride_page;
+    int pages, page;
+} b2sp_pages;
+typedef struct {
+    int *entries; long long ld;
+    int requests, width;
+} b2sp_page_tables;
+b2sp_status b2sp_paged_tables(const b2sp_page_tables *tables, int pages, int page, const int *lengths, const int *added, int *free_pages,
+                              int free_room, const int *free_count, int tokens, int *lengths_out, int *row_ptr, int *rows, int *seen, int *slots,
+                              int *counts, void *stream);
+b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *tables, int pages, int page, const int *rows, const int *seen, long long entries,
+                             int *row_ptr, int *col_idx, void *stream);
+b2sp_status b2sp_paged_write(int tokens, int kv_heads, int d, const float *K, long long ldk, long long stride_head_k, const float *V, long long ldv,
+                             long long stride_head_v, const int *row_ptr, const int *lengths, const b2sp_page_tables *tables,
+                             const b2sp_pages *k_pages, const b2sp_pages *v_pages, const b2sp_pages *means, void *stream);
+b2sp_status b2sp_paged_write_bf16(int tokens, int kv_heads, int d, const void *K, long long ldk, long long stride_head_k, const void *V, long long ldv,
+                                  long long stride_head_v, const int *row_ptr, const int *lengths, const b2sp_page_tables *tables,
+                                  const b2sp_pages *k_pages, const b2sp_pages *v_pages, const b2sp_pages *means, void *stream);
+size_t b2sp_paged_select_workspace_bytes(int M, int kv_heads, int width);   /* 0 on invalid arguments */
+b2sp_status b2sp_paged_select(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long stride_head_q, const b2sp_pages *means,
+                              const b2sp_page_tables *tables, const int *rows, const int *seen, int keep, int first, int last, int *lists,
+                              void *workspace, size_t workspace_bytes, void *stream);
+b2sp_status b2sp_paged_select_bf16(int M, int heads, int kv_heads, int d, const void *Q, long long ldq, long long stride_head_q,
+                                   const b2sp_pages *means, const b2sp_page_tables *tables, const int *rows, const int *seen, int keep, int first, int last,
+                                   int *lists, void *workspace, size_t workspace_bytes, void *stream);
+size_t b2sp_attention_paged_workspace_bytes(int M, int heads, int kv_heads, int d);   /* 0 on invalid arguments; either type */
+b2sp_status b2sp_attention_paged(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long stride_head_q,
+                                 const b2sp_pages *k_pages, const b2sp_pages *v_pages, const b2sp_page_tables *tables, const int *rows, const int *seen,
+                                 const int *lists, int keep, float scale, float *O, long long ldo, long long stride_head_o, float *lse, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+b2sp_status b2sp_attention_paged_bf16(int M, int heads, int kv_heads, int d, const void *Q, long long ldq, long long stride_head_q,
+                                      const b2sp_pages *k_pages, const b2sp_pages *v_pages, const b2sp_page_tables *tables, const int *rows,
+                                      const int *seen, const int *lists, int keep, float scale, void *O, long long ldo, long long stride_head_o,
+                                      float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Host-buffer forms of the three ops: every data pointer is a HOST pointer (pinned memory
  * makes the copies asynchronous and faster, pageable memory also works).  Each call copies
  * its inputs to the device, runs the device entry point above with algo = B2SP_ALGO_AUTO,

@@ -139,6 +139,23 @@ lib.b2sp_attention_kv4_workspace_bytes.argtypes = [_i, _i, _i, _i, _ll]
 lib.b2sp_attention_kv4.restype = _i
 lib.b2sp_attention_kv4.argtypes = [_i, _i, _i, _i, _ll, _vp, _vp, _vp, _ll, _ll, _pk, _pk, ctypes.c_float, _vp, _ll, _ll, _vp, _vp, _sz, _vp]
 
+_PAGES = struct.Struct("Pqqqii").pack                      # b2sp_pages
+_PAGE_TABLES = struct.Struct("Pqii").pack                  # b2sp_page_tables
+lib.b2sp_paged_tables.restype = _i
+lib.b2sp_paged_tables.argtypes = [_vp, _i, _i, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.b2sp_paged_lists.restype = _i
+lib.b2sp_paged_lists.argtypes = [_i, _vp, _i, _i, _vp, _vp, _ll, _vp, _vp, _vp]
+lib.b2sp_paged_select_workspace_bytes.restype = _sz
+lib.b2sp_paged_select_workspace_bytes.argtypes = [_i, _i, _i]
+lib.b2sp_attention_paged_workspace_bytes.restype = _sz
+lib.b2sp_attention_paged_workspace_bytes.argtypes = [_i, _i, _i, _i]
+for _name, _types in (("b2sp_paged_write", [_i, _i, _i, _vp, _ll, _ll, _vp, _ll, _ll, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+                      ("b2sp_paged_select", [_i, _i, _i, _i, _vp, _ll, _ll, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _sz, _vp]),
+                      ("b2sp_attention_paged", [_i, _i, _i, _i, _vp, _ll, _ll, _vp, _vp, _vp, _vp, _vp, _vp, _i, ctypes.c_float, _vp, _ll, _ll,
+                                                _vp, _vp, _sz, _vp])):
+    for _fn in (getattr(lib, _name), getattr(lib, _name + "_bf16")):
+        _fn.restype, _fn.argtypes = _i, _types
+
 
 class B2spError(RuntimeError):
     def __init__(self, status: int, where: str):
@@ -788,4 +805,203 @@ def attention_kv4(row_ptr, col_idx, q, k_codes, k_scales, v_codes, v_scales, sca
     _check(lib.b2sp_attention_kv4(M, H, Hkv, d, nnz, row_ptr.data_ptr(), col_idx.data_ptr(), q.data_ptr(), s[0], s[1], k, v,
                                   d ** -0.5 if scale is None else scale, out.data_ptr(), t[0], t[1], lse.data_ptr(), ws.data_ptr(),
                                   ws.numel(), stream), "b2sp_attention_kv4")
+    return out, lse
+
+
+# ---- a cache of keys or values in pages --------------------------------------------------------------------------------------------
+def paged_cache(pages: int, kv_heads: int, page: int, d: int, dtype=torch.float32, device=None):
+    """[pages, kv_heads, page, d], zeros: a cache of keys or values for paged_write.  Rows lie on multiples of 16 bytes, as the calls
+    need them: [..., :d] of a wider tensor where d is no multiple of that."""
+    wide = -(-d * dtype.itemsize // 16) * 16 // dtype.itemsize
+    return torch.zeros((pages, kv_heads, page, wide), dtype=dtype, device=device or "cuda")[..., :d]
+
+
+def paged_means(pages: int, kv_heads: int, d: int, dtype=torch.float32, device=None):
+    """[pages, kv_heads, d], zeros: room for the mean keys of a cache's pages (see paged_write and paged_select)."""
+    return paged_cache(pages, kv_heads, 1, d, dtype, device)[:, :, 0]
+
+
+def _int32(t, name, shape):
+    if t.dtype is not torch.int32:
+        raise TypeError(f"{name} must be torch.int32")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be {list(shape)}, contiguous")
+    return t.data_ptr()
+
+
+def _page_tables(tables):
+    """[requests, width] as b2sp_page_tables."""
+    if tables.dtype is not torch.int32:
+        raise TypeError("tables must be torch.int32")
+    s = tables.stride()
+    if len(s) != 2 or (s[1] != 1 and tables.shape[1] > 1):
+        raise ValueError("tables must be [requests, width] with neighbouring elements in a row")
+    R, width = tables.shape
+    return _PAGE_TABLES(tables.data_ptr(), s[0], R, width)
+
+
+def _pages(t, dtype, name):
+    """A [pages, kv_heads, page, d] cache as b2sp_pages, and its shape."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    shape, s = t.shape, t.stride()
+    if len(shape) != 4 or (s[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{name} must be [pages, kv_heads, page, d] with neighbouring elements along d")
+    if shape[2] < 1:
+        raise ValueError(f"{name}: pages have at least one row")
+    # (the stride of a dimension of one says nothing; the library wants multiples of 16 bytes)
+    P, H, page, d = shape
+    return _PAGES(t.data_ptr(), s[2] if page > 1 else -(-d // 8) * 8, s[1] if H > 1 else 0, s[0] if P > 1 else 0, P, page), shape
+
+
+def _page_means(t, page, dtype):
+    if t.dtype is not dtype:
+        raise TypeError(f"means must be {dtype}")
+    shape, s = t.shape, t.stride()
+    if len(shape) != 3 or (s[2] != 1 and shape[2] > 1):
+        raise ValueError("means must be [pages, kv_heads, d] with neighbouring elements along d")
+    return _PAGES(t.data_ptr(), 0, s[1] if shape[1] > 1 else 0, s[0] if shape[0] > 1 else 0, shape[0], page), shape
+
+
+def _of_tokens(q, dtype, name):
+    """(M, heads, d), strides of a [M, heads, d] tensor."""
+    if q.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    s = q.stride()
+    if len(s) != 3 or (s[2] != 1 and q.shape[2] > 1):
+        raise ValueError(f"{name} must be [tokens, heads, d] with neighbouring elements along d")
+    return q.shape, s
+
+
+def paged_tables(lengths, added, tables, free_pages, free_count, page, pages, tokens, out=None):
+    """b2sp_paged_tables: (lengths after, row_ptr [requests + 1], rows, seen and slots [tokens], counts [4]) of a step in which request r of
+    lengths[r] positions gets added[r] new ones, or ends (added[r] < 0).  tables [requests, width] gets the pages that are missing, from the stack of free
+    ones: free_count (int32 of one element or more, the first counts) of them in free_pages, to which the pages of the requests that end are added.  pages
+    of `page` rows; tokens: room of the step.  counts[:1] is the next step's free_count; counts[2] > 0: not all fitted (see the header).
+    out: the six tensors, which must not be the inputs."""
+    R, device = tables.shape[0], tables.device
+    t = _page_tables(tables)
+    at = _int32(lengths, "lengths", (R,)), _int32(added, "added", (R,))
+    if free_pages.dtype is not torch.int32 or free_count.dtype is not torch.int32:
+        raise TypeError("free_pages and free_count must be torch.int32")
+    if free_pages.dim() != 1 or not free_pages.is_contiguous() or free_count.numel() < 1:
+        raise ValueError("free_pages must be contiguous, free_count of one element")
+    sizes = (R, R + 1, tokens, tokens, tokens, 4)
+    if out is None:
+        if tokens < 0:
+            raise ValueError("tokens must not be negative")
+        # (one allocation; each part begins on 16 bytes)
+        room = [(n + 3) & ~3 for n in sizes]
+        memory = torch.empty(sum(room), dtype=torch.int32, device=device)
+        out = tuple(part[:n] for part, n in zip(memory.split(room), sizes))
+    names = ("lengths after", "row_ptr", "rows", "seen", "slots", "counts")
+    to = [_int32(x, name, (n,)) for x, name, n in zip(out, names, sizes)]
+    _ready(device, lengths, added, free_pages, free_count, *out)
+    _check(lib.b2sp_paged_tables(t, pages, page, *at, free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(), tokens, *to,
+                                 _raw_stream(device.index)), "b2sp_paged_tables")
+    return tuple(out)
+
+
+def paged_lists(tables, seen, page, pages, entries, rows=None, out=None):
+    """b2sp_paged_lists: (row_ptr [M + 1], col_idx [entries]), the slots that tokens see, as attention_kv4 takes them: token i the first seen[i]
+    positions of request rows[i] (of request i without rows).  Lists are cut at `entries`; -1 for missing pages and behind the last list."""
+    M, device = seen.shape[0], tables.device
+    t = _page_tables(tables)
+    at = None if rows is None else _int32(rows, "rows", (M,)), _int32(seen, "seen", (M,))
+    if out is None:
+        if entries < 0:
+            raise ValueError("entries must not be negative")
+        out = (torch.empty(M + 1, dtype=torch.int32, device=device), torch.empty(entries, dtype=torch.int32, device=device))
+    to = _int32(out[0], "row_ptr", (M + 1,)), _int32(out[1], "col_idx", (entries,))
+    _ready(device, seen, *out, *(() if rows is None else (rows,)))
+    _check(lib.b2sp_paged_lists(M, t, pages, page, *at, entries, *to, _raw_stream(device.index)), "b2sp_paged_lists")
+    return tuple(out)
+
+
+def paged_write(k, v, row_ptr, lengths, tables, k_pages, v_pages, means=None, dtype=torch.float32):
+    """b2sp_paged_write: tokens row_ptr[r] to row_ptr[r + 1] - 1 of k and v [tokens, kv_heads, d] become request r's positions from lengths[r] (before
+    the step) on, in the caches k_pages and v_pages [pages, kv_heads, page, d]; means [pages, kv_heads, d] gets the mean of k's rows of every page
+    that was written to.  Row strides of the caches are multiples of 16 bytes (see paged_cache)."""
+    (T, H, d), s = _of_tokens(k, dtype, "k")
+    shape, z = _of_tokens(v, dtype, "v")
+    kp, a = _pages(k_pages, dtype, "k_pages")
+    vp, b = _pages(v_pages, dtype, "v_pages")
+    if shape != (T, H, d) or a != b or a[1] != H or a[3] != d:
+        raise ValueError("k and v must be [tokens, kv_heads, d], k_pages and v_pages [pages, kv_heads, page, d]")
+    R, device = tables.shape[0], tables.device
+    t, mp = _page_tables(tables), None
+    if means is not None:
+        mp, c = _page_means(means, a[2], dtype)
+        if c != (a[0], H, d):
+            raise ValueError("means must be [pages, kv_heads, d]")
+        _ready(device, means)
+    at = _int32(row_ptr, "row_ptr", (R + 1,)), _int32(lengths, "lengths", (R,))
+    _ready(device, k, v, row_ptr, lengths, k_pages, v_pages)
+    fn, name = (lib.b2sp_paged_write, "b2sp_paged_write") if dtype == torch.float32 else (lib.b2sp_paged_write_bf16, "b2sp_paged_write_bf16")
+    _check(fn(T, H, d, k.data_ptr(), s[0], s[1], v.data_ptr(), z[0], z[1], *at, t, kp, vp, mp, _raw_stream(device.index)), name)
+
+
+def paged_select(q, means, tables, seen, page, keep, first=1, last=1, rows=None, out=None, workspace=None, dtype=torch.float32):
+    """b2sp_paged_select: lists [M, kv_heads, keep] of the pages that suit the tokens q [M, heads, d] best, for attention_paged: of the pages of which
+    token i sees rows the first `first`, the last `last`, and those whose mean key has the largest product with the sum of the group's queries."""
+    (M, H, d), s = _of_tokens(q, dtype, "q")
+    mp, a = _page_means(means, page, dtype)
+    Hkv, device = a[1], q.device
+    if a[2] != d or Hkv < 1 or H % Hkv:
+        raise ValueError("means must be [pages, kv_heads, d], heads a multiple of kv_heads")
+    t = _page_tables(tables)
+    at = None if rows is None else _int32(rows, "rows", (M,)), _int32(seen, "seen", (M,))
+    if out is None:
+        if keep < 1:
+            raise ValueError("keep must be at least 1")
+        out = torch.empty((M, Hkv, keep), dtype=torch.int32, device=device)
+    to = _int32(out, "out", (M, Hkv, keep))
+    _ready(device, means, tables, seen, out, *(() if rows is None else (rows,)))
+    stream = _raw_stream(device.index)
+    ws = _scratch(lib.b2sp_paged_select_workspace_bytes(M, Hkv, tables.shape[1]), device, workspace, stream)
+    fn, name = (lib.b2sp_paged_select, "b2sp_paged_select") if dtype == torch.float32 else (lib.b2sp_paged_select_bf16, "b2sp_paged_select_bf16")
+    _check(fn(M, H, Hkv, d, q.data_ptr(), s[0], s[1], mp, t, *at, keep, first, last, to, ws.data_ptr(), ws.numel(), stream), name)
+    return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _attention_paged_need(M, heads, kv_heads, d):
+    return lib.b2sp_attention_paged_workspace_bytes(M, heads, kv_heads, d)
+
+
+def attention_paged(q, k_pages, v_pages, tables, seen, rows=None, lists=None, scale=None, out=None, lse=None, workspace=None, dtype=torch.float32):
+    """b2sp_attention_paged: (O, lse) of tokens q [M, heads, d] over caches in pages; token i sees the first seen[i] positions of request rows[i]
+    (of request i without rows), or with lists [M, kv_heads, keep] (see paged_select) those of them that lie in the pages listed.  O is like q, lse fp32
+    [M, heads] (-inf, and a zero row of O, where nothing is seen); scale d ** -0.5 unless given."""
+    (M, H, d), s = _of_tokens(q, dtype, "q")
+    kp, a = _pages(k_pages, dtype, "k_pages")
+    vp, b = _pages(v_pages, dtype, "v_pages")
+    Hkv, device = a[1], q.device
+    if a != b or a[3] != d or Hkv < 1 or H % Hkv:
+        raise ValueError("k_pages and v_pages must be [pages, kv_heads, page, d], heads a multiple of kv_heads")
+    t, at_lists, keep = _page_tables(tables), None, 0
+    at = None if rows is None else _int32(rows, "rows", (M,)), _int32(seen, "seen", (M,))
+    others = [k_pages, v_pages, tables, seen]
+    if rows is not None:
+        others.append(rows)
+    if lists is not None:
+        keep = lists.shape[-1]
+        at_lists = _int32(lists, "lists", (M, Hkv, keep))
+        others.append(lists)
+    if out is None:
+        out = torch.empty_like(q) if 0 not in s else torch.empty((M, H, d), dtype=dtype, device=device)
+    z = out.stride()
+    if out.dtype is not dtype or out.shape != (M, H, d) or (d > 1 and z[2] != 1):
+        raise ValueError("out must be like q, with neighbouring elements along d")
+    if lse is None:
+        lse = torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=device)
+    else:
+        _lse(lse, (M, H))
+    _ready(device, out, lse, *others)
+    stream = _raw_stream(device.index)
+    ws = _scratch(_attention_paged_need(M, H, Hkv, d), device, workspace, stream)
+    fn, name = ((lib.b2sp_attention_paged, "b2sp_attention_paged") if dtype == torch.float32
+                else (lib.b2sp_attention_paged_bf16, "b2sp_attention_paged_bf16"))
+    _check(fn(M, H, Hkv, d, q.data_ptr(), s[0], s[1], kp, vp, t, *at, at_lists, keep, d ** -0.5 if scale is None else scale, out.data_ptr(), z[0], z[1],
+              lse.data_ptr(), ws.data_ptr(), ws.numel(), stream), name)
     return out, lse

@@ -13,6 +13,7 @@
 #include <type_traits>
 
 #include "attention_rows.cuh"
+#include "div.h"
 
 namespace b2sp {
 namespace kv4 {
@@ -24,18 +25,6 @@ struct Cache {
     Bf16 *scales;        // scales + h * scale_head + slot * scale_ld, elements
     long long code_ld, code_head, scale_ld, scale_head;
     int slots;
-};
-
-// n / d for 0 <= n < 2^31 by one multiplication (Granlund and Montgomery's round-up method).
-struct Div {
-    unsigned d, m, s;
-    Div() = default;
-    explicit Div(unsigned d_) : d(d_), s(0)
-    {
-        while ((1ull << s) < d) ++s;
-        m = (unsigned)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
-    }
-    __device__ __forceinline__ unsigned operator()(unsigned n) const { return (__umulhi(n, m) + n) >> s; }
 };
 
 // i * a + j * b

@@ -1,0 +1,257 @@
+// Entry points of the cache in pages: argument checks and launches.  See include/b2sp.h.
+#include <algorithm>
+#include <climits>
+
+#include "paged_attention.cuh"
+
+namespace b2sp {
+namespace paged {
+
+inline b2sp_status launched() { return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA; }
+constexpr int kSMs = 148;
+
+// Kernels that hold prefix sums over the requests in more shared memory than a launch gets unasked (at the most requests; once per device would do).
+template <typename K> bool allow_shared(K *kernel, size_t bytes)
+{
+    return bytes <= 48 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+}
+
+b2sp_status check_tables(const b2sp_page_tables *t, int page)
+{
+    if (!t || t->requests < 0 || t->width < 0 || t->ld < 0 || page < 1) return B2SP_ERR_INVALID_ARG;
+    if (t->requests && t->width && !t->entries) return B2SP_ERR_INVALID_ARG;
+    return B2SP_OK;
+}
+Tables tables(const b2sp_page_tables *t) { return Tables{t->entries, t->ld, t->requests, t->width}; }
+
+// rows: rows of a page (a cache) or 1 (means: ld is not looked at).
+template <typename T> b2sp_status check_pages(const b2sp_pages *c, int heads, int d, int rows)
+{
+    if (!c || c->pages < 0 || c->page < 1 || c->ld < 0 || c->stride_head < 0 || c->stride_page < 0) return B2SP_ERR_INVALID_ARG;
+    if (c->pages && !c->data) return B2SP_ERR_INVALID_ARG;
+    const uintptr_t strides = (rows > 1 ? (uintptr_t)c->ld : 0) | (uintptr_t)c->stride_head | (uintptr_t)c->stride_page;
+    if ((reinterpret_cast<uintptr_t>(c->data) | strides * sizeof(T)) & 15) return B2SP_ERR_INVALID_ARG;
+    if (rows > 1 && c->ld < d) return B2SP_ERR_INVALID_ARG;
+    return B2SP_OK;
+}
+// What is written must not overlap: sorted by stride, each dimension's stride is at least the extent of those within it.
+bool apart(int d, std::initializer_list<std::pair<long long, long long>> dims)   // (size, stride)
+{
+    std::pair<long long, long long> v[3];
+    int n = 0;
+    for (const auto &x : dims)
+        if (x.first > 1) v[n++] = x;
+    std::sort(v, v + n, [](const auto &x, const auto &y) { return x.second < y.second; });
+    __int128 extent = d;
+    for (int i = 0; i < n; ++i) {
+        if (v[i].second < extent) return false;
+        extent += (__int128)(v[i].first - 1) * v[i].second;
+    }
+    return true;
+}
+template <typename T> Pages<T> pages(const b2sp_pages *c) { return Pages<T>{static_cast<T *>(c->data), c->ld, c->stride_head, c->stride_page, c->pages}; }
+bool same_slots(const b2sp_pages *a, const b2sp_pages *b) { return a->pages == b->pages && a->page == b->page; }
+bool meet(const void *a, size_t an, const void *b, size_t bn)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return an && bn && x < y + bn && y < x + an;
+}
+
+template <typename T>
+b2sp_status write(int tokens, int heads, int d, const T *K, long long ldk, long long shk, const T *V, long long ldv, long long shv, const int *row_ptr,
+                  const int *lengths, const b2sp_page_tables *t, const b2sp_pages *kp, const b2sp_pages *vp, const b2sp_pages *means, void *stream)
+{
+    if (tokens < 0 || heads < 1 || d < 1 || ldk < 0 || shk < 0 || ldv < 0 || shv < 0) return B2SP_ERR_INVALID_ARG;
+    b2sp_status rc = check_pages<T>(kp, heads, d, 2);
+    if (rc == B2SP_OK) rc = check_pages<T>(vp, heads, d, 2);
+    if (rc == B2SP_OK && means) rc = check_pages<T>(means, heads, d, 1);
+    if (rc == B2SP_OK) rc = check_tables(t, kp->page);
+    if (rc != B2SP_OK) return rc;
+    if (!same_slots(kp, vp) || (means && means->pages != kp->pages)) return B2SP_ERR_INVALID_ARG;
+    for (const b2sp_pages *c : {kp, vp})
+        if (!apart(d, {{c->pages, c->stride_page}, {heads, c->stride_head}, {c->page, c->ld}})) return B2SP_ERR_INVALID_ARG;
+    if (means && !apart(d, {{means->pages, means->stride_page}, {heads, means->stride_head}})) return B2SP_ERR_INVALID_ARG;
+    if (t->requests && (!row_ptr || !lengths)) return B2SP_ERR_INVALID_ARG;
+    if (tokens && (!K || !V)) return B2SP_ERR_INVALID_ARG;
+    if (t->requests > kMostRequests || d > 1024) return B2SP_ERR_UNSUPPORTED;
+    if (tokens == 0 || t->requests == 0 || kp->pages == 0) return B2SP_OK;
+    WriteArgs<T> a = {};
+    a.t = tables(t);
+    a.k = K; a.v = V; a.k_ld = ldk; a.k_sh = shk; a.v_ld = ldv; a.v_sh = shv;
+    a.heads = heads; a.d = d; a.page = kp->page; a.tokens = tokens; a.row_ptr = row_ptr; a.lengths = lengths;
+    a.kp = pages<T>(kp); a.vp = pages<T>(vp);
+    if (means) a.means = pages<T>(means);
+    // as many pages as the tokens can touch: at most two that are not full for each request that has any
+    const long long units = (tokens / kp->page + 2ll * std::min(t->requests, tokens)) * heads;
+    const unsigned blocks = (unsigned)std::min(units, 16ll * kSMs);
+    const size_t shared = (t->requests + 1) * sizeof(int);
+    paged_write_kernel<T><<<blocks, kWriteThreads, shared, static_cast<cudaStream_t>(stream)>>>(a);
+    return launched();
+}
+
+bool token_args_ok(int M, int heads, int kv_heads, int d) { return M >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1; }
+
+size_t select_bytes(int M, int kv_heads, int width) { return std::max<size_t>(256, attn::up256((size_t)M * kv_heads * width * 8)); }
+
+template <typename T>
+b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long ldq, long long shq, const b2sp_pages *means, const b2sp_page_tables *t,
+                   const int *rows, const int *seen, int keep, int first, int last, int *lists, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!token_args_ok(M, heads, kv_heads, d) || ldq < 0 || shq < 0 || keep < 1 || first < 0 || last < 0 || first > keep - last) return B2SP_ERR_INVALID_ARG;
+    b2sp_status rc = check_pages<T>(means, kv_heads, d, 1);
+    if (rc == B2SP_OK) rc = check_tables(t, means->page);
+    if (rc != B2SP_OK) return rc;
+    if (M && (!Q || !seen || !lists)) return B2SP_ERR_INVALID_ARG;
+    if (d > 256) return B2SP_ERR_UNSUPPORTED;
+    const long long units = (long long)M * kv_heads * ((t->width + kScorePages - 1) / kScorePages), ctas = (long long)M * kv_heads;
+    if (ctas > INT_MAX || (units + 7) / 8 > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
+    if (M == 0) return B2SP_OK;
+    SelectArgs<T> a = {};
+    a.t = tables(t);
+    a.tok = Tokens{rows, seen};
+    a.q = Q; a.q_ld = ldq; a.q_sh = shq;
+    a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.page = means->page; a.keep = keep; a.first = first; a.last = last;
+    a.means = pages<T>(means);
+    a.keys = static_cast<unsigned long long *>(workspace);
+    a.lists = lists;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (t->width > keep) {
+        paged_score_kernel<T><<<(unsigned)((units + 7) / 8), kThreads, 0, st>>>(a);
+        attn::launch_behind(paged_select_kernel<T>, (unsigned)ctas, kThreads, st, a);
+    } else {
+        paged_select_kernel<T><<<(unsigned)ctas, kThreads, 0, st>>>(a);   // no more pages than a list holds
+    }
+    return launched();
+}
+
+size_t attention_bytes(int M, int heads, int kv_heads, int d) { return 256; }
+
+template <typename T>
+b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long long ldq, long long shq, const b2sp_pages *kp, const b2sp_pages *vp,
+                      const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists, int keep, float scale, T *O, long long ldo,
+                      long long sho, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!token_args_ok(M, heads, kv_heads, d) || ldq < 0 || shq < 0 || ldo < 0 || sho < 0 || !(scale == scale) || (lists && keep < 1)) return B2SP_ERR_INVALID_ARG;
+    b2sp_status rc = check_pages<T>(kp, kv_heads, d, 2);
+    if (rc == B2SP_OK) rc = check_pages<T>(vp, kv_heads, d, 2);
+    if (rc == B2SP_OK) rc = check_tables(t, kp->page);
+    if (rc != B2SP_OK) return rc;
+    if (!same_slots(kp, vp)) return B2SP_ERR_INVALID_ARG;
+    if (M && (!Q || !O || !lse || !seen)) return B2SP_ERR_INVALID_ARG;
+    if (!apart(d, {{M, ldo}, {heads, sho}})) return B2SP_ERR_INVALID_ARG;
+    if (d > 256 || (lists && (long long)keep * kp->page > INT_MAX) || (long long)M * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < attention_bytes(M, heads, kv_heads, d)) return B2SP_ERR_WORKSPACE;
+    if (M == 0) return B2SP_OK;
+    AttnArgs<T> a = {};
+    a.t = tables(t);
+    a.tok = Tokens{rows, seen};
+    a.q = Q; a.q_ld = ldq; a.q_sh = shq;
+    a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.page = kp->page;
+    a.k = pages<T>(kp); a.v = pages<T>(vp);
+    a.lists = lists; a.keep = lists ? keep : 0; a.scale = scale;
+    a.out = O; a.out_ld = ldo; a.out_sh = sho; a.lse = lse;
+    paged_attention_kernel<T><<<(unsigned)(M * heads), kAttnWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    return launched();
+}
+
+}  // namespace paged
+}  // namespace b2sp
+
+using namespace b2sp;
+using namespace b2sp::paged;
+
+extern "C" b2sp_status b2sp_paged_tables(const b2sp_page_tables *t, int pages, int page, const int *lengths, const int *added, int *free_pages,
+                                         int free_room, const int *free_count, int tokens, int *lengths_out, int *row_ptr, int *rows, int *seen,
+                                         int *slots, int *counts, void *stream)
+{
+    b2sp_status rc = check_tables(t, page);
+    if (rc != B2SP_OK) return rc;
+    const int R = t->requests;
+    if (pages < 0 || free_room < 0 || tokens < 0 || (R > 1 && t->ld < t->width)) return B2SP_ERR_INVALID_ARG;
+    if (!row_ptr || !counts || !free_count || (R && (!lengths || !added || !lengths_out)) || (free_room && !free_pages)) return B2SP_ERR_INVALID_ARG;
+    if (tokens && (!rows || !seen || !slots)) return B2SP_ERR_INVALID_ARG;
+    if (meet(lengths, 4ull * R, lengths_out, 4ull * R) || meet(counts, 16, free_count, 4)) return B2SP_ERR_INVALID_ARG;   // CTAs read the one while others write the other
+    if (R > kMostRequests || (long long)pages * page > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    const size_t shared = 3 * (R + 1) * sizeof(int);
+    if (!allow_shared(paged_tables_kernel, shared)) return B2SP_ERR_CUDA;
+    TablesArgs a = {};
+    a.t = tables(t);
+    a.page = page; a.pages = pages; a.tokens = tokens; a.free_room = free_room;
+    a.lengths = lengths; a.added = added; a.free_count = free_count; a.free_pages = free_pages;
+    a.lengths_out = lengths_out; a.row_ptr = row_ptr; a.rows = rows; a.seen = seen; a.slots = slots; a.counts = counts;
+    const unsigned blocks = (unsigned)std::min(std::max(((long long)std::max(tokens, R) + kThreads - 1) / kThreads, 1ll), 2ll * kSMs);
+    paged_tables_kernel<<<blocks, kThreads, shared, static_cast<cudaStream_t>(stream)>>>(a);
+    return launched();
+}
+
+extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pages, int page, const int *rows, const int *seen, long long entries,
+                                        int *row_ptr, int *col_idx, void *stream)
+{
+    b2sp_status rc = check_tables(t, page);
+    if (rc != B2SP_OK) return rc;
+    if (M < 0 || pages < 0 || entries < 0 || !row_ptr || (M && !seen) || (entries && !col_idx)) return B2SP_ERR_INVALID_ARG;
+    if (entries > INT_MAX || (long long)pages * page > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    ListsArgs a = {};
+    a.t = tables(t);
+    a.tok = Tokens{rows, seen};
+    a.M = M; a.page = page; a.pages = pages; a.entries = entries; a.row_ptr = row_ptr; a.col_idx = col_idx; a.by_page = Div(page);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    paged_list_ends_kernel<<<1, kScanThreads, 0, st>>>(a);
+    constexpr long long share = (long long)kListShare * (kThreads / 32);
+    if (entries) attn::launch_behind(paged_list_kernel, (unsigned)((entries + share - 1) / share), kThreads, st, a);
+    return launched();
+}
+
+extern "C" b2sp_status b2sp_paged_write(int tokens, int heads, int d, const float *K, long long ldk, long long shk, const float *V, long long ldv,
+                                        long long shv, const int *row_ptr, const int *lengths, const b2sp_page_tables *t, const b2sp_pages *kp,
+                                        const b2sp_pages *vp, const b2sp_pages *means, void *stream)
+{
+    return write<float>(tokens, heads, d, K, ldk, shk, V, ldv, shv, row_ptr, lengths, t, kp, vp, means, stream);
+}
+extern "C" b2sp_status b2sp_paged_write_bf16(int tokens, int heads, int d, const void *K, long long ldk, long long shk, const void *V, long long ldv,
+                                             long long shv, const int *row_ptr, const int *lengths, const b2sp_page_tables *t, const b2sp_pages *kp,
+                                             const b2sp_pages *vp, const b2sp_pages *means, void *stream)
+{
+    return write<Bf16>(tokens, heads, d, static_cast<const Bf16 *>(K), ldk, shk, static_cast<const Bf16 *>(V), ldv, shv, row_ptr, lengths, t, kp, vp,
+                       means, stream);
+}
+
+extern "C" size_t b2sp_paged_select_workspace_bytes(int M, int kv_heads, int width)
+{
+    return M < 0 || kv_heads < 1 || width < 0 ? 0 : select_bytes(M, kv_heads, width);
+}
+extern "C" b2sp_status b2sp_paged_select(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long shq, const b2sp_pages *means,
+                                         const b2sp_page_tables *t, const int *rows, const int *seen, int keep, int first, int last, int *lists,
+                                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    return paged::select<float>(M, heads, kv_heads, d, Q, ldq, shq, means, t, rows, seen, keep, first, last, lists, workspace, workspace_bytes, stream);
+}
+extern "C" b2sp_status b2sp_paged_select_bf16(int M, int heads, int kv_heads, int d, const void *Q, long long ldq, long long shq, const b2sp_pages *means,
+                                              const b2sp_page_tables *t, const int *rows, const int *seen, int keep, int first, int last, int *lists,
+                                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    return paged::select<Bf16>(M, heads, kv_heads, d, static_cast<const Bf16 *>(Q), ldq, shq, means, t, rows, seen, keep, first, last, lists, workspace,
+                               workspace_bytes, stream);
+}
+
+extern "C" size_t b2sp_attention_paged_workspace_bytes(int M, int heads, int kv_heads, int d)
+{
+    return token_args_ok(M, heads, kv_heads, d) && d <= 256 ? attention_bytes(M, heads, kv_heads, d) : 0;
+}
+extern "C" b2sp_status b2sp_attention_paged(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long shq, const b2sp_pages *kp,
+                                            const b2sp_pages *vp, const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists, int keep,
+                                            float scale, float *O, long long ldo, long long sho, float *lse, void *workspace, size_t workspace_bytes,
+                                            void *stream)
+{
+    return attention<float>(M, heads, kv_heads, d, Q, ldq, shq, kp, vp, t, rows, seen, lists, keep, scale, O, ldo, sho, lse, workspace, workspace_bytes,
+                            stream);
+}
+extern "C" b2sp_status b2sp_attention_paged_bf16(int M, int heads, int kv_heads, int d, const void *Q, long long ldq, long long shq, const b2sp_pages *kp,
+                                                 const b2sp_pages *vp, const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists,
+                                                 int keep, float scale, void *O, long long ldo, long long sho, float *lse, void *workspace,
+                                                 size_t workspace_bytes, void *stream)
+{
+    return attention<Bf16>(M, heads, kv_heads, d, static_cast<const Bf16 *>(Q), ldq, shq, kp, vp, t, rows, seen, lists, keep, scale,
+                           static_cast<Bf16 *>(O), ldo, sho, lse, workspace, workspace_bytes, stream);
+}
