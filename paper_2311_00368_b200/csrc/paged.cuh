@@ -469,8 +469,8 @@ __global__ void __launch_bounds__(kThreads) paged_select_kernel(const SelectArgs
     int *list = a.lists + (long long)blockIdx.x * a.keep;
     for (int p = threadIdx.x; p < a.keep; p += kThreads)
         if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // (by all CTAs: what comes behind this launch counts on the one ahead of it)
     if (n <= a.keep) return;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.t.width;
     const int each = (n + kThreads - 1) / kThreads, p0 = (int)min((long long)n, threadIdx.x * (long long)each), mine = min(n - p0, each);
     const auto key = [&](int p) { return p < a.first || p >= n - a.last ? ~0ull : keys[p]; };

@@ -10,10 +10,10 @@ namespace paged {
 inline b2sp_status launched() { return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA; }
 constexpr int kSMs = 148;
 
-// Kernels that hold prefix sums over the requests in more shared memory than a launch gets unasked (at the most requests; once per device would do).
+// More shared memory than a launch gets unasked (48 KB with what the kernel has of its own).
 template <typename K> bool allow_shared(K *kernel, size_t bytes)
 {
-    return bytes <= 48 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    return bytes <= 40 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 
 b2sp_status check_tables(const b2sp_page_tables *t, int page)
@@ -125,7 +125,56 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     return launched();
 }
 
-size_t attention_bytes(int M, int heads, int kv_heads, int d) { return 256; }
+// Warps and workspace of an attention call.
+struct AttnPlan {
+    int nt, heads_of_unit, blocks, warps;   // nt: eights of heads of a unit; blocks: units of a token and key head; warps: at most
+    size_t ml, part, bytes;
+};
+template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d)
+{
+    AttnPlan p;
+    const int group = heads / kv_heads, w = d <= 64 ? 64 : d <= 128 ? 128 : 256;
+    p.nt = sizeof(T) == 2 && group > 8 ? 2 : 1;
+    p.heads_of_unit = 8 * p.nt;
+    p.blocks = (group + p.heads_of_unit - 1) / p.heads_of_unit;
+    p.warps = kSMs * kAttnWarps * (w == 64 ? Form<T, 64>::CTAS : w == 128 ? Form<T, 128>::CTAS : Form<T, 256>::CTAS);
+    const size_t parts = 2ull * p.warps * p.heads_of_unit;
+    p.ml = attn::up256(p.warps * sizeof(int4));
+    p.part = p.ml + attn::up256(parts * sizeof(float2));
+    p.bytes = p.part + attn::up256(parts * w * sizeof(float));
+    return p;
+}
+
+// A launch that may begin before the one ahead of it has ended (the kernels wait for that themselves).
+template <typename K, typename... Args> bool launch_early(K *kernel, dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
+{
+    if (!allow_shared(kernel, shared)) return false;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = blocks;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+}
+
+template <typename T, int W, int NT> b2sp_status launch_attention(AttnArgs<T> &a, const AttnPlan &p, long long most_tiles, cudaStream_t st)
+{
+    using F = Form<T, W>;
+    const long long units = (long long)a.M * a.kv_heads * a.blocks;
+    // no more CTAs than have a share, if every token sees all that it can
+    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_tiles + kLeastTiles * kAttnWarps - 1) / (kLeastTiles * kAttnWarps));
+    a.by_unit = units <= ctas * (long long)kAttnWarps;
+    const bool ok = a.page % F::ROWS == 0 ? launch_early(paged_attention_kernel<T, W, NT, true>, ctas, kAttnWarps * 32, F::SHARED, st, a)
+                                          : launch_early(paged_attention_kernel<T, W, NT, false>, ctas, kAttnWarps * 32, F::SHARED, st, a);
+    const unsigned joins = a.by_unit ? (unsigned)units : ctas * kAttnWarps;
+    if (!ok || !launch_early(paged_join_kernel<T, W>, dim3(joins, std::min(a.group, p.heads_of_unit)), kJoinWarps * 32, 0, st, a, p.heads_of_unit)) return B2SP_ERR_CUDA;
+    return launched();
+}
 
 template <typename T>
 b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long long ldq, long long shq, const b2sp_pages *kp, const b2sp_pages *vp,
@@ -141,7 +190,9 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     if (M && (!Q || !O || !lse || !seen)) return B2SP_ERR_INVALID_ARG;
     if (!apart(d, {{M, ldo}, {heads, sho}})) return B2SP_ERR_INVALID_ARG;
     if (d > 256 || (lists && (long long)keep * kp->page > INT_MAX) || (long long)M * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < attention_bytes(M, heads, kv_heads, d)) return B2SP_ERR_WORKSPACE;
+    const AttnPlan p = attention_plan<T>(heads, kv_heads, d);
+    if ((long long)M * kv_heads * p.blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
     AttnArgs<T> a = {};
     a.t = tables(t);
@@ -151,8 +202,24 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     a.k = pages<T>(kp); a.v = pages<T>(vp);
     a.lists = lists; a.keep = lists ? keep : 0; a.scale = scale;
     a.out = O; a.out_ld = ldo; a.out_sh = sho; a.lse = lse;
-    paged_attention_kernel<T><<<(unsigned)(M * heads), kAttnWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return launched();
+    const auto fits = [](const void *x, long long ld, long long sh, size_t bytes) {
+        return ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(ld * (long long)sizeof(T)) | (uintptr_t)(sh * (long long)sizeof(T))) & (bytes - 1)) == 0;
+    };
+    a.group = heads / kv_heads; a.blocks = p.blocks; a.by_page = Div(a.page);
+    a.q_pairs = fits(Q, ldq, shq, 4); a.q_fours = fits(Q, ldq, shq, 16); a.out_pairs = fits(O, ldo, sho, 4);
+    char *ws = static_cast<char *>(workspace);
+    a.joins = reinterpret_cast<int4 *>(ws);
+    a.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
+    a.part = reinterpret_cast<float *>(ws + p.part);
+    const long long most_rows = lists ? (long long)keep * a.page : (long long)t->width * a.page, units = (long long)M * kv_heads * p.blocks;
+    const __int128 tiles = (__int128)units * std::max(1ll, (most_rows + 7) / 8);
+    const long long most = (long long)std::min<__int128>(tiles, 1ll << 40);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int w = d <= 64 ? 64 : d <= 128 ? 128 : 256;
+    if constexpr (sizeof(T) == 2) {
+        if (p.nt == 2) return w == 64 ? launch_attention<T, 64, 2>(a, p, most, st) : w == 128 ? launch_attention<T, 128, 2>(a, p, most, st) : launch_attention<T, 256, 2>(a, p, most, st);
+    }
+    return w == 64 ? launch_attention<T, 64, 1>(a, p, most, st) : w == 128 ? launch_attention<T, 128, 1>(a, p, most, st) : launch_attention<T, 256, 1>(a, p, most, st);
 }
 
 }  // namespace paged
@@ -237,7 +304,8 @@ extern "C" b2sp_status b2sp_paged_select_bf16(int M, int heads, int kv_heads, in
 
 extern "C" size_t b2sp_attention_paged_workspace_bytes(int M, int heads, int kv_heads, int d)
 {
-    return token_args_ok(M, heads, kv_heads, d) && d <= 256 ? attention_bytes(M, heads, kv_heads, d) : 0;
+    if (!token_args_ok(M, heads, kv_heads, d) || d > 256) return 0;
+    return std::max(attention_plan<float>(heads, kv_heads, d).bytes, attention_plan<Bf16>(heads, kv_heads, d).bytes);
 }
 extern "C" b2sp_status b2sp_attention_paged(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long shq, const b2sp_pages *kp,
                                             const b2sp_pages *vp, const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists, int keep,
