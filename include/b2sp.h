@@ -388,7 +388,8 @@ b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long 
  *   indices into the request's table, -1 behind the last.  means->page: rows of the cache's pages.  first + last <= keep, d <= 256.
  * b2sp_attention_paged: O and lse[M][heads] as for b2sp_attention_kv4, of M tokens over the positions that they see, or (lists not NULL, as above; each
  *   entry is its own term) those of them that lie in the pages named for the token and key head.  Q, O: token i, head h at i * ld + h * stride_head.
- *   Any M, but made for few tokens with long rows: a row is cut into parts and joined.  d <= 256.
+ *   Any M, but made for few tokens with long rows: a row is cut into parts and joined; neighbouring tokens of one request read its rows together.  d <= 256;
+ *   strides below 2^32 bytes.
  */
 typedef struct {
     void *data; long long ld, stride_head, stride_page;

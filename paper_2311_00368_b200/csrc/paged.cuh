@@ -77,6 +77,50 @@ __device__ __forceinline__ long long block_before(long long x, long long *warps,
     }
     return before + up - x;
 }
+// Tokens' costs in a line, dealt to `parts` warps in equal shares of at least `least`: what warp `me` has.
+struct Share {
+    long long lo, hi, share, rest;   // [lo, hi) of the line; every warp's share; lo is `rest` behind the begin of token `row`
+    int row;
+};
+// False: nothing.  All threads call it.
+template <int THREADS, typename Cost> __device__ __forceinline__ bool deal(int M, Cost cost, int parts, int me, int least, Share &s)
+{
+    __shared__ long long before[THREADS], warps[THREADS / 32];
+    const int lane = threadIdx.x & 31, each = (M + THREADS - 1) / THREADS;
+    const int i0 = (int)min((long long)M, threadIdx.x * (long long)each), i1 = min(M, i0 + each);
+    long long n = 0, all;
+    for (int i = i0; i < i1; ++i) n += cost(i);
+    before[threadIdx.x] = block_before(n, warps, all);
+    s.share = max((all + parts - 1) / parts, (long long)least);
+    s.lo = me * s.share;
+    s.hi = min(s.lo + s.share, all);
+    __syncthreads();
+    if (s.lo >= s.hi) return false;
+    int chunk = -1;   // the thread that summed the token which lo lies in
+#pragma unroll
+    for (int j = 0; j < THREADS / 32; ++j) chunk += __popc(__ballot_sync(~0u, before[j * 32 + lane] <= s.lo));
+    s.rest = s.lo - before[chunk];
+    s.row = chunk * each;
+    if (each == 1) return true;
+    for (; s.row < M; s.row += 32) {   // 32 tokens at a time
+        const long long c = s.row + lane < M ? cost(s.row + lane) : 0;
+        long long up = c;
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) {
+            const long long y = __shfl_up_sync(~0u, up, w);
+            if (lane >= w) up += y;
+        }
+        const unsigned behind = __ballot_sync(~0u, up > s.rest);
+        if (behind) {
+            const int k = __ffs(behind) - 1;
+            s.rest -= __shfl_sync(~0u, up - c, k);
+            s.row += k;
+            return true;
+        }
+        s.rest -= __shfl_sync(~0u, up, 31);
+    }
+    return false;   // (not with lengths that stay as they are)
+}
 // The last r in [0, n) with ptr[r] <= x < ptr[r + 1]; ptr[0] = 0 <= x < ptr[n].
 __device__ __forceinline__ int segment_of(const int *ptr, int n, int x)
 {
@@ -402,6 +446,7 @@ template <typename T> struct SelectArgs {
     const T *q;
     long long q_ld, q_sh;
     int M, heads, kv_heads, d, page, keep, first, last;
+    bool q_wide;                // 16-byte loads of q
     Pages<T> means;
     unsigned long long *keys;   // [M][kv_heads][width]
     int *lists;                 // [M][kv_heads][keep]
@@ -418,113 +463,210 @@ __device__ __forceinline__ unsigned long long ordered(double x)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// Scores: a warp per 32 pages of a token and key head, the sum of the group's queries in its lanes.  Sums are formed in 64 bits: the result is a
-// choice, and between two close scores sums of 32 bits would choose by their order.
+// Scores of the pages of tokens that see more than a list holds.  Sums are formed in 64 bits: the result is a choice, and between two close scores sums of
+// 32 bits would choose by their order.  The blocks of 32 pages of all tokens and key heads are dealt to the warps in equal shares; the sum of the group's
+// queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, eight instructions at a time.
 constexpr int kScorePages = 32;
-template <typename T>
+template <typename T, int LANES, int HALVES>
 __global__ void __launch_bounds__(kThreads) paged_score_kernel(const SelectArgs<T> a)
 {
-    const int lane = threadIdx.x & 31, blocks = (a.t.width + kScorePages - 1) / kScorePages;
-    const long long unit = blockIdx.x * (long long)(kThreads / 32) + (threadIdx.x >> 5);
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (unit >= (long long)a.M * a.kv_heads * blocks) return;
-    const int b = (int)(unit % blocks), g = (int)(unit / blocks % a.kv_heads), i = (int)(unit / blocks / a.kv_heads);
-    const int n = pages_seen(a, i), p0 = b * kScorePages, p1 = min(n, p0 + kScorePages);
-    if (n <= a.keep || p0 >= n) return;
-    const int *table = a.t.entries + row_of(a.tok, i) * a.t.ld;
-    const int group = a.heads / a.kv_heads;
-    unsigned long long *keys = a.keys + ((long long)i * a.kv_heads + g) * a.t.width;
-    for (int p = p0; p < p1; ++p) {
-        const int held = table[p];
-        double x = 0;
-        if ((unsigned)held < (unsigned)a.means.pages) {
-            const T *mean = a.means.row(held, g, 0);
-            for (int e = lane; e < a.d; e += 32) {
-                double q = 0;
-                for (int h = 0; h < group; ++h) q += attn::widen(a.q[i * a.q_ld + (g * group + h) * a.q_sh + e]);
-                x += q * attn::widen(mean[e]);
-            }
+    constexpr int N = 16 / sizeof(T), AT_ONCE = 8, STEP = 32 / LANES, BATCH = AT_ONCE * STEP;   // pages of an instruction, of a batch
+    const int lane = threadIdx.x & 31, me = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), group = a.heads / a.kv_heads;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const auto blocks_of = [&](int i) {
+        const int n = pages_seen(a, i);
+        return n > a.keep ? (n + kScorePages - 1) / kScorePages : 0;
+    };
+    Share w;
+    if (!deal<kThreads>(a.M, [&](int i) { return (long long)blocks_of(i) * a.kv_heads; }, gridDim.x * (kThreads / 32), me, 1, w)) return;
+    int i = w.row, n = pages_seen(a, i), blocks = blocks_of(i), g = (int)(w.rest / blocks), b = (int)(w.rest - (long long)g * blocks);
+    double q[HALVES][N];
+    bool fresh = true;
+    for (long long left = w.hi - w.lo; left > 0; --left) {
+        const int p0 = b * kScorePages;
+        int held = p0 + lane < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p0 + lane] : -1;
+        if (fresh) {
 #pragma unroll
-            for (int w = 16; w; w >>= 1) x += __shfl_xor_sync(~0u, x, w);
-        } else {
-            x = -CUDART_INF;
+            for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+                for (int k = 0; k < N; ++k) q[x][k] = 0;
+            for (int h = 0; h < group; ++h) {
+                const T *from = a.q + i * a.q_ld + (g * group + h) * a.q_sh;
+#pragma unroll
+                for (int x = 0; x < HALVES; ++x) {
+                    const int e = (lane % LANES + x * 32) * N;
+                    Chunk<T> c;
+                    float f[N] = {};
+                    c.load(from, e, a.d, a.q_wide && e + N <= a.d);
+                    c.add_to(f);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) q[x][k] += f[k];
+                }
+            }
+            fresh = false;
         }
-        if (lane == 0) keys[p] = ordered(x);
+        unsigned long long *keys = a.keys + ((long long)i * a.kv_heads + g) * a.t.width;
+        for (int s = 0; s < kScorePages && p0 + s < n; s += BATCH) {
+            uint4 c[AT_ONCE][HALVES];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int p = __shfl_sync(~0u, held, s + j * STEP + lane / LANES);
+#pragma unroll
+                for (int x = 0; x < HALVES; ++x) {
+                    const int e = (lane % LANES + x * 32) * N;
+                    c[j][x] = make_uint4(0, 0, 0, 0);
+                    if ((unsigned)p < (unsigned)a.means.pages && e < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(a.means.row(p, g, 0) + e);
+                }
+            }
+            double sum[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                sum[j] = 0;
+#pragma unroll
+                for (int x = 0; x < HALVES; ++x) {
+                    float f[N] = {};
+                    Chunk<T>{c[j][x]}.add_to(f);
+#pragma unroll
+                    for (int k = 0; k < N; ++k)   // (what lies behind d may be anything)
+                        if ((lane % LANES + x * 32) * N + k < a.d) sum[j] += q[x][k] * f[k];
+                }
+            }
+            // LANES lanes' sums of eight: halves of what is left are exchanged until each lane has one, which is then summed up
+            int mine = 0;
+#pragma unroll
+            for (int x = LANES / 2, v = AT_ONCE; x; x >>= 1) {
+                if (v > 1) {
+                    v >>= 1;
+                    const bool up = lane & x;
+                    mine += up ? v : 0;
+#pragma unroll
+                    for (int j = 0; j < AT_ONCE / 2; ++j)
+                        if (j < v) sum[j] = (up ? sum[j + v] : sum[j]) + __shfl_xor_sync(~0u, up ? sum[j] : sum[j + v], x);
+                } else {
+                    sum[0] += __shfl_xor_sync(~0u, sum[0], x);
+                }
+            }
+            const int k = s + mine * STEP + lane / LANES, page = __shfl_sync(~0u, held, k);
+            if (lane % (LANES / AT_ONCE) == 0 && p0 + k < n) keys[p0 + k] = (unsigned)page < (unsigned)a.means.pages ? ordered(sum[0]) : ordered(-CUDART_INF);
+        }
+        if (++b == blocks) {
+            b = 0;
+            fresh = true;
+            if (++g == a.kv_heads) {
+                g = 0;
+                do
+                    if (++i >= a.M) return;
+                while (!(blocks = blocks_of(i)));
+                n = pages_seen(a, i);
+            }
+        }
     }
 }
 
-// The best `keep` of a token's pages, a CTA per token and key head.  The keep-th largest key is found bit by bit from the first in which the keys differ,
-// each time by counting the keys that are at least as large; it ends early where exactly `keep` are.  A thread holds neighbouring pages, so
-// that ties and the ascending order of the list follow from prefix sums over the threads.
-constexpr int kHeld = 8;   // keys of a thread in registers; those behind are read again for each bit
-template <typename T>
-__global__ void __launch_bounds__(kThreads) paged_select_kernel(const SelectArgs<T> a)
+// The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS keys a lane in registers (0: any number, read again each time).  The
+// keep-th largest key is found bit by bit, each time by counting those that are at least as large, first by the keys' upper halves and, where several
+// have that of the border, by their lower ones; it ends early where exactly `keep` are.
+template <int WARPS> __device__ __forceinline__ int count_all(int c, int (&sums)[2][WARPS], int &turn)
 {
-    constexpr int W = kThreads / 32;
-    __shared__ unsigned long long ands[W], ors[W];
-    __shared__ int counts[2][W];
-    __shared__ long long warps[W];
-    const int i = blockIdx.x / a.kv_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int n = pages_seen(a, i);
+    c = __reduce_add_sync(~0u, c);
+    if (WARPS == 1) return c;
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) sums[turn][threadIdx.x >> 5] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) c += sums[turn][w];
+    return c;
+}
+template <int WARPS, int KEYS>
+__device__ __forceinline__ void select_best(const unsigned long long *keys, int n, int keep, int first, int last, int *list, int (&sums)[2][WARPS])
+{
+    const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
+    const int each = ((n + WARPS - 1) / WARPS + 31) & ~31, p0 = warp * each, p1 = min(n, p0 + each), rounds = KEYS ? KEYS : each / 32;   // this warp's pages
+    const auto key = [&](int j) {
+        const int p = p0 + j * 32 + lane;
+        return p >= p1 ? 0 : p < first || p >= n - last ? ~0ull : keys[p];
+    };
+    unsigned highs[KEYS ? KEYS : 1], lows[KEYS ? KEYS : 1];
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) {
+            const unsigned long long k = key(j);
+            highs[j] = (unsigned)(k >> 32);
+            lows[j] = (unsigned)k;
+        }
+    }
+    const auto high = [&](int j) { if constexpr (KEYS > 0) return highs[j]; else return (unsigned)(key(j) >> 32); };
+    const auto low = [&](int j) { if constexpr (KEYS > 0) return lows[j]; else return (unsigned)key(j); };
+    const auto there = [&](int j) { return p0 + j * 32 + lane < p1; };
+    int turn = 0, at_least = n;
+    const auto count = [&](auto in) {
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < rounds; ++j) c += in(j);
+        return count_all<WARPS>(c, sums, turn);
+    };
+    // the largest border with at least `want` at or above it (0: none but that), and how many are
+    unsigned border = 0, lower = 0;
+    for (int bit = 31; bit >= 0 && at_least != keep; --bit) {
+        const unsigned to = border | 1u << bit;
+        const int c = count([&](int j) { return high(j) >= to; });
+        if (c >= keep) { border = to; at_least = c; }
+    }
+    int ties = INT_MAX;   // how many keys that are exactly the border's are taken: all, unless there are more than fit
+    if (at_least != keep) {
+        const int above = count([&](int j) { return high(j) > border; }), want = keep - above;
+        int same = at_least - above;
+        for (int bit = 31; bit >= 0 && same != want; --bit) {
+            const unsigned to = lower | 1u << bit;
+            const int c = count([&](int j) { return high(j) == border && low(j) >= to; });   // (keys that are not there are 0, which is below `to`)
+            if (c >= want) { lower = to; same = c; }
+        }
+        if (same != want) ties = want - count([&](int j) { return high(j) == border && low(j) > lower; });
+    }
+    const auto over = [&](int j) { return high(j) > border || (high(j) == border && low(j) > lower); };
+    const auto tie = [&](int j) { return there(j) && high(j) == border && low(j) == lower; };
+    // in order of pages; with several warps each first counts what the ones before it take
+    int to = 0, tied = 0;
+    if (WARPS > 1) {
+        int mine = 0, mine_tied = 0;
+#pragma unroll
+        for (int j = 0; j < rounds; ++j) { mine += over(j); mine_tied += tie(j); }
+        mine = __reduce_add_sync(~0u, mine);
+        mine_tied = __reduce_add_sync(~0u, mine_tied);
+        __syncthreads();
+        if (lane == 0) { sums[0][warp] = mine; sums[1][warp] = mine_tied; }
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) { to += sums[0][w]; tied += sums[1][w]; }
+        to += min(tied, ties);
+    }
+#pragma unroll
+    for (int j = 0; j < rounds; ++j) {
+        if (p0 + j * 32 >= p1) break;
+        const unsigned equal = __ballot_sync(~0u, tie(j)), below = (1u << lane) - 1;
+        const bool take = tie(j) ? tied + __popc(equal & below) < ties : over(j);
+        const unsigned taken = __ballot_sync(~0u, take);
+        if (take) list[to + __popc(taken & below)] = p0 + j * 32 + lane;
+        to += __popc(taken);
+        tied += __popc(equal);
+    }
+}
+
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) paged_select_kernel(const SelectArgs<T> a)
+{
+    __shared__ int sums[2][WARPS];
+    const int n = pages_seen(a, blockIdx.x / a.kv_heads);
     int *list = a.lists + (long long)blockIdx.x * a.keep;
-    for (int p = threadIdx.x; p < a.keep; p += kThreads)
+    for (int p = threadIdx.x; p < a.keep; p += WARPS * 32)
         if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (by all CTAs: what comes behind this launch counts on the one ahead of it)
     if (n <= a.keep) return;
     const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.t.width;
-    const int each = (n + kThreads - 1) / kThreads, p0 = (int)min((long long)n, threadIdx.x * (long long)each), mine = min(n - p0, each);
-    const auto key = [&](int p) { return p < a.first || p >= n - a.last ? ~0ull : keys[p]; };
-    unsigned long long held[kHeld];
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j) held[j] = j < mine ? key(p0 + j) : 0;
-    unsigned long long all_and = ~0ull, all_or = 0;
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j)
-        if (j < mine) { all_and &= held[j]; all_or |= held[j]; }
-    for (int j = kHeld; j < mine; ++j) { all_and &= key(p0 + j); all_or |= key(p0 + j); }
-#pragma unroll
-    for (int w = 16; w; w >>= 1) { all_and &= __shfl_xor_sync(~0u, all_and, w); all_or |= __shfl_xor_sync(~0u, all_or, w); }
-    if (lane == 0) { ands[warp] = all_and; ors[warp] = all_or; }
-    __syncthreads();
-    for (int w = 0; w < W; ++w) { all_and &= ands[w]; all_or |= ors[w]; }
-    const auto count = [&](auto &&inside, int turn) {
-        int c = 0;
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j) c += j < mine && inside(held[j]);
-        for (int j = kHeld; j < mine; ++j) c += inside(key(p0 + j));
-        c = __reduce_add_sync(~0u, c);
-        if (lane == 0) counts[turn & 1][warp] = c;
-        __syncthreads();
-        c = 0;
-        for (int w = 0; w < W; ++w) c += counts[turn & 1][w];
-        return c;
-    };
-    unsigned long long border = all_and;   // the bits above the first difference; then the largest border with at least keep keys above or at it
-    int at_least = n, turn = 0;
-    const unsigned long long differ = all_and ^ all_or;
-    for (int bit = differ ? 63 - __clzll((long long)differ) : -1; bit >= 0 && at_least != a.keep; --bit, ++turn) {
-        if (turn == 0) border = all_and >> bit << bit;   // (this bit is zero in it)
-        const unsigned long long to = border | 1ull << bit;
-        const int c = count([&](unsigned long long x) { return x >= to; }, turn);
-        if (c >= a.keep) { border = to; at_least = c; }
-    }
-    // all above the border, and as many at it as there is room for, the lower pages first
-    int above = 0, at = 0;
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j) { above += j < mine && held[j] > border; at += j < mine && held[j] == border; }
-    for (int j = kHeld; j < mine; ++j) { above += key(p0 + j) > border; at += key(p0 + j) == border; }
-    long long total_above, total;
-    block_before(above, warps, total_above);
-    const long long at_before = block_before(at, warps, total);
-    const int room = (int)min(max((long long)a.keep - total_above - at_before, 0ll), (long long)at);   // of this thread's
-    int to = (int)block_before(above + room, warps, total), left = room;
-    const auto enter = [&](int j, unsigned long long x) {
-        if (x > border || (x == border && left-- > 0)) list[to++] = p0 + j;
-    };
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j)
-        if (j < mine) enter(j, held[j]);
-    for (int j = kHeld; j < mine; ++j) enter(j, key(p0 + j));
+    if (n <= 256 * WARPS) select_best<WARPS, 8>(keys, n, a.keep, a.first, a.last, list, sums);
+    else if (n <= 1024 * WARPS) select_best<WARPS, 32>(keys, n, a.keep, a.first, a.last, list, sums);
+    else if (n <= 2048 * WARPS) select_best<WARPS, 64>(keys, n, a.keep, a.first, a.last, list, sums);
+    else if (WARPS > 1) select_best<WARPS, 0>(keys, n, a.keep, a.first, a.last, list, sums);
 }
 }  // namespace paged
 }  // namespace b2sp

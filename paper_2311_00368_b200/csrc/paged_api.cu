@@ -16,6 +16,23 @@ template <typename K> bool allow_shared(K *kernel, size_t bytes)
     return bytes <= 40 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 
+// A launch that may begin before the one ahead of it has ended (the kernels wait for that themselves).
+template <typename K, typename... Args> bool launch_early(K *kernel, dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
+{
+    if (!allow_shared(kernel, shared)) return false;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = blocks;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+}
+
 b2sp_status check_tables(const b2sp_page_tables *t, int page)
 {
     if (!t || t->requests < 0 || t->width < 0 || t->ld < 0 || page < 1) return B2SP_ERR_INVALID_ARG;
@@ -55,6 +72,11 @@ bool meet(const void *a, size_t an, const void *b, size_t bn)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return an && bn && x < y + bn && y < x + an;
+}
+
+template <typename T> bool fits(const void *x, long long ld, long long sh, size_t bytes)   // rows begin on multiples of `bytes`
+{
+    return ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(ld * (long long)sizeof(T)) | (uintptr_t)(sh * (long long)sizeof(T))) & (bytes - 1)) == 0;
 }
 
 template <typename T>
@@ -103,8 +125,8 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     if (rc != B2SP_OK) return rc;
     if (M && (!Q || !seen || !lists)) return B2SP_ERR_INVALID_ARG;
     if (d > 256) return B2SP_ERR_UNSUPPORTED;
-    const long long units = (long long)M * kv_heads * ((t->width + kScorePages - 1) / kScorePages), ctas = (long long)M * kv_heads;
-    if (ctas > INT_MAX || (units + 7) / 8 > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    const long long blocks = (long long)M * kv_heads * (((long long)t->width + kScorePages - 1) / kScorePages), ctas = (long long)M * kv_heads;
+    if (ctas > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
     SelectArgs<T> a = {};
@@ -116,64 +138,64 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     a.keys = static_cast<unsigned long long *>(workspace);
     a.lists = lists;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (t->width > keep) {
-        paged_score_kernel<T><<<(unsigned)((units + 7) / 8), kThreads, 0, st>>>(a);
-        attn::launch_behind(paged_select_kernel<T>, (unsigned)ctas, kThreads, st, a);
-    } else {
-        paged_select_kernel<T><<<(unsigned)ctas, kThreads, 0, st>>>(a);   // no more pages than a list holds
+    a.q_wide = fits<T>(Q, ldq, shq, 16);
+    const bool scored = t->width > keep;   // else no token sees more pages than a list holds
+    if (scored) {
+        const unsigned grid = (unsigned)std::min((blocks + 7) / 8, 4ll * kSMs);
+        constexpr int N = 16 / sizeof(T);
+        bool ok = false;
+        if (d <= 8 * N) ok = launch_early(paged_score_kernel<T, 8, 1>, grid, kThreads, 0, st, a);
+        else if (d <= 16 * N) ok = launch_early(paged_score_kernel<T, 16, 1>, grid, kThreads, 0, st, a);
+        else if (d <= 32 * N) ok = launch_early(paged_score_kernel<T, 32, 1>, grid, kThreads, 0, st, a);
+        else if constexpr (sizeof(T) == 4) ok = launch_early(paged_score_kernel<T, 32, 2>, grid, kThreads, 0, st, a);
+        if (!ok) return B2SP_ERR_CUDA;
+    }
+    // a warp holds 2048 keys
+    if (t->width <= 2048) {
+        if (!launch_early(paged_select_kernel<T, 1>, (unsigned)ctas, 32, 0, st, a)) return B2SP_ERR_CUDA;
+    } else if (!launch_early(paged_select_kernel<T, 8>, (unsigned)ctas, 256, 0, st, a)) {
+        return B2SP_ERR_CUDA;
     }
     return launched();
 }
 
 // Warps and workspace of an attention call.
 struct AttnPlan {
-    int nt, heads_of_unit, blocks, warps;   // nt: eights of heads of a unit; blocks: units of a token and key head; warps: at most
+    int nt, queries, blocks, warps;   // nt: eights of queries of a unit; blocks: units of a token and key head; warps: at most
     size_t ml, part, bytes;
 };
-template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d)
+// together: tokens of a request that are likely to be neighbours (1 with lists or without `rows`).
+template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d, long long together)
 {
     AttnPlan p;
     const int group = heads / kv_heads, w = d <= 64 ? 64 : d <= 128 ? 128 : 256;
-    p.nt = sizeof(T) == 2 && group > 8 ? 2 : 1;
-    p.heads_of_unit = 8 * p.nt;
-    p.blocks = (group + p.heads_of_unit - 1) / p.heads_of_unit;
+    p.nt = sizeof(T) == 2 && group * together > 8 ? 2 : 1;
+    p.queries = 8 * p.nt;
+    p.blocks = (group + p.queries - 1) / p.queries;
     p.warps = kSMs * kAttnWarps * (w == 64 ? Form<T, 64>::CTAS : w == 128 ? Form<T, 128>::CTAS : Form<T, 256>::CTAS);
-    const size_t parts = 2ull * p.warps * p.heads_of_unit;
+    const size_t parts = 2ull * p.warps * p.queries;
     p.ml = attn::up256(p.warps * sizeof(int4));
     p.part = p.ml + attn::up256(parts * sizeof(float2));
     p.bytes = p.part + attn::up256(parts * w * sizeof(float));
     return p;
 }
 
-// A launch that may begin before the one ahead of it has ended (the kernels wait for that themselves).
-template <typename K, typename... Args> bool launch_early(K *kernel, dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
-{
-    if (!allow_shared(kernel, shared)) return false;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = blocks;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = shared;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
-}
-
 template <typename T, int W, int NT> b2sp_status launch_attention(AttnArgs<T> &a, const AttnPlan &p, long long most_tiles, cudaStream_t st)
 {
     using F = Form<T, W>;
-    const long long units = (long long)a.M * a.kv_heads * a.blocks;
+    const long long units = (long long)a.M * a.kv_heads * a.blocks, most_cost = most_tiles + units * kUnitCost;
     // no more CTAs than have a share, if every token sees all that it can
-    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_tiles + kLeastTiles * kAttnWarps - 1) / (kLeastTiles * kAttnWarps));
+    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps));
     a.by_unit = units <= ctas * (long long)kAttnWarps;
     const bool ok = a.page % F::ROWS == 0 ? launch_early(paged_attention_kernel<T, W, NT, true>, ctas, kAttnWarps * 32, F::SHARED, st, a)
                                           : launch_early(paged_attention_kernel<T, W, NT, false>, ctas, kAttnWarps * 32, F::SHARED, st, a);
-    const unsigned joins = a.by_unit ? (unsigned)units : ctas * kAttnWarps;
-    if (!ok || !launch_early(paged_join_kernel<T, W>, dim3(joins, std::min(a.group, p.heads_of_unit)), kJoinWarps * 32, 0, st, a, p.heads_of_unit)) return B2SP_ERR_CUDA;
-    return launched();
+    if (!ok) return B2SP_ERR_CUDA;
+    // Few units have many parts each: sixteen warps for a query, else one.
+    const unsigned joins = a.by_unit ? (unsigned)units : ctas * kAttnWarps, queries = std::min(a.pack * a.group, p.queries);
+    const bool joined = units * 16 <= ctas * kAttnWarps
+                            ? launch_early(paged_join_kernel<T, W, 16>, dim3(joins, queries), 512, 0, st, a, p.queries)
+                            : launch_early(paged_join_kernel<T, W, 1>, dim3(joins, (queries + 7) / 8), 256, 0, st, a, p.queries);
+    return joined ? launched() : B2SP_ERR_CUDA;
 }
 
 template <typename T>
@@ -190,7 +212,10 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     if (M && (!Q || !O || !lse || !seen)) return B2SP_ERR_INVALID_ARG;
     if (!apart(d, {{M, ldo}, {heads, sho}})) return B2SP_ERR_INVALID_ARG;
     if (d > 256 || (lists && (long long)keep * kp->page > INT_MAX) || (long long)M * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    const AttnPlan p = attention_plan<T>(heads, kv_heads, d);
+    constexpr long long most_stride = UINT_MAX / sizeof(T);
+    for (const b2sp_pages *c : {kp, vp})
+        if (std::max({c->ld, c->stride_head, c->stride_page}) > most_stride) return B2SP_ERR_UNSUPPORTED;
+    const AttnPlan p = attention_plan<T>(heads, kv_heads, d, rows && !lists && t->requests ? M / t->requests : 1);
     if ((long long)M * kv_heads * p.blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
@@ -199,14 +224,18 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     a.tok = Tokens{rows, seen};
     a.q = Q; a.q_ld = ldq; a.q_sh = shq;
     a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.page = kp->page;
-    a.k = pages<T>(kp); a.v = pages<T>(vp);
+    const auto side = [](const b2sp_pages *c) {
+        return Side{static_cast<const char *>(c->data), (unsigned)(c->ld * sizeof(T)), (unsigned)(c->stride_head * sizeof(T)), (unsigned)(c->stride_page * sizeof(T))};
+    };
+    a.k = side(kp); a.v = side(vp); a.pages = kp->pages;
     a.lists = lists; a.keep = lists ? keep : 0; a.scale = scale;
     a.out = O; a.out_ld = ldo; a.out_sh = sho; a.lse = lse;
-    const auto fits = [](const void *x, long long ld, long long sh, size_t bytes) {
-        return ((reinterpret_cast<uintptr_t>(x) | (uintptr_t)(ld * (long long)sizeof(T)) | (uintptr_t)(sh * (long long)sizeof(T))) & (bytes - 1)) == 0;
-    };
     a.group = heads / kv_heads; a.blocks = p.blocks; a.by_page = Div(a.page);
-    a.q_pairs = fits(Q, ldq, shq, 4); a.q_fours = fits(Q, ldq, shq, 16); a.out_pairs = fits(O, ldo, sho, 4);
+    a.pack = 1;
+    if (rows && !lists)
+        while (a.pack * 2 * a.group <= p.queries) a.pack *= 2;
+    a.by_heads = Div(a.pack > 1 ? a.group : p.queries);
+    a.q_pairs = fits<T>(Q, ldq, shq, 4); a.q_fours = fits<T>(Q, ldq, shq, 16); a.out_pairs = fits<T>(O, ldo, sho, 4);
     char *ws = static_cast<char *>(workspace);
     a.joins = reinterpret_cast<int4 *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
@@ -305,7 +334,7 @@ extern "C" b2sp_status b2sp_paged_select_bf16(int M, int heads, int kv_heads, in
 extern "C" size_t b2sp_attention_paged_workspace_bytes(int M, int heads, int kv_heads, int d)
 {
     if (!token_args_ok(M, heads, kv_heads, d) || d > 256) return 0;
-    return std::max(attention_plan<float>(heads, kv_heads, d).bytes, attention_plan<Bf16>(heads, kv_heads, d).bytes);
+    return std::max(attention_plan<float>(heads, kv_heads, d, 1).bytes, attention_plan<Bf16>(heads, kv_heads, d, INT_MAX).bytes);
 }
 extern "C" b2sp_status b2sp_attention_paged(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long shq, const b2sp_pages *kp,
                                             const b2sp_pages *vp, const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists, int keep,

@@ -5,10 +5,11 @@
 // over the positions j that a token sees, or those of them in the pages that its list names.  Every row of the cache is read once for the heads that
 // share it and used 2 to 16 times, so HBM bounds the work and everything else has to keep out of its way.
 //
-// A unit is a token, a key head and up to 8 (16) of its query heads; its rows come in tiles of kTileRows.  All units' tiles in a line are dealt to the warps
-// in equal shares: a warp takes its share by itself, with a ring of tiles of its own in shared memory that asynchronous copies fill two tiles ahead, and
-// waits for no other warp.  It knows its share from prefix sums over the tokens, so lengths stay on the device and a long row is spread over the GPU as
-// well as many short ones.  Units that end up in several shares leave their sums in the workspace, and a second kernel joins them in order.
+// A unit is a key head and up to 8 (16) queries that look at it: the heads that share it, of one token or of neighbouring tokens of one request; its rows
+// come in tiles of 16 (8).  All units' tiles in a line are dealt to the warps in equal shares: a warp takes its share by itself, with a ring of tiles of its
+// own in shared memory that asynchronous copies fill two tiles ahead, and waits for no other warp.  It knows its share from prefix sums over the tokens, so
+// lengths stay on the device and a long row is spread over the GPU as well as many short ones.  Units that end up in several shares leave their sums in
+// the workspace, and a second kernel joins them in order.
 // Rows that are not there (behind what is seen, of missing pages) are filled with zeros by the copies instead of read: what memory holds there does not
 // enter.
 #pragma once
@@ -17,7 +18,10 @@
 namespace b2sp {
 namespace paged {
 
-constexpr int kAttnWarps = 4, kStages = 3, kLeastTiles = 4;   // warps of a CTA; tiles of a warp in shared memory; of a share
+constexpr int kAttnWarps = 4, kStages = 3;   // warps of a CTA; tiles of a warp in shared memory
+// A unit costs its tiles and, before the first one, a chain of latencies (lengths, table, rows), as long as about four tiles take: without it warps whose
+// shares were many short units took twice as long as the others.  Shares are of at least kLeastCost.
+constexpr int kUnitCost = 4, kLeastCost = 8;
 
 // W: width class of d (64, 128, 256).
 template <typename T, int W> struct Form {
@@ -28,33 +32,53 @@ template <typename T, int W> struct Form {
     static constexpr int CTAS = SHARED <= 56 * 1024 ? 4 : SHARED <= 113 * 1024 ? 2 : 1;   // of an SM
 };
 
+struct Side {   // K or V: byte strides
+    const char *data;
+    unsigned ld, sh, sp;
+};
 template <typename T> struct AttnArgs {
     Tables t;
     Tokens tok;
     const T *q;
     long long q_ld, q_sh;
-    int M, heads, kv_heads, d, page, group, blocks;   // blocks: of a key head's query heads
-    Pages<T> k, v;
+    int M, heads, kv_heads, d, page, pages, group, blocks, pack;   // blocks: of a key head's queries; pack: most tokens of a unit, a power of two
+    Side k, v;
     const int *lists;        // [M][kv_heads][keep] or NULL
     int keep;
     float scale;
-    Div by_page;
+    Div by_page, by_heads;   // by_heads: heads of one token in a unit
     bool q_pairs, q_fours, out_pairs, by_unit;        // by_unit: `joins` are indexed by unit, else by warp
     T *out;
     long long out_ld, out_sh;
     float *lse;
-    float *part;             // two of [heads of a unit][W] per warp: of the unit it begins in the middle of, of the one it leaves in the middle
+    float *part;             // two of [queries of a unit][W] per warp: of the unit it begins in the middle of, of the one it leaves in the middle
     float2 *part_ml;         // (maximum to base 2, sum) of each
-    int4 *joins;             // (unit, first warp, last warp, 0) of units in several shares; first warp -1: none
+    int4 *joins;             // (unit, first warp, last warp, queries) of units in several shares; first warp -1: none
 };
 
-struct Work { int row, unit, tile; };   // token, unit of the token, tile of the unit
-
-template <typename T, int ROWS> __device__ __forceinline__ int tiles_of(const AttnArgs<T> &a, int i, int &seen)
+// The tokens of a unit: `n` from token i on (0: token i belongs to the unit of one before it).  They are of one request, and do not cross multiples of
+// `pack`.  most, least: of the positions that they see.
+struct Pack { int n, most, least; };
+template <typename T> __device__ __forceinline__ Pack pack_of(const AttnArgs<T> &a, int i)
 {
-    seen = seen_of(a.tok, a.t, a.page, i);
-    const int n = a.lists && seen ? a.keep * a.page : seen;
-    return max(1, (int)((n + (ROWS - 1ll)) / ROWS));   // (a token that sees nothing has a tile of nothing)
+    Pack p;
+    p.most = p.least = seen_of(a.tok, a.t, a.page, i);
+    p.n = 1;
+    if (a.pack == 1) return p;
+    const int r = a.tok.rows[i], end = min((i & -a.pack) + a.pack, a.M);   // (packs of several tokens: rows are given)
+    if ((i & (a.pack - 1)) && a.tok.rows[i - 1] == r) { p.n = 0; return p; }
+    while (i + p.n < end && a.tok.rows[i + p.n] == r) {
+        const int s = seen_of(a.tok, a.t, a.page, i + p.n);
+        p.most = max(p.most, s);
+        p.least = min(p.least, s);
+        ++p.n;
+    }
+    return p;
+}
+template <int ROWS, typename T> __device__ __forceinline__ int tiles_of(const AttnArgs<T> &a, const Pack &p)
+{
+    const int n = a.lists && p.most ? a.keep * a.page : p.most;
+    return max(1, (int)((n + (ROWS - 1ll)) / ROWS));   // (tokens that see nothing have a tile of nothing)
 }
 
 // 16 bytes, the first n of them from memory and zeros behind.
@@ -62,25 +86,37 @@ __device__ __forceinline__ void copy16(unsigned to, const void *from, int n)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
 }
+__device__ __forceinline__ unsigned long long times(int a, unsigned b) { return (unsigned long long)(unsigned)a * b; }
 
 // The rows of a unit's tiles.  ALIGNED: pages are whole tiles, so a tile lies in one page and its rows are a stride apart; else lane r finds row r.
 template <typename T, int W, bool ALIGNED> struct Rows {
     using F = Form<T, W>;
     static constexpr int N = 16 / sizeof(T), CHUNKS = F::ROW / 16, PER = F::ROWS * CHUNKS / 32;   // elements of 16 bytes; of a row; copies of a lane
+    static constexpr int AT_ONCE = CHUNKS > 32 ? 1 : 32 / CHUNKS;                                   // rows of a warp's copy (1024 bytes: half of one)
     const AttnArgs<T> &a;
     const int *table, *list;
+    const char *k, *v;
     int seen, n, lane, size0, size1;   // n: positions of the unit's line; bytes that this lane's copies take (rows of 1024 bytes: two kinds)
-    long long head_k, head_v;
+    unsigned place;
 
     __device__ __forceinline__ Rows(const AttnArgs<T> &a_, int i, int g, int seen_, int lane_) : a(a_), seen(seen_), lane(lane_)
     {
         table = a.t.entries + (seen ? row_of(a.tok, i) * a.t.ld : 0);
         list = a.lists ? a.lists + ((long long)i * a.kv_heads + g) * a.keep : nullptr;
         n = seen == 0 ? 0 : list ? a.keep * a.page : seen;
-        size0 = min(max((a.d - lane % CHUNKS * N) * (int)sizeof(T), 0), 16);
+        const int row = lane / CHUNKS, chunk = lane % CHUNKS;
+        size0 = min(max((a.d - chunk * N) * (int)sizeof(T), 0), 16);
         size1 = CHUNKS > 32 ? min(max((a.d - (lane + 32) * N) * (int)sizeof(T), 0), 16) : size0;
-        head_k = g * a.k.sh;
-        head_v = g * a.v.sh;
+        k = a.k.data + times(g, a.k.sh);
+        v = a.v.data + times(g, a.v.sh);
+        if (ALIGNED) {   // (what a lane does not read is not pointed to either)
+            k += times(row, a.k.ld);
+            v += times(row, a.v.ld);
+        }
+        k += size0 ? chunk * 16 : 0;
+        v += size0 ? chunk * 16 : 0;
+        // bfloat16: a row's 16-byte pieces are turned by the row, so that eight rows' pieces at one place lie in different banks
+        place = row * F::ROW + (sizeof(T) == 2 ? chunk ^ row : chunk) * 16;
     }
     // In three steps, a tile apart, so that nothing waits for them: the page's index in the table, the page, the copies.
     struct At { int c, r, held; };   // index in the table (-1: nothing is there), row of the page (ALIGNED: the tile's first), page
@@ -98,48 +134,48 @@ template <typename T, int W, bool ALIGNED> struct Rows {
     }
     __device__ __forceinline__ void page(At &x) const
     {
-        if (x.c < 0 || x.c * (long long)a.page + x.r >= seen) x.c = -1;
+        if (list && (x.c < 0 || x.c * (long long)a.page + x.r >= seen)) x.c = -1;
         x.held = x.c < 0 ? -1 : table[x.c];
+    }
+    static __device__ __forceinline__ unsigned to_of(unsigned to, unsigned place, int i)   // of copy i
+    {
+        if (CHUNKS > 32) return to + (i / 2) * F::ROW + (i & 1) * 512 + place;
+        return to + i * AT_ONCE * F::ROW + (sizeof(T) == 2 ? place ^ ((i * AT_ONCE & 7) * 16) : place);
     }
     // Begins the copies of a tile; which of its rows are there.
     __device__ __forceinline__ unsigned copy(const At &x, unsigned to) const
     {
-        const bool on = (unsigned)x.held < (unsigned)a.k.pages;
+        constexpr unsigned ALL = (1u << F::ROWS) - 1;
+        const bool on = (unsigned)x.held < (unsigned)a.pages;
         if (ALIGNED) {
             if (!on) return 0;
-            const int rows = (int)min((long long)F::ROWS, seen - (x.c * (long long)a.page + x.r));
-            const char *k = reinterpret_cast<const char *>(a.k.data + (x.held * a.k.sp + head_k + x.r * a.k.ld)) + lane % CHUNKS * 16;
-            const char *v = reinterpret_cast<const char *>(a.v.data + (x.held * a.v.sp + head_v + x.r * a.v.ld)) + lane % CHUNKS * 16;
-            const long long k_ld = a.k.ld * (long long)sizeof(T), v_ld = a.v.ld * (long long)sizeof(T);
+            const int rows = seen - (x.c * a.page + x.r);   // (c * page + r < seen)
+            const char *kr = k + times(x.held, a.k.sp) + times(x.r, a.k.ld), *vr = v + times(x.held, a.v.sp) + times(x.r, a.v.ld);
+            const unsigned long long k_step = (unsigned long long)a.k.ld * AT_ONCE, v_step = (unsigned long long)a.v.ld * AT_ONCE;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int row = CHUNKS > 32 ? i / 2 : i * (32 / CHUNKS) + lane / CHUNKS, col = CHUNKS > 32 && (i & 1) ? 512 : 0;
-                const int size = row < rows ? (col ? size1 : size0) : 0;
-                const unsigned at = to + row * F::ROW + place(row, lane % CHUNKS) + col;
-                copy16(at, k + (size ? row * k_ld + col : 0), size);
-                copy16(at + F::ROWS * F::ROW, v + (size ? row * v_ld + col : 0), size);
+                const int row = CHUNKS > 32 ? i / 2 : i * AT_ONCE + lane / CHUNKS, half = CHUNKS > 32 ? i & 1 : 0;
+                const int whole = half ? size1 : size0, size = row < rows ? whole : 0, more = half && size1 ? 512 : 0;
+                copy16(to_of(to, place, i), kr + more, size);
+                copy16(to_of(to, place, i) + F::ROWS * F::ROW, vr + more, size);
+                if (CHUNKS <= 32 || half) { kr += k_step; vr += v_step; }
             }
-            return rows == F::ROWS ? (1u << F::ROWS) - 1 : (1u << rows) - 1;
+            return rows >= F::ROWS ? ALL : (1u << rows) - 1;
         } else {
-            const unsigned there = __ballot_sync(~0u, on) & ((1u << F::ROWS) - 1);
+            const unsigned there = __ballot_sync(~0u, on) & ALL;
             if (!there) return 0;
-            const int held = max(x.held, 0);
-            // lanes below 16 keep K's rows, the others V's
-            const char *mine = lane < 16 ? reinterpret_cast<const char *>(a.k.data + (on ? held * a.k.sp + head_k + x.r * a.k.ld : 0))
-                                         : reinterpret_cast<const char *>(a.v.data + (on ? held * a.v.sp + head_v + x.r * a.v.ld : 0));
+            // lanes below 16 find K's rows, the others V's
+            const unsigned long long mine = !on ? 0 : lane < 16 ? times(x.held, a.k.sp) + times(x.r, a.k.ld) : times(x.held, a.v.sp) + times(x.r, a.v.ld);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int row = CHUNKS > 32 ? i / 2 : i * (32 / CHUNKS) + lane / CHUNKS, col = CHUNKS > 32 && (i & 1) ? 512 : 0;
-                const int size = there >> row & 1 ? (col ? size1 : size0) : 0, from = size ? lane % CHUNKS * 16 + col : 0;
-                const unsigned at = to + row * F::ROW + place(row, lane % CHUNKS) + col;
-                copy16(at, reinterpret_cast<const char *>(__shfl_sync(~0u, (unsigned long long)mine, row)) + from, size);
-                copy16(at + F::ROWS * F::ROW, reinterpret_cast<const char *>(__shfl_sync(~0u, (unsigned long long)mine, row + 16)) + from, size);
+                const int row = CHUNKS > 32 ? i / 2 : i * AT_ONCE + lane / CHUNKS, half = CHUNKS > 32 ? i & 1 : 0;
+                const int size = there >> row & 1 ? (half ? size1 : size0) : 0, more = half && size1 ? 512 : 0;
+                copy16(to_of(to, place, i), k + __shfl_sync(~0u, mine, row) + more, size);
+                copy16(to_of(to, place, i) + F::ROWS * F::ROW, v + __shfl_sync(~0u, mine, row + 16) + more, size);
             }
             return there;
         }
     }
-    // Where 16 bytes of a row lie in it.  bfloat16: turned by the row, so that eight rows' bytes at one place lie in different banks.
-    static __device__ __forceinline__ int place(int row, int chunk) { return (sizeof(T) == 2 ? chunk ^ (row & 7) : chunk) * 16; }
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1)
@@ -162,57 +198,87 @@ __device__ __forceinline__ unsigned transposed(unsigned x)   // of 8 x 8 16-bit 
     return y;
 }
 
-// What a warp holds of a unit, bfloat16: the tile's rows are the long side of the products (S^T = K Q^T, O^T = V^T P^T), the heads the side of eight, so
-// that no more than the heads there are is padded, and K and V come straight from their rows by ldmatrix.
+// Where a unit's queries are: query c is head first + c % heads of token i + c / heads.
+template <typename T> struct Queries {
+    const AttnArgs<T> &a;
+    int i, first, n;
+    __device__ __forceinline__ void of(int c, int &token, int &head) const
+    {
+        const int j = (int)a.by_heads((unsigned)c);
+        token = i + j;
+        head = first + c - j * (int)a.by_heads.d;
+    }
+    __device__ __forceinline__ const T *query(int c) const { int t, h; of(c, t, h); return a.q + t * a.q_ld + h * a.q_sh; }
+    __device__ __forceinline__ T *out(int c) const { int t, h; of(c, t, h); return a.out + t * a.out_ld + h * a.out_sh; }
+    __device__ __forceinline__ float *lse(int c) const { int t, h; of(c, t, h); return a.lse + (long long)t * a.heads + h; }
+    __device__ __forceinline__ int sees(int c) const
+    {
+        if (c >= n) return INT_MAX;
+        int t, h;
+        of(c, t, h);
+        return seen_of(a.tok, a.t, a.page, t);
+    }
+};
+__device__ __forceinline__ float lse_of(float base, float sum) { return sum == 0.f ? -CUDART_INF_F : (base + log2f(sum)) * attn::kLn2; }
+constexpr float kAhead = 8.f;   // the reference of the exponentials follows the maximum when that is 2^8 ahead of it
+
+// What a warp holds of a unit, bfloat16: the tile's rows are the long side of the products (S^T = K Q^T, O^T = V^T P^T), the queries the side of eight, so
+// that no more than the queries there are is padded, and K and V come straight from their rows by ldmatrix.
 // A weight goes into its product as two bfloat16 that make up 16 bits of it; what bounds the kernel leaves the tensor cores time for that.  With an infinity in V
 // the lower part would make 0 * inf or inf - inf of it, so a unit whose sums are not finite is taken again with the upper part alone.
 template <int W, int NT> struct Tile16 {
-    static constexpr int HEADS = 8 * NT, KS = W / 16;
+    static constexpr int QUERIES = 8 * NT, KS = W / 16;
     unsigned q[KS][NT][2];
-    float o[KS][NT][4];       // [columns 16 x ..][heads 8 x ..]: columns g, g + 8 (pairs), heads 2 t, 2 t + 1
-    float top[NT][2], base[NT][2], sum[NT][2];   // of heads 2 t, 2 t + 1; base: top, or 0 as long as that is -inf
+    float o[KS][NT][4];       // [columns 16 x ..][queries 8 x ..]: columns g, g + 8 (pairs), queries 2 t, 2 t + 1
+    float base[NT][2], ahead[NT][2], sum[NT][2];   // of queries 2 t, 2 t + 1; ahead: by how much a logit may exceed base (-inf: none has been met)
+    int sees[NT][2];
     bool lower;
 
-    __device__ __forceinline__ void begin(const AttnArgs<Bf16> &a, const Bf16 *rows, int heads, int lane)   // queries
+    __device__ __forceinline__ void begin(const Queries<Bf16> &u, int lane, bool alike)
     {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-        for (int m = 0; m < NT; ++m)
+        for (int m = 0; m < NT; ++m) {
+            const int c = m * 8 + g;
+            const Bf16 *p = c < u.n ? u.query(c) : nullptr;
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int h = m * 8 + g, e = s * 16 + x * 8 + t * 2;
-                    unsigned u = 0;
-                    if (h < heads) {
-                        const Bf16 *p = rows + h * a.q_sh + e;
-                        if (a.q_pairs && e + 1 < a.d) u = *reinterpret_cast<const unsigned *>(p);
-                        else u = (e < a.d ? p[0].bits : 0) | (unsigned)(e + 1 < a.d ? p[1].bits : 0) << 16;
+                    const int e = s * 16 + x * 8 + t * 2;
+                    unsigned y = 0;
+                    if (p) {
+                        if (u.a.q_pairs && e + 1 < u.a.d) y = *reinterpret_cast<const unsigned *>(p + e);
+                        else y = (e < u.a.d ? p[e].bits : 0) | (unsigned)(e + 1 < u.a.d ? p[e + 1].bits : 0) << 16;
                     }
-                    q[s][m][x] = u;
+                    q[s][m][x] = y;
                 }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) sees[m][e] = alike ? INT_MAX : u.sees(m * 8 + 2 * t + e);
+        }
     }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { top[m][e] = -CUDART_INF_F; base[m][e] = 0.f; sum[m][e] = 0.f; }
+            for (int e = 0; e < 2; ++e) { ahead[m][e] = -CUDART_INF_F; base[m][e] = 0.f; sum[m][e] = 0.f; }
 #pragma unroll
             for (int s = 0; s < KS; ++s) o[s][m][0] = o[s][m][1] = o[s][m][2] = o[s][m][3] = 0.f;
         }
     }
-    __device__ __forceinline__ void take(unsigned at, unsigned there, float scale2, int lane, float *)
+    // there: the tile's rows that are there; first: the position of its row 0, or -1 if all queries see all of them.
+    __device__ __forceinline__ void take(unsigned at, unsigned there, int first, float scale2, int lane, float *)
     {
-        using R = Rows<Bf16, W, true>;
         using F = Form<Bf16, W>;
         float x[NT][4] = {}, y[NT][4] = {};   // two sums, so that half as many products wait for one another
         {
             const int row = lane & 15;
+            const unsigned from = at + row * F::ROW, turn = ((lane >> 4) ^ (row & 7)) * 16;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 unsigned k[4];
-                load_matrices(k, at + row * F::ROW + R::place(row, 2 * s + (lane >> 4)));
+                load_matrices(k, from + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
 #pragma unroll
                 for (int m = 0; m < NT; ++m) mma_bf16(s & 1 ? y[m] : x[m], k, q[s][m][0], q[s][m][1]);
             }
@@ -223,22 +289,37 @@ template <int W, int NT> struct Tile16 {
         for (int m = 0; m < NT; ++m)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[m][e] = (x[m][e] + y[m][e]) * scale2;
-                if (!(there >> (e < 2 ? g : g + 8) & 1)) x[m][e] = -CUDART_INF_F;
-                move |= x[m][e] > top[m][e & 1] + 8.f;
+                x[m][e] += y[m][e];
+                x[m][e] = fmaf(x[m][e], scale2, -base[m][e & 1]);
             }
-        if (__any_sync(~0u, move)) {   // the reference of the exponentials follows the maximum when that is 2^8 ahead
+        if (there != 0xffffu || first >= 0) {
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int row = e < 2 ? g : g + 8;
+                    if (!(there >> row & 1) || (first >= 0 && first + row >= sees[m][e & 1])) x[m][e] = -CUDART_INF_F;
+                }
+        }
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) move |= fmaxf(x[m][e], x[m][e + 2]) > ahead[m][e];
+        if (__any_sync(~0u, move)) {
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float to = fmaxf(x[m][e], x[m][e + 2]);
+                    float by = fmaxf(x[m][e], x[m][e + 2]);
 #pragma unroll
-                    for (int w = 4; w < 32; w <<= 1) to = fmaxf(to, __shfl_xor_sync(~0u, to, w));
-                    to = fmaxf(to, top[m][e]);
-                    base[m][e] = to == -CUDART_INF_F ? 0.f : to;
-                    const float fall = attn::ex2(top[m][e] - base[m][e]);
-                    top[m][e] = to;
+                    for (int w = 4; w < 32; w <<= 1) by = fmaxf(by, __shfl_xor_sync(~0u, by, w));
+                    float fall = 1.f;
+                    if (by == -CUDART_INF_F) by = 0.f;
+                    else if (ahead[m][e] == kAhead) fall = attn::ex2(-(by = fmaxf(by, 0.f)));
+                    else ahead[m][e] = kAhead;   // the first logit, which may lie far below 0
+                    base[m][e] += by;
+                    x[m][e] -= by;
+                    x[m][e + 2] -= by;
                     sum[m][e] *= fall;
 #pragma unroll
                     for (int s = 0; s < KS; ++s) { o[s][m][e] *= fall; o[s][m][e + 2] *= fall; }
@@ -249,7 +330,7 @@ template <int W, int NT> struct Tile16 {
         for (int m = 0; m < NT; ++m) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[m][e] = attn::ex2(x[m][e] - base[m][e & 1]);
+                x[m][e] = attn::ex2(x[m][e]);
                 sum[m][e & 1] += x[m][e];
             }
 #pragma unroll
@@ -259,12 +340,12 @@ template <int W, int NT> struct Tile16 {
                 low[m][j] = transposed(attn::bf16x2(x[m][2 * j] - __uint_as_float(u << 16), x[m][2 * j + 1] - __uint_as_float(u & 0xffff0000u)));
             }
         }
-        const unsigned v_at = at + F::ROWS * F::ROW;
         const int row = (lane >> 4) * 8 + (lane & 7);
+        const unsigned from = at + (F::ROWS + row) * F::ROW, turn = ((lane >> 3 & 1) ^ (lane & 7)) * 16;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             unsigned v[4];
-            load_transposed(v, v_at + row * F::ROW + R::place(row, 2 * s + (lane >> 3 & 1)));
+            load_transposed(v, from + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
 #pragma unroll
             for (int m = 0; m < NT; ++m) {
                 mma_bf16(o[s][m], v, high[m][0], high[m][1]);
@@ -295,77 +376,81 @@ template <int W, int NT> struct Tile16 {
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) sum[m][e] += __shfl_xor_sync(~0u, sum[m][e], w);
     }
-    __device__ __forceinline__ void write(const AttnArgs<Bf16> &a, Bf16 *out, float *lse, int heads, int lane)
+    __device__ __forceinline__ void write(const Queries<Bf16> &u, int lane)
     {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
+            if (m * 8 >= u.n) break;
             float f[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 f[e] = sum[m][e] == 0.f ? 0.f : 1.f / sum[m][e];
-                const int h = m * 8 + 2 * t + e;
-                if (g == 0 && h < heads) lse[h] = sum[m][e] == 0.f ? -CUDART_INF_F : (top[m][e] + log2f(sum[m][e])) * attn::kLn2;
+                const int c = m * 8 + 2 * t + e;
+                if (g == 0 && c < u.n) *u.lse(c) = lse_of(base[m][e], sum[m][e]);
             }
+            const int c = m * 8 + g;
+            Bf16 *out = c < u.n ? u.out(c) : nullptr;
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    // columns by heads to heads by columns: this lane's head g, columns 2 t and 2 t + 1
-                    const unsigned u = transposed(attn::bf16x2(o[s][m][2 * j] * f[0], o[s][m][2 * j + 1] * f[1]));
-                    const int h = m * 8 + g, c = s * 16 + j * 8 + 2 * t;
-                    if (h >= heads) continue;
-                    Bf16 *to = out + h * a.out_sh + c;
-                    if (a.out_pairs && c + 1 < a.d) { *reinterpret_cast<unsigned *>(to) = u; continue; }
-                    if (c < a.d) to[0].bits = (unsigned short)u;
-                    if (c + 1 < a.d) to[1].bits = (unsigned short)(u >> 16);
+                    // columns by queries to queries by columns: this lane's query g, columns 2 t and 2 t + 1
+                    const unsigned y = transposed(attn::bf16x2(o[s][m][2 * j] * f[0], o[s][m][2 * j + 1] * f[1]));
+                    const int e = s * 16 + j * 8 + 2 * t;
+                    if (!out) continue;
+                    if (u.a.out_pairs && e + 1 < u.a.d) { *reinterpret_cast<unsigned *>(out + e) = y; continue; }
+                    if (e < u.a.d) out[e].bits = (unsigned short)y;
+                    if (e + 1 < u.a.d) out[e + 1].bits = (unsigned short)(y >> 16);
                 }
         }
     }
-    __device__ __forceinline__ void leave(float *part, float2 *ml, int heads, int lane)
+    __device__ __forceinline__ void leave(float *part, float2 *ml, int queries, int lane)
     {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int h = m * 8 + 2 * t + e;
-                if (h >= heads) continue;
-                if (g == 0) ml[h] = make_float2(top[m][e], sum[m][e]);
+                const int c = m * 8 + 2 * t + e;
+                if (c >= queries) continue;
+                if (g == 0) ml[c] = make_float2(ahead[m][e] == kAhead ? base[m][e] : -CUDART_INF_F, sum[m][e]);
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    part[h * W + s * 16 + g] = o[s][m][e];
-                    part[h * W + s * 16 + g + 8] = o[s][m][e + 2];
+                    part[c * W + s * 16 + g] = o[s][m][e];
+                    part[c * W + s * 16 + g + 8] = o[s][m][e + 2];
                 }
             }
     }
 };
 
-// The same in fp32, on the CUDA cores, two sums an instruction.  A lane of S has a head (lane & 7) and every fourth 16 bytes of its query in registers, and
-// reads those of each row of K along with the seven other heads' lanes; four lanes' sums then go to one of them for each row.  A lane of O has W / 32 columns of
-// all eight heads and reads the weights, which pass through shared memory.
+// The same in fp32, on the CUDA cores, two sums an instruction.  A lane of S has a query (lane & 7) and every fourth 16 bytes of it in registers, and
+// reads those of each row of K along with the seven other queries' lanes; four lanes' sums then go to one of them for each row.  A lane of O has W / 32 columns
+// of all eight queries and reads the weights, which pass through shared memory.
 template <int W> struct Tile32 {
-    static constexpr int HEADS = 8, ROWS = Form<float, W>::ROWS, MINE = ROWS / 4, COLS = W / 32;
-    uint64_t q[W / 16][2], o[4][COLS];   // o: pairs of heads, columns
-    float top, base, sum;
+    static constexpr int QUERIES = 8, ROWS = Form<float, W>::ROWS, MINE = ROWS / 4, COLS = W / 32;
+    uint64_t q[W / 16][2], o[4][COLS];   // o: pairs of queries, columns
+    float base, ahead, sum;
+    int sees;
     bool lower;
 
-    __device__ __forceinline__ void begin(const AttnArgs<float> &a, const float *rows, int heads, int lane)
+    __device__ __forceinline__ void begin(const Queries<float> &u, int lane, bool alike)
     {
-        const int h = lane & 7, part = lane >> 3;
+        const int c = lane & 7, part = lane >> 3;
+        const float *p = c < u.n ? u.query(c) : nullptr;
+        sees = alike ? INT_MAX : u.sees(c);
 #pragma unroll
         for (int i = 0; i < W / 16; ++i) {
             const int e = (i * 4 + part) * 4;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (h < heads) {
-                const float *p = rows + h * a.q_sh + e;
-                if (a.q_fours && e + 3 < a.d) {
-                    x = *reinterpret_cast<const float4 *>(p);
+            if (p) {
+                if (u.a.q_fours && e + 3 < u.a.d) {
+                    x = *reinterpret_cast<const float4 *>(p + e);
                 } else {
-                    if (e < a.d) x.x = p[0];
-                    if (e + 1 < a.d) x.y = p[1];
-                    if (e + 2 < a.d) x.z = p[2];
-                    if (e + 3 < a.d) x.w = p[3];
+                    if (e < u.a.d) x.x = p[e];
+                    if (e + 1 < u.a.d) x.y = p[e + 1];
+                    if (e + 2 < u.a.d) x.z = p[e + 2];
+                    if (e + 3 < u.a.d) x.w = p[e + 3];
                 }
             }
             q[i][0] = attn::two(x.x, x.y);
@@ -374,14 +459,14 @@ template <int W> struct Tile32 {
     }
     __device__ __forceinline__ void clear()
     {
-        top = -CUDART_INF_F; base = 0.f; sum = 0.f;
+        ahead = -CUDART_INF_F; base = 0.f; sum = 0.f;
 #pragma unroll
         for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int c = 0; c < COLS; ++c) o[h][c] = 0;
     }
     static __device__ __forceinline__ int weights_of(int row) { return row * 8 + row / MINE * 8; }   // (four rows that are written at once: different banks)
-    __device__ __forceinline__ void take(unsigned at, unsigned there, float scale2, int lane, float *weights)
+    __device__ __forceinline__ void take(unsigned at, unsigned there, int first, float scale2, int lane, float *weights)
     {
         using F = Form<float, W>;
         const int part = lane >> 3;
@@ -412,20 +497,25 @@ template <int W> struct Tile32 {
 #pragma unroll
         for (int r = 0; r < MINE; ++r) {
             const float give = odd ? s[r] : s[r + MINE], keep = odd ? s[r + MINE] : s[r];
-            s[r] = (keep + __shfl_xor_sync(~0u, give, 8)) * scale2;
-            if (!(there >> (part * MINE + r) & 1)) s[r] = -CUDART_INF_F;
-            move |= s[r] > top + 8.f;
+            s[r] = fmaf(keep + __shfl_xor_sync(~0u, give, 8), scale2, -base);
+            const int row = part * MINE + r;
+            if (!(there >> row & 1) || (first >= 0 && first + row >= sees)) s[r] = -CUDART_INF_F;
+            move |= s[r] > ahead;
         }
         if (__any_sync(~0u, move)) {
-            float to = top;
+            float by = s[0];
 #pragma unroll
-            for (int r = 0; r < MINE; ++r) to = fmaxf(to, s[r]);
-            to = fmaxf(to, __shfl_xor_sync(~0u, to, 8));
-            to = fmaxf(to, __shfl_xor_sync(~0u, to, 16));
-            base = to == -CUDART_INF_F ? 0.f : to;
-            const float fall = attn::ex2(top - base);
-            top = to;
+            for (int r = 1; r < MINE; ++r) by = fmaxf(by, s[r]);
+            by = fmaxf(by, __shfl_xor_sync(~0u, by, 8));
+            by = fmaxf(by, __shfl_xor_sync(~0u, by, 16));
+            float fall = 1.f;
+            if (by == -CUDART_INF_F) by = 0.f;
+            else if (ahead == kAhead) fall = attn::ex2(-(by = fmaxf(by, 0.f)));
+            else ahead = kAhead;
+            base += by;
             sum *= fall;
+#pragma unroll
+            for (int r = 0; r < MINE; ++r) s[r] -= by;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 const uint64_t f = attn::two(__shfl_sync(~0u, fall, 2 * h), __shfl_sync(~0u, fall, 2 * h + 1));
@@ -435,7 +525,7 @@ template <int W> struct Tile32 {
         }
 #pragma unroll
         for (int r = 0; r < MINE; ++r) {
-            s[r] = attn::ex2(s[r] - base);
+            s[r] = attn::ex2(s[r]);
             sum += s[r];
             weights[weights_of(part * MINE + r) + (lane & 7)] = s[r];
         }
@@ -471,34 +561,36 @@ template <int W> struct Tile32 {
         sum += __shfl_xor_sync(~0u, sum, 16);
     }
     static __device__ __forceinline__ int column(int c, int lane) { return COLS == 2 ? lane * 2 + c : lane * 4 + c / 4 * 128 + c % 4; }
-    __device__ __forceinline__ void write(const AttnArgs<float> &a, float *out, float *lse, int heads, int lane)
+    __device__ __forceinline__ void write(const Queries<float> &u, int lane)
     {
         const float f = sum == 0.f ? 0.f : 1.f / sum;
-        if (lane < heads) lse[lane] = sum == 0.f ? -CUDART_INF_F : (top + log2f(sum)) * attn::kLn2;
+        if (lane < u.n) *u.lse(lane) = lse_of(base, sum);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
+            if (2 * h >= u.n) break;
             const float f0 = __shfl_sync(~0u, f, 2 * h), f1 = __shfl_sync(~0u, f, 2 * h + 1);
+            float *out0 = u.out(2 * h), *out1 = 2 * h + 1 < u.n ? u.out(2 * h + 1) : nullptr;
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
                 const int e = column(c, lane);
                 float x, y;
                 attn::split(o[h][c], x, y);
-                if (e < a.d && 2 * h < heads) out[2 * h * a.out_sh + e] = x * f0;
-                if (e < a.d && 2 * h + 1 < heads) out[(2 * h + 1) * a.out_sh + e] = y * f1;
+                if (e < u.a.d) out0[e] = x * f0;
+                if (e < u.a.d && out1) out1[e] = y * f1;
             }
         }
     }
-    __device__ __forceinline__ void leave(float *part, float2 *ml, int heads, int lane)
+    __device__ __forceinline__ void leave(float *part, float2 *ml, int queries, int lane)
     {
-        if (lane < heads) ml[lane] = make_float2(top, sum);
+        if (lane < queries) ml[lane] = make_float2(ahead == kAhead ? base : -CUDART_INF_F, sum);
 #pragma unroll
         for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
                 float x, y;
                 attn::split(o[h][c], x, y);
-                if (2 * h < heads) part[2 * h * W + column(c, lane)] = x;
-                if (2 * h + 1 < heads) part[(2 * h + 1) * W + column(c, lane)] = y;
+                if (2 * h < queries) part[2 * h * W + column(c, lane)] = x;
+                if (2 * h + 1 < queries) part[(2 * h + 1) * W + column(c, lane)] = y;
             }
     }
 };
@@ -510,164 +602,138 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
 {
     using F = Form<T, W>;
     using Tile = typename TileOf<T, W, NT>::type;
-    constexpr int THREADS = kAttnWarps * 32;
     extern __shared__ __align__(128) char shared[];
-    __shared__ long long before[THREADS], warps[kAttnWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x * kAttnWarps + warp;
     const int units = a.kv_heads * a.blocks;   // of a token
-    const int each = (a.M + THREADS - 1) / THREADS;
     char *ring = shared + warp * F::RING;
     float *weights = reinterpret_cast<float *>(shared + kAttnWarps * F::RING + warp * F::WEIGHTS);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    long long lo, hi, share;
-    {
-        const int i0 = (int)min((long long)a.M, threadIdx.x * (long long)each), i1 = min(a.M, i0 + each);
-        long long n = 0, all;
-        int seen;
-        for (int i = i0; i < i1; ++i) n += tiles_of<T, F::ROWS>(a, i, seen);
-        before[threadIdx.x] = block_before(n, warps, all) * units;
-        all *= units;
-        share = max((all + gridDim.x * kAttnWarps - 1) / (gridDim.x * kAttnWarps), (long long)kLeastTiles);
-        lo = me * share;
-        hi = min(lo + share, all);
-        __syncthreads();   // `before`
-        if (lo >= hi) {
-            if (!a.by_unit && lane == 0) a.joins[me] = make_int4(0, -1, 0, 0);
-            return;
-        }
-    }
-    // the token that the share begins in
-    Work w;
-    int seen, tiles;
-    {
-        int chunk = -1;
-#pragma unroll
-        for (int j = 0; j < kAttnWarps; ++j) chunk += __popc(__ballot_sync(~0u, before[j * 32 + lane] <= lo));
-        long long rest = lo - before[chunk];
-        int i = chunk * each;
-        for (;;) {   // 32 tokens at a time
-            long long n = i + lane < a.M ? (long long)tiles_of<T, F::ROWS>(a, i + lane, seen) * units : 0;
-            long long up = n;
-#pragma unroll
-            for (int x = 1; x < 32; x <<= 1) {
-                const long long y = __shfl_up_sync(~0u, up, x);
-                if (lane >= x) up += y;
-            }
-            const unsigned behind = __ballot_sync(~0u, up > rest);
-            if (behind) {
-                const int k = __ffs(behind) - 1;
-                rest -= __shfl_sync(~0u, up - n, k);
-                i += k;
-                break;
-            }
-            rest -= __shfl_sync(~0u, up, 31);
-            i += 32;
-        }
-        tiles = tiles_of<T, F::ROWS>(a, i, seen);
-        w.row = i;
-        w.unit = (int)(rest / tiles);
-        w.tile = (int)(rest - (long long)w.unit * tiles);
+    const auto cost = [&](int i) {
+        const Pack p = pack_of(a, i);
+        return p.n ? (long long)(tiles_of<F::ROWS>(a, p) + kUnitCost) * units : 0ll;
+    };
+    Share w;
+    if (!deal<kAttnWarps * 32>(a.M, cost, gridDim.x * kAttnWarps, me, kLeastCost, w)) {
+        if (!a.by_unit && lane == 0) a.joins[me] = make_int4(0, -1, 0, 0);
+        return;
     }
     int4 join = make_int4(0, -1, 0, 0);
     const float scale2 = a.scale * attn::kLog2e;
+    Pack p = pack_of(a, w.row);
+    int i = w.row, tiles = tiles_of<F::ROWS>(a, p), unit;   // unit of the token; what of it lies before this warp's share
+    long long before;
+    if (w.rest >> 31) {
+        unit = (int)(w.rest / (tiles + kUnitCost));
+        before = w.rest - (long long)unit * (tiles + kUnitCost);
+    } else {
+        unit = (int)w.rest / (tiles + kUnitCost);
+        before = (int)w.rest - unit * (tiles + kUnitCost);
+    }
     Tile x;
-    for (long long left = hi - lo; left > 0;) {
-        const int g = w.unit / a.blocks, b = w.unit - g * a.blocks, h0 = g * a.group + b * Tile::HEADS, heads = min(Tile::HEADS, a.group - b * Tile::HEADS);
-        const int ends = (int)min((long long)tiles, w.tile + left);
-        const Rows<T, W, ALIGNED> rows(a, w.row, g, seen, lane);
-        x.begin(a, a.q + w.row * a.q_ld + h0 * a.q_sh, heads, lane);
-        x.lower = true;
-        do {
-            x.clear();
+    for (long long at = w.lo;;) {
+        // position `at` of the line is `before` behind the unit's begin; tile t of the unit lies at kUnitCost + t
+        const long long begin = at - before, end = min(begin + tiles + kUnitCost, w.hi);
+        const int first = (int)max(before - kUnitCost, 0ll), last = (int)(end - begin) - kUnitCost;   // tiles
+        if (last > first) {
+            const int g = unit / a.blocks, b = unit - g * a.blocks;
+            const Queries<T> u{a, i, g * a.group + b * Tile::QUERIES, a.pack > 1 ? p.n * a.group : min(Tile::QUERIES, a.group - b * Tile::QUERIES)};
+            const Rows<T, W, ALIGNED> rows(a, i, g, p.most, lane);
             // a tile's index is found four tiles ahead of its use, its page three, and its copies begin two ahead
-            typename Rows<T, W, ALIGNED>::At at = rows.index(w.tile), next = rows.index(w.tile + 1), third = rows.index(w.tile + 2), fourth = rows.index(w.tile + 3);
-            unsigned there, there1, there2;
-            const unsigned to = (unsigned)__cvta_generic_to_shared(ring);
-            rows.page(at);
-            rows.page(next);
-            rows.page(third);
-            there = rows.copy(at, to);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            there1 = w.tile + 1 < ends ? rows.copy(next, to + F::TILE) : 0;
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            int stage = 0;
-            for (int j = w.tile; j < ends; ++j) {
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-                __syncwarp();
-                const int free = stage == 0 ? 2 : stage - 1;
-                there2 = j + 2 < ends ? rows.copy(third, to + free * F::TILE) : 0;
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                third = fourth;
+            typename Rows<T, W, ALIGNED>::At now = rows.index(first), next = rows.index(first + 1), third = rows.index(first + 2), fourth = rows.index(first + 3);
+            x.begin(u, lane, p.n == 1);
+            x.lower = true;
+            do {
+                x.clear();
+                unsigned there, there1, there2;
+                const unsigned to = (unsigned)__cvta_generic_to_shared(ring);
+                rows.page(now);
+                rows.page(next);
                 rows.page(third);
-                fourth = rows.index(j + 4);
-                if (there) x.take(to + stage * F::TILE, there, scale2, lane, weights);
-                there = there1;
-                there1 = there2;
-                stage = stage == 2 ? 0 : stage + 1;
+                there = rows.copy(now, to);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                there1 = first + 1 < last ? rows.copy(next, to + F::TILE) : 0;
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                int stage = 0;
+                for (int j = first; j < last; ++j) {
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    __syncwarp();
+                    const int free = stage == 0 ? 2 : stage - 1;
+                    there2 = j + 2 < last ? rows.copy(third, to + free * F::TILE) : 0;
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    third = fourth;
+                    rows.page(third);
+                    fourth = rows.index(j + 4);
+                    if (there) x.take(to + stage * F::TILE, there, (j + 1) * F::ROWS > p.least && p.n > 1 ? j * F::ROWS : -1, scale2, lane, weights);
+                    there = there1;
+                    there1 = there2;
+                    stage = stage == 2 ? 0 : stage + 1;
+                    __syncwarp();
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
                 __syncwarp();
+                if (!x.again()) break;
+                now = rows.index(first); next = rows.index(first + 1); third = rows.index(first + 2); fourth = rows.index(first + 3);
+            } while (true);
+            x.total();
+            const int id = i * units + unit;
+            const bool all = first == 0 && last == tiles;
+            if (all) {
+                x.write(u, lane);
+            } else {
+                const long long slot = me * 2ll + (first == 0);
+                x.leave(a.part + slot * Tile::QUERIES * W, a.part_ml + slot * Tile::QUERIES, u.n, lane);
+                if (first == 0) join = make_int4(id, me, (int)((begin + tiles + kUnitCost - 1) / w.share), u.n);   // (the warp that the last tile lies with)
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            __syncwarp();
-        } while (x.again());
-        x.total();
-        const int unit = w.row * units + w.unit;
-        if (w.tile == 0 && ends == tiles) {
-            x.write(a, a.out + w.row * a.out_ld + h0 * a.out_sh, a.lse + (long long)w.row * a.heads + h0, heads, lane);
-            if (a.by_unit && lane == 0) a.joins[unit] = make_int4(unit, -1, 0, 0);
-        } else {
-            const long long slot = me * 2ll + (w.tile == 0);
-            x.leave(a.part + slot * Tile::HEADS * W, a.part_ml + slot * Tile::HEADS, heads, lane);
-            if (w.tile == 0) {   // the warps that the others lie with: the last tile's is the last one
-                join = make_int4(unit, me, (int)((hi - left + tiles - 1) / share), 0);
-                if (a.by_unit && lane == 0) a.joins[unit] = join;
-            }
+            if (first == 0 && a.by_unit && lane < p.n) a.joins[id + lane * units] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
         }
-        left -= ends - w.tile;
-        w.tile = 0;
-        if (++w.unit == units && left > 0) {
-            w.unit = 0;
-            tiles = tiles_of<T, F::ROWS>(a, ++w.row, seen);
+        at = end;
+        if (at >= w.hi) break;
+        before = 0;
+        if (++unit == units) {
+            unit = 0;
+            if ((i += p.n) >= a.M) break;   // (not with lengths that stay as they are)
+            p = pack_of(a, i);
+            tiles = tiles_of<F::ROWS>(a, p);
         }
     }
     if (!a.by_unit && lane == 0) a.joins[me] = join;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// A CTA per entry of `joins` and head of a unit: each warp takes every eighth part (the loads of eight at once), then the warps' sums are joined in order.
-constexpr int kJoinWarps = 8;
-template <typename T, int W>
-__global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const AttnArgs<T> a, int heads_of_unit)
+// Joins the parts of units in several shares.  WARPS: warps that take a query of an entry of `joins`, kJoinAt parts of it at a time each, whose results are
+// joined in order; with one the CTA takes eight queries.
+constexpr int kJoinAt = 10;
+template <typename T, int W, int WARPS>
+__global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) paged_join_kernel(const AttnArgs<T> a, int queries)   // queries: of a unit, at most
 {
-    constexpr int V = W == 256 ? 2 : 1;   // groups of four columns of a lane
-    __shared__ float sums[kJoinWarps][W], weight[kJoinWarps], highs[kJoinWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int V = W == 256 ? 2 : 1, AT = W == 256 ? kJoinAt / 2 : kJoinAt;   // V: groups of four columns of a lane
+    __shared__ float sums[WARPS][W], weight[WARPS], highs[WARPS];
+    const int warp = WARPS == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int4 j = a.joins[blockIdx.x];
-    const int units = a.kv_heads * a.blocks, row = j.x / units, u = j.x - row * units, g = u / a.blocks, b = u - g * a.blocks, m = blockIdx.y;
-    if (j.y < 0 || b * heads_of_unit + m >= a.group) return;
-    const int h = g * a.group + b * heads_of_unit + m;
+    const int m = WARPS == 1 ? blockIdx.y * 8 + (threadIdx.x >> 5) : blockIdx.y;
+    if (j.y < 0 || m >= j.w) return;
+    const int units = a.kv_heads * a.blocks, i = j.x / units, unit = j.x - i * units, g = unit / a.blocks, b = unit - g * a.blocks;
+    const Queries<T> u{a, i, g * a.group + b * queries, j.w};
     float x[V][4] = {}, high = -CUDART_INF_F, l = 0.f;
-    constexpr int AT = 8;
-    for (int p = j.y + warp; p <= j.z; p += kJoinWarps * AT) {
+    for (int p = j.y + warp; p <= j.z; p += WARPS * AT) {
         float y[AT][V][4];
         float2 ml[AT];
 #pragma unroll
-        for (int i = 0; i < AT; ++i) {
-            const int c = p + i * kJoinWarps;
-            ml[i] = make_float2(-CUDART_INF_F, 0.f);
-#pragma unroll
-            for (int v = 0; v < V; ++v) y[i][v][0] = y[i][v][1] = y[i][v][2] = y[i][v][3] = 0.f;
+        for (int k = 0; k < AT; ++k) {
+            const int c = p + k * WARPS;
+            ml[k] = make_float2(-CUDART_INF_F, 0.f);
             if (c <= j.z) {
-                const long long slot = (c * 2ll + (c == j.y)) * heads_of_unit + m;
-                ml[i] = a.part_ml[slot];
+                const long long slot = (c * 2ll + (c == j.y)) * queries + m;
+                ml[k] = a.part_ml[slot];
 #pragma unroll
-                for (int v = 0; v < V; ++v) attn::load_part(a.part + slot * W, (lane + 32 * v) * 4, W, y[i][v]);
+                for (int v = 0; v < V; ++v) attn::load_part(a.part + slot * W, (lane + 32 * v) * 4, W, y[k][v]);
             }
         }
         float to = high;
 #pragma unroll
-        for (int i = 0; i < AT; ++i) to = fmaxf(to, ml[i].x);
-        const float ref = to == -CUDART_INF_F ? 0.f : to, fall = exp2f(high - ref);
+        for (int k = 0; k < AT; ++k) to = fmaxf(to, ml[k].x);
+        const float ref = to == -CUDART_INF_F ? 0.f : to, fall = attn::ex2(high - ref);
         high = to;
         l *= fall;
 #pragma unroll
@@ -675,36 +741,47 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const AttnA
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[v][k] *= fall;
 #pragma unroll
-        for (int i = 0; i < AT; ++i) {
-            if (p + i * kJoinWarps > j.z) break;
-            const float f = exp2f(ml[i].x - ref);
-            l = fmaf(ml[i].y, f, l);
+        for (int k = 0; k < AT; ++k) {
+            if (p + k * WARPS > j.z) break;
+            const float f = attn::ex2(ml[k].x - ref);
+            l = fmaf(ml[k].y, f, l);
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[v][k] = fmaf(f, y[i][v][k], x[v][k]);
+                for (int e = 0; e < 4; ++e) x[v][e] = fmaf(f, y[k][v][e], x[v][e]);
         }
     }
+    if constexpr (WARPS == 1) {
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        T *out = u.out(m);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if ((lane + 32 * v) * 4 < W) *reinterpret_cast<float4 *>(&sums[warp][(lane + 32 * v) * 4]) = make_float4(x[v][0], x[v][1], x[v][2], x[v][3]);
-    if (lane == 0) { weight[warp] = l; highs[warp] = high; }
-    __syncthreads();
-    high = -CUDART_INF_F;
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) high = fmaxf(high, highs[w]);
-    const float ref = high == -CUDART_INF_F ? 0.f : high;
-    l = 0.f;
+            for (int e = 0; e < 4; ++e)
+                if ((lane + 32 * v) * 4 + e < a.d) attn::narrow(x[v][e] * f, out[(lane + 32 * v) * 4 + e]);
+        if (lane == 0) *u.lse(m) = lse_of(high, l);
+    } else {
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) l = fmaf(exp2f(highs[w] - ref), weight[w], l);
-    const float f = l == 0.f ? 0.f : 1.f / l;
-    for (int e = threadIdx.x; e < a.d; e += kJoinWarps * 32) {
+        for (int v = 0; v < V; ++v)
+            if ((lane + 32 * v) * 4 < W) *reinterpret_cast<float4 *>(&sums[warp][(lane + 32 * v) * 4]) = make_float4(x[v][0], x[v][1], x[v][2], x[v][3]);
+        if (lane == 0) { weight[warp] = l; highs[warp] = high; }
+        __syncthreads();
+        if (threadIdx.x >= W) return;
+        high = -CUDART_INF_F;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) high = fmaxf(high, highs[w]);
+        const float ref = high == -CUDART_INF_F ? 0.f : high;
         float y = 0.f;
+        l = 0.f;
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) y = fmaf(exp2f(highs[w] - ref), sums[w][e], y);
-        attn::narrow(y * f, a.out[row * a.out_ld + h * a.out_sh + e]);
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = attn::ex2(highs[w] - ref);
+            l = fmaf(f, weight[w], l);
+            y = fmaf(f, sums[w][threadIdx.x], y);
+        }
+        if (threadIdx.x < a.d) attn::narrow(l == 0.f ? 0.f : y / l, u.out(m)[threadIdx.x]);
+        if (threadIdx.x == 0) *u.lse(m) = lse_of(high, l);
     }
-    if (threadIdx.x == 0) a.lse[(long long)row * a.heads + h] = l == 0.f ? -CUDART_INF_F : (high + log2f(l)) * attn::kLn2;
 }
 
 }  // namespace paged

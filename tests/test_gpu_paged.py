@@ -226,7 +226,7 @@ class Cache:
 @pytest.mark.parametrize("seen,H,Hkv,d,page,keep,first,last", [
     ([1], 1, 1, 64, 16, 1, 0, 0), ([200], 4, 1, 64, 1, 7, 2, 3), ([0, 16, 17, 160, 161], 8, 2, 128, 16, 4, 1, 2), ([700, 64, 650], 6, 3, 50, 24, 13, 1, 2),
     ([5000], 8, 8, 80, 2, 100, 0, 5), ([900], 2, 1, 256, 3, 299, 1, 1), ([9000, 8193], 2, 2, 17, 1, 33, 1, 1), ([300] * 70, 4, 4, 96, 5, 8, 3, 0),
-    ([40, 3], 4, 2, 33, 8, 2, 0, 2),
+    ([40, 3], 4, 2, 33, 8, 2, 0, 2), ([20000, 16385], 2, 1, 64, 1, 50, 1, 1), ([2049, 2048, 1025, 257, 256], 2, 1, 64, 1, 20, 0, 0),
 ])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_select(seen, H, Hkv, d, page, keep, first, last, dtype):
@@ -279,6 +279,28 @@ CASES = [
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_attention_paged(seen, H, Hkv, d, page, dtype):
     Cache(len(seen) + d, seen, H, Hkv, d, page, dtype, layout="row" if d % 3 else "head").check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,Hkv,d,page", [(4, 1, 64, 16), (2, 2, 128, 16), (6, 2, 80, 24), (16, 2, 64, 64), (3, 1, 256, 7)])
+def test_attention_tokens_of_one_request(H, Hkv, d, page, dtype):
+    """Neighbouring tokens of a request read its rows together, whatever each sees; rows in any order, tokens of no request among them."""
+    rows = [0] * 4 + [1] * 4 + [2] * 3 + [3] * 7 + [1, 2, -1, -1, 3, 3, 0, 0, 0, 2] + [4] * 17
+    rng = np.random.default_rng(H)
+    seen = [int(x) for x in np.concatenate([np.arange(97, 101), rng.integers(0, 300, len(rows) - 4)])]
+    seen[7] = seen[12] = 0
+    Cache(H + d, seen, H, Hkv, d, page, dtype, rows=rows).check()
+    Cache(H + d, [5 + i for i in range(16)], H, Hkv, d, page, dtype, rows=[0] * 16).check()
+    # every token of one long row, cut into many parts
+    Cache(H + d, [3000 + i for i in range(9)], H, Hkv, d, page, dtype, rows=[0] * 9).check()
+
+
+def test_attention_logits_far_below_zero():
+    for dtype in (torch.float32, torch.bfloat16):
+        c = Cache(16, [300, 40], 4, 2, 64, 16, dtype)
+        c.k.copy_(-c.k.abs() - 20)
+        c.q.copy_(c.q.abs() + 20)
+        c.check(scale=1.0)                                               # products of about -28000
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
