@@ -43,6 +43,10 @@ __device__ __forceinline__ int seen_of(const Tokens &t, const Tables &tab, int p
     return (int)min((long long)max(s, 0), (long long)tab.width * page);
 }
 
+__device__ __forceinline__ long long quotient(long long a, long long b)   // of numbers that are not negative
+{
+    return (a | b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
+}
 __device__ __forceinline__ int saturated(long long x) { return (int)min(x, (long long)INT_MAX); }
 // Sum over the block, for all threads (8 warps of shared memory).
 __device__ __forceinline__ long long block_sum(long long x, long long *warps)
@@ -82,44 +86,100 @@ struct Share {
     long long lo, hi, share, rest;   // [lo, hi) of the line; every warp's share; lo is `rest` behind the begin of token `row`
     int row;
 };
-// False: nothing.  All threads call it.
-template <int THREADS, typename Cost> __device__ __forceinline__ bool deal(int M, Cost cost, int parts, int me, int least, Share &s)
+__device__ __forceinline__ long long lanes_up_to(int x)   // sum over the lanes up to this one
 {
-    __shared__ long long before[THREADS], warps[THREADS / 32];
-    const int lane = threadIdx.x & 31, each = (M + THREADS - 1) / THREADS;
-    const int i0 = (int)min((long long)M, threadIdx.x * (long long)each), i1 = min(M, i0 + each);
-    long long n = 0, all;
-    for (int i = i0; i < i1; ++i) n += cost(i);
-    before[threadIdx.x] = block_before(n, warps, all);
-    s.share = max((all + parts - 1) / parts, (long long)least);
-    s.lo = me * s.share;
-    s.hi = min(s.lo + s.share, all);
-    __syncthreads();
-    if (s.lo >= s.hi) return false;
-    int chunk = -1;   // the thread that summed the token which lo lies in
-#pragma unroll
-    for (int j = 0; j < THREADS / 32; ++j) chunk += __popc(__ballot_sync(~0u, before[j * 32 + lane] <= s.lo));
-    s.rest = s.lo - before[chunk];
-    s.row = chunk * each;
-    if (each == 1) return true;
-    for (; s.row < M; s.row += 32) {   // 32 tokens at a time
-        const long long c = s.row + lane < M ? cost(s.row + lane) : 0;
-        long long up = c;
+    const int lane = threadIdx.x & 31;
+    if (!__any_sync(~0u, x >> 26)) {
 #pragma unroll
         for (int w = 1; w < 32; w <<= 1) {
-            const long long y = __shfl_up_sync(~0u, up, w);
-            if (lane >= w) up += y;
+            const int y = __shfl_up_sync(~0u, x, w);
+            if (lane >= w) x += y;
         }
-        const unsigned behind = __ballot_sync(~0u, up > s.rest);
-        if (behind) {
-            const int k = __ffs(behind) - 1;
-            s.rest -= __shfl_sync(~0u, up - c, k);
-            s.row += k;
-            return true;
-        }
-        s.rest -= __shfl_sync(~0u, up, 31);
+        return x;
     }
-    return false;   // (not with lengths that stay as they are)
+    long long up = x;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+        const long long y = __shfl_up_sync(~0u, up, w);
+        if (lane >= w) up += y;
+    }
+    return up;
+}
+// load(base): what cost() needs of the tokens from base (a multiple of 32) on, one in a lane; cost(window): what each of the `units` units of a lane's token
+// costs, for all lanes of a warp (0 behind the last).  The last window that cost() gets is the one that `row` lies in.  False: nothing.  All threads call it.
+template <int THREADS, typename Load, typename Cost>
+__device__ __forceinline__ bool deal(int M, int units, Load load, Cost cost, int parts, int me, int least, Share &s)
+{
+    constexpr int WARPS = THREADS / 32, KEPT = 256;   // KEPT: windows of 32 tokens whose sums are kept (8192 tokens; beyond them they are formed again)
+    __shared__ long long sums[KEPT], others[WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, windows = (M + 31) / 32;
+    long long all, up = 0;
+    int c = 0;
+    if (windows == 1) {   // each warp for itself
+        c = cost(load(0));
+        up = lanes_up_to(c);
+        all = __shfl_sync(~0u, up, 31);
+    } else {
+        all = 0;
+        // (a loop, not copies of it: instructions that run once wait for their own way into the cache)
+        auto next = load(warp * 32);
+#pragma unroll 1
+        for (int w = warp; w < windows; w += WARPS) {
+            const auto now = next;
+            next = load((w + WARPS) * 32);
+            const int x = cost(now);
+            long long n;
+            if (!__any_sync(~0u, x >> 26)) {
+                n = __reduce_add_sync(~0u, x);
+            } else {
+                n = x;
+#pragma unroll
+                for (int d = 16; d; d >>= 1) n += __shfl_xor_sync(~0u, n, d);
+            }
+            if (lane == 0 && w < KEPT) sums[w] = n;
+            all += n;
+        }
+        if (lane == 0) others[warp] = all;
+        __syncthreads();
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) all += others[w];
+    }
+    all *= units;
+    s.share = max((long long)least, quotient(all + parts - 1, parts));
+    s.lo = me * s.share;
+    s.hi = min(s.lo + s.share, all);
+    if (s.lo >= s.hi) return false;
+    s.rest = s.lo;
+    s.row = 0;
+    if (windows > 1) {
+        for (int w0 = 0; w0 < min(windows, KEPT); w0 += 32) {   // 32 windows at a time
+            long long n = w0 + lane < min(windows, KEPT) ? sums[w0 + lane] * units : 0, x = n;
+#pragma unroll
+            for (int w = 1; w < 32; w <<= 1) {
+                const long long y = __shfl_up_sync(~0u, x, w);
+                if (lane >= w) x += y;
+            }
+            const unsigned behind = __ballot_sync(~0u, x > s.rest);
+            const int k = behind ? __ffs(behind) - 1 : 31;
+            s.rest -= __shfl_sync(~0u, behind ? x - n : x, k);
+            s.row = (w0 + k + !behind) * 32;
+            if (behind) break;
+        }
+        for (;; s.row += 32) {   // (more than one round only behind the sums that are kept)
+            if (s.row >= M) return false;   // (not with lengths that stay as they are)
+            c = cost(load(s.row));
+            up = lanes_up_to(c);
+            const long long n = __shfl_sync(~0u, up, 31) * units;
+            if (n > s.rest) break;
+            s.rest -= n;
+        }
+    }
+    const unsigned behind = __ballot_sync(~0u, up * units > s.rest);
+    const int k = __ffs(behind) - 1;
+    s.rest -= __shfl_sync(~0u, up - c, k) * units;
+    s.row += k;
+    return behind != 0;
 }
 // The last r in [0, n) with ptr[r] <= x < ptr[r + 1]; ptr[0] = 0 <= x < ptr[n].
 __device__ __forceinline__ int segment_of(const int *ptr, int n, int x)
@@ -466,58 +526,74 @@ __device__ __forceinline__ unsigned long long ordered(double x)
 // Scores of the pages of tokens that see more than a list holds.  Sums are formed in 64 bits: the result is a choice, and between two close scores sums of
 // 32 bits would choose by their order.  The blocks of 32 pages of all tokens and key heads are dealt to the warps in equal shares; the sum of the group's
 // queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, eight instructions at a time.
-constexpr int kScorePages = 32;
+constexpr int kScorePages = 32, kScoreThreads = 128, kScoreCTAs = 4;   // CTAs of an SM
 template <typename T, int LANES, int HALVES>
-__global__ void __launch_bounds__(kThreads) paged_score_kernel(const SelectArgs<T> a)
+__global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) paged_score_kernel(const SelectArgs<T> a)
 {
     constexpr int N = 16 / sizeof(T), AT_ONCE = 8, STEP = 32 / LANES, BATCH = AT_ONCE * STEP;   // pages of an instruction, of a batch
-    const int lane = threadIdx.x & 31, me = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), group = a.heads / a.kv_heads;
+    const int lane = threadIdx.x & 31, me = blockIdx.x * (kScoreThreads / 32) + (threadIdx.x >> 5), group = a.heads / a.kv_heads;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const auto blocks_of = [&](int i) {
         const int n = pages_seen(a, i);
         return n > a.keep ? (n + kScorePages - 1) / kScorePages : 0;
     };
     Share w;
-    if (!deal<kThreads>(a.M, [&](int i) { return (long long)blocks_of(i) * a.kv_heads; }, gridDim.x * (kThreads / 32), me, 1, w)) return;
-    int i = w.row, n = pages_seen(a, i), blocks = blocks_of(i), g = (int)(w.rest / blocks), b = (int)(w.rest - (long long)g * blocks);
+    const auto load = [&](int base) { return base + lane < a.M ? blocks_of(base + lane) : 0; };
+    if (!deal<kScoreThreads>(a.M, a.kv_heads, load, [](int blocks) { return blocks; }, gridDim.x * (kScoreThreads / 32), me, 1, w)) return;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    int i = w.row, n = pages_seen(a, i), blocks = (n + kScorePages - 1) / kScorePages, g = (int)w.rest / blocks, b = (int)w.rest - g * blocks;
     double q[HALVES][N];
     bool fresh = true;
-    for (long long left = w.hi - w.lo; left > 0; --left) {
+    const int e0 = lane % LANES * N;   // this lane's first element
+    for (int left = (int)(w.hi - w.lo); left > 0; --left) {
         const int p0 = b * kScorePages;
-        int held = p0 + lane < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p0 + lane] : -1;
-        if (fresh) {
+        const int held = p0 + lane < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p0 + lane] : -1;
+        const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int s) {
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int p = __shfl_sync(~0u, held, s + j * STEP + lane / LANES);
+                const T *mean = a.means.row(p, g, 0) + e0;
+#pragma unroll
+                for (int x = 0; x < HALVES; ++x) {
+                    c[j][x] = make_uint4(0, 0, 0, 0);
+                    if ((unsigned)p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(mean + x * 32 * N);
+                }
+            }
+        };
+        uint4 c[AT_ONCE][HALVES];
+        if (fresh) {   // the queries' loads first, four heads at once; the sums when the means are on their way
 #pragma unroll
             for (int x = 0; x < HALVES; ++x)
 #pragma unroll
                 for (int k = 0; k < N; ++k) q[x][k] = 0;
-            for (int h = 0; h < group; ++h) {
-                const T *from = a.q + i * a.q_ld + (g * group + h) * a.q_sh;
+            const T *from = a.q + i * a.q_ld + (long long)g * group * a.q_sh;
+            for (int h = 0; h < group; h += 4) {
+                Chunk<T> y[4][HALVES];
 #pragma unroll
-                for (int x = 0; x < HALVES; ++x) {
-                    const int e = (lane % LANES + x * 32) * N;
-                    Chunk<T> c;
-                    float f[N] = {};
-                    c.load(from, e, a.d, a.q_wide && e + N <= a.d);
-                    c.add_to(f);
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int k = 0; k < N; ++k) q[x][k] += f[k];
-                }
+                    for (int x = 0; x < HALVES; ++x) {
+                        y[k][x].u = make_uint4(0, 0, 0, 0);
+                        if (h + k < group) y[k][x].load(from + (h + k) * a.q_sh, e0 + x * 32 * N, a.d, a.q_wide && e0 + x * 32 * N + N <= a.d);
+                    }
+                if (h == 0) read(c, 0);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int x = 0; x < HALVES; ++x) {
+                        float f[N] = {};
+                        y[k][x].add_to(f);
+#pragma unroll
+                        for (int m = 0; m < N; ++m) q[x][m] += f[m];
+                    }
             }
             fresh = false;
+        } else {
+            read(c, 0);
         }
         unsigned long long *keys = a.keys + ((long long)i * a.kv_heads + g) * a.t.width;
         for (int s = 0; s < kScorePages && p0 + s < n; s += BATCH) {
-            uint4 c[AT_ONCE][HALVES];
-#pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                const int p = __shfl_sync(~0u, held, s + j * STEP + lane / LANES);
-#pragma unroll
-                for (int x = 0; x < HALVES; ++x) {
-                    const int e = (lane % LANES + x * 32) * N;
-                    c[j][x] = make_uint4(0, 0, 0, 0);
-                    if ((unsigned)p < (unsigned)a.means.pages && e < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(a.means.row(p, g, 0) + e);
-                }
-            }
+            if (s) read(c, s);
             double sum[AT_ONCE];
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j) {
@@ -526,9 +602,13 @@ __global__ void __launch_bounds__(kThreads) paged_score_kernel(const SelectArgs<
                 for (int x = 0; x < HALVES; ++x) {
                     float f[N] = {};
                     Chunk<T>{c[j][x]}.add_to(f);
+                    if (e0 + x * 32 * N + N > a.d) {   // what lies behind d may be anything
 #pragma unroll
-                    for (int k = 0; k < N; ++k)   // (what lies behind d may be anything)
-                        if ((lane % LANES + x * 32) * N + k < a.d) sum[j] += q[x][k] * f[k];
+                        for (int k = 0; k < N; ++k)
+                            if (e0 + x * 32 * N + k >= a.d) f[k] = 0.f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < N; ++k) sum[j] += q[x][k] * f[k];
                 }
             }
             // LANES lanes' sums of eight: halves of what is left are exchanged until each lane has one, which is then summed up

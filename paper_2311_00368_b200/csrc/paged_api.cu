@@ -10,12 +10,13 @@ namespace paged {
 inline b2sp_status launched() { return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA; }
 constexpr int kSMs = 148;
 
-// More shared memory than a launch gets unasked (48 KB with what the kernel has of its own).
+// More shared memory than a launch gets unasked (48 KB with what the kernel has of its own).  The kernels of a call all ask for the same split between
+// shared memory and cache: an SM changes it only when it is empty.
 template <typename K> bool allow_shared(K *kernel, size_t bytes)
 {
-    return bytes <= 40 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) == cudaSuccess &&
+           (bytes <= 40 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess);
 }
-
 // A launch that may begin before the one ahead of it has ended (the kernels wait for that themselves).
 template <typename K, typename... Args> bool launch_early(K *kernel, dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
 {
@@ -141,13 +142,13 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     a.q_wide = fits<T>(Q, ldq, shq, 16);
     const bool scored = t->width > keep;   // else no token sees more pages than a list holds
     if (scored) {
-        const unsigned grid = (unsigned)std::min((blocks + 7) / 8, 4ll * kSMs);
+        const unsigned grid = (unsigned)std::min((blocks + kScoreThreads / 32 - 1) / (kScoreThreads / 32), (long long)kSMs * kScoreCTAs);
         constexpr int N = 16 / sizeof(T);
         bool ok = false;
-        if (d <= 8 * N) ok = launch_early(paged_score_kernel<T, 8, 1>, grid, kThreads, 0, st, a);
-        else if (d <= 16 * N) ok = launch_early(paged_score_kernel<T, 16, 1>, grid, kThreads, 0, st, a);
-        else if (d <= 32 * N) ok = launch_early(paged_score_kernel<T, 32, 1>, grid, kThreads, 0, st, a);
-        else if constexpr (sizeof(T) == 4) ok = launch_early(paged_score_kernel<T, 32, 2>, grid, kThreads, 0, st, a);
+        if (d <= 8 * N) ok = launch_early(paged_score_kernel<T, 8, 1>, grid, kScoreThreads, 0, st, a);
+        else if (d <= 16 * N) ok = launch_early(paged_score_kernel<T, 16, 1>, grid, kScoreThreads, 0, st, a);
+        else if (d <= 32 * N) ok = launch_early(paged_score_kernel<T, 32, 1>, grid, kScoreThreads, 0, st, a);
+        else if constexpr (sizeof(T) == 4) ok = launch_early(paged_score_kernel<T, 32, 2>, grid, kScoreThreads, 0, st, a);
         if (!ok) return B2SP_ERR_CUDA;
     }
     // a warp holds 2048 keys
@@ -161,7 +162,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
 
 // Warps and workspace of an attention call.
 struct AttnPlan {
-    int nt, queries, blocks, warps;   // nt: eights of queries of a unit; blocks: units of a token and key head; warps: at most
+    int queries, blocks, warps;   // queries: of a unit; blocks: units of a token and key head; warps: at most
     size_t ml, part, bytes;
 };
 // together: tokens of a request that are likely to be neighbours (1 with lists or without `rows`).
@@ -169,8 +170,7 @@ template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d, lo
 {
     AttnPlan p;
     const int group = heads / kv_heads, w = d <= 64 ? 64 : d <= 128 ? 128 : 256;
-    p.nt = sizeof(T) == 2 && group * together > 8 ? 2 : 1;
-    p.queries = 8 * p.nt;
+    p.queries = sizeof(T) == 2 ? (group * together > 8 ? 16 : 8) : group * together > 4 ? 8 : 4;
     p.blocks = (group + p.queries - 1) / p.queries;
     p.warps = kSMs * kAttnWarps * (w == 64 ? Form<T, 64>::CTAS : w == 128 ? Form<T, 128>::CTAS : Form<T, 256>::CTAS);
     const size_t parts = 2ull * p.warps * p.queries;
@@ -180,15 +180,16 @@ template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d, lo
     return p;
 }
 
-template <typename T, int W, int NT> b2sp_status launch_attention(AttnArgs<T> &a, const AttnPlan &p, long long most_tiles, cudaStream_t st)
+template <typename T, int W, int Q> b2sp_status launch_attention(AttnArgs<T> &a, const AttnPlan &p, long long most_tiles, cudaStream_t st)
 {
     using F = Form<T, W>;
     const long long units = (long long)a.M * a.kv_heads * a.blocks, most_cost = most_tiles + units * kUnitCost;
     // no more CTAs than have a share, if every token sees all that it can
     const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps));
+    if (most_cost / (ctas * kAttnWarps) >= 1 << 30) return B2SP_ERR_UNSUPPORTED;   // (a warp counts its share in 32 bits)
     a.by_unit = units <= ctas * (long long)kAttnWarps;
-    const bool ok = a.page % F::ROWS == 0 ? launch_early(paged_attention_kernel<T, W, NT, true>, ctas, kAttnWarps * 32, F::SHARED, st, a)
-                                          : launch_early(paged_attention_kernel<T, W, NT, false>, ctas, kAttnWarps * 32, F::SHARED, st, a);
+    const bool ok = a.page % F::ROWS == 0 ? launch_early(paged_attention_kernel<T, W, Q, true>, ctas, kAttnWarps * 32, F::SHARED, st, a)
+                                          : launch_early(paged_attention_kernel<T, W, Q, false>, ctas, kAttnWarps * 32, F::SHARED, st, a);
     if (!ok) return B2SP_ERR_CUDA;
     // Few units have many parts each: sixteen warps for a query, else one.
     const unsigned joins = a.by_unit ? (unsigned)units : ctas * kAttnWarps, queries = std::min(a.pack * a.group, p.queries);
@@ -214,7 +215,7 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     if (d > 256 || (lists && (long long)keep * kp->page > INT_MAX) || (long long)M * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     constexpr long long most_stride = UINT_MAX / sizeof(T);
     for (const b2sp_pages *c : {kp, vp})
-        if (std::max({c->ld, c->stride_head, c->stride_page}) > most_stride) return B2SP_ERR_UNSUPPORTED;
+        if (std::max({c->ld, c->stride_head, c->stride_page, ldq, shq, ldo, sho, t->ld}) > most_stride) return B2SP_ERR_UNSUPPORTED;
     const AttnPlan p = attention_plan<T>(heads, kv_heads, d, rows && !lists && t->requests ? M / t->requests : 1);
     if ((long long)M * kv_heads * p.blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes) return B2SP_ERR_WORKSPACE;
@@ -222,20 +223,22 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     AttnArgs<T> a = {};
     a.t = tables(t);
     a.tok = Tokens{rows, seen};
-    a.q = Q; a.q_ld = ldq; a.q_sh = shq;
+    a.q = Q; a.q_ld = (unsigned)ldq; a.q_sh = (unsigned)shq;
     a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.page = kp->page;
     const auto side = [](const b2sp_pages *c) {
         return Side{static_cast<const char *>(c->data), (unsigned)(c->ld * sizeof(T)), (unsigned)(c->stride_head * sizeof(T)), (unsigned)(c->stride_page * sizeof(T))};
     };
     a.k = side(kp); a.v = side(vp); a.pages = kp->pages;
     a.lists = lists; a.keep = lists ? keep : 0; a.scale = scale;
-    a.out = O; a.out_ld = ldo; a.out_sh = sho; a.lse = lse;
+    a.out = O; a.out_ld = (unsigned)ldo; a.out_sh = (unsigned)sho; a.lse = lse;
     a.group = heads / kv_heads; a.blocks = p.blocks; a.by_page = Div(a.page);
     a.pack = 1;
     if (rows && !lists)
         while (a.pack * 2 * a.group <= p.queries) a.pack *= 2;
+    a.by_blocks = Div(p.blocks);
     a.by_heads = Div(a.pack > 1 ? a.group : p.queries);
-    a.q_pairs = fits<T>(Q, ldq, shq, 4); a.q_fours = fits<T>(Q, ldq, shq, 16); a.out_pairs = fits<T>(O, ldo, sho, 4);
+    a.pairs = fits<T>(Q, ldq, shq, 4) && fits<T>(O, ldo, sho, 4) && d % 2 == 0;
+    a.fours = fits<T>(Q, ldq, shq, 16) && d % 4 == 0;
     char *ws = static_cast<char *>(workspace);
     a.joins = reinterpret_cast<int4 *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
@@ -245,10 +248,9 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     const long long most = (long long)std::min<__int128>(tiles, 1ll << 40);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int w = d <= 64 ? 64 : d <= 128 ? 128 : 256;
-    if constexpr (sizeof(T) == 2) {
-        if (p.nt == 2) return w == 64 ? launch_attention<T, 64, 2>(a, p, most, st) : w == 128 ? launch_attention<T, 128, 2>(a, p, most, st) : launch_attention<T, 256, 2>(a, p, most, st);
-    }
-    return w == 64 ? launch_attention<T, 64, 1>(a, p, most, st) : w == 128 ? launch_attention<T, 128, 1>(a, p, most, st) : launch_attention<T, 256, 1>(a, p, most, st);
+    constexpr int MOST = sizeof(T) == 2 ? 16 : 8;
+    if (p.queries == MOST) return w == 64 ? launch_attention<T, 64, MOST>(a, p, most, st) : w == 128 ? launch_attention<T, 128, MOST>(a, p, most, st) : launch_attention<T, 256, MOST>(a, p, most, st);
+    return w == 64 ? launch_attention<T, 64, MOST / 2>(a, p, most, st) : w == 128 ? launch_attention<T, 128, MOST / 2>(a, p, most, st) : launch_attention<T, 256, MOST / 2>(a, p, most, st);
 }
 
 }  // namespace paged
@@ -334,7 +336,7 @@ extern "C" b2sp_status b2sp_paged_select_bf16(int M, int heads, int kv_heads, in
 extern "C" size_t b2sp_attention_paged_workspace_bytes(int M, int heads, int kv_heads, int d)
 {
     if (!token_args_ok(M, heads, kv_heads, d) || d > 256) return 0;
-    return std::max(attention_plan<float>(heads, kv_heads, d, 1).bytes, attention_plan<Bf16>(heads, kv_heads, d, INT_MAX).bytes);
+    return std::max(attention_plan<float>(heads, kv_heads, d, INT_MAX).bytes, attention_plan<Bf16>(heads, kv_heads, d, INT_MAX).bytes);
 }
 extern "C" b2sp_status b2sp_attention_paged(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long shq, const b2sp_pages *kp,
                                             const b2sp_pages *vp, const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists, int keep,

@@ -25,11 +25,11 @@ constexpr int kUnitCost = 4, kLeastCost = 8;
 
 // W: width class of d (64, 128, 256).
 template <typename T, int W> struct Form {
-    static constexpr int ROW = W * (int)sizeof(T), ROWS = ROW == 1024 ? 8 : 16;   // bytes of a row in shared memory; rows of a tile
+    static constexpr int ROW = W * (int)sizeof(T), ROWS = ROW == 1024 ? 8 : ROW == 128 ? 32 : 16;   // bytes of a row in shared memory; rows of a tile
     static constexpr int TILE = 2 * ROWS * ROW, RING = kStages * TILE;             // K's rows, then V's
     static constexpr int WEIGHTS = sizeof(T) == 4 ? 640 : 0;                       // fp32: a tile's weights
     static constexpr int SHARED = kAttnWarps * (RING + WEIGHTS);
-    static constexpr int CTAS = SHARED <= 56 * 1024 ? 4 : SHARED <= 113 * 1024 ? 2 : 1;   // of an SM
+    static constexpr int CTAS = SHARED <= 113 * 1024 ? 2 : 1;   // of an SM
 };
 
 struct Side {   // K or V: byte strides
@@ -40,45 +40,76 @@ template <typename T> struct AttnArgs {
     Tables t;
     Tokens tok;
     const T *q;
-    long long q_ld, q_sh;
+    unsigned q_ld, q_sh;
     int M, heads, kv_heads, d, page, pages, group, blocks, pack;   // blocks: of a key head's queries; pack: most tokens of a unit, a power of two
     Side k, v;
     const int *lists;        // [M][kv_heads][keep] or NULL
     int keep;
     float scale;
-    Div by_page, by_heads;   // by_heads: heads of one token in a unit
-    bool q_pairs, q_fours, out_pairs, by_unit;        // by_unit: `joins` are indexed by unit, else by warp
+    Div by_page, by_heads, by_blocks;   // by_heads: heads of one token in a unit
+    bool pairs, fours, by_unit;   // pairs: Q and O begin on four bytes and d is even; fours: Q on sixteen, d a multiple of four; by_unit: `joins` are indexed by unit, else by warp
     T *out;
-    long long out_ld, out_sh;
+    unsigned out_ld, out_sh;
     float *lse;
     float *part;             // two of [queries of a unit][W] per warp: of the unit it begins in the middle of, of the one it leaves in the middle
     float2 *part_ml;         // (maximum to base 2, sum) of each
     int4 *joins;             // (unit, first warp, last warp, queries) of units in several shares; first warp -1: none
 };
 
-// The tokens of a unit: `n` from token i on (0: token i belongs to the unit of one before it).  They are of one request, and do not cross multiples of
-// `pack`.  most, least: of the positions that they see.
+// The tokens of a unit: `n` from token i on.  They are of one request, and do not cross multiples of `pack`.  most, least: of the positions that they see.
 struct Pack { int n, most, least; };
-template <typename T> __device__ __forceinline__ Pack pack_of(const AttnArgs<T> &a, int i)
+// 32 tokens from a multiple of 32 on, one in a lane (`pack` is a power of two below 32, so units do not cross windows).
+struct Window { int base, row, seen; };
+template <typename T> __device__ __forceinline__ Window window_of(const AttnArgs<T> &a, int base, int lane)
+{
+    Window w;
+    const int i = base + lane;
+    w.base = base;
+    w.row = INT_MIN;   // (no token)
+    w.seen = 0;
+    if (i < a.M) {
+        const int s = a.tok.seen[i];
+        w.row = row_of(a.tok, i);
+        w.seen = (unsigned)w.row < (unsigned)a.t.requests ? (int)min((long long)max(s, 0), (long long)a.t.width * a.page) : 0;
+    }
+    return w;
+}
+template <typename T> __device__ __forceinline__ Pack pack_of(const AttnArgs<T> &a, const Window &w, int i, int lane)
 {
     Pack p;
-    p.most = p.least = seen_of(a.tok, a.t, a.page, i);
+    const int at = i - w.base, row = __shfl_sync(~0u, w.row, at);
     p.n = 1;
-    if (a.pack == 1) return p;
-    const int r = a.tok.rows[i], end = min((i & -a.pack) + a.pack, a.M);   // (packs of several tokens: rows are given)
-    if ((i & (a.pack - 1)) && a.tok.rows[i - 1] == r) { p.n = 0; return p; }
-    while (i + p.n < end && a.tok.rows[i + p.n] == r) {
-        const int s = seen_of(a.tok, a.t, a.page, i + p.n);
-        p.most = max(p.most, s);
-        p.least = min(p.least, s);
-        ++p.n;
+    p.most = p.least = __shfl_sync(~0u, w.seen, at);
+    if (a.pack > 1) {
+        const unsigned same = __ballot_sync(~0u, w.row == row) >> at;
+        p.n = min(min(same == ~0u ? 32 : __ffs(~same) - 1, a.pack - (at & (a.pack - 1))), a.M - i);
+        const bool in = lane >= at && lane < at + p.n;
+        p.most = __reduce_max_sync(~0u, in ? w.seen : 0);
+        p.least = __reduce_min_sync(~0u, in ? w.seen : INT_MAX);
     }
     return p;
 }
-template <int ROWS, typename T> __device__ __forceinline__ int tiles_of(const AttnArgs<T> &a, const Pack &p)
+template <int ROWS, typename T> __device__ __forceinline__ int tiles_of(const AttnArgs<T> &a, int most)
 {
-    const int n = a.lists && p.most ? a.keep * a.page : p.most;
+    const int n = a.lists && most ? a.keep * a.page : most;
     return max(1, (int)((n + (ROWS - 1ll)) / ROWS));   // (tokens that see nothing have a tile of nothing)
+}
+// What each unit of a window's token `lane` costs: nothing if the token belongs to the units of one before it.
+template <int ROWS, typename T> __device__ __forceinline__ int cost_of(const AttnArgs<T> &a, const Window &w, int lane)
+{
+    int most = w.seen;
+    bool begins = true;
+    if (a.pack > 1) {
+        const int ahead = __shfl_up_sync(~0u, w.row, 1);
+        begins = (lane & (a.pack - 1)) == 0 || ahead != w.row;
+        const unsigned begin = __ballot_sync(~0u, begins);
+        const int mine = 31 - __clz(begin & (2u << lane) - 1);   // where this lane's unit begins
+        for (int d = 1; d < a.pack; d *= 2) {
+            const int x = __shfl_down_sync(~0u, most, d), its = __shfl_down_sync(~0u, mine, d);
+            if (lane + d < 32 && its == mine) most = max(most, x);
+        }
+    }
+    return w.base + lane < a.M && begins ? tiles_of<ROWS>(a, most) + kUnitCost : 0;
 }
 
 // 16 bytes, the first n of them from memory and zeros behind.
@@ -88,90 +119,121 @@ __device__ __forceinline__ void copy16(unsigned to, const void *from, int n)
 }
 __device__ __forceinline__ unsigned long long times(int a, unsigned b) { return (unsigned long long)(unsigned)a * b; }
 
-// The rows of a unit's tiles.  ALIGNED: pages are whole tiles, so a tile lies in one page and its rows are a stride apart; else lane r finds row r.
-template <typename T, int W, bool ALIGNED> struct Rows {
+// A piece of a unit: tiles [first, last) of `tiles`.
+struct Piece {
+    int i, unit, first, last, tiles;
+    Pack p;
+};
+
+// The rows of a piece's tiles on their way into shared memory.  ALIGNED: pages are whole tiles, so a tile lies in one page and its rows are a stride apart;
+// a lane looks up a tile, 32 at a time; else it looks up a row, the 2 (4) tiles of 32 rows at a time.  The next lot is looked up in two steps, the index in
+// the table and the page, while the tiles of this one are taken.
+template <typename T, int W, bool ALIGNED> struct Feed {
     using F = Form<T, W>;
     static constexpr int N = 16 / sizeof(T), CHUNKS = F::ROW / 16, PER = F::ROWS * CHUNKS / 32;   // elements of 16 bytes; of a row; copies of a lane
     static constexpr int AT_ONCE = CHUNKS > 32 ? 1 : 32 / CHUNKS;                                   // rows of a warp's copy (1024 bytes: half of one)
+    static constexpr int LOT = ALIGNED ? 32 : 32 / F::ROWS;                                         // tiles
+    static constexpr unsigned ALL = ~0u >> (32 - F::ROWS);
     const AttnArgs<T> &a;
     const int *table, *list;
     const char *k, *v;
-    int seen, n, lane, size0, size1;   // n: positions of the unit's line; bytes that this lane's copies take (rows of 1024 bytes: two kinds)
+    int lane, seen, n, tile, last, lot;   // n: positions of the unit's line; the next tile to copy, the piece's end; the lot's first tile
+    int held, row, left;                  // of the lot: page (-1: nothing there), row of it, ALIGNED: rows that are there
+    int next_index, next_row, next_held;  // of the next lot
+    bool looked_up;                       // next_held is known
+    int size0, size1;                     // bytes that this lane's copies take (rows of 1024 bytes: two kinds)
     unsigned place;
 
-    __device__ __forceinline__ Rows(const AttnArgs<T> &a_, int i, int g, int seen_, int lane_) : a(a_), seen(seen_), lane(lane_)
+    __device__ __forceinline__ Feed(const AttnArgs<T> &a_, int lane_) : a(a_), lane(lane_)
     {
-        table = a.t.entries + (seen ? row_of(a.tok, i) * a.t.ld : 0);
-        list = a.lists ? a.lists + ((long long)i * a.kv_heads + g) * a.keep : nullptr;
-        n = seen == 0 ? 0 : list ? a.keep * a.page : seen;
-        const int row = lane / CHUNKS, chunk = lane % CHUNKS;
+        const int r = lane / CHUNKS, chunk = lane % CHUNKS;
         size0 = min(max((a.d - chunk * N) * (int)sizeof(T), 0), 16);
         size1 = CHUNKS > 32 ? min(max((a.d - (lane + 32) * N) * (int)sizeof(T), 0), 16) : size0;
+        // bfloat16: a row's 16-byte pieces are turned by the row, so that eight rows' pieces at one place lie in different banks
+        place = r * F::ROW + (sizeof(T) == 2 ? chunk ^ r : chunk) * 16;
+        tile = last = 0;
+    }
+    __device__ __forceinline__ void index(int first)   // of the next lot, from tile `first` on
+    {
+        const unsigned p = ALIGNED ? ((unsigned)first + lane) * F::ROWS : (unsigned)first * F::ROWS + lane;
+        next_index = -1;
+        next_row = 0;
+        if (p < (unsigned)n) {
+            next_index = (int)a.by_page(p);
+            next_row = (int)p - next_index * a.page;
+            if (list) next_index = list[next_index];
+        }
+        looked_up = false;
+    }
+    __device__ __forceinline__ void look_up()
+    {
+        if (looked_up) return;
+        if (list && (next_index < 0 || next_index * (long long)a.page + next_row >= seen)) next_index = -1;
+        next_held = next_index < 0 ? -1 : table[next_index];
+        looked_up = true;
+    }
+    __device__ __forceinline__ void begin(const Piece &x, int request)
+    {
+        const int g = (int)a.by_blocks((unsigned)x.unit);
+        seen = x.p.most;
+        table = a.t.entries + (seen ? times(request, (unsigned)a.t.ld) : 0);
+        list = a.lists ? a.lists + times(x.i * a.kv_heads + g, a.keep) : nullptr;
+        n = seen == 0 ? 0 : list ? a.keep * a.page : seen;
         k = a.k.data + times(g, a.k.sh);
         v = a.v.data + times(g, a.v.sh);
         if (ALIGNED) {   // (what a lane does not read is not pointed to either)
-            k += times(row, a.k.ld);
-            v += times(row, a.v.ld);
+            k += times(lane / CHUNKS, a.k.ld);
+            v += times(lane / CHUNKS, a.v.ld);
         }
-        k += size0 ? chunk * 16 : 0;
-        v += size0 ? chunk * 16 : 0;
-        // bfloat16: a row's 16-byte pieces are turned by the row, so that eight rows' pieces at one place lie in different banks
-        place = row * F::ROW + (sizeof(T) == 2 ? chunk ^ row : chunk) * 16;
+        k += size0 ? lane % CHUNKS * 16 : 0;
+        v += size0 ? lane % CHUNKS * 16 : 0;
+        tile = x.first;
+        last = x.last;
+        lot = x.first - LOT;   // (the next one begins with the piece)
+        index(x.first);
     }
-    // In three steps, a tile apart, so that nothing waits for them: the page's index in the table, the page, the copies.
-    struct At { int c, r, held; };   // index in the table (-1: nothing is there), row of the page (ALIGNED: the tile's first), page
-    __device__ __forceinline__ At index(int tile) const
-    {
-        At x;
-        const unsigned p = (unsigned)tile * F::ROWS + (ALIGNED ? 0 : lane % F::ROWS);
-        x.c = -1; x.r = 0; x.held = -1;
-        if (p < (unsigned)n) {
-            x.c = (int)a.by_page(p);
-            x.r = (int)p - x.c * a.page;
-            if (list) x.c = list[x.c];
-        }
-        return x;
-    }
-    __device__ __forceinline__ void page(At &x) const
-    {
-        if (list && (x.c < 0 || x.c * (long long)a.page + x.r >= seen)) x.c = -1;
-        x.held = x.c < 0 ? -1 : table[x.c];
-    }
+    __device__ __forceinline__ bool ready() const { return tile - lot < LOT || looked_up; }
     static __device__ __forceinline__ unsigned to_of(unsigned to, unsigned place, int i)   // of copy i
     {
         if (CHUNKS > 32) return to + (i / 2) * F::ROW + (i & 1) * 512 + place;
         return to + i * AT_ONCE * F::ROW + (sizeof(T) == 2 ? place ^ ((i * AT_ONCE & 7) * 16) : place);
     }
-    // Begins the copies of a tile; which of its rows are there.
-    __device__ __forceinline__ unsigned copy(const At &x, unsigned to) const
+    // Begins the copies of the next tile; which of its rows are there.
+    __device__ __forceinline__ unsigned copy(unsigned to)
     {
-        constexpr unsigned ALL = (1u << F::ROWS) - 1;
-        const bool on = (unsigned)x.held < (unsigned)a.pages;
+        if (tile - lot == LOT) {   // a new lot
+            look_up();
+            lot = tile;
+            held = (unsigned)next_held < (unsigned)a.pages ? next_held : -1;
+            row = next_row;
+            if (ALIGNED) left = held < 0 ? 0 : min(seen - (next_index * a.page + next_row), F::ROWS);
+            if (tile + LOT < last) index(tile + LOT);
+        }
+        const int at = tile++ - lot;
         if (ALIGNED) {
-            if (!on) return 0;
-            const int rows = seen - (x.c * a.page + x.r);   // (c * page + r < seen)
-            const char *kr = k + times(x.held, a.k.sp) + times(x.r, a.k.ld), *vr = v + times(x.held, a.v.sp) + times(x.r, a.v.ld);
+            const int rows = __shfl_sync(~0u, left, at), page = __shfl_sync(~0u, held, at), first = __shfl_sync(~0u, row, at);
+            if (rows == 0) return 0;
+            const char *kr = k + times(page, a.k.sp) + times(first, a.k.ld), *vr = v + times(page, a.v.sp) + times(first, a.v.ld);
             const unsigned long long k_step = (unsigned long long)a.k.ld * AT_ONCE, v_step = (unsigned long long)a.v.ld * AT_ONCE;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int row = CHUNKS > 32 ? i / 2 : i * AT_ONCE + lane / CHUNKS, half = CHUNKS > 32 ? i & 1 : 0;
-                const int whole = half ? size1 : size0, size = row < rows ? whole : 0, more = half && size1 ? 512 : 0;
+                const int r = CHUNKS > 32 ? i / 2 : i * AT_ONCE + lane / CHUNKS, half = CHUNKS > 32 ? i & 1 : 0;
+                const int size = r < rows ? (half ? size1 : size0) : 0, more = half && size1 ? 512 : 0;
                 copy16(to_of(to, place, i), kr + more, size);
                 copy16(to_of(to, place, i) + F::ROWS * F::ROW, vr + more, size);
                 if (CHUNKS <= 32 || half) { kr += k_step; vr += v_step; }
             }
-            return rows >= F::ROWS ? ALL : (1u << rows) - 1;
+            return ALL >> (F::ROWS - rows);
         } else {
-            const unsigned there = __ballot_sync(~0u, on) & ALL;
+            const unsigned there = __ballot_sync(~0u, held >= 0) >> (at * F::ROWS & 31) & ALL;
             if (!there) return 0;
-            // lanes below 16 find K's rows, the others V's
-            const unsigned long long mine = !on ? 0 : lane < 16 ? times(x.held, a.k.sp) + times(x.r, a.k.ld) : times(x.held, a.v.sp) + times(x.r, a.v.ld);
+            const unsigned long long at_k = held < 0 ? 0 : times(held, a.k.sp) + times(row, a.k.ld), at_v = held < 0 ? 0 : times(held, a.v.sp) + times(row, a.v.ld);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int row = CHUNKS > 32 ? i / 2 : i * AT_ONCE + lane / CHUNKS, half = CHUNKS > 32 ? i & 1 : 0;
-                const int size = there >> row & 1 ? (half ? size1 : size0) : 0, more = half && size1 ? 512 : 0;
-                copy16(to_of(to, place, i), k + __shfl_sync(~0u, mine, row) + more, size);
-                copy16(to_of(to, place, i) + F::ROWS * F::ROW, v + __shfl_sync(~0u, mine, row + 16) + more, size);
+                const int r = CHUNKS > 32 ? i / 2 : i * AT_ONCE + lane / CHUNKS, half = CHUNKS > 32 ? i & 1 : 0;
+                const int size = there >> r & 1 ? (half ? size1 : size0) : 0, more = half && size1 ? 512 : 0;
+                copy16(to_of(to, place, i), k + __shfl_sync(~0u, at_k, at * F::ROWS + r) + more, size);
+                copy16(to_of(to, place, i) + F::ROWS * F::ROW, v + __shfl_sync(~0u, at_v, at * F::ROWS + r) + more, size);
             }
             return there;
         }
@@ -208,9 +270,9 @@ template <typename T> struct Queries {
         token = i + j;
         head = first + c - j * (int)a.by_heads.d;
     }
-    __device__ __forceinline__ const T *query(int c) const { int t, h; of(c, t, h); return a.q + t * a.q_ld + h * a.q_sh; }
-    __device__ __forceinline__ T *out(int c) const { int t, h; of(c, t, h); return a.out + t * a.out_ld + h * a.out_sh; }
-    __device__ __forceinline__ float *lse(int c) const { int t, h; of(c, t, h); return a.lse + (long long)t * a.heads + h; }
+    __device__ __forceinline__ const T *query(int c) const { int t, h; of(c, t, h); return a.q + (times(t, a.q_ld) + times(h, a.q_sh)); }
+    __device__ __forceinline__ T *out(int c) const { int t, h; of(c, t, h); return a.out + (times(t, a.out_ld) + times(h, a.out_sh)); }
+    __device__ __forceinline__ float *lse(int c) const { int t, h; of(c, t, h); return a.lse + (t * a.heads + h); }
     __device__ __forceinline__ int sees(int c) const
     {
         if (c >= n) return INT_MAX;
@@ -228,34 +290,59 @@ constexpr float kAhead = 8.f;   // the reference of the exponentials follows the
 // the lower part would make 0 * inf or inf - inf of it, so a unit whose sums are not finite is taken again with the upper part alone.
 template <int W, int NT> struct Tile16 {
     static constexpr int QUERIES = 8 * NT, KS = W / 16;
-    unsigned q[KS][NT][2];
+    static constexpr bool EARLY = W < 256;   // a unit's queries are loaded while the one before it is taken (wider ones would not fit)
+    unsigned q[KS][NT][2], early[EARLY ? KS : 1][NT][2];
     float o[KS][NT][4];       // [columns 16 x ..][queries 8 x ..]: columns g, g + 8 (pairs), queries 2 t, 2 t + 1
     float base[NT][2], ahead[NT][2], sum[NT][2];   // of queries 2 t, 2 t + 1; ahead: by how much a logit may exceed base (-inf: none has been met)
     int sees[NT][2];
     bool lower;
 
-    __device__ __forceinline__ void begin(const Queries<Bf16> &u, int lane, bool alike)
+    static __device__ __forceinline__ void load(const Queries<Bf16> &u, int lane, unsigned (&to)[KS][NT][2])
     {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
             const int c = m * 8 + g;
-            const Bf16 *p = c < u.n ? u.query(c) : nullptr;
+            const Bf16 *p = u.query(c < u.n ? c : 0);
+            const int d = c < u.n ? u.a.d : 0;
+            if (u.a.pairs) {   // (the same for all: no branches around single loads)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int e = s * 16 + x * 8 + t * 2;
+                        to[s][m][x] = e < d ? *reinterpret_cast<const unsigned *>(p + e) : 0;
+                    }
+            } else {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int e = s * 16 + x * 8 + t * 2;
+                        const unsigned y = e < d ? p[e].bits : 0, z = e + 1 < d ? p[e + 1].bits : 0;
+                        to[s][m][x] = y | z << 16;
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ void look_ahead(const Queries<Bf16> &u, int lane) { if constexpr (EARLY) load(u, lane, early); }
+    // at_once: nothing was loaded early
+    __device__ __forceinline__ void begin(const Queries<Bf16> &u, int lane, bool alike, bool at_once)
+    {
+        if (EARLY && !at_once) {
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int e = s * 16 + x * 8 + t * 2;
-                    unsigned y = 0;
-                    if (p) {
-                        if (u.a.q_pairs && e + 1 < u.a.d) y = *reinterpret_cast<const unsigned *>(p + e);
-                        else y = (e < u.a.d ? p[e].bits : 0) | (unsigned)(e + 1 < u.a.d ? p[e + 1].bits : 0) << 16;
-                    }
-                    q[s][m][x] = y;
-                }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) sees[m][e] = alike ? INT_MAX : u.sees(m * 8 + 2 * t + e);
+                for (int m = 0; m < NT; ++m) { q[s][m][0] = early[EARLY ? s : 0][m][0]; q[s][m][1] = early[EARLY ? s : 0][m][1]; }
+        } else {
+            load(u, lane, q);
         }
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) sees[m][e] = alike ? INT_MAX : u.sees(m * 8 + 2 * (lane & 3) + e);
+        lower = true;
+        clear();
     }
     __device__ __forceinline__ void clear()
     {
@@ -268,49 +355,66 @@ template <int W, int NT> struct Tile16 {
         }
     }
     // there: the tile's rows that are there; first: the position of its row 0, or -1 if all queries see all of them.
-    __device__ __forceinline__ void take(unsigned at, unsigned there, int first, float scale2, int lane, float *)
+    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, float *)
     {
         using F = Form<Bf16, W>;
-        float x[NT][4] = {}, y[NT][4] = {};   // two sums, so that half as many products wait for one another
+        constexpr int H = F::ROWS / 16, SUMS = H == 1 ? 2 : 1;   // sixteens of rows; sums of a product (so that few products wait for one another)
+        const unsigned at = (unsigned)__cvta_generic_to_shared(tile);
+        float x[H][NT][4] = {};
         {
+            float y[H][NT][4] = {};
             const int row = lane & 15;
             const unsigned from = at + row * F::ROW, turn = ((lane >> 4) ^ (row & 7)) * 16;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                unsigned k[4];
-                load_matrices(k, from + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
+            for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int m = 0; m < NT; ++m) mma_bf16(s & 1 ? y[m] : x[m], k, q[s][m][0], q[s][m][1]);
+                for (int h = 0; h < H; ++h) {
+                    unsigned k[4];
+                    load_matrices(k, from + h * 16 * F::ROW + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) mma_bf16(s % SUMS ? y[h][m] : x[h][m], k, q[s][m][0], q[s][m][1]);
+                }
+            if (SUMS == 2) {
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[0][m][e] += y[0][m][e];
             }
         }
         const int g = lane >> 2;
         bool move = false;
 #pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[m][e] += y[m][e];
-                x[m][e] = fmaf(x[m][e], scale2, -base[m][e & 1]);
-            }
-        if (there != 0xffffu || first >= 0) {
+        for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = e < 2 ? g : g + 8;
-                    if (!(there >> row & 1) || (first >= 0 && first + row >= sees[m][e & 1])) x[m][e] = -CUDART_INF_F;
-                }
+                for (int e = 0; e < 4; ++e) x[h][m][e] = fmaf(x[h][m][e], scale2, -base[m][e & 1]);
+        if (there != ~0u >> (32 - F::ROWS) || first >= 0) {
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int row = h * 16 + (e < 2 ? g : g + 8);
+                        if (!(there >> row & 1) || (first >= 0 && first + row >= sees[m][e & 1])) x[h][m][e] = -CUDART_INF_F;
+                    }
         }
+        float most[NT][2];
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) move |= fmaxf(x[m][e], x[m][e + 2]) > ahead[m][e];
+            for (int e = 0; e < 2; ++e) {
+                most[m][e] = fmaxf(x[0][m][e], x[0][m][e + 2]);
+                if (H == 2) most[m][e] = fmaxf(most[m][e], fmaxf(x[H - 1][m][e], x[H - 1][m][e + 2]));
+                move |= most[m][e] > ahead[m][e];
+            }
         if (__any_sync(~0u, move)) {
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float by = fmaxf(x[m][e], x[m][e + 2]);
+                    float by = most[m][e];
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) by = fmaxf(by, __shfl_xor_sync(~0u, by, w));
                     float fall = 1.f;
@@ -318,40 +422,44 @@ template <int W, int NT> struct Tile16 {
                     else if (ahead[m][e] == kAhead) fall = attn::ex2(-(by = fmaxf(by, 0.f)));
                     else ahead[m][e] = kAhead;   // the first logit, which may lie far below 0
                     base[m][e] += by;
-                    x[m][e] -= by;
-                    x[m][e + 2] -= by;
+#pragma unroll
+                    for (int h = 0; h < H; ++h) { x[h][m][e] -= by; x[h][m][e + 2] -= by; }
                     sum[m][e] *= fall;
 #pragma unroll
                     for (int s = 0; s < KS; ++s) { o[s][m][e] *= fall; o[s][m][e + 2] *= fall; }
                 }
         }
-        unsigned high[NT][2], low[NT][2];
+        unsigned high[H][NT][2], low[H][NT][2];
 #pragma unroll
-        for (int m = 0; m < NT; ++m) {
+        for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[m][e] = attn::ex2(x[m][e]);
-                sum[m][e & 1] += x[m][e];
+            for (int m = 0; m < NT; ++m) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[h][m][e] = attn::ex2(x[h][m][e]);
+                    sum[m][e & 1] += x[h][m][e];
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const unsigned u = attn::bf16x2(x[h][m][2 * j], x[h][m][2 * j + 1]);
+                    high[h][m][j] = transposed(u);
+                    low[h][m][j] = transposed(attn::bf16x2(x[h][m][2 * j] - __uint_as_float(u << 16), x[h][m][2 * j + 1] - __uint_as_float(u & 0xffff0000u)));
+                }
             }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const unsigned u = attn::bf16x2(x[m][2 * j], x[m][2 * j + 1]);
-                high[m][j] = transposed(u);
-                low[m][j] = transposed(attn::bf16x2(x[m][2 * j] - __uint_as_float(u << 16), x[m][2 * j + 1] - __uint_as_float(u & 0xffff0000u)));
-            }
-        }
         const int row = (lane >> 4) * 8 + (lane & 7);
         const unsigned from = at + (F::ROWS + row) * F::ROW, turn = ((lane >> 3 & 1) ^ (lane & 7)) * 16;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            unsigned v[4];
-            load_transposed(v, from + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
+        for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                mma_bf16(o[s][m], v, high[m][0], high[m][1]);
-                if (lower) mma_bf16(o[s][m], v, low[m][0], low[m][1]);
+            for (int s = 0; s < KS; ++s) {
+                unsigned v[4];
+                load_transposed(v, from + h * 16 * F::ROW + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    mma_bf16(o[s][m], v, high[h][m][0], high[h][m][1]);
+                    if (lower) mma_bf16(o[s][m], v, low[h][m][0], low[h][m][1]);
+                }
             }
-        }
     }
     // True: to be taken again.
     __device__ __forceinline__ bool again()
@@ -389,20 +497,29 @@ template <int W, int NT> struct Tile16 {
                 const int c = m * 8 + 2 * t + e;
                 if (g == 0 && c < u.n) *u.lse(c) = lse_of(base[m][e], sum[m][e]);
             }
-            const int c = m * 8 + g;
-            Bf16 *out = c < u.n ? u.out(c) : nullptr;
+            const int c = m * 8 + g, d = c < u.n ? u.a.d : 0;
+            Bf16 *out = u.out(c < u.n ? c : 0) + 2 * t;
+            unsigned y[KS][2];   // columns by queries to queries by columns: this lane's query g, columns 2 t and 2 t + 1 of eight
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    // columns by queries to queries by columns: this lane's query g, columns 2 t and 2 t + 1
-                    const unsigned y = transposed(attn::bf16x2(o[s][m][2 * j] * f[0], o[s][m][2 * j + 1] * f[1]));
-                    const int e = s * 16 + j * 8 + 2 * t;
-                    if (!out) continue;
-                    if (u.a.out_pairs && e + 1 < u.a.d) { *reinterpret_cast<unsigned *>(out + e) = y; continue; }
-                    if (e < u.a.d) out[e].bits = (unsigned short)y;
-                    if (e + 1 < u.a.d) out[e + 1].bits = (unsigned short)(y >> 16);
-                }
+                for (int j = 0; j < 2; ++j) y[s][j] = transposed(attn::bf16x2(o[s][m][2 * j] * f[0], o[s][m][2 * j + 1] * f[1]));
+            if (u.a.pairs) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (s * 16 + j * 8 + 2 * t < d) *reinterpret_cast<unsigned *>(out + s * 16 + j * 8) = y[s][j];
+            } else {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int e = s * 16 + j * 8 + 2 * t;
+                        if (e < d) out[s * 16 + j * 8].bits = (unsigned short)y[s][j];
+                        if (e + 1 < d) out[s * 16 + j * 8 + 1].bits = (unsigned short)(y[s][j] >> 16);
+                    }
+            }
         }
     }
     __device__ __forceinline__ void leave(float *part, float2 *ml, int queries, int lane)
@@ -413,91 +530,107 @@ template <int W, int NT> struct Tile16 {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int c = m * 8 + 2 * t + e;
-                if (c >= queries) continue;
-                if (g == 0) ml[c] = make_float2(ahead[m][e] == kAhead ? base[m][e] : -CUDART_INF_F, sum[m][e]);
+                const bool on = c < queries;
+                float *to = part + c * W + g;
+                if (on && g == 0) ml[c] = make_float2(ahead[m][e] == kAhead ? base[m][e] : -CUDART_INF_F, sum[m][e]);
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    part[c * W + s * 16 + g] = o[s][m][e];
-                    part[c * W + s * 16 + g + 8] = o[s][m][e + 2];
+                    if (on) to[s * 16] = o[s][m][e];
+                    if (on) to[s * 16 + 8] = o[s][m][e + 2];
                 }
             }
     }
 };
 
-// The same in fp32, on the CUDA cores, two sums an instruction.  A lane of S has a query (lane & 7) and every fourth 16 bytes of it in registers, and
-// reads those of each row of K along with the seven other queries' lanes; four lanes' sums then go to one of them for each row.  A lane of O has W / 32 columns
-// of all eight queries and reads the weights, which pass through shared memory.
-template <int W> struct Tile32 {
-    static constexpr int QUERIES = 8, ROWS = Form<float, W>::ROWS, MINE = ROWS / 4, COLS = W / 32;
-    uint64_t q[W / 16][2], o[4][COLS];   // o: pairs of queries, columns
+// The same in fp32, on the CUDA cores, two sums an instruction, for Q = 4 or 8 queries.  A lane of S has a query (lane % Q) and every PARTS-th 16 bytes of it in
+// registers, and reads those of each row of K along with the other queries' lanes; PARTS lanes' sums then go to one of them for each row.  A lane of
+// O has W / 32 columns of all queries and reads the weights, which pass through shared memory.
+template <int W, int Q> struct Tile32 {
+    static constexpr int QUERIES = Q, PARTS = 32 / Q, ROWS = Form<float, W>::ROWS, MINE = ROWS / PARTS, COLS = W / 32, FOURS = W / 4 / PARTS;
+    static constexpr bool EARLY = W < 128;   // as above
+    uint64_t q[FOURS][2], early[EARLY ? FOURS : 1][2], o[Q / 2][COLS];   // o: pairs of queries, columns
     float base, ahead, sum;
     int sees;
-    bool lower;
 
-    __device__ __forceinline__ void begin(const Queries<float> &u, int lane, bool alike)
+    static __device__ __forceinline__ void load(const Queries<float> &u, int lane, uint64_t (&to)[FOURS][2])
     {
-        const int c = lane & 7, part = lane >> 3;
-        const float *p = c < u.n ? u.query(c) : nullptr;
-        sees = alike ? INT_MAX : u.sees(c);
+        const int c = lane % Q, part = lane / Q;
+        const float *p = u.query(c < u.n ? c : 0) + part * 4;
+        const int d = c < u.n ? u.a.d - part * 4 : 0;
+        if (u.a.fours) {
 #pragma unroll
-        for (int i = 0; i < W / 16; ++i) {
-            const int e = (i * 4 + part) * 4;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (p) {
-                if (u.a.q_fours && e + 3 < u.a.d) {
-                    x = *reinterpret_cast<const float4 *>(p + e);
-                } else {
-                    if (e < u.a.d) x.x = p[e];
-                    if (e + 1 < u.a.d) x.y = p[e + 1];
-                    if (e + 2 < u.a.d) x.z = p[e + 2];
-                    if (e + 3 < u.a.d) x.w = p[e + 3];
-                }
+            for (int i = 0; i < FOURS; ++i) {
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i * PARTS * 4 < d) x = *reinterpret_cast<const float4 *>(p + i * PARTS * 4);
+                to[i][0] = attn::two(x.x, x.y);
+                to[i][1] = attn::two(x.z, x.w);
             }
-            q[i][0] = attn::two(x.x, x.y);
-            q[i][1] = attn::two(x.z, x.w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < FOURS; ++i) {
+                float x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = i * PARTS * 4 + k < d ? p[i * PARTS * 4 + k] : 0.f;
+                to[i][0] = attn::two(x[0], x[1]);
+                to[i][1] = attn::two(x[2], x[3]);
+            }
         }
+    }
+    __device__ __forceinline__ void look_ahead(const Queries<float> &u, int lane) { if constexpr (EARLY) load(u, lane, early); }
+    __device__ __forceinline__ void begin(const Queries<float> &u, int lane, bool alike, bool at_once)
+    {
+        if (EARLY && !at_once) {
+#pragma unroll
+            for (int i = 0; i < FOURS; ++i) { q[i][0] = early[EARLY ? i : 0][0]; q[i][1] = early[EARLY ? i : 0][1]; }
+        } else {
+            load(u, lane, q);
+        }
+        sees = alike ? INT_MAX : u.sees(lane % Q);
+        clear();
     }
     __device__ __forceinline__ void clear()
     {
         ahead = -CUDART_INF_F; base = 0.f; sum = 0.f;
 #pragma unroll
-        for (int h = 0; h < 4; ++h)
+        for (int h = 0; h < Q / 2; ++h)
 #pragma unroll
             for (int c = 0; c < COLS; ++c) o[h][c] = 0;
     }
-    static __device__ __forceinline__ int weights_of(int row) { return row * 8 + row / MINE * 8; }   // (four rows that are written at once: different banks)
-    __device__ __forceinline__ void take(unsigned at, unsigned there, int first, float scale2, int lane, float *weights)
+    static __device__ __forceinline__ int weights_of(int row) { return row * Q + row / MINE * Q; }   // (rows that are written at once lie in different banks)
+    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, float *weights)
     {
         using F = Form<float, W>;
-        const int part = lane >> 3;
+        const int part = lane / Q;
         float s[ROWS];
+        const char *from = tile + part * 16;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             uint64_t x = 0, y = 0;
 #pragma unroll
-            for (int i = 0; i < W / 16; ++i) {
-                uint64_t k0, k1;
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(k0), "=l"(k1) : "r"(at + r * F::ROW + (i * 4 + part) * 16) : "memory");
-                x = attn::fma2(q[i][0], k0, x);
-                y = attn::fma2(q[i][1], k1, y);
+            for (int i = 0; i < FOURS; ++i) {
+                const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(from + r * F::ROW + i * PARTS * 16);
+                x = attn::fma2(q[i][0], k.x, x);
+                y = attn::fma2(q[i][1], k.y, y);
             }
-            float u, v, w, z;
-            attn::split(x, u, v);
-            attn::split(y, w, z);
-            s[r] = (u + w) + (v + z);
+            float u, v;
+            attn::split(attn::add2(x, y), u, v);
+            s[r] = u + v;
         }
-        // four lanes' sums of every row -> one lane's: rows part * MINE ...
-        const bool up = part & 2, odd = part & 1;
+        // PARTS lanes' sums of every row -> one lane's: rows part * MINE ...
 #pragma unroll
-        for (int r = 0; r < ROWS / 2; ++r) {
-            const float give = up ? s[r] : s[r + ROWS / 2], keep = up ? s[r + ROWS / 2] : s[r];
-            s[r] = keep + __shfl_xor_sync(~0u, give, 16);
+        for (int w = 16, n = ROWS / 2; w >= Q; w >>= 1, n >>= 1) {
+            const bool up = lane & w;
+#pragma unroll
+            for (int r = 0; r < ROWS / 2; ++r)
+                if (r < n) {
+                    const float give = up ? s[r] : s[r + n], keep = up ? s[r + n] : s[r];
+                    s[r] = keep + __shfl_xor_sync(~0u, give, w);
+                }
         }
         bool move = false;
 #pragma unroll
         for (int r = 0; r < MINE; ++r) {
-            const float give = odd ? s[r] : s[r + MINE], keep = odd ? s[r + MINE] : s[r];
-            s[r] = fmaf(keep + __shfl_xor_sync(~0u, give, 8), scale2, -base);
+            s[r] = fmaf(s[r], scale2, -base);
             const int row = part * MINE + r;
             if (!(there >> row & 1) || (first >= 0 && first + row >= sees)) s[r] = -CUDART_INF_F;
             move |= s[r] > ahead;
@@ -506,8 +639,8 @@ template <int W> struct Tile32 {
             float by = s[0];
 #pragma unroll
             for (int r = 1; r < MINE; ++r) by = fmaxf(by, s[r]);
-            by = fmaxf(by, __shfl_xor_sync(~0u, by, 8));
-            by = fmaxf(by, __shfl_xor_sync(~0u, by, 16));
+#pragma unroll
+            for (int w = Q; w < 32; w <<= 1) by = fmaxf(by, __shfl_xor_sync(~0u, by, w));
             float fall = 1.f;
             if (by == -CUDART_INF_F) by = 0.f;
             else if (ahead == kAhead) fall = attn::ex2(-(by = fmaxf(by, 0.f)));
@@ -517,7 +650,7 @@ template <int W> struct Tile32 {
 #pragma unroll
             for (int r = 0; r < MINE; ++r) s[r] -= by;
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
+            for (int h = 0; h < Q / 2; ++h) {
                 const uint64_t f = attn::two(__shfl_sync(~0u, fall, 2 * h), __shfl_sync(~0u, fall, 2 * h + 1));
 #pragma unroll
                 for (int c = 0; c < COLS; ++c) o[h][c] = attn::mul2(o[h][c], f);
@@ -527,38 +660,42 @@ template <int W> struct Tile32 {
         for (int r = 0; r < MINE; ++r) {
             s[r] = attn::ex2(s[r]);
             sum += s[r];
-            weights[weights_of(part * MINE + r) + (lane & 7)] = s[r];
+            weights[weights_of(part * MINE + r) + lane % Q] = s[r];
         }
         __syncwarp();
-        const unsigned v_at = at + ROWS * F::ROW;
+        const char *v_from = tile + ROWS * F::ROW + lane * (COLS == 2 ? 8 : 16);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             float v[COLS];
             if constexpr (COLS == 2) {
-                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(v_at + r * F::ROW + lane * 8) : "memory");
+                const float2 y = *reinterpret_cast<const float2 *>(v_from + r * F::ROW);
+                v[0] = y.x; v[1] = y.y;
             } else {
 #pragma unroll
-                for (int c = 0; c < COLS; c += 4)
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[c]), "=f"(v[c + 1]), "=f"(v[c + 2]), "=f"(v[c + 3])
-                                 : "r"(v_at + r * F::ROW + lane * 16 + c * 128) : "memory");
+                for (int c = 0; c < COLS; c += 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(v_from + r * F::ROW + c * 128);
+                    v[c] = y.x; v[c + 1] = y.y; v[c + 2] = y.z; v[c + 3] = y.w;
+                }
             }
-            const ulonglong2 *p = reinterpret_cast<const ulonglong2 *>(weights + weights_of(r));
-            const ulonglong2 p0 = p[0], p1 = p[1];
+            uint64_t p[Q / 2];
+#pragma unroll
+            for (int h = 0; h < Q / 2; h += 2) {
+                const ulonglong2 y = reinterpret_cast<const ulonglong2 *>(weights + weights_of(r))[h / 2];
+                p[h] = y.x; p[h + 1] = y.y;
+            }
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
                 const uint64_t x = attn::two(v[c], v[c]);
-                o[0][c] = attn::fma2(p0.x, x, o[0][c]);
-                o[1][c] = attn::fma2(p0.y, x, o[1][c]);
-                o[2][c] = attn::fma2(p1.x, x, o[2][c]);
-                o[3][c] = attn::fma2(p1.y, x, o[3][c]);
+#pragma unroll
+                for (int h = 0; h < Q / 2; ++h) o[h][c] = attn::fma2(p[h], x, o[h][c]);
             }
         }
     }
     __device__ __forceinline__ bool again() { return false; }
     __device__ __forceinline__ void total()
     {
-        sum += __shfl_xor_sync(~0u, sum, 8);
-        sum += __shfl_xor_sync(~0u, sum, 16);
+#pragma unroll
+        for (int w = Q; w < 32; w <<= 1) sum += __shfl_xor_sync(~0u, sum, w);
     }
     static __device__ __forceinline__ int column(int c, int lane) { return COLS == 2 ? lane * 2 + c : lane * 4 + c / 4 * 128 + c % 4; }
     __device__ __forceinline__ void write(const Queries<float> &u, int lane)
@@ -566,17 +703,18 @@ template <int W> struct Tile32 {
         const float f = sum == 0.f ? 0.f : 1.f / sum;
         if (lane < u.n) *u.lse(lane) = lse_of(base, sum);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
+        for (int h = 0; h < Q / 2; ++h) {
             if (2 * h >= u.n) break;
             const float f0 = __shfl_sync(~0u, f, 2 * h), f1 = __shfl_sync(~0u, f, 2 * h + 1);
-            float *out0 = u.out(2 * h), *out1 = 2 * h + 1 < u.n ? u.out(2 * h + 1) : nullptr;
+            float *out0 = u.out(2 * h), *out1 = u.out(min(2 * h + 1, u.n - 1));
+            const int d0 = u.a.d, d1 = 2 * h + 1 < u.n ? d0 : 0;
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
                 const int e = column(c, lane);
                 float x, y;
                 attn::split(o[h][c], x, y);
-                if (e < u.a.d) out0[e] = x * f0;
-                if (e < u.a.d && out1) out1[e] = y * f1;
+                if (e < d0) out0[e] = x * f0;
+                if (e < d1) out1[e] = y * f1;
             }
         }
     }
@@ -584,7 +722,7 @@ template <int W> struct Tile32 {
     {
         if (lane < queries) ml[lane] = make_float2(ahead == kAhead ? base : -CUDART_INF_F, sum);
 #pragma unroll
-        for (int h = 0; h < 4; ++h)
+        for (int h = 0; h < Q / 2; ++h)
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
                 float x, y;
@@ -594,110 +732,134 @@ template <int W> struct Tile32 {
             }
     }
 };
-template <typename T, int W, int NT> struct TileOf { using type = Tile16<W, NT>; };
-template <int W, int NT> struct TileOf<float, W, NT> { using type = Tile32<W>; };
+template <typename T, int W, int Q> struct TileOf { using type = Tile16<W, Q / 8>; };
+template <int W, int Q> struct TileOf<float, W, Q> { using type = Tile32<W, Q>; };
 
-template <typename T, int W, int NT, bool ALIGNED>
+// The warp's pieces follow one another without a pause: while one is taken, the rows of the next one are looked up and copied and its queries loaded.
+template <typename T, int W, int Q, bool ALIGNED>
 __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_attention_kernel(const AttnArgs<T> a)
 {
     using F = Form<T, W>;
-    using Tile = typename TileOf<T, W, NT>::type;
+    using Tile = typename TileOf<T, W, Q>::type;
     extern __shared__ __align__(128) char shared[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x * kAttnWarps + warp;
     const int units = a.kv_heads * a.blocks;   // of a token
-    char *ring = shared + warp * F::RING;
+    const char *ring = shared + warp * F::RING;
+    const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
     float *weights = reinterpret_cast<float *>(shared + kAttnWarps * F::RING + warp * F::WEIGHTS);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const auto cost = [&](int i) {
-        const Pack p = pack_of(a, i);
-        return p.n ? (long long)(tiles_of<F::ROWS>(a, p) + kUnitCost) * units : 0ll;
-    };
-    Share w;
-    if (!deal<kAttnWarps * 32>(a.M, cost, gridDim.x * kAttnWarps, me, kLeastCost, w)) {
+    Share share;
+    Window window;
+    const auto load = [&](int base) { return window_of(a, base, lane); };
+    const auto cost = [&](const Window &w) { return cost_of<F::ROWS>(a, window = w, lane); };
+    if (!deal<kAttnWarps * 32>(a.M, units, load, cost, gridDim.x * kAttnWarps, me, kLeastCost, share)) {
         if (!a.by_unit && lane == 0) a.joins[me] = make_int4(0, -1, 0, 0);
         return;
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the joining CTAs wait for the end of this launch)
     int4 join = make_int4(0, -1, 0, 0);
     const float scale2 = a.scale * attn::kLog2e;
-    Pack p = pack_of(a, w.row);
-    int i = w.row, tiles = tiles_of<F::ROWS>(a, p), unit;   // unit of the token; what of it lies before this warp's share
-    long long before;
-    if (w.rest >> 31) {
-        unit = (int)(w.rest / (tiles + kUnitCost));
-        before = w.rest - (long long)unit * (tiles + kUnitCost);
-    } else {
-        unit = (int)w.rest / (tiles + kUnitCost);
-        before = (int)w.rest - unit * (tiles + kUnitCost);
-    }
+
+    // Where the next piece begins: `at` behind the share's begin, `before` behind the begin of a unit; tile t of the unit lies at kUnitCost + t.
+    Pack pack = pack_of(a, window, share.row, lane);
+    int token = share.row, tiles = tiles_of<F::ROWS>(a, pack.most), unit = (int)quotient(share.rest, tiles + kUnitCost);
+    const int size = (int)(share.hi - share.lo);   // (of 2^27 tiles of a row and 2^31 rows at most, in shares of thousands of them)
+    int at = 0, before = (int)(share.rest - (long long)unit * (tiles + kUnitCost));
+    const auto queries_of = [&](const Piece &x) {
+        const int g = (int)a.by_blocks((unsigned)x.unit), b = x.unit - g * a.blocks;
+        return Queries<T>{a, x.i, g * a.group + b * Tile::QUERIES, a.pack > 1 ? x.p.n * a.group : min(Tile::QUERIES, a.group - b * Tile::QUERIES)};
+    };
+    Feed<T, W, ALIGNED> feed(a, lane);
     Tile x;
-    for (long long at = w.lo;;) {
-        // position `at` of the line is `before` behind the unit's begin; tile t of the unit lies at kUnitCost + t
-        const long long begin = at - before, end = min(begin + tiles + kUnitCost, w.hi);
-        const int first = (int)max(before - kUnitCost, 0ll), last = (int)(end - begin) - kUnitCost;   // tiles
-        if (last > first) {
-            const int g = unit / a.blocks, b = unit - g * a.blocks;
-            const Queries<T> u{a, i, g * a.group + b * Tile::QUERIES, a.pack > 1 ? p.n * a.group : min(Tile::QUERIES, a.group - b * Tile::QUERIES)};
-            const Rows<T, W, ALIGNED> rows(a, i, g, p.most, lane);
-            // a tile's index is found four tiles ahead of its use, its page three, and its copies begin two ahead
-            typename Rows<T, W, ALIGNED>::At now = rows.index(first), next = rows.index(first + 1), third = rows.index(first + 2), fourth = rows.index(first + 3);
-            x.begin(u, lane, p.n == 1);
-            x.lower = true;
-            do {
-                x.clear();
-                unsigned there, there1, there2;
-                const unsigned to = (unsigned)__cvta_generic_to_shared(ring);
-                rows.page(now);
-                rows.page(next);
-                rows.page(third);
-                there = rows.copy(now, to);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                there1 = first + 1 < last ? rows.copy(next, to + F::TILE) : 0;
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                int stage = 0;
-                for (int j = first; j < last; ++j) {
-                    asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    __syncwarp();
-                    const int free = stage == 0 ? 2 : stage - 1;
-                    there2 = j + 2 < last ? rows.copy(third, to + free * F::TILE) : 0;
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    third = fourth;
-                    rows.page(third);
-                    fourth = rows.index(j + 4);
-                    if (there) x.take(to + stage * F::TILE, there, (j + 1) * F::ROWS > p.least && p.n > 1 ? j * F::ROWS : -1, scale2, lane, weights);
-                    there = there1;
-                    there1 = there2;
-                    stage = stage == 2 ? 0 : stage + 1;
-                    __syncwarp();
+    const auto next_piece = [&](Piece &to) {   // false: there is none
+        while (at < size) {
+            const int begin = at - before, end = min(begin + tiles + kUnitCost, size);
+            to.i = token; to.unit = unit; to.tiles = tiles; to.p = pack;
+            to.first = max(before - kUnitCost, 0);
+            to.last = end - begin - kUnitCost;
+            // a unit that begins here and ends elsewhere: its last tile lies with the last warp
+            if (to.first == 0 && to.last > 0 && to.last < tiles)
+                join = make_int4(token * units + unit, me, me + (int)((unsigned)(begin + tiles + kUnitCost - 1) / (unsigned)share.share), 0);
+            at = end;
+            before = 0;
+            if (++unit == units) {
+                unit = 0;
+                token += pack.n;
+                if (at < size && token < a.M) {
+                    if (token >= window.base + 32) window = window_of(a, token & ~31, lane);
+                    pack = pack_of(a, window, token, lane);
+                    tiles = tiles_of<F::ROWS>(a, pack.most);
                 }
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                __syncwarp();
-                if (!x.again()) break;
-                now = rows.index(first); next = rows.index(first + 1); third = rows.index(first + 2); fourth = rows.index(first + 3);
-            } while (true);
-            x.total();
-            const int id = i * units + unit;
-            const bool all = first == 0 && last == tiles;
-            if (all) {
-                x.write(u, lane);
-            } else {
-                const long long slot = me * 2ll + (first == 0);
-                x.leave(a.part + slot * Tile::QUERIES * W, a.part_ml + slot * Tile::QUERIES, u.n, lane);
-                if (first == 0) join = make_int4(id, me, (int)((begin + tiles + kUnitCost - 1) / w.share), u.n);   // (the warp that the last tile lies with)
             }
-            if (first == 0 && a.by_unit && lane < p.n) a.joins[id + lane * units] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
+            if (to.last > to.first) return true;
+            if (token >= a.M) return false;   // (not with lengths that stay as they are)
         }
-        at = end;
-        if (at >= w.hi) break;
-        before = 0;
-        if (++unit == units) {
-            unit = 0;
-            if ((i += p.n) >= a.M) break;   // (not with lengths that stay as they are)
-            p = pack_of(a, i);
-            tiles = tiles_of<F::ROWS>(a, p);
+        return false;
+    };
+    const auto start = [&](const Piece &p) { feed.begin(p, p.p.most ? row_of(a.tok, p.i) : 0); };   // its rows
+    Piece now, next;
+    if (!next_piece(now)) {
+        if (!a.by_unit && lane == 0) a.joins[me] = join;
+        return;
+    }
+    start(now);
+    bool more = false, fed = false;   // there is a next piece; its rows are being copied
+    x.begin(queries_of(now), lane, now.p.n == 1, true);
+    int ahead = 0, stage = 0, j = now.first;   // tiles that are on their way; the stage of the oldest, the tile that it is
+    unsigned there0 = 0, there1 = 0, there2 = 0;
+    for (;;) {
+        while (ahead < kStages && feed.tile < feed.last && (ahead < 2 || feed.ready())) {
+            const int to = stage + ahead;
+            const unsigned there = feed.copy(ring_at + (to >= kStages ? to - kStages : to) * F::TILE);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (ahead == 0) there0 = there; else if (ahead == 1) there1 = there; else there2 = there;
+            ++ahead;
         }
+        if (ahead == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (ahead == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        if (there0) x.take(ring + stage * F::TILE, there0, now.p.n > 1 && (j + 1) * F::ROWS > now.p.least ? j * F::ROWS : -1, scale2, lane, weights);
+        there0 = there1;
+        there1 = there2;
+        --ahead;
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        feed.look_up();
+        __syncwarp();
+        if (feed.tile == feed.last && !fed) {   // all of this piece is on its way: the next one
+            if (!more) more = next_piece(next);
+            if (more) { start(next); fed = true; x.look_ahead(queries_of(next), lane); }
+        }
+        if (++j < now.last) continue;
+        if (x.again()) {   // from its first tile on, without what is on its way of the next
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            x.clear();
+            ahead = 0;
+            fed = false;
+            j = now.first;
+            start(now);
+            continue;
+        }
+        x.total();
+        const int id = now.i * units + now.unit;
+        const bool all = now.first == 0 && now.last == now.tiles;
+        const Queries<T> u = queries_of(now);
+        if (all) {
+            x.write(u, lane);
+        } else {
+            const long long slot = me * 2ll + (now.first == 0);
+            x.leave(a.part + slot * Tile::QUERIES * W, a.part_ml + slot * Tile::QUERIES, u.n, lane);
+            if (now.first == 0) join.w = u.n;
+        }
+        if (now.first == 0 && a.by_unit && lane < now.p.n) a.joins[id + lane * units] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
+        if (!more) break;
+        now = next;
+        more = fed = false;
+        j = now.first;
+        x.begin(queries_of(now), lane, now.p.n == 1, false);
     }
     if (!a.by_unit && lane == 0) a.joins[me] = join;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // Joins the parts of units in several shares.  WARPS: warps that take a query of an entry of `joins`, kJoinAt parts of it at a time each, whose results are
