@@ -81,6 +81,25 @@ __device__ __forceinline__ long long block_before(long long x, long long *warps,
     }
     return before + up - x;
 }
+// The same for three sums (each becomes what is before this thread).
+__device__ __forceinline__ void block_before3(long long &x, long long &y, long long &z, long long *warps, long long &all_x, long long &all_y, long long &all_z)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockDim.x / 32;
+    long long a = x, b = y, c = z;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+        const long long u = __shfl_up_sync(~0u, a, w), v = __shfl_up_sync(~0u, b, w), t = __shfl_up_sync(~0u, c, w);
+        if (lane >= w) { a += u; b += v; c += t; }
+    }
+    if (lane == 31) { warps[warp] = a; warps[n + warp] = b; warps[2 * n + warp] = c; }
+    __syncthreads();
+    x = a - x; y = b - y; z = c - z;
+    all_x = all_y = all_z = 0;
+    for (int w = 0; w < n; ++w) {
+        if (w < warp) { x += warps[w]; y += warps[n + w]; z += warps[2 * n + w]; }
+        all_x += warps[w]; all_y += warps[n + w]; all_z += warps[2 * n + w];
+    }
+}
 // Tokens' costs in a line, dealt to `parts` warps in equal shares of at least `least`: what warp `me` has.
 struct Share {
     long long lo, hi, share, rest;   // [lo, hi) of the line; every warp's share; lo is `rest` behind the begin of token `row`
@@ -222,7 +241,7 @@ __device__ __forceinline__ Request request(const TablesArgs &a, int r)
 __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs a)
 {
     extern __shared__ int prefix[];
-    __shared__ long long warps[kThreads / 32];
+    __shared__ long long warps[3 * kThreads / 32];
     const int R = a.t.requests, each = (R + kThreads - 1) / kThreads, r0 = min(R, (int)threadIdx.x * each), r1 = min(R, r0 + each);
     int *take = prefix, *back = prefix + R + 1, *ptr = prefix + 2 * (R + 1);
     long long n_take = 0, n_back = 0, n_new = 0, all_take, all_back, all_new;
@@ -230,10 +249,8 @@ __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs
         const Request q = request(a, r);
         n_take += q.need; n_back += q.back; n_new += q.fresh;
     }
-    n_take = block_before(n_take, warps, all_take);
-    n_back = block_before(n_back, warps, all_back);
-    n_new = block_before(n_new, warps, all_new);
     const int count = min(max(*a.free_count, 0), a.free_room);
+    block_before3(n_take, n_back, n_new, warps, all_take, all_back, all_new);
     const long long top = min(count + all_back, (long long)a.free_room);   // free pages before any is taken
     long long fit = 0;                                                      // tokens that get a row
     for (int r = r0; r < r1; ++r) {
@@ -302,12 +319,14 @@ struct ListsArgs {
     int *row_ptr, *col_idx;
     Div by_page;
 };
-constexpr int kScanThreads = 1024;
+// More than kListTokens tokens: the ends of their lists in a launch of their own.
+constexpr int kScanThreads = 1024, kListTokens = 8192;
 __global__ void __launch_bounds__(kScanThreads) paged_list_ends_kernel(const ListsArgs a)
 {
     __shared__ long long warps[kScanThreads / 32];
     const int each = (a.M + kScanThreads - 1) / kScanThreads, i0 = (int)min((long long)a.M, threadIdx.x * (long long)each), i1 = min(a.M, i0 + each);
     long long n = 0, all;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int i = i0; i < i1; ++i) n += seen_of(a.tok, a.t, a.page, i);
     n = block_before(n, warps, all);
     for (int i = i0; i < i1; ++i) {
@@ -317,58 +336,59 @@ __global__ void __launch_bounds__(kScanThreads) paged_list_ends_kernel(const Lis
     if (threadIdx.x == 0) a.row_ptr[a.M] = (int)min(all, a.entries);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
-// A warp takes kListShare neighbouring entries.  32 ends of rows are in its lanes at a time; an entry's row is found among them by five shuffles, so
-// rows of one entry cost what rows of many do.  Bound by the stores.
-constexpr int kListShare = 512;
+// A thread takes four neighbouring entries: their list by a binary search over the ends, which each CTA forms for itself in shared memory (KEPT), then
+// a page of the table for all four unless a page or a list ends among them.  Bound by latency (lengths, table), then by the stores.
+template <bool KEPT>
 __global__ void __launch_bounds__(kThreads) paged_list_kernel(const ListsArgs a)
 {
-    const int lane = threadIdx.x & 31;
-    const long long lo = (blockIdx.x * (long long)(kThreads / 32) + (threadIdx.x >> 5)) * kListShare, hi = min(lo + kListShare, a.entries);
+    extern __shared__ int kept[];
+    __shared__ long long warps[kThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (lo >= hi) return;
-    const int all = a.row_ptr[a.M];
-    // the first row that ends behind lo (M if none does), by 32 probes at a time
-    int base = 0;
-    for (int len = a.M; len > 0;) {   // it lies in [base, base + len]
-        const int step = (len + 31) / 32, at = base + lane * step;
-        const bool inside = lane * (long long)step < len;
-        const unsigned behind = __ballot_sync(~0u, inside && a.row_ptr[at + 1] > lo), probes = __ballot_sync(~0u, inside);
-        const int k = behind ? __ffs(behind) - 1 : __popc(probes);   // probes before k end at or before lo
-        if (k == 0) break;
-        const int past = (k - 1) * step + 1;
-        len = (behind ? k * step : len) - past;
-        base += past;
-    }
-    int end = 0, start = 0;
-    const auto window = [&](int at) {   // lane: start and end of row at + lane
-        const int i = min(at + lane, a.M);
-        start = a.row_ptr[i];
-        end = at + lane < a.M ? a.row_ptr[i + 1] : INT_MAX;
-    };
-    window(base);
-    for (long long e0 = lo; e0 < hi; e0 += 32) {
-        const int e = (int)min(e0 + lane, (long long)INT_MAX);
-        int slot = -1;
-        bool open = e0 + lane < hi && e < all;
-        while (__any_sync(~0u, open)) {
-            int k = 0;   // ends at or before e among the 32
-#pragma unroll
-            for (int s = 16; s; s >>= 1) {
-                const int y = __shfl_sync(~0u, end, k + s - 1);
-                if (y <= e) k += s;
-            }
-            const int last = __shfl_sync(~0u, end, 31), k1 = min(k, 31);
-            if (k == 31 && last <= e) k = 32;
-            const int first = __shfl_sync(~0u, start, k1);
-            if (open && k < 32) {
-                const int i = base + k, p = e - first;
-                const int c = (int)a.by_page((unsigned)p), held = a.t.entries[(long long)row_of(a.tok, i) * a.t.ld + c];
-                if ((unsigned)held < (unsigned)a.pages) slot = held * a.page + (p - c * a.page);
-                open = false;
-            }
-            if (__any_sync(~0u, open)) { base += 32; window(base); }
+    const int *ends = KEPT ? kept : a.row_ptr;
+    if (KEPT) {
+        const int each = (a.M + kThreads - 1) / kThreads, i0 = min(a.M, (int)threadIdx.x * each), i1 = min(a.M, i0 + each);
+        long long n = 0, all;
+        for (int i = i0; i < i1; ++i) n += seen_of(a.tok, a.t, a.page, i);
+        n = block_before(n, warps, all);
+        for (int i = i0; i < i1; ++i) {
+            kept[i] = (int)min(n, a.entries);
+            if (blockIdx.x == 0) a.row_ptr[i] = kept[i];
+            n += seen_of(a.tok, a.t, a.page, i);
         }
-        if (e0 + lane < hi) a.col_idx[e0 + lane] = slot;
+        if (threadIdx.x == 0) {
+            kept[a.M] = (int)min(all, a.entries);
+            if (blockIdx.x == 0) a.row_ptr[a.M] = kept[a.M];
+        }
+        __syncthreads();
+    }
+    const int all = ends[a.M];
+    const bool fours = (reinterpret_cast<uintptr_t>(a.col_idx) & 15) == 0;
+    for (long long e0 = (blockIdx.x * (long long)kThreads + threadIdx.x) * 4; e0 < a.entries; e0 += gridDim.x * (long long)kThreads * 4) {
+        int slots[4];
+        int i = -1, end = 0, first = 0, base = 0, c_of = -1, held = -1;   // the list that the last entry was of; its page
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const long long e = e0 + k;
+            slots[k] = -1;
+            if (e >= all) continue;
+            if (i < 0 || e >= end) {
+                i = segment_of(ends, a.M, (int)e);
+                first = ends[i];
+                end = ends[i + 1];
+                base = row_of(a.tok, i);
+                c_of = -1;
+            }
+            const int p = (int)e - first, c = (int)a.by_page((unsigned)p);
+            if (c != c_of) held = a.t.entries[base * a.t.ld + (c_of = c)];
+            if ((unsigned)held < (unsigned)a.pages) slots[k] = held * a.page + (p - c * a.page);
+        }
+        if (fours && e0 + 3 < a.entries) {
+            *reinterpret_cast<int4 *>(a.col_idx + e0) = make_int4(slots[0], slots[1], slots[2], slots[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (e0 + k < a.entries) a.col_idx[e0 + k] = slots[k];
+        }
     }
 }
 
@@ -431,7 +451,7 @@ template <typename T> struct Chunk {
 
 // A CTA per touched page and head: the request's new rows that lie in it are copied, and the mean of K's rows is formed from them and those that were
 // there.  So a page's rows are summed in one place and order (in fp32, rounded once to the cache's type), and no row is written twice.
-constexpr int kWriteThreads = 128;
+constexpr int kWriteThreads = 128, kWriteRows = 4;
 template <typename T>
 __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const WriteArgs<T> a)
 {
@@ -470,18 +490,29 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const WriteA
             if (group < groups) {
                 const int e = (c0 + threadIdx.x % lanes) * C::N;
                 const bool whole = e + C::N <= a.d;
-                for (int i = (means ? 0 : old) + group; i < end; i += groups) {
-                    C y;
-                    if (i < old) {
-                        y.load(a.kp.row(held, h, i), e, a.d, whole);
-                    } else {
-                        y.load(k + i * a.k_ld, e, a.d, k_wide && whole);
-                        y.store(a.kp.row(held, h, i), e, a.d);
-                        C z;
-                        z.load(v + i * a.v_ld, e, a.d, v_wide && whole);
-                        z.store(a.vp.row(held, h, i), e, a.d);
+                for (int i0 = (means ? 0 : old) + group; i0 < end; i0 += kWriteRows * groups) {   // kWriteRows rows' loads at once
+                    C y[kWriteRows], z[kWriteRows];
+#pragma unroll
+                    for (int n = 0; n < kWriteRows; ++n) {
+                        const int i = i0 + n * groups;
+                        y[n].u = make_uint4(0, 0, 0, 0);
+                        if (i >= end) continue;
+                        if (i < old) {
+                            y[n].load(a.kp.row(held, h, i), e, a.d, whole);
+                        } else {
+                            y[n].load(k + i * a.k_ld, e, a.d, k_wide && whole);
+                            z[n].load(v + i * a.v_ld, e, a.d, v_wide && whole);
+                        }
                     }
-                    if (means) y.add_to(x);
+#pragma unroll
+                    for (int n = 0; n < kWriteRows; ++n) {
+                        const int i = i0 + n * groups;
+                        if (i >= old && i < end) {
+                            y[n].store(a.kp.row(held, h, i), e, a.d);
+                            z[n].store(a.vp.row(held, h, i), e, a.d);
+                        }
+                        if (means) y[n].add_to(x);
+                    }
                 }
             }
             if (means) {

@@ -295,9 +295,15 @@ extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pa
     a.tok = Tokens{rows, seen};
     a.M = M; a.page = page; a.pages = pages; a.entries = entries; a.row_ptr = row_ptr; a.col_idx = col_idx; a.by_page = Div(page);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    paged_list_ends_kernel<<<1, kScanThreads, 0, st>>>(a);
-    constexpr long long share = (long long)kListShare * (kThreads / 32);
-    if (entries) attn::launch_behind(paged_list_kernel, (unsigned)((entries + share - 1) / share), kThreads, st, a);
+    const unsigned blocks = (unsigned)std::min(std::max((entries + 4 * kThreads - 1) / (4 * kThreads), 1ll), 8ll * kSMs);
+    bool ok;
+    if (M <= kListTokens) {
+        ok = launch_early(paged_list_kernel<true>, blocks, kThreads, (M + 1) * sizeof(int), st, a);
+    } else {
+        ok = launch_early(paged_list_ends_kernel, 1, kScanThreads, 0, st, a);
+        if (ok && entries) ok = launch_early(paged_list_kernel<false>, blocks, kThreads, 0, st, a);
+    }
+    if (!ok) return B2SP_ERR_CUDA;
     return launched();
 }
 

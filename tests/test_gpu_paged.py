@@ -97,7 +97,7 @@ def test_tables_layouts_and_outputs():
 
 @pytest.mark.parametrize("seen,page,rows", [
     ([0], 4, None), ([1], 1, None), ([5, 0, 0, 9], 4, [3, 1, 2, 0]), ([40] * 33 + [0] * 70 + [2], 16, None), ([1] * 3000, 8, None),
-    ([0] * 2000 + [1, 0, 3], 5, None), ([2000, 1, 3000], 24, [2, -1, 0]), ([100, 7000], 150, [1, 1]), ([3] * 1100 + [1500], 64, None),
+    ([0] * 2000 + [1, 0, 3], 5, None), ([2000, 1, 3000], 24, [2, -1, 0]), ([100, 7000], 150, [1, 1]), ([3] * 1100 + [1500], 64, None), ([2, 0, 5] * 3000 + [40], 4, None),
 ])
 @pytest.mark.parametrize("slack", [0, 37, -1])
 def test_lists(seen, page, rows, slack):
