@@ -573,26 +573,29 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
     if (!deal<kScoreThreads>(a.M, a.kv_heads, load, [](int blocks) { return blocks; }, gridDim.x * (kScoreThreads / 32), me, 1, w)) return;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int i = w.row, n = pages_seen(a, i), blocks = (n + kScorePages - 1) / kScorePages, g = (int)w.rest / blocks, b = (int)w.rest - g * blocks;
-    double q[HALVES][N];
-    bool fresh = true;
     const int e0 = lane % LANES * N;   // this lane's first element
-    for (int left = (int)(w.hi - w.lo); left > 0; --left) {
-        const int p0 = b * kScorePages;
-        const int held = p0 + lane < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p0 + lane] : -1;
-        const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int s) {
+    double q[HALVES][N];
+    uint4 now[AT_ONCE][HALVES], next[AT_ONCE][HALVES];
+    const auto look_up = [&](int p) { return p < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p] : -1; };
+    const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int held, int g, int s) {   // means of pages s ... of a block whose pages the lanes hold
 #pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                const int p = __shfl_sync(~0u, held, s + j * STEP + lane / LANES);
-                const T *mean = a.means.row(p, g, 0) + e0;
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int p = __shfl_sync(~0u, held, s + j * STEP + lane / LANES);
+            const T *mean = a.means.row(p, g, 0) + e0;
 #pragma unroll
-                for (int x = 0; x < HALVES; ++x) {
-                    c[j][x] = make_uint4(0, 0, 0, 0);
-                    if ((unsigned)p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(mean + x * 32 * N);
-                }
+            for (int x = 0; x < HALVES; ++x) {
+                c[j][x] = make_uint4(0, 0, 0, 0);
+                if ((unsigned)p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(mean + x * 32 * N);
             }
-        };
-        uint4 c[AT_ONCE][HALVES];
-        if (fresh) {   // the queries' loads first, four heads at once; the sums when the means are on their way
+        }
+    };
+    int held = look_up(b * kScorePages + lane);
+    read(now, held, g, 0);
+    bool fresh = true;
+    // Means are on their way a batch ahead, pages a block ahead.
+    for (int left = (int)(w.hi - w.lo);;) {
+        const int of_i = i, of_g = g, of_n = n, p0 = b * kScorePages, mine_held = held;
+        if (fresh) {   // the sum of the queries, four heads' loads at once
 #pragma unroll
             for (int x = 0; x < HALVES; ++x)
 #pragma unroll
@@ -607,7 +610,6 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                         y[k][x].u = make_uint4(0, 0, 0, 0);
                         if (h + k < group) y[k][x].load(from + (h + k) * a.q_sh, e0 + x * 32 * N, a.d, a.q_wide && e0 + x * 32 * N + N <= a.d);
                     }
-                if (h == 0) read(c, 0);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -619,12 +621,28 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                     }
             }
             fresh = false;
-        } else {
-            read(c, 0);
         }
-        unsigned long long *keys = a.keys + ((long long)i * a.kv_heads + g) * a.t.width;
-        for (int s = 0; s < kScorePages && p0 + s < n; s += BATCH) {
-            if (s) read(c, s);
+        // the next block
+        const bool more = --left > 0;
+        if (more) {
+            if (++b == blocks) {
+                b = 0;
+                fresh = true;
+                if (++g == a.kv_heads) {
+                    g = 0;
+                    do
+                        if (++i >= a.M) return;
+                    while (!(blocks = blocks_of(i)));
+                    n = pages_seen(a, i);
+                }
+            }
+            held = look_up(b * kScorePages + lane);
+        }
+        unsigned long long *keys = a.keys + ((long long)of_i * a.kv_heads + of_g) * a.t.width;
+#pragma unroll 1
+        for (int s = 0; s < kScorePages; s += BATCH) {
+            if (s + BATCH < kScorePages) read(next, mine_held, of_g, s + BATCH);
+            else if (more) read(next, held, g, 0);
             double sum[AT_ONCE];
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j) {
@@ -632,7 +650,7 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
 #pragma unroll
                 for (int x = 0; x < HALVES; ++x) {
                     float f[N] = {};
-                    Chunk<T>{c[j][x]}.add_to(f);
+                    Chunk<T>{now[j][x]}.add_to(f);
                     if (e0 + x * 32 * N + N > a.d) {   // what lies behind d may be anything
 #pragma unroll
                         for (int k = 0; k < N; ++k)
@@ -657,20 +675,14 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                     sum[0] += __shfl_xor_sync(~0u, sum[0], x);
                 }
             }
-            const int k = s + mine * STEP + lane / LANES, page = __shfl_sync(~0u, held, k);
-            if (lane % (LANES / AT_ONCE) == 0 && p0 + k < n) keys[p0 + k] = (unsigned)page < (unsigned)a.means.pages ? ordered(sum[0]) : ordered(-CUDART_INF);
+            const int k = s + mine * STEP + lane / LANES, page = __shfl_sync(~0u, mine_held, k);
+            if (lane % (LANES / AT_ONCE) == 0 && p0 + k < of_n) keys[p0 + k] = (unsigned)page < (unsigned)a.means.pages ? ordered(sum[0]) : ordered(-CUDART_INF);
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+                for (int x = 0; x < HALVES; ++x) now[j][x] = next[j][x];
         }
-        if (++b == blocks) {
-            b = 0;
-            fresh = true;
-            if (++g == a.kv_heads) {
-                g = 0;
-                do
-                    if (++i >= a.M) return;
-                while (!(blocks = blocks_of(i)));
-                n = pages_seen(a, i);
-            }
-        }
+        if (!more) return;
     }
 }
 
