@@ -821,8 +821,11 @@ def paged_means(pages: int, kv_heads: int, d: int, dtype=torch.float32, device=N
     return paged_cache(pages, kv_heads, 1, d, dtype, device)[:, :, 0]
 
 
+_I32 = torch.int32
+
+
 def _int32(t, name, shape):
-    if t.dtype is not torch.int32:
+    if t.dtype is not _I32:
         raise TypeError(f"{name} must be torch.int32")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be {list(shape)}, contiguous")
@@ -831,13 +834,12 @@ def _int32(t, name, shape):
 
 def _page_tables(tables):
     """[requests, width] as b2sp_page_tables."""
-    if tables.dtype is not torch.int32:
+    if tables.dtype is not _I32:
         raise TypeError("tables must be torch.int32")
-    s = tables.stride()
-    if len(s) != 2 or (s[1] != 1 and tables.shape[1] > 1):
+    s, shape = tables.stride(), tables.shape
+    if len(s) != 2 or (s[1] != 1 and shape[1] > 1):
         raise ValueError("tables must be [requests, width] with neighbouring elements in a row")
-    R, width = tables.shape
-    return _PAGE_TABLES(tables.data_ptr(), s[0], R, width)
+    return _PAGE_TABLES(tables.data_ptr(), s[0], shape[0], shape[1])
 
 
 def _pages(t, dtype, name):
@@ -849,8 +851,10 @@ def _pages(t, dtype, name):
         raise ValueError(f"{name} must be [pages, kv_heads, page, d] with neighbouring elements along d")
     if shape[2] < 1:
         raise ValueError(f"{name}: pages have at least one row")
-    # (the stride of a dimension of one says nothing; the library wants multiples of 16 bytes)
     P, H, page, d = shape
+    if P > 1 and H > 1 and page > 1:
+        return _PAGES(t.data_ptr(), s[2], s[1], s[0], P, page), shape
+    # (the stride of a dimension of one says nothing; the library wants multiples of 16 bytes)
     return _PAGES(t.data_ptr(), s[2] if page > 1 else -(-d // 8) * 8, s[1] if H > 1 else 0, s[0] if P > 1 else 0, P, page), shape
 
 
@@ -879,10 +883,10 @@ def paged_tables(lengths, added, tables, free_pages, free_count, page, pages, to
     ones: free_count (int32 of one element or more, the first counts) of them in free_pages, to which the pages of the requests that end are added.  pages
     of `page` rows; tokens: room of the step.  counts[:1] is the next step's free_count; counts[2] > 0: not all fitted (see the header).
     out: the six tensors, which must not be the inputs."""
-    R, device = tables.shape[0], tables.device
-    t = _page_tables(tables)
-    at = _int32(lengths, "lengths", (R,)), _int32(added, "added", (R,))
-    if free_pages.dtype is not torch.int32 or free_count.dtype is not torch.int32:
+    t, R, device = _page_tables(tables), tables.shape[0], tables.device
+    shape = (R,)
+    at, more = _int32(lengths, "lengths", shape), _int32(added, "added", shape)
+    if free_pages.dtype is not _I32 or free_count.dtype is not _I32:
         raise TypeError("free_pages and free_count must be torch.int32")
     if free_pages.dim() != 1 or not free_pages.is_contiguous() or free_count.numel() < 1:
         raise ValueError("free_pages must be contiguous, free_count of one element")
@@ -890,32 +894,40 @@ def paged_tables(lengths, added, tables, free_pages, free_count, page, pages, to
     if out is None:
         if tokens < 0:
             raise ValueError("tokens must not be negative")
-        # (one allocation; each part begins on 16 bytes)
-        room = [(n + 3) & ~3 for n in sizes]
-        memory = torch.empty(sum(room), dtype=torch.int32, device=device)
-        out = tuple(part[:n] for part, n in zip(memory.split(room), sizes))
-    names = ("lengths after", "row_ptr", "rows", "seen", "slots", "counts")
-    to = [_int32(x, name, (n,)) for x, name, n in zip(out, names, sizes)]
-    _ready(device, lengths, added, free_pages, free_count, *out)
-    _check(lib.b2sp_paged_tables(t, pages, page, *at, free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(), tokens, *to,
+        memory = torch.empty(2 * R + 5 + 3 * tokens, dtype=_I32, device=device)   # (one allocation, and one call that cuts it up)
+        out = torch.unsafe_split_with_sizes(memory, sizes)
+        p = memory.data_ptr()
+        to = (p, p + 4 * R, p + 8 * R + 4, p + 8 * R + 4 + 4 * tokens, p + 8 * R + 4 + 8 * tokens, p + 8 * R + 4 + 12 * tokens)
+        _ready(device, lengths, added, free_pages, free_count)
+    else:
+        names = ("lengths after", "row_ptr", "rows", "seen", "slots", "counts")
+        to = [_int32(x, name, (n,)) for x, name, n in zip(out, names, sizes)]
+        _ready(device, lengths, added, free_pages, free_count, *out)
+    _check(lib.b2sp_paged_tables(t, pages, page, at, more, free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(), tokens, *to,
                                  _raw_stream(device.index)), "b2sp_paged_tables")
-    return tuple(out)
+    return out
 
 
 def paged_lists(tables, seen, page, pages, entries, rows=None, out=None):
     """b2sp_paged_lists: (row_ptr [M + 1], col_idx [entries]), the slots that tokens see, as attention_kv4 takes them: token i the first seen[i]
     positions of request rows[i] (of request i without rows).  Lists are cut at `entries`; -1 for missing pages and behind the last list."""
     M, device = seen.shape[0], tables.device
-    t = _page_tables(tables)
-    at = None if rows is None else _int32(rows, "rows", (M,)), _int32(seen, "seen", (M,))
+    t, m = _page_tables(tables), (M,)
+    of, at = None if rows is None else _int32(rows, "rows", m), _int32(seen, "seen", m)
     if out is None:
         if entries < 0:
             raise ValueError("entries must not be negative")
-        out = (torch.empty(M + 1, dtype=torch.int32, device=device), torch.empty(entries, dtype=torch.int32, device=device))
-    to = _int32(out[0], "row_ptr", (M + 1,)), _int32(out[1], "col_idx", (entries,))
-    _ready(device, seen, *out, *(() if rows is None else (rows,)))
-    _check(lib.b2sp_paged_lists(M, t, pages, page, *at, entries, *to, _raw_stream(device.index)), "b2sp_paged_lists")
-    return tuple(out)
+        row_ptr, col_idx = torch.empty(M + 1, dtype=_I32, device=device), torch.empty(entries, dtype=_I32, device=device)
+        ptr, col = row_ptr.data_ptr(), col_idx.data_ptr()
+        _ready(device, seen)
+    else:
+        row_ptr, col_idx = out
+        ptr, col = _int32(row_ptr, "row_ptr", (M + 1,)), _int32(col_idx, "col_idx", (entries,))
+        _ready(device, seen, row_ptr, col_idx)
+    if rows is not None:
+        _ready(device, rows)
+    _check(lib.b2sp_paged_lists(M, t, pages, page, of, at, entries, ptr, col, _raw_stream(device.index)), "b2sp_paged_lists")
+    return row_ptr, col_idx
 
 
 def paged_write(k, v, row_ptr, lengths, tables, k_pages, v_pages, means=None, dtype=torch.float32):
@@ -935,10 +947,15 @@ def paged_write(k, v, row_ptr, lengths, tables, k_pages, v_pages, means=None, dt
         if c != (a[0], H, d):
             raise ValueError("means must be [pages, kv_heads, d]")
         _ready(device, means)
-    at = _int32(row_ptr, "row_ptr", (R + 1,)), _int32(lengths, "lengths", (R,))
+    ptr, at = _int32(row_ptr, "row_ptr", (R + 1,)), _int32(lengths, "lengths", (R,))
     _ready(device, k, v, row_ptr, lengths, k_pages, v_pages)
     fn, name = (lib.b2sp_paged_write, "b2sp_paged_write") if dtype == torch.float32 else (lib.b2sp_paged_write_bf16, "b2sp_paged_write_bf16")
-    _check(fn(T, H, d, k.data_ptr(), s[0], s[1], v.data_ptr(), z[0], z[1], *at, t, kp, vp, mp, _raw_stream(device.index)), name)
+    _check(fn(T, H, d, k.data_ptr(), s[0], s[1], v.data_ptr(), z[0], z[1], ptr, at, t, kp, vp, mp, _raw_stream(device.index)), name)
+
+
+@functools.lru_cache(maxsize=4096)
+def _paged_select_need(M, kv_heads, width):
+    return lib.b2sp_paged_select_workspace_bytes(M, kv_heads, width)
 
 
 def paged_select(q, means, tables, seen, page, keep, first=1, last=1, rows=None, out=None, workspace=None, dtype=torch.float32):
@@ -949,18 +966,23 @@ def paged_select(q, means, tables, seen, page, keep, first=1, last=1, rows=None,
     Hkv, device = a[1], q.device
     if a[2] != d or Hkv < 1 or H % Hkv:
         raise ValueError("means must be [pages, kv_heads, d], heads a multiple of kv_heads")
-    t = _page_tables(tables)
-    at = None if rows is None else _int32(rows, "rows", (M,)), _int32(seen, "seen", (M,))
+    t, m = _page_tables(tables), (M,)
+    of, at = None if rows is None else _int32(rows, "rows", m), _int32(seen, "seen", m)
     if out is None:
         if keep < 1:
             raise ValueError("keep must be at least 1")
-        out = torch.empty((M, Hkv, keep), dtype=torch.int32, device=device)
-    to = _int32(out, "out", (M, Hkv, keep))
-    _ready(device, means, tables, seen, out, *(() if rows is None else (rows,)))
+        out = torch.empty_strided((M, Hkv, keep), (Hkv * keep, keep, 1), dtype=_I32, device=device)
+        to = out.data_ptr()
+    else:
+        to = _int32(out, "out", (M, Hkv, keep))
+        _ready(device, out)
+    _ready(device, means, tables, seen)
+    if rows is not None:
+        _ready(device, rows)
     stream = _raw_stream(device.index)
-    ws = _scratch(lib.b2sp_paged_select_workspace_bytes(M, Hkv, tables.shape[1]), device, workspace, stream)
+    ws = _scratch(_paged_select_need(M, Hkv, tables.shape[1]), device, workspace, stream)
     fn, name = (lib.b2sp_paged_select, "b2sp_paged_select") if dtype == torch.float32 else (lib.b2sp_paged_select_bf16, "b2sp_paged_select_bf16")
-    _check(fn(M, H, Hkv, d, q.data_ptr(), s[0], s[1], mp, t, *at, keep, first, last, to, ws.data_ptr(), ws.numel(), stream), name)
+    _check(fn(M, H, Hkv, d, q.data_ptr(), s[0], s[1], mp, t, of, at, keep, first, last, to, ws.data_ptr(), ws.numel(), stream), name)
     return out
 
 
@@ -979,29 +1001,30 @@ def attention_paged(q, k_pages, v_pages, tables, seen, rows=None, lists=None, sc
     Hkv, device = a[1], q.device
     if a != b or a[3] != d or Hkv < 1 or H % Hkv:
         raise ValueError("k_pages and v_pages must be [pages, kv_heads, page, d], heads a multiple of kv_heads")
-    t, at_lists, keep = _page_tables(tables), None, 0
-    at = None if rows is None else _int32(rows, "rows", (M,)), _int32(seen, "seen", (M,))
-    others = [k_pages, v_pages, tables, seen]
-    if rows is not None:
-        others.append(rows)
+    t, m, at_lists, keep = _page_tables(tables), (M,), None, 0
+    of, at = None if rows is None else _int32(rows, "rows", m), _int32(seen, "seen", m)
     if lists is not None:
         keep = lists.shape[-1]
         at_lists = _int32(lists, "lists", (M, Hkv, keep))
-        others.append(lists)
+        _ready(device, lists)
+    if rows is not None:
+        _ready(device, rows)
     if out is None:
         out = torch.empty_like(q) if 0 not in s else torch.empty((M, H, d), dtype=dtype, device=device)
+    elif out.dtype is not dtype or out.shape != (M, H, d):
+        raise ValueError("out must be like q")
     z = out.stride()
-    if out.dtype is not dtype or out.shape != (M, H, d) or (d > 1 and z[2] != 1):
-        raise ValueError("out must be like q, with neighbouring elements along d")
+    if d > 1 and z[2] != 1:
+        raise ValueError("out must have neighbouring elements along d")
     if lse is None:
         lse = torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=device)
     else:
         _lse(lse, (M, H))
-    _ready(device, out, lse, *others)
+    _ready(device, out, lse, k_pages, v_pages, tables, seen)
     stream = _raw_stream(device.index)
     ws = _scratch(_attention_paged_need(M, H, Hkv, d), device, workspace, stream)
     fn, name = ((lib.b2sp_attention_paged, "b2sp_attention_paged") if dtype == torch.float32
                 else (lib.b2sp_attention_paged_bf16, "b2sp_attention_paged_bf16"))
-    _check(fn(M, H, Hkv, d, q.data_ptr(), s[0], s[1], kp, vp, t, *at, at_lists, keep, d ** -0.5 if scale is None else scale, out.data_ptr(), z[0], z[1],
+    _check(fn(M, H, Hkv, d, q.data_ptr(), s[0], s[1], kp, vp, t, of, at, at_lists, keep, d ** -0.5 if scale is None else scale, out.data_ptr(), z[0], z[1],
               lse.data_ptr(), ws.data_ptr(), ws.numel(), stream), name)
     return out, lse

@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs
     __shared__ long long warps[3 * kThreads / 32];
     const int R = a.t.requests, each = (R + kThreads - 1) / kThreads, r0 = min(R, (int)threadIdx.x * each), r1 = min(R, r0 + each);
     int *take = prefix, *back = prefix + R + 1, *ptr = prefix + 2 * (R + 1);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     long long n_take = 0, n_back = 0, n_new = 0, all_take, all_back, all_new;
     for (int r = r0; r < r1; ++r) {
         const Request q = request(a, r);
@@ -451,15 +452,16 @@ template <typename T> struct Chunk {
 
 // A CTA per touched page and head: the request's new rows that lie in it are copied, and the mean of K's rows is formed from them and those that were
 // there.  So a page's rows are summed in one place and order (in fp32, rounded once to the cache's type), and no row is written twice.
-constexpr int kWriteThreads = 128, kWriteRows = 4;
+constexpr int kWriteThreads = 128, kWriteRows = 2, kWriteCTAs = 8;   // CTAs of an SM
 template <typename T>
-__global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const WriteArgs<T> a)
+__global__ void __launch_bounds__(kWriteThreads, kWriteCTAs) paged_write_kernel(const WriteArgs<T> a)
 {
     using C = Chunk<T>;
     extern __shared__ int prefix[];   // [R + 1] touched pages before request r
     __shared__ long long warps[kWriteThreads / 32];
     __shared__ float sums[kWriteThreads][C::N];
     const int R = a.t.requests, each = (R + kWriteThreads - 1) / kWriteThreads, r0 = min(R, (int)threadIdx.x * each), r1 = min(R, r0 + each);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const auto touched = [&](int r) {
         const Added q = added(a, r);
         return q.n ? (int)((q.length + (long long)q.n + a.page - 1) / a.page) - q.length / a.page : 0;
@@ -779,11 +781,11 @@ template <typename T, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32) paged_select_kernel(const SelectArgs<T> a)
 {
     __shared__ int sums[2][WARPS];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int n = pages_seen(a, blockIdx.x / a.kv_heads);
     int *list = a.lists + (long long)blockIdx.x * a.keep;
     for (int p = threadIdx.x; p < a.keep; p += WARPS * 32)
         if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // (by all CTAs: what comes behind this launch counts on the one ahead of it)
     if (n <= a.keep) return;
     const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.t.width;
     if (n <= 256 * WARPS) select_best<WARPS, 8>(keys, n, a.keep, a.first, a.last, list, sums);

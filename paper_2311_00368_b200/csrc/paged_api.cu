@@ -1,5 +1,6 @@
 // Entry points of the cache in pages: argument checks and launches.  See include/b2sp.h.
 #include <algorithm>
+#include <atomic>
 #include <climits>
 
 #include "paged_attention.cuh"
@@ -9,18 +10,29 @@ namespace paged {
 
 inline b2sp_status launched() { return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA; }
 constexpr int kSMs = 148;
+constexpr size_t kMostShared = 227 * 1024;   // of a CTA
 
-// More shared memory than a launch gets unasked (48 KB with what the kernel has of its own).  The kernels of a call all ask for the same split between
-// shared memory and cache: an SM changes it only when it is empty.
-template <typename K> bool allow_shared(K *kernel, size_t bytes)
+// More shared memory than a launch gets unasked (48 KB with what the kernel has of its own): asked for once on each device.
+template <auto Kernel> bool allow_shared(size_t bytes)
 {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) == cudaSuccess &&
-           (bytes <= 40 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess);
+    if (bytes <= 40 * 1024) return true;
+    static std::atomic<size_t> allowed[64];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return false;
+    std::atomic<size_t> *mine = device < 64 ? allowed + device : nullptr;
+    if (mine && mine->load() >= bytes) return true;
+    // as much as the kernel can have, whatever this call needs: so no call takes away what another has asked for
+    cudaFuncAttributes has;
+    if (cudaFuncGetAttributes(&has, Kernel) != cudaSuccess) return false;
+    const size_t most = kMostShared - has.sharedSizeBytes;
+    if (bytes > most || cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) != cudaSuccess) return false;
+    if (mine) mine->store(most);
+    return true;
 }
 // A launch that may begin before the one ahead of it has ended (the kernels wait for that themselves).
-template <typename K, typename... Args> bool launch_early(K *kernel, dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
+template <auto Kernel, typename... Args> bool launch_early(dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
 {
-    if (!allow_shared(kernel, shared)) return false;
+    if (!allow_shared<Kernel>(shared)) return false;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = blocks;
     cfg.blockDim = dim3(threads);
@@ -31,7 +43,7 @@ template <typename K, typename... Args> bool launch_early(K *kernel, dim3 blocks
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+    return cudaLaunchKernelEx(&cfg, Kernel, args...) == cudaSuccess;
 }
 
 b2sp_status check_tables(const b2sp_page_tables *t, int page)
@@ -106,10 +118,9 @@ b2sp_status write(int tokens, int heads, int d, const T *K, long long ldk, long 
     if (means) a.means = pages<T>(means);
     // as many pages as the tokens can touch: at most two that are not full for each request that has any
     const long long units = (tokens / kp->page + 2ll * std::min(t->requests, tokens)) * heads;
-    const unsigned blocks = (unsigned)std::min(units, 16ll * kSMs);
+    const unsigned blocks = (unsigned)std::min(units, (long long)kWriteCTAs * kSMs);
     const size_t shared = (t->requests + 1) * sizeof(int);
-    paged_write_kernel<T><<<blocks, kWriteThreads, shared, static_cast<cudaStream_t>(stream)>>>(a);
-    return launched();
+    return launch_early<paged_write_kernel<T>>(blocks, kWriteThreads, shared, static_cast<cudaStream_t>(stream), a) ? launched() : B2SP_ERR_CUDA;
 }
 
 bool token_args_ok(int M, int heads, int kv_heads, int d) { return M >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1; }
@@ -145,16 +156,16 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
         const unsigned grid = (unsigned)std::min((blocks + kScoreThreads / 32 - 1) / (kScoreThreads / 32), (long long)kSMs * kScoreCTAs);
         constexpr int N = 16 / sizeof(T);
         bool ok = false;
-        if (d <= 8 * N) ok = launch_early(paged_score_kernel<T, 8, 1>, grid, kScoreThreads, 0, st, a);
-        else if (d <= 16 * N) ok = launch_early(paged_score_kernel<T, 16, 1>, grid, kScoreThreads, 0, st, a);
-        else if (d <= 32 * N) ok = launch_early(paged_score_kernel<T, 32, 1>, grid, kScoreThreads, 0, st, a);
-        else if constexpr (sizeof(T) == 4) ok = launch_early(paged_score_kernel<T, 32, 2>, grid, kScoreThreads, 0, st, a);
+        if (d <= 8 * N) ok = launch_early<paged_score_kernel<T, 8, 1>>(grid, kScoreThreads, 0, st, a);
+        else if (d <= 16 * N) ok = launch_early<paged_score_kernel<T, 16, 1>>(grid, kScoreThreads, 0, st, a);
+        else if (d <= 32 * N) ok = launch_early<paged_score_kernel<T, 32, 1>>(grid, kScoreThreads, 0, st, a);
+        else if constexpr (sizeof(T) == 4) ok = launch_early<paged_score_kernel<T, 32, 2>>(grid, kScoreThreads, 0, st, a);
         if (!ok) return B2SP_ERR_CUDA;
     }
     // a warp holds 2048 keys
     if (t->width <= 2048) {
-        if (!launch_early(paged_select_kernel<T, 1>, (unsigned)ctas, 32, 0, st, a)) return B2SP_ERR_CUDA;
-    } else if (!launch_early(paged_select_kernel<T, 8>, (unsigned)ctas, 256, 0, st, a)) {
+        if (!launch_early<paged_select_kernel<T, 1>>((unsigned)ctas, 32, 0, st, a)) return B2SP_ERR_CUDA;
+    } else if (!launch_early<paged_select_kernel<T, 8>>((unsigned)ctas, 256, 0, st, a)) {
         return B2SP_ERR_CUDA;
     }
     return launched();
@@ -180,6 +191,11 @@ template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d, lo
     return p;
 }
 
+size_t attention_bytes(int heads, int kv_heads, int d)   // for either type and any tokens
+{
+    return std::max(attention_plan<float>(heads, kv_heads, d, INT_MAX).bytes, attention_plan<Bf16>(heads, kv_heads, d, INT_MAX).bytes);
+}
+
 template <typename T, int W, int Q> b2sp_status launch_attention(AttnArgs<T> &a, const AttnPlan &p, long long most_tiles, cudaStream_t st)
 {
     using F = Form<T, W>;
@@ -188,14 +204,14 @@ template <typename T, int W, int Q> b2sp_status launch_attention(AttnArgs<T> &a,
     const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps));
     if (most_cost / (ctas * kAttnWarps) >= 1 << 30) return B2SP_ERR_UNSUPPORTED;   // (a warp counts its share in 32 bits)
     a.by_unit = units <= ctas * (long long)kAttnWarps;
-    const bool ok = a.page % F::ROWS == 0 ? launch_early(paged_attention_kernel<T, W, Q, true>, ctas, kAttnWarps * 32, F::SHARED, st, a)
-                                          : launch_early(paged_attention_kernel<T, W, Q, false>, ctas, kAttnWarps * 32, F::SHARED, st, a);
+    const bool ok = a.page % F::ROWS == 0 ? launch_early<paged_attention_kernel<T, W, Q, true>>(ctas, kAttnWarps * 32, F::SHARED, st, a)
+                                          : launch_early<paged_attention_kernel<T, W, Q, false>>(ctas, kAttnWarps * 32, F::SHARED, st, a);
     if (!ok) return B2SP_ERR_CUDA;
     // Few units have many parts each: sixteen warps for a query, else one.
     const unsigned joins = a.by_unit ? (unsigned)units : ctas * kAttnWarps, queries = std::min(a.pack * a.group, p.queries);
     const bool joined = units * 16 <= ctas * kAttnWarps
-                            ? launch_early(paged_join_kernel<T, W, 16>, dim3(joins, queries), 512, 0, st, a, p.queries)
-                            : launch_early(paged_join_kernel<T, W, 1>, dim3(joins, (queries + 7) / 8), 256, 0, st, a, p.queries);
+                            ? launch_early<paged_join_kernel<T, W, 16>>(dim3(joins, queries), 512, 0, st, a, p.queries)
+                            : launch_early<paged_join_kernel<T, W, 1>>(dim3(joins, (queries + 7) / 8), 256, 0, st, a, p.queries);
     return joined ? launched() : B2SP_ERR_CUDA;
 }
 
@@ -218,7 +234,7 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
         if (std::max({c->ld, c->stride_head, c->stride_page, ldq, shq, ldo, sho, t->ld}) > most_stride) return B2SP_ERR_UNSUPPORTED;
     const AttnPlan p = attention_plan<T>(heads, kv_heads, d, rows && !lists && t->requests ? M / t->requests : 1);
     if ((long long)M * kv_heads * p.blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes) return B2SP_ERR_WORKSPACE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < attention_bytes(heads, kv_heads, d)) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
     AttnArgs<T> a = {};
     a.t = tables(t);
@@ -272,15 +288,13 @@ extern "C" b2sp_status b2sp_paged_tables(const b2sp_page_tables *t, int pages, i
     if (meet(lengths, 4ull * R, lengths_out, 4ull * R) || meet(counts, 16, free_count, 4)) return B2SP_ERR_INVALID_ARG;   // CTAs read the one while others write the other
     if (R > kMostRequests || (long long)pages * page > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     const size_t shared = 3 * (R + 1) * sizeof(int);
-    if (!allow_shared(paged_tables_kernel, shared)) return B2SP_ERR_CUDA;
     TablesArgs a = {};
     a.t = tables(t);
     a.page = page; a.pages = pages; a.tokens = tokens; a.free_room = free_room;
     a.lengths = lengths; a.added = added; a.free_count = free_count; a.free_pages = free_pages;
     a.lengths_out = lengths_out; a.row_ptr = row_ptr; a.rows = rows; a.seen = seen; a.slots = slots; a.counts = counts;
     const unsigned blocks = (unsigned)std::min(std::max(((long long)std::max(tokens, R) + kThreads - 1) / kThreads, 1ll), 2ll * kSMs);
-    paged_tables_kernel<<<blocks, kThreads, shared, static_cast<cudaStream_t>(stream)>>>(a);
-    return launched();
+    return launch_early<paged_tables_kernel>(blocks, kThreads, shared, static_cast<cudaStream_t>(stream), a) ? launched() : B2SP_ERR_CUDA;
 }
 
 extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pages, int page, const int *rows, const int *seen, long long entries,
@@ -298,10 +312,10 @@ extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pa
     const unsigned blocks = (unsigned)std::min(std::max((entries + 4 * kThreads - 1) / (4 * kThreads), 1ll), 8ll * kSMs);
     bool ok;
     if (M <= kListTokens) {
-        ok = launch_early(paged_list_kernel<true>, blocks, kThreads, (M + 1) * sizeof(int), st, a);
+        ok = launch_early<paged_list_kernel<true>>(blocks, kThreads, (M + 1) * sizeof(int), st, a);
     } else {
-        ok = launch_early(paged_list_ends_kernel, 1, kScanThreads, 0, st, a);
-        if (ok && entries) ok = launch_early(paged_list_kernel<false>, blocks, kThreads, 0, st, a);
+        ok = launch_early<paged_list_ends_kernel>(1, kScanThreads, 0, st, a);
+        if (ok && entries) ok = launch_early<paged_list_kernel<false>>(blocks, kThreads, 0, st, a);
     }
     if (!ok) return B2SP_ERR_CUDA;
     return launched();
@@ -342,7 +356,7 @@ extern "C" b2sp_status b2sp_paged_select_bf16(int M, int heads, int kv_heads, in
 extern "C" size_t b2sp_attention_paged_workspace_bytes(int M, int heads, int kv_heads, int d)
 {
     if (!token_args_ok(M, heads, kv_heads, d) || d > 256) return 0;
-    return std::max(attention_plan<float>(heads, kv_heads, d, INT_MAX).bytes, attention_plan<Bf16>(heads, kv_heads, d, INT_MAX).bytes);
+    return attention_bytes(heads, kv_heads, d);
 }
 extern "C" b2sp_status b2sp_attention_paged(int M, int heads, int kv_heads, int d, const float *Q, long long ldq, long long shq, const b2sp_pages *kp,
                                             const b2sp_pages *vp, const b2sp_page_tables *t, const int *rows, const int *seen, const int *lists, int keep,

@@ -21,7 +21,7 @@ namespace paged {
 constexpr int kAttnWarps = 4, kStages = 3;   // warps of a CTA; tiles of a warp in shared memory
 // A unit costs its tiles and, before the first one, a chain of latencies (lengths, table, rows), as long as about four tiles take: without it warps whose
 // shares were many short units took twice as long as the others.  Shares are of at least kLeastCost.
-constexpr int kUnitCost = 4, kLeastCost = 8;
+constexpr int kUnitCost = 4, kLeastCost = 3;
 
 // W: width class of d (64, 128, 256).
 template <typename T, int W> struct Form {
