@@ -198,10 +198,12 @@ size_t attention_bytes(int heads, int kv_heads, int d)   // for either type and 
 
 template <typename T, int W, int Q> b2sp_status launch_attention(AttnArgs<T> &a, const AttnPlan &p, long long most_tiles, cudaStream_t st)
 {
-    using F = Form<T, W>;
+    using F = Form<T, W, Q>;
+    static_assert(F::CTAS == Form<T, W>::CTAS, "");
     const long long units = (long long)a.M * a.kv_heads * a.blocks, most_cost = most_tiles + units * kUnitCost;
     // no more CTAs than have a share, if every token sees all that it can
-    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps));
+    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, std::max((most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps), (a.blocks + kAttnWarps - 1ll) / kAttnWarps));
+    if ((long long)a.blocks > ctas * (long long)kAttnWarps) return B2SP_ERR_UNSUPPORTED;   // (each warp has one block of a key head's queries)
     if (most_cost / (ctas * kAttnWarps) >= 1 << 30) return B2SP_ERR_UNSUPPORTED;   // (a warp counts its share in 32 bits)
     a.by_unit = units <= ctas * (long long)kAttnWarps;
     const bool ok = a.page % F::ROWS == 0 ? launch_early<paged_attention_kernel<T, W, Q, true>>(ctas, kAttnWarps * 32, F::SHARED, st, a)
@@ -254,7 +256,7 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     a.by_blocks = Div(p.blocks);
     a.by_heads = Div(a.pack > 1 ? a.group : p.queries);
     a.pairs = fits<T>(Q, ldq, shq, 4) && fits<T>(O, ldo, sho, 4) && d % 2 == 0;
-    a.fours = fits<T>(Q, ldq, shq, 16) && d % 4 == 0;
+    a.fours = fits<T>(Q, ldq, shq, 16) && (sizeof(T) == 2 || d % 4 == 0);
     char *ws = static_cast<char *>(workspace);
     a.joins = reinterpret_cast<int4 *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.ml);

@@ -24,11 +24,11 @@ constexpr int kAttnWarps = 4, kStages = 3;   // warps of a CTA; tiles of a warp 
 constexpr int kUnitCost = 4, kLeastCost = 3;
 
 // W: width class of d (64, 128, 256).
-template <typename T, int W> struct Form {
+template <typename T, int W, int Q = 8> struct Form {
     static constexpr int ROW = W * (int)sizeof(T), ROWS = ROW == 1024 ? 8 : ROW == 128 ? 32 : 16;   // bytes of a row in shared memory; rows of a tile
     static constexpr int TILE = 2 * ROWS * ROW, RING = kStages * TILE;             // K's rows, then V's
-    static constexpr int WEIGHTS = sizeof(T) == 4 ? 640 : 0;                       // fp32: a tile's weights
-    static constexpr int SHARED = kAttnWarps * (RING + WEIGHTS);
+    static constexpr int STORED = sizeof(T) == 4 ? 640 : W == 256 && Q == 16 ? Q * ROW : 0;   // what a warp keeps there beside its ring: fp32 a tile's weights
+    static constexpr int SHARED = kAttnWarps * (RING + STORED);
     static constexpr int CTAS = SHARED <= 113 * 1024 ? 2 : 1;   // of an SM
 };
 
@@ -47,7 +47,7 @@ template <typename T> struct AttnArgs {
     int keep;
     float scale;
     Div by_page, by_heads, by_blocks;   // by_heads: heads of one token in a unit
-    bool pairs, fours, by_unit;   // pairs: Q and O begin on four bytes and d is even; fours: Q on sixteen, d a multiple of four; by_unit: `joins` are indexed by unit, else by warp
+    bool pairs, fours, by_unit;   // pairs: Q and O begin on four bytes and d is even; fours: Q on sixteen, and fp32's d is a multiple of four; by_unit: `joins` are indexed by unit, else by warp
     T *out;
     unsigned out_ld, out_sh;
     float *lse;
@@ -121,7 +121,7 @@ __device__ __forceinline__ unsigned long long times(int a, unsigned b) { return 
 
 // A piece of a unit: tiles [first, last) of `tiles`.
 struct Piece {
-    int i, unit, first, last, tiles;
+    int i, unit, first, last, tiles;   // unit: key head
     Pack p;
 };
 
@@ -174,7 +174,7 @@ template <typename T, int W, bool ALIGNED> struct Feed {
     }
     __device__ __forceinline__ void begin(const Piece &x, int request)
     {
-        const int g = (int)a.by_blocks((unsigned)x.unit);
+        const int g = x.unit;
         seen = x.p.most;
         table = a.t.entries + (seen ? times(request, (unsigned)a.t.ld) : 0);
         list = a.lists ? a.lists + times(x.i * a.kv_heads + g, a.keep) : nullptr;
@@ -290,8 +290,9 @@ constexpr float kAhead = 8.f;   // the reference of the exponentials follows the
 // the lower part would make 0 * inf or inf - inf of it, so a unit whose sums are not finite is taken again with the upper part alone.
 template <int W, int NT> struct Tile16 {
     static constexpr int QUERIES = 8 * NT, KS = W / 16;
-    static constexpr bool EARLY = W < 256;   // a unit's queries are loaded while the one before it is taken (wider ones would not fit)
-    unsigned q[KS][NT][2], early[EARLY ? KS : 1][NT][2];
+    // a unit's queries are loaded while the one before it is taken (wider ones would not fit); sixteen of the widest stay in shared memory
+    static constexpr bool EARLY = W < 256, STORED = W == 256 && NT == 2;
+    unsigned q[STORED ? 1 : KS][NT][2], early[EARLY ? KS : 1][NT][2];
     float o[KS][NT][4];       // [columns 16 x ..][queries 8 x ..]: columns g, g + 8 (pairs), queries 2 t, 2 t + 1
     float base[NT][2], ahead[NT][2], sum[NT][2];   // of queries 2 t, 2 t + 1; ahead: by how much a logit may exceed base (-inf: none has been met)
     int sees[NT][2];
@@ -327,14 +328,23 @@ template <int W, int NT> struct Tile16 {
     }
     __device__ __forceinline__ void look_ahead(const Queries<Bf16> &u, int lane) { if constexpr (EARLY) load(u, lane, early); }
     // at_once: nothing was loaded early
-    __device__ __forceinline__ void begin(const Queries<Bf16> &u, int lane, bool alike, bool at_once)
+    __device__ __forceinline__ void begin(const Queries<Bf16> &u, int lane, bool alike, bool at_once, char *stored)
     {
-        if (EARLY && !at_once) {
+        if constexpr (STORED) {
+            for (int x = lane; x < QUERIES * (W / 8); x += 32) {   // (of eight neighbouring elements each)
+                const int c = x / (W / 8), chunk = x % (W / 8), e = chunk * 8;
+                Chunk<Bf16> y;
+                y.u = make_uint4(0, 0, 0, 0);
+                if (c < u.n) y.load(u.query(c), e, u.a.d, u.a.fours && e + 8 <= u.a.d);
+                *reinterpret_cast<uint4 *>(stored + c * Form<Bf16, W>::ROW + (chunk ^ (c & 7)) * 16) = y.u;
+            }
+            __syncwarp();
+        } else if (EARLY && !at_once) {
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
                 for (int m = 0; m < NT; ++m) { q[s][m][0] = early[EARLY ? s : 0][m][0]; q[s][m][1] = early[EARLY ? s : 0][m][1]; }
-        } else {
+        } else if constexpr (!STORED) {
             load(u, lane, q);
         }
 #pragma unroll
@@ -355,7 +365,7 @@ template <int W, int NT> struct Tile16 {
         }
     }
     // there: the tile's rows that are there; first: the position of its row 0, or -1 if all queries see all of them.
-    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, float *)
+    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, char *stored)
     {
         using F = Form<Bf16, W>;
         constexpr int H = F::ROWS / 16, SUMS = H == 1 ? 2 : 1;   // sixteens of rows; sums of a product (so that few products wait for one another)
@@ -371,8 +381,16 @@ template <int W, int NT> struct Tile16 {
                 for (int h = 0; h < H; ++h) {
                     unsigned k[4];
                     load_matrices(k, from + h * 16 * F::ROW + (turn ^ (s & 3) * 32) + (s >> 2) * 128);
+                    if constexpr (STORED) {
+                        unsigned b[4];
+                        const int c = (lane >> 4) * 8 + (lane & 7);
+                        load_matrices(b, (unsigned)__cvta_generic_to_shared(stored) + c * F::ROW + (((lane >> 3 & 1) ^ (lane & 7)) * 16 ^ (s & 3) * 32) + (s >> 2) * 128);
 #pragma unroll
-                    for (int m = 0; m < NT; ++m) mma_bf16(s % SUMS ? y[h][m] : x[h][m], k, q[s][m][0], q[s][m][1]);
+                        for (int m = 0; m < NT; ++m) mma_bf16(s % SUMS ? y[h][m] : x[h][m], k, b[2 * m], b[2 * m + 1]);
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < NT; ++m) mma_bf16(s % SUMS ? y[h][m] : x[h][m], k, q[s][m][0], q[s][m][1]);
+                    }
                 }
             if (SUMS == 2) {
 #pragma unroll
@@ -577,7 +595,7 @@ template <int W, int Q> struct Tile32 {
         }
     }
     __device__ __forceinline__ void look_ahead(const Queries<float> &u, int lane) { if constexpr (EARLY) load(u, lane, early); }
-    __device__ __forceinline__ void begin(const Queries<float> &u, int lane, bool alike, bool at_once)
+    __device__ __forceinline__ void begin(const Queries<float> &u, int lane, bool alike, bool at_once, char *)
     {
         if (EARLY && !at_once) {
 #pragma unroll
@@ -597,8 +615,9 @@ template <int W, int Q> struct Tile32 {
             for (int c = 0; c < COLS; ++c) o[h][c] = 0;
     }
     static __device__ __forceinline__ int weights_of(int row) { return row * Q + row / MINE * Q; }   // (rows that are written at once lie in different banks)
-    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, float *weights)
+    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, char *stored)
     {
+        float *weights = reinterpret_cast<float *>(stored);
         using F = Form<float, W>;
         const int part = lane / Q;
         float s[ROWS];
@@ -737,22 +756,23 @@ template <int W, int Q> struct TileOf<float, W, Q> { using type = Tile32<W, Q>; 
 
 // The warp's pieces follow one another without a pause: while one is taken, the rows of the next one are looked up and copied and its queries loaded.
 template <typename T, int W, int Q, bool ALIGNED>
-__global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_attention_kernel(const AttnArgs<T> a)
+__global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_attention_kernel(const AttnArgs<T> a)
 {
-    using F = Form<T, W>;
+    using F = Form<T, W, Q>;
     using Tile = typename TileOf<T, W, Q>::type;
     extern __shared__ __align__(128) char shared[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x * kAttnWarps + warp;
-    const int units = a.kv_heads * a.blocks;   // of a token
+    // neighbouring warps have the same share for the blocks of a key head's queries, so that rows come from HBM once
+    const int units = a.kv_heads, part = (int)a.by_blocks((unsigned)me), block = me - part * a.blocks, parts = gridDim.x * kAttnWarps / a.blocks;
     const char *ring = shared + warp * F::RING;
     const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
-    float *weights = reinterpret_cast<float *>(shared + kAttnWarps * F::RING + warp * F::WEIGHTS);
+    char *stored = shared + kAttnWarps * F::RING + warp * F::STORED;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     Share share;
     Window window;
     const auto load = [&](int base) { return window_of(a, base, lane); };
     const auto cost = [&](const Window &w) { return cost_of<F::ROWS>(a, window = w, lane); };
-    if (!deal<kAttnWarps * 32>(a.M, units, load, cost, gridDim.x * kAttnWarps, me, kLeastCost, share)) {
+    if (!deal<kAttnWarps * 32>(a.M, units, load, cost, parts, part, kLeastCost, share) || part >= parts) {
         if (!a.by_unit && lane == 0) a.joins[me] = make_int4(0, -1, 0, 0);
         return;
     }
@@ -766,8 +786,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
     const int size = (int)(share.hi - share.lo);   // (of 2^27 tiles of a row and 2^31 rows at most, in shares of thousands of them)
     int at = 0, before = (int)(share.rest - (long long)unit * (tiles + kUnitCost));
     const auto queries_of = [&](const Piece &x) {
-        const int g = (int)a.by_blocks((unsigned)x.unit), b = x.unit - g * a.blocks;
-        return Queries<T>{a, x.i, g * a.group + b * Tile::QUERIES, a.pack > 1 ? x.p.n * a.group : min(Tile::QUERIES, a.group - b * Tile::QUERIES)};
+        return Queries<T>{a, x.i, x.unit * a.group + block * Tile::QUERIES, a.pack > 1 ? x.p.n * a.group : min(Tile::QUERIES, a.group - block * Tile::QUERIES)};
     };
     Feed<T, W, ALIGNED> feed(a, lane);
     Tile x;
@@ -779,7 +798,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
             to.last = end - begin - kUnitCost;
             // a unit that begins here and ends elsewhere: its last tile lies with the last warp
             if (to.first == 0 && to.last > 0 && to.last < tiles)
-                join = make_int4(token * units + unit, me, me + (int)((unsigned)(begin + tiles + kUnitCost - 1) / (unsigned)share.share), 0);
+                join = make_int4((token * units + unit) * a.blocks + block, me, me + (int)((unsigned)(begin + tiles + kUnitCost - 1) / (unsigned)share.share) * a.blocks, 0);
             at = end;
             before = 0;
             if (++unit == units) {
@@ -804,7 +823,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
     }
     start(now);
     bool more = false, fed = false;   // there is a next piece; its rows are being copied
-    x.begin(queries_of(now), lane, now.p.n == 1, true);
+    x.begin(queries_of(now), lane, now.p.n == 1, true, stored);
     int ahead = 0, stage = 0, j = now.first;   // tiles that are on their way; the stage of the oldest, the tile that it is
     unsigned there0 = 0, there1 = 0, there2 = 0;
     for (;;) {
@@ -819,7 +838,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
         else if (ahead == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
-        if (there0) x.take(ring + stage * F::TILE, there0, now.p.n > 1 && (j + 1) * F::ROWS > now.p.least ? j * F::ROWS : -1, scale2, lane, weights);
+        if (there0) x.take(ring + stage * F::TILE, there0, now.p.n > 1 && (j + 1) * F::ROWS > now.p.least ? j * F::ROWS : -1, scale2, lane, stored);
         there0 = there1;
         there1 = there2;
         --ahead;
@@ -842,7 +861,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
             continue;
         }
         x.total();
-        const int id = now.i * units + now.unit;
+        const int id = (now.i * units + now.unit) * a.blocks + block;
         const bool all = now.first == 0 && now.last == now.tiles;
         const Queries<T> u = queries_of(now);
         if (all) {
@@ -852,12 +871,12 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W>::CTAS) paged_atten
             x.leave(a.part + slot * Tile::QUERIES * W, a.part_ml + slot * Tile::QUERIES, u.n, lane);
             if (now.first == 0) join.w = u.n;
         }
-        if (now.first == 0 && a.by_unit && lane < now.p.n) a.joins[id + lane * units] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
+        if (now.first == 0 && a.by_unit && lane < now.p.n) a.joins[id + lane * units * a.blocks] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
         if (!more) break;
         now = next;
         more = fed = false;
         j = now.first;
-        x.begin(queries_of(now), lane, now.p.n == 1, false);
+        x.begin(queries_of(now), lane, now.p.n == 1, false, stored);
     }
     if (!a.by_unit && lane == 0) a.joins[me] = join;
 }
@@ -878,12 +897,12 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) paged_join_kern
     const int units = a.kv_heads * a.blocks, i = j.x / units, unit = j.x - i * units, g = unit / a.blocks, b = unit - g * a.blocks;
     const Queries<T> u{a, i, g * a.group + b * queries, j.w};
     float x[V][4] = {}, high = -CUDART_INF_F, l = 0.f;
-    for (int p = j.y + warp; p <= j.z; p += WARPS * AT) {
+    for (int p = j.y + warp * a.blocks; p <= j.z; p += WARPS * AT * a.blocks) {   // (the parts lie with every a.blocks-th warp)
         float y[AT][V][4];
         float2 ml[AT];
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            const int c = p + k * WARPS;
+            const int c = p + k * WARPS * a.blocks;
             ml[k] = make_float2(-CUDART_INF_F, 0.f);
             if (c <= j.z) {
                 const long long slot = (c * 2ll + (c == j.y)) * queries + m;
@@ -904,7 +923,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) paged_join_kern
             for (int k = 0; k < 4; ++k) x[v][k] *= fall;
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            if (p + k * WARPS > j.z) break;
+            if (p + k * WARPS * a.blocks > j.z) break;
             const float f = attn::ex2(ml[k].x - ref);
             l = fmaf(ml[k].y, f, l);
 #pragma unroll

@@ -271,7 +271,7 @@ CASES = [
     ([1], 1, 1, 64, 1), ([15, 16, 17, 0, 1], 4, 2, 128, 16), ([70, 0, 64, 65, 3, 500], 8, 1, 64, 64), ([129, 1000], 16, 1, 32, 24),
     ([300, 20, 7], 20, 1, 96, 7), ([200, 31], 6, 2, 17, 150), ([5000], 8, 2, 128, 64), ([40] * 33, 32, 8, 80, 16), ([3000, 10, 0, 800], 40, 1, 128, 128),
     ([2, 0, 4, 1] * 30, 4, 4, 128, 5), ([1, 3] * 100 + [3000], 8, 2, 64, 16), ([500, 90], 4, 2, 256, 32), ([77, 260], 9, 3, 200, 11), ([33], 2, 2, 1, 4),
-    ([700] * 3, 64, 1, 64, 64),
+    ([700] * 3, 64, 1, 64, 64), ([900, 3, 0, 2000], 16, 1, 256, 64), ([300, 70], 48, 1, 200, 24), ([5, 1500], 100, 2, 128, 32), ([40], 1000, 1, 64, 16),
 ]
 
 
