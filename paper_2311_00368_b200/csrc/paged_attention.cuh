@@ -89,10 +89,16 @@ template <typename T> __device__ __forceinline__ Pack pack_of(const AttnArgs<T> 
     }
     return p;
 }
+// Positions of the line of a unit whose tokens see `most`: these, or those of as many entries of the list as there are pages in them.
+template <typename T> __device__ __forceinline__ int line_of(const AttnArgs<T> &a, int most)
+{
+    if (!a.lists) return most;
+    const int c = (int)a.by_page((unsigned)most);
+    return min(a.keep, c + (c * a.page < most)) * a.page;
+}
 template <int ROWS, typename T> __device__ __forceinline__ int tiles_of(const AttnArgs<T> &a, int most)
 {
-    const int n = a.lists && most ? a.keep * a.page : most;
-    return max(1, (int)((n + (ROWS - 1ll)) / ROWS));   // (tokens that see nothing have a tile of nothing)
+    return max(1, (int)(((unsigned)line_of(a, most) + (ROWS - 1u)) / ROWS));   // (tokens that see nothing have a tile of nothing)
 }
 // What each unit of a window's token `lane` costs: nothing if the token belongs to the units of one before it.
 template <int ROWS, typename T> __device__ __forceinline__ int cost_of(const AttnArgs<T> &a, const Window &w, int lane)
@@ -178,7 +184,7 @@ template <typename T, int W, bool ALIGNED> struct Feed {
         seen = x.p.most;
         table = a.t.entries + (seen ? times(request, (unsigned)a.t.ld) : 0);
         list = a.lists ? a.lists + times(x.i * a.kv_heads + g, a.keep) : nullptr;
-        n = seen == 0 ? 0 : list ? a.keep * a.page : seen;
+        n = line_of(a, seen);
         k = a.k.data + times(g, a.k.sh);
         v = a.v.data + times(g, a.v.sh);
         if (ALIGNED) {   // (what a lane does not read is not pointed to either)

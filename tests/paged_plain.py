@@ -46,7 +46,8 @@ def positions(tables, row, seen, page, pages, listed=None):
     if not 0 <= row < len(tables):
         return []
     seen = min(max(seen, 0), len(tables[row]) * page)
-    at = range(seen) if listed is None else [c * page + i for c in listed if c >= 0 for i in range(page)]
+    # of a list the first entries count, as many as there are pages
+    at = range(seen) if listed is None else [c * page + i for c in listed[:-(-seen // page)] if c >= 0 for i in range(page)]
     return [(tables[row][p // page], p % page) for p in at if p < seen and 0 <= tables[row][p // page] < pages]
 
 
