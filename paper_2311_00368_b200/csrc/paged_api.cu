@@ -202,8 +202,7 @@ template <typename T, int W, int Q> b2sp_status launch_attention(AttnArgs<T> &a,
     static_assert(F::CTAS == Form<T, W>::CTAS, "");
     const long long units = (long long)a.M * a.kv_heads * a.blocks, most_cost = most_tiles + units * kUnitCost;
     // no more CTAs than have a share, if every token sees all that it can
-    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, std::max((most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps), (a.blocks + kAttnWarps - 1ll) / kAttnWarps));
-    if ((long long)a.blocks > ctas * (long long)kAttnWarps) return B2SP_ERR_UNSUPPORTED;   // (each warp has one block of a key head's queries)
+    const unsigned ctas = (unsigned)std::min((long long)kSMs * F::CTAS, (most_cost + kLeastCost * kAttnWarps - 1) / (kLeastCost * kAttnWarps));
     if (most_cost / (ctas * kAttnWarps) >= 1 << 30) return B2SP_ERR_UNSUPPORTED;   // (a warp counts its share in 32 bits)
     a.by_unit = units <= ctas * (long long)kAttnWarps;
     const bool ok = a.page % F::ROWS == 0 ? launch_early<paged_attention_kernel<T, W, Q, true>>(ctas, kAttnWarps * 32, F::SHARED, st, a)

@@ -127,7 +127,7 @@ __device__ __forceinline__ unsigned long long times(int a, unsigned b) { return 
 
 // A piece of a unit: tiles [first, last) of `tiles`.
 struct Piece {
-    int i, unit, first, last, tiles;   // unit: key head
+    int i, unit, first, last, tiles;   // unit: of the token
     Pack p;
 };
 
@@ -180,7 +180,7 @@ template <typename T, int W, bool ALIGNED> struct Feed {
     }
     __device__ __forceinline__ void begin(const Piece &x, int request)
     {
-        const int g = x.unit;
+        const int g = (int)a.by_blocks((unsigned)x.unit);
         seen = x.p.most;
         table = a.t.entries + (seen ? times(request, (unsigned)a.t.ld) : 0);
         list = a.lists ? a.lists + times(x.i * a.kv_heads + g, a.keep) : nullptr;
@@ -768,8 +768,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
     using Tile = typename TileOf<T, W, Q>::type;
     extern __shared__ __align__(128) char shared[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x * kAttnWarps + warp;
-    // neighbouring warps have the same share for the blocks of a key head's queries, so that rows come from HBM once
-    const int units = a.kv_heads, part = (int)a.by_blocks((unsigned)me), block = me - part * a.blocks, parts = gridDim.x * kAttnWarps / a.blocks;
+    const int units = a.kv_heads * a.blocks;   // of a token
     const char *ring = shared + warp * F::RING;
     const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
     char *stored = shared + kAttnWarps * F::RING + warp * F::STORED;
@@ -778,7 +777,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
     Window window;
     const auto load = [&](int base) { return window_of(a, base, lane); };
     const auto cost = [&](const Window &w) { return cost_of<F::ROWS>(a, window = w, lane); };
-    if (!deal<kAttnWarps * 32>(a.M, units, load, cost, parts, part, kLeastCost, share) || part >= parts) {
+    if (!deal<kAttnWarps * 32>(a.M, units, load, cost, gridDim.x * kAttnWarps, me, kLeastCost, share)) {
         if (!a.by_unit && lane == 0) a.joins[me] = make_int4(0, -1, 0, 0);
         return;
     }
@@ -792,7 +791,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
     const int size = (int)(share.hi - share.lo);   // (of 2^27 tiles of a row and 2^31 rows at most, in shares of thousands of them)
     int at = 0, before = (int)(share.rest - (long long)unit * (tiles + kUnitCost));
     const auto queries_of = [&](const Piece &x) {
-        return Queries<T>{a, x.i, x.unit * a.group + block * Tile::QUERIES, a.pack > 1 ? x.p.n * a.group : min(Tile::QUERIES, a.group - block * Tile::QUERIES)};
+        const int g = (int)a.by_blocks((unsigned)x.unit), b = x.unit - g * a.blocks;
+        return Queries<T>{a, x.i, g * a.group + b * Tile::QUERIES, a.pack > 1 ? x.p.n * a.group : min(Tile::QUERIES, a.group - b * Tile::QUERIES)};
     };
     Feed<T, W, ALIGNED> feed(a, lane);
     Tile x;
@@ -804,7 +804,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
             to.last = end - begin - kUnitCost;
             // a unit that begins here and ends elsewhere: its last tile lies with the last warp
             if (to.first == 0 && to.last > 0 && to.last < tiles)
-                join = make_int4((token * units + unit) * a.blocks + block, me, me + (int)((unsigned)(begin + tiles + kUnitCost - 1) / (unsigned)share.share) * a.blocks, 0);
+                join = make_int4(token * units + unit, me, me + (int)((unsigned)(begin + tiles + kUnitCost - 1) / (unsigned)share.share), 0);
             at = end;
             before = 0;
             if (++unit == units) {
@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
             continue;
         }
         x.total();
-        const int id = (now.i * units + now.unit) * a.blocks + block;
+        const int id = now.i * units + now.unit;
         const bool all = now.first == 0 && now.last == now.tiles;
         const Queries<T> u = queries_of(now);
         if (all) {
@@ -877,7 +877,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
             x.leave(a.part + slot * Tile::QUERIES * W, a.part_ml + slot * Tile::QUERIES, u.n, lane);
             if (now.first == 0) join.w = u.n;
         }
-        if (now.first == 0 && a.by_unit && lane < now.p.n) a.joins[id + lane * units * a.blocks] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
+        if (now.first == 0 && a.by_unit && lane < now.p.n) a.joins[id + lane * units] = lane == 0 && !all ? join : make_int4(0, -1, 0, 0);
         if (!more) break;
         now = next;
         more = fed = false;
@@ -903,12 +903,12 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) paged_join_kern
     const int units = a.kv_heads * a.blocks, i = j.x / units, unit = j.x - i * units, g = unit / a.blocks, b = unit - g * a.blocks;
     const Queries<T> u{a, i, g * a.group + b * queries, j.w};
     float x[V][4] = {}, high = -CUDART_INF_F, l = 0.f;
-    for (int p = j.y + warp * a.blocks; p <= j.z; p += WARPS * AT * a.blocks) {   // (the parts lie with every a.blocks-th warp)
+    for (int p = j.y + warp; p <= j.z; p += WARPS * AT) {
         float y[AT][V][4];
         float2 ml[AT];
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            const int c = p + k * WARPS * a.blocks;
+            const int c = p + k * WARPS;
             ml[k] = make_float2(-CUDART_INF_F, 0.f);
             if (c <= j.z) {
                 const long long slot = (c * 2ll + (c == j.y)) * queries + m;
@@ -929,7 +929,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 256 : WARPS * 32) paged_join_kern
             for (int k = 0; k < 4; ++k) x[v][k] *= fall;
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            if (p + k * WARPS * a.blocks > j.z) break;
+            if (p + k * WARPS > j.z) break;
             const float f = attn::ex2(ml[k].x - ref);
             l = fmaf(ml[k].y, f, l);
 #pragma unroll
