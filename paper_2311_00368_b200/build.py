@@ -17,6 +17,7 @@ NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-shared", "-Xcompiler", "-fPIC",
+    "--threads", "4",   # source files at a time
 ]
 
 

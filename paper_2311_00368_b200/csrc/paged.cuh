@@ -541,7 +541,7 @@ template <typename T> struct SelectArgs {
     int M, heads, kv_heads, d, page, keep, first, last;
     bool q_wide;                // 16-byte loads of q
     Pages<T> means;
-    unsigned long long *keys;   // [M][kv_heads][width]
+    float2 *scores;             // [M][kv_heads][width]: a score in 32 bits and how far it may be off
     int *lists;                 // [M][kv_heads][keep]
 };
 template <typename T> __device__ __forceinline__ int pages_seen(const SelectArgs<T> &a, int i)
@@ -556,10 +556,16 @@ __device__ __forceinline__ unsigned long long ordered(double x)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// Scores of the pages of tokens that see more than a list holds.  Sums are formed in 64 bits: the result is a choice, and between two close scores sums of
-// 32 bits would choose by their order.  The blocks of 32 pages of all tokens and key heads are dealt to the warps in equal shares; the sum of the group's
-// queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, eight instructions at a time.
-constexpr int kScorePages = 32, kScoreThreads = 128, kScoreCTAs = 4;   // CTAs of an SM
+// The choice is defined by scores in 64 bits, since between two close ones sums of 32 bits would choose by their order.  Few scores are that close: they
+// are formed in 32 bits with a bound of the error, and a token whose border lies between two scores that are further apart than that is done; only
+// where others lie within reach of the border these are formed again in 64 bits.  (All of them in 64 bits took twice as long: conversions and long chains.)
+//
+// Scores of the pages of tokens that see more than a list holds: all tokens' and key heads' blocks of pages are dealt to the warps in equal shares; the sum of the
+// group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  A lane adds up eight products and the lanes' sums come together in at most five steps, so a score is off
+// by at most 14 half steps of the sum of the products' magnitudes (one of them the query's rounding), and by what underflows; kScoreOff leaves room for the
+// rounding of that sum itself and of what the choice makes of it.
+constexpr float kScoreOff = 24.f * 5.9604645e-8f, kUnderflow = 1e-42f;
+constexpr int kScoreThreads = 128, kScoreCTAs = 4;   // CTAs of an SM
 template <typename T, int LANES, int HALVES>
 __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) paged_score_kernel(const SelectArgs<T> a)
 {
@@ -568,21 +574,21 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const auto blocks_of = [&](int i) {
         const int n = pages_seen(a, i);
-        return n > a.keep ? (n + kScorePages - 1) / kScorePages : 0;
+        return n > a.keep ? (n + BATCH - 1) / BATCH : 0;
     };
     Share w;
     const auto load = [&](int base) { return base + lane < a.M ? blocks_of(base + lane) : 0; };
     if (!deal<kScoreThreads>(a.M, a.kv_heads, load, [](int blocks) { return blocks; }, gridDim.x * (kScoreThreads / 32), me, 1, w)) return;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    int i = w.row, n = pages_seen(a, i), blocks = (n + kScorePages - 1) / kScorePages, g = (int)w.rest / blocks, b = (int)w.rest - g * blocks;
+    int i = w.row, n = pages_seen(a, i), blocks = (n + BATCH - 1) / BATCH, g = (int)w.rest / blocks, b = (int)w.rest - g * blocks;
     const int e0 = lane % LANES * N;   // this lane's first element
-    double q[HALVES][N];
+    float q[HALVES][N];
     uint4 now[AT_ONCE][HALVES], next[AT_ONCE][HALVES];
     const auto look_up = [&](int p) { return p < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p] : -1; };
-    const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int held, int g, int s) {   // means of pages s ... of a block whose pages the lanes hold
+    const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int held, int g) {   // means of a block whose pages the lanes hold
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-            const int p = __shfl_sync(~0u, held, s + j * STEP + lane / LANES);
+            const int p = __shfl_sync(~0u, held, j * STEP + lane / LANES);
             const T *mean = a.means.row(p, g, 0) + e0;
 #pragma unroll
             for (int x = 0; x < HALVES; ++x) {
@@ -591,17 +597,14 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
             }
         }
     };
-    int held = look_up(b * kScorePages + lane);
-    read(now, held, g, 0);
+    int held = look_up(b * BATCH + lane % BATCH);
+    read(now, held, g);
     bool fresh = true;
-    // Means are on their way a batch ahead, pages a block ahead.
+    // Means are on their way a block ahead.
     for (int left = (int)(w.hi - w.lo);;) {
-        const int of_i = i, of_g = g, of_n = n, p0 = b * kScorePages, mine_held = held;
+        const int of_i = i, of_g = g, of_n = n, p0 = b * BATCH, mine_held = held;
         if (fresh) {   // the sum of the queries, four heads' loads at once
-#pragma unroll
-            for (int x = 0; x < HALVES; ++x)
-#pragma unroll
-                for (int k = 0; k < N; ++k) q[x][k] = 0;
+            double total[HALVES][N] = {};
             const T *from = a.q + i * a.q_ld + (long long)g * group * a.q_sh;
             for (int h = 0; h < group; h += 4) {
                 Chunk<T> y[4][HALVES];
@@ -619,9 +622,13 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                         float f[N] = {};
                         y[k][x].add_to(f);
 #pragma unroll
-                        for (int m = 0; m < N; ++m) q[x][m] += f[m];
+                        for (int m = 0; m < N; ++m) total[x][m] += f[m];
                     }
             }
+#pragma unroll
+            for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+                for (int k = 0; k < N; ++k) q[x][k] = (float)total[x][k];
             fresh = false;
         }
         // the next block
@@ -638,28 +645,31 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                     n = pages_seen(a, i);
                 }
             }
-            held = look_up(b * kScorePages + lane);
+            held = look_up(b * BATCH + lane % BATCH);
         }
-        unsigned long long *keys = a.keys + ((long long)of_i * a.kv_heads + of_g) * a.t.width;
-#pragma unroll 1
-        for (int s = 0; s < kScorePages; s += BATCH) {
-            if (s + BATCH < kScorePages) read(next, mine_held, of_g, s + BATCH);
-            else if (more) read(next, held, g, 0);
-            double sum[AT_ONCE];
+        float2 *scores = a.scores + ((long long)of_i * a.kv_heads + of_g) * a.t.width;
+        {
+            if (more) read(next, held, g);
+            float sum[AT_ONCE], size[AT_ONCE];
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j) {
-                sum[j] = 0;
+                sum[j] = size[j] = 0.f;
 #pragma unroll
                 for (int x = 0; x < HALVES; ++x) {
                     float f[N] = {};
                     Chunk<T>{now[j][x]}.add_to(f);
+                    // (0 stays 0 for a mean of zeros alone, whose score is exact)
+                    if ((now[j][x].x | now[j][x].y | now[j][x].z | now[j][x].w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) size[j] += kUnderflow;
                     if (e0 + x * 32 * N + N > a.d) {   // what lies behind d may be anything
 #pragma unroll
                         for (int k = 0; k < N; ++k)
                             if (e0 + x * 32 * N + k >= a.d) f[k] = 0.f;
                     }
 #pragma unroll
-                    for (int k = 0; k < N; ++k) sum[j] += q[x][k] * f[k];
+                    for (int k = 0; k < N; ++k) {
+                        sum[j] = fmaf(q[x][k], f[k], sum[j]);
+                        size[j] = fmaf(fabsf(q[x][k]), fabsf(f[k]), size[j]);
+                    }
                 }
             }
             // LANES lanes' sums of eight: halves of what is left are exchanged until each lane has one, which is then summed up
@@ -672,13 +682,21 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                     mine += up ? v : 0;
 #pragma unroll
                     for (int j = 0; j < AT_ONCE / 2; ++j)
-                        if (j < v) sum[j] = (up ? sum[j + v] : sum[j]) + __shfl_xor_sync(~0u, up ? sum[j] : sum[j + v], x);
+                        if (j < v) {
+                            sum[j] = (up ? sum[j + v] : sum[j]) + __shfl_xor_sync(~0u, up ? sum[j] : sum[j + v], x);
+                            size[j] = (up ? size[j + v] : size[j]) + __shfl_xor_sync(~0u, up ? size[j] : size[j + v], x);
+                        }
                 } else {
                     sum[0] += __shfl_xor_sync(~0u, sum[0], x);
+                    size[0] += __shfl_xor_sync(~0u, size[0], x);
                 }
             }
-            const int k = s + mine * STEP + lane / LANES, page = __shfl_sync(~0u, mine_held, k);
-            if (lane % (LANES / AT_ONCE) == 0 && p0 + k < of_n) keys[p0 + k] = (unsigned)page < (unsigned)a.means.pages ? ordered(sum[0]) : ordered(-CUDART_INF);
+            const int k = mine * STEP + lane / LANES, page = __shfl_sync(~0u, mine_held, k);
+            if (lane % (LANES / AT_ONCE) == 0 && p0 + k < of_n) {
+                // (a page that is none scores -inf)
+                const bool none = (unsigned)page >= (unsigned)a.means.pages;
+                scores[p0 + k] = none ? make_float2(-CUDART_INF_F, 0.f) : make_float2(sum[0], size[0] == 0.f ? 0.f : fmaf(size[0], kScoreOff, kUnderflow));
+            }
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j)
 #pragma unroll
@@ -688,9 +706,6 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
     }
 }
 
-// The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS keys a lane in registers (0: any number, read again each time).  The
-// keep-th largest key is found bit by bit, each time by counting those that are at least as large, first by the keys' upper halves and, where several
-// have that of the border, by their lower ones; it ends early where exactly `keep` are.
 template <int WARPS> __device__ __forceinline__ int count_all(int c, int (&sums)[2][WARPS], int &turn)
 {
     c = __reduce_add_sync(~0u, c);
@@ -703,57 +718,30 @@ template <int WARPS> __device__ __forceinline__ int count_all(int c, int (&sums)
     for (int w = 0; w < WARPS; ++w) c += sums[turn][w];
     return c;
 }
-template <int WARPS, int KEYS>
-__device__ __forceinline__ void select_best(const unsigned long long *keys, int n, int keep, int first, int last, int *list, int (&sums)[2][WARPS])
+// The largest border with at least `want` of the numbers at or above it (in(j, to): whether this lane's j-th is), found bit by bit; at_least: how many are.  It
+// ends early where that is `want`.
+template <int WARPS, typename In>
+__device__ __forceinline__ unsigned border_of(In in, int rounds, int want, int &at_least, int (&sums)[2][WARPS], int &turn)
 {
-    const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
-    const int each = ((n + WARPS - 1) / WARPS + 31) & ~31, p0 = warp * each, p1 = min(n, p0 + each), rounds = KEYS ? KEYS : each / 32;   // this warp's pages
-    const auto key = [&](int j) {
-        const int p = p0 + j * 32 + lane;
-        return p >= p1 ? 0 : p < first || p >= n - last ? ~0ull : keys[p];
-    };
-    unsigned highs[KEYS ? KEYS : 1], lows[KEYS ? KEYS : 1];
-    if constexpr (KEYS > 0) {
-#pragma unroll
-        for (int j = 0; j < KEYS; ++j) {
-            const unsigned long long k = key(j);
-            highs[j] = (unsigned)(k >> 32);
-            lows[j] = (unsigned)k;
-        }
-    }
-    const auto high = [&](int j) { if constexpr (KEYS > 0) return highs[j]; else return (unsigned)(key(j) >> 32); };
-    const auto low = [&](int j) { if constexpr (KEYS > 0) return lows[j]; else return (unsigned)key(j); };
-    const auto there = [&](int j) { return p0 + j * 32 + lane < p1; };
-    int turn = 0, at_least = n;
-    const auto count = [&](auto in) {
+    unsigned border = 0;
+    for (int bit = 31; bit >= 0 && at_least != want; --bit) {
+        const unsigned to = border | 1u << bit;
         int c = 0;
 #pragma unroll
-        for (int j = 0; j < rounds; ++j) c += in(j);
-        return count_all<WARPS>(c, sums, turn);
-    };
-    // the largest border with at least `want` at or above it (0: none but that), and how many are
-    unsigned border = 0, lower = 0;
-    for (int bit = 31; bit >= 0 && at_least != keep; --bit) {
-        const unsigned to = border | 1u << bit;
-        const int c = count([&](int j) { return high(j) >= to; });
-        if (c >= keep) { border = to; at_least = c; }
+        for (int j = 0; j < rounds; ++j) c += in(j, to);
+        c = count_all<WARPS>(c, sums, turn);
+        if (c >= want) { border = to; at_least = c; }
     }
-    int ties = INT_MAX;   // how many keys that are exactly the border's are taken: all, unless there are more than fit
-    if (at_least != keep) {
-        const int above = count([&](int j) { return high(j) > border; }), want = keep - above;
-        int same = at_least - above;
-        for (int bit = 31; bit >= 0 && same != want; --bit) {
-            const unsigned to = lower | 1u << bit;
-            const int c = count([&](int j) { return high(j) == border && low(j) >= to; });   // (keys that are not there are 0, which is below `to`)
-            if (c >= want) { lower = to; same = c; }
-        }
-        if (same != want) ties = want - count([&](int j) { return high(j) == border && low(j) > lower; });
-    }
-    const auto over = [&](int j) { return high(j) > border || (high(j) == border && low(j) > lower); };
-    const auto tie = [&](int j) { return there(j) && high(j) == border && low(j) == lower; };
-    // in order of pages; with several warps each first counts what the ones before it take
+    return border;
+}
+// Enters those pages p0 + 32 j + lane of each warp in `list` that are over the border, and as many of those at it as there is room for, the lower ones
+// first: `ties`, INT_MAX for all.
+template <int WARPS, typename Over, typename Tie>
+__device__ __forceinline__ void enter(Over over, Tie tie, int rounds, int p0, int p1, int ties, int *list, int (&sums)[2][WARPS])
+{
+    const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
     int to = 0, tied = 0;
-    if (WARPS > 1) {
+    if (WARPS > 1) {   // each warp first counts what the ones before it enter
         int mine = 0, mine_tied = 0;
 #pragma unroll
         for (int j = 0; j < rounds; ++j) { mine += over(j); mine_tied += tie(j); }
@@ -776,22 +764,167 @@ __device__ __forceinline__ void select_best(const unsigned long long *keys, int 
         tied += __popc(equal);
     }
 }
+// By keys of 64 bits in memory: first by their upper halves, then, among those that have that of the border, by their lower ones.
+template <int WARPS> __device__ __noinline__ void select_exactly(const unsigned long long *keys, int n, int keep, int p0, int p1, int each, int *list, int (&sums)[2][WARPS])
+{
+    const int lane = threadIdx.x & 31, rounds = each / 32;
+    const auto key = [&](int j) { const int p = p0 + j * 32 + lane; return p < p1 ? keys[p] : 0; };
+    const auto high = [&](int j) { return (unsigned)(key(j) >> 32); };
+    const auto low = [&](int j) { return (unsigned)key(j); };
+    int turn = 0, at_least = n, ties = INT_MAX;
+    unsigned lower = 0;
+    const unsigned border = border_of<WARPS>([&](int j, unsigned to) { return high(j) >= to; }, rounds, keep, at_least, sums, turn);
+    const auto count = [&](auto in) {
+        int c = 0;
+        for (int j = 0; j < rounds; ++j) c += in(j);
+        return count_all<WARPS>(c, sums, turn);
+    };
+    if (at_least != keep) {
+        const int above = count([&](int j) { return high(j) > border; }), want = keep - above;
+        int same = at_least - above;
+        // (keys that are not there are 0, which is below any `to`)
+        lower = border_of<WARPS>([&](int j, unsigned to) { return high(j) == border && low(j) >= to; }, rounds, want, same, sums, turn);
+        if (same != want) ties = want - count([&](int j) { return high(j) == border && low(j) > lower; });
+    }
+    const auto over = [&](int j) { return high(j) > border || (high(j) == border && low(j) > lower); };
+    const auto tie = [&](int j) { return p0 + j * 32 + lane < p1 && high(j) == border && low(j) == lower; };
+    enter<WARPS>(over, tie, rounds, p0, p1, ties, list, sums);
+}
+
+__device__ __forceinline__ unsigned ordered(float x)
+{
+    const unsigned u = __float_as_uint(x + 0.f);
+    return u >> 31 ? ~u : u | 1u << 31;
+}
+__device__ __forceinline__ float from_ordered(unsigned u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
+
+// The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS pages a lane in registers (0: any number, read again each time).
+template <typename T, int WARPS, int KEYS>
+__device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g, int n, float2 *scores, int *list, int (&sums)[2][WARPS], unsigned (&ends)[3][WARPS])
+{
+    const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5, keep = a.keep;
+    const int each = ((n + WARPS - 1) / WARPS + 31) & ~31, p0 = warp * each, p1 = min(n, p0 + each), rounds = KEYS ? KEYS : each / 32;   // this warp's pages
+    const auto always = [&](int p) { return p < a.first || p >= n - a.last; };
+    unsigned off = 0;   // the largest error's bits; those of a NaN or an infinity where a score or an error is one
+    const auto load = [&](int j) { return scores[min(p0 + j * 32 + lane, n - 1)]; };
+    const auto key = [&](int j, float2 s) {
+        const int p = p0 + j * 32 + lane;
+        const bool scored = p < p1 && !always(p);
+        off = max(off, !scored ? 0u : s.x < CUDART_INF_F && (s.x > -CUDART_INF_F || s.y == 0.f) ? __float_as_uint(s.y) : 0x7f800000u);
+        return scored ? ordered(s.x) : p < p1 ? ~0u : 0u;
+    };
+    unsigned held[KEYS ? KEYS : 1];
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int j0 = 0; j0 < KEYS; j0 += 8) {   // (eight loads on their way)
+            if (p0 + j0 * 32 >= p1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) held[j0 + j] = 0;
+                continue;
+            }
+            float2 s[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = load(j0 + j);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) held[j0 + j] = key(j0 + j, s[j]);
+        }
+    } else {
+        for (int j = 0; j < rounds; ++j) key(j, load(j));
+    }
+    const auto at = [&](int j) { if constexpr (KEYS > 0) return held[j]; else return key(j, load(j)); };
+    int turn = 0, at_least = n;
+    const unsigned border = border_of<WARPS>([&](int j, unsigned to) { return at(j) >= to; }, rounds, keep, at_least, sums, turn);
+    // the lowest score that is in, the highest that is not, the error
+    unsigned lowest = ~0u, highest = 0;
+#pragma unroll
+    for (int j = 0; j < rounds; ++j) {
+        const unsigned x = at(j);
+        if (x >= border && x) lowest = min(lowest, x);
+        if (x < border) highest = max(highest, x);
+    }
+    lowest = __reduce_min_sync(~0u, lowest);
+    highest = __reduce_max_sync(~0u, highest);
+    off = __reduce_max_sync(~0u, off);
+    if (WARPS > 1) {
+        if (lane == 0) { ends[0][warp] = lowest; ends[1][warp] = highest; ends[2][warp] = off; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) { lowest = min(lowest, ends[0][w]); highest = max(highest, ends[1][w]); off = max(off, ends[2][w]); }
+    }
+    const float reach = 2.1f * __uint_as_float(off), in = from_ordered(lowest), out = from_ordered(highest);
+    // (what is always taken scores more than any number)
+    if (at_least == keep && off < 0x7f800000u && (lowest == ~0u || in - out > reach)) {
+        enter<WARPS>([&](int j) { return at(j) >= border; }, [](int) { return false; }, rounds, p0, p1, INT_MAX, list, sums);
+        return;
+    }
+    // Pages within reach of the border get scores of 64 bits, four at a time; those above are in, those below are out (keys that no score has).
+    const bool all = off >= 0x7f800000u;
+    const float from = in - reach, to = in + reach;
+    unsigned long long *keys = reinterpret_cast<unsigned long long *>(scores);
+    const int group = a.heads / a.kv_heads;
+    const int *table = a.t.entries + row_of(a.tok, i) * a.t.ld;
+    double q[8];   // elements lane, lane + 32 ...
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        q[e] = 0;
+        if (lane + 32 * e < a.d)
+            for (int h = 0; h < group; ++h) q[e] += attn::widen(a.q[i * a.q_ld + (g * group + h) * a.q_sh + lane + 32 * e]);
+    }
+    for (int j = 0; j < each / 32; ++j) {
+        const int p = p0 + j * 32 + lane;
+        unsigned long long key = 0;
+        bool again = false;
+        if (p < p1) {
+            const float2 s = scores[p];
+            again = !always(p) && (all || (s.x >= from && s.x <= to));
+            key = always(p) || (!all && s.x > to) ? ~0ull : 0;
+            if (again && !all && s.y == 0.f) { key = ordered((double)s.x); again = false; }   // (exact, or no page)
+        }
+        for (unsigned left = __ballot_sync(~0u, again); left;) {
+            int which[4];
+            double x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                which[k] = left ? __ffs(left) - 1 : -1;
+                left &= left - 1;
+                x[k] = 0;
+                const int held = which[k] < 0 ? -1 : table[p0 + j * 32 + which[k]];
+                if ((unsigned)held >= (unsigned)a.means.pages) { x[k] = lane ? 0 : -CUDART_INF; continue; }
+                const T *mean = a.means.row(held, g, 0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (lane + 32 * e < a.d) x[k] += q[e] * attn::widen(mean[lane + 32 * e]);
+            }
+#pragma unroll
+            for (int w = 16; w; w >>= 1)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] += __shfl_xor_sync(~0u, x[k], w);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (which[k] == lane) key = ordered(x[k]);
+        }
+        if (p < p1) keys[p] = key;
+    }
+    __syncwarp();   // (a warp's keys are read by itself alone)
+    select_exactly<WARPS>(keys, n, keep, p0, p1, each, list, sums);
+}
 
 template <typename T, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32) paged_select_kernel(const SelectArgs<T> a)
 {
     __shared__ int sums[2][WARPS];
+    __shared__ unsigned ends[3][WARPS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int n = pages_seen(a, blockIdx.x / a.kv_heads);
+    const int i = blockIdx.x / a.kv_heads, g = blockIdx.x - i * a.kv_heads, n = pages_seen(a, i);
     int *list = a.lists + (long long)blockIdx.x * a.keep;
     for (int p = threadIdx.x; p < a.keep; p += WARPS * 32)
         if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
     if (n <= a.keep) return;
-    const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.t.width;
-    if (n <= 256 * WARPS) select_best<WARPS, 8>(keys, n, a.keep, a.first, a.last, list, sums);
-    else if (n <= 1024 * WARPS) select_best<WARPS, 32>(keys, n, a.keep, a.first, a.last, list, sums);
-    else if (n <= 2048 * WARPS) select_best<WARPS, 64>(keys, n, a.keep, a.first, a.last, list, sums);
-    else if (WARPS > 1) select_best<WARPS, 0>(keys, n, a.keep, a.first, a.last, list, sums);
+    float2 *scores = a.scores + (long long)blockIdx.x * a.t.width;
+    if (n <= 256 * WARPS) select_best<T, WARPS, 8>(a, i, g, n, scores, list, sums, ends);
+    else if (n <= 1024 * WARPS) select_best<T, WARPS, 32>(a, i, g, n, scores, list, sums, ends);
+    else if (n <= 2048 * WARPS) select_best<T, WARPS, 64>(a, i, g, n, scores, list, sums, ends);
+    else if (WARPS > 1) select_best<T, WARPS, 0>(a, i, g, n, scores, list, sums, ends);
 }
 }  // namespace paged
 }  // namespace b2sp

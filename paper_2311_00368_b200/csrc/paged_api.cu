@@ -137,7 +137,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     if (rc != B2SP_OK) return rc;
     if (M && (!Q || !seen || !lists)) return B2SP_ERR_INVALID_ARG;
     if (d > 256) return B2SP_ERR_UNSUPPORTED;
-    const long long blocks = (long long)M * kv_heads * (((long long)t->width + kScorePages - 1) / kScorePages), ctas = (long long)M * kv_heads;
+    const long long blocks = (long long)M * kv_heads * (((long long)t->width + 7) / 8), ctas = (long long)M * kv_heads;   // blocks: of eight pages at least
     if (ctas > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
@@ -147,7 +147,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     a.q = Q; a.q_ld = ldq; a.q_sh = shq;
     a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.page = means->page; a.keep = keep; a.first = first; a.last = last;
     a.means = pages<T>(means);
-    a.keys = static_cast<unsigned long long *>(workspace);
+    a.scores = static_cast<float2 *>(workspace);
     a.lists = lists;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     a.q_wide = fits<T>(Q, ldq, shq, 16);

@@ -254,6 +254,34 @@ def test_select_ties_infinities_and_nan():
     c.check_select(7, 0, 0)
 
 
+@pytest.mark.parametrize("n", [40, 600, 2300])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_select_between_close_scores(n, dtype):
+    """Scores that sums in 32 bits cannot tell apart: means that differ in the last place of one element, in elements that weigh next to nothing,
+    and not at all; some that are 0; scores that underflow or overflow in 32 bits."""
+    c = Cache(3, [n * 4, n * 4 - 5], 4, 2, 64, 4, dtype)
+    gen = torch.Generator().manual_seed(n)
+    base = torch.randn((1, 2, 64), generator=gen).to(dtype).cuda()
+    order = torch.randperm(n, generator=gen)
+    for i in range(2):
+        at = c.tables[i].long()
+        c.means[at] = base
+        step = torch.finfo(dtype).eps * base[0, :, 5].float().abs() * 2.0 ** -14     # far below the last place of a score
+        c.means[at[order], :, 63] = ((torch.arange(n).cuda()[:, None] // 2 - n // 4) * step).to(dtype)
+    for keep in (3, 17, n // 2, n - 1):
+        c.check_select(keep)
+    c.means[c.tables[0, ::3].long()] = 0
+    c.means[c.tables[1, 1::2].long(), 1] = -0.0
+    for keep in (5, n // 3, n - 2):
+        c.check_select(keep)
+    keep_q = c.q.clone()
+    for f in (2.0 ** -100, 2.0 ** 100):
+        c.q, means = (keep_q.float() * f).to(dtype), c.means.clone()
+        c.means.copy_((means.float() * f).to(dtype))
+        c.check_select(n // 2)
+        c.means.copy_(means)
+
+
 def test_select_rows_and_layout():
     c = Cache(2, [300, 299, 298, 0, 120, 500], 4, 2, 64, 16, rows=[1, 1, 1, 0, -1, 2])
     c.check_select(6)
