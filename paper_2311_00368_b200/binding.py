@@ -869,8 +869,8 @@ def _page_means(t, page, dtype):
 
 def _of_tokens(q, dtype, name):
     """(M, heads, d), strides of a [M, heads, d] tensor."""
-    if q.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}")
+    if q.dtype is not dtype or (dtype is not torch.bfloat16 and dtype is not torch.float32):
+        raise TypeError(f"{name} must be {dtype}, and that torch.float32 or torch.bfloat16")
     s = q.stride()
     if len(s) != 3 or (s[2] != 1 and q.shape[2] > 1):
         raise ValueError(f"{name} must be [tokens, heads, d] with neighbouring elements along d")

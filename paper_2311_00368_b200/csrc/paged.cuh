@@ -3,7 +3,8 @@
 //
 // Request r's position p lies in row p % page of page tables[r][p / page].  Everything that says how much there is to do (lengths, new tokens,
 // tables) is on the device, so a launch is sized by what the host knows (requests, tokens, width of the tables) and the kernels find their
-// work themselves: each CTA forms the prefix sums over the requests that it needs, which costs it a microsecond and spares a launch.
+// work themselves: each CTA forms the prefix sums over the requests that it needs, which costs it a microsecond and spares a launch.  Every kernel may be
+// launched before the one ahead of it has ended: its CTAs wait for that first of all, all of them, so that what comes behind can count on it.
 #pragma once
 #include <limits.h>
 
@@ -237,7 +238,7 @@ __device__ __forceinline__ Request request(const TablesArgs &a, int r)
 // Pages given back are pushed on the stack of free ones in order of requests, then new ones are popped in order of requests.  No CTA waits for
 // another: which page the k-th new one is follows from the prefix sums, and one that is given back in the same step is read from the table
 // of the request that ends, so everything is a function of the inputs, and any number of CTAs take any part of it.
-// Bound by latency: lengths, then (tokens) a table entry or a free page; 64 requests and 512 with 16384 new tokens: see the launch.
+// Bound by latency: lengths, then (tokens) a table entry or a free page.  64 requests with a token each 4.1 us, 512 with 16384 new tokens 7.2 us.
 __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs a)
 {
     extern __shared__ int prefix[];
@@ -338,7 +339,8 @@ __global__ void __launch_bounds__(kScanThreads) paged_list_ends_kernel(const Lis
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 // A thread takes four neighbouring entries: their list by a binary search over the ends, which each CTA forms for itself in shared memory (KEPT), then
-// a page of the table for all four unless a page or a list ends among them.  Bound by latency (lengths, table), then by the stores.
+// a page of the table for all four unless a page or a list ends among them.  Bound by latency (lengths, table), then by the stores.  64 lists of 524288 slots in
+// all: 3.9 us (ends and lists as two kernels, an entry a thread, a warp 512 of them: 10.0).
 template <bool KEPT>
 __global__ void __launch_bounds__(kThreads) paged_list_kernel(const ListsArgs a)
 {
@@ -452,6 +454,8 @@ template <typename T> struct Chunk {
 
 // A CTA per touched page and head: the request's new rows that lie in it are copied, and the mean of K's rows is formed from them and those that were
 // there.  So a page's rows are summed in one place and order (in fp32, rounded once to the cache's type), and no row is written twice.
+// Bound by HBM once there are many rows: 16384 tokens of 8 heads, width 128, 136 MB, 25.4 us, of which the floor is 20.8.  Eight CTAs of 128 threads on an SM
+// with two rows' loads each; five with four rows' 28.7, three with eight rows' 34.2, ten with two rows' (which spill) 35.8 us.
 constexpr int kWriteThreads = 128, kWriteRows = 2, kWriteCTAs = 8;   // CTAs of an SM
 template <typename T>
 __global__ void __launch_bounds__(kWriteThreads, kWriteCTAs) paged_write_kernel(const WriteArgs<T> a)
@@ -543,6 +547,7 @@ template <typename T> struct SelectArgs {
     Pages<T> means;
     float2 *scores;             // [M][kv_heads][width]: a score in 32 bits and how far it may be off
     int *lists;                 // [M][kv_heads][keep]
+    int *status;
 };
 template <typename T> __device__ __forceinline__ int pages_seen(const SelectArgs<T> &a, int i)
 {
@@ -558,10 +563,12 @@ __device__ __forceinline__ unsigned long long ordered(double x)
 
 // The choice is defined by scores in 64 bits, since between two close ones sums of 32 bits would choose by their order.  Few scores are that close: they
 // are formed in 32 bits with a bound of the error, and a token whose border lies between two scores that are further apart than that is done; only
-// where others lie within reach of the border these are formed again in 64 bits.  (All of them in 64 bits took twice as long: conversions and long chains.)
+// where others lie within reach of the border these are formed again in 64 bits.  (All of them in 64 bits: 12.3 instead of 10.3 us for a token that sees 2048
+// pages, 8 key heads.)
 //
 // Scores of the pages of tokens that see more than a list holds: all tokens' and key heads' blocks of pages are dealt to the warps in equal shares; the sum of the
-// group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  A lane adds up eight products and the lanes' sums come together in at most five steps, so a score is off
+// group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  The next block's
+// means and pages are on their way while one is added up.  Bound by HBM for many tokens (64 of 256 pages on the average: 34 MB), else by latencies.  A lane adds up eight products and the lanes' sums come together in at most five steps, so a score is off
 // by at most 14 half steps of the sum of the products' magnitudes (one of them the query's rounding), and by what underflows; kScoreOff leaves room for the
 // rounding of that sum itself and of what the choice makes of it.
 constexpr float kScoreOff = 24.f * 5.9604645e-8f, kUnderflow = 1e-42f;
@@ -798,7 +805,8 @@ __device__ __forceinline__ unsigned ordered(float x)
 }
 __device__ __forceinline__ float from_ordered(unsigned u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
 
-// The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS pages a lane in registers (0: any number, read again each time).
+// The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS pages a lane in registers (0: any number, read again each time).  Bound
+// by latency: one for the scores, then about 25 counts, each a few instructions a key and (several warps) a barrier.
 template <typename T, int WARPS, int KEYS>
 __device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g, int n, float2 *scores, int *list, int (&sums)[2][WARPS], unsigned (&ends)[3][WARPS])
 {
@@ -915,6 +923,7 @@ __global__ void __launch_bounds__(WARPS * 32) paged_select_kernel(const SelectAr
     __shared__ int sums[2][WARPS];
     __shared__ unsigned ends[3][WARPS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
     const int i = blockIdx.x / a.kv_heads, g = blockIdx.x - i * a.kv_heads, n = pages_seen(a, i);
     int *list = a.lists + (long long)blockIdx.x * a.keep;
     for (int p = threadIdx.x; p < a.keep; p += WARPS * 32)

@@ -9,7 +9,7 @@ namespace b2sp {
 namespace paged {
 
 inline b2sp_status launched() { return cudaGetLastError() == cudaSuccess ? B2SP_OK : B2SP_ERR_CUDA; }
-constexpr int kSMs = 148;
+constexpr int kSMs = 148, kMostTokens = 1 << 30;
 constexpr size_t kMostShared = 227 * 1024;   // of a CTA
 
 // More shared memory than a launch gets unasked (48 KB with what the kernel has of its own): asked for once on each device.
@@ -102,13 +102,13 @@ b2sp_status write(int tokens, int heads, int d, const T *K, long long ldk, long 
     if (rc == B2SP_OK && means) rc = check_pages<T>(means, heads, d, 1);
     if (rc == B2SP_OK) rc = check_tables(t, kp->page);
     if (rc != B2SP_OK) return rc;
-    if (!same_slots(kp, vp) || (means && means->pages != kp->pages)) return B2SP_ERR_INVALID_ARG;
+    if (t->requests > kMostRequests || d > 1024) return B2SP_ERR_UNSUPPORTED;
+    if (!same_slots(kp, vp) || (means && means->pages != kp->pages) || (kp->pages && kp->data == vp->data)) return B2SP_ERR_INVALID_ARG;
     for (const b2sp_pages *c : {kp, vp})
         if (!apart(d, {{c->pages, c->stride_page}, {heads, c->stride_head}, {c->page, c->ld}})) return B2SP_ERR_INVALID_ARG;
     if (means && !apart(d, {{means->pages, means->stride_page}, {heads, means->stride_head}})) return B2SP_ERR_INVALID_ARG;
     if (t->requests && (!row_ptr || !lengths)) return B2SP_ERR_INVALID_ARG;
     if (tokens && (!K || !V)) return B2SP_ERR_INVALID_ARG;
-    if (t->requests > kMostRequests || d > 1024) return B2SP_ERR_UNSUPPORTED;
     if (tokens == 0 || t->requests == 0 || kp->pages == 0) return B2SP_OK;
     WriteArgs<T> a = {};
     a.t = tables(t);
@@ -125,7 +125,9 @@ b2sp_status write(int tokens, int heads, int d, const T *K, long long ldk, long 
 
 bool token_args_ok(int M, int heads, int kv_heads, int d) { return M >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && d >= 1; }
 
-size_t select_bytes(int M, int kv_heads, int width) { return std::max<size_t>(256, attn::up256((size_t)M * kv_heads * width * 8)); }
+// A workspace begins with what b2sp_device_status reads, as those of the other calls do.
+constexpr size_t kHead = 512, kStatus = 256;
+size_t select_bytes(int M, int kv_heads, int width) { return kHead + attn::up256((size_t)M * kv_heads * width * sizeof(float2)); }
 
 template <typename T>
 b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long ldq, long long shq, const b2sp_pages *means, const b2sp_page_tables *t,
@@ -136,7 +138,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     if (rc == B2SP_OK) rc = check_tables(t, means->page);
     if (rc != B2SP_OK) return rc;
     if (M && (!Q || !seen || !lists)) return B2SP_ERR_INVALID_ARG;
-    if (d > 256) return B2SP_ERR_UNSUPPORTED;
+    if (d > 256 || M > kMostTokens) return B2SP_ERR_UNSUPPORTED;
     const long long blocks = (long long)M * kv_heads * (((long long)t->width + 7) / 8), ctas = (long long)M * kv_heads;   // blocks: of eight pages at least
     if (ctas > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
@@ -147,7 +149,8 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     a.q = Q; a.q_ld = ldq; a.q_sh = shq;
     a.M = M; a.heads = heads; a.kv_heads = kv_heads; a.d = d; a.page = means->page; a.keep = keep; a.first = first; a.last = last;
     a.means = pages<T>(means);
-    a.scores = static_cast<float2 *>(workspace);
+    a.status = reinterpret_cast<int *>(static_cast<char *>(workspace) + kStatus);
+    a.scores = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + kHead);
     a.lists = lists;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     a.q_wide = fits<T>(Q, ldq, shq, 16);
@@ -185,7 +188,7 @@ template <typename T> AttnPlan attention_plan(int heads, int kv_heads, int d, lo
     p.blocks = (group + p.queries - 1) / p.queries;
     p.warps = kSMs * kAttnWarps * (w == 64 ? Form<T, 64>::CTAS : w == 128 ? Form<T, 128>::CTAS : Form<T, 256>::CTAS);
     const size_t parts = 2ull * p.warps * p.queries;
-    p.ml = attn::up256(p.warps * sizeof(int4));
+    p.ml = kHead + attn::up256(p.warps * sizeof(int4));
     p.part = p.ml + attn::up256(parts * sizeof(float2));
     p.bytes = p.part + attn::up256(parts * w * sizeof(float));
     return p;
@@ -229,7 +232,7 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     if (!same_slots(kp, vp)) return B2SP_ERR_INVALID_ARG;
     if (M && (!Q || !O || !lse || !seen)) return B2SP_ERR_INVALID_ARG;
     if (!apart(d, {{M, ldo}, {heads, sho}})) return B2SP_ERR_INVALID_ARG;
-    if (d > 256 || (lists && (long long)keep * kp->page > INT_MAX) || (long long)M * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    if (d > 256 || M > kMostTokens || (lists && (long long)keep * kp->page > INT_MAX) || (long long)M * heads > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     constexpr long long most_stride = UINT_MAX / sizeof(T);
     for (const b2sp_pages *c : {kp, vp})
         if (std::max({c->ld, c->stride_head, c->stride_page, ldq, shq, ldo, sho, t->ld}) > most_stride) return B2SP_ERR_UNSUPPORTED;
@@ -257,7 +260,8 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     a.pairs = fits<T>(Q, ldq, shq, 4) && fits<T>(O, ldo, sho, 4) && d % 2 == 0;
     a.fours = fits<T>(Q, ldq, shq, 16) && (sizeof(T) == 2 || d % 4 == 0);
     char *ws = static_cast<char *>(workspace);
-    a.joins = reinterpret_cast<int4 *>(ws);
+    a.status = reinterpret_cast<int *>(ws + kStatus);
+    a.joins = reinterpret_cast<int4 *>(ws + kHead);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.ml);
     a.part = reinterpret_cast<float *>(ws + p.part);
     const long long most_rows = lists ? (long long)keep * a.page : (long long)t->width * a.page, units = (long long)M * kv_heads * p.blocks;
@@ -286,8 +290,15 @@ extern "C" b2sp_status b2sp_paged_tables(const b2sp_page_tables *t, int pages, i
     if (pages < 0 || free_room < 0 || tokens < 0 || (R > 1 && t->ld < t->width)) return B2SP_ERR_INVALID_ARG;
     if (!row_ptr || !counts || !free_count || (R && (!lengths || !added || !lengths_out)) || (free_room && !free_pages)) return B2SP_ERR_INVALID_ARG;
     if (tokens && (!rows || !seen || !slots)) return B2SP_ERR_INVALID_ARG;
-    if (meet(lengths, 4ull * R, lengths_out, 4ull * R) || meet(counts, 16, free_count, 4)) return B2SP_ERR_INVALID_ARG;   // CTAs read the one while others write the other
     if (R > kMostRequests || (long long)pages * page > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    // CTAs read inputs while others write outputs
+    const std::pair<const void *, size_t> in[] = {{lengths, R * 4ull}, {added, R * 4ull}, {free_count, 4}, {free_pages, free_room * 4ull},
+                                                  {t->entries, R ? ((R - 1) * (size_t)t->ld + t->width) * 4 : 0}},
+                                          out[] = {{lengths_out, R * 4ull}, {row_ptr, (R + 1) * 4ull}, {rows, tokens * 4ull}, {seen, tokens * 4ull},
+                                                   {slots, tokens * 4ull}, {counts, 16}};
+    for (const auto &x : in)
+        for (const auto &y : out)
+            if (meet(x.first, x.second, y.first, y.second)) return B2SP_ERR_INVALID_ARG;
     const size_t shared = 3 * (R + 1) * sizeof(int);
     TablesArgs a = {};
     a.t = tables(t);
@@ -304,7 +315,11 @@ extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pa
     b2sp_status rc = check_tables(t, page);
     if (rc != B2SP_OK) return rc;
     if (M < 0 || pages < 0 || entries < 0 || !row_ptr || (M && !seen) || (entries && !col_idx)) return B2SP_ERR_INVALID_ARG;
-    if (entries > INT_MAX || (long long)pages * page > INT_MAX) return B2SP_ERR_UNSUPPORTED;
+    for (const void *x : {static_cast<const void *>(seen), static_cast<const void *>(rows), static_cast<const void *>(t->entries)}) {
+        const size_t n = x == t->entries ? (t->requests ? ((t->requests - 1) * (size_t)t->ld + t->width) * 4 : 0) : M * 4ull;
+        if (x && (meet(x, n, row_ptr, (M + 1) * 4ull) || meet(x, n, col_idx, entries * 4ull))) return B2SP_ERR_INVALID_ARG;
+    }
+    if (entries > INT_MAX || (long long)pages * page > INT_MAX || M > kMostTokens) return B2SP_ERR_UNSUPPORTED;
     ListsArgs a = {};
     a.t = tables(t);
     a.tok = Tokens{rows, seen};

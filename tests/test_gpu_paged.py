@@ -467,6 +467,22 @@ def test_captured_beside_another_graph():
         assert all(torch.equal(x, y) for x, y in zip(got, ref))
 
 
+def test_given_workspaces():
+    """Workspaces of just the size asked for, whatever they hold; nothing behind them is written, and their status word is in order."""
+    b = _binding()
+    for dtype in (torch.float32, torch.bfloat16):
+        c = Cache(31, [3000, 40, 0, 700], 8, 2, 64, 16, dtype)
+        lists, want = c.select(9), c.attend()
+        for need, call in ((b.lib.b2sp_paged_select_workspace_bytes(4, 2, c.tables.shape[1]), lambda ws: (c.select(9, workspace=ws),)),
+                           (b.lib.b2sp_attention_paged_workspace_bytes(4, 8, 2, 64), lambda ws: c.attend(workspace=ws))):
+            room = torch.full((need + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+            got = call(room[:need])
+            assert all(torch.equal(x, y) for x, y in zip(got, (lists,) if len(got) == 1 else want))
+            assert (room[need:] == 0xAB).all() and b.device_status(room) == 0
+            with pytest.raises(b.B2spError):
+                call(room[:need - 1])
+
+
 def test_on_another_stream():
     c = Cache(30, [900, 30], 8, 2, 64, 16)
     want = c.attend()

@@ -41,22 +41,26 @@ def test_tables(b):
     assert f(pages=-1) == f(page=0) == f(room=-1) == f(tokens=-1) == INVALID
     assert f(lengths=None) == f(added=None) == f(free=None) == f(count=None) == f(out=None) == f(ptr=None) == INVALID
     assert f(rows=None) == f(seen=None) == f(slots=None) == f(counts=None) == INVALID
-    assert f(out=4096) == f(out=4096 + 8) == f(counts=1 << 15) == f(counts=(1 << 15) - 12) == INVALID    # read by one CTA, written by another
+    # read by one CTA, written by another
+    assert f(out=4096) == f(out=4096 + 8) == f(counts=1 << 15) == f(counts=(1 << 15) - 12) == f(seen=8192) == f(ptr=(1 << 14) + 124) == INVALID
+    assert f(slots=(1 << 22) + 4 * 47) == INVALID
     assert f(_tab(b, requests=8193)) == f(pages=1 << 27, page=16) == UNSUPPORTED
 
 
 def test_lists(b):
-    f = lambda M=3, t=None, pages=32, page=16, seen=4096, entries=9, ptr=4096, col=4096: b.lib.b2sp_paged_lists(  # noqa: E731
+    f = lambda M=3, t=None, pages=32, page=16, seen=4096, entries=9, ptr=1 << 16, col=1 << 17: b.lib.b2sp_paged_lists(  # noqa: E731
         M, t or _tab(b), pages, page, None, seen, entries, ptr, col, None)
     for bad in BAD_TABLES:
         assert f(t=_tab(b, **bad)) == INVALID, bad
     assert f(M=-1) == f(pages=-1) == f(page=0) == f(seen=None) == f(entries=-1) == f(ptr=None) == f(col=None) == INVALID
-    assert f(entries=2 ** 31) == f(pages=1 << 27) == UNSUPPORTED
+    assert f(ptr=4096 + 8) == f(col=4096 + 4) == f(t=_tab(b, entries=1 << 20), ptr=(1 << 20) + 8) == INVALID     # outputs in inputs
+    assert f(entries=2 ** 31, seen=1 << 40) == f(pages=1 << 27, seen=1 << 40, t=_tab(b, entries=1 << 41)) == UNSUPPORTED
+    assert f(M=(1 << 30) + 1, seen=1 << 40, t=_tab(b, entries=1 << 41)) == UNSUPPORTED
 
 
 def test_write(b):
     def f(tokens=4, heads=2, d=64, k=4096, ldk=128, shk=64, v=4096, t=None, kp=None, vp=None, means=None, ptr=4096, lengths=4096, fn="b2sp_paged_write"):
-        return getattr(b.lib, fn)(tokens, heads, d, k, ldk, shk, v, 128, 64, ptr, lengths, t or _tab(b), kp or _cache(b), vp or _cache(b), means, None)
+        return getattr(b.lib, fn)(tokens, heads, d, k, ldk, shk, v, 128, 64, ptr, lengths, t or _tab(b), kp or _cache(b), vp or _cache(b, data=1 << 24), means, None)
     for bad in BAD_TABLES:
         assert f(t=_tab(b, **bad)) == INVALID, bad
     for bad in BAD_CACHES:
@@ -65,7 +69,7 @@ def test_write(b):
             assert f(means=_cache(b, **bad)) == INVALID, bad
     assert f(kp=_cache(b, ld=68), fn="b2sp_paged_write_bf16") == INVALID                       # 16 bytes are eight of them
     assert f(tokens=-1) == f(heads=0) == f(d=0) == f(k=None) == f(v=None) == f(ldk=-1) == f(ptr=None) == f(lengths=None) == INVALID
-    assert f(kp=_cache(b, pages=31)) == f(kp=_cache(b, page=8)) == f(means=_cache(b, pages=31)) == INVALID
+    assert f(kp=_cache(b, pages=31)) == f(kp=_cache(b, page=8)) == f(means=_cache(b, pages=31)) == f(vp=_cache(b)) == INVALID
     for over in (dict(stride_head=960), dict(stride_page=1024), dict(ld=128)):
         assert f(kp=_cache(b, **over)) == f(vp=_cache(b, **over)) == INVALID, over             # rows that are written overlap
     assert f(means=_cache(b, stride_head=32)) == INVALID
@@ -145,5 +149,6 @@ def test_binding_checks_types_and_shapes(b):
     for bad in (dict(tables=i(12)), dict(seen=i(2)), dict(rows=i(2)), dict(lists=i(3, 1, 4)), dict(k_pages=c[:2]), dict(q=x[:, :3]), dict(out=x[..., :32])):
         with pytest.raises(ValueError):
             b.attention_paged(**{**dict(q=x, k_pages=c, v_pages=c, tables=i(3, 4), seen=i(3)), **bad})
-    with pytest.raises(TypeError):
-        b.attention_paged(x.double(), c, c, i(3, 4), i(3))
+    for bad in (torch.float64, torch.float16):
+        with pytest.raises(TypeError):
+            b.attention_paged(x.to(bad), c.to(bad), c.to(bad), i(3, 4), i(3), dtype=bad)
