@@ -568,10 +568,11 @@ __device__ __forceinline__ unsigned long long ordered(double x)
 //
 // Scores of the pages of tokens that see more than a list holds: all tokens' and key heads' blocks of pages are dealt to the warps in equal shares; the sum of the
 // group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  The next block's
-// means and pages are on their way while one is added up.  Bound by HBM for many tokens (64 of 256 pages on the average: 34 MB), else by latencies.  A lane adds up eight products and the lanes' sums come together in at most five steps, so a score is off
-// by at most 14 half steps of the sum of the products' magnitudes (one of them the query's rounding), and by what underflows; kScoreOff leaves room for the
-// rounding of that sum itself and of what the choice makes of it.
-constexpr float kScoreOff = 24.f * 5.9604645e-8f, kUnderflow = 1e-42f;
+// means are on their way while this one's are added up.  Bound by HBM for many tokens (64 of 256 pages on the average: 34 MB), else by latencies.  A lane adds up eight products (in pairs) and the lanes' sums come together in at most five steps, so a score is off
+// by at most 14 half steps of the sum of the products' magnitudes (one of them the query's rounding), and by what underflows.  That sum is no more than the
+// product of the query's and the mean's lengths (Cauchy and Schwarz), which costs as many instructions as the score; kTiny is what squares lose that underflow.
+// kScoreOff leaves room for the roundings of the bound itself and of what the choice makes of it.
+constexpr float kScoreOff = 24.f * 5.9604645e-8f, kUnderflow = 1e-42f, kTiny = 1e-42f;
 constexpr int kScoreThreads = 128, kScoreCTAs = 4;   // CTAs of an SM
 template <typename T, int LANES, int HALVES>
 __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) paged_score_kernel(const SelectArgs<T> a)
@@ -589,27 +590,36 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int i = w.row, n = pages_seen(a, i), blocks = (n + BATCH - 1) / BATCH, g = (int)w.rest / blocks, b = (int)w.rest - g * blocks;
     const int e0 = lane % LANES * N;   // this lane's first element
-    float q[HALVES][N];
-    uint4 now[AT_ONCE][HALVES], next[AT_ONCE][HALVES];
+    const bool ragged = a.d % N != 0;
+    const unsigned head = (unsigned)(a.means.sh * sizeof(T)), per_page = (unsigned)(a.means.sp * sizeof(T));   // (below 2^32)
+    uint64_t q[HALVES][N / 2];
+    float norm = 0.f;   // of the query
+    uint4 c[AT_ONCE][HALVES], next[AT_ONCE][HALVES];
     const auto look_up = [&](int p) { return p < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p] : -1; };
     const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int held, int g) {   // means of a block whose pages the lanes hold
+        const char *base = reinterpret_cast<const char *>(a.means.data + e0) + (unsigned long long)g * head;
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-            const int p = __shfl_sync(~0u, held, j * STEP + lane / LANES);
-            const T *mean = a.means.row(p, g, 0) + e0;
+            const unsigned p = (unsigned)__shfl_sync(~0u, held, j * STEP + lane / LANES);
+            const char *mean = base + (unsigned long long)p * per_page;
 #pragma unroll
             for (int x = 0; x < HALVES; ++x) {
                 c[j][x] = make_uint4(0, 0, 0, 0);
-                if ((unsigned)p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(mean + x * 32 * N);
+                if (p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(mean + x * 32 * 16);
             }
         }
     };
+    const auto pair = [](const uint4 &u, int k) {   // elements 2 k and 2 k + 1 of sixteen bytes
+        const unsigned w[4] = {u.x, u.y, u.z, u.w};
+        if constexpr (sizeof(T) == 2) return attn::two(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+        else return attn::two(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
+    };
     int held = look_up(b * BATCH + lane % BATCH);
-    read(now, held, g);
+    read(c, held, g);
     bool fresh = true;
-    // Means are on their way a block ahead.
     for (int left = (int)(w.hi - w.lo);;) {
-        const int of_i = i, of_g = g, of_n = n, p0 = b * BATCH, mine_held = held;
+        const int of_n = n, p0 = b * BATCH, mine_held = held;
+        float2 *scores = a.scores + ((long long)i * a.kv_heads + g) * a.t.width + p0;
         if (fresh) {   // the sum of the queries, four heads' loads at once
             double total[HALVES][N] = {};
             const T *from = a.q + i * a.q_ld + (long long)g * group * a.q_sh;
@@ -632,13 +642,21 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                         for (int m = 0; m < N; ++m) total[x][m] += f[m];
                     }
             }
+            norm = 0.f;
 #pragma unroll
             for (int x = 0; x < HALVES; ++x)
 #pragma unroll
-                for (int k = 0; k < N; ++k) q[x][k] = (float)total[x][k];
+                for (int k = 0; k < N / 2; ++k) {
+                    const float y = (float)total[x][2 * k], z = (float)total[x][2 * k + 1];
+                    q[x][k] = attn::two(y, z);
+                    norm = fmaf(y, y, fmaf(z, z, norm));
+                }
+#pragma unroll
+            for (int x = 1; x < LANES; x <<= 1) norm += __shfl_xor_sync(~0u, norm, x);
+            norm = sqrtf(fmaf(norm, 1.0001f, kTiny));
             fresh = false;
         }
-        // the next block
+        // the next block's pages
         const bool more = --left > 0;
         if (more) {
             if (++b == blocks) {
@@ -653,61 +671,73 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                 }
             }
             held = look_up(b * BATCH + lane % BATCH);
+            read(next, held, g);
         }
-        float2 *scores = a.scores + ((long long)of_i * a.kv_heads + of_g) * a.t.width;
-        {
-            if (more) read(next, held, g);
-            float sum[AT_ONCE], size[AT_ONCE];
+        float sum[AT_ONCE], size[AT_ONCE];   // of the products, and of the mean's squares
+        bool nothing = false;
 #pragma unroll
-            for (int j = 0; j < AT_ONCE; ++j) {
-                sum[j] = size[j] = 0.f;
+        for (int j = 0; j < AT_ONCE; ++j) {
+            uint64_t s2 = 0, m2 = 0;
 #pragma unroll
-                for (int x = 0; x < HALVES; ++x) {
-                    float f[N] = {};
-                    Chunk<T>{now[j][x]}.add_to(f);
-                    // (0 stays 0 for a mean of zeros alone, whose score is exact)
-                    if ((now[j][x].x | now[j][x].y | now[j][x].z | now[j][x].w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) size[j] += kUnderflow;
-                    if (e0 + x * 32 * N + N > a.d) {   // what lies behind d may be anything
+            for (int x = 0; x < HALVES; ++x) {
+                if (ragged && e0 + x * 32 * N + N > a.d) {   // what lies behind d may be anything
+                    unsigned *u = &c[j][x].x;
 #pragma unroll
-                        for (int k = 0; k < N; ++k)
-                            if (e0 + x * 32 * N + k >= a.d) f[k] = 0.f;
-                    }
-#pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        sum[j] = fmaf(q[x][k], f[k], sum[j]);
-                        size[j] = fmaf(fabsf(q[x][k]), fabsf(f[k]), size[j]);
+                    for (int k = 0; k < 4; ++k) {
+                        const int left_of = a.d - (e0 + x * 32 * N) - k * (N / 4);   // elements of this word
+                        u[k] = left_of <= 0 ? 0u : N == 8 && left_of == 1 ? u[k] & 0xffffu : u[k];
                     }
                 }
-            }
-            // LANES lanes' sums of eight: halves of what is left are exchanged until each lane has one, which is then summed up
-            int mine = 0;
 #pragma unroll
-            for (int x = LANES / 2, v = AT_ONCE; x; x >>= 1) {
-                if (v > 1) {
-                    v >>= 1;
-                    const bool up = lane & x;
-                    mine += up ? v : 0;
-#pragma unroll
-                    for (int j = 0; j < AT_ONCE / 2; ++j)
-                        if (j < v) {
-                            sum[j] = (up ? sum[j + v] : sum[j]) + __shfl_xor_sync(~0u, up ? sum[j] : sum[j + v], x);
-                            size[j] = (up ? size[j + v] : size[j]) + __shfl_xor_sync(~0u, up ? size[j] : size[j + v], x);
-                        }
-                } else {
-                    sum[0] += __shfl_xor_sync(~0u, sum[0], x);
-                    size[0] += __shfl_xor_sync(~0u, size[0], x);
+                for (int k = 0; k < N / 2; ++k) {
+                    const uint64_t f = pair(c[j][x], k);
+                    s2 = attn::fma2(q[x][k], f, s2);
+                    m2 = attn::fma2(f, f, m2);
                 }
             }
-            const int k = mine * STEP + lane / LANES, page = __shfl_sync(~0u, mine_held, k);
-            if (lane % (LANES / AT_ONCE) == 0 && p0 + k < of_n) {
-                // (a page that is none scores -inf)
-                const bool none = (unsigned)page >= (unsigned)a.means.pages;
-                scores[p0 + k] = none ? make_float2(-CUDART_INF_F, 0.f) : make_float2(sum[0], size[0] == 0.f ? 0.f : fmaf(size[0], kScoreOff, kUnderflow));
-            }
+            float y, z;
+            attn::split(s2, y, z);
+            sum[j] = y + z;
+            attn::split(m2, y, z);
+            size[j] = y + z;
+            nothing |= size[j] == 0.f;
+        }
+        if (__any_sync(~0u, nothing && e0 < a.d)) {   // squares that underflow are something; a mean of zeros alone has an exact score
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j)
 #pragma unroll
-                for (int x = 0; x < HALVES; ++x) now[j][x] = next[j][x];
+                for (int x = 0; x < HALVES; ++x)
+                    if ((c[j][x].x | c[j][x].y | c[j][x].z | c[j][x].w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) size[j] += kTiny;
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int x = 0; x < HALVES; ++x) c[j][x] = next[j][x];
+        // LANES lanes' sums of eight: halves of what is left are exchanged until each lane has one, which is then summed up
+        int mine = 0;
+#pragma unroll
+        for (int x = LANES / 2, v = AT_ONCE; x; x >>= 1) {
+            if (v > 1) {
+                v >>= 1;
+                const bool up = lane & x;
+                mine += up ? v : 0;
+#pragma unroll
+                for (int j = 0; j < AT_ONCE / 2; ++j)
+                    if (j < v) {
+                        sum[j] = (up ? sum[j + v] : sum[j]) + __shfl_xor_sync(~0u, up ? sum[j] : sum[j + v], x);
+                        size[j] = (up ? size[j + v] : size[j]) + __shfl_xor_sync(~0u, up ? size[j] : size[j + v], x);
+                    }
+            } else {
+                sum[0] += __shfl_xor_sync(~0u, sum[0], x);
+                size[0] += __shfl_xor_sync(~0u, size[0], x);
+            }
+        }
+        const int k = mine * STEP + lane / LANES, page = __shfl_sync(~0u, mine_held, k);
+        if (lane % (LANES / AT_ONCE) == 0 && p0 + k < of_n) {
+            // (a page that is none scores -inf)
+            const bool none = (unsigned)page >= (unsigned)a.means.pages;
+            const float off = size[0] == 0.f ? 0.f : fmaf(norm * sqrtf(fmaf(size[0], 1.0001f, kTiny)), kScoreOff, kUnderflow);
+            scores[k] = none ? make_float2(-CUDART_INF_F, 0.f) : make_float2(sum[0], off);
         }
         if (!more) return;
     }
@@ -805,10 +835,16 @@ __device__ __forceinline__ unsigned ordered(float x)
 }
 __device__ __forceinline__ float from_ordered(unsigned u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
 
+// Pages next to the border, with their scores of 64 bits.
+constexpr int kNear = 32;
+struct Few {
+    unsigned long long key[kNear];
+    int page[kNear], n;
+};
 // The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS pages a lane in registers (0: any number, read again each time).  Bound
 // by latency: one for the scores, then about 25 counts, each a few instructions a key and (several warps) a barrier.
 template <typename T, int WARPS, int KEYS>
-__device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g, int n, float2 *scores, int *list, int (&sums)[2][WARPS], unsigned (&ends)[3][WARPS])
+__device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g, int n, float2 *scores, int *list, int (&sums)[2][WARPS], unsigned (&ends)[3][WARPS], Few &few)
 {
     const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5, keep = a.keep;
     const int each = ((n + WARPS - 1) / WARPS + 31) & ~31, p0 = warp * each, p1 = min(n, p0 + each), rounds = KEYS ? KEYS : each / 32;   // this warp's pages
@@ -868,26 +904,22 @@ __device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g
     // Pages within reach of the border get scores of 64 bits, four at a time; those above are in, those below are out (keys that no score has).
     const bool all = off >= 0x7f800000u;
     const float from = in - reach, to = in + reach;
+    const auto close = [&](float s) { return s >= from && s <= to; };
     unsigned long long *keys = reinterpret_cast<unsigned long long *>(scores);
     const int group = a.heads / a.kv_heads;
     const int *table = a.t.entries + row_of(a.tok, i) * a.t.ld;
-    double q[8];   // elements lane, lane + 32 ...
+    double q[8] = {};   // elements lane, lane + 32 ...
+    // (loops, not copies of them, here and below: hardly any token comes here, and what few do waits for each instruction)
+#pragma unroll 1
+    for (int h = 0; h < group; ++h) {
+        const T *from = a.q + i * a.q_ld + (g * group + h) * a.q_sh + lane;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        q[e] = 0;
-        if (lane + 32 * e < a.d)
-            for (int h = 0; h < group; ++h) q[e] += attn::widen(a.q[i * a.q_ld + (g * group + h) * a.q_sh + lane + 32 * e]);
+        for (int e = 0; e < 8; ++e)
+            if (lane + 32 * e < a.d) q[e] += attn::widen(from[32 * e]);
     }
-    for (int j = 0; j < each / 32; ++j) {
-        const int p = p0 + j * 32 + lane;
+    // scores of 64 bits of those of a lane's pages that are to have one (all lanes call it; page p0 + 32 j + lane)
+    const auto exact_of = [&](int j, bool again) {
         unsigned long long key = 0;
-        bool again = false;
-        if (p < p1) {
-            const float2 s = scores[p];
-            again = !always(p) && (all || (s.x >= from && s.x <= to));
-            key = always(p) || (!all && s.x > to) ? ~0ull : 0;
-            if (again && !all && s.y == 0.f) { key = ordered((double)s.x); again = false; }   // (exact, or no page)
-        }
         for (unsigned left = __ballot_sync(~0u, again); left;) {
             int which[4];
             double x[4];
@@ -911,29 +943,100 @@ __device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g
             for (int k = 0; k < 4; ++k)
                 if (which[k] == lane) key = ordered(x[k]);
         }
+        return key;
+    };
+    if constexpr (KEYS > 0) {
+        int near = 0, above = 0;
+        unsigned long long taken = 0, next_to = 0;   // bit j: this lane's j-th page is taken, is next to the border
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) {
+            const float s = from_ordered(held[j]);
+            const bool there = p0 + j * 32 + lane < p1, over = there && (held[j] == ~0u || s > to);
+            const bool next = there && held[j] != ~0u && close(s);
+            near += next;
+            next_to |= (unsigned long long)next << j;
+            above += over;
+            taken |= (unsigned long long)over << j;
+        }
+        near = count_all<WARPS>(near, sums, turn);
+        above = count_all<WARPS>(above, sums, turn);
+        if (!all && near <= kNear) {   // the usual case: a few, each of which counts those that are before it
+            const auto sync = [] { if (WARPS > 1) __syncthreads(); else __syncwarp(); };
+            if ((WARPS == 1 ? lane : threadIdx.x) == 0) few.n = 0;
+            sync();
+            for (; next_to; next_to &= next_to - 1) few.page[atomicAdd(&few.n, 1)] = p0 + (__ffsll((long long)next_to) - 1) * 32 + lane;   // (in any order)
+            sync();
+#pragma unroll 1
+            for (int x = warp; x < near; x += WARPS) {
+                const int p = few.page[x], held = table[p];
+                const float2 s = scores[p];
+                double y = 0;
+                if (s.y != 0.f) {   // (else exact, or no page)
+                    const T *mean = a.means.row(held, g, 0) + lane;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (lane + 32 * e < a.d) y += q[e] * attn::widen(mean[32 * e]);
+#pragma unroll
+                    for (int w = 16; w; w >>= 1) y += __shfl_xor_sync(~0u, y, w);
+                } else {
+                    y = s.x;
+                }
+                if (lane == 0) few.key[x] = ordered(y);
+            }
+            sync();
+            for (int x = 0; x < near; ++x) {
+                const int p = few.page[x];
+                if (p < p0 || p >= p1 || (p & 31) != ((p0 + lane) & 31)) continue;
+                int before = above;
+                for (int y = 0; y < near; ++y) before += few.key[y] > few.key[x] || (few.key[y] == few.key[x] && few.page[y] < p);
+                if (before < keep) taken |= 1ull << (p - p0) / 32;
+            }
+            enter<WARPS>([&](int j) { return (bool)(taken >> j & 1); }, [](int) { return false; }, rounds, p0, p1, INT_MAX, list, sums);
+            return;
+        }
+    }
+    for (int j = 0; j < each / 32; ++j) {
+        const int p = p0 + j * 32 + lane;
+        unsigned long long key = 0;
+        bool again = false;
+        if (p < p1) {
+            const float2 s = scores[p];
+            again = !always(p) && (all || close(s.x));
+            key = always(p) || (!all && s.x > to) ? ~0ull : 0;
+            if (again && !all && s.y == 0.f) { key = ordered((double)s.x); again = false; }   // (exact, or no page)
+        }
+        const unsigned long long exact = exact_of(j, again);
+        if (again) key = exact;
         if (p < p1) keys[p] = key;
     }
     __syncwarp();   // (a warp's keys are read by itself alone)
     select_exactly<WARPS>(keys, n, keep, p0, p1, each, list, sums);
 }
 
+// WARPS = 1: a CTA has four tokens and key heads (CTAs of one warp take longer to come and go than the choice).
 template <typename T, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32) paged_select_kernel(const SelectArgs<T> a)
+__global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) paged_select_kernel(const SelectArgs<T> a)
 {
+    constexpr int UNITS = WARPS == 1 ? 4 : 1;
     __shared__ int sums[2][WARPS];
     __shared__ unsigned ends[3][WARPS];
+    __shared__ Few few_of[UNITS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-    const int i = blockIdx.x / a.kv_heads, g = blockIdx.x - i * a.kv_heads, n = pages_seen(a, i);
-    int *list = a.lists + (long long)blockIdx.x * a.keep;
-    for (int p = threadIdx.x; p < a.keep; p += WARPS * 32)
+    const int mine = UNITS == 1 ? 0 : threadIdx.x >> 5, thread = UNITS == 1 ? threadIdx.x : threadIdx.x & 31;
+    const int unit = blockIdx.x * UNITS + mine;
+    if (unit >= a.M * a.kv_heads) return;
+    Few &few = few_of[mine];
+    const int i = unit / a.kv_heads, g = unit - i * a.kv_heads, n = pages_seen(a, i);
+    int *list = a.lists + (long long)unit * a.keep;
+    for (int p = thread; p < a.keep; p += WARPS * 32)
         if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
     if (n <= a.keep) return;
-    float2 *scores = a.scores + (long long)blockIdx.x * a.t.width;
-    if (n <= 256 * WARPS) select_best<T, WARPS, 8>(a, i, g, n, scores, list, sums, ends);
-    else if (n <= 1024 * WARPS) select_best<T, WARPS, 32>(a, i, g, n, scores, list, sums, ends);
-    else if (n <= 2048 * WARPS) select_best<T, WARPS, 64>(a, i, g, n, scores, list, sums, ends);
-    else if (WARPS > 1) select_best<T, WARPS, 0>(a, i, g, n, scores, list, sums, ends);
+    float2 *scores = a.scores + (long long)unit * a.t.width;
+    if (n <= 256 * WARPS) select_best<T, WARPS, 8>(a, i, g, n, scores, list, sums, ends, few);
+    else if (n <= 1024 * WARPS) select_best<T, WARPS, 32>(a, i, g, n, scores, list, sums, ends, few);
+    else if (n <= 2048 * WARPS) select_best<T, WARPS, 64>(a, i, g, n, scores, list, sums, ends, few);
+    else if (WARPS > 1) select_best<T, WARPS, 0>(a, i, g, n, scores, list, sums, ends, few);
 }
 }  // namespace paged
 }  // namespace b2sp

@@ -138,7 +138,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     if (rc == B2SP_OK) rc = check_tables(t, means->page);
     if (rc != B2SP_OK) return rc;
     if (M && (!Q || !seen || !lists)) return B2SP_ERR_INVALID_ARG;
-    if (d > 256 || M > kMostTokens) return B2SP_ERR_UNSUPPORTED;
+    if (d > 256 || M > kMostTokens || std::max(means->stride_head, means->stride_page) > (long long)(UINT_MAX / sizeof(T))) return B2SP_ERR_UNSUPPORTED;
     const long long blocks = (long long)M * kv_heads * (((long long)t->width + 7) / 8), ctas = (long long)M * kv_heads;   // blocks: of eight pages at least
     if (ctas > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
@@ -167,7 +167,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     }
     // a warp holds 2048 keys
     if (t->width <= 2048) {
-        if (!launch_early<paged_select_kernel<T, 1>>((unsigned)ctas, 32, 0, st, a)) return B2SP_ERR_CUDA;
+        if (!launch_early<paged_select_kernel<T, 1>>((unsigned)((ctas + 3) / 4), 128, 0, st, a)) return B2SP_ERR_CUDA;
     } else if (!launch_early<paged_select_kernel<T, 8>>((unsigned)ctas, 256, 0, st, a)) {
         return B2SP_ERR_CUDA;
     }
