@@ -385,12 +385,14 @@ b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long 
  *   request alone.  At most 8192 requests, d <= 1024.
  * b2sp_paged_select chooses pages by a score, (sum of the queries of the head's group) . (mean of the page), formed in 64 bits: of the pages that a token
  *   sees the first `first`, the last `last` and the best others, `keep` in all; of equal scores the lower page; NaN scores last.  lists[M][kv_heads][keep]: ascending
- *   indices into the request's table, -1 behind the last.  means->page: rows of the cache's pages.  first + last <= keep, d <= 256.
+ *   indices into the request's table, -1 behind the last.  means->page: rows of the cache's pages.  first + last <= keep, d <= 256;
+ *   strides of the means below 2^32 bytes.
  * b2sp_attention_paged: O and lse[M][heads] as for b2sp_attention_kv4, of M tokens over the positions that they see, or (lists not NULL) those of them
  *   that lie in the pages listed for the token and key head: of a list's entries the first ones count, as many as the token sees pages; each is its own
  *   term, in any order, and one that is no page seen is left out.  Q, O: token i, head h at i * ld + h * stride_head.
  *   Any M, but made for few tokens with long rows: a row is cut into parts and joined; neighbouring tokens of one request read its rows together.  d <= 256;
- *   strides below 2^32 bytes.
+ *   strides below 2^32 bytes.  O may be Q itself, with its strides.
+ * Other than that no call may write to what it reads (K and V of a write may be rows of the caches that it leaves as they are).  At most 2^30 tokens.
  */
 typedef struct {
     void *data; long long ld, stride_head, stride_page;

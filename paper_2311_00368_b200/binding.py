@@ -994,7 +994,7 @@ def _attention_paged_need(M, heads, kv_heads, d):
 def attention_paged(q, k_pages, v_pages, tables, seen, rows=None, lists=None, scale=None, out=None, lse=None, workspace=None, dtype=torch.float32):
     """b2sp_attention_paged: (O, lse) of tokens q [M, heads, d] over caches in pages; token i sees the first seen[i] positions of request rows[i]
     (of request i without rows), or with lists [M, kv_heads, keep] (see paged_select) those of them that lie in the pages listed.  O is like q, lse fp32
-    [M, heads] (-inf, and a zero row of O, where nothing is seen); scale d ** -0.5 unless given."""
+    [M, heads] (-inf, and a zero row of O, where nothing is seen); scale d ** -0.5 unless given.  out may be q."""
     (M, H, d), s = _of_tokens(q, dtype, "q")
     kp, a = _pages(k_pages, dtype, "k_pages")
     vp, b = _pages(v_pages, dtype, "v_pages")

@@ -86,6 +86,12 @@ bool meet(const void *a, size_t an, const void *b, size_t bn)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return an && bn && x < y + bn && y < x + an;
 }
+// Whether an output lies in what tells of the tokens.
+bool of_tokens(const void *out, size_t n, int M, const b2sp_page_tables *t, const int *rows, const int *seen)
+{
+    const size_t entries = t->requests ? ((t->requests - 1) * (size_t)t->ld + t->width) * 4 : 0;
+    return meet(out, n, seen, M * 4ull) || (rows && meet(out, n, rows, M * 4ull)) || meet(out, n, t->entries, entries);
+}
 
 template <typename T> bool fits(const void *x, long long ld, long long sh, size_t bytes)   // rows begin on multiples of `bytes`
 {
@@ -142,6 +148,7 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     const long long blocks = (long long)M * kv_heads * (((long long)t->width + 7) / 8), ctas = (long long)M * kv_heads;   // blocks: of eight pages at least
     if (ctas > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
+    if (of_tokens(lists, (size_t)ctas * keep * 4, M, t, rows, seen)) return B2SP_ERR_INVALID_ARG;
     if (M == 0) return B2SP_OK;
     SelectArgs<T> a = {};
     a.t = tables(t);
@@ -315,10 +322,7 @@ extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pa
     b2sp_status rc = check_tables(t, page);
     if (rc != B2SP_OK) return rc;
     if (M < 0 || pages < 0 || entries < 0 || !row_ptr || (M && !seen) || (entries && !col_idx)) return B2SP_ERR_INVALID_ARG;
-    for (const void *x : {static_cast<const void *>(seen), static_cast<const void *>(rows), static_cast<const void *>(t->entries)}) {
-        const size_t n = x == t->entries ? (t->requests ? ((t->requests - 1) * (size_t)t->ld + t->width) * 4 : 0) : M * 4ull;
-        if (x && (meet(x, n, row_ptr, (M + 1) * 4ull) || meet(x, n, col_idx, entries * 4ull))) return B2SP_ERR_INVALID_ARG;
-    }
+    if (of_tokens(row_ptr, (M + 1) * 4ull, M, t, rows, seen) || of_tokens(col_idx, entries * 4ull, M, t, rows, seen)) return B2SP_ERR_INVALID_ARG;
     if (entries > INT_MAX || (long long)pages * page > INT_MAX || M > kMostTokens) return B2SP_ERR_UNSUPPORTED;
     ListsArgs a = {};
     a.t = tables(t);

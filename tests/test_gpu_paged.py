@@ -424,6 +424,20 @@ def test_attention_other_layouts():
         c.check()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("seen,H,Hkv,d,rows", [([20000, 0, 5], 8, 2, 128, None), ([7] * 3000, 4, 2, 64, None), ([900, 3, 40, 40, 41] * 60, 20, 1, 50, None),
+                                               ([300, 301, 302, 303] * 50, 2, 1, 64, [i // 4 for i in range(200)])])
+def test_the_output_in_place_of_the_queries(seen, H, Hkv, d, rows, dtype):
+    c = Cache(31, seen, H, Hkv, d, 16, dtype, rows=rows)
+    o, lse = c.attend()
+    room = torch.randn((len(seen), H + 3, d), device="cuda").to(dtype)     # queries among other heads
+    room[:, 1:H + 1] = c.q
+    before, c.q = room.clone(), room[:, 1:H + 1]
+    got, got_lse = c.attend(out=c.q)
+    assert got.data_ptr() == c.q.data_ptr() and torch.equal(got, o) and torch.equal(got_lse, lse)
+    assert torch.equal(room[:, :1], before[:, :1]) and torch.equal(room[:, H + 1:], before[:, H + 1:])
+
+
 def test_offsets_beyond_32_bits():
     """A cache of more than 2^32 bytes and elements apart: pages near its end."""
     b = _binding()

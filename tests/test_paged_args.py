@@ -96,6 +96,14 @@ def test_select(b):
     assert f(M=0) == OK
 
 
+def test_select_lists_in_what_is_read(b):
+    f = lambda out: b.lib.b2sp_paged_select(3, 4, 2, 64, 4096, 256, 64, _cache(b, stride_head=64, stride_page=128),  # noqa: E731
+                                            _tab(b, entries=1 << 21), 1 << 22, 1 << 23, 4, 1, 1, out, 1 << 30, 1 << 20, None)
+    for at in (1 << 21, 1 << 22, 1 << 23):                                                     # tables (48 entries), rows, seen (3 of each); 24 are written
+        n = 48 if at == 1 << 21 else 3
+        assert f(at) == f(at + 4 * n - 4) == f(at - 4 * 23) == INVALID
+
+
 def test_attention(b):
     need = b.lib.b2sp_attention_paged_workspace_bytes
     def f(M=3, H=4, Hkv=2, d=64, q=4096, ldq=256, kp=None, vp=None, t=None, seen=4096, lists=None, keep=0, scale=0.1, o=4096, ldo=256, sho=64, lse=4096,
