@@ -563,8 +563,8 @@ __device__ __forceinline__ unsigned long long ordered(double x)
 
 // The choice is defined by scores in 64 bits, since between two close ones sums of 32 bits would choose by their order.  Few scores are that close: they
 // are formed in 32 bits with a bound of the error, and a token whose border lies between two scores that are further apart than that is done; only
-// where others lie within reach of the border these are formed again in 64 bits.  (All of them in 64 bits: 12.3 instead of 10.3 us for a token that sees 2048
-// pages, 8 key heads.)
+// where others lie within reach of the border these are formed again in 64 bits.  (All of them in 64 bits: 2 us more of the 9 to 10 for a token that sees
+// 2048 pages, 8 key heads.)
 //
 // Scores of the pages of tokens that see more than a list holds: all tokens' and key heads' blocks of pages are dealt to the warps in equal shares; the sum of the
 // group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  The next block's
@@ -835,27 +835,32 @@ __device__ __forceinline__ unsigned ordered(float x)
 }
 __device__ __forceinline__ float from_ordered(unsigned u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
 
-// Pages next to the border, with their scores of 64 bits.
+// Pages next to the border, with their scores of 64 bits; in: whether those of 32 bits are at or above it.
 constexpr int kNear = 32;
 struct Few {
     unsigned long long key[kNear];
-    int page[kNear], n;
+    int page[kNear], in[kNear], n;
 };
 // The best `keep` of a token's pages, WARPS warps per token and key head with up to KEYS pages a lane in registers (0: any number, read again each time).  Bound
-// by latency: one for the scores, then about 25 counts, each a few instructions a key and (several warps) a barrier.
+// by latency: one for the scores, then about ten counts, each a few instructions a key and (several warps) a barrier: a border is looked for between the best
+// score and one that `keep` reach surely, the least of the lanes' best where there are lanes enough.
 template <typename T, int WARPS, int KEYS>
-__device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g, int n, float2 *scores, int *list, int (&sums)[2][WARPS], unsigned (&ends)[3][WARPS], Few &few)
+__device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g, int n, float2 *scores, int *list, int (&sums)[2][WARPS], unsigned (&ends)[6][WARPS], Few &few)
 {
     const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5, keep = a.keep;
     const int each = ((n + WARPS - 1) / WARPS + 31) & ~31, p0 = warp * each, p1 = min(n, p0 + each), rounds = KEYS ? KEYS : each / 32;   // this warp's pages
     const auto always = [&](int p) { return p < a.first || p >= n - a.last; };
     unsigned off = 0;   // the largest error's bits; those of a NaN or an infinity where a score or an error is one
+    unsigned top = 0, bottom = ~0u;   // of this lane's scores
     const auto load = [&](int j) { return scores[min(p0 + j * 32 + lane, n - 1)]; };
     const auto key = [&](int j, float2 s) {
         const int p = p0 + j * 32 + lane;
         const bool scored = p < p1 && !always(p);
+        const unsigned x = ordered(s.x);
         off = max(off, !scored ? 0u : s.x < CUDART_INF_F && (s.x > -CUDART_INF_F || s.y == 0.f) ? __float_as_uint(s.y) : 0x7f800000u);
-        return scored ? ordered(s.x) : p < p1 ? ~0u : 0u;
+        top = max(top, scored ? x : 0u);
+        bottom = min(bottom, scored ? x : ~0u);
+        return scored ? x : p < p1 ? ~0u : 0u;
     };
     unsigned held[KEYS ? KEYS : 1];
     if constexpr (KEYS > 0) {
@@ -876,167 +881,221 @@ __device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g
         for (int j = 0; j < rounds; ++j) key(j, load(j));
     }
     const auto at = [&](int j) { if constexpr (KEYS > 0) return held[j]; else return key(j, load(j)); };
-    int turn = 0, at_least = n;
-    const unsigned border = border_of<WARPS>([&](int j, unsigned to) { return at(j) >= to; }, rounds, keep, at_least, sums, turn);
-    // the lowest score that is in, the highest that is not, the error
-    unsigned lowest = ~0u, highest = 0;
-#pragma unroll
-    for (int j = 0; j < rounds; ++j) {
-        const unsigned x = at(j);
-        if (x >= border && x) lowest = min(lowest, x);
-        if (x < border) highest = max(highest, x);
-    }
-    lowest = __reduce_min_sync(~0u, lowest);
-    highest = __reduce_max_sync(~0u, highest);
+    unsigned least = __reduce_min_sync(~0u, top);
+    top = __reduce_max_sync(~0u, top);
+    bottom = __reduce_min_sync(~0u, bottom);
     off = __reduce_max_sync(~0u, off);
     if (WARPS > 1) {
-        if (lane == 0) { ends[0][warp] = lowest; ends[1][warp] = highest; ends[2][warp] = off; }
+        if (lane == 0) { ends[0][warp] = least; ends[1][warp] = top; ends[2][warp] = bottom; ends[3][warp] = off; }
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) { lowest = min(lowest, ends[0][w]); highest = max(highest, ends[1][w]); off = max(off, ends[2][w]); }
+        for (int w = 0; w < WARPS; ++w) { least = min(least, ends[0][w]); top = max(top, ends[1][w]); bottom = min(bottom, ends[2][w]); off = max(off, ends[3][w]); }
     }
-    const float reach = 2.1f * __uint_as_float(off), in = from_ordered(lowest), out = from_ordered(highest);
-    // (what is always taken scores more than any number)
-    if (at_least == keep && off < 0x7f800000u && (lowest == ~0u || in - out > reach)) {
-        enter<WARPS>([&](int j) { return at(j) >= border; }, [](int) { return false; }, rounds, p0, p1, INT_MAX, list, sums);
-        return;
-    }
-    // Pages within reach of the border get scores of 64 bits, four at a time; those above are in, those below are out (keys that no score has).
-    const bool all = off >= 0x7f800000u;
-    const float from = in - reach, to = in + reach;
-    const auto close = [&](float s) { return s >= from && s <= to; };
-    unsigned long long *keys = reinterpret_cast<unsigned long long *>(scores);
-    const int group = a.heads / a.kv_heads;
-    const int *table = a.t.entries + row_of(a.tok, i) * a.t.ld;
-    double q[8] = {};   // elements lane, lane + 32 ...
-    // (loops, not copies of them, here and below: hardly any token comes here, and what few do waits for each instruction)
+    const bool all = off >= 0x7f800000u;   // nothing is known of the scores
+    int turn = 0, at_least = a.first + a.last;
+    unsigned border = ~0u;   // (of what is always taken)
+    bool sure = at_least == keep && !all;
+    float reach = 0.f, in = 0.f;
+    if (!sure && !all) {
+        const auto count = [&](unsigned to) {
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < rounds; ++j) c += at(j) >= to;
+            return count_all<WARPS>(c, sums, turn);
+        };
+        if (keep - at_least <= 32 * WARPS && least) {
+            border = least;
+            at_least = count(border);
+        } else {
+            border = bottom;
+            at_least = n;
+        }
+        unsigned behind = top + 1;   // what is always taken is all that is left there
 #pragma unroll 1
-    for (int h = 0; h < group; ++h) {
-        const T *from = a.q + i * a.q_ld + (g * group + h) * a.q_sh + lane;
+        for (int step = 0; at_least != keep && behind - border > 1; ++step) {
+            // halves of the scores' range, then (a few far out) of the numbers'
+            unsigned to = ordered(0.5f * from_ordered(border) + 0.5f * from_ordered(behind));
+            if (step >= 12 || to <= border || to >= behind) to = border + (behind - border) / 2;
+            const int c = count(to);
+            if (c >= keep) { border = to; at_least = c; } else { behind = to; }
+        }
+        // the lowest score that is in, the highest that is not
+        unsigned lowest = ~0u, highest = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (lane + 32 * e < a.d) q[e] += attn::widen(from[32 * e]);
+        for (int j = 0; j < rounds; ++j) {
+            const unsigned x = at(j);
+            if (x >= border) lowest = min(lowest, x); else highest = max(highest, x);
+        }
+        lowest = __reduce_min_sync(~0u, lowest);
+        highest = __reduce_max_sync(~0u, highest);
+        if (WARPS > 1) {
+            if (lane == 0) { ends[4][warp] = lowest; ends[5][warp] = highest; }
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) { lowest = min(lowest, ends[4][w]); highest = max(highest, ends[5][w]); }
+        }
+        reach = 2.1f * __uint_as_float(off);
+        in = from_ordered(lowest);
+        sure = at_least == keep && in - from_ordered(highest) > reach;
     }
-    // scores of 64 bits of those of a lane's pages that are to have one (all lanes call it; page p0 + 32 j + lane)
-    const auto exact_of = [&](int j, bool again) {
-        unsigned long long key = 0;
-        for (unsigned left = __ballot_sync(~0u, again); left;) {
-            int which[4];
-            double x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                which[k] = left ? __ffs(left) - 1 : -1;
-                left &= left - 1;
-                x[k] = 0;
-                const int held = which[k] < 0 ? -1 : table[p0 + j * 32 + which[k]];
-                if ((unsigned)held >= (unsigned)a.means.pages) { x[k] = lane ? 0 : -CUDART_INF; continue; }
-                const T *mean = a.means.row(held, g, 0);
+    unsigned long long flip = 0;   // bit j: this lane's j-th page is on the other side of the border than its score of 32 bits
+    if (!sure) {
+        // Pages within reach of the border get scores of 64 bits; those above are in, those below are out (keys that no score has).
+        const float from = in - reach, to = in + reach;
+        const auto close = [&](float s) { return s >= from && s <= to; };
+        unsigned long long *keys = reinterpret_cast<unsigned long long *>(scores);
+        const int group = a.heads / a.kv_heads;
+        const int *table = a.t.entries + row_of(a.tok, i) * a.t.ld;
+        const auto sync = [] { if (WARPS > 1) __syncthreads(); else __syncwarp(); };
+        double q[8] = {};   // the sum of the group's queries, elements lane, lane + 32 ...
+        if ((WARPS == 1 ? lane : threadIdx.x) == 0) few.n = 0;
+        // (loops, not copies of them, here and below: hardly any token comes here, and what few do waits for each instruction)
+        if constexpr (WARPS == 1) {
+#pragma unroll 1
+            for (int h = 0; h < group; ++h) {
+                const T *from = a.q + i * a.q_ld + (g * group + h) * a.q_sh + lane;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (lane + 32 * e < a.d) x[k] += q[e] * attn::widen(mean[lane + 32 * e]);
+                    if (lane + 32 * e < a.d) q[e] += attn::widen(from[32 * e]);
             }
-#pragma unroll
-            for (int w = 16; w; w >>= 1)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] += __shfl_xor_sync(~0u, x[k], w);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (which[k] == lane) key = ordered(x[k]);
-        }
-        return key;
-    };
-    if constexpr (KEYS > 0) {
-        int near = 0, above = 0;
-        unsigned long long taken = 0, next_to = 0;   // bit j: this lane's j-th page is taken, is next to the border
-#pragma unroll
-        for (int j = 0; j < KEYS; ++j) {
-            const float s = from_ordered(held[j]);
-            const bool there = p0 + j * 32 + lane < p1, over = there && (held[j] == ~0u || s > to);
-            const bool next = there && held[j] != ~0u && close(s);
-            near += next;
-            next_to |= (unsigned long long)next << j;
-            above += over;
-            taken |= (unsigned long long)over << j;
-        }
-        near = count_all<WARPS>(near, sums, turn);
-        above = count_all<WARPS>(above, sums, turn);
-        if (!all && near <= kNear) {   // the usual case: a few, each of which counts those that are before it
-            const auto sync = [] { if (WARPS > 1) __syncthreads(); else __syncwarp(); };
-            if ((WARPS == 1 ? lane : threadIdx.x) == 0) few.n = 0;
-            sync();
-            for (; next_to; next_to &= next_to - 1) few.page[atomicAdd(&few.n, 1)] = p0 + (__ffsll((long long)next_to) - 1) * 32 + lane;   // (in any order)
-            sync();
+            __syncwarp();
+        } else {
+            __shared__ double sum[256];
 #pragma unroll 1
-            for (int x = warp; x < near; x += WARPS) {
-                const int p = few.page[x], held = table[p];
-                const float2 s = scores[p];
+            for (int e = threadIdx.x; e < a.d; e += WARPS * 32) {
+                const T *from = a.q + i * a.q_ld + (long long)g * group * a.q_sh + e;
                 double y = 0;
-                if (s.y != 0.f) {   // (else exact, or no page)
-                    const T *mean = a.means.row(held, g, 0) + lane;
+#pragma unroll 4
+                for (int h = 0; h < group; ++h, from += a.q_sh) y += attn::widen(*from);
+                sum[e] = y;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (lane + 32 * e < a.d) q[e] = sum[lane + 32 * e];
+        }
+        // scores of 64 bits of those of a lane's pages that are to have one (all lanes call it; page p0 + 32 j + lane)
+        const auto exact_of = [&](int j, bool again) {
+            unsigned long long key = 0;
+            for (unsigned left = __ballot_sync(~0u, again); left;) {
+                int which[4];
+                double x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    which[k] = left ? __ffs(left) - 1 : -1;
+                    left &= left - 1;
+                    x[k] = 0;
+                    const int held = which[k] < 0 ? -1 : table[p0 + j * 32 + which[k]];
+                    if ((unsigned)held >= (unsigned)a.means.pages) { x[k] = lane ? 0 : -CUDART_INF; continue; }
+                    const T *mean = a.means.row(held, g, 0);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (lane + 32 * e < a.d) y += q[e] * attn::widen(mean[32 * e]);
-#pragma unroll
-                    for (int w = 16; w; w >>= 1) y += __shfl_xor_sync(~0u, y, w);
-                } else {
-                    y = s.x;
+                        if (lane + 32 * e < a.d) x[k] += q[e] * attn::widen(mean[lane + 32 * e]);
                 }
-                if (lane == 0) few.key[x] = ordered(y);
+#pragma unroll
+                for (int w = 16; w; w >>= 1)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] += __shfl_xor_sync(~0u, x[k], w);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (which[k] == lane) key = ordered(x[k]);
             }
-            sync();
-            for (int x = 0; x < near; ++x) {
-                const int p = few.page[x];
-                if (p < p0 || p >= p1 || (p & 31) != ((p0 + lane) & 31)) continue;
-                int before = above;
-                for (int y = 0; y < near; ++y) before += few.key[y] > few.key[x] || (few.key[y] == few.key[x] && few.page[y] < p);
-                if (before < keep) taken |= 1ull << (p - p0) / 32;
+            return key;
+        };
+        int near = kNear + 1;
+        if constexpr (KEYS > 0)
+            if (!all) {
+                unsigned long long next_to = 0;   // bit j: this lane's j-th page is next to the border
+                const unsigned first = ordered(from), range = ordered(to) - first;   // (no other key lies between two scores)
+#pragma unroll
+                for (int j = 0; j < KEYS; ++j) next_to |= (unsigned long long)(held[j] - first <= range) << j;
+                near = count_all<WARPS>(__popcll(next_to), sums, turn);
+                if (near <= kNear) {   // the usual case: a few, each of which counts those that are before it
+                    for (; next_to; next_to &= next_to - 1) few.page[atomicAdd(&few.n, 1)] = p0 + (__ffsll((long long)next_to) - 1) * 32 + lane;   // (in any order)
+                    sync();
+#pragma unroll 1
+                    for (int x = 2 * warp; x < near; x += 2 * WARPS) {
+                        double y[2] = {};
+                        float2 s[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int p = few.page[min(x + k, near - 1)], held = table[p];
+                            s[k] = scores[p];
+                            const bool read = (unsigned)held < (unsigned)a.means.pages;
+                            const T *mean = a.means.row(read ? held : 0, g, 0) + lane;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (read && lane + 32 * e < a.d) y[k] += q[e] * attn::widen(mean[32 * e]);
+                        }
+#pragma unroll
+                        for (int w = 16; w; w >>= 1) { y[0] += __shfl_xor_sync(~0u, y[0], w); y[1] += __shfl_xor_sync(~0u, y[1], w); }
+                        if (lane < 2 && x + lane < near) {
+                            const float2 z = lane ? s[1] : s[0];
+                            few.key[x + lane] = ordered(z.y == 0.f ? (double)z.x : lane ? y[1] : y[0]);   // (exact, or no page)
+                            few.in[x + lane] = ordered(z.x) >= border;
+                        }
+                    }
+                    sync();
+                    int above = at_least;
+                    for (int x = 0; x < near; ++x) above -= few.in[x];
+                    for (int x = 0; x < near; ++x) {
+                        const int p = few.page[x];
+                        if (p < p0 || p >= p1 || (p & 31) != lane) continue;
+                        int before = above;
+                        for (int y = 0; y < near; ++y) before += few.key[y] > few.key[x] || (few.key[y] == few.key[x] && few.page[y] < p);
+                        if ((before < keep) != (bool)few.in[x]) flip |= 1ull << (p - p0) / 32;
+                    }
+                }
             }
-            enter<WARPS>([&](int j) { return (bool)(taken >> j & 1); }, [](int) { return false; }, rounds, p0, p1, INT_MAX, list, sums);
+        if (near > kNear) {
+            for (int j = 0; j < each / 32; ++j) {
+                const int p = p0 + j * 32 + lane;
+                unsigned long long key = 0;
+                bool again = false;
+                if (p < p1) {
+                    const float2 s = scores[p];
+                    again = !always(p) && (all || close(s.x));
+                    key = always(p) || (!all && s.x > to) ? ~0ull : 0;
+                    if (again && !all && s.y == 0.f) { key = ordered((double)s.x); again = false; }   // (exact, or no page)
+                }
+                const unsigned long long exact = exact_of(j, again);
+                if (again) key = exact;
+                if (p < p1) keys[p] = key;
+            }
+            __syncwarp();   // (a warp's keys are read by itself alone)
+            select_exactly<WARPS>(keys, n, keep, p0, p1, each, list, sums);
             return;
         }
     }
-    for (int j = 0; j < each / 32; ++j) {
-        const int p = p0 + j * 32 + lane;
-        unsigned long long key = 0;
-        bool again = false;
-        if (p < p1) {
-            const float2 s = scores[p];
-            again = !always(p) && (all || close(s.x));
-            key = always(p) || (!all && s.x > to) ? ~0ull : 0;
-            if (again && !all && s.y == 0.f) { key = ordered((double)s.x); again = false; }   // (exact, or no page)
-        }
-        const unsigned long long exact = exact_of(j, again);
-        if (again) key = exact;
-        if (p < p1) keys[p] = key;
-    }
-    __syncwarp();   // (a warp's keys are read by itself alone)
-    select_exactly<WARPS>(keys, n, keep, p0, p1, each, list, sums);
+    enter<WARPS>([&](int j) { bool in = at(j) >= border; if constexpr (KEYS > 0) in ^= flip >> j & 1; return in; }, [](int) { return false; }, rounds, p0, p1, INT_MAX, list, sums);
 }
 
-// WARPS = 1: a CTA has four tokens and key heads (CTAs of one warp take longer to come and go than the choice).
-template <typename T, int WARPS>
-__global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) paged_select_kernel(const SelectArgs<T> a)
+// WARPS = 1: a CTA has four tokens and key heads (CTAs of one warp take longer to come and go than the choice).  MOST: most pages of a lane in registers;
+// early: the launch ahead is that of the scores, which has begun after all that made the tokens' numbers.
+template <typename T, int WARPS, int MOST>
+__global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) paged_select_kernel(const SelectArgs<T> a, bool early)
 {
     constexpr int UNITS = WARPS == 1 ? 4 : 1;
     __shared__ int sums[2][WARPS];
-    __shared__ unsigned ends[3][WARPS];
+    __shared__ unsigned ends[6][WARPS];
     __shared__ Few few_of[UNITS];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
+    if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
     const int mine = UNITS == 1 ? 0 : threadIdx.x >> 5, thread = UNITS == 1 ? threadIdx.x : threadIdx.x & 31;
-    const int unit = blockIdx.x * UNITS + mine;
-    if (unit >= a.M * a.kv_heads) return;
+    const int unit = blockIdx.x * UNITS + mine, units = a.M * a.kv_heads;
     Few &few = few_of[mine];
-    const int i = unit / a.kv_heads, g = unit - i * a.kv_heads, n = pages_seen(a, i);
+    const int i = unit / a.kv_heads, g = unit - i * a.kv_heads, n = unit < units ? pages_seen(a, i) : 0;
     int *list = a.lists + (long long)unit * a.keep;
-    for (int p = thread; p < a.keep; p += WARPS * 32)
-        if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
+    if (unit < units)
+        for (int p = thread; p < a.keep; p += WARPS * 32)
+            if (p >= n) list[p] = -1; else if (n <= a.keep) list[p] = p;
+    if (early) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
     if (n <= a.keep) return;
     float2 *scores = a.scores + (long long)unit * a.t.width;
-    if (n <= 256 * WARPS) select_best<T, WARPS, 8>(a, i, g, n, scores, list, sums, ends, few);
+    if (MOST == 8 || n <= 256 * WARPS) select_best<T, WARPS, 8>(a, i, g, n, scores, list, sums, ends, few);
     else if (n <= 1024 * WARPS) select_best<T, WARPS, 32>(a, i, g, n, scores, list, sums, ends, few);
     else if (n <= 2048 * WARPS) select_best<T, WARPS, 64>(a, i, g, n, scores, list, sums, ends, few);
-    else if (WARPS > 1) select_best<T, WARPS, 0>(a, i, g, n, scores, list, sums, ends, few);
+    else select_best<T, WARPS, 0>(a, i, g, n, scores, list, sums, ends, few);
 }
 }  // namespace paged
 }  // namespace b2sp

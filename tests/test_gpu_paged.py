@@ -254,7 +254,7 @@ def test_select_ties_infinities_and_nan():
     c.check_select(7, 0, 0)
 
 
-@pytest.mark.parametrize("n", [40, 600, 2300])
+@pytest.mark.parametrize("n", [40, 600, 1500, 2300])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_select_between_close_scores(n, dtype):
     """Scores that sums in 32 bits cannot tell apart: means that differ in the last place of one element, in elements that weigh next to nothing,
@@ -280,6 +280,38 @@ def test_select_between_close_scores(n, dtype):
         c.means.copy_((means.float() * f).to(dtype))
         c.check_select(n // 2)
         c.means.copy_(means)
+
+
+@pytest.mark.parametrize("n", [33, 256, 257, 1500, 2048, 3000, 9000, 17000])
+def test_select_scores_of_any_spread(n):
+    """Scores that are far apart, far out, all alike, tiny, or of pages that are not there: one query of a one, so that a score is a number of the mean."""
+    c = Cache(5, [n] * 8, 2, 2, 8, 1, torch.float32)
+    gen = torch.Generator().manual_seed(n)
+    c.q[:] = 0
+    c.q[:, :, 0] = 1
+    x = torch.randn((8, n, 2), generator=gen)
+    x[0] = torch.exp(x[0] * 8)                                            # over 20 decades
+    x[1, n // 2] = 1e4                                                    # far out, to either side
+    x[1, n // 3] = -1e4
+    x[2] = 3.25                                                           # all alike
+    x[3] = torch.exp(x[3] * 3) * 1e-44                                    # multiples of the smallest number
+    x[4] = (x[4] * 2).round()                                             # many alike
+    x[5] = -torch.exp(x[5])                                               # below zero, a page above it
+    x[5, n - 2] = 1.5
+    x[6] = 1 + (torch.arange(n).flip(0)[:, None] % 4096) * 2.0 ** -23     # neighbouring numbers
+    for i in range(8):
+        c.means[c.tables[i].long(), :, 0] = x[i].cuda()
+    gone = torch.randperm(n, generator=gen)[:n - 5]
+    c.tables[7, gone.cuda()] = -1                                         # hardly a page is there
+    x[7, gone] = -float("inf")
+    score = x.double().numpy()
+    for keep, first, last in ((2, 1, 1), (3, 1, 1), (32, 0, 0), (32, 5, 20), (n // 2 + 10, 1, 1), (n - 1, 0, 1)):
+        got = c.select(keep, first, last).cpu().numpy()
+        for i in range(8):
+            for g in range(2):
+                y = score[i, :, g].copy()
+                y[:first] = y[n - last:] = np.inf
+                assert (got[i, g] == np.sort(np.lexsort((np.arange(n), -y))[:keep])).all(), (i, g, keep)
 
 
 def test_select_rows_and_layout():
