@@ -567,15 +567,17 @@ __device__ __forceinline__ unsigned long long ordered(double x)
 // 2048 pages, 8 key heads.)
 //
 // Scores of the pages of tokens that see more than a list holds: all tokens' and key heads' blocks of pages are dealt to the warps in equal shares; the sum of the
-// group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  The next block's
-// means are on their way while this one's are added up.  Bound by HBM for many tokens (64 of 256 pages on the average: 34 MB), else by latencies.  A lane adds up eight products (in pairs) and the lanes' sums come together in at most five steps, so a score is off
+// group's queries is spread over LANES lanes, 16 bytes (HALVES: twice) of the mean each, and 32 / LANES pages are read by an instruction, a block by eight.  The
+// next blocks' means are on their way to shared memory while this one's are added up (in registers they left room for fewer: 50.6 instead of 39.4 us for 64 tokens
+// that see up to 2048 pages, 8 key heads, both kernels; their 134 MB take 20).  Few pages: bound by latencies.  A lane adds up eight products (in pairs) and
+// the lanes' sums come together in at most five steps, so a score is off
 // by at most 14 half steps of the sum of the products' magnitudes (one of them the query's rounding), and by what underflows.  That sum is no more than the
 // product of the query's and the mean's lengths (Cauchy and Schwarz), which costs as many instructions as the score; kTiny is what squares lose that underflow.
 // kScoreOff leaves room for the roundings of the bound itself and of what the choice makes of it.
 constexpr float kScoreOff = 24.f * 5.9604645e-8f, kUnderflow = 1e-42f, kTiny = 1e-42f;
-constexpr int kScoreThreads = 128, kScoreCTAs = 4;   // CTAs of an SM
+constexpr int kScoreThreads = 128, kScoreCTAs = 4, kScoreAhead = 1;   // CTAs of an SM (six: 22.3 instead of 18.9 us); blocks on their way (two: 40.7 instead of 39.4)
 template <typename T, int LANES, int HALVES>
-__global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) paged_score_kernel(const SelectArgs<T> a)
+__global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : kScoreCTAs / 2) paged_score_kernel(const SelectArgs<T> a)
 {
     constexpr int N = 16 / sizeof(T), AT_ONCE = 8, STEP = 32 / LANES, BATCH = AT_ONCE * STEP;   // pages of an instruction, of a batch
     const int lane = threadIdx.x & 31, me = blockIdx.x * (kScoreThreads / 32) + (threadIdx.x >> 5), group = a.heads / a.kv_heads;
@@ -588,41 +590,79 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
     const auto load = [&](int base) { return base + lane < a.M ? blocks_of(base + lane) : 0; };
     if (!deal<kScoreThreads>(a.M, a.kv_heads, load, [](int blocks) { return blocks; }, gridDim.x * (kScoreThreads / 32), me, 1, w)) return;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    int i = w.row, n = pages_seen(a, i), blocks = (n + BATCH - 1) / BATCH, g = (int)w.rest / blocks, b = (int)w.rest - g * blocks;
+    struct At {   // a block
+        int i, g, b, n, blocks;
+    } at, front;   // the one that is added up, the one that is asked for
+    at.i = w.row;
+    at.n = pages_seen(a, at.i);
+    at.blocks = (at.n + BATCH - 1) / BATCH;
+    at.g = (int)w.rest / at.blocks;
+    at.b = (int)w.rest - at.g * at.blocks;
+    front = at;
+    const auto step = [&](At &x) {   // whether it is another token's or head's
+        if (++x.b < x.blocks) return false;
+        x.b = 0;
+        if (++x.g == a.kv_heads) {
+            x.g = 0;
+            do
+                if (++x.i >= a.M) return false;
+            while (!(x.blocks = blocks_of(x.i)));
+            x.n = pages_seen(a, x.i);
+        }
+        return true;
+    };
     const int e0 = lane % LANES * N;   // this lane's first element
     const bool ragged = a.d % N != 0;
     const unsigned head = (unsigned)(a.means.sh * sizeof(T)), per_page = (unsigned)(a.means.sp * sizeof(T));   // (below 2^32)
     uint64_t q[HALVES][N / 2];
     float norm = 0.f;   // of the query
-    uint4 c[AT_ONCE][HALVES], next[AT_ONCE][HALVES];
-    const auto look_up = [&](int p) { return p < n ? a.t.entries[row_of(a.tok, i) * a.t.ld + p] : -1; };
-    const auto read = [&](uint4 (&c)[AT_ONCE][HALVES], int held, int g) {   // means of a block whose pages the lanes hold
-        const char *base = reinterpret_cast<const char *>(a.means.data + e0) + (unsigned long long)g * head;
+    // each lane asks for what it reads itself, kScoreAhead blocks ahead
+    extern __shared__ uint4 score_room[];
+    uint4 *room = score_room + (threadIdx.x >> 5) * (kScoreAhead + 1) * AT_ONCE * HALVES * 32 + lane;
+    const auto look_up = [&] {
+        const int p = front.b * BATCH + lane % BATCH;
+        return p < front.n ? a.t.entries[row_of(a.tok, front.i) * a.t.ld + p] : -1;
+    };
+    int entry = look_up(), held[kScoreAhead + 1], left = (int)(w.hi - w.lo), to_ask = left, asked = 0, summed = 0;   // asked, summed: places in the room
+    const auto ask = [&] {   // for means of a block whose pages the lanes hold; entries are one more block ahead
+        const int had = entry;
+        if (to_ask > 0) {
+            const char *base = reinterpret_cast<const char *>(a.means.data + e0) + (unsigned long long)front.g * head;
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const unsigned p = (unsigned)__shfl_sync(~0u, held, j * STEP + lane / LANES);
-            const char *mean = base + (unsigned long long)p * per_page;
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const unsigned p = (unsigned)__shfl_sync(~0u, had, j * STEP + lane / LANES);
+                const char *mean = base + (unsigned long long)p * per_page;
 #pragma unroll
-            for (int x = 0; x < HALVES; ++x) {
-                c[j][x] = make_uint4(0, 0, 0, 0);
-                if (p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d) c[j][x] = *reinterpret_cast<const uint4 *>(mean + x * 32 * 16);
+                for (int x = 0; x < HALVES; ++x) {
+                    const bool there = p < (unsigned)a.means.pages && e0 + x * 32 * N < a.d;
+                    const unsigned dst = (unsigned)__cvta_generic_to_shared(room + ((asked * AT_ONCE + j) * HALVES + x) * 32);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(there ? mean + x * 32 * 16 : reinterpret_cast<const char *>(a.means.data)),
+                                 "r"(there ? 16 : 0) : "memory");
+                }
+            }
+            if (--to_ask > 0) {
+                step(front);
+                entry = look_up();
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asked = asked == kScoreAhead ? 0 : asked + 1;
+        return had;
     };
     const auto pair = [](const uint4 &u, int k) {   // elements 2 k and 2 k + 1 of sixteen bytes
         const unsigned w[4] = {u.x, u.y, u.z, u.w};
         if constexpr (sizeof(T) == 2) return attn::two(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
         else return attn::two(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
     };
-    int held = look_up(b * BATCH + lane % BATCH);
-    read(c, held, g);
-    bool fresh = true;
-    for (int left = (int)(w.hi - w.lo);;) {
-        const int of_n = n, p0 = b * BATCH, mine_held = held;
-        float2 *scores = a.scores + ((long long)i * a.kv_heads + g) * a.t.width + p0;
+#pragma unroll
+    for (int x = 0; x < kScoreAhead; ++x) held[x] = ask();
+    for (bool fresh = true;;) {
+        held[kScoreAhead] = ask();
+        const int p0 = at.b * BATCH;
+        float2 *scores = a.scores + ((long long)at.i * a.kv_heads + at.g) * a.t.width + p0;
         if (fresh) {   // the sum of the queries, four heads' loads at once
             double total[HALVES][N] = {};
-            const T *from = a.q + i * a.q_ld + (long long)g * group * a.q_sh;
+            const T *from = a.q + at.i * a.q_ld + (long long)at.g * group * a.q_sh;
             for (int h = 0; h < group; h += 4) {
                 Chunk<T> y[4][HALVES];
 #pragma unroll
@@ -654,25 +694,9 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
 #pragma unroll
             for (int x = 1; x < LANES; x <<= 1) norm += __shfl_xor_sync(~0u, norm, x);
             norm = sqrtf(fmaf(norm, 1.0001f, kTiny));
-            fresh = false;
         }
-        // the next block's pages
-        const bool more = --left > 0;
-        if (more) {
-            if (++b == blocks) {
-                b = 0;
-                fresh = true;
-                if (++g == a.kv_heads) {
-                    g = 0;
-                    do
-                        if (++i >= a.M) return;
-                    while (!(blocks = blocks_of(i)));
-                    n = pages_seen(a, i);
-                }
-            }
-            held = look_up(b * BATCH + lane % BATCH);
-            read(next, held, g);
-        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kScoreAhead) : "memory");
+        const uint4 *mean = room + summed * AT_ONCE * HALVES * 32;
         float sum[AT_ONCE], size[AT_ONCE];   // of the products, and of the mean's squares
         bool nothing = false;
 #pragma unroll
@@ -680,8 +704,9 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
             uint64_t s2 = 0, m2 = 0;
 #pragma unroll
             for (int x = 0; x < HALVES; ++x) {
+                uint4 c = mean[(j * HALVES + x) * 32];
                 if (ragged && e0 + x * 32 * N + N > a.d) {   // what lies behind d may be anything
-                    unsigned *u = &c[j][x].x;
+                    unsigned *u = &c.x;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int left_of = a.d - (e0 + x * 32 * N) - k * (N / 4);   // elements of this word
@@ -690,7 +715,7 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                 }
 #pragma unroll
                 for (int k = 0; k < N / 2; ++k) {
-                    const uint64_t f = pair(c[j][x], k);
+                    const uint64_t f = pair(c, k);
                     s2 = attn::fma2(q[x][k], f, s2);
                     m2 = attn::fma2(f, f, m2);
                 }
@@ -707,12 +732,11 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
             for (int j = 0; j < AT_ONCE; ++j)
 #pragma unroll
                 for (int x = 0; x < HALVES; ++x)
-                    if ((c[j][x].x | c[j][x].y | c[j][x].z | c[j][x].w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) size[j] += kTiny;
+                {
+                    const uint4 c = mean[(j * HALVES + x) * 32];   // (with what lies behind d: a bound may be larger)
+                    if ((c.x | c.y | c.z | c.w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) size[j] += kTiny;
+                }
         }
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j)
-#pragma unroll
-            for (int x = 0; x < HALVES; ++x) c[j][x] = next[j][x];
         // LANES lanes' sums of eight: halves of what is left are exchanged until each lane has one, which is then summed up
         int mine = 0;
 #pragma unroll
@@ -732,14 +756,18 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : 2) p
                 size[0] += __shfl_xor_sync(~0u, size[0], x);
             }
         }
-        const int k = mine * STEP + lane / LANES, page = __shfl_sync(~0u, mine_held, k);
-        if (lane % (LANES / AT_ONCE) == 0 && p0 + k < of_n) {
+        const int k = mine * STEP + lane / LANES, page = __shfl_sync(~0u, held[0], k);
+        if (lane % (LANES / AT_ONCE) == 0 && p0 + k < at.n) {
             // (a page that is none scores -inf)
             const bool none = (unsigned)page >= (unsigned)a.means.pages;
             const float off = size[0] == 0.f ? 0.f : fmaf(norm * sqrtf(fmaf(size[0], 1.0001f, kTiny)), kScoreOff, kUnderflow);
             scores[k] = none ? make_float2(-CUDART_INF_F, 0.f) : make_float2(sum[0], off);
         }
-        if (!more) return;
+        if (--left == 0) return;
+        fresh = step(at);
+        summed = summed == kScoreAhead ? 0 : summed + 1;
+#pragma unroll
+        for (int x = 0; x < kScoreAhead; ++x) held[x] = held[x + 1];
     }
 }
 

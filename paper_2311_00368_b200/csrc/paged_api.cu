@@ -163,13 +163,14 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     a.q_wide = fits<T>(Q, ldq, shq, 16);
     const bool scored = t->width > keep;   // else no token sees more pages than a list holds
     if (scored) {
-        const unsigned grid = (unsigned)std::min((blocks + kScoreThreads / 32 - 1) / (kScoreThreads / 32), (long long)kSMs * kScoreCTAs);
         constexpr int N = 16 / sizeof(T);
+        const unsigned grid = (unsigned)std::min((blocks + kScoreThreads / 32 - 1) / (kScoreThreads / 32), (long long)kSMs * (d <= 32 * N ? kScoreCTAs : kScoreCTAs / 2));
+        constexpr size_t room = kScoreThreads * (kScoreAhead + 1) * 8 * 16;   // eight loads of 16 bytes of a lane
         bool ok = false;
-        if (d <= 8 * N) ok = launch_early<paged_score_kernel<T, 8, 1>>(grid, kScoreThreads, 0, st, a);
-        else if (d <= 16 * N) ok = launch_early<paged_score_kernel<T, 16, 1>>(grid, kScoreThreads, 0, st, a);
-        else if (d <= 32 * N) ok = launch_early<paged_score_kernel<T, 32, 1>>(grid, kScoreThreads, 0, st, a);
-        else if constexpr (sizeof(T) == 4) ok = launch_early<paged_score_kernel<T, 32, 2>>(grid, kScoreThreads, 0, st, a);
+        if (d <= 8 * N) ok = launch_early<paged_score_kernel<T, 8, 1>>(grid, kScoreThreads, room, st, a);
+        else if (d <= 16 * N) ok = launch_early<paged_score_kernel<T, 16, 1>>(grid, kScoreThreads, room, st, a);
+        else if (d <= 32 * N) ok = launch_early<paged_score_kernel<T, 32, 1>>(grid, kScoreThreads, room, st, a);
+        else if constexpr (sizeof(T) == 4) ok = launch_early<paged_score_kernel<T, 32, 2>>(grid, kScoreThreads, 2 * room, st, a);
         if (!ok) return B2SP_ERR_CUDA;
     }
     // Eight keys a lane where that can be: more of them are more code, which runs once (one warp's 64: 69.7 instead of 50.8 us for 64 tokens that see up to 2048
