@@ -509,10 +509,11 @@ def _ready(device, *others):
     """Raises where tensors are not on `device`, or that is not the current one."""
     if device.type != "cuda":
         raise ValueError("tensors must be on a CUDA device")
+    index = device.index
     for t in others:
-        if t.device != device:
+        if t.get_device() != index:   # (-1: not on a GPU; half the time of comparing devices)
             raise ValueError(f"tensors on {device} and {t.device}")
-    if device.index != _current_device():
+    if index != _current_device():
         raise ValueError(f"tensors are on {device}, the current device is cuda:{_current_device()}: "
                          "call under torch.cuda.device(...)")
 
@@ -976,9 +977,7 @@ def paged_select(q, means, tables, seen, page, keep, first=1, last=1, rows=None,
     else:
         to = _int32(out, "out", (M, Hkv, keep))
         _ready(device, out)
-    _ready(device, means, tables, seen)
-    if rows is not None:
-        _ready(device, rows)
+    _ready(device, means, tables, seen, seen if rows is None else rows)
     stream = _raw_stream(device.index)
     ws = _scratch(_paged_select_need(M, Hkv, tables.shape[1]), device, workspace, stream)
     fn, name = (lib.b2sp_paged_select, "b2sp_paged_select") if dtype == torch.float32 else (lib.b2sp_paged_select_bf16, "b2sp_paged_select_bf16")
@@ -1006,9 +1005,6 @@ def attention_paged(q, k_pages, v_pages, tables, seen, rows=None, lists=None, sc
     if lists is not None:
         keep = lists.shape[-1]
         at_lists = _int32(lists, "lists", (M, Hkv, keep))
-        _ready(device, lists)
-    if rows is not None:
-        _ready(device, rows)
     if out is None:
         out = torch.empty_like(q) if 0 not in s else torch.empty((M, H, d), dtype=dtype, device=device)
     elif out.dtype is not dtype or out.shape != (M, H, d):
@@ -1020,7 +1016,7 @@ def attention_paged(q, k_pages, v_pages, tables, seen, rows=None, lists=None, sc
         lse = torch.empty_strided((M, H), (H, 1), dtype=torch.float32, device=device)
     else:
         _lse(lse, (M, H))
-    _ready(device, out, lse, k_pages, v_pages, tables, seen)
+    _ready(device, out, lse, k_pages, v_pages, tables, seen, seen if rows is None else rows, seen if lists is None else lists)
     stream = _raw_stream(device.index)
     ws = _scratch(_attention_paged_need(M, H, Hkv, d), device, workspace, stream)
     fn, name = ((lib.b2sp_attention_paged, "b2sp_attention_paged") if dtype == torch.float32
