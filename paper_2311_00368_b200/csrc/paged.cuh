@@ -771,6 +771,8 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : kSco
     }
 }
 
+// The block's sum of c.  One barrier a count: two places take turns, so that a warp that is ahead writes where nobody still adds up.  So all counts between
+// two barriers of other kinds go by one `turn`.
 template <int WARPS> __device__ __forceinline__ int count_all(int c, int (&sums)[2][WARPS], int &turn)
 {
     c = __reduce_add_sync(~0u, c);
@@ -829,14 +831,16 @@ __device__ __forceinline__ void enter(Over over, Tie tie, int rounds, int p0, in
         tied += __popc(equal);
     }
 }
-// By keys of 64 bits in memory: first by their upper halves, then, among those that have that of the border, by their lower ones.
-template <int WARPS> __device__ __noinline__ void select_exactly(const unsigned long long *keys, int n, int keep, int p0, int p1, int each, int *list, int (&sums)[2][WARPS])
+// By keys of 64 bits in memory: first by their upper halves, then, among those that have that of the border, by their lower ones.  turn: of the caller's
+// counts, which some warps may still be adding up.
+template <int WARPS>
+__device__ __noinline__ void select_exactly(const unsigned long long *keys, int n, int keep, int p0, int p1, int each, int *list, int (&sums)[2][WARPS], int turn)
 {
     const int lane = threadIdx.x & 31, rounds = each / 32;
     const auto key = [&](int j) { const int p = p0 + j * 32 + lane; return p < p1 ? keys[p] : 0; };
     const auto high = [&](int j) { return (unsigned)(key(j) >> 32); };
     const auto low = [&](int j) { return (unsigned)key(j); };
-    int turn = 0, at_least = n, ties = INT_MAX;
+    int at_least = n, ties = INT_MAX;
     unsigned lower = 0;
     const unsigned border = border_of<WARPS>([&](int j, unsigned to) { return high(j) >= to; }, rounds, keep, at_least, sums, turn);
     const auto count = [&](auto in) {
@@ -1091,7 +1095,7 @@ __device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g
                 if (p < p1) keys[p] = key;
             }
             __syncwarp();   // (a warp's keys are read by itself alone)
-            select_exactly<WARPS>(keys, n, keep, p0, p1, each, list, sums);
+            select_exactly<WARPS>(keys, n, keep, p0, p1, each, list, sums, turn);
             return;
         }
     }
