@@ -13,7 +13,7 @@
 // 64 tokens over 1 to 16384 positions, 32 heads over 8, width 128, bfloat16: 2.15 GB in 330 to 350 us, 94 to 99% of the copy bandwidth; one token over 32768:
 // 30.5 us, of which 20.5 are its bytes and the rest is launch, prologue and joining.
 // Rows that are not there (behind what is seen, of missing pages) are filled with zeros by the copies instead of read: what memory holds there does not
-// enter.
+// enter.  Rows that some queries of a unit see and others do not have a weight of 0 for these, which is nothing unless a value is not finite; see Tile16.
 #pragma once
 #include "paged.cuh"
 
@@ -297,8 +297,9 @@ constexpr float kAhead = 8.f;   // the reference of the exponentials follows the
 // What a warp holds of a unit, bfloat16: the tile's rows are the long side of the products (S^T = K Q^T, O^T = V^T P^T), the queries the side of eight, so
 // that no more than the queries there are is padded, and K and V come straight from their rows by ldmatrix.
 // A weight goes into its product as two bfloat16 that make up 16 bits of it, so that results are as far from the formula as their own rounding alone makes
-// them; with one the products take a third less, which the largest case does not notice (198 instead of 203 us) and calls of short rows do (36 instead of 39).  With an infinity in V
-// the lower part would make 0 * inf or inf - inf of it, so a unit whose sums are not finite is taken again with the upper part alone.
+// them; with one the products take a third less, which the largest case does not notice (198 instead of 203 us) and calls of short rows do (36 instead of 39).
+// A weight of 0 (of a query that does not see a row which others of its unit see) or a lower part makes NaN of an infinity in V, so a unit whose sums are not
+// finite is taken again, and then what is not finite goes into the sums of those that see it by itself, and not into the products.
 template <int W, int NT> struct Tile16 {
     static constexpr int QUERIES = 8 * NT, KS = W / 16;
     // a unit's queries are loaded while the one before it is taken (wider ones would not fit); sixteen of the widest stay in shared memory
@@ -307,7 +308,7 @@ template <int W, int NT> struct Tile16 {
     float o[KS][NT][4];       // [columns 16 x ..][queries 8 x ..]: columns g, g + 8 (pairs), queries 2 t, 2 t + 1
     float base[NT][2], ahead[NT][2], sum[NT][2];   // of queries 2 t, 2 t + 1; ahead: by how much a logit may exceed base (-inf: none has been met)
     int sees[NT][2];
-    bool lower;
+    bool apart;               // what is not finite in V is not in the products
 
     static __device__ __forceinline__ void load(const Queries<Bf16> &u, int lane, unsigned (&to)[KS][NT][2])
     {
@@ -362,7 +363,7 @@ template <int W, int NT> struct Tile16 {
         for (int m = 0; m < NT; ++m)
 #pragma unroll
             for (int e = 0; e < 2; ++e) sees[m][e] = alike ? INT_MAX : u.sees(m * 8 + 2 * (lane & 3) + e);
-        lower = true;
+        apart = false;
         clear();
     }
     __device__ __forceinline__ void clear()
@@ -376,7 +377,7 @@ template <int W, int NT> struct Tile16 {
         }
     }
     // there: the tile's rows that are there; first: the position of its row 0, or -1 if all queries see all of them.
-    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, char *stored)
+    __device__ __forceinline__ void take(char *tile, unsigned there, int first, float scale2, int lane, char *stored)
     {
         using F = Form<Bf16, W>;
         constexpr int H = F::ROWS / 16, SUMS = H == 1 ? 2 : 1;   // sixteens of rows; sums of a product (so that few products wait for one another)
@@ -458,16 +459,21 @@ template <int W, int NT> struct Tile16 {
                     for (int s = 0; s < KS; ++s) { o[s][m][e] *= fall; o[s][m][e + 2] *= fall; }
                 }
         }
-        unsigned high[H][NT][2], low[H][NT][2];
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int m = 0; m < NT; ++m) {
+            for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[h][m][e] = attn::ex2(x[h][m][e]);
                     sum[m][e & 1] += x[h][m][e];
                 }
+        if (apart) set_apart<H>(tile + F::ROWS * F::ROW, there, first, x, lane);
+        unsigned high[H][NT][2], low[H][NT][2];
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int m = 0; m < NT; ++m) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const unsigned u = attn::bf16x2(x[h][m][2 * j], x[h][m][2 * j + 1]);
@@ -486,12 +492,47 @@ template <int W, int NT> struct Tile16 {
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
                     mma_bf16(o[s][m], v, high[h][m][0], high[h][m][1]);
-                    if (lower) mma_bf16(o[s][m], v, low[h][m][0], low[h][m][1]);
+                    if (!apart) mma_bf16(o[s][m], v, low[h][m][0], low[h][m][1]);
                 }
             }
     }
-    // True: to be taken again.
-    __device__ __forceinline__ bool again()
+    // A tile's values that are not finite: into the sums of the queries that see their rows, and zeros in their place.  p: the weights, as `take` has them.
+    template <int H> __device__ __forceinline__ void set_apart(char *values, unsigned there, int first, const float (&p)[H][NT][4], int lane)
+    {
+        using F = Form<Bf16, W>;
+        const int g = lane >> 2, t = lane & 3;
+#pragma unroll 1
+        for (int row = 0; row < F::ROWS; ++row) {
+            if (!(there >> row & 1)) continue;   // (zeros)
+            float w[NT][2];
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = row & 8 ? p[0][m][e + 2] : p[0][m][e];
+                    if (H == 2 && row >= 16) x = row & 8 ? p[H - 1][m][e + 2] : p[H - 1][m][e];
+                    w[m][e] = __shfl_sync(~0u, x, (row & 7) * 4 + t);
+                }
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    Bf16 *at = reinterpret_cast<Bf16 *>(values + row * F::ROW + ((2 * s + j) ^ (row & 7)) * 16) + g;
+                    const unsigned u = at->bits;
+                    const bool odd = (u & 0x7f80) == 0x7f80;
+                    if (!__any_sync(~0u, odd)) continue;
+#pragma unroll
+                    for (int m = 0; m < NT; ++m)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (odd && (first < 0 || first + row < sees[m][e])) o[s][m][2 * j + e] = fmaf(w[m][e], __uint_as_float(u << 16), o[s][m][2 * j + e]);
+                    if (odd && t == 0) at->bits = 0;   // (all four lanes that look at it have read it)
+                }
+        }
+        __syncwarp();
+    }
+    // True: to be taken again.  uneven: not all queries see the same.
+    __device__ __forceinline__ bool again(bool uneven)
     {
         bool odd = false;
 #pragma unroll
@@ -500,8 +541,8 @@ template <int W, int NT> struct Tile16 {
             for (int s = 0; s < KS; ++s)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[s][m][e]) <= 3.402823466e38f);
-        odd = __any_sync(~0u, odd) && lower;
-        if (odd) lower = false;
+        odd = __any_sync(~0u, odd) && !apart;
+        apart |= odd;
         return odd;
     }
     __device__ __forceinline__ void total()
@@ -580,6 +621,7 @@ template <int W, int Q> struct Tile32 {
     uint64_t q[FOURS][2], early[EARLY ? FOURS : 1][2], o[Q / 2][COLS];   // o: pairs of queries, columns
     float base, ahead, sum;
     int sees;
+    bool apart;               // as above
 
     static __device__ __forceinline__ void load(const Queries<float> &u, int lane, uint64_t (&to)[FOURS][2])
     {
@@ -615,6 +657,7 @@ template <int W, int Q> struct Tile32 {
             load(u, lane, q);
         }
         sees = alike ? INT_MAX : u.sees(lane % Q);
+        apart = false;
         clear();
     }
     __device__ __forceinline__ void clear()
@@ -626,7 +669,7 @@ template <int W, int Q> struct Tile32 {
             for (int c = 0; c < COLS; ++c) o[h][c] = 0;
     }
     static __device__ __forceinline__ int weights_of(int row) { return row * Q + row / MINE * Q; }   // (rows that are written at once lie in different banks)
-    __device__ __forceinline__ void take(const char *tile, unsigned there, int first, float scale2, int lane, char *stored)
+    __device__ __forceinline__ void take(char *tile, unsigned there, int first, float scale2, int lane, char *stored)
     {
         float *weights = reinterpret_cast<float *>(stored);
         using F = Form<float, W>;
@@ -693,6 +736,7 @@ template <int W, int Q> struct Tile32 {
             weights[weights_of(part * MINE + r) + lane % Q] = s[r];
         }
         __syncwarp();
+        if (apart) set_apart(tile + ROWS * F::ROW, there, first, weights, lane);
         const char *v_from = tile + ROWS * F::ROW + lane * (COLS == 2 ? 8 : 16);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -721,7 +765,47 @@ template <int W, int Q> struct Tile32 {
             }
         }
     }
-    __device__ __forceinline__ bool again() { return false; }
+    // As above; weights: of the tile.  A lane looks at its own columns.
+    __device__ __forceinline__ void set_apart(char *values, unsigned there, int first, const float *weights, int lane)
+    {
+        using F = Form<float, W>;
+#pragma unroll 1
+        for (int row = 0; row < ROWS; ++row) {
+            if (!(there >> row & 1)) continue;
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) {
+                float *at = reinterpret_cast<float *>(values + row * F::ROW) + column(c, lane);
+                const float v = *at;
+                const bool odd = !(fabsf(v) <= 3.402823466e38f);
+                if (!__any_sync(~0u, odd)) continue;
+#pragma unroll
+                for (int h = 0; h < Q / 2; ++h) {
+                    const bool see0 = first < 0 || first + row < __shfl_sync(~0u, sees, 2 * h), see1 = first < 0 || first + row < __shfl_sync(~0u, sees, 2 * h + 1);
+                    float x, y;
+                    attn::split(o[h][c], x, y);
+                    if (odd && see0) x = fmaf(weights[weights_of(row) + 2 * h], v, x);
+                    if (odd && see1) y = fmaf(weights[weights_of(row) + 2 * h + 1], v, y);
+                    o[h][c] = attn::two(x, y);
+                }
+                if (odd) *at = 0.f;
+            }
+        }
+    }
+    // (a weight of 0 that is not one of a row unseen is the formula's own)
+    __device__ __forceinline__ bool again(bool uneven)
+    {
+        if (!uneven || apart) return false;
+        bool odd = false;
+#pragma unroll
+        for (int h = 0; h < Q / 2; ++h)
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) {
+                float x, y;
+                attn::split(o[h][c], x, y);
+                odd |= !(fabsf(x) <= 3.402823466e38f) || !(fabsf(y) <= 3.402823466e38f);
+            }
+        return apart = __any_sync(~0u, odd);
+    }
     __device__ __forceinline__ void total()
     {
 #pragma unroll
@@ -774,7 +858,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
     extern __shared__ __align__(128) char shared[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x * kAttnWarps + warp;
     const int units = a.kv_heads * a.blocks;   // of a token
-    const char *ring = shared + warp * F::RING;
+    char *ring = shared + warp * F::RING;
     const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
     char *stored = shared + kAttnWarps * F::RING + warp * F::STORED;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -862,7 +946,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
             if (more) { start(next); fed = true; x.look_ahead(queries_of(next), lane); }
         }
         if (++j < now.last) continue;
-        if (x.again()) {   // from its first tile on, without what is on its way of the next
+        if (x.again(now.p.least < now.p.most)) {   // from its first tile on, without what is on its way of the next
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();
             x.clear();
