@@ -376,8 +376,8 @@ template <int W, int NT> struct Tile16 {
             for (int s = 0; s < KS; ++s) o[s][m][0] = o[s][m][1] = o[s][m][2] = o[s][m][3] = 0.f;
         }
     }
-    // there: the tile's rows that are there; first: the position of its row 0, or -1 if all queries see all of them.
-    __device__ __forceinline__ void take(char *tile, unsigned there, int first, float scale2, int lane, char *stored)
+    // there: the tile's rows that are there; first: the position of its row 0, or -1 if all queries see all of them.  APART: see `apart`.
+    template <bool APART> __device__ __forceinline__ void take(char *tile, unsigned there, int first, float scale2, int lane, char *stored)
     {
         using F = Form<Bf16, W>;
         constexpr int H = F::ROWS / 16, SUMS = H == 1 ? 2 : 1;   // sixteens of rows; sums of a product (so that few products wait for one another)
@@ -468,7 +468,7 @@ template <int W, int NT> struct Tile16 {
                     x[h][m][e] = attn::ex2(x[h][m][e]);
                     sum[m][e & 1] += x[h][m][e];
                 }
-        if (apart) set_apart<H>(tile + F::ROWS * F::ROW, there, first, x, lane);
+        if (APART) set_apart<H>(tile + F::ROWS * F::ROW, there, first, x, lane);
         unsigned high[H][NT][2], low[H][NT][2];
 #pragma unroll
         for (int h = 0; h < H; ++h)
@@ -492,42 +492,34 @@ template <int W, int NT> struct Tile16 {
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
                     mma_bf16(o[s][m], v, high[h][m][0], high[h][m][1]);
-                    if (!apart) mma_bf16(o[s][m], v, low[h][m][0], low[h][m][1]);
+                    mma_bf16(o[s][m], v, low[h][m][0], low[h][m][1]);
                 }
             }
     }
     // A tile's values that are not finite: into the sums of the queries that see their rows, and zeros in their place.  p: the weights, as `take` has them.
-    template <int H> __device__ __forceinline__ void set_apart(char *values, unsigned there, int first, const float (&p)[H][NT][4], int lane)
+    template <int H> __device__ void set_apart(char *values, unsigned there, int first, const float (&p)[H][NT][4], int lane)
     {
         using F = Form<Bf16, W>;
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll 1
         for (int row = 0; row < F::ROWS; ++row) {
             if (!(there >> row & 1)) continue;   // (zeros)
-            float w[NT][2];
-#pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float x = row & 8 ? p[0][m][e + 2] : p[0][m][e];
-                    if (H == 2 && row >= 16) x = row & 8 ? p[H - 1][m][e + 2] : p[H - 1][m][e];
-                    w[m][e] = __shfl_sync(~0u, x, (row & 7) * 4 + t);
-                }
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    Bf16 *at = reinterpret_cast<Bf16 *>(values + row * F::ROW + ((2 * s + j) ^ (row & 7)) * 16) + g;
-                    const unsigned u = at->bits;
-                    const bool odd = (u & 0x7f80) == 0x7f80;
-                    if (!__any_sync(~0u, odd)) continue;
-#pragma unroll
-                    for (int m = 0; m < NT; ++m)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (odd && (first < 0 || first + row < sees[m][e])) o[s][m][2 * j + e] = fmaf(w[m][e], __uint_as_float(u << 16), o[s][m][2 * j + e]);
-                    if (odd && t == 0) at->bits = 0;   // (all four lanes that look at it have read it)
-                }
+#pragma unroll 1
+            for (int s = 0; s < 2 * KS; ++s) {
+                Bf16 *at = reinterpret_cast<Bf16 *>(values + row * F::ROW + (s ^ (row & 7)) * 16) + g;
+                const unsigned u = at->bits;
+                const bool odd = (u & 0x7f80) == 0x7f80;
+                if (!__any_sync(~0u, odd)) continue;
+#pragma unroll 1
+                for (int m = 0; m < NT; ++m)
+#pragma unroll 1
+                    for (int e = 0; e < 2; ++e) {
+                        const float w = __shfl_sync(~0u, p[row >> 4][m][(row >> 3 & 1) * 2 + e], (row & 7) * 4 + t);
+                        float &to = o[s >> 1][m][(s & 1) * 2 + e];
+                        if (odd && (first < 0 || first + row < sees[m][e])) to = fmaf(w, __uint_as_float(u << 16), to);
+                    }
+                if (odd && t == 0) at->bits = 0;   // (all four lanes that look at it have read it)
+            }
         }
         __syncwarp();
     }
@@ -669,7 +661,7 @@ template <int W, int Q> struct Tile32 {
             for (int c = 0; c < COLS; ++c) o[h][c] = 0;
     }
     static __device__ __forceinline__ int weights_of(int row) { return row * Q + row / MINE * Q; }   // (rows that are written at once lie in different banks)
-    __device__ __forceinline__ void take(char *tile, unsigned there, int first, float scale2, int lane, char *stored)
+    template <bool APART> __device__ __forceinline__ void take(char *tile, unsigned there, int first, float scale2, int lane, char *stored)
     {
         float *weights = reinterpret_cast<float *>(stored);
         using F = Form<float, W>;
@@ -736,7 +728,7 @@ template <int W, int Q> struct Tile32 {
             weights[weights_of(part * MINE + r) + lane % Q] = s[r];
         }
         __syncwarp();
-        if (apart) set_apart(tile + ROWS * F::ROW, there, first, weights, lane);
+        if (APART) set_apart(tile + ROWS * F::ROW, there, first, weights, lane);
         const char *v_from = tile + ROWS * F::ROW + lane * (COLS == 2 ? 8 : 16);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -766,19 +758,19 @@ template <int W, int Q> struct Tile32 {
         }
     }
     // As above; weights: of the tile.  A lane looks at its own columns.
-    __device__ __forceinline__ void set_apart(char *values, unsigned there, int first, const float *weights, int lane)
+    __device__ void set_apart(char *values, unsigned there, int first, const float *weights, int lane)
     {
         using F = Form<float, W>;
 #pragma unroll 1
         for (int row = 0; row < ROWS; ++row) {
             if (!(there >> row & 1)) continue;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < COLS; ++c) {
                 float *at = reinterpret_cast<float *>(values + row * F::ROW) + column(c, lane);
                 const float v = *at;
                 const bool odd = !(fabsf(v) <= 3.402823466e38f);
                 if (!__any_sync(~0u, odd)) continue;
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < Q / 2; ++h) {
                     const bool see0 = first < 0 || first + row < __shfl_sync(~0u, sees, 2 * h), see1 = first < 0 || first + row < __shfl_sync(~0u, sees, 2 * h + 1);
                     float x, y;
@@ -846,6 +838,12 @@ template <int W, int Q> struct Tile32 {
             }
     }
 };
+// A tile on the second pass over a unit.  (Out of line and on a copy, so that what hardly any unit needs is not among the instructions and registers of all: in line
+// fp32 with 64 heads over 4 took 242 instead of 223 us.)
+template <typename Tile> __device__ __noinline__ void take_apart(Tile &x, char *tile, unsigned there, int first, float scale2, int lane, char *stored)
+{
+    x.template take<true>(tile, there, first, scale2, lane, stored);
+}
 template <typename T, int W, int Q> struct TileOf { using type = Tile16<W, Q / 8>; };
 template <int W, int Q> struct TileOf<float, W, Q> { using type = Tile32<W, Q>; };
 
@@ -934,7 +932,17 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
         else if (ahead == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
-        if (there0) x.take(ring + stage * F::TILE, there0, now.p.n > 1 && (j + 1) * F::ROWS > now.p.least ? j * F::ROWS : -1, scale2, lane, stored);
+        if (there0) {
+            char *tile = ring + stage * F::TILE;
+            const int first = now.p.n > 1 && (j + 1) * F::ROWS > now.p.least ? j * F::ROWS : -1;
+            if (__builtin_expect(!x.apart, 1)) {
+                x.template take<false>(tile, there0, first, scale2, lane, stored);
+            } else {
+                Tile y = x;
+                take_apart(y, tile, there0, first, scale2, lane, stored);
+                x = y;
+            }
+        }
         there0 = there1;
         there1 = there2;
         --ahead;
