@@ -882,7 +882,8 @@ def paged_tables(lengths, added, tables, free_pages, free_count, page, pages, to
     """b2sp_paged_tables: (lengths after, row_ptr [requests + 1], rows, seen and slots [tokens], counts [4]) of a step in which request r of
     lengths[r] positions gets added[r] new ones, or ends (added[r] < 0).  tables [requests, width] gets the pages that are missing, from the stack of free
     ones: free_count (int32 of one element or more, the first counts) of them in free_pages, to which the pages of the requests that end are added.  pages
-    of `page` rows; tokens: room of the step.  counts[:1] is the next step's free_count; counts[2] > 0: not all fitted (see the header).
+    of `page` rows; tokens: room of the step.  counts[:1] is the next step's free_count; counts[2] > 0: not all fitted.  counts[0] < 0: pages were missing;
+    the step has to be made again, from the same lengths and free_count, and steps on top of it (free_count < 0) do nothing (see the header).
     out: the six tensors, which must not be the inputs."""
     t, R, device = _page_tables(tables), tables.shape[0], tables.device
     shape = (R,)

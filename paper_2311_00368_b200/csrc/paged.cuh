@@ -238,6 +238,8 @@ __device__ __forceinline__ Request request(const TablesArgs &a, int r)
 // Pages given back are pushed on the stack of free ones in order of requests, then new ones are popped in order of requests.  No CTA waits for
 // another: which page the k-th new one is follows from the prefix sums, and one that is given back in the same step is read from the table
 // of the request that ends, so everything is a function of the inputs, and any number of CTAs take any part of it.
+// A count below 0 is what a step leaves that found too few pages.  Its lengths count positions that no page holds, so a step on top of it would push entries
+// that are no pages and lose tokens without a word: it does nothing instead, and what the short step read is still there for it to be made again.
 // Bound by latency: lengths, then (tokens) a table entry or a free page.  64 requests with a token each 4.1 us, 512 with 16384 new tokens 7.2 us.
 __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs a)
 {
@@ -251,8 +253,18 @@ __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs
         const Request q = request(a, r);
         n_take += q.need; n_back += q.back; n_new += q.fresh;
     }
-    const int count = min(max(*a.free_count, 0), a.free_room);
+    const int given = *a.free_count, count = min(max(given, 0), a.free_room);
     block_before3(n_take, n_back, n_new, warps, all_take, all_back, all_new);
+    const long long me = blockIdx.x * (long long)kThreads + threadIdx.x, all = gridDim.x * (long long)kThreads;
+    if (given < 0) {
+        for (long long r = me; r < R; r += all) { a.lengths_out[r] = request(a, (int)r).length; a.row_ptr[r] = 0; }
+        for (long long t = me; t < a.tokens; t += all) { a.rows[t] = -1; a.seen[t] = 0; a.slots[t] = -1; }
+        if (me == 0) {
+            a.row_ptr[R] = 0;
+            a.counts[0] = given; a.counts[1] = 0; a.counts[2] = saturated(all_new); a.counts[3] = 0;
+        }
+        return;
+    }
     const long long top = min(count + all_back, (long long)a.free_room);   // free pages before any is taken
     long long fit = 0;                                                      // tokens that get a row
     for (int r = r0; r < r1; ++r) {
@@ -287,7 +299,6 @@ __global__ void __launch_bounds__(kThreads) paged_tables_kernel(const TablesArgs
         const int j = (int)(at - count), r = segment_of(back, R, j);
         return valid(a.t.entries[r * a.t.ld + (j - back[r])]);
     };
-    const long long me = blockIdx.x * (long long)kThreads + threadIdx.x, all = gridDim.x * (long long)kThreads;
     for (long long t = me; t < a.tokens; t += all) {
         int r = -1, seen = 0, slot = -1;
         if (t < ptr[R]) {
