@@ -397,7 +397,8 @@ b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long 
  *   term, in any order, and one that is no page seen is left out.  Q, O: token i, head h at i * ld + h * stride_head.
  *   Any M, but made for few tokens with long rows: a row is cut into parts and joined; neighbouring tokens of one request read its rows together.  d <= 256;
  *   strides below 2^32 bytes.  O may be Q itself, with its strides.
- * Other than that no call may write to what it reads (K and V of a write may be rows of the caches that it leaves as they are).  At most 2^30 tokens.
+ * Other than that no call may write to what it reads (K and V of a write may be rows of the caches that it leaves as they are), nor may its outputs share
+ *   memory: calls whose arguments show that they do are refused.  Rows of one tensor between those of another are fine.  At most 2^30 tokens.
  */
 typedef struct {
     void *data; long long ld, stride_head, stride_page;

@@ -3,6 +3,7 @@
 #include <atomic>
 #include <climits>
 
+#include "overlap.h"
 #include "paged_attention.cuh"
 
 namespace b2sp {
@@ -81,16 +82,27 @@ bool apart(int d, std::initializer_list<std::pair<long long, long long>> dims)  
 }
 template <typename T> Pages<T> pages(const b2sp_pages *c) { return Pages<T>{static_cast<T *>(c->data), c->ld, c->stride_head, c->stride_page, c->pages}; }
 bool same_slots(const b2sp_pages *a, const b2sp_pages *b) { return a->pages == b->pages && a->page == b->page; }
-bool meet(const void *a, size_t an, const void *b, size_t bn)
+long long bytes_of(long long stride, size_t wide) { return std::min(stride, 1ll << 58) * (long long)wide; }   // (no two rows lie further apart)
+template <typename T> Spread spread(const b2sp_pages *c, int heads, int d, int rows)   // rows: of a page, 1 for means
 {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return an && bn && x < y + bn && y < x + an;
+    return Spread(c->data, d * sizeof(T), {{c->pages, bytes_of(c->stride_page, sizeof(T))}, {heads, bytes_of(c->stride_head, sizeof(T))}, {rows, bytes_of(c->ld, sizeof(T))}});
 }
-// Whether an output lies in what tells of the tokens.
-bool of_tokens(const void *out, size_t n, int M, const b2sp_page_tables *t, const int *rows, const int *seen)
+template <typename T> Spread spread(const T *x, int tokens, long long ld, int heads, long long sh, int d)
 {
-    const size_t entries = t->requests ? ((t->requests - 1) * (size_t)t->ld + t->width) * 4 : 0;
-    return meet(out, n, seen, M * 4ull) || (rows && meet(out, n, rows, M * 4ull)) || meet(out, n, t->entries, entries);
+    return Spread(x, d * sizeof(T), {{tokens, bytes_of(ld, sizeof(T))}, {heads, bytes_of(sh, sizeof(T))}});
+}
+Spread spread(const b2sp_page_tables *t) { return Spread(t->entries, t->width * 4ll, {{t->requests, bytes_of(t->ld, 4)}}); }
+Spread ints(const int *x, long long n) { return Spread(x, std::min(n, 1ll << 58) * 4); }
+// Whether an output lies in one of the inputs or in another output: CTAs read the ones while others write.
+bool mixed(std::initializer_list<Spread> out, std::initializer_list<Spread> in)
+{
+    for (auto x = out.begin(); x != out.end(); ++x) {
+        for (const Spread &y : in)
+            if (share(*x, y)) return true;
+        for (auto y = x + 1; y != out.end(); ++y)
+            if (share(*x, *y)) return true;
+    }
+    return false;
 }
 
 template <typename T> bool fits(const void *x, long long ld, long long sh, size_t bytes)   // rows begin on multiples of `bytes`
@@ -109,12 +121,16 @@ b2sp_status write(int tokens, int heads, int d, const T *K, long long ldk, long 
     if (rc == B2SP_OK) rc = check_tables(t, kp->page);
     if (rc != B2SP_OK) return rc;
     if (t->requests > kMostRequests || d > 1024) return B2SP_ERR_UNSUPPORTED;
-    if (!same_slots(kp, vp) || (means && means->pages != kp->pages) || (kp->pages && kp->data == vp->data)) return B2SP_ERR_INVALID_ARG;
+    if (!same_slots(kp, vp) || (means && means->pages != kp->pages)) return B2SP_ERR_INVALID_ARG;
     for (const b2sp_pages *c : {kp, vp})
         if (!apart(d, {{c->pages, c->stride_page}, {heads, c->stride_head}, {c->page, c->ld}})) return B2SP_ERR_INVALID_ARG;
     if (means && !apart(d, {{means->pages, means->stride_page}, {heads, means->stride_head}})) return B2SP_ERR_INVALID_ARG;
     if (t->requests && (!row_ptr || !lengths)) return B2SP_ERR_INVALID_ARG;
     if (tokens && (!K || !V)) return B2SP_ERR_INVALID_ARG;
+    const int R = t->requests;
+    if (mixed({spread<T>(kp, heads, d, kp->page), spread<T>(vp, heads, d, kp->page), means ? spread<T>(means, heads, d, 1) : Spread(nullptr, 0)},
+              {ints(row_ptr, R + 1), ints(lengths, R), spread(t)}))
+        return B2SP_ERR_INVALID_ARG;
     if (tokens == 0 || t->requests == 0 || kp->pages == 0) return B2SP_OK;
     WriteArgs<T> a = {};
     a.t = tables(t);
@@ -148,8 +164,9 @@ b2sp_status select(int M, int heads, int kv_heads, int d, const T *Q, long long 
     const long long blocks = (long long)M * kv_heads * (((long long)t->width + 7) / 8), ctas = (long long)M * kv_heads;   // blocks: of eight pages at least
     if (ctas > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < select_bytes(M, kv_heads, t->width)) return B2SP_ERR_WORKSPACE;
-    if (of_tokens(lists, (size_t)ctas * keep * 4, M, t, rows, seen)) return B2SP_ERR_INVALID_ARG;
     if (M == 0) return B2SP_OK;
+    if (mixed({ints(lists, ctas * keep)}, {ints(seen, M), ints(rows, M), spread(t), spread(Q, M, ldq, heads, shq, d), spread<T>(means, kv_heads, d, 1)}))
+        return B2SP_ERR_INVALID_ARG;
     SelectArgs<T> a = {};
     a.t = tables(t);
     a.tok = Tokens{rows, seen};
@@ -249,6 +266,11 @@ b2sp_status attention(int M, int heads, int kv_heads, int d, const T *Q, long lo
     if ((long long)M * kv_heads * p.blocks > INT_MAX) return B2SP_ERR_UNSUPPORTED;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < attention_bytes(heads, kv_heads, d)) return B2SP_ERR_WORKSPACE;
     if (M == 0) return B2SP_OK;
+    const Spread q = spread(Q, M, ldq, heads, shq, d), o = spread(O, M, ldo, heads, sho, d);
+    if (mixed({o, Spread(lse, (long long)M * heads * 4)}, {ints(seen, M), ints(rows, M), spread(t), ints(lists, (long long)M * kv_heads * keep),
+                                                           spread<T>(kp, kv_heads, d, kp->page), spread<T>(vp, kv_heads, d, kp->page)}))
+        return B2SP_ERR_INVALID_ARG;
+    if (!(q == o) && mixed({o, Spread(lse, (long long)M * heads * 4)}, {q})) return B2SP_ERR_INVALID_ARG;
     AttnArgs<T> a = {};
     a.t = tables(t);
     a.tok = Tokens{rows, seen};
@@ -300,14 +322,9 @@ extern "C" b2sp_status b2sp_paged_tables(const b2sp_page_tables *t, int pages, i
     if (!row_ptr || !counts || !free_count || (R && (!lengths || !added || !lengths_out)) || (free_room && !free_pages)) return B2SP_ERR_INVALID_ARG;
     if (tokens && (!rows || !seen || !slots)) return B2SP_ERR_INVALID_ARG;
     if (R > kMostRequests || (long long)pages * page > INT_MAX) return B2SP_ERR_UNSUPPORTED;
-    // CTAs read inputs while others write outputs
-    const std::pair<const void *, size_t> in[] = {{lengths, R * 4ull}, {added, R * 4ull}, {free_count, 4}, {free_pages, free_room * 4ull},
-                                                  {t->entries, R ? ((R - 1) * (size_t)t->ld + t->width) * 4 : 0}},
-                                          out[] = {{lengths_out, R * 4ull}, {row_ptr, (R + 1) * 4ull}, {rows, tokens * 4ull}, {seen, tokens * 4ull},
-                                                   {slots, tokens * 4ull}, {counts, 16}};
-    for (const auto &x : in)
-        for (const auto &y : out)
-            if (meet(x.first, x.second, y.first, y.second)) return B2SP_ERR_INVALID_ARG;
+    if (mixed({ints(lengths_out, R), ints(row_ptr, R + 1), ints(rows, tokens), ints(seen, tokens), ints(slots, tokens), ints(counts, 4), ints(free_pages, free_room),
+               spread(t)}, {ints(lengths, R), ints(added, R), ints(free_count, 1)}))
+        return B2SP_ERR_INVALID_ARG;
     const size_t shared = 3 * (R + 1) * sizeof(int);
     TablesArgs a = {};
     a.t = tables(t);
@@ -324,8 +341,8 @@ extern "C" b2sp_status b2sp_paged_lists(int M, const b2sp_page_tables *t, int pa
     b2sp_status rc = check_tables(t, page);
     if (rc != B2SP_OK) return rc;
     if (M < 0 || pages < 0 || entries < 0 || !row_ptr || (M && !seen) || (entries && !col_idx)) return B2SP_ERR_INVALID_ARG;
-    if (of_tokens(row_ptr, (M + 1) * 4ull, M, t, rows, seen) || of_tokens(col_idx, entries * 4ull, M, t, rows, seen)) return B2SP_ERR_INVALID_ARG;
     if (entries > INT_MAX || (long long)pages * page > INT_MAX || M > kMostTokens) return B2SP_ERR_UNSUPPORTED;
+    if (mixed({ints(row_ptr, M + 1ll), ints(col_idx, entries)}, {ints(seen, M), ints(rows, M), spread(t)})) return B2SP_ERR_INVALID_ARG;
     ListsArgs a = {};
     a.t = tables(t);
     a.tok = Tokens{rows, seen};
