@@ -934,7 +934,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, Form<T, W, Q>::CTAS) paged_at
         __syncwarp();
         if (there0) {
             char *tile = ring + stage * F::TILE;
-            const int first = now.p.n > 1 && (j + 1) * F::ROWS > now.p.least ? j * F::ROWS : -1;
+            const int first = now.p.n > 1 && j * F::ROWS > now.p.least - F::ROWS ? j * F::ROWS : -1;   // (the end of a row's last tile may lie at 2^31)
             if (__builtin_expect(!x.apart, 1)) {
                 x.template take<false>(tile, there0, first, scale2, lane, stored);
             } else {
