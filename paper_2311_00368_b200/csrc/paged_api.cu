@@ -33,7 +33,7 @@ template <auto Kernel> bool allow_shared(size_t bytes)
 // A launch that may begin before the one ahead of it has ended (the kernels wait for that themselves).
 template <auto Kernel, typename... Args> bool launch_early(dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, const Args &...args)
 {
-    if (!allow_shared<Kernel>(shared)) return false;
+    if (!allow_shared<Kernel>(shared)) { cudaGetLastError(); return false; }   // (an error that stays is the next call's)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = blocks;
     cfg.blockDim = dim3(threads);
@@ -44,7 +44,9 @@ template <auto Kernel, typename... Args> bool launch_early(dim3 blocks, unsigned
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, Kernel, args...) == cudaSuccess;
+    if (cudaLaunchKernelEx(&cfg, Kernel, args...) == cudaSuccess) return true;
+    cudaGetLastError();
+    return false;
 }
 
 b2sp_status check_tables(const b2sp_page_tables *t, int page)
