@@ -4,7 +4,9 @@
 // Request r's position p lies in row p % page of page tables[r][p / page].  Everything that says how much there is to do (lengths, new tokens,
 // tables) is on the device, so a launch is sized by what the host knows (requests, tokens, width of the tables) and the kernels find their
 // work themselves: each CTA forms the prefix sums over the requests that it needs, which costs it a microsecond and spares a launch.  Every kernel may be
-// launched before the one ahead of it has ended: its CTAs wait for that first of all, all of them, so that what comes behind can count on it.
+// launched before the one ahead of it has ended: its CTAs wait for that first of all, all of them, so that what comes behind can count on it.  One does a
+// little before: paged_select_kernel behind paged_score_kernel, which lets it begin only when all of its own CTAs have waited, and neither writes what tells of
+// the tokens nor reads the lists.
 #pragma once
 #include <limits.h>
 
@@ -600,7 +602,7 @@ __global__ void __launch_bounds__(kScoreThreads, HALVES == 1 ? kScoreCTAs : kSco
     Share w;
     const auto load = [&](int base) { return base + lane < a.M ? blocks_of(base + lane) : 0; };
     if (!deal<kScoreThreads>(a.M, a.kv_heads, load, [](int blocks) { return blocks; }, gridDim.x * (kScoreThreads / 32), me, 1, w)) return;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (behind the wait: the choice reads lengths and writes lists before its own)
     struct At {   // a block
         int i, g, b, n, blocks;
     } at, front;   // the one that is added up, the one that is asked for
@@ -1114,7 +1116,7 @@ __device__ __forceinline__ void select_best(const SelectArgs<T> &a, int i, int g
 }
 
 // WARPS = 1: a CTA has four tokens and key heads (CTAs of one warp take longer to come and go than the choice).  MOST: most pages of a lane in registers;
-// early: the launch ahead is that of the scores, which has begun after all that made the tokens' numbers.
+// early: the launch ahead is that of the scores, whose CTAs have all waited for what made the tokens' numbers and read the lists before they let this one begin.
 template <typename T, int WARPS, int MOST>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : WARPS * 32) paged_select_kernel(const SelectArgs<T> a, bool early)
 {
