@@ -379,8 +379,8 @@ b2sp_status b2sp_attention_kv4(int M, int heads, int kv_heads, int d, long long 
  *   step gives the same.  A step that found too few pages (counts[0] < 0) has to be made again, with fewer tokens or more requests that end, before there is
  *   another: its lengths_out counts positions that no page holds.  A call with free_count < 0 does nothing and says so: lengths_out are the lengths, no token
  *   is new, counts are free_count, 0, the new tokens that it did not take, 0.  So steps may be queued before the host has seen the first one's counts.
- *   Entries within the lengths that are no page for another reason are the caller's: a token there gets slot -1 and does not count as one without a
- *   page, and a request that ends gives them back as they are.
+ *   Entries within the lengths and numbers on the stack that are no page for another reason are the caller's: a token there gets slot -1 and does not count
+ *   as one without a page, and a request that ends gives them back as they are.
  *   lengths_out and counts must not lie in lengths or free_count.  At most 8192 requests; pages * page < 2^31.
  * b2sp_paged_lists gives the slots that tokens see as lists for b2sp_attention_kv4 over caches whose rows are given out by pages: row_ptr[M + 1],
  *   col_idx[entries]; lists are cut where `entries` end, -1 stands for a missing page and behind the last list.

@@ -10,7 +10,7 @@
 // own in shared memory that asynchronous copies fill two tiles ahead, and waits for no other warp.  It knows its share from prefix sums over the tokens, so
 // lengths stay on the device and a long row is spread over the GPU as well as many short ones.  Units that end up in several shares leave their sums in
 // the workspace, and a second kernel joins them in order.
-// 64 tokens over 1 to 16384 positions, 32 heads over 8, width 128, bfloat16: 2.15 GB in 330 to 350 us, 94 to 99% of the copy bandwidth; one token over 32768:
+// 64 tokens over 1 to 16384 positions, 32 heads over 8, width 128, bfloat16: 2.28 GB in 358 us, 97% of the copy bandwidth; one token over 32768:
 // 30.5 us, of which 20.5 are its bytes and the rest is launch, prologue and joining.
 // Rows that are not there (behind what is seen, of missing pages) are filled with zeros by the copies instead of read: what memory holds there does not
 // enter.  Rows that some queries of a unit see and others do not have a weight of 0 for these, which is nothing unless a value is not finite; see Tile16.
