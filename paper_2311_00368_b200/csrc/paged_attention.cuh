@@ -523,8 +523,8 @@ template <int W, int NT> struct Tile16 {
         }
         __syncwarp();
     }
-    // True: to be taken again.  uneven: not all queries see the same.
-    __device__ __forceinline__ bool again(bool uneven)
+    // True: to be taken again.  (Tile32: only where not all queries see the same)
+    __device__ __forceinline__ bool again(bool)
     {
         bool odd = false;
 #pragma unroll
